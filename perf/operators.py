@@ -289,9 +289,6 @@ def prepare(case, seed):
                  mask=_padded(mask, c["pad"]), loss=torch.empty(1, device=DEV),
                  pair=torch.empty(P, device=DEV), rewards=torch.empty(2 * P, device=DEV),
                  d=torch.empty((2 * P, T), device=DEV), beta=2.0 if c["mean"] else 0.1)
-        if own:
-            import paper_2606_11660_gb300 as bg
-            s["ws"] = bg.workspace_tensor(bg.bergson_preference_loss_workspace(P, T), DEV)
         return s
     if op == "adamw":
         return _prepare_adamw(c, s, g, seed)
@@ -543,7 +540,7 @@ def _preference(s):
                 "squared": bg.BERGSON_PREFERENCE_SQUARED}[c["kind"]]
         bg.bergson_preference_loss(s["logp"], s["ref"], s["mask"], kind, s["beta"], c["margin"],
                                    c["smooth"], c["mean"], s["loss"], s["pair"], s["rewards"],
-                                   s["d"], s["ws"])
+                                   s["d"])
         return {k: s[k] for k in ("loss", "pair", "rewards", "d")}
     on, beta = s["mask"] != 0, s["beta"]
     gap = s["logp"] - s["ref"] if c["ref"] else s["logp"]
