@@ -79,6 +79,39 @@ typedef enum {
                                      on (-1, 1), v = top 24 bits of h_e */
 } bergson_proj_kind;
 
+/* Element types of the training-side operators' tensors. */
+typedef enum {
+  BERGSON_F32 = 0,
+  BERGSON_BF16 = 1,
+  BERGSON_F16 = 2
+} bergson_dtype;
+
+/* How bergson_policy_loss weighs the tokens of a batch (its token weight w). */
+typedef enum {
+  BERGSON_POLICY_TOKEN_MEAN = 0,  /* 1 / number of valid tokens in the batch */
+  BERGSON_POLICY_SEQ_MEAN = 1,    /* 1 / (B * number of valid tokens in the sequence) */
+  BERGSON_POLICY_SUM_NORM = 2     /* 1 / (B * norm_tokens): no sequence's length enters */
+} bergson_policy_reduction;
+
+typedef enum {
+  BERGSON_PREFERENCE_SIGMOID = 0, /* f(x) = log(1 + exp(-x)) */
+  BERGSON_PREFERENCE_HINGE = 1,   /* f(x) = max(0, 1 - x) */
+  BERGSON_PREFERENCE_SQUARED = 2  /* f(x) = ((x - 1/2) / beta)^2 */
+} bergson_preference_kind;
+
+/* How AdamW's m and v are held. */
+typedef enum {
+  BERGSON_STATE_F32 = 0,
+  BERGSON_STATE_8BIT = 1          /* u8 codes, one fp32 scale per 256 elements */
+} bergson_state_kind;
+
+typedef enum {
+  BERGSON_MOMENT_FIRST = 0,       /* m: sign, 4 bits of exponent, 3 of mantissa */
+  BERGSON_MOMENT_SECOND = 1       /* v: 5 bits of exponent, 3 of mantissa */
+} bergson_moment;
+
+#define BERGSON_STATE_BLOCK 256   /* elements that share a scale of an 8-bit state */
+
 /*
  * One nn.Linear module's captured tensors (Bergson App. B, "Gradients": gradient
  * collection from linear layers; Fig. 1: Adafactor normalisation and the
@@ -477,7 +510,8 @@ BERGSON_API int bergson_projection_matrix(uint64_t seed, int64_t d, int64_t k, i
 /*
  * Synchronises `stream`, then reports and clears the device status word:
  * BERGSON_OK, BERGSON_EDEVICE_TIMEOUT (a bounded device wait gave up),
- * BERGSON_EMOMENT (a factored second-moment entry was not > 0) or
+ * BERGSON_EMOMENT (a factored second-moment entry was not > 0), BERGSON_EINVAL
+ * (a token's target was past the vocabulary) or
  * BERGSON_ECUDA (the stream carried a CUDA error).  The word keeps the first
  * status recorded since it was last cleared.
  */
@@ -639,6 +673,252 @@ BERGSON_API int bergson_store_load(const char* path, int64_t file_row_offset, in
 BERGSON_API int bergson_project_grads_noalloc(const bergson_layer* layers, int n_layers,
                                               int64_t B, int64_t T, const uint8_t* mask,
                                               float* out, int64_t ld_out, void* stream);
+
+/*
+ * ---- Training-side operators ----
+ *
+ * What a program that fine-tunes a model and attributes the result calls next
+ * to the collection: the losses whose gradients are collected (App. B: losses
+ * of the gradient collection; Sec. 5.4's policy optimisation), token by token,
+ * the optimiser step, and the second moments r, c that a layer takes (Fig. 1:
+ * Adam and Adafactor normalisation).  Rows need no alignment beyond their
+ * element type's.
+ */
+
+/*
+ * Token log-probabilities under a softmax over V logits at temperature tau,
+ * z = logits[r] / tau:
+ *
+ *   lse[r] = log sum_v exp(z_v),   logp[r] = z_targets[r] - lse[r],
+ *   entropy[r] = -sum_v p_v log p_v,   p_v = exp(z_v - lse[r]).
+ *
+ *   logits    [rows, ld] of `dtype` (bergson_dtype), ld >= V >= 1.  An entry of
+ *             -inf takes no part (p_v = 0); a row of nothing else has lse = logp =
+ *             -inf and entropy 0.  NaN or +inf makes the row's outputs NaN.
+ *   targets   int64 [rows].  A negative target marks a row to be left out: its
+ *             logits are not read and its outputs are 0.  A target >= V makes
+ *             the row's logp NaN and is recorded as BERGSON_EINVAL in the device
+ *             status word.
+ *   tau       > 0, finite.
+ *   logp, lse fp32 [rows];  entropy fp32 [rows] or NULL.
+ * Sums are fp32, in an order fixed by the sizes.  rows in [0, 2^31), V < 2^31.
+ * Errors: EINVAL, EALIGN, ECUDA.
+ */
+BERGSON_API int bergson_token_logprobs(const void* logits, int dtype, int64_t rows, int64_t V,
+                                       int64_t ld, const int64_t* targets, double tau, float* logp,
+                                       float* lse, float* entropy, void* stream);
+
+/*
+ * The backward pass: with w = d_logp[r] and h = d_entropy[r] (0 where NULL; one
+ * of the two must be given),
+ *
+ *   d_logits[r, v] = ( w ([v == target] - p_v) - h p_v (log p_v + entropy[r]) ) / tau
+ *
+ * in the logits' type: as bf16 this is the G that bergson_layer takes of the
+ * model's last linear layer.
+ *   lse, entropy   what the forward pass wrote (entropy only with d_entropy).
+ *   d_logits  [rows, ld_d], ld_d >= V; may be `logits` itself with ld_d == ld.
+ * A row whose target is negative, whose w and h are both 0, or whose lse is below
+ * -1e30 (nothing but -inf or a type's lowest value, beside which lse cannot hold
+ * log V) gets zeros and its logits are not read.  A target >= V makes the row NaN and
+ * is recorded as BERGSON_EINVAL in the device status word.
+ * Errors: EINVAL, EALIGN, ECUDA.
+ */
+BERGSON_API int bergson_token_logprobs_backward(const void* logits, int dtype, int64_t rows,
+                                                int64_t V, int64_t ld, const int64_t* targets,
+                                                double tau, const float* lse,
+                                                const float* entropy, const float* d_logp,
+                                                const float* d_entropy, void* d_logits,
+                                                int64_t ld_d, void* stream);
+
+/*
+ * Clipped policy loss with a KL term and an entropy bonus (App. B's policy
+ * losses), forward and backward in one call.  For every valid token, with
+ * ratio = exp(logp - old_logp) and A its advantage,
+ *
+ *   l   = -min(ratio A, clamp(ratio, 1 - clip_low, 1 + clip_high) A)
+ *         + kl_coef k - entropy_coef entropy,
+ *   k   = exp(ref_logp - logp) - (ref_logp - logp) - 1,
+ *   loss = sum_t w_t l_t   with the token weight w of `reduction`,
+ *   d_logp = w ( -A ratio [ratio A <= clamped A] - kl_coef (exp(ref_logp - logp) - 1) ),
+ *   d_entropy = -w entropy_coef.
+ *
+ * A masked token contributes nothing and gets gradient 0, whatever the inputs
+ * hold there; a sequence, or a batch, without valid tokens has loss 0.
+ *
+ *   logp, old_logp   fp32 [B, ld] each.
+ *   ref_logp  fp32 [B, ld_ref], NULL only with kl_coef == 0 (the term is then left out).
+ *   entropy   fp32 [B, ld_entropy], NULL only with entropy_coef == 0.
+ *   advantages  fp32: [B], one a sequence, with ld_adv == 0; else [B, ld_adv].
+ *   mask      u8 [B, ld_mask] (nonzero = valid) or NULL (all valid).
+ *   clip_low in [0, 1], clip_high >= 0, norm_tokens > 0 (SUM_NORM only).
+ *   loss      fp32 [1];  seq_loss  fp32 [B] or NULL: the sequences' shares of it.
+ *   stats     fp32 [3] or NULL: mean of k, share of tokens whose ratio is clipped
+ *             (ratio A > clamped A), number of valid tokens.
+ *   d_logp    fp32 [B, ld_d];  d_entropy  fp32 [B, ld_de] or NULL.
+ *   workspace 256-byte aligned, contents on entry ignored.
+ * Leading dimensions are >= T.  B, T >= 0, B * T < 2^40.  Sums run in fp32 within 512
+ * tokens and fp64 above, in an order fixed by the sizes.
+ * Errors: EINVAL, EALIGN, EUNSUPPORTED, EWORKSPACE, ECUDA.
+ */
+typedef struct bergson_policy_args {
+  const float* logp;
+  const float* old_logp;
+  const float* ref_logp;
+  const float* entropy;
+  const float* advantages;
+  const uint8_t* mask;
+  int64_t ld_logp, ld_old, ld_ref, ld_entropy, ld_adv, ld_mask;
+  int64_t B, T;
+  double clip_low, clip_high, kl_coef, entropy_coef, norm_tokens;
+  float* loss;
+  float* seq_loss;
+  float* stats;
+  float* d_logp;
+  float* d_entropy;
+  int64_t ld_d, ld_de;
+  int32_t reduction;              /* bergson_policy_reduction */
+  int32_t reserved;               /* 0 */
+} bergson_policy_args;
+
+BERGSON_API int bergson_policy_loss_workspace(int64_t B, int64_t T, size_t* ws_bytes);
+BERGSON_API int bergson_policy_loss(const bergson_policy_args* args, void* workspace,
+                                    size_t ws_bytes, void* stream);
+
+/*
+ * Preference loss over P pairs of answers, forward and backward in one call.
+ * Row p of logp is the preferred answer of pair p and row P + p the other one;
+ * with the sums over an answer's n valid tokens
+ *
+ *   s = sum_t (logp_t - ref_logp_t)   (mean_logp != 0: divided by n),
+ *   x = beta (s_p - s_{P+p}) - margin,
+ *   pair_loss = (1 - label_smoothing) f(x) + label_smoothing f(-x),
+ *   loss = (1 / P) sum pair_loss,   rewards = beta s,
+ *   d_logp = d loss / d logp.
+ *
+ * f is given by `kind` (bergson_preference_kind).  A masked token contributes
+ * nothing and gets gradient 0, whatever the inputs hold there; an answer
+ * without valid tokens has s = 0.
+ *   logp      fp32 [2P, ld];  ref_logp  fp32 [2P, ld_ref] or NULL (taken as 0).
+ *   mask      u8 [2P, ld_mask] (nonzero = valid) or NULL (all valid).
+ *   beta > 0, label_smoothing in [0, 1].
+ *   loss fp32 [1], pair_loss fp32 [P], rewards fp32 [2P] or NULL, d_logp fp32 [2P, ld_d].
+ * Leading dimensions are >= T.  P, T >= 0, P < 2^30, 2 P T < 2^40; P = 0 gives loss 0.
+ * Sums over tokens and pairs run in an order fixed by the sizes.
+ * Errors: EINVAL, EALIGN, EUNSUPPORTED, ECUDA.
+ */
+typedef struct bergson_preference_args {
+  const float* logp;
+  const float* ref_logp;
+  const uint8_t* mask;
+  int64_t ld_logp, ld_ref, ld_mask;
+  int64_t P, T;
+  double beta, margin, label_smoothing;
+  float* loss;
+  float* pair_loss;
+  float* rewards;
+  float* d_logp;
+  int64_t ld_d;
+  int32_t kind;                   /* bergson_preference_kind */
+  int32_t mean_logp;
+} bergson_preference_args;
+
+BERGSON_API int bergson_preference_loss(const bergson_preference_args* args, void* stream);
+
+/*
+ * One tensor of an AdamW step.
+ *   param     n elements of param_dtype, updated in place.
+ *   grad      n elements of grad_dtype.
+ *   master    fp32 [n] or NULL.  With it the step is taken on `master` and param
+ *             receives its rounding; without, on param.
+ *   m, v      the moments, updated in place: fp32 [n] each (BERGSON_STATE_F32), or u8 [n] codes
+ *             with m_scale and v_scale, fp32 [ceil(n / 256)] (BERGSON_STATE_8BIT).  Zeros
+ *             (codes and scales) are the state before the first step.
+ *   lr_scale  multiplies the call's lr;  weight_decay  decoupled.
+ * All tensors are contiguous and share no memory.
+ */
+typedef struct bergson_adamw_tensor {
+  void* param;
+  const void* grad;
+  float* master;
+  void* m;
+  void* v;
+  float* m_scale;
+  float* v_scale;
+  int64_t n;
+  float lr_scale;
+  float weight_decay;
+  int32_t param_dtype, grad_dtype;   /* bergson_dtype */
+  int32_t state_kind;                /* bergson_state_kind */
+  int32_t reserved;                  /* 0 */
+} bergson_adamw_tensor;
+
+/*
+ * One AdamW step over many tensors (the optimiser whose second moments Fig. 1's
+ * Adam normalisation takes).  With g the gradient times *grad_scale,
+ *
+ *   m <- beta1 m + (1 - beta1) g,   v <- beta2 v + (1 - beta2) g^2,
+ *   param <- param - lr lr_scale ( (m / (1 - beta1^step)) /
+ *              (sqrt(v / (1 - beta2^step)) + eps) + weight_decay param ).
+ *
+ * 8-bit states hold code value * block scale, the scale such that the block's
+ * largest magnitude takes the largest code.  m and v are rounded to a code up
+ * or down by chance, so that on average no part of a small change is lost (a
+ * moment that moves by 1% a step would never leave its code otherwise); the
+ * 16 bits of chance of elements 4q .. 4q + 3 of tensor i are output q + 1 of the
+ * SplitMix64 sequence that starts at mix(i ^ mix(seed ^ mix(step))).  A v > 0 below
+ * the smallest code takes that code.  The parameters see m and v before rounding.
+ *
+ *   tensors   HOST array of n_tensors (>= 0) records.
+ *   step      >= 1: the number of this step.  beta1, beta2 in [0, 1), eps >= 0.
+ *   seed      of the 8-bit states' rounding.
+ *   grad_scale  device fp32 [1] or NULL (1), e.g. a clipping factor.
+ * All tensors live on one device.
+ * Errors: EINVAL, EALIGN, EUNSUPPORTED, ECUDA.
+ */
+BERGSON_API int bergson_adamw_step(const bergson_adamw_tensor* tensors, int n_tensors, double lr,
+                                   double beta1, double beta2, double eps, int64_t step,
+                                   uint64_t seed, const float* grad_scale, void* stream);
+
+/* The values of an 8-bit state: out[i] = value of codes[i] * scale[i / 256], i < n. */
+BERGSON_API int bergson_adamw_state_values(const uint8_t* codes, const float* scale, int64_t n,
+                                           int moment, float* out, void* stream);
+
+/*
+ * One matrix of bergson_factor_moments: AdamW's v of a weight [d_out, d_in],
+ * contiguous (fp32, or u8 codes with their scales), and the outputs r [d_out]
+ * and c [d_in], fp32.
+ */
+typedef struct bergson_moment_matrix {
+  const void* v;
+  const float* v_scale;
+  int64_t d_out;
+  int64_t d_in;
+  float* r;
+  float* c;
+  int32_t state_kind;             /* bergson_state_kind */
+  int32_t reserved;               /* 0 */
+} bergson_moment_matrix;
+
+/*
+ * Factored second moments of AdamW's v, as bergson_layer takes them (Fig. 1:
+ * Adafactor normalisation): with v' = correction * v + floor,
+ *
+ *   r_i = mean_j v'_ij,   c_j = mean_i v'_ij / mean_ij v'_ij,
+ *
+ * so that r_i c_j is the rank-one approximation of v' that has its row and
+ * column sums.  correction > 0 is the bias correction 1 / (1 - beta2^step);
+ * floor > 0 keeps r and c positive where no gradient has arrived.
+ *   mats      HOST array of n_mats (>= 0) records; d_out, d_in >= 1.
+ *   workspace 256-byte aligned, contents on entry ignored.
+ * Sums are fp32, in an order fixed by the sizes.
+ * Errors: EINVAL, EALIGN, EUNSUPPORTED, EWORKSPACE, ECUDA.
+ */
+BERGSON_API int bergson_factor_moments_workspace(const bergson_moment_matrix* mats, int n_mats,
+                                                 size_t* ws_bytes);
+BERGSON_API int bergson_factor_moments(const bergson_moment_matrix* mats, int n_mats,
+                                       double correction, double floor, void* workspace,
+                                       size_t ws_bytes, void* stream);
 
 #ifdef __cplusplus
 }

@@ -27,4 +27,13 @@ from .binding import (  # noqa: F401
     bergson_score_topk_workspace, bergson_score_grads, bergson_score_grads_workspace,
     bergson_sync_status, bergson_token_scores, bergson_token_scores_workspace, bergson_version, bergson_layer, lib,
     workspace_tensor,
+    BERGSON_BF16, BERGSON_F16, BERGSON_F32,
+    BERGSON_MOMENT_FIRST, BERGSON_MOMENT_SECOND, BERGSON_STATE_8BIT, BERGSON_STATE_BLOCK,
+    BERGSON_STATE_F32, BERGSON_POLICY_SEQ_MEAN, BERGSON_POLICY_SUM_NORM, BERGSON_POLICY_TOKEN_MEAN,
+    BERGSON_PREFERENCE_HINGE, BERGSON_PREFERENCE_SIGMOID, BERGSON_PREFERENCE_SQUARED,
+    AdamWTensor, MomentMatrix, bergson_adamw_state_values, bergson_adamw_step, bergson_adamw_tensor,
+    bergson_adamw_tensors, bergson_factor_moments, bergson_factor_moments_workspace,
+    bergson_moment_matrices, bergson_moment_matrix, bergson_policy_args, bergson_policy_loss,
+    bergson_policy_loss_workspace, bergson_preference_args, bergson_preference_loss,
+    bergson_token_logprobs, bergson_token_logprobs_backward,
 )

@@ -37,6 +37,25 @@ BERGSON_AGG_MEAN = 1
 BERGSON_FISHER_INV_SQRT = 0
 BERGSON_FISHER_INV = 1
 
+BERGSON_F32 = 0
+BERGSON_BF16 = 1
+BERGSON_F16 = 2
+
+BERGSON_POLICY_TOKEN_MEAN = 0
+BERGSON_POLICY_SEQ_MEAN = 1
+BERGSON_POLICY_SUM_NORM = 2
+
+BERGSON_PREFERENCE_SIGMOID = 0
+BERGSON_PREFERENCE_HINGE = 1
+BERGSON_PREFERENCE_SQUARED = 2
+
+BERGSON_STATE_F32 = 0
+BERGSON_STATE_8BIT = 1
+BERGSON_STATE_BLOCK = 256
+
+BERGSON_MOMENT_FIRST = 0
+BERGSON_MOMENT_SECOND = 1
+
 STATUS_NAMES = {
     0: "BERGSON_OK", -1: "BERGSON_EINVAL", -2: "BERGSON_EALIGN", -3: "BERGSON_EUNSUPPORTED",
     -4: "BERGSON_EWORKSPACE", -5: "BERGSON_ECUDA", -6: "BERGSON_EDEVICE_TIMEOUT",
@@ -60,6 +79,9 @@ EXPORTED = (
     "bergson_build_store_blocks", "bergson_score_topk_update_workspace",
     "bergson_score_topk_update", "bergson_score_bottomk_update",
     "bergson_score_topk_host_workspace", "bergson_score_topk_host",
+    "bergson_token_logprobs", "bergson_token_logprobs_backward", "bergson_policy_loss_workspace",
+    "bergson_policy_loss", "bergson_preference_loss", "bergson_adamw_step",
+    "bergson_adamw_state_values", "bergson_factor_moments_workspace", "bergson_factor_moments",
 )
 
 
@@ -81,6 +103,43 @@ class bergson_layer(ctypes.Structure):
     ]
 
 
+class bergson_policy_args(ctypes.Structure):
+    _fields_ = (
+        [(n, ctypes.c_void_p) for n in ("logp", "old_logp", "ref_logp", "entropy", "advantages",
+                                        "mask")]
+        + [(n, ctypes.c_int64) for n in ("ld_logp", "ld_old", "ld_ref", "ld_entropy", "ld_adv",
+                                         "ld_mask", "B", "T")]
+        + [(n, ctypes.c_double) for n in ("clip_low", "clip_high", "kl_coef", "entropy_coef",
+                                          "norm_tokens")]
+        + [(n, ctypes.c_void_p) for n in ("loss", "seq_loss", "stats", "d_logp", "d_entropy")]
+        + [("ld_d", ctypes.c_int64), ("ld_de", ctypes.c_int64), ("reduction", ctypes.c_int32),
+           ("reserved", ctypes.c_int32)])
+
+
+class bergson_preference_args(ctypes.Structure):
+    _fields_ = (
+        [(n, ctypes.c_void_p) for n in ("logp", "ref_logp", "mask")]
+        + [(n, ctypes.c_int64) for n in ("ld_logp", "ld_ref", "ld_mask", "P", "T")]
+        + [(n, ctypes.c_double) for n in ("beta", "margin", "label_smoothing")]
+        + [(n, ctypes.c_void_p) for n in ("loss", "pair_loss", "rewards", "d_logp")]
+        + [("ld_d", ctypes.c_int64), ("kind", ctypes.c_int32), ("mean_logp", ctypes.c_int32)])
+
+
+class bergson_adamw_tensor(ctypes.Structure):
+    _fields_ = (
+        [(n, ctypes.c_void_p) for n in ("param", "grad", "master", "m", "v", "m_scale", "v_scale")]
+        + [("n", ctypes.c_int64), ("lr_scale", ctypes.c_float), ("weight_decay", ctypes.c_float)]
+        + [(n, ctypes.c_int32) for n in ("param_dtype", "grad_dtype", "state_kind", "reserved")])
+
+
+class bergson_moment_matrix(ctypes.Structure):
+    _fields_ = [
+        ("v", ctypes.c_void_p), ("v_scale", ctypes.c_void_p), ("d_out", ctypes.c_int64),
+        ("d_in", ctypes.c_int64), ("r", ctypes.c_void_p), ("c", ctypes.c_void_p),
+        ("state_kind", ctypes.c_int32), ("reserved", ctypes.c_int32),
+    ]
+
+
 _LIB = None
 
 
@@ -93,6 +152,7 @@ def lib() -> ctypes.CDLL:
         raise RuntimeError(f"{LIB_PATH} is missing: build it with __graft_entry__.build()")
     L = ctypes.CDLL(LIB_PATH)
     i64, u64, vp, i32 = ctypes.c_int64, ctypes.c_uint64, ctypes.c_void_p, ctypes.c_int
+    f64 = ctypes.c_double
     szp = ctypes.POINTER(ctypes.c_size_t)
     i64p = ctypes.POINTER(ctypes.c_int64)
     lp = ctypes.POINTER(bergson_layer)
@@ -153,6 +213,20 @@ def lib() -> ctypes.CDLL:
                                        ctypes.c_size_t, vp]),
         "bergson_score_grads": (i32, [vp, i64, i64, i64, vp, i64, i64, i32, vp, i64, vp,
                                       ctypes.c_size_t, vp]),
+        "bergson_token_logprobs": (i32, [vp, i32, i64, i64, i64, vp, f64, vp, vp, vp, vp]),
+        "bergson_token_logprobs_backward": (i32, [vp, i32, i64, i64, i64, vp, f64, vp, vp, vp, vp,
+                                                  vp, i64, vp]),
+        "bergson_policy_loss_workspace": (i32, [i64, i64, szp]),
+        "bergson_policy_loss": (i32, [ctypes.POINTER(bergson_policy_args), vp, ctypes.c_size_t,
+                                      vp]),
+        "bergson_preference_loss": (i32, [ctypes.POINTER(bergson_preference_args), vp]),
+        "bergson_adamw_step": (i32, [ctypes.POINTER(bergson_adamw_tensor), i32, f64, f64, f64, f64,
+                                     i64, u64, vp, vp]),
+        "bergson_adamw_state_values": (i32, [vp, vp, i64, i32, vp, vp]),
+        "bergson_factor_moments_workspace": (i32, [ctypes.POINTER(bergson_moment_matrix), i32,
+                                                   szp]),
+        "bergson_factor_moments": (i32, [ctypes.POINTER(bergson_moment_matrix), i32, f64, f64, vp,
+                                         ctypes.c_size_t, vp]),
     }
     for name, (res, args) in sig.items():
         fn = getattr(L, name)
@@ -548,6 +622,234 @@ def bergson_debug_xgemm_plan(B: int, Q: int, K: int) -> dict:
     buf = (ctypes.c_int64 * 19)()
     _check(lib().bergson_debug_xgemm_plan(int(B), int(Q), int(K), buf, 19))
     return dict(zip(XGEMM_PLAN_FIELDS, buf))
+
+
+# ------------------------------------------------------------------ training side
+
+_DTYPES = {}
+
+
+def _dtype(t) -> int:
+    """The bergson_dtype of a torch tensor."""
+    if not _DTYPES:
+        import torch
+        _DTYPES.update({torch.float32: BERGSON_F32, torch.bfloat16: BERGSON_BF16,
+                        torch.float16: BERGSON_F16})
+    code = _DTYPES.get(t.dtype)
+    if code is None:
+        raise TypeError(f"expected float32, bfloat16 or float16, got {t.dtype}")
+    return code
+
+
+def _rows(t, what: str) -> tuple[int, int]:
+    """(device pointer, leading dimension) of a matrix with consecutive columns."""
+    ld, col = t.stride()
+    if col != 1 and t.shape[1] > 1:
+        raise ValueError(f"{what}: elements of a row must be consecutive")
+    return t.data_ptr(), ld if t.shape[0] > 1 else max(ld, t.shape[1])
+
+
+def _opt_rows(t, what: str) -> tuple[Optional[int], int]:
+    return (None, 0) if t is None else _rows(t, what)
+
+
+def _need(t, name: str, dtype: str, shape=None) -> None:
+    """Raises unless t has this torch dtype and, where given, this shape."""
+    if str(t.dtype) != dtype:
+        raise TypeError(f"{name} must be {dtype}, got {t.dtype}")
+    if shape is not None and tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{name} must have shape {tuple(shape)}, got {tuple(t.shape)}")
+
+
+def bergson_token_logprobs(logits, targets, tau: float, logp, lse, entropy=None,
+                           stream=None) -> None:
+    """logp[r] = logits[r, targets[r]] / tau - lse[r] (and entropies); targets < 0 leave a row out."""
+    rows, V = logits.shape
+    x, ld = _rows(logits, "logits")
+    _check(lib().bergson_token_logprobs(x, _dtype(logits), rows, V, ld, targets.data_ptr(), tau,
+                                        logp.data_ptr(), lse.data_ptr(), _ptr(entropy),
+                                        _stream(stream)))
+
+
+def bergson_token_logprobs_backward(logits, targets, tau: float, lse, entropy, d_logp, d_entropy,
+                                    d_logits, stream=None) -> None:
+    """d_logits from the gradients at logp and entropy (either may be None)."""
+    rows, V = logits.shape
+    x, ld = _rows(logits, "logits")
+    d, ld_d = _rows(d_logits, "d_logits")
+    if d_logits.dtype != logits.dtype or d_logits.shape != logits.shape:
+        raise ValueError("d_logits must have the logits' type and shape")
+    _check(lib().bergson_token_logprobs_backward(x, _dtype(logits), rows, V, ld,
+                                                 targets.data_ptr(), tau, lse.data_ptr(),
+                                                 _ptr(entropy), _ptr(d_logp), _ptr(d_entropy), d,
+                                                 ld_d, _stream(stream)))
+
+
+def bergson_policy_loss_workspace(B: int, T: int) -> int:
+    n = ctypes.c_size_t()
+    _check(lib().bergson_policy_loss_workspace(int(B), int(T), ctypes.byref(n)))
+    return n.value
+
+
+def bergson_policy_loss(logp, old_logp, ref_logp, entropy, advantages, mask, clip_low: float,
+                        clip_high: float, kl_coef: float, entropy_coef: float, reduction: int,
+                        norm_tokens: float, loss, seq_loss, stats, d_logp, d_entropy, workspace,
+                        stream=None) -> None:
+    """Clipped policy loss with a KL term and an entropy bonus: the loss, the
+    sequences' shares, statistics and the gradients at logp and entropy.
+    advantages: [B] (one a sequence) or [B, T]; ref_logp, entropy, mask,
+    seq_loss, stats and d_entropy may be None."""
+    B, T = logp.shape
+    x, ld = _rows(logp, "logp")
+    old, ld_old = _rows(old_logp, "old_logp")
+    ref, ld_ref = _opt_rows(ref_logp, "ref_logp")
+    ent, ld_ent = _opt_rows(entropy, "entropy")
+    adv, ld_adv = (advantages.data_ptr(), 0) if advantages.dim() == 1 else _rows(advantages,
+                                                                                 "advantages")
+    on, ld_mask = _opt_rows(mask, "mask")
+    d, ld_d = _rows(d_logp, "d_logp")
+    de, ld_de = _opt_rows(d_entropy, "d_entropy")
+    args = bergson_policy_args(x, old, ref, ent, adv, on, ld, ld_old, ld_ref, ld_ent, ld_adv,
+                               ld_mask, B, T, clip_low, clip_high, kl_coef, entropy_coef,
+                               norm_tokens, loss.data_ptr(), _ptr(seq_loss), _ptr(stats), d, de,
+                               ld_d, ld_de, reduction, 0)
+    _check(lib().bergson_policy_loss(args, workspace.data_ptr(),
+                                     workspace.numel() * workspace.element_size(),
+                                     _stream(stream)))
+
+
+def bergson_preference_loss(logp, ref_logp, mask, kind: int, beta: float, margin: float,
+                            label_smoothing: float, mean_logp: bool, loss, pair_loss, rewards,
+                            d_logp, stream=None) -> None:
+    """Preference loss over pairs (rows p and P + p of logp [2P, T]): the loss,
+    the pairs' losses, rewards and the gradient at logp.  ref_logp, mask and
+    rewards may be None."""
+    rows, T = logp.shape
+    if rows % 2:
+        raise ValueError("logp must have an even number of rows")
+    x, ld = _rows(logp, "logp")
+    ref, ld_ref = _opt_rows(ref_logp, "ref_logp")
+    on, ld_mask = _opt_rows(mask, "mask")
+    d, ld_d = _rows(d_logp, "d_logp")
+    args = bergson_preference_args(x, ref, on, ld, ld_ref, ld_mask, rows // 2, T, beta, margin,
+                                   label_smoothing, loss.data_ptr(), pair_loss.data_ptr(),
+                                   _ptr(rewards), d, ld_d, kind, 1 if mean_logp else 0)
+    _check(lib().bergson_preference_loss(args, _stream(stream)))
+
+
+@dataclasses.dataclass
+class AdamWTensor:
+    """One tensor of an AdamW step (see bergson_adamw_tensor); 8-bit states come
+    with their scales.  Contiguous tensors, which share no memory."""
+    param: object
+    grad: object
+    m: object
+    v: object
+    master: object = None
+    m_scale: object = None
+    v_scale: object = None
+    lr_scale: float = 1.0
+    weight_decay: float = 0.0
+
+    def to_c(self) -> bergson_adamw_tensor:
+        n = self.param.numel()
+        eight = self.m_scale is not None
+        if eight != (self.v_scale is not None):
+            raise ValueError("m_scale and v_scale must both be given or both be None")
+        blocks = (-(-n // BERGSON_STATE_BLOCK),)
+        state = "torch.uint8" if eight else "torch.float32"
+        for name, t, dtype, size in (
+                ("param", self.param, None, n), ("grad", self.grad, None, n),
+                ("master", self.master, "torch.float32", n), ("m", self.m, state, n),
+                ("v", self.v, state, n), ("m_scale", self.m_scale, "torch.float32", blocks[0]),
+                ("v_scale", self.v_scale, "torch.float32", blocks[0])):
+            if t is None:
+                continue
+            if dtype is not None:
+                _need(t, name, dtype)
+            if t.numel() != size or not t.is_contiguous():
+                raise ValueError(f"{name} must be contiguous and hold {size} elements")
+        return bergson_adamw_tensor(
+            _ptr(self.param), _ptr(self.grad), _ptr(self.master), _ptr(self.m), _ptr(self.v),
+            _ptr(self.m_scale), _ptr(self.v_scale), n, float(self.lr_scale),
+            float(self.weight_decay), _dtype(self.param), _dtype(self.grad),
+            BERGSON_STATE_8BIT if eight else BERGSON_STATE_F32, 0)
+
+
+def _records(kind, items) -> "ctypes.Array":
+    """The C array of a list of records; one that is an array already is returned."""
+    if isinstance(items, ctypes.Array):
+        return items
+    arr = (kind * len(items))()
+    for i, item in enumerate(items):
+        arr[i] = item if isinstance(item, kind) else item.to_c()
+    return arr
+
+
+def bergson_adamw_tensors(tensors: Sequence) -> "ctypes.Array":
+    """The record array of bergson_adamw_step, to be kept from step to step.  It
+    holds addresses: keep the tensors alive and in place."""
+    return _records(bergson_adamw_tensor, tensors)
+
+
+def bergson_adamw_step(tensors, lr: float, beta1: float, beta2: float, eps: float, step: int,
+                       seed: int = 0, grad_scale=None, stream=None) -> None:
+    """One AdamW step over tensors (AdamWTensor list, or bergson_adamw_tensors' array)."""
+    arr = _records(bergson_adamw_tensor, tensors)
+    _check(lib().bergson_adamw_step(arr, len(arr), lr, beta1, beta2, eps, step, seed,
+                                    _ptr(grad_scale), _stream(stream)))
+
+
+def bergson_adamw_state_values(codes, scale, moment: int, out, stream=None) -> None:
+    """out = the fp32 values of an 8-bit state (moment: BERGSON_MOMENT_FIRST or _SECOND)."""
+    n = codes.numel()
+    if out.numel() != n or scale.numel() < -(-n // BERGSON_STATE_BLOCK):
+        raise ValueError("out must hold a value per code and scale one per block of codes")
+    _check(lib().bergson_adamw_state_values(codes.data_ptr(), scale.data_ptr(), n, moment,
+                                            out.data_ptr(), _stream(stream)))
+
+
+@dataclasses.dataclass
+class MomentMatrix:
+    """AdamW's v [d_out, d_in] (fp32, or u8 codes with their scales) and its factors."""
+    v: object
+    r: object
+    c: object
+    v_scale: object = None
+
+    def to_c(self) -> bergson_moment_matrix:
+        d_out, d_in = self.v.shape
+        _need(self.v, "v", "torch.float32" if self.v_scale is None else "torch.uint8")
+        _need(self.r, "r", "torch.float32", (d_out,))
+        _need(self.c, "c", "torch.float32", (d_in,))
+        if self.v_scale is not None:
+            _need(self.v_scale, "v_scale", "torch.float32",
+                  (-(-d_out * d_in // BERGSON_STATE_BLOCK),))
+        if not (self.v.is_contiguous() and self.r.is_contiguous() and self.c.is_contiguous()):
+            raise ValueError("v, r and c must be contiguous")
+        return bergson_moment_matrix(
+            _ptr(self.v), _ptr(self.v_scale), d_out, d_in, _ptr(self.r), _ptr(self.c),
+            BERGSON_STATE_F32 if self.v_scale is None else BERGSON_STATE_8BIT, 0)
+
+
+def bergson_moment_matrices(mats: Sequence) -> "ctypes.Array":
+    """The record array of bergson_factor_moments, to be kept (it holds addresses)."""
+    return _records(bergson_moment_matrix, mats)
+
+
+def bergson_factor_moments_workspace(mats) -> int:
+    arr = _records(bergson_moment_matrix, mats)
+    n = ctypes.c_size_t()
+    _check(lib().bergson_factor_moments_workspace(arr, len(arr), ctypes.byref(n)))
+    return n.value
+
+
+def bergson_factor_moments(mats, correction: float, floor: float, workspace, stream=None) -> None:
+    """r and c of every matrix (MomentMatrix list, or bergson_moment_matrices' array)."""
+    arr = _records(bergson_moment_matrix, mats)
+    _check(lib().bergson_factor_moments(arr, len(arr), correction, floor, workspace.data_ptr(),
+                                        workspace.numel() * workspace.element_size(),
+                                        _stream(stream)))
 
 
 # ------------------------------------------------------------------ helpers

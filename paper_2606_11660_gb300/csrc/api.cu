@@ -112,29 +112,6 @@ PFN_cuTensorMapEncodeTiled_v12000 encode_fn() {
   return fn;
 }
 
-// Makes the device owning `ptr` current for the lifetime of the guard.
-struct DeviceGuard {
-  int prev = -1;
-  int dev = -1;
-  cudaError_t err = cudaSuccess;
-  explicit DeviceGuard(const void* ptr) {
-    cudaPointerAttributes at;
-    err = cudaPointerGetAttributes(&at, ptr);
-    if (err != cudaSuccess) return;
-    if (at.type != cudaMemoryTypeDevice && at.type != cudaMemoryTypeManaged) {
-      err = cudaErrorInvalidDevicePointer;
-      return;
-    }
-    err = cudaGetDevice(&prev);
-    if (err != cudaSuccess) return;
-    dev = at.device;
-    if (dev != prev) err = cudaSetDevice(dev);
-  }
-  ~DeviceGuard() {
-    if (prev >= 0 && dev >= 0 && prev != dev) cudaSetDevice(prev);
-  }
-};
-
 int* status_word(int dev) {
   static std::mutex mu;
   static int* ptrs[kMaxDevices] = {};
@@ -817,6 +794,10 @@ int record_error(int code, const char* fmt, ...) {
   g_last_error = buf;
   return code;
 }
+
+int injected_status() { return injected(); }
+int* device_status_word(int dev) { return status_word(dev); }
+int device_sm_count(int dev) { return sm_count(dev); }
 
 CUresult encode_tmap_2d(CUtensorMap* tm, CUtensorMapDataType dt, const void* ptr, int64_t inner,
                         int64_t outer, int64_t row_bytes, int box_inner, int box_outer) {
@@ -1813,6 +1794,9 @@ int bergson_sync_status(void* stream) {
     if (v == BERGSON_EMOMENT)
       return fail(v, "a factored second-moment entry (r or c) was not > 0; the projected "
                      "values computed from it are inf or NaN (device status %d)", v);
+    if (v == BERGSON_EINVAL)
+      return fail(v, "a token's target was past the vocabulary; its outputs are NaN (device "
+                     "status %d)", v);
     return fail(v, "a bounded device wait gave up (device status %d)", v);
   }
   return BERGSON_OK;

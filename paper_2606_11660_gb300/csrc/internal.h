@@ -187,6 +187,34 @@ struct ScoreParams {
 
 // Sets this thread's bergson_last_error() message (printf format) and returns `code`.
 int record_error(int code, const char* fmt, ...);
+// The status a pending bergson_debug_inject_status() asks this call to return.
+int injected_status();
+// The device status word of `dev` (current), or nullptr; its SM count, or 0.
+int* device_status_word(int dev);
+int device_sm_count(int dev);
+
+// Makes the device owning `ptr` current for the lifetime of the guard.
+struct DeviceGuard {
+  int prev = -1;
+  int dev = -1;
+  cudaError_t err = cudaSuccess;
+  explicit DeviceGuard(const void* ptr) {
+    cudaPointerAttributes at;
+    err = cudaPointerGetAttributes(&at, ptr);
+    if (err != cudaSuccess) return;
+    if (at.type != cudaMemoryTypeDevice && at.type != cudaMemoryTypeManaged) {
+      err = cudaErrorInvalidDevicePointer;
+      return;
+    }
+    err = cudaGetDevice(&prev);
+    if (err != cudaSuccess) return;
+    dev = at.device;
+    if (dev != prev) err = cudaSetDevice(dev);
+  }
+  ~DeviceGuard() {
+    if (prev >= 0 && dev >= 0 && prev != dev) cudaSetDevice(prev);
+  }
+};
 
 // The least workspace bergson_project_grads takes for these arguments (its query
 // reports more).  Returns the validation status.
