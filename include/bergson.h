@@ -758,7 +758,7 @@ BERGSON_API int bergson_token_logprobs_backward(const void* logits, int dtype, i
  *   d_logp    fp32 [B, ld_d];  d_entropy  fp32 [B, ld_de] or NULL.
  *   workspace 256-byte aligned, contents on entry ignored.
  * Leading dimensions are >= T.  B, T >= 0, B * T < 2^40.  Sums run in fp32 within 512
- * tokens and fp64 above, in an order fixed by the sizes.
+ * tokens and in twice its bits above, in an order fixed by the sizes.
  * Errors: EINVAL, EALIGN, EUNSUPPORTED, EWORKSPACE, ECUDA.
  */
 typedef struct bergson_policy_args {

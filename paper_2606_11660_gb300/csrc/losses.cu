@@ -1,5 +1,13 @@
-// The clipped policy loss and the preference loss, forward and backward: one
-// pass over the tokens, whose gradients follow from their own values and a weight.
+// The clipped policy loss and the preference loss, forward and backward.
+//
+// Both read every token once and write its gradient: 4 bytes a tensor and one of
+// mask, some 30 operations, so they are bound by memory, and below some 10^5 tokens by
+// their launches.  A token's gradient needs a weight that depends on others: the
+// policy loss counts the valid tokens beforehand (a byte a token), the preference
+// loss holds a pair in a CTA (or a cluster that shares its sums) and comes back to
+// write.  Sums over tokens follow an order fixed by the sizes.
+
+#include <algorithm>
 
 #include "internal.h"
 #include "train.cuh"
@@ -10,121 +18,383 @@ namespace {
 
 constexpr int kThreads = 256;
 constexpr int kWarps = kThreads / 32;
-constexpr int kSegment = 512;                  // tokens of a row a warp takes at once
+
+// ------------------------------------------------ four tokens of a row a lane
+//
+// A warp takes 128 tokens of a row at a time, four a lane: neighbours in one load
+// where the rows allow it (kVec), else 32 apart in loads of one.
+
+template <bool kVec>
+__device__ __forceinline__ int64_t token_of(int64_t t0, int lane, int j) {
+  return kVec ? t0 + 4 * lane + j : t0 + lane + 32 * j;
+}
+
+// Which of a lane's tokens are valid: bit j.
+template <bool kVec>
+__device__ __forceinline__ uint32_t valid_tokens(const uint8_t* mask, int64_t t0, int64_t T,
+                                                 int lane) {
+  uint32_t on = 0;
+  if (kVec && token_of<kVec>(t0, lane, 3) < T) {
+    if (mask == nullptr) return 15u;
+    const uchar4 m = *reinterpret_cast<const uchar4*>(mask + t0 + 4 * lane);
+    return (m.x != 0 ? 1u : 0u) | (m.y != 0 ? 2u : 0u) | (m.z != 0 ? 4u : 0u) |
+           (m.w != 0 ? 8u : 0u);
+  }
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    const int64_t t = token_of<kVec>(t0, lane, j);
+    if (t < T && (mask == nullptr || mask[t] != 0)) on |= 1u << j;
+  }
+  return on;
+}
+
+// The values of the tokens in `on` (0 for the others).
+template <bool kVec>
+__device__ __forceinline__ void load_tokens(const float* row, int64_t t0, int64_t T, int lane,
+                                            uint32_t on, float (&x)[4]) {
+  if (kVec && token_of<kVec>(t0, lane, 3) < T) {
+    float4 f = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+    if (on != 0) f = __ldcs(reinterpret_cast<const float4*>(row + t0 + 4 * lane));
+    x[0] = f.x; x[1] = f.y; x[2] = f.z; x[3] = f.w;
+    return;
+  }
+#pragma unroll
+  for (int j = 0; j < 4; ++j)
+    x[j] = (on >> j & 1u) != 0 ? __ldcs(row + token_of<kVec>(t0, lane, j)) : 0.0f;
+}
+
+template <bool kVec>
+__device__ __forceinline__ void store_tokens(float* row, int64_t t0, int64_t T, int lane,
+                                             const float (&x)[4]) {
+  if (kVec && token_of<kVec>(t0, lane, 3) < T) {
+    __stcs(reinterpret_cast<float4*>(row + t0 + 4 * lane), make_float4(x[0], x[1], x[2], x[3]));
+    return;
+  }
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    const int64_t t = token_of<kVec>(t0, lane, j);
+    if (t < T) __stcs(row + t, x[j]);
+  }
+}
+
+// Nonzero bytes among n from p, counted by a warp (the sum is in every lane).
+__device__ __forceinline__ unsigned count_bytes(const uint8_t* p, int64_t n) {
+  const int lane = threadIdx.x & 31;
+  int64_t head = (16 - (reinterpret_cast<uintptr_t>(p) & 15)) & 15;
+  head = head < n ? head : n;
+  const int64_t vecs = (n - head) / 16;
+  const uint4* body = reinterpret_cast<const uint4*>(p + head);
+  unsigned c = 0;
+#pragma unroll 4
+  for (int64_t i = lane; i < vecs; i += 32) {
+    const uint4 v = body[i];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      const uint32_t w = word(v, k);
+      c += __popc((w | ((w & 0x7f7f7f7fu) + 0x7f7f7f7fu)) & 0x80808080u);
+    }
+  }
+  const int64_t tail = head + 16 * vecs + lane;
+  if (lane < head) c += p[lane] != 0;
+  if (tail < n) c += p[tail] != 0;
+  return __reduce_add_sync(0xffffffffu, c);
+}
 
 // ---------------------------------------------------------------- policy
 
+constexpr int kSegment = 512;                  // tokens of a row a warp takes
+constexpr int kCountSegment = 4096;            // mask bytes a warp counts at once
+constexpr int kCountCtas = 304;
+constexpr int kPolicyCtas = 152 * 4;
+constexpr int kFinishCtas = 152;
+constexpr int kSmallItems = 512;               // (row, segment) items of the one-launch form
+constexpr int64_t kSmallTokens = 1 << 15;      // ... and its tokens: each CTA counts them all
+
+struct Totals {
+  Sum2 loss, kl;
+  unsigned long long clipped = 0, valid = 0;
+  __device__ __forceinline__ void add(const Totals& o) {
+    loss.add(o.loss);
+    kl.add(o.kl);
+    clipped += o.clipped;
+    valid += o.valid;
+  }
+};
+__device__ __forceinline__ Totals totals_sum(const Totals& t) {
+  Totals r;
+  r.loss = warp_sum(t.loss);
+  r.kl = warp_sum(t.kl);
+  r.clipped = warp_sum(t.clipped);
+  r.valid = warp_sum(t.valid);
+  return r;
+}
+
 struct PolicyParams {
   bergson_policy_args a;
-  int64_t segments;            // per row
-  unsigned* counts;            // valid tokens: per row
+  int64_t segments, count_segments;            // per row
+  unsigned* counts;            // valid tokens: per CTA (TOKEN_MEAN) or [B, count_segments]
+  int n_counts;                // CTAs that counted (TOKEN_MEAN)
   float4* sums;                // [B, segments] of l, k, clipped, valid tokens
+  Totals* totals;             // [kFinishCtas] of the same, l weighed
+  unsigned* ticket;
   float low, high, kl, ent;
+  float norm;                  // 1 / (B norm_tokens) (SUM_NORM)
+  int vec;
 };
 
 __global__ void __launch_bounds__(kThreads) policy_count_kernel(const PolicyParams p) {
-  const int64_t b = static_cast<int64_t>(blockIdx.x) * kWarps + (threadIdx.x >> 5);
-  if (b >= p.a.B) return;
-  const uint8_t* row = p.a.mask + b * p.a.ld_mask;
-  unsigned n = 0;
-  for (int64_t t = threadIdx.x & 31; t < p.a.T; t += 32) n += row[t] != 0;
-  n = __reduce_add_sync(0xffffffffu, n);
-  if ((threadIdx.x & 31) == 0) p.counts[b] = n;
-}
-
-__device__ __forceinline__ double policy_weight(const PolicyParams& p, int64_t b, double total) {
-  switch (p.a.reduction) {
-    case BERGSON_POLICY_TOKEN_MEAN: return 1.0 / fmax(total, 1.0);
-    case BERGSON_POLICY_SEQ_MEAN: {
-      const double n = p.a.mask != nullptr ? p.counts[b] : p.a.T;
-      return 1.0 / (p.a.B * fmax(n, 1.0));
+  __shared__ unsigned red[kWarps];
+  griddep_launch_dependents();
+  const int64_t items = p.a.B * p.count_segments;
+  const int64_t warps = static_cast<int64_t>(gridDim.x) * kWarps;
+  unsigned mine = 0;
+  for (int64_t i = static_cast<int64_t>(blockIdx.x) * kWarps + (threadIdx.x >> 5); i < items;
+       i += warps) {
+    const int64_t b = i / p.count_segments, t = (i % p.count_segments) * kCountSegment;
+    const int64_t n = min(p.a.T - t, static_cast<int64_t>(kCountSegment));
+    const unsigned c = count_bytes(p.a.mask + b * p.a.ld_mask + t, n);
+    if (p.a.reduction == BERGSON_POLICY_SEQ_MEAN) {
+      if ((threadIdx.x & 31) == 0) p.counts[i] = c;
     }
-    default: return 1.0 / (p.a.B * p.a.norm_tokens);
+    mine += c;
   }
-}
-
-// Valid tokens of the batch, in every thread.
-__device__ __forceinline__ double policy_total(const PolicyParams& p, double* red) {
-  if (p.a.mask == nullptr) return static_cast<double>(p.a.B) * p.a.T;
-  double n = 0.0;
-  for (int64_t b = threadIdx.x; b < p.a.B; b += blockDim.x) n += p.counts[b];
-  return block_sum(n, red);
-}
-
-__global__ void __launch_bounds__(kThreads) policy_kernel(const PolicyParams p) {
-  __shared__ double red[kWarps];
-  const double total =
-      p.a.reduction == BERGSON_POLICY_TOKEN_MEAN ? policy_total(p, red) : 0.0;
-  const int64_t item = static_cast<int64_t>(blockIdx.x) * kWarps + (threadIdx.x >> 5);
-  if (item >= p.a.B * p.segments) return;
-  const int64_t b = item / p.segments, seg = item % p.segments;
-  const float w = static_cast<float>(policy_weight(p, b, total));
-  const int64_t end = min(p.a.T, (seg + 1) * kSegment);
-  float loss = 0.0f, kls = 0.0f, clipped = 0.0f, valid = 0.0f;
-  for (int64_t t = seg * kSegment + (threadIdx.x & 31); t < end; t += 32) {
-    const bool on = p.a.mask == nullptr || p.a.mask[b * p.a.ld_mask + t] != 0;
-    float grad = 0.0f, l = 0.0f;
-    if (on) {
-      const float lp = p.a.logp[b * p.a.ld_logp + t];
-      const float adv = p.a.advantages[p.a.ld_adv == 0 ? b : b * p.a.ld_adv + t];
-      const float ratio = expf(lp - p.a.old_logp[b * p.a.ld_old + t]);
-      const float free = ratio * adv;
-      const float held = fminf(fmaxf(ratio, p.low), p.high) * adv;
-      const bool clip = free > held;
-      l = clip ? -held : -free;
-      grad = clip ? 0.0f : -free;
-      if (p.a.ref_logp != nullptr) {
-        const float gap = p.a.ref_logp[b * p.a.ld_ref + t] - lp;
-        const float up = expm1f(gap);
-        const float k = up - gap;
-        l += p.kl * k;
-        grad -= p.kl * up;
-        kls += k;
-      }
-      if (p.a.entropy != nullptr) l -= p.ent * p.a.entropy[b * p.a.ld_entropy + t];
-      loss += l;
-      clipped += clip ? 1.0f : 0.0f;
-      valid += 1.0f;
-    }
-    p.a.d_logp[b * p.a.ld_d + t] = on ? w * grad : 0.0f;
-    if (p.a.d_entropy != nullptr) p.a.d_entropy[b * p.a.ld_de + t] = on ? -w * p.ent : 0.0f;
-  }
-  loss = warp_sum(loss);
-  kls = warp_sum(kls);
-  clipped = warp_sum(clipped);
-  valid = warp_sum(valid);
-  if ((threadIdx.x & 31) == 0) p.sums[item] = make_float4(loss, kls, clipped, valid);
-}
-
-__global__ void __launch_bounds__(1024) policy_finish_kernel(const PolicyParams p) {
-  __shared__ double red[32];
-  const double total =
-      p.a.reduction == BERGSON_POLICY_TOKEN_MEAN ? policy_total(p, red) : 0.0;
-  double loss = 0.0, kl = 0.0, clipped = 0.0, valid = 0.0;
-  for (int64_t b = threadIdx.x; b < p.a.B; b += blockDim.x) {
-    double l = 0.0;
-    for (int64_t i = b * p.segments; i < (b + 1) * p.segments; ++i) {
-      const float4 v = p.sums[i];
-      l += v.x;
-      kl += v.y;
-      clipped += v.z;
-      valid += v.w;
-    }
-    l *= policy_weight(p, b, total);
-    if (p.a.seq_loss != nullptr) p.a.seq_loss[b] = static_cast<float>(l);
-    loss += l;
-  }
-  loss = block_sum(loss, red);
-  kl = block_sum(kl, red);
-  clipped = block_sum(clipped, red);
-  valid = block_sum(valid, red);
+  if (p.a.reduction != BERGSON_POLICY_TOKEN_MEAN) return;
+  if ((threadIdx.x & 31) == 0) red[threadIdx.x >> 5] = mine;
+  __syncthreads();
   if (threadIdx.x == 0) {
-    *p.a.loss = static_cast<float>(loss);
-    if (p.a.stats != nullptr) {
-      p.a.stats[0] = static_cast<float>(kl / fmax(valid, 1.0));
-      p.a.stats[1] = static_cast<float>(clipped / fmax(valid, 1.0));
-      p.a.stats[2] = static_cast<float>(valid);
+    unsigned c = 0;                            // 2^40 tokens over 304 CTAs fit 32 bits
+    for (int w = 0; w < kWarps; ++w) c += red[w];
+    p.counts[blockIdx.x] = c;
+  }
+}
+
+// The token weight where the batch (TOKEN_MEAN) or the row (SEQ_MEAN) has n valid tokens.
+__device__ __forceinline__ float weight_of(const PolicyParams& p, unsigned long long n) {
+  if (p.a.reduction == BERGSON_POLICY_SUM_NORM) return p.norm;
+  n = n > 1 ? n : 1;
+  if (p.a.reduction == BERGSON_POLICY_SEQ_MEAN) n *= static_cast<unsigned long long>(p.a.B);
+  return 1.0f / static_cast<float>(n);
+}
+
+// What the counts before say: of the batch, and of row b, in every lane of a warp.
+__device__ __forceinline__ unsigned long long counted_batch(const PolicyParams& p) {
+  if (p.a.reduction != BERGSON_POLICY_TOKEN_MEAN) return 0;
+  if (p.a.mask == nullptr) return static_cast<unsigned long long>(p.a.B) * p.a.T;
+  unsigned long long n = 0;
+  for (int i = threadIdx.x & 31; i < p.n_counts; i += 32) n += p.counts[i];
+  return warp_sum(n);
+}
+__device__ __forceinline__ unsigned long long counted_row(const PolicyParams& p, int64_t b) {
+  if (p.a.mask == nullptr) return static_cast<unsigned long long>(p.a.T);
+  unsigned long long n = 0;
+  if (p.count_segments <= 8) {
+    for (int i = 0; i < static_cast<int>(p.count_segments); ++i)
+      n += p.counts[b * p.count_segments + i];
+    return n;
+  }
+  for (int64_t i = threadIdx.x & 31; i < p.count_segments; i += 32)
+    n += p.counts[b * p.count_segments + i];
+  return warp_sum(n);
+}
+__device__ __forceinline__ float counted_weight(const PolicyParams& p, unsigned long long batch,
+                                                int64_t b) {
+  return weight_of(p, p.a.reduction == BERGSON_POLICY_SEQ_MEAN ? counted_row(p, b) : batch);
+}
+
+// A warp takes a segment of row b with token weight w; the segment's sums are in every lane.
+template <bool kVec>
+__device__ __forceinline__ float4 policy_segment(const PolicyParams& p, int64_t b, int64_t seg,
+                                                 float w) {
+  const int lane = threadIdx.x & 31;
+  const int64_t T = p.a.T;
+  const uint8_t* mask = p.a.mask == nullptr ? nullptr : p.a.mask + b * p.a.ld_mask;
+  const bool by_token = p.a.ld_adv != 0;
+  const float adv_row = by_token ? 0.0f : p.a.advantages[b];
+  constexpr int kSteps = kSegment / 128;
+  uint32_t on[kSteps];
+#pragma unroll
+  for (int k = 0; k < kSteps; ++k)
+    on[k] = valid_tokens<kVec>(mask, seg * kSegment + 128 * k, T, lane);
+  float loss = 0.0f, kls = 0.0f;
+  int clipped = 0, valid = 0;
+#pragma unroll
+  for (int k = 0; k < kSteps; ++k) {
+    const int64_t t0 = seg * kSegment + 128 * k;
+    if (t0 >= T) break;
+    float lp[4], old[4], adv[4], ref[4], ent[4], d[4], dh[4];
+    load_tokens<kVec>(p.a.logp + b * p.a.ld_logp, t0, T, lane, on[k], lp);
+    load_tokens<kVec>(p.a.old_logp + b * p.a.ld_old, t0, T, lane, on[k], old);
+    if (p.a.ref_logp != nullptr)
+      load_tokens<kVec>(p.a.ref_logp + b * p.a.ld_ref, t0, T, lane, on[k], ref);
+    if (p.a.entropy != nullptr)
+      load_tokens<kVec>(p.a.entropy + b * p.a.ld_entropy, t0, T, lane, on[k], ent);
+    if (by_token) load_tokens<kVec>(p.a.advantages + b * p.a.ld_adv, t0, T, lane, on[k], adv);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      d[j] = dh[j] = 0.0f;
+      if ((on[k] >> j & 1u) == 0) continue;
+      const float a = by_token ? adv[j] : adv_row;
+      const float ratio = expf(lp[j] - old[j]);
+      const float free = ratio * a;
+      const float held = fminf(fmaxf(ratio, p.low), p.high) * a;
+      const bool clip = free > held;
+      float l = clip ? -held : -free;
+      float grad = clip ? 0.0f : -free;
+      if (p.a.ref_logp != nullptr) {
+        const float gap = ref[j] - lp[j];
+        const float up = expm1f(gap);
+        l = fmaf(p.kl, up - gap, l);
+        grad = fmaf(-p.kl, up, grad);
+        kls += up - gap;
+      }
+      if (p.a.entropy != nullptr) l = fmaf(-p.ent, ent[j], l);
+      loss += l;
+      clipped += clip ? 1 : 0;
+      valid += 1;
+      d[j] = w * grad;
+      dh[j] = -w * p.ent;
     }
+    store_tokens<kVec>(p.a.d_logp + b * p.a.ld_d, t0, T, lane, d);
+    if (p.a.d_entropy != nullptr)
+      store_tokens<kVec>(p.a.d_entropy + b * p.a.ld_de, t0, T, lane, dh);
+  }
+  return make_float4(warp_sum(loss), warp_sum(kls),
+                     static_cast<float>(__reduce_add_sync(0xffffffffu, clipped)),
+                     static_cast<float>(__reduce_add_sync(0xffffffffu, valid)));
+}
+
+__device__ __forceinline__ void write_stats(const PolicyParams& p, const Totals& t) {
+  *p.a.loss = t.loss.value();
+  if (p.a.stats == nullptr) return;
+  const float n = static_cast<float>(t.valid > 1 ? t.valid : 1);
+  p.a.stats[0] = t.kl.value() / n;
+  p.a.stats[1] = static_cast<float>(t.clipped) / n;
+  p.a.stats[2] = static_cast<float>(t.valid);
+}
+
+// A warp's sums over the segments of row b, as `part`(i) gives them.
+template <typename F>
+__device__ __forceinline__ Totals row_totals(int64_t segments, F part) {
+  Totals r;
+  for (int64_t i = threadIdx.x & 31; i < segments; i += 32) {
+    const float4 v = part(i);
+    r.loss.add(v.x);
+    r.kl.add(v.y);
+    r.clipped += static_cast<unsigned>(v.z);
+    r.valid += static_cast<unsigned>(v.w);
+  }
+  return totals_sum(r);
+}
+
+template <bool kVec>
+__global__ void __launch_bounds__(kThreads) policy_kernel(const PolicyParams p) {
+  const int64_t items = p.a.B * p.segments;
+  const int64_t warps = static_cast<int64_t>(gridDim.x) * kWarps;
+  int64_t item = static_cast<int64_t>(blockIdx.x) * kWarps + (threadIdx.x >> 5);
+  griddep_launch_dependents();
+  griddep_wait();
+  if (blockIdx.x == 0 && threadIdx.x == 0) *p.ticket = 0;      // for the grid after this one
+  const unsigned long long batch = counted_batch(p);
+  for (; item < items; item += warps) {
+    const int64_t b = item / p.segments;
+    const float4 s = policy_segment<kVec>(p, b, item - b * p.segments, counted_weight(p, batch, b));
+    if ((threadIdx.x & 31) == 0) p.sums[item] = s;
+  }
+}
+
+// Rows' losses, a warp each; the last CTA to finish adds the CTAs' totals in order.
+__global__ void __launch_bounds__(kThreads) policy_finish_kernel(const PolicyParams p) {
+  __shared__ Totals red[kWarps];
+  __shared__ bool last;
+  const int lane = threadIdx.x & 31;
+  griddep_wait();
+  const unsigned long long batch = counted_batch(p);
+  Totals t;
+  for (int64_t b = static_cast<int64_t>(blockIdx.x) * kWarps + (threadIdx.x >> 5); b < p.a.B;
+       b += static_cast<int64_t>(gridDim.x) * kWarps) {
+    Totals r = row_totals(p.segments, [&](int64_t i) { return p.sums[b * p.segments + i]; });
+    const float l = r.loss.value() * counted_weight(p, batch, b);
+    if (p.a.seq_loss != nullptr && lane == 0) p.a.seq_loss[b] = l;
+    r.loss = Sum2();
+    r.loss.add(l);
+    t.add(r);
+  }
+  if (lane == 0) red[threadIdx.x >> 5] = t;
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    t = red[0];
+    for (int w = 1; w < kWarps; ++w) t.add(red[w]);
+    p.totals[blockIdx.x] = t;
+    __threadfence();
+    last = atomicAdd(p.ticket, 1u) == gridDim.x - 1;
+  }
+  __syncthreads();
+  if (!last || threadIdx.x >= 32) return;
+  __threadfence();
+  t = Totals();
+  for (int i = lane; i < static_cast<int>(gridDim.x); i += 32) t.add(p.totals[i]);
+  t = totals_sum(t);
+  if (lane == 0) write_stats(p, t);
+}
+
+// The whole of a small batch in one cluster: each CTA counts every row's valid tokens, takes
+// its share of the segments and leaves their sums with the first, which finishes.
+template <bool kVec>
+__global__ void __launch_bounds__(kThreads) policy_small_kernel(const PolicyParams p) {
+  __shared__ unsigned counts[kSmallItems];               // per row
+  __shared__ float4 sums[kSmallItems];
+  __shared__ Totals red[kWarps];
+  const int parts = static_cast<int>(cluster_size());
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int B = static_cast<int>(p.a.B), segments = static_cast<int>(p.segments);
+  unsigned total = 0;
+  if (p.a.reduction != BERGSON_POLICY_SUM_NORM) {
+    for (int b = warp; b < B; b += kWarps) {
+      const unsigned c = p.a.mask == nullptr ? static_cast<unsigned>(p.a.T)
+                                             : count_bytes(p.a.mask + b * p.a.ld_mask, p.a.T);
+      if (lane == 0) counts[b] = c;
+    }
+    __syncthreads();
+    if (p.a.reduction == BERGSON_POLICY_TOKEN_MEAN) {
+      for (int b = lane; b < B; b += 32) total += counts[b];
+      total = __reduce_add_sync(0xffffffffu, total);
+    }
+  }
+  const auto weight = [&](int b) {
+    return weight_of(p, p.a.reduction == BERGSON_POLICY_SEQ_MEAN ? counts[b] : total);
+  };
+  if (parts > 1) cluster_sync();                         // the first CTA has started
+  for (int i = static_cast<int>(blockIdx.x) * kWarps + warp; i < B * segments; i += parts * kWarps) {
+    const int b = i / segments;
+    const float4 s = policy_segment<kVec>(p, b, i - b * segments, weight(b));
+    if (lane < 4) {
+      const float x = lane == 0 ? s.x : lane == 1 ? s.y : lane == 2 ? s.z : s.w;
+      st_cluster(reinterpret_cast<float*>(&sums[i]) + lane, 0, x);
+    }
+  }
+  if (parts > 1) cluster_sync(); else __syncthreads();
+  if (blockIdx.x != 0) return;
+  Totals t;
+  for (int b = threadIdx.x; b < B; b += kThreads) {      // a row a thread
+    Sum2 l;
+    for (int i = b * segments; i < (b + 1) * segments; ++i) {
+      const float4 v = sums[i];
+      l.add(v.x);
+      t.kl.add(v.y);
+      t.clipped += static_cast<unsigned>(v.z);
+      t.valid += static_cast<unsigned>(v.w);
+    }
+    const float x = l.value() * weight(b);
+    if (p.a.seq_loss != nullptr) p.a.seq_loss[b] = x;
+    t.loss.add(x);
+  }
+  t = totals_sum(t);
+  if (lane == 0) red[warp] = t;
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    t = red[0];
+    for (int w = 1; w < kWarps; ++w) t.add(red[w]);
+    write_stats(p, t);
   }
 }
 
@@ -132,6 +402,7 @@ __global__ void __launch_bounds__(1024) policy_finish_kernel(const PolicyParams 
 
 struct PreferenceParams {
   bergson_preference_args a;
+  int vec;
 };
 
 // f(x) and its slope.
@@ -140,6 +411,7 @@ __device__ __forceinline__ void preference_f(int kind, float x, float beta, floa
     const float e = expf(-fabsf(x));
     *f = fmaxf(-x, 0.0f) + log1pf(e);
     *df = -(x >= 0.0f ? e : 1.0f) / (1.0f + e);
+    if (x != x) *f = *df = x;
   } else if (kind == BERGSON_PREFERENCE_HINGE) {
     *f = fmaxf(1.0f - x, 0.0f);
     *df = x < 1.0f ? -1.0f : 0.0f;
@@ -151,103 +423,315 @@ __device__ __forceinline__ void preference_f(int kind, float x, float beta, floa
   }
 }
 
-__global__ void __launch_bounds__(kThreads) preference_kernel(const PreferenceParams p) {
-  __shared__ double red[kWarps];
-  const int64_t pair = blockIdx.x;
-  double s[2], n[2];
-  for (int side = 0; side < 2; ++side) {
-    const int64_t r = pair + side * p.a.P;
-    float sum = 0.0f, count = 0.0f;
-    for (int64_t t = threadIdx.x; t < p.a.T; t += kThreads) {
-      if (p.a.mask != nullptr && p.a.mask[r * p.a.ld_mask + t] == 0) continue;
-      float v = p.a.logp[r * p.a.ld_logp + t];
-      if (p.a.ref_logp != nullptr) v -= p.a.ref_logp[r * p.a.ld_ref + t];
-      sum += v;
-      count += 1.0f;
+// A CTA's sums over its share [t0, t1) of a row (both multiples of 128, but for T).
+template <bool kVec>
+__device__ __forceinline__ void row_sums(const PreferenceParams& p, int64_t r, int64_t t0,
+                                         int64_t t1, Sum2* red, unsigned* counts, Sum2* sum,
+                                         unsigned* count) {
+  const int lane = threadIdx.x & 31;
+  const uint8_t* mask = p.a.mask == nullptr ? nullptr : p.a.mask + r * p.a.ld_mask;
+  const float* x = p.a.logp + r * p.a.ld_logp;
+  const float* ref = p.a.ref_logp == nullptr ? nullptr : p.a.ref_logp + r * p.a.ld_ref;
+  constexpr int kSteps = 4;
+  Sum2 s;
+  unsigned n = 0;
+  for (int64_t t = t0 + 128 * (threadIdx.x >> 5); t < t1; t += kSteps * 128 * kWarps) {
+    uint32_t on[kSteps];
+    float v[kSteps][4], u[kSteps][4];
+#pragma unroll
+    for (int k = 0; k < kSteps; ++k) {
+      const int64_t tk = t + 128 * kWarps * k;
+      on[k] = tk < t1 ? valid_tokens<kVec>(mask, tk, t1, lane) : 0u;
     }
-    s[side] = block_sum(static_cast<double>(sum), red);
-    n[side] = p.a.mean_logp ? fmax(block_sum(static_cast<double>(count), red), 1.0) : 1.0;
-    s[side] /= n[side];
+#pragma unroll
+    for (int k = 0; k < kSteps; ++k)
+      load_tokens<kVec>(x, t + 128 * kWarps * k, t1, lane, on[k], v[k]);
+    if (ref != nullptr) {
+#pragma unroll
+      for (int k = 0; k < kSteps; ++k)
+        load_tokens<kVec>(ref, t + 128 * kWarps * k, t1, lane, on[k], u[k]);
+    }
+    float f = 0.0f;
+#pragma unroll
+    for (int k = 0; k < kSteps; ++k) {
+      n += __popc(on[k]);
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        if ((on[k] >> j & 1u) != 0) f += ref != nullptr ? v[k][j] - u[k][j] : v[k][j];
+    }
+    s.add(f);
   }
-  const float beta = static_cast<float>(p.a.beta);
-  const float x = static_cast<float>(p.a.beta * (s[0] - s[1]) - p.a.margin);
-  const float eps = static_cast<float>(p.a.label_smoothing);
+  s = warp_sum(s);
+  n = __reduce_add_sync(0xffffffffu, n);
+  if (lane == 0) {
+    red[threadIdx.x >> 5] = s;
+    counts[threadIdx.x >> 5] = n;
+  }
+  __syncthreads();
+  s = red[0];
+  n = counts[0];
+#pragma unroll
+  for (int w = 1; w < kWarps; ++w) {
+    s.add(red[w]);
+    n += counts[w];
+  }
+  __syncthreads();
+  *sum = s;
+  *count = n;
+}
+
+// What follows from a pair's sums, in every thread.
+struct PairGrad {
+  float loss, d[2], reward[2];
+};
+
+__device__ __forceinline__ PairGrad pair_grad(const bergson_preference_args& a, const Sum2* sum,
+                                              const unsigned* count) {
+  const float beta = static_cast<float>(a.beta), eps = static_cast<float>(a.label_smoothing);
+  float n[2], s[2], gap;
+  for (int k = 0; k < 2; ++k) {
+    n[k] = a.mean_logp && count[k] > 1 ? static_cast<float>(count[k]) : 1.0f;
+    s[k] = sum[k].value() / n[k];
+  }
+  // without means the sums' second parts still count in their difference
+  gap = a.mean_logp ? s[0] - s[1] : sum[0].hi - sum[1].hi;
+  if (!a.mean_logp && gap - gap == 0.0f) gap += sum[0].lo - sum[1].lo;
+  const float x = fmaf(beta, gap, -static_cast<float>(a.margin));
   float f, df, g, dg;
-  preference_f(p.a.kind, x, beta, &f, &df);
-  preference_f(p.a.kind, -x, beta, &g, &dg);
+  preference_f(a.kind, x, beta, &f, &df);
+  preference_f(a.kind, -x, beta, &g, &dg);
+  PairGrad o;
   // a side of weight 0 takes no part, even where it is infinite
-  const float loss = (eps < 1.0f ? (1.0f - eps) * f : 0.0f) + (eps > 0.0f ? eps * g : 0.0f);
+  o.loss = (eps < 1.0f ? (1.0f - eps) * f : 0.0f) + (eps > 0.0f ? eps * g : 0.0f);
   const float slope = (eps < 1.0f ? (1.0f - eps) * df : 0.0f) - (eps > 0.0f ? eps * dg : 0.0f);
-  if (threadIdx.x == 0) {
-    p.a.pair_loss[pair] = loss;
-    if (p.a.rewards != nullptr) {
-      p.a.rewards[pair] = static_cast<float>(p.a.beta * s[0]);
-      p.a.rewards[pair + p.a.P] = static_cast<float>(p.a.beta * s[1]);
+  for (int k = 0; k < 2; ++k) {
+    o.d[k] = (k ? -slope : slope) * beta / (static_cast<float>(a.P) * n[k]);
+    o.reward[k] = beta * s[k];
+  }
+  return o;
+}
+
+template <bool kVec>
+__device__ __forceinline__ void write_row(const PreferenceParams& p, int64_t r, int64_t t0,
+                                          int64_t t1, float d) {
+  const int lane = threadIdx.x & 31;
+  const uint8_t* mask = p.a.mask == nullptr ? nullptr : p.a.mask + r * p.a.ld_mask;
+  float* out = p.a.d_logp + r * p.a.ld_d;
+#pragma unroll 4
+  for (int64_t t = t0 + 128 * (threadIdx.x >> 5); t < t1; t += 128 * kWarps) {
+    const uint32_t on = valid_tokens<kVec>(mask, t, t1, lane);
+    float x[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) x[j] = (on >> j & 1u) != 0 ? d : 0.0f;
+    store_tokens<kVec>(out, t, t1, lane, x);
+  }
+}
+
+// kTogether: a pair a CTA, all of them in one cluster, whose first CTA adds the losses.
+// Else a pair a cluster, its CTAs each a share of the tokens.
+template <bool kVec, bool kTogether>
+__global__ void __launch_bounds__(kThreads) preference_kernel(const PreferenceParams p) {
+  __shared__ Sum2 red[kWarps];
+  __shared__ unsigned counts[kWarps];
+  __shared__ float shared[8][6];               // from each CTA: two sums and counts
+  const int parts = static_cast<int>(cluster_size());
+  const int rank = static_cast<int>(blockIdx.x) % parts;
+  const int64_t pair = kTogether ? blockIdx.x : blockIdx.x / parts;
+  const bool live = pair < p.a.P;
+  const int64_t blocks = (p.a.T + 127) / 128;
+  const int64_t per = kTogether ? blocks : (blocks + parts - 1) / parts;
+  const int64_t t0 = kTogether ? 0 : min(p.a.T, per * rank * 128);
+  const int64_t t1 = min(p.a.T, t0 + per * 128);
+  Sum2 sum[2];
+  unsigned count[2] = {};
+  if (live) {
+    for (int k = 0; k < 2; ++k)
+      row_sums<kVec>(p, pair + k * p.a.P, t0, t1, red, counts, &sum[k], &count[k]);
+  }
+  if (!kTogether && parts > 1) {
+    cluster_sync();                            // every CTA has started
+    if (threadIdx.x < parts) {
+#pragma unroll
+      for (int k = 0; k < 2; ++k) {
+        st_cluster(&shared[rank][3 * k], threadIdx.x, sum[k].hi);
+        st_cluster(&shared[rank][3 * k + 1], threadIdx.x, sum[k].lo);
+        st_cluster(&shared[rank][3 * k + 2], threadIdx.x, __uint_as_float(count[k]));
+      }
+    }
+    cluster_sync();
+    for (int k = 0; k < 2; ++k) {
+      sum[k] = Sum2();
+      count[k] = 0;
+      for (int c = 0; c < parts; ++c) {
+        Sum2 o;
+        o.hi = shared[c][3 * k];
+        o.lo = shared[c][3 * k + 1];
+        sum[k].add(o);
+        count[k] += __float_as_uint(shared[c][3 * k + 2]);
+      }
     }
   }
-  for (int side = 0; side < 2; ++side) {
-    const int64_t r = pair + side * p.a.P;
-    const float d = static_cast<float>((side ? -1.0 : 1.0) * slope * p.a.beta /
-                                       (static_cast<double>(p.a.P) * n[side]));
-    for (int64_t t = threadIdx.x; t < p.a.T; t += kThreads) {
-      const bool on = p.a.mask == nullptr || p.a.mask[r * p.a.ld_mask + t] != 0;
-      p.a.d_logp[r * p.a.ld_d + t] = on ? d : 0.0f;
+  PairGrad g = {};
+  if (live) {
+    g = pair_grad(p.a, sum, count);
+    if (threadIdx.x == 0 && (kTogether || rank == 0)) {
+      p.a.pair_loss[pair] = g.loss;
+      if (p.a.rewards != nullptr) {
+        p.a.rewards[pair] = g.reward[0];
+        p.a.rewards[pair + p.a.P] = g.reward[1];
+      }
     }
+  }
+  if (kTogether) {
+    cluster_sync();
+    if (threadIdx.x == 0) st_cluster(&shared[rank][0], 0, g.loss);
+    cluster_sync();
+    if (rank == 0 && threadIdx.x == 0) {
+      Sum2 l;
+      for (int c = 0; c < static_cast<int>(p.a.P); ++c) l.add(shared[c][0]);
+      *p.a.loss = l.value() / static_cast<float>(p.a.P);
+    }
+  } else {
+    griddep_launch_dependents();
+  }
+  if (live) {
+    for (int k = 0; k < 2; ++k) write_row<kVec>(p, pair + k * p.a.P, t0, t1, g.d[k]);
   }
 }
 
 __global__ void __launch_bounds__(1024) preference_finish_kernel(const float* pair_loss,
                                                                  int64_t P, float* loss) {
-  __shared__ double red[32];
-  double s = 0.0;
-  for (int64_t i = threadIdx.x; i < P; i += blockDim.x) s += pair_loss[i];
+  __shared__ Sum2 red[32];
+  griddep_wait();
+  Sum2 s;
+#pragma unroll 4
+  for (int64_t i = threadIdx.x; i < P; i += blockDim.x) s.add(pair_loss[i]);
   s = block_sum(s, red);
-  if (threadIdx.x == 0) *loss = P > 0 ? static_cast<float>(s / static_cast<double>(P)) : 0.0f;
+  if (threadIdx.x == 0) *loss = P > 0 ? s.value() / static_cast<float>(P) : 0.0f;
 }
 
-int64_t segments_of(int64_t T) { return (T + kSegment - 1) / kSegment; }
+// ------------------------------------------------------------------- host
 
+int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 size_t align256(size_t n) { return (n + 255) / 256 * 256; }
+size_t counts_bytes(int64_t B, int64_t T) {
+  return align256(4 * static_cast<size_t>(std::max<int64_t>(kCountCtas, B * ceil_div(T, kCountSegment))));
+}
+
+// Rows whose 16-byte loads of four tokens are aligned.
+bool fits(const void* p, int64_t ld, size_t elem) {
+  return p == nullptr || (reinterpret_cast<uintptr_t>(p) % (4 * elem) == 0 && ld % 4 == 0);
+}
+
+template <typename K, typename P>
+cudaError_t launch_cluster(K kernel, int64_t grid, int cluster, const P& p, cudaStream_t s) {
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(static_cast<unsigned>(grid));
+  cfg.blockDim = dim3(kThreads);
+  cfg.stream = s;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeClusterDimension;
+  attr[0].val.clusterDim.x = cluster;
+  attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  return cudaLaunchKernelEx(&cfg, kernel, p);
+}
+
+template <bool kVec>
+cudaError_t run_policy(PolicyParams p, cudaStream_t s) {
+  const int64_t items = p.a.B * p.segments;
+  if (items <= kSmallItems && p.a.B <= kSmallItems && p.a.B * p.a.T <= kSmallTokens) {
+    int parts = 1;
+    while (parts < 8 && parts * kWarps < items) parts *= 2;
+    return launch_cluster(policy_small_kernel<kVec>, parts, parts, p, s);
+  }
+  if (p.a.mask != nullptr && p.a.reduction != BERGSON_POLICY_SUM_NORM) {
+    p.n_counts = static_cast<int>(
+        std::min<int64_t>(kCountCtas, ceil_div(p.a.B * p.count_segments, kWarps)));
+    policy_count_kernel<<<p.n_counts, kThreads, 0, s>>>(p);
+    const cudaError_t e = cudaGetLastError();
+    if (e != cudaSuccess) return e;
+  }
+  cudaError_t e = launch_dependent(policy_kernel<kVec>,
+                                   dim3(static_cast<unsigned>(
+                                       std::min<int64_t>(kPolicyCtas, ceil_div(items, kWarps)))),
+                                   dim3(kThreads), 0, s, p);
+  if (e != cudaSuccess) return e;
+  const int64_t finish = std::min<int64_t>(kFinishCtas, ceil_div(p.a.B, kWarps));
+  return launch_dependent(policy_finish_kernel, dim3(static_cast<unsigned>(finish)),
+                          dim3(kThreads), 0, s, p);
+}
+
+template <bool kVec>
+cudaError_t run_preference(const PreferenceParams& p, int sms, cudaStream_t s) {
+  const int64_t P = p.a.P;
+  if (P <= 8 && 2 * p.a.T <= 8192) {
+    int n = 1;
+    while (n < P) n *= 2;
+    return launch_cluster(preference_kernel<kVec, true>, n, n, p, s);
+  }
+  int parts = 1;
+  while (parts < 8 && P * parts < 2 * sms && p.a.T / parts > 2048) parts *= 2;
+  cudaError_t e = launch_cluster(preference_kernel<kVec, false>, P * parts, parts, p, s);
+  if (e != cudaSuccess) return e;
+  return launch_dependent(preference_finish_kernel, dim3(1), dim3(1024), 0, s,
+                          static_cast<const float*>(p.a.pair_loss), P, p.a.loss);
+}
 
 }  // namespace
 
+// counts, the totals and their ticket, the segments' sums
 size_t policy_workspace(int64_t B, int64_t T) {
-  return 256 + align256(4 * static_cast<size_t>(B)) +
-         align256(16 * static_cast<size_t>(B) * static_cast<size_t>(segments_of(T)));
+  return counts_bytes(B, T) + align256(sizeof(Totals) * kFinishCtas) + 256 +
+         align256(sizeof(float4) * static_cast<size_t>(B) * static_cast<size_t>(ceil_div(T, kSegment)));
 }
 
 cudaError_t launch_policy_loss(const bergson_policy_args& a, void* ws, cudaStream_t s) {
   PolicyParams p;
   p.a = a;
-  p.segments = segments_of(a.T);
-  p.counts = static_cast<unsigned*>(ws);
-  p.sums = reinterpret_cast<float4*>(static_cast<char*>(ws) +
-                                     align256(4 * static_cast<size_t>(a.B)));
+  p.segments = ceil_div(a.T, kSegment);
+  p.count_segments = ceil_div(a.T, kCountSegment);
+  p.n_counts = 0;
+  char* at = static_cast<char*>(ws);
+  p.counts = reinterpret_cast<unsigned*>(at);
+  at += counts_bytes(a.B, a.T);
+  p.totals = reinterpret_cast<Totals*>(at);
+  at += align256(sizeof(Totals) * kFinishCtas);
+  p.ticket = reinterpret_cast<unsigned*>(at);
+  p.sums = reinterpret_cast<float4*>(at + 256);
   p.low = static_cast<float>(1.0 - a.clip_low);
   p.high = static_cast<float>(1.0 + a.clip_high);
   p.kl = static_cast<float>(a.kl_coef);
   p.ent = static_cast<float>(a.entropy_coef);
+  p.norm = static_cast<float>(1.0 / (static_cast<double>(a.B) * a.norm_tokens));
   if (a.kl_coef == 0.0) p.a.ref_logp = nullptr;
   if (a.entropy_coef == 0.0) p.a.entropy = nullptr;
-  const int64_t items = a.B * p.segments;
-  if (items > 0) {
-    if (a.mask != nullptr && a.reduction != BERGSON_POLICY_SUM_NORM)
-      policy_count_kernel<<<static_cast<unsigned>((a.B + kWarps - 1) / kWarps), kThreads, 0, s>>>(p);
-    policy_kernel<<<static_cast<unsigned>((items + kWarps - 1) / kWarps), kThreads, 0, s>>>(p);
-  } else {
-    // nothing reads the counts of a batch without tokens: every loss is 0
-    p.a.mask = nullptr;
+  if (a.B == 0 || a.T == 0) {                  // no token: zeros
+    cudaError_t e = cudaMemsetAsync(a.loss, 0, sizeof(float), s);
+    if (e == cudaSuccess && a.stats != nullptr)
+      e = cudaMemsetAsync(a.stats, 0, 3 * sizeof(float), s);
+    if (e == cudaSuccess && a.seq_loss != nullptr && a.B > 0)
+      e = cudaMemsetAsync(a.seq_loss, 0, sizeof(float) * static_cast<size_t>(a.B), s);
+    return e;
   }
-  policy_finish_kernel<<<1, 1024, 0, s>>>(p);
-  return cudaGetLastError();
+  p.vec = fits(a.logp, a.ld_logp, 4) && fits(a.old_logp, a.ld_old, 4) &&
+          fits(p.a.ref_logp, a.ld_ref, 4) && fits(p.a.entropy, a.ld_entropy, 4) &&
+          (a.ld_adv == 0 || fits(a.advantages, a.ld_adv, 4)) && fits(a.mask, a.ld_mask, 1) &&
+          fits(a.d_logp, a.ld_d, 4) && fits(a.d_entropy, a.ld_de, 4);
+  return p.vec ? run_policy<true>(p, s) : run_policy<false>(p, s);
 }
 
-cudaError_t launch_preference_loss(const bergson_preference_args& a, int, cudaStream_t s) {
+cudaError_t launch_preference_loss(const bergson_preference_args& a, int sms, cudaStream_t s) {
+  if (a.P == 0) {
+    preference_finish_kernel<<<1, 1024, 0, s>>>(a.pair_loss, 0, a.loss);
+    return cudaGetLastError();
+  }
   PreferenceParams p;
   p.a = a;
-  if (a.P > 0) preference_kernel<<<static_cast<unsigned>(a.P), kThreads, 0, s>>>(p);
-  preference_finish_kernel<<<1, 1024, 0, s>>>(a.pair_loss, a.P, a.loss);
-  return cudaGetLastError();
+  p.vec = fits(a.logp, a.ld_logp, 4) && fits(a.ref_logp, a.ld_ref, 4) &&
+          fits(a.mask, a.ld_mask, 1) && fits(a.d_logp, a.ld_d, 4);
+  return p.vec ? run_preference<true>(p, sms, s) : run_preference<false>(p, sms, s);
 }
 
 }  // namespace bergson

@@ -10,9 +10,10 @@ namespace {
 
 constexpr int kThreads = 256;
 constexpr int kWarps = kThreads / 32;
-constexpr int kBand = 64;                      // rows of a tile
-constexpr int kStrip = kThreads;               // columns of a tile
-constexpr int kMaxEntries = 300;
+constexpr int kWarpRows = 16;                  // rows a warp takes
+constexpr int kBand = kWarps * kWarpRows;      // rows of a tile
+constexpr int kStrip = 256;                    // columns of a tile, 8 a lane
+constexpr int kFew = 24, kMany = 300;          // records a launch can take
 
 struct Entry {
   const void* v;
@@ -24,15 +25,17 @@ struct Entry {
   float* col_part;             // [bands, cols]
   float* tile_part;            // [bands, strips]
   int bands, strips;
-  int st, pad;
+  int st;
+  int vec;                     // rows start on boundaries of a lane's 8 elements
 };
 
+template <int N>
 struct MomentParams {
-  Entry e[kMaxEntries];
-  uint32_t tiles[kMaxEntries + 1];
-  uint32_t outs[kMaxEntries + 1];      // CTAs of the second pass
-  int n;
   float correction, floor;
+  int n;
+  uint32_t tiles[N + 1];               // first CTA of each matrix in the first pass
+  uint32_t outs[N + 1];                // ... and in the second
+  Entry e[N];
 };
 
 __device__ __forceinline__ int find(const uint32_t* begin, int n, uint32_t at) {
@@ -44,61 +47,181 @@ __device__ __forceinline__ int find(const uint32_t* begin, int n, uint32_t at) {
   return lo;
 }
 
-__global__ void __launch_bounds__(kThreads) moment_tiles_kernel(
-    const __grid_constant__ MomentParams p) {
-  __shared__ float rows[kWarps][kBand];
-  __shared__ float red[kWarps];
-  const Entry& e = p.e[find(p.tiles, p.n, blockIdx.x)];
-  const uint32_t tile = blockIdx.x - p.tiles[find(p.tiles, p.n, blockIdx.x)];
-  const int band = tile / e.strips, strip = tile % e.strips;
-  const int64_t c = static_cast<int64_t>(strip) * kStrip + threadIdx.x;
-  const int64_t r0 = static_cast<int64_t>(band) * kBand;
-  float col = 0.0f;
-  for (int k = 0; k < kBand; ++k) {
-    float x = 0.0f;
-    if (r0 + k < e.rows && c < e.cols) {
-      const int64_t i = (r0 + k) * e.cols + c;
-      x = e.st == BERGSON_STATE_8BIT
-              ? __fmul_rn(decode_second(static_cast<const uint8_t*>(e.v)[i]), e.vs[i / kStateBlock])
-              : static_cast<const float*>(e.v)[i];
+// The sums over the lanes of each of N values: lane l has that of value l / (32 / N).
+template <int N>
+__device__ __forceinline__ float sum_each(float (&x)[N]) {
+  const int lane = threadIdx.x & 31;
+  int o = 16;
+#pragma unroll
+  for (int n = N / 2; n > 0; n /= 2) {
+    const bool up = (lane & o) != 0;
+#pragma unroll
+    for (int k = 0; k < n; ++k) {
+      const float give = up ? x[k] : x[k + n];
+      x[k] = (up ? x[k + n] : x[k]) + __shfl_xor_sync(0xffffffffu, give, o);
     }
-    col += x;
-    x = warp_sum(x);
-    if ((threadIdx.x & 31) == 0) rows[threadIdx.x >> 5][k] = x;
+    o /= 2;
   }
-  if (c < e.cols) e.col_part[static_cast<int64_t>(band) * e.cols + c] = col;
-  __syncthreads();
-  if (threadIdx.x < kBand && r0 + threadIdx.x < e.rows) {
-    float x = 0.0f;
-    for (int w = 0; w < kWarps; ++w) x += rows[w][threadIdx.x];
-    e.row_part[static_cast<int64_t>(strip) * e.rows + r0 + threadIdx.x] = x;
-  }
-  const float all = block_sum(col, red);
-  if (threadIdx.x == 0) e.tile_part[tile] = all;
+  float t = x[0];
+  for (; o > 0; o /= 2) t += __shfl_xor_sync(0xffffffffu, t, o);
+  return t;
 }
 
+// A warp's rows r0 .. r0 + kWarpRows of a tile: lane sums of the columns in col[], the
+// rows' sums to row_part.  Vectors: columns c0 + 8 lane + k; else c0 + lane + 32 k.
+template <bool kEight, bool kVec>
+__device__ __forceinline__ void take_rows(const Entry& e, int64_t r0, int64_t c0, float* row_part,
+                                          float (&col)[8]) {
+  constexpr int kRows = 8;                     // on the way at once
+  const int lane = threadIdx.x & 31;
+  float2 col2[4] = {};
+#pragma unroll 1
+  for (int64_t r = r0; r < r0 + kWarpRows && r < e.rows; r += kRows) {
+    float sums[kRows];
+    if constexpr (kVec && !kEight) {
+      uint32_t x[kRows][8];
+      const int64_t c = c0 + 8 * lane;
+#pragma unroll
+      for (int k = 0; k < kRows; ++k) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) x[k][j] = 0;
+        if (r + k < e.rows && c < e.cols)
+          load32(static_cast<const float*>(e.v) + (r + k) * e.cols + c, x[k]);
+      }
+#pragma unroll
+      for (int k = 0; k < kRows; ++k) {
+        float2 s = {0.0f, 0.0f};
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const float2 y = make_float2(__uint_as_float(x[k][2 * j]), __uint_as_float(x[k][2 * j + 1]));
+          col2[j] = add2(col2[j], y);
+          s = add2(s, y);
+        }
+        sums[k] = s.x + s.y;
+      }
+    } else if constexpr (kVec) {
+      uint2 u[kRows];
+      float sc[kRows];
+      const int64_t c = c0 + 8 * lane;
+#pragma unroll
+      for (int k = 0; k < kRows; ++k) {
+        u[k] = make_uint2(0, 0);
+        sc[k] = 0.0f;
+        if (r + k < e.rows && c < e.cols) {
+          const int64_t i = (r + k) * e.cols + c;
+          u[k] = *reinterpret_cast<const uint2*>(static_cast<const uint8_t*>(e.v) + i);
+          sc[k] = e.vs[i / kStateBlock];
+        }
+      }
+#pragma unroll
+      for (int k = 0; k < kRows; ++k) {
+        float y[8];
+        decode_second4(u[k].x, y);
+        decode_second4(u[k].y, y + 4);
+        float2 s = {0.0f, 0.0f};
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const float2 y2 = make_float2(y[2 * j], y[2 * j + 1]);
+          col2[j] = fma2(y2, pair(sc[k]), col2[j]);
+          s = add2(s, y2);
+        }
+        sums[k] = (s.x + s.y) * sc[k];
+      }
+    } else {
+#pragma unroll
+      for (int k = 0; k < kRows; ++k) {
+        float y[8];
+        const int64_t row = (r + k) * e.cols;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          const int64_t c = c0 + lane + 32 * j;
+          y[j] = 0.0f;
+          if (r + k < e.rows && c < e.cols)
+            y[j] = kEight ? decode_second(static_cast<const uint8_t*>(e.v)[row + c]) *
+                                e.vs[(row + c) / kStateBlock]
+                          : static_cast<const float*>(e.v)[row + c];
+        }
+        float2 s = {0.0f, 0.0f};
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const float2 y2 = make_float2(y[2 * j], y[2 * j + 1]);
+          col2[j] = add2(col2[j], y2);
+          s = add2(s, y2);
+        }
+        sums[k] = s.x + s.y;
+      }
+    }
+    const float t = sum_each(sums);
+    const int k = lane / (32 / kRows);
+    if (lane % (32 / kRows) == 0 && r + k < e.rows) row_part[r + k] = t;
+  }
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    col[2 * j] = col2[j].x;
+    col[2 * j + 1] = col2[j].y;
+  }
+}
+
+template <int N>
+__global__ void __launch_bounds__(kThreads) moment_tiles_kernel(
+    const __grid_constant__ MomentParams<N> p) {
+  __shared__ float cols[kWarps][kStrip];
+  __shared__ float red[kWarps];
+  const int at = find(p.tiles, p.n, blockIdx.x);
+  const Entry& e = p.e[at];
+  const uint32_t tile = blockIdx.x - p.tiles[at];
+  const int band = tile / e.strips, strip = tile % e.strips;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int64_t r0 = static_cast<int64_t>(band) * kBand + warp * kWarpRows;
+  const int64_t c0 = static_cast<int64_t>(strip) * kStrip;
+  float* row_part = e.row_part + static_cast<int64_t>(strip) * e.rows;
+  float col[8];
+  if (e.st == BERGSON_STATE_8BIT) {
+    if (e.vec) take_rows<true, true>(e, r0, c0, row_part, col);
+    else take_rows<true, false>(e, r0, c0, row_part, col);
+  } else {
+    if (e.vec) take_rows<false, true>(e, r0, c0, row_part, col);
+    else take_rows<false, false>(e, r0, c0, row_part, col);
+  }
+#pragma unroll
+  for (int j = 0; j < 8; ++j) cols[warp][e.vec ? 8 * lane + j : lane + 32 * j] = col[j];
+  __syncthreads();
+  float x = 0.0f;
+#pragma unroll
+  for (int w = 0; w < kWarps; ++w) x += cols[w][threadIdx.x];
+  const int64_t c = c0 + threadIdx.x;
+  if (c < e.cols) e.col_part[static_cast<int64_t>(band) * e.cols + c] = x;
+  x = block_sum(x, red);
+  if (threadIdx.x == 0) e.tile_part[tile] = x;
+}
+static_assert(kStrip == kThreads, "a thread sums a column of the tile");
+
+template <int N>
 __global__ void __launch_bounds__(kThreads) moment_finish_kernel(
-    const __grid_constant__ MomentParams p) {
+    const __grid_constant__ MomentParams<N> p) {
   __shared__ float red[kWarps];
   const int at = find(p.outs, p.n, blockIdx.x);
   const Entry& e = p.e[at];
   const int64_t i = static_cast<int64_t>(blockIdx.x - p.outs[at]) * kThreads + threadIdx.x;
+  griddep_wait();
+  const bool row = i < e.rows;
+  const int64_t j = i - e.rows;
+  CompensatedSum x;
+  if (row || j < e.cols) {
+    const float* part = row ? e.row_part + i : e.col_part + j;
+    const int64_t step = row ? e.rows : e.cols;
+    const int n = row ? e.strips : e.bands;
+#pragma unroll 8
+    for (int k = 0; k < n; ++k) x.add(part[k * step]);
+  }
   CompensatedSum sum;
-  for (int64_t k = threadIdx.x; k < static_cast<int64_t>(e.bands) * e.strips; k += kThreads)
-    sum.add(e.tile_part[k]);
+  const int64_t tiles = static_cast<int64_t>(e.bands) * e.strips;
+  for (int64_t k = threadIdx.x; k < tiles; k += kThreads) sum.add(e.tile_part[k]);
   const float all = block_sum(sum.s, red);
   const float rows = static_cast<float>(e.rows), cols = static_cast<float>(e.cols);
-  const float mean = all / rows / cols * p.correction + p.floor;
-  if (i < e.rows) {
-    CompensatedSum x;
-    for (int k = 0; k < e.strips; ++k) x.add(e.row_part[k * e.rows + i]);
-    e.r[i] = x.s / cols * p.correction + p.floor;
-  } else if (i - e.rows < e.cols) {
-    const int64_t j = i - e.rows;
-    CompensatedSum x;
-    for (int k = 0; k < e.bands; ++k) x.add(e.col_part[k * e.cols + j]);
-    e.c[j] = (x.s / rows * p.correction + p.floor) / mean;
-  }
+  if (row) e.r[i] = x.s / cols * p.correction + p.floor;
+  else if (j < e.cols)
+    e.c[j] = (x.s / rows * p.correction + p.floor) / (all / rows / cols * p.correction + p.floor);
 }
 
 int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
@@ -106,6 +229,56 @@ int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 size_t floats_of(const bergson_moment_matrix& m) {
   const size_t bands = ceil_div(m.d_out, kBand), strips = ceil_div(m.d_in, kStrip);
   return strips * m.d_out + bands * m.d_in + bands * strips;
+}
+
+template <int N>
+cudaError_t run_moments(const bergson_moment_matrix* m, int n, double correction, double floor,
+                        void* ws, cudaStream_t s) {
+  MomentParams<N> p;
+  p.correction = static_cast<float>(correction);
+  p.floor = static_cast<float>(floor);
+  int k = 0;
+  p.tiles[0] = p.outs[0] = 0;
+  float* at = static_cast<float*>(ws);
+  const auto flush = [&]() -> cudaError_t {
+    if (k == 0) return cudaSuccess;
+    p.n = k;
+    moment_tiles_kernel<N><<<p.tiles[k], kThreads, 0, s>>>(p);
+    const cudaError_t e = cudaGetLastError();
+    if (e != cudaSuccess) return e;
+    const dim3 grid(p.outs[k]);
+    k = 0;
+    return launch_dependent(moment_finish_kernel<N>, grid, dim3(kThreads), 0, s, p);
+  };
+  for (int i = 0; i < n; ++i) {
+    const int64_t bands = ceil_div(m[i].d_out, kBand), strips = ceil_div(m[i].d_in, kStrip);
+    const int64_t outs = ceil_div(m[i].d_out + m[i].d_in, kThreads);
+    if (k == N ||
+        (k > 0 && (p.tiles[k] + bands * strips > INT32_MAX || p.outs[k] + outs > INT32_MAX))) {
+      const cudaError_t e = flush();
+      if (e != cudaSuccess) return e;
+    }
+    Entry& e = p.e[k];
+    e.v = m[i].v;
+    e.vs = m[i].v_scale;
+    e.rows = m[i].d_out;
+    e.cols = m[i].d_in;
+    e.r = m[i].r;
+    e.c = m[i].c;
+    e.st = m[i].state_kind;
+    e.vec = m[i].d_in % 8 == 0 &&
+            reinterpret_cast<uintptr_t>(m[i].v) % (e.st == BERGSON_STATE_8BIT ? 8 : 32) == 0;
+    e.bands = static_cast<int>(bands);
+    e.strips = static_cast<int>(strips);
+    e.row_part = at;
+    e.col_part = e.row_part + strips * e.rows;
+    e.tile_part = e.col_part + bands * e.cols;
+    at = e.tile_part + bands * strips;
+    p.tiles[k + 1] = p.tiles[k] + static_cast<uint32_t>(bands * strips);
+    p.outs[k + 1] = p.outs[k] + static_cast<uint32_t>(outs);
+    ++k;
+  }
+  return flush();
 }
 
 }  // namespace
@@ -118,46 +291,8 @@ size_t moments_workspace(const bergson_moment_matrix* m, int n) {
 
 cudaError_t launch_factor_moments(const bergson_moment_matrix* m, int n, double correction,
                                   double floor, void* ws, cudaStream_t s) {
-  MomentParams p;
-  p.correction = static_cast<float>(correction);
-  p.floor = static_cast<float>(floor);
-  p.n = 0;
-  p.tiles[0] = p.outs[0] = 0;
-  float* at = static_cast<float*>(ws);
-  const auto flush = [&]() -> cudaError_t {
-    if (p.n == 0) return cudaSuccess;
-    moment_tiles_kernel<<<p.tiles[p.n], kThreads, 0, s>>>(p);
-    moment_finish_kernel<<<p.outs[p.n], kThreads, 0, s>>>(p);
-    p.n = 0;
-    return cudaGetLastError();
-  };
-  for (int i = 0; i < n; ++i) {
-    const int64_t bands = ceil_div(m[i].d_out, kBand), strips = ceil_div(m[i].d_in, kStrip);
-    const int64_t outs = ceil_div(m[i].d_out + m[i].d_in, kThreads);
-    if (p.n == kMaxEntries ||
-        (p.n > 0 && (p.tiles[p.n] + bands * strips > INT32_MAX || p.outs[p.n] + outs > INT32_MAX))) {
-      const cudaError_t e = flush();
-      if (e != cudaSuccess) return e;
-    }
-    Entry& e = p.e[p.n];
-    e.v = m[i].v;
-    e.vs = m[i].v_scale;
-    e.rows = m[i].d_out;
-    e.cols = m[i].d_in;
-    e.r = m[i].r;
-    e.c = m[i].c;
-    e.st = m[i].state_kind;
-    e.bands = static_cast<int>(bands);
-    e.strips = static_cast<int>(strips);
-    e.row_part = at;
-    e.col_part = e.row_part + strips * e.rows;
-    e.tile_part = e.col_part + bands * e.cols;
-    at = e.tile_part + bands * strips;
-    p.tiles[p.n + 1] = p.tiles[p.n] + static_cast<uint32_t>(bands * strips);
-    p.outs[p.n + 1] = p.outs[p.n] + static_cast<uint32_t>(outs);
-    ++p.n;
-  }
-  return flush();
+  return n <= kFew ? run_moments<kFew>(m, n, correction, floor, ws, s)
+                   : run_moments<kMany>(m, n, correction, floor, ws, s);
 }
 
 }  // namespace bergson
