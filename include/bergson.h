@@ -757,7 +757,7 @@ BERGSON_API int bergson_token_logprobs_backward(const void* logits, int dtype, i
  *             (ratio A > clamped A), number of valid tokens.
  *   d_logp    fp32 [B, ld_d];  d_entropy  fp32 [B, ld_de] or NULL.
  *   workspace 256-byte aligned, contents on entry ignored.
- * Leading dimensions are >= T.  B, T >= 0, B * T < 2^40.  Sums run in fp32 within 512
+ * Leading dimensions are >= T.  B, T >= 0, T <= 2^30, B * T <= 2^40.  Sums run in fp32 within 512
  * tokens and in twice its bits above, in an order fixed by the sizes.
  * Errors: EINVAL, EALIGN, EUNSUPPORTED, EWORKSPACE, ECUDA.
  */
@@ -803,7 +803,7 @@ BERGSON_API int bergson_policy_loss(const bergson_policy_args* args, void* works
  *   mask      u8 [2P, ld_mask] (nonzero = valid) or NULL (all valid).
  *   beta > 0, label_smoothing in [0, 1].
  *   loss fp32 [1], pair_loss fp32 [P], rewards fp32 [2P] or NULL, d_logp fp32 [2P, ld_d].
- * Leading dimensions are >= T.  P, T >= 0, P < 2^30, 2 P T < 2^40; P = 0 gives loss 0.
+ * Leading dimensions are >= T.  P, T >= 0, P < 2^30, T <= 2^30, 2 P T <= 2^40; P = 0 gives loss 0.
  * Sums over tokens and pairs run in an order fixed by the sizes.
  * Errors: EINVAL, EALIGN, EUNSUPPORTED, ECUDA.
  */

@@ -19,61 +19,108 @@ namespace {
 constexpr int kThreads = 256;
 constexpr int kWarps = kThreads / 32;
 
-// ------------------------------------------------ four tokens of a row a lane
+// ------------------------------------------------ several tokens of a row a lane
 //
-// A warp takes 128 tokens of a row at a time, four a lane: neighbours in one load
-// where the rows allow it (kVec), else 32 apart in loads of one.
+// A warp takes 32 N tokens of a row at a time, N (4 or 8) a lane: neighbours in one
+// load where the rows allow it (kVec), else 32 apart in loads of one.  Their mask
+// bytes stay in words; tokens past the end have mask 0.  Masked tokens are not read
+// (in a vector, where all of it is masked).
 
-template <bool kVec>
-__device__ __forceinline__ int64_t token_of(int64_t t0, int lane, int j) {
-  return kVec ? t0 + 4 * lane + j : t0 + lane + 32 * j;
+template <int N>
+struct Mask {
+  uint32_t w[N / 4];
+  __device__ __forceinline__ bool on(int j) const {
+    return (w[j / 4] & (0xffu << (8 * (j % 4)))) != 0;
+  }
+  __device__ __forceinline__ bool any() const { return N == 4 ? w[0] != 0 : (w[0] | w[N / 4 - 1]) != 0; }
+  __device__ __forceinline__ int count() const {
+    int c = 0;
+#pragma unroll
+    for (int k = 0; k < N / 4; ++k)
+      c += __popc((w[k] | ((w[k] & 0x7f7f7f7fu) + 0x7f7f7f7fu)) & 0x80808080u);
+    return c;
+  }
+};
+
+template <int N, bool kVec>
+__device__ __forceinline__ int token_of(int t0, int j) {
+  const int lane = threadIdx.x & 31;
+  return kVec ? t0 + N * lane + j : t0 + lane + 32 * j;
+}
+// Whether all of a lane's tokens lie before T, and in one vector.
+template <int N, bool kVec>
+__device__ __forceinline__ bool whole(int t0, int T) {
+  return kVec && token_of<N, kVec>(t0, N - 1) < T;
 }
 
-// Which of a lane's tokens are valid: bit j.
-template <bool kVec>
-__device__ __forceinline__ uint32_t valid_tokens(const uint8_t* mask, int64_t t0, int64_t T,
-                                                 int lane) {
-  uint32_t on = 0;
-  if (kVec && token_of<kVec>(t0, lane, 3) < T) {
-    if (mask == nullptr) return 15u;
-    const uchar4 m = *reinterpret_cast<const uchar4*>(mask + t0 + 4 * lane);
-    return (m.x != 0 ? 1u : 0u) | (m.y != 0 ? 2u : 0u) | (m.z != 0 ? 4u : 0u) |
-           (m.w != 0 ? 8u : 0u);
+template <int N, bool kVec>
+__device__ __forceinline__ Mask<N> load_mask(const uint8_t* mask, int t0, int T) {
+  Mask<N> m;
+  if (whole<N, kVec>(t0, T)) {
+    if (mask == nullptr) {
+#pragma unroll
+      for (int k = 0; k < N / 4; ++k) m.w[k] = 0x01010101u;
+    } else if constexpr (N == 8) {
+      const uint2 u = *reinterpret_cast<const uint2*>(mask + token_of<N, kVec>(t0, 0));
+      m.w[0] = u.x;
+      m.w[1] = u.y;
+    } else {
+      m.w[0] = *reinterpret_cast<const uint32_t*>(mask + token_of<N, kVec>(t0, 0));
+    }
+    return m;
   }
 #pragma unroll
-  for (int j = 0; j < 4; ++j) {
-    const int64_t t = token_of<kVec>(t0, lane, j);
-    if (t < T && (mask == nullptr || mask[t] != 0)) on |= 1u << j;
+  for (int k = 0; k < N / 4; ++k) m.w[k] = 0;
+#pragma unroll
+  for (int j = 0; j < N; ++j) {
+    const int t = token_of<N, kVec>(t0, j);
+    if (t >= 0 && t < T)
+      m.w[j / 4] |= (mask == nullptr ? 1u : static_cast<uint32_t>(mask[t])) << (8 * (j % 4));
   }
-  return on;
+  return m;
 }
 
-// The values of the tokens in `on` (0 for the others).
-template <bool kVec>
-__device__ __forceinline__ void load_tokens(const float* row, int64_t t0, int64_t T, int lane,
-                                            uint32_t on, float (&x)[4]) {
-  if (kVec && token_of<kVec>(t0, lane, 3) < T) {
-    float4 f = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-    if (on != 0) f = __ldcs(reinterpret_cast<const float4*>(row + t0 + 4 * lane));
-    x[0] = f.x; x[1] = f.y; x[2] = f.z; x[3] = f.w;
+// The values of the tokens that are on (others: anything).
+template <int N, bool kVec>
+__device__ __forceinline__ void load_tokens(const float* row, int t0, int T, const Mask<N>& m,
+                                            float (&x)[N]) {
+  if (whole<N, kVec>(t0, T)) {
+    if (!m.any()) return;
+    const float* at = row + token_of<N, kVec>(t0, 0);
+    if constexpr (N == 8) {
+      uint32_t r[8];
+      load32(at, r);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) x[j] = __uint_as_float(r[j]);
+    } else {
+      const float4 f = __ldcs(reinterpret_cast<const float4*>(at));
+      x[0] = f.x; x[1] = f.y; x[2] = f.z; x[3] = f.w;
+    }
     return;
   }
 #pragma unroll
-  for (int j = 0; j < 4; ++j)
-    x[j] = (on >> j & 1u) != 0 ? __ldcs(row + token_of<kVec>(t0, lane, j)) : 0.0f;
+  for (int j = 0; j < N; ++j)
+    if (m.on(j)) x[j] = __ldcs(row + token_of<N, kVec>(t0, j));
 }
 
-template <bool kVec>
-__device__ __forceinline__ void store_tokens(float* row, int64_t t0, int64_t T, int lane,
-                                             const float (&x)[4]) {
-  if (kVec && token_of<kVec>(t0, lane, 3) < T) {
-    __stcs(reinterpret_cast<float4*>(row + t0 + 4 * lane), make_float4(x[0], x[1], x[2], x[3]));
+template <int N, bool kVec>
+__device__ __forceinline__ void store_tokens(float* row, int t0, int T, const float (&x)[N]) {
+  if (whole<N, kVec>(t0, T)) {
+    float* at = row + token_of<N, kVec>(t0, 0);
+    if constexpr (N == 8) {
+      uint32_t r[8];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) r[j] = __float_as_uint(x[j]);
+      store32(at, r);
+    } else {
+      __stcs(reinterpret_cast<float4*>(at), make_float4(x[0], x[1], x[2], x[3]));
+    }
     return;
   }
 #pragma unroll
-  for (int j = 0; j < 4; ++j) {
-    const int64_t t = token_of<kVec>(t0, lane, j);
-    if (t < T) __stcs(row + t, x[j]);
+  for (int j = 0; j < N; ++j) {
+    const int t = token_of<N, kVec>(t0, j);
+    if (t >= 0 && t < T) __stcs(row + t, x[j]);
   }
 }
 
@@ -102,10 +149,11 @@ __device__ __forceinline__ unsigned count_bytes(const uint8_t* p, int64_t n) {
 
 // ---------------------------------------------------------------- policy
 
-constexpr int kSegment = 512;                  // tokens of a row a warp takes
+constexpr int kSegment = 1024;                 // tokens of a row a warp takes
 constexpr int kCountSegment = 4096;            // mask bytes a warp counts at once
 constexpr int kCountCtas = 304;
-constexpr int kPolicyCtas = 152 * 4;
+constexpr int kPolicyPerSm = 4;                // CTAs of the policy kernel an SM holds
+constexpr int kPolicyCtas = 152 * kPolicyPerSm;
 constexpr int kFinishCtas = 152;
 constexpr int kSmallItems = 512;               // (row, segment) items of the one-launch form
 constexpr int64_t kSmallTokens = 1 << 15;      // ... and its tokens: each CTA counts them all
@@ -139,7 +187,6 @@ struct PolicyParams {
   unsigned* ticket;
   float low, high, kl, ent;
   float norm;                  // 1 / (B norm_tokens) (SUM_NORM)
-  int vec;
 };
 
 __global__ void __launch_bounds__(kThreads) policy_count_kernel(const PolicyParams p) {
@@ -203,36 +250,34 @@ __device__ __forceinline__ float counted_weight(const PolicyParams& p, unsigned 
 
 // A warp takes a segment of row b with token weight w; the segment's sums are in every lane.
 template <bool kVec>
-__device__ __forceinline__ float4 policy_segment(const PolicyParams& p, int64_t b, int64_t seg,
+__device__ __forceinline__ float4 policy_segment(const PolicyParams& p, int64_t b, int seg,
                                                  float w) {
-  const int lane = threadIdx.x & 31;
-  const int64_t T = p.a.T;
+  const int T = static_cast<int>(p.a.T);
   const uint8_t* mask = p.a.mask == nullptr ? nullptr : p.a.mask + b * p.a.ld_mask;
   const bool by_token = p.a.ld_adv != 0;
   const float adv_row = by_token ? 0.0f : p.a.advantages[b];
-  constexpr int kSteps = kSegment / 128;
-  uint32_t on[kSteps];
-#pragma unroll
-  for (int k = 0; k < kSteps; ++k)
-    on[k] = valid_tokens<kVec>(mask, seg * kSegment + 128 * k, T, lane);
+  const float minus_we = -w * p.ent;
   float loss = 0.0f, kls = 0.0f;
   int clipped = 0, valid = 0;
-#pragma unroll
-  for (int k = 0; k < kSteps; ++k) {
-    const int64_t t0 = seg * kSegment + 128 * k;
-    if (t0 >= T) break;
+  int t0 = seg * kSegment;
+  Mask<4> next = load_mask<4, kVec>(mask, t0, T);
+#pragma unroll 1
+  for (int left = min(T - t0, kSegment); left > 0; left -= 128, t0 += 128) {
+    const Mask<4> m = next;
+    if (left > 128) next = load_mask<4, kVec>(mask, t0 + 128, T);
     float lp[4], old[4], adv[4], ref[4], ent[4], d[4], dh[4];
-    load_tokens<kVec>(p.a.logp + b * p.a.ld_logp, t0, T, lane, on[k], lp);
-    load_tokens<kVec>(p.a.old_logp + b * p.a.ld_old, t0, T, lane, on[k], old);
+    load_tokens<4, kVec>(p.a.logp + b * p.a.ld_logp, t0, T, m, lp);
+    load_tokens<4, kVec>(p.a.old_logp + b * p.a.ld_old, t0, T, m, old);
     if (p.a.ref_logp != nullptr)
-      load_tokens<kVec>(p.a.ref_logp + b * p.a.ld_ref, t0, T, lane, on[k], ref);
+      load_tokens<4, kVec>(p.a.ref_logp + b * p.a.ld_ref, t0, T, m, ref);
     if (p.a.entropy != nullptr)
-      load_tokens<kVec>(p.a.entropy + b * p.a.ld_entropy, t0, T, lane, on[k], ent);
-    if (by_token) load_tokens<kVec>(p.a.advantages + b * p.a.ld_adv, t0, T, lane, on[k], adv);
+      load_tokens<4, kVec>(p.a.entropy + b * p.a.ld_entropy, t0, T, m, ent);
+    if (by_token) load_tokens<4, kVec>(p.a.advantages + b * p.a.ld_adv, t0, T, m, adv);
+    valid += m.count();
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
       d[j] = dh[j] = 0.0f;
-      if ((on[k] >> j & 1u) == 0) continue;
+      if (!m.on(j)) continue;
       const float a = by_token ? adv[j] : adv_row;
       const float ratio = expf(lp[j] - old[j]);
       const float free = ratio * a;
@@ -250,13 +295,12 @@ __device__ __forceinline__ float4 policy_segment(const PolicyParams& p, int64_t 
       if (p.a.entropy != nullptr) l = fmaf(-p.ent, ent[j], l);
       loss += l;
       clipped += clip ? 1 : 0;
-      valid += 1;
       d[j] = w * grad;
-      dh[j] = -w * p.ent;
+      dh[j] = minus_we;
     }
-    store_tokens<kVec>(p.a.d_logp + b * p.a.ld_d, t0, T, lane, d);
+    store_tokens<4, kVec>(p.a.d_logp + b * p.a.ld_d, t0, T, d);
     if (p.a.d_entropy != nullptr)
-      store_tokens<kVec>(p.a.d_entropy + b * p.a.ld_de, t0, T, lane, dh);
+      store_tokens<4, kVec>(p.a.d_entropy + b * p.a.ld_de, t0, T, dh);
   }
   return make_float4(warp_sum(loss), warp_sum(kls),
                      static_cast<float>(__reduce_add_sync(0xffffffffu, clipped)),
@@ -287,7 +331,7 @@ __device__ __forceinline__ Totals row_totals(int64_t segments, F part) {
 }
 
 template <bool kVec>
-__global__ void __launch_bounds__(kThreads) policy_kernel(const PolicyParams p) {
+__global__ void __launch_bounds__(kThreads, kPolicyPerSm) policy_kernel(const PolicyParams p) {
   const int64_t items = p.a.B * p.segments;
   const int64_t warps = static_cast<int64_t>(gridDim.x) * kWarps;
   int64_t item = static_cast<int64_t>(blockIdx.x) * kWarps + (threadIdx.x >> 5);
@@ -297,7 +341,8 @@ __global__ void __launch_bounds__(kThreads) policy_kernel(const PolicyParams p) 
   const unsigned long long batch = counted_batch(p);
   for (; item < items; item += warps) {
     const int64_t b = item / p.segments;
-    const float4 s = policy_segment<kVec>(p, b, item - b * p.segments, counted_weight(p, batch, b));
+    const float4 s = policy_segment<kVec>(p, b, static_cast<int>(item - b * p.segments),
+                                          counted_weight(p, batch, b));
     if ((threadIdx.x & 31) == 0) p.sums[item] = s;
   }
 }
@@ -400,9 +445,14 @@ __global__ void __launch_bounds__(kThreads) policy_small_kernel(const PolicyPara
 
 // ------------------------------------------------------------ preference
 
+constexpr int kPairThreads = 256;
+constexpr int kPairWarps = kPairThreads / 32;
+constexpr int kPairPerSm = 5, kPairPerSmRef = 4;
+constexpr int kPairCtas = 2;                   // CTAs an SM up to which a pair is split,
+constexpr int64_t kPairTokens = 2048;          // into shares of more than half of this
+
 struct PreferenceParams {
   bergson_preference_args a;
-  int vec;
 };
 
 // f(x) and its slope.
@@ -423,61 +473,74 @@ __device__ __forceinline__ void preference_f(int kind, float x, float beta, floa
   }
 }
 
-// A CTA's sums over its share [t0, t1) of a row (both multiples of 128, but for T).
-template <bool kVec>
-__device__ __forceinline__ void row_sums(const PreferenceParams& p, int64_t r, int64_t t0,
-                                         int64_t t1, Sum2* red, unsigned* counts, Sum2* sum,
-                                         unsigned* count) {
-  const int lane = threadIdx.x & 31;
-  const uint8_t* mask = p.a.mask == nullptr ? nullptr : p.a.mask + r * p.a.ld_mask;
-  const float* x = p.a.logp + r * p.a.ld_logp;
-  const float* ref = p.a.ref_logp == nullptr ? nullptr : p.a.ref_logp + r * p.a.ld_ref;
-  constexpr int kSteps = 4;
-  Sum2 s;
-  unsigned n = 0;
-  for (int64_t t = t0 + 128 * (threadIdx.x >> 5); t < t1; t += kSteps * 128 * kWarps) {
-    uint32_t on[kSteps];
-    float v[kSteps][4], u[kSteps][4];
+// A CTA's sums over its share [t0, t1) of a pair's rows (both multiples of 256, but for T).
+template <int N, bool kVec, bool kRef>
+__device__ __forceinline__ void pair_sums(const PreferenceParams& p, int64_t pair, int t0, int t1,
+                                          Sum2 (*red)[2], int (*counts)[2], Sum2* sum, int* count) {
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  constexpr int kStride = 32 * N * kPairWarps;
+  const uint8_t* mask[2];
+  const float* x[2];
+  const float* ref[2];
+  Sum2 s[2];
+  int n[2] = {0, 0};
 #pragma unroll
-    for (int k = 0; k < kSteps; ++k) {
-      const int64_t tk = t + 128 * kWarps * k;
-      on[k] = tk < t1 ? valid_tokens<kVec>(mask, tk, t1, lane) : 0u;
-    }
-#pragma unroll
-    for (int k = 0; k < kSteps; ++k)
-      load_tokens<kVec>(x, t + 128 * kWarps * k, t1, lane, on[k], v[k]);
-    if (ref != nullptr) {
-#pragma unroll
-      for (int k = 0; k < kSteps; ++k)
-        load_tokens<kVec>(ref, t + 128 * kWarps * k, t1, lane, on[k], u[k]);
-    }
-    float f = 0.0f;
-#pragma unroll
-    for (int k = 0; k < kSteps; ++k) {
-      n += __popc(on[k]);
-#pragma unroll
-      for (int j = 0; j < 4; ++j)
-        if ((on[k] >> j & 1u) != 0) f += ref != nullptr ? v[k][j] - u[k][j] : v[k][j];
-    }
-    s.add(f);
+  for (int k = 0; k < 2; ++k) {
+    const int64_t r = pair + k * p.a.P;
+    mask[k] = p.a.mask == nullptr ? nullptr : p.a.mask + r * p.a.ld_mask;
+    x[k] = p.a.logp + r * p.a.ld_logp;
+    ref[k] = kRef ? p.a.ref_logp + r * p.a.ld_ref : nullptr;
   }
-  s = warp_sum(s);
-  n = __reduce_add_sync(0xffffffffu, n);
-  if (lane == 0) {
-    red[threadIdx.x >> 5] = s;
-    counts[threadIdx.x >> 5] = n;
+  int t = t0 + 32 * N * warp, left = t1 - t;
+  Mask<N> next[2];
+  if (left > 0) {
+    next[0] = load_mask<N, kVec>(mask[0], t, t1);
+    next[1] = load_mask<N, kVec>(mask[1], t, t1);
+  }
+#pragma unroll 1
+  for (; left > 0; left -= kStride, t += kStride) {
+    float v[2][N], u[2][N];
+    const Mask<N> m[2] = {next[0], next[1]};
+    load_tokens<N, kVec>(x[0], t, t1, m[0], v[0]);
+    load_tokens<N, kVec>(x[1], t, t1, m[1], v[1]);
+    if (kRef) {
+      load_tokens<N, kVec>(ref[0], t, t1, m[0], u[0]);
+      load_tokens<N, kVec>(ref[1], t, t1, m[1], u[1]);
+    }
+    if (left > kStride) {
+      next[0] = load_mask<N, kVec>(mask[0], t + kStride, t1);
+      next[1] = load_mask<N, kVec>(mask[1], t + kStride, t1);
+    }
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+      float f = 0.0f;
+#pragma unroll
+      for (int j = 0; j < N; ++j)
+        if (m[k].on(j)) f += kRef ? v[k][j] - u[k][j] : v[k][j];
+      n[k] += m[k].count();
+      s[k].add(f);
+    }
+  }
+#pragma unroll
+  for (int k = 0; k < 2; ++k) {
+    s[k] = warp_sum(s[k]);
+    n[k] = __reduce_add_sync(0xffffffffu, n[k]);
+    if (lane == 0) {
+      red[warp][k] = s[k];
+      counts[warp][k] = n[k];
+    }
   }
   __syncthreads();
-  s = red[0];
-  n = counts[0];
 #pragma unroll
-  for (int w = 1; w < kWarps; ++w) {
-    s.add(red[w]);
-    n += counts[w];
+  for (int k = 0; k < 2; ++k) {
+    sum[k] = red[0][k];
+    count[k] = counts[0][k];
+#pragma unroll
+    for (int w = 1; w < kPairWarps; ++w) {
+      sum[k].add(red[w][k]);
+      count[k] += counts[w][k];
+    }
   }
-  __syncthreads();
-  *sum = s;
-  *count = n;
 }
 
 // What follows from a pair's sums, in every thread.
@@ -486,7 +549,7 @@ struct PairGrad {
 };
 
 __device__ __forceinline__ PairGrad pair_grad(const bergson_preference_args& a, const Sum2* sum,
-                                              const unsigned* count) {
+                                              const int* count) {
   const float beta = static_cast<float>(a.beta), eps = static_cast<float>(a.label_smoothing);
   float n[2], s[2], gap;
   for (int k = 0; k < 2; ++k) {
@@ -511,43 +574,51 @@ __device__ __forceinline__ PairGrad pair_grad(const bergson_preference_args& a, 
   return o;
 }
 
-template <bool kVec>
-__device__ __forceinline__ void write_row(const PreferenceParams& p, int64_t r, int64_t t0,
-                                          int64_t t1, float d) {
-  const int lane = threadIdx.x & 31;
-  const uint8_t* mask = p.a.mask == nullptr ? nullptr : p.a.mask + r * p.a.ld_mask;
-  float* out = p.a.d_logp + r * p.a.ld_d;
-#pragma unroll 4
-  for (int64_t t = t0 + 128 * (threadIdx.x >> 5); t < t1; t += 128 * kWarps) {
-    const uint32_t on = valid_tokens<kVec>(mask, t, t1, lane);
-    float x[4];
+template <int N, bool kVec>
+__device__ __forceinline__ void write_pair(const PreferenceParams& p, int64_t pair, int t0, int t1,
+                                           const float* d) {
+  const int warp = threadIdx.x >> 5;
+  constexpr int kStride = 32 * N * kPairWarps;
+  const uint8_t* mask[2];
+  float* out[2];
 #pragma unroll
-    for (int j = 0; j < 4; ++j) x[j] = (on >> j & 1u) != 0 ? d : 0.0f;
-    store_tokens<kVec>(out, t, t1, lane, x);
+  for (int k = 0; k < 2; ++k) {
+    const int64_t r = pair + k * p.a.P;
+    mask[k] = p.a.mask == nullptr ? nullptr : p.a.mask + r * p.a.ld_mask;
+    out[k] = p.a.d_logp + r * p.a.ld_d;
+  }
+  int t = t0 + 32 * N * warp;
+#pragma unroll 2
+  for (int left = t1 - t; left > 0; left -= kStride, t += kStride) {
+    const Mask<N> m[2] = {load_mask<N, kVec>(mask[0], t, t1), load_mask<N, kVec>(mask[1], t, t1)};
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+      float x[N];
+#pragma unroll
+      for (int j = 0; j < N; ++j) x[j] = m[k].on(j) ? d[k] : 0.0f;
+      store_tokens<N, kVec>(out[k], t, t1, x);
+    }
   }
 }
 
 // kTogether: a pair a CTA, all of them in one cluster, whose first CTA adds the losses.
 // Else a pair a cluster, its CTAs each a share of the tokens.
-template <bool kVec, bool kTogether>
-__global__ void __launch_bounds__(kThreads) preference_kernel(const PreferenceParams p) {
-  __shared__ Sum2 red[kWarps];
-  __shared__ unsigned counts[kWarps];
+template <int N, bool kVec, bool kRef, bool kTogether>
+__global__ void __launch_bounds__(kPairThreads, kRef ? kPairPerSmRef : kPairPerSm) preference_kernel(const PreferenceParams p) {
+  __shared__ Sum2 red[kPairWarps][2];
+  __shared__ int counts[kPairWarps][2];
   __shared__ float shared[8][6];               // from each CTA: two sums and counts
   const int parts = static_cast<int>(cluster_size());
   const int rank = static_cast<int>(blockIdx.x) % parts;
   const int64_t pair = kTogether ? blockIdx.x : blockIdx.x / parts;
   const bool live = pair < p.a.P;
-  const int64_t blocks = (p.a.T + 127) / 128;
-  const int64_t per = kTogether ? blocks : (blocks + parts - 1) / parts;
-  const int64_t t0 = kTogether ? 0 : min(p.a.T, per * rank * 128);
-  const int64_t t1 = min(p.a.T, t0 + per * 128);
+  const int T = static_cast<int>(p.a.T), blocks = (T - 1) / 256 + 1;
+  const int per = kTogether ? blocks : (blocks + parts - 1) / parts;
+  const int t0 = kTogether ? 0 : static_cast<int>(min(static_cast<int64_t>(T), int64_t{256} * per * rank));
+  const int t1 = static_cast<int>(min(static_cast<int64_t>(T), t0 + int64_t{256} * per));
   Sum2 sum[2];
-  unsigned count[2] = {};
-  if (live) {
-    for (int k = 0; k < 2; ++k)
-      row_sums<kVec>(p, pair + k * p.a.P, t0, t1, red, counts, &sum[k], &count[k]);
-  }
+  int count[2] = {};
+  if (live) pair_sums<N, kVec, kRef>(p, pair, t0, t1, red, counts, sum, count);
   if (!kTogether && parts > 1) {
     cluster_sync();                            // every CTA has started
     if (threadIdx.x < parts) {
@@ -555,7 +626,7 @@ __global__ void __launch_bounds__(kThreads) preference_kernel(const PreferencePa
       for (int k = 0; k < 2; ++k) {
         st_cluster(&shared[rank][3 * k], threadIdx.x, sum[k].hi);
         st_cluster(&shared[rank][3 * k + 1], threadIdx.x, sum[k].lo);
-        st_cluster(&shared[rank][3 * k + 2], threadIdx.x, __uint_as_float(count[k]));
+        st_cluster(&shared[rank][3 * k + 2], threadIdx.x, __int_as_float(count[k]));
       }
     }
     cluster_sync();
@@ -567,7 +638,7 @@ __global__ void __launch_bounds__(kThreads) preference_kernel(const PreferencePa
         o.hi = shared[c][3 * k];
         o.lo = shared[c][3 * k + 1];
         sum[k].add(o);
-        count[k] += __float_as_uint(shared[c][3 * k + 2]);
+        count[k] += __float_as_int(shared[c][3 * k + 2]);
       }
     }
   }
@@ -594,9 +665,7 @@ __global__ void __launch_bounds__(kThreads) preference_kernel(const PreferencePa
   } else {
     griddep_launch_dependents();
   }
-  if (live) {
-    for (int k = 0; k < 2; ++k) write_row<kVec>(p, pair + k * p.a.P, t0, t1, g.d[k]);
-  }
+  if (live) write_pair<N, kVec>(p, pair, t0, t1, g.d);
 }
 
 __global__ void __launch_bounds__(1024) preference_finish_kernel(const float* pair_loss,
@@ -618,16 +687,17 @@ size_t counts_bytes(int64_t B, int64_t T) {
   return align256(4 * static_cast<size_t>(std::max<int64_t>(kCountCtas, B * ceil_div(T, kCountSegment))));
 }
 
-// Rows whose 16-byte loads of four tokens are aligned.
-bool fits(const void* p, int64_t ld, size_t elem) {
-  return p == nullptr || (reinterpret_cast<uintptr_t>(p) % (4 * elem) == 0 && ld % 4 == 0);
+// Rows whose loads of n tokens at once are aligned.
+bool fits(const void* p, int64_t ld, size_t elem, int n) {
+  return p == nullptr || (reinterpret_cast<uintptr_t>(p) % (n * elem) == 0 && ld % n == 0);
 }
 
 template <typename K, typename P>
-cudaError_t launch_cluster(K kernel, int64_t grid, int cluster, const P& p, cudaStream_t s) {
+cudaError_t launch_cluster(K kernel, int64_t grid, int threads, int cluster, const P& p,
+                           cudaStream_t s) {
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(static_cast<unsigned>(grid));
-  cfg.blockDim = dim3(kThreads);
+  cfg.blockDim = dim3(threads);
   cfg.stream = s;
   cudaLaunchAttribute attr[1];
   attr[0].id = cudaLaunchAttributeClusterDimension;
@@ -644,7 +714,7 @@ cudaError_t run_policy(PolicyParams p, cudaStream_t s) {
   if (items <= kSmallItems && p.a.B <= kSmallItems && p.a.B * p.a.T <= kSmallTokens) {
     int parts = 1;
     while (parts < 8 && parts * kWarps < items) parts *= 2;
-    return launch_cluster(policy_small_kernel<kVec>, parts, parts, p, s);
+    return launch_cluster(policy_small_kernel<kVec>, parts, kThreads, parts, p, s);
   }
   if (p.a.mask != nullptr && p.a.reduction != BERGSON_POLICY_SUM_NORM) {
     p.n_counts = static_cast<int>(
@@ -663,20 +733,26 @@ cudaError_t run_policy(PolicyParams p, cudaStream_t s) {
                           dim3(kThreads), 0, s, p);
 }
 
-template <bool kVec>
+template <int N, bool kVec, bool kRef>
 cudaError_t run_preference(const PreferenceParams& p, int sms, cudaStream_t s) {
   const int64_t P = p.a.P;
   if (P <= 8 && 2 * p.a.T <= 8192) {
     int n = 1;
     while (n < P) n *= 2;
-    return launch_cluster(preference_kernel<kVec, true>, n, n, p, s);
+    return launch_cluster(preference_kernel<N, kVec, kRef, true>, n, kPairThreads, n, p, s);
   }
   int parts = 1;
-  while (parts < 8 && P * parts < 2 * sms && p.a.T / parts > 2048) parts *= 2;
-  cudaError_t e = launch_cluster(preference_kernel<kVec, false>, P * parts, parts, p, s);
+  while (parts < 8 && P * parts < kPairCtas * sms && p.a.T / parts > kPairTokens) parts *= 2;
+  cudaError_t e = launch_cluster(preference_kernel<N, kVec, kRef, false>, P * parts, kPairThreads, parts, p, s);
   if (e != cudaSuccess) return e;
   return launch_dependent(preference_finish_kernel, dim3(1), dim3(1024), 0, s,
                           static_cast<const float*>(p.a.pair_loss), P, p.a.loss);
+}
+
+template <int N, bool kVec>
+cudaError_t run_preference(const PreferenceParams& p, int sms, cudaStream_t s) {
+  return p.a.ref_logp != nullptr ? run_preference<N, kVec, true>(p, sms, s)
+                                 : run_preference<N, kVec, false>(p, sms, s);
 }
 
 }  // namespace
@@ -715,11 +791,12 @@ cudaError_t launch_policy_loss(const bergson_policy_args& a, void* ws, cudaStrea
       e = cudaMemsetAsync(a.seq_loss, 0, sizeof(float) * static_cast<size_t>(a.B), s);
     return e;
   }
-  p.vec = fits(a.logp, a.ld_logp, 4) && fits(a.old_logp, a.ld_old, 4) &&
-          fits(p.a.ref_logp, a.ld_ref, 4) && fits(p.a.entropy, a.ld_entropy, 4) &&
-          (a.ld_adv == 0 || fits(a.advantages, a.ld_adv, 4)) && fits(a.mask, a.ld_mask, 1) &&
-          fits(a.d_logp, a.ld_d, 4) && fits(a.d_entropy, a.ld_de, 4);
-  return p.vec ? run_policy<true>(p, s) : run_policy<false>(p, s);
+  const bool vec = fits(a.logp, a.ld_logp, 4, 4) && fits(a.old_logp, a.ld_old, 4, 4) &&
+                   fits(p.a.ref_logp, a.ld_ref, 4, 4) && fits(p.a.entropy, a.ld_entropy, 4, 4) &&
+                   (a.ld_adv == 0 || fits(a.advantages, a.ld_adv, 4, 4)) &&
+                   fits(a.mask, a.ld_mask, 1, 4) && fits(a.d_logp, a.ld_d, 4, 4) &&
+                   fits(a.d_entropy, a.ld_de, 4, 4);
+  return vec ? run_policy<true>(p, s) : run_policy<false>(p, s);
 }
 
 cudaError_t launch_preference_loss(const bergson_preference_args& a, int sms, cudaStream_t s) {
@@ -729,9 +806,12 @@ cudaError_t launch_preference_loss(const bergson_preference_args& a, int sms, cu
   }
   PreferenceParams p;
   p.a = a;
-  p.vec = fits(a.logp, a.ld_logp, 4) && fits(a.ref_logp, a.ld_ref, 4) &&
-          fits(a.mask, a.ld_mask, 1) && fits(a.d_logp, a.ld_d, 4);
-  return p.vec ? run_preference<true>(p, sms, s) : run_preference<false>(p, sms, s);
+  const auto all_fit = [&](int n) {
+    return fits(a.logp, a.ld_logp, 4, n) && fits(a.ref_logp, a.ld_ref, 4, n) &&
+           fits(a.mask, a.ld_mask, 1, n) && fits(a.d_logp, a.ld_d, 4, n);
+  };
+  if (all_fit(8)) return run_preference<8, true>(p, sms, s);
+  return all_fit(4) ? run_preference<4, true>(p, sms, s) : run_preference<4, false>(p, sms, s);
 }
 
 }  // namespace bergson

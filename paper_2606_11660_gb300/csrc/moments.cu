@@ -10,7 +10,9 @@ namespace {
 
 constexpr int kThreads = 256;
 constexpr int kWarps = kThreads / 32;
-constexpr int kWarpRows = 16;                  // rows a warp takes
+constexpr int kWarpRows = 32;                  // rows a warp takes
+constexpr int kRows = 4;                       // of them on the way at once
+constexpr int kTileCtas = 3;
 constexpr int kBand = kWarps * kWarpRows;      // rows of a tile
 constexpr int kStrip = 256;                    // columns of a tile, 8 a lane
 constexpr int kFew = 24, kMany = 300;          // records a launch can take
@@ -72,7 +74,6 @@ __device__ __forceinline__ float sum_each(float (&x)[N]) {
 template <bool kEight, bool kVec>
 __device__ __forceinline__ void take_rows(const Entry& e, int64_t r0, int64_t c0, float* row_part,
                                           float (&col)[8]) {
-  constexpr int kRows = 8;                     // on the way at once
   const int lane = threadIdx.x & 31;
   float2 col2[4] = {};
 #pragma unroll 1
@@ -163,7 +164,7 @@ __device__ __forceinline__ void take_rows(const Entry& e, int64_t r0, int64_t c0
 }
 
 template <int N>
-__global__ void __launch_bounds__(kThreads) moment_tiles_kernel(
+__global__ void __launch_bounds__(kThreads, kTileCtas) moment_tiles_kernel(
     const __grid_constant__ MomentParams<N> p) {
   __shared__ float cols[kWarps][kStrip];
   __shared__ float red[kWarps];

@@ -73,11 +73,13 @@ int check_logits(const void* logits, int dtype, int64_t rows, int64_t V, int64_t
   } while (0)
 
 constexpr int64_t kMaxLossTokens = 1ll << 40;
+constexpr int64_t kMaxRowTokens = 1ll << 30;   // the kernels' places within a row are 32-bit
 
 int check_policy_sizes(int64_t B, int64_t T) {
   if (B < 0 || B > INT32_MAX || T < 0 || T > INT32_MAX)
     return fail(BERGSON_EINVAL, "B and T must be in [0, 2^31)");
-  if (B * T > kMaxLossTokens) return fail(BERGSON_EUNSUPPORTED, "B*T too large");
+  if (T > kMaxRowTokens || B * T > kMaxLossTokens)
+    return fail(BERGSON_EUNSUPPORTED, "T or B*T too large");
   return BERGSON_OK;
 }
 
@@ -201,7 +203,8 @@ int bergson_preference_loss(const bergson_preference_args* args, void* stream) {
   const bergson_preference_args& a = *args;
   if (a.P < 0 || a.P >= (1ll << 30) || a.T < 0 || a.T > INT32_MAX)
     return fail(BERGSON_EINVAL, "P must be in [0, 2^30) and T in [0, 2^31)");
-  if (2 * a.P * a.T > kMaxLossTokens) return fail(BERGSON_EUNSUPPORTED, "2*P*T too large");
+  if (a.T > kMaxRowTokens || 2 * a.P * a.T > kMaxLossTokens)
+    return fail(BERGSON_EUNSUPPORTED, "T or 2*P*T too large");
   if (a.kind != BERGSON_PREFERENCE_SIGMOID && a.kind != BERGSON_PREFERENCE_HINGE &&
       a.kind != BERGSON_PREFERENCE_SQUARED)
     return fail(BERGSON_EINVAL, "unknown kind %d", a.kind);
