@@ -757,7 +757,7 @@ BERGSON_API int bergson_token_logprobs_backward(const void* logits, int dtype, i
  *             (ratio A > clamped A), number of valid tokens.
  *   d_logp    fp32 [B, ld_d];  d_entropy  fp32 [B, ld_de] or NULL.
  *   workspace 256-byte aligned, contents on entry ignored.
- * Leading dimensions are >= T.  B, T >= 0, T <= 2^30, B * T <= 2^40.  Sums run in fp32 within 512
+ * Leading dimensions are >= T.  B, T >= 0, T <= 2^30, B * T <= 2^40.  Sums run in fp32 within 1024
  * tokens and in twice its bits above, in an order fixed by the sizes.
  * Errors: EINVAL, EALIGN, EUNSUPPORTED, EWORKSPACE, ECUDA.
  */

@@ -277,6 +277,7 @@ __global__ void __launch_bounds__(kThreads) adamw_kernel(const __grid_constant__
     if (p.begin[mid] <= blockIdx.x) lo = mid; else hi = mid;
   }
   const Entry& e = p.e[lo];
+  griddep_wait();
   const float gs = p.s.grad_scale != nullptr ? *p.s.grad_scale : 1.0f;
   const int64_t first =
       (static_cast<int64_t>(blockIdx.x - p.begin[lo]) * kWarps + (threadIdx.x >> 5)) * kStateBlock;
@@ -291,6 +292,7 @@ __global__ void __launch_bounds__(kThreads) state_values_kernel(
     const uint8_t* __restrict__ codes, const float* __restrict__ scale, int64_t n, int moment,
     int vec, float* __restrict__ out) {
   const int64_t i = 8 * (static_cast<int64_t>(blockIdx.x) * kThreads + threadIdx.x);
+  griddep_wait();
   if (i >= n) return;
   const float sc = scale[i / kStateBlock];
   if (vec && i + 8 <= n) {
@@ -344,9 +346,9 @@ cudaError_t run_adamw(const bergson_adamw_tensor* t, int n, const AdamwScalars& 
   const auto flush = [&]() -> cudaError_t {
     if (k == 0) return cudaSuccess;
     p.s.n = k;
-    adamw_kernel<N><<<p.begin[k], kThreads, 0, s>>>(p);
+    const dim3 grid(p.begin[k]);
     k = 0;
-    return cudaGetLastError();
+    return launch_dependent(adamw_kernel<N>, grid, dim3(kThreads), 0, s, p);
   };
   for (int i = 0; i < n; ++i) {
     if (t[i].n == 0) continue;
@@ -387,9 +389,8 @@ cudaError_t launch_adamw(const bergson_adamw_tensor* t, int n, const AdamwScalar
 cudaError_t launch_state_values(const uint8_t* codes, const float* scale, int64_t n, int moment,
                                 float* out, cudaStream_t s) {
   const int64_t grid = (n + 8 * kThreads - 1) / (8 * kThreads);
-  state_values_kernel<<<static_cast<unsigned>(grid), kThreads, 0, s>>>(
-      codes, scale, n, moment, on(codes, 8) && on(out, 32) ? 1 : 0, out);
-  return cudaGetLastError();
+  return launch_dependent(state_values_kernel, dim3(static_cast<unsigned>(grid)), dim3(kThreads),
+                          0, s, codes, scale, n, moment, on(codes, 8) && on(out, 32) ? 1 : 0, out);
 }
 
 }  // namespace bergson

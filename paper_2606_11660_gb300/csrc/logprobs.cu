@@ -231,13 +231,15 @@ __global__ void __launch_bounds__(kThreads, kFwdCtas) logprobs_row_kernel(const 
   const int parts = static_cast<int>(cluster_size());
   const int part = static_cast<int>(blockIdx.x) % parts;
   const int64_t r = blockIdx.x / parts;
+  griddep_wait();
   const int64_t t = p.targets[r];
   if (t < 0) {
     if (threadIdx.x == 0 && part == 0) write_left_out(p, r);
     return;
   }
-  RowSums a = scan_row<T, kEntropy>(static_cast<const T*>(p.x) + r * p.ld, p.V, p.c, threadIdx.x,
-                                    kThreads, part, parts);
+  const T* row = static_cast<const T*>(p.x) + r * p.ld;
+  if (parts > 1) cluster_arrive();
+  RowSums a = scan_row<T, kEntropy>(row, p.V, p.c, threadIdx.x, kThreads, part, parts);
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) merge(a, shuffle(a, o), p.c);
   if ((threadIdx.x & 31) == 0) red[threadIdx.x >> 5] = a;
@@ -248,7 +250,7 @@ __global__ void __launch_bounds__(kThreads, kFwdCtas) logprobs_row_kernel(const 
     for (int o = kThreads / 64; o > 0; o >>= 1) merge(a, shuffle(a, o), p.c);
   }
   if (parts > 1) {
-    cluster_sync();                            // the first CTA has started
+    cluster_wait();                            // the first CTA has started
     if (threadIdx.x == 0) {
       st_cluster(&ranks[part].m, 0, a.m);
       st_cluster(&ranks[part].s, 0, a.s);
@@ -267,6 +269,7 @@ __global__ void __launch_bounds__(kThreads, kFwdCtas) logprobs_row_kernel(const 
 // A warp takes a row.
 template <typename T, bool kEntropy>
 __global__ void __launch_bounds__(kThreads, kFwdCtas) logprobs_warp_kernel(const ForwardParams p) {
+  griddep_wait();
   const int64_t r = static_cast<int64_t>(blockIdx.x) * (kThreads / 32) + (threadIdx.x >> 5);
   if (r >= p.rows) return;
   const int lane = threadIdx.x & 31;
@@ -275,7 +278,8 @@ __global__ void __launch_bounds__(kThreads, kFwdCtas) logprobs_warp_kernel(const
     if (lane == 0) write_left_out(p, r);
     return;
   }
-  RowSums a = scan_row<T, kEntropy>(static_cast<const T*>(p.x) + r * p.ld, p.V, p.c, lane, 32, 0, 1);
+  const T* row = static_cast<const T*>(p.x) + r * p.ld;
+  RowSums a = scan_row<T, kEntropy>(row, p.V, p.c, lane, 32, 0, 1);
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) merge(a, shuffle(a, o), p.c);
   if (lane == 0) write_row<T>(p, r, t, a);
@@ -410,12 +414,14 @@ __device__ __forceinline__ void backward_row(const BackwardParams& p, int64_t r,
 
 template <typename T, bool kEntropy>
 __global__ void __launch_bounds__(kThreads, kBwdCtas) logprobs_backward_kernel(const BackwardParams p) {
+  griddep_wait();
   backward_row<T, kEntropy>(p, blockIdx.x / p.slices, threadIdx.x, kThreads,
                             static_cast<int>(blockIdx.x % p.slices));
 }
 
 template <typename T, bool kEntropy>
 __global__ void __launch_bounds__(kThreads, kBwdCtas) logprobs_backward_warp_kernel(const BackwardParams p) {
+  griddep_wait();
   const int64_t r = static_cast<int64_t>(blockIdx.x) * (kThreads / 32) + (threadIdx.x >> 5);
   if (r < p.rows) backward_row<T, kEntropy>(p, r, threadIdx.x & 31, 32, 0);
 }
@@ -434,8 +440,8 @@ cudaError_t run_forward(const LogprobArgs& a, cudaStream_t s) {
   const int64_t bytes = a.V * static_cast<int64_t>(sizeof(T));
   if (bytes <= kWarpRowBytes) {
     const int64_t grid = (a.rows + kThreads / 32 - 1) / (kThreads / 32);
-    logprobs_warp_kernel<T, kEntropy><<<static_cast<unsigned>(grid), kThreads, 0, s>>>(p);
-    return cudaGetLastError();
+    return launch_dependent(logprobs_warp_kernel<T, kEntropy>, dim3(static_cast<unsigned>(grid)),
+                            dim3(kThreads), 0, s, p);
   }
   // Few rows: the CTAs of a cluster share one.
   int parts = 1;
@@ -444,12 +450,14 @@ cudaError_t run_forward(const LogprobArgs& a, cudaStream_t s) {
   cfg.gridDim = dim3(static_cast<unsigned>(a.rows * parts));
   cfg.blockDim = dim3(kThreads);
   cfg.stream = s;
-  cudaLaunchAttribute attr[1];
+  cudaLaunchAttribute attr[2];
   attr[0].id = cudaLaunchAttributeClusterDimension;
   attr[0].val.clusterDim.x = parts;
   attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+  attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[1].val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = attr;
-  cfg.numAttrs = 1;
+  cfg.numAttrs = 2;
   return cudaLaunchKernelEx(&cfg, logprobs_row_kernel<T, kEntropy>, p);
 }
 
@@ -460,14 +468,13 @@ cudaError_t run_backward(const LogprobGradArgs& a, cudaStream_t s) {
   const int64_t bytes = a.V * static_cast<int64_t>(sizeof(T));
   if (bytes <= kWarpRowBytes) {
     const int64_t grid = (a.rows + kThreads / 32 - 1) / (kThreads / 32);
-    logprobs_backward_warp_kernel<T, kEntropy><<<static_cast<unsigned>(grid), kThreads, 0, s>>>(p);
-    return cudaGetLastError();
+    return launch_dependent(logprobs_backward_warp_kernel<T, kEntropy>,
+                            dim3(static_cast<unsigned>(grid)), dim3(kThreads), 0, s, p);
   }
   const int64_t slices = (bytes + kSliceBytes - 1) / kSliceBytes;
   p.slices = static_cast<int>(slices * a.rows < INT32_MAX ? slices : 1);
-  logprobs_backward_kernel<T, kEntropy>
-      <<<static_cast<unsigned>(a.rows * p.slices), kThreads, 0, s>>>(p);
-  return cudaGetLastError();
+  return launch_dependent(logprobs_backward_kernel<T, kEntropy>,
+                          dim3(static_cast<unsigned>(a.rows * p.slices)), dim3(kThreads), 0, s, p);
 }
 
 template <typename T>

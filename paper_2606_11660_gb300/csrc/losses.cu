@@ -132,13 +132,18 @@ __device__ __forceinline__ unsigned count_bytes(const uint8_t* p, int64_t n) {
   const int64_t vecs = (n - head) / 16;
   const uint4* body = reinterpret_cast<const uint4*>(p + head);
   unsigned c = 0;
-#pragma unroll 4
-  for (int64_t i = lane; i < vecs; i += 32) {
-    const uint4 v = body[i];
+  for (int64_t i = lane; i < vecs; i += 4 * 32) {
+    uint4 v[4];
 #pragma unroll
-    for (int k = 0; k < 4; ++k) {
-      const uint32_t w = word(v, k);
-      c += __popc((w | ((w & 0x7f7f7f7fu) + 0x7f7f7f7fu)) & 0x80808080u);
+    for (int j = 0; j < 4; ++j)
+      v[j] = i + 32 * j < vecs ? body[i + 32 * j] : make_uint4(0, 0, 0, 0);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const uint32_t w = word(v[j], k);
+        c += __popc((w | ((w & 0x7f7f7f7fu) + 0x7f7f7f7fu)) & 0x80808080u);
+      }
     }
   }
   const int64_t tail = head + 16 * vecs + lane;
@@ -151,9 +156,8 @@ __device__ __forceinline__ unsigned count_bytes(const uint8_t* p, int64_t n) {
 
 constexpr int kSegment = 1024;                 // tokens of a row a warp takes
 constexpr int kCountSegment = 4096;            // mask bytes a warp counts at once
-constexpr int kCountCtas = 304;
+constexpr int kCountCtas = 1216;
 constexpr int kPolicyPerSm = 4;                // CTAs of the policy kernel an SM holds
-constexpr int kPolicyCtas = 152 * kPolicyPerSm;
 constexpr int kFinishCtas = 152;
 constexpr int kSmallItems = 512;               // (row, segment) items of the one-launch form
 constexpr int64_t kSmallTokens = 1 << 15;      // ... and its tokens: each CTA counts them all
@@ -191,7 +195,7 @@ struct PolicyParams {
 
 __global__ void __launch_bounds__(kThreads) policy_count_kernel(const PolicyParams p) {
   __shared__ unsigned red[kWarps];
-  griddep_launch_dependents();
+  griddep_wait();
   const int64_t items = p.a.B * p.count_segments;
   const int64_t warps = static_cast<int64_t>(gridDim.x) * kWarps;
   unsigned mine = 0;
@@ -209,7 +213,7 @@ __global__ void __launch_bounds__(kThreads) policy_count_kernel(const PolicyPara
   if ((threadIdx.x & 31) == 0) red[threadIdx.x >> 5] = mine;
   __syncthreads();
   if (threadIdx.x == 0) {
-    unsigned c = 0;                            // 2^40 tokens over 304 CTAs fit 32 bits
+    unsigned c = 0;                            // at most 2^40 tokens over 1216 CTAs: 32 bits hold them
     for (int w = 0; w < kWarps; ++w) c += red[w];
     p.counts[blockIdx.x] = c;
   }
@@ -246,6 +250,22 @@ __device__ __forceinline__ unsigned long long counted_row(const PolicyParams& p,
 __device__ __forceinline__ float counted_weight(const PolicyParams& p, unsigned long long batch,
                                                 int64_t b) {
   return weight_of(p, p.a.reduction == BERGSON_POLICY_SEQ_MEAN ? counted_row(p, b) : batch);
+}
+
+// up = exp(g) - 1 and k = up - g.  Below 1/4 by the series of k = g^2 (1/2 + g/6 + ...),
+// where the difference would cancel (six terms: 2^-24 of up); above, exp's few units
+// of error are at most 4e-6 of k.
+__device__ __forceinline__ void kl_of(float g, float* k, float* up) {
+  float s = fmaf(g, 1.0f / 5040.0f, 1.0f / 720.0f);
+  s = fmaf(g, s, 1.0f / 120.0f);
+  s = fmaf(g, s, 1.0f / 24.0f);
+  s = fmaf(g, s, 1.0f / 6.0f);
+  s = fmaf(g, s, 0.5f);
+  s *= g * g;
+  const float e = __expf(g) - 1.0f;
+  const bool small = fabsf(g) < 0.25f;
+  *k = small ? s : e - g;
+  *up = small ? s + g : e;
 }
 
 // A warp takes a segment of row b with token weight w; the segment's sums are in every lane.
@@ -286,11 +306,11 @@ __device__ __forceinline__ float4 policy_segment(const PolicyParams& p, int64_t 
       float l = clip ? -held : -free;
       float grad = clip ? 0.0f : -free;
       if (p.a.ref_logp != nullptr) {
-        const float gap = ref[j] - lp[j];
-        const float up = expm1f(gap);
-        l = fmaf(p.kl, up - gap, l);
+        float k, up;
+        kl_of(ref[j] - lp[j], &k, &up);
+        l = fmaf(p.kl, k, l);
         grad = fmaf(-p.kl, up, grad);
-        kls += up - gap;
+        kls += k;
       }
       if (p.a.entropy != nullptr) l = fmaf(-p.ent, ent[j], l);
       loss += l;
@@ -332,19 +352,14 @@ __device__ __forceinline__ Totals row_totals(int64_t segments, F part) {
 
 template <bool kVec>
 __global__ void __launch_bounds__(kThreads, kPolicyPerSm) policy_kernel(const PolicyParams p) {
-  const int64_t items = p.a.B * p.segments;
-  const int64_t warps = static_cast<int64_t>(gridDim.x) * kWarps;
-  int64_t item = static_cast<int64_t>(blockIdx.x) * kWarps + (threadIdx.x >> 5);
-  griddep_launch_dependents();
+  const int64_t item = static_cast<int64_t>(blockIdx.x) * kWarps + (threadIdx.x >> 5);
   griddep_wait();
   if (blockIdx.x == 0 && threadIdx.x == 0) *p.ticket = 0;      // for the grid after this one
-  const unsigned long long batch = counted_batch(p);
-  for (; item < items; item += warps) {
-    const int64_t b = item / p.segments;
-    const float4 s = policy_segment<kVec>(p, b, static_cast<int>(item - b * p.segments),
-                                          counted_weight(p, batch, b));
-    if ((threadIdx.x & 31) == 0) p.sums[item] = s;
-  }
+  if (item >= p.a.B * p.segments) return;
+  const int64_t b = item / p.segments;
+  const float4 s = policy_segment<kVec>(p, b, static_cast<int>(item - b * p.segments),
+                                        counted_weight(p, counted_batch(p), b));
+  if ((threadIdx.x & 31) == 0) p.sums[item] = s;
 }
 
 // Rows' losses, a warp each; the last CTA to finish adds the CTAs' totals in order.
@@ -393,6 +408,7 @@ __global__ void __launch_bounds__(kThreads) policy_small_kernel(const PolicyPara
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int B = static_cast<int>(p.a.B), segments = static_cast<int>(p.segments);
   unsigned total = 0;
+  griddep_wait();
   if (p.a.reduction != BERGSON_POLICY_SUM_NORM) {
     for (int b = warp; b < B; b += kWarps) {
       const unsigned c = p.a.mask == nullptr ? static_cast<unsigned>(p.a.T)
@@ -618,6 +634,7 @@ __global__ void __launch_bounds__(kPairThreads, kRef ? kPairPerSmRef : kPairPerS
   const int t1 = static_cast<int>(min(static_cast<int64_t>(T), t0 + int64_t{256} * per));
   Sum2 sum[2];
   int count[2] = {};
+  griddep_wait();
   if (live) pair_sums<N, kVec, kRef>(p, pair, t0, t1, red, counts, sum, count);
   if (!kTogether && parts > 1) {
     cluster_sync();                            // every CTA has started
@@ -653,8 +670,10 @@ __global__ void __launch_bounds__(kPairThreads, kRef ? kPairPerSmRef : kPairPerS
       }
     }
   }
+
+  if (live) write_pair<N, kVec>(p, pair, t0, t1, g.d);
   if (kTogether) {
-    cluster_sync();
+    cluster_sync();                            // every CTA has started
     if (threadIdx.x == 0) st_cluster(&shared[rank][0], 0, g.loss);
     cluster_sync();
     if (rank == 0 && threadIdx.x == 0) {
@@ -662,10 +681,7 @@ __global__ void __launch_bounds__(kPairThreads, kRef ? kPairPerSmRef : kPairPerS
       for (int c = 0; c < static_cast<int>(p.a.P); ++c) l.add(shared[c][0]);
       *p.a.loss = l.value() / static_cast<float>(p.a.P);
     }
-  } else {
-    griddep_launch_dependents();
   }
-  if (live) write_pair<N, kVec>(p, pair, t0, t1, g.d);
 }
 
 __global__ void __launch_bounds__(1024) preference_finish_kernel(const float* pair_loss,
@@ -699,12 +715,14 @@ cudaError_t launch_cluster(K kernel, int64_t grid, int threads, int cluster, con
   cfg.gridDim = dim3(static_cast<unsigned>(grid));
   cfg.blockDim = dim3(threads);
   cfg.stream = s;
-  cudaLaunchAttribute attr[1];
+  cudaLaunchAttribute attr[2];
   attr[0].id = cudaLaunchAttributeClusterDimension;
   attr[0].val.clusterDim.x = cluster;
   attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+  attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[1].val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = attr;
-  cfg.numAttrs = 1;
+  cfg.numAttrs = 2;
   return cudaLaunchKernelEx(&cfg, kernel, p);
 }
 
@@ -719,13 +737,12 @@ cudaError_t run_policy(PolicyParams p, cudaStream_t s) {
   if (p.a.mask != nullptr && p.a.reduction != BERGSON_POLICY_SUM_NORM) {
     p.n_counts = static_cast<int>(
         std::min<int64_t>(kCountCtas, ceil_div(p.a.B * p.count_segments, kWarps)));
-    policy_count_kernel<<<p.n_counts, kThreads, 0, s>>>(p);
-    const cudaError_t e = cudaGetLastError();
+    const cudaError_t e =
+        launch_dependent(policy_count_kernel, dim3(p.n_counts), dim3(kThreads), 0, s, p);
     if (e != cudaSuccess) return e;
   }
   cudaError_t e = launch_dependent(policy_kernel<kVec>,
-                                   dim3(static_cast<unsigned>(
-                                       std::min<int64_t>(kPolicyCtas, ceil_div(items, kWarps)))),
+                                   dim3(static_cast<unsigned>(ceil_div(items, kWarps))),
                                    dim3(kThreads), 0, s, p);
   if (e != cudaSuccess) return e;
   const int64_t finish = std::min<int64_t>(kFinishCtas, ceil_div(p.a.B, kWarps));

@@ -10,10 +10,9 @@ namespace {
 
 constexpr int kThreads = 256;
 constexpr int kWarps = kThreads / 32;
-constexpr int kWarpRows = 32;                  // rows a warp takes
+constexpr int kMostRows = 32, kLeastRows = 4;  // rows a warp takes (a power of two between)
 constexpr int kRows = 4;                       // of them on the way at once
 constexpr int kTileCtas = 3;
-constexpr int kBand = kWarps * kWarpRows;      // rows of a tile
 constexpr int kStrip = 256;                    // columns of a tile, 8 a lane
 constexpr int kFew = 24, kMany = 300;          // records a launch can take
 
@@ -26,7 +25,8 @@ struct Entry {
   float* row_part;             // [strips, rows]
   float* col_part;             // [bands, cols]
   float* tile_part;            // [bands, strips]
-  int bands, strips;
+  int bands, strips;           // tiles of kWarps warp_rows rows and kStrip columns
+  int warp_rows;
   int st;
   int vec;                     // rows start on boundaries of a lane's 8 elements
 };
@@ -69,7 +69,7 @@ __device__ __forceinline__ float sum_each(float (&x)[N]) {
   return t;
 }
 
-// A warp's rows r0 .. r0 + kWarpRows of a tile: lane sums of the columns in col[], the
+// A warp's rows r0 .. r0 + e.warp_rows of a tile: lane sums of the columns in col[], the
 // rows' sums to row_part.  Vectors: columns c0 + 8 lane + k; else c0 + lane + 32 k.
 template <bool kEight, bool kVec>
 __device__ __forceinline__ void take_rows(const Entry& e, int64_t r0, int64_t c0, float* row_part,
@@ -77,7 +77,7 @@ __device__ __forceinline__ void take_rows(const Entry& e, int64_t r0, int64_t c0
   const int lane = threadIdx.x & 31;
   float2 col2[4] = {};
 #pragma unroll 1
-  for (int64_t r = r0; r < r0 + kWarpRows && r < e.rows; r += kRows) {
+  for (int64_t r = r0; r < r0 + e.warp_rows && r < e.rows; r += kRows) {
     float sums[kRows];
     if constexpr (kVec && !kEight) {
       uint32_t x[kRows][8];
@@ -171,9 +171,10 @@ __global__ void __launch_bounds__(kThreads, kTileCtas) moment_tiles_kernel(
   const int at = find(p.tiles, p.n, blockIdx.x);
   const Entry& e = p.e[at];
   const uint32_t tile = blockIdx.x - p.tiles[at];
+  griddep_wait();
   const int band = tile / e.strips, strip = tile % e.strips;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const int64_t r0 = static_cast<int64_t>(band) * kBand + warp * kWarpRows;
+  const int64_t r0 = (static_cast<int64_t>(band) * kWarps + warp) * e.warp_rows;
   const int64_t c0 = static_cast<int64_t>(strip) * kStrip;
   float* row_part = e.row_part + static_cast<int64_t>(strip) * e.rows;
   float col[8];
@@ -212,8 +213,13 @@ __global__ void __launch_bounds__(kThreads) moment_finish_kernel(
     const float* part = row ? e.row_part + i : e.col_part + j;
     const int64_t step = row ? e.rows : e.cols;
     const int n = row ? e.strips : e.bands;
-#pragma unroll 8
-    for (int k = 0; k < n; ++k) x.add(part[k * step]);
+    for (int k = 0; k < n; k += 8) {
+      float v[8];
+#pragma unroll
+      for (int o = 0; o < 8; ++o) v[o] = k + o < n ? part[(k + o) * step] : 0.0f;
+#pragma unroll
+      for (int o = 0; o < 8; ++o) x.add(v[o]);
+    }
   }
   CompensatedSum sum;
   const int64_t tiles = static_cast<int64_t>(e.bands) * e.strips;
@@ -227,8 +233,20 @@ __global__ void __launch_bounds__(kThreads) moment_finish_kernel(
 
 int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
+// Rows a warp takes of a matrix, by its own size alone (so that its sums are the same
+// in any company): as many as leave kTilesWanted tiles.
+constexpr int64_t kTilesWanted = 64;
+int warp_rows_of(const bergson_moment_matrix& m) {
+  int rows = kMostRows;
+  while (rows > kLeastRows &&
+         ceil_div(m.d_out, kWarps * rows) * ceil_div(m.d_in, kStrip) < kTilesWanted)
+    rows /= 2;
+  return rows;
+}
+
 size_t floats_of(const bergson_moment_matrix& m) {
-  const size_t bands = ceil_div(m.d_out, kBand), strips = ceil_div(m.d_in, kStrip);
+  const size_t bands = ceil_div(m.d_out, kWarps * warp_rows_of(m));
+  const size_t strips = ceil_div(m.d_in, kStrip);
   return strips * m.d_out + bands * m.d_in + bands * strips;
 }
 
@@ -244,15 +262,17 @@ cudaError_t run_moments(const bergson_moment_matrix* m, int n, double correction
   const auto flush = [&]() -> cudaError_t {
     if (k == 0) return cudaSuccess;
     p.n = k;
-    moment_tiles_kernel<N><<<p.tiles[k], kThreads, 0, s>>>(p);
-    const cudaError_t e = cudaGetLastError();
+    const cudaError_t e = launch_dependent(moment_tiles_kernel<N>, dim3(p.tiles[k]),
+                                           dim3(kThreads), 0, s, p);
     if (e != cudaSuccess) return e;
     const dim3 grid(p.outs[k]);
     k = 0;
     return launch_dependent(moment_finish_kernel<N>, grid, dim3(kThreads), 0, s, p);
   };
   for (int i = 0; i < n; ++i) {
-    const int64_t bands = ceil_div(m[i].d_out, kBand), strips = ceil_div(m[i].d_in, kStrip);
+    const int warp_rows = warp_rows_of(m[i]);
+    const int64_t bands = ceil_div(m[i].d_out, kWarps * warp_rows);
+    const int64_t strips = ceil_div(m[i].d_in, kStrip);
     const int64_t outs = ceil_div(m[i].d_out + m[i].d_in, kThreads);
     if (k == N ||
         (k > 0 && (p.tiles[k] + bands * strips > INT32_MAX || p.outs[k] + outs > INT32_MAX))) {
@@ -269,6 +289,7 @@ cudaError_t run_moments(const bergson_moment_matrix* m, int n, double correction
     e.st = m[i].state_kind;
     e.vec = m[i].d_in % 8 == 0 &&
             reinterpret_cast<uintptr_t>(m[i].v) % (e.st == BERGSON_STATE_8BIT ? 8 : 32) == 0;
+    e.warp_rows = warp_rows;
     e.bands = static_cast<int>(bands);
     e.strips = static_cast<int>(strips);
     e.row_part = at;

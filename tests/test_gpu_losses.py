@@ -3,7 +3,7 @@
 Tolerances: a token's loss and gradient take a handful of fp32 operations
 (exp and expm1 at 2 units, a difference of log-probabilities at half a unit
 of their size), so they are held to 2e-6 of the sizes that enter; sums over
-tokens are fp32 within 512 and fp64 above, held to 2e-6 of the sum of
+tokens are fp32 within 1024 and twice its bits above, held to 2e-6 of the sum of
 magnitudes.
 """
 import numpy as np
