@@ -157,8 +157,17 @@ __device__ __forceinline__ void block_vectors(const StepScalars& s, const Entry&
   if (kEight) {
 #pragma unroll
     for (int q = 0; q < 2; ++q) {
-      decode_first4(rm[q], m + 4 * q);
-      decode_second4(rv[q], v + 4 * q);
+      decode_nonzero_first4(rm[q], m + 4 * q);
+      decode_nonzero_second4(rv[q], v + 4 * q);
+    }
+    // codes of 0 are rare but where there is no gradient: a branch of the warp
+    if (__any_sync(0xffffffffu, (zero_bytes(rm[0] & 0x7f7f7f7fu) | zero_bytes(rm[1] & 0x7f7f7f7fu) |
+                                 zero_bytes(rv[0]) | zero_bytes(rv[1])) != 0)) {
+#pragma unroll
+      for (int q = 0; q < 2; ++q) {
+        put_zeros4(rm[q] & 0x7f7f7f7fu, m + 4 * q);
+        put_zeros4(rv[q], v + 4 * q);
+      }
     }
   } else {
 #pragma unroll
@@ -197,8 +206,10 @@ __device__ __forceinline__ void block_vectors(const StepScalars& s, const Entry&
     top_m = max_nan(top_m, m[k]);
     top_v = max_nan(top_v, v[k]);
   }
-  const float ms1 = block_scale(block_top(top_m)), vs1 = block_scale(block_top(top_v));
-  const float im = block_inverse(ms1), iv = block_inverse(vs1);
+  // the lower lanes take m's scale and its inverse, the upper ones v's
+  const float all_m = block_top(top_m), all_v = block_top(top_v);
+  const float scale = block_scale(lane < 16 ? all_m : all_v), inverse = block_inverse(scale);
+  const float im = __shfl_sync(0xffffffffu, inverse, 0), iv = __shfl_sync(0xffffffffu, inverse, 16);
   uint32_t cm[2], cv[2];
   const uint64_t at = e.key + (static_cast<uint64_t>(i >> 2) + 1) * kSplitMixGamma;
 #pragma unroll
@@ -208,12 +219,13 @@ __device__ __forceinline__ void block_vectors(const StepScalars& s, const Entry&
     cm[q] = encode_first4(m + 4 * q, im, c);
     cv[q] = encode_second4(v + 4 * q, iv, c);
   }
+  if (__any_sync(0xffffffffu, (zero_bytes(cv[0]) | zero_bytes(cv[1])) != 0)) {
+    cv[0] = raise_zeros4(cv[0], v);
+    cv[1] = raise_zeros4(cv[1], v + 4);
+  }
   *reinterpret_cast<uint2*>(static_cast<uint8_t*>(e.m) + i) = make_uint2(cm[0], cm[1]);
   *reinterpret_cast<uint2*>(static_cast<uint8_t*>(e.v) + i) = make_uint2(cv[0], cv[1]);
-  if (lane == 0) {
-    e.ms[first / kStateBlock] = ms1;
-    e.vs[first / kStateBlock] = vs1;
-  }
+  if (lane % 16 == 0) (lane == 0 ? e.ms : e.vs)[first / kStateBlock] = scale;
 }
 
 // Any block: element by element, neighbouring lanes at neighbouring elements.

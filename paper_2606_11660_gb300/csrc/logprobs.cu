@@ -428,9 +428,15 @@ __global__ void __launch_bounds__(kThreads, kBwdCtas) logprobs_backward_warp_ker
 
 // ------------------------------------------------------------------- host
 
-constexpr int64_t kWarpRowBytes = 4096;        // rows up to this go to warps
+// Rows of up to kWarpRowBytes go to warps, of up to kManyRowBytes where there are kManyRows.
+constexpr int64_t kWarpRowBytes = 4096;
+constexpr int64_t kManyRowBytes = 16384, kManyRows = 1216;
 constexpr int64_t kPartBytes = 32768;          // and a row is split down to this
 constexpr int64_t kSliceBytes = 32768;
+
+bool rows_to_warps(int64_t rows, int64_t bytes) {
+  return bytes <= (rows >= kManyRows ? kManyRowBytes : kWarpRowBytes);
+}
 
 template <typename T, bool kEntropy>
 cudaError_t run_forward(const LogprobArgs& a, cudaStream_t s) {
@@ -438,7 +444,7 @@ cudaError_t run_forward(const LogprobArgs& a, cudaStream_t s) {
                         static_cast<float>(1.4426950408889634 / a.tau), a.logp, a.lse, a.entropy,
                         a.status};
   const int64_t bytes = a.V * static_cast<int64_t>(sizeof(T));
-  if (bytes <= kWarpRowBytes) {
+  if (rows_to_warps(a.rows, bytes)) {
     const int64_t grid = (a.rows + kThreads / 32 - 1) / (kThreads / 32);
     return launch_dependent(logprobs_warp_kernel<T, kEntropy>, dim3(static_cast<unsigned>(grid)),
                             dim3(kThreads), 0, s, p);
@@ -466,7 +472,7 @@ cudaError_t run_backward(const LogprobGradArgs& a, cudaStream_t s) {
   BackwardParams p{a.x, a.rows, a.V, a.ld, a.targets, static_cast<float>(1.0 / a.tau), a.lse,
                    a.entropy, a.d_logp, a.d_entropy, a.dx, a.ld_d, 1, a.status};
   const int64_t bytes = a.V * static_cast<int64_t>(sizeof(T));
-  if (bytes <= kWarpRowBytes) {
+  if (rows_to_warps(a.rows, bytes)) {
     const int64_t grid = (a.rows + kThreads / 32 - 1) / (kThreads / 32);
     return launch_dependent(logprobs_backward_warp_kernel<T, kEntropy>,
                             dim3(static_cast<unsigned>(grid)), dim3(kThreads), 0, s, p);

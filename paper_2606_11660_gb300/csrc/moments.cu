@@ -11,7 +11,9 @@ namespace {
 constexpr int kThreads = 256;
 constexpr int kWarps = kThreads / 32;
 constexpr int kMostRows = 32, kLeastRows = 4;  // rows a warp takes (a power of two between)
-constexpr int kRows = 4;                       // of them on the way at once
+// Rows on the way at once, fp32 and 8-bit (1 KB and 256 bytes a row), and CTAs an SM.
+// 201M fp32 elements, us: 8 rows at 3 CTAs 157, 4 at 1 / 3 / 4 CTAs 149 / 136 / 142.
+constexpr int kRows32 = 4, kRows8 = 8;
 constexpr int kTileCtas = 3;
 constexpr int kStrip = 256;                    // columns of a tile, 8 a lane
 constexpr int kFew = 24, kMany = 300;          // records a launch can take
@@ -69,25 +71,84 @@ __device__ __forceinline__ float sum_each(float (&x)[N]) {
   return t;
 }
 
+// The 8 codes from element i on, which may lie across two 8-byte words and two scales.
+// A word that reaches past the matrix is read byte by byte.
+__device__ __forceinline__ uint2 load_codes(const uint8_t* v, int64_t i, int count, int64_t n) {
+  const uintptr_t at = reinterpret_cast<uintptr_t>(v) + i, base = at & ~uintptr_t{7};
+  const int skip = static_cast<int>(at & 7);
+  if (base < reinterpret_cast<uintptr_t>(v) || base + 16 > reinterpret_cast<uintptr_t>(v) + n) {
+    uint2 u = make_uint2(0, 0);
+    for (int j = 0; j < count; ++j) {
+      const uint32_t c = v[i + j];
+      if (j < 4) u.x |= c << (8 * j); else u.y |= c << (8 * (j - 4));
+    }
+    return u;
+  }
+  const uint2 a = *reinterpret_cast<const uint2*>(base), b = *reinterpret_cast<const uint2*>(base + 8);
+  const uint32_t w[4] = {a.x, a.y, b.x, b.y};
+  const bool far = skip >= 4;
+  const uint32_t w0 = far ? w[1] : w[0], w1 = far ? w[2] : w[1], w2 = far ? w[3] : w[2];
+  uint2 u;
+  u.x = __funnelshift_r(w0, w1, 8 * (skip & 3));
+  u.y = __funnelshift_r(w1, w2, 8 * (skip & 3));
+  // codes past the row's end belong to the next one
+  if (count < 8) {
+    u.y = count <= 4 ? 0u : u.y & ((1u << (8 * (count - 4))) - 1u);
+    if (count < 4) u.x &= (1u << (8 * count)) - 1u;
+  }
+  return u;
+}
+
+// The values of a lane's 8 codes added up, and to the columns.  By all lanes of a warp;
+// one that has none gives scale 0.
+__device__ __forceinline__ float add_codes(uint2 u, float scale, float2 (&col)[4]) {
+  float y[8];
+  decode_nonzero_second4(u.x, y);
+  decode_nonzero_second4(u.y, y + 4);
+  if (__any_sync(0xffffffffu, (zero_bytes(u.x) | zero_bytes(u.y)) != 0)) {
+    put_zeros4(u.x, y);
+    put_zeros4(u.y, y + 4);
+  }
+  float2 s = {0.0f, 0.0f};
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    const float2 y2 = make_float2(y[2 * j], y[2 * j + 1]);
+    col[j] = fma2(y2, pair(scale), col[j]);
+    s = add2(s, y2);
+  }
+  return (s.x + s.y) * scale;
+}
+
 // A warp's rows r0 .. r0 + e.warp_rows of a tile: lane sums of the columns in col[], the
-// rows' sums to row_part.  Vectors: columns c0 + 8 lane + k; else c0 + lane + 32 k.
+// rows' sums to row_part.  Columns c0 + 8 lane + k, or of fp32 rows that start off a
+// lane's 32 bytes c0 + lane + 32 k.
 template <bool kEight, bool kVec>
 __device__ __forceinline__ void take_rows(const Entry& e, int64_t r0, int64_t c0, float* row_part,
                                           float (&col)[8]) {
+  constexpr int kRows = kEight ? kRows8 : kRows32;
   const int lane = threadIdx.x & 31;
+  const int64_t r1 = min(e.rows, r0 + e.warp_rows);
+  const int64_t c = c0 + 8 * lane;
+  const int count = static_cast<int>(min(static_cast<int64_t>(8), e.cols - c));   // of the lane's
   float2 col2[4] = {};
 #pragma unroll 1
-  for (int64_t r = r0; r < r0 + e.warp_rows && r < e.rows; r += kRows) {
+  for (int64_t r = r0; r < r1; r += kRows) {
     float sums[kRows];
-    if constexpr (kVec && !kEight) {
+    if constexpr (!kEight) {
       uint32_t x[kRows][8];
-      const int64_t c = c0 + 8 * lane;
 #pragma unroll
       for (int k = 0; k < kRows; ++k) {
 #pragma unroll
         for (int j = 0; j < 8; ++j) x[k][j] = 0;
-        if (r + k < e.rows && c < e.cols)
-          load32(static_cast<const float*>(e.v) + (r + k) * e.cols + c, x[k]);
+        if (r + k >= r1) continue;
+        const float* row = static_cast<const float*>(e.v) + (r + k) * e.cols;
+        if (kVec) {
+          if (count > 0) load32(row + c, x[k]);
+        } else {
+#pragma unroll
+          for (int j = 0; j < 8; ++j)
+            if (c0 + lane + 32 * j < e.cols) x[k][j] = __float_as_uint(row[c0 + lane + 32 * j]);
+        }
       }
 #pragma unroll
       for (int k = 0; k < kRows; ++k) {
@@ -103,58 +164,46 @@ __device__ __forceinline__ void take_rows(const Entry& e, int64_t r0, int64_t c0
     } else if constexpr (kVec) {
       uint2 u[kRows];
       float sc[kRows];
-      const int64_t c = c0 + 8 * lane;
 #pragma unroll
       for (int k = 0; k < kRows; ++k) {
-        u[k] = make_uint2(0, 0);
+        u[k] = make_uint2(0x01010101u, 0x01010101u);
         sc[k] = 0.0f;
-        if (r + k < e.rows && c < e.cols) {
-          const int64_t i = (r + k) * e.cols + c;
+        if (r + k < r1 && count > 0) {
+          const uint64_t i = (r + k) * e.cols + c;
           u[k] = *reinterpret_cast<const uint2*>(static_cast<const uint8_t*>(e.v) + i);
           sc[k] = e.vs[i / kStateBlock];
         }
       }
 #pragma unroll
-      for (int k = 0; k < kRows; ++k) {
-        float y[8];
-        decode_second4(u[k].x, y);
-        decode_second4(u[k].y, y + 4);
-        float2 s = {0.0f, 0.0f};
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          const float2 y2 = make_float2(y[2 * j], y[2 * j + 1]);
-          col2[j] = fma2(y2, pair(sc[k]), col2[j]);
-          s = add2(s, y2);
-        }
-        sums[k] = (s.x + s.y) * sc[k];
-      }
+      for (int k = 0; k < kRows; ++k) sums[k] = add_codes(u[k], sc[k], col2);
     } else {
+      const int64_t n = e.rows * e.cols;
 #pragma unroll
       for (int k = 0; k < kRows; ++k) {
-        float y[8];
-        const int64_t row = (r + k) * e.cols;
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-          const int64_t c = c0 + lane + 32 * j;
-          y[j] = 0.0f;
-          if (r + k < e.rows && c < e.cols)
-            y[j] = kEight ? decode_second(static_cast<const uint8_t*>(e.v)[row + c]) *
-                                e.vs[(row + c) / kStateBlock]
-                          : static_cast<const float*>(e.v)[row + c];
+        uint2 u = make_uint2(0x01010101u, 0x01010101u), v = u;
+        float sc = 0.0f, sc2 = 0.0f;
+        if (r + k < r1 && count > 0) {
+          const uint64_t i = (r + k) * e.cols + c;
+          const int near = kStateBlock - static_cast<int>(i % kStateBlock);   // with the first scale
+          u = load_codes(static_cast<const uint8_t*>(e.v), i, count, n);
+          sc = e.vs[i / kStateBlock];
+          if (near < count) {                    // below 8 here
+            const uint32_t lo = near >= 4 ? 0xffffffffu : (1u << (8 * near)) - 1u;
+            const uint32_t hi = near <= 4 ? 0u : (1u << (8 * (near - 4))) - 1u;
+            v.x = u.x & ~lo;
+            v.y = u.y & ~hi;
+            u.x &= lo;
+            u.y &= hi;
+            sc2 = e.vs[i / kStateBlock + 1];
+          }
         }
-        float2 s = {0.0f, 0.0f};
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          const float2 y2 = make_float2(y[2 * j], y[2 * j + 1]);
-          col2[j] = add2(col2[j], y2);
-          s = add2(s, y2);
-        }
-        sums[k] = s.x + s.y;
+        sums[k] = add_codes(u, sc, col2);
+        if (__any_sync(0xffffffffu, sc2 != 0.0f)) sums[k] += add_codes(v, sc2, col2);
       }
     }
     const float t = sum_each(sums);
     const int k = lane / (32 / kRows);
-    if (lane % (32 / kRows) == 0 && r + k < e.rows) row_part[r + k] = t;
+    if (lane % (32 / kRows) == 0 && r + k < r1) row_part[r + k] = t;
   }
 #pragma unroll
   for (int j = 0; j < 4; ++j) {
@@ -186,7 +235,8 @@ __global__ void __launch_bounds__(kThreads, kTileCtas) moment_tiles_kernel(
     else take_rows<false, false>(e, r0, c0, row_part, col);
   }
 #pragma unroll
-  for (int j = 0; j < 8; ++j) cols[warp][e.vec ? 8 * lane + j : lane + 32 * j] = col[j];
+  for (int j = 0; j < 8; ++j)
+    cols[warp][e.vec || e.st == BERGSON_STATE_8BIT ? 8 * lane + j : lane + 32 * j] = col[j];
   __syncthreads();
   float x = 0.0f;
 #pragma unroll

@@ -261,9 +261,9 @@ template <int K>
 __device__ __forceinline__ uint32_t byte_to_code_bits(uint32_t w) {   // byte K at bit 20 on
   return K == 0 ? w << 20 : K == 1 ? w << 12 : K == 2 ? w << 4 : w >> 4;
 }
-// Whether a byte of w is 0.
-__device__ __forceinline__ bool has_zero_byte(uint32_t w) {
-  return ((w - 0x01010101u) & ~w & 0x80808080u) != 0;
+// Nonzero where a byte of w is 0.
+__device__ __forceinline__ uint32_t zero_bytes(uint32_t w) {
+  return (w - 0x01010101u) & ~w & 0x80808080u;
 }
 template <int K>
 __device__ __forceinline__ float first_bits(uint32_t w) {
@@ -276,27 +276,32 @@ __device__ __forceinline__ float second_bits(uint32_t w) {
   return __uint_as_float((byte_to_code_bits<K>(w) & 0x0ff00000u) |
                          static_cast<uint32_t>(kSecondBase << kCodeShift));
 }
-__device__ __forceinline__ void decode_first4(uint32_t w, float* x) {
+// The values of codes of which none is 0 (a 0 would read as the smallest magnitude) ...
+__device__ __forceinline__ void decode_nonzero_first4(uint32_t w, float* x) {
   x[0] = first_bits<0>(w);
   x[1] = first_bits<1>(w);
   x[2] = first_bits<2>(w);
   x[3] = first_bits<3>(w);
-  if (has_zero_byte(w & 0x7f7f7f7fu)) {
-#pragma unroll
-    for (int k = 0; k < 4; ++k)
-      if (((w >> (8 * k)) & 127u) == 0) x[k] = 0.0f;
-  }
 }
-__device__ __forceinline__ void decode_second4(uint32_t w, float* x) {
+__device__ __forceinline__ void decode_nonzero_second4(uint32_t w, float* x) {
   x[0] = second_bits<0>(w);
   x[1] = second_bits<1>(w);
   x[2] = second_bits<2>(w);
   x[3] = second_bits<3>(w);
-  if (has_zero_byte(w)) {
+}
+// ... and zeros where the bytes of w say so.
+__device__ __forceinline__ void put_zeros4(uint32_t w, float* x) {
 #pragma unroll
-    for (int k = 0; k < 4; ++k)
-      if (((w >> (8 * k)) & 255u) == 0) x[k] = 0.0f;
-  }
+  for (int k = 0; k < 4; ++k)
+    if (((w >> (8 * k)) & 255u) == 0) x[k] = 0.0f;
+}
+__device__ __forceinline__ void decode_first4(uint32_t w, float* x) {
+  decode_nonzero_first4(w, x);
+  put_zeros4(w & 0x7f7f7f7fu, x);
+}
+__device__ __forceinline__ void decode_second4(uint32_t w, float* x) {
+  decode_nonzero_second4(w, x);
+  put_zeros4(w, x);
 }
 // Where the four elements' chances stand below the cut: bits 4 .. 19.
 __device__ __forceinline__ void chances(uint64_t h, uint32_t (&c)[4]) {
@@ -306,7 +311,7 @@ __device__ __forceinline__ void chances(uint64_t h, uint32_t (&c)[4]) {
   c[2] = (hi << 4) & 0xffff0u;
   c[3] = (hi >> 12) & 0xffff0u;
 }
-// encode_first and encode_second of four elements.  Magnitudes are packed with one
+// encode_first and encode_second (but for raise_zeros4) of four elements.  Magnitudes are packed with one
 // bit more, so that holding them to a byte holds them to 7 bits.
 __device__ __forceinline__ uint32_t encode_first4(const float* m, float inv, const uint32_t* c) {
   int x[4];
@@ -325,12 +330,13 @@ __device__ __forceinline__ uint32_t encode_second4(const float* v, float inv, co
   for (int k = 0; k < 4; ++k)
     x[k] = (__float_as_int(__fmul_rn(v[k], inv)) + static_cast<int>(c[k]) -
             (kSecondBase << kCodeShift)) >> kCodeShift;
-  uint32_t w = pack_bytes(x[0], x[1], x[2], x[3]);
-  if (has_zero_byte(w)) {                        // only 0 takes code 0
+  return pack_bytes(x[0], x[1], x[2], x[3]);
+}
+// Only a v of 0 takes code 0: others get the smallest.
+__device__ __forceinline__ uint32_t raise_zeros4(uint32_t w, const float* v) {
 #pragma unroll
-    for (int k = 0; k < 4; ++k)
-      if (((w >> (8 * k)) & 255u) == 0 && v[k] > 0.0f) w |= 1u << (8 * k);
-  }
+  for (int k = 0; k < 4; ++k)
+    if (((w >> (8 * k)) & 255u) == 0 && v[k] > 0.0f) w |= 1u << (8 * k);
   return w;
 }
 
