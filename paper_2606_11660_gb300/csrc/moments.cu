@@ -15,7 +15,8 @@ constexpr int kMostRows = 32, kLeastRows = 4;  // rows a warp takes (a power of 
 // 201M fp32 elements, us: 8 rows at 3 CTAs 157, 4 at 1 / 3 / 4 CTAs 149 / 136 / 142.
 constexpr int kRows32 = 4, kRows8 = 8;
 constexpr int kTileCtas = 3;
-constexpr int kStrip = 256;                    // columns of a tile, 8 a lane
+// Columns of a tile: 32 bytes of fp32 a lane, 16 codes of 8 bits.
+constexpr int kStrip32 = 256, kStrip8 = 512;
 constexpr int kFew = 24, kMany = 300;          // records a launch can take
 
 struct Entry {
@@ -27,10 +28,10 @@ struct Entry {
   float* row_part;             // [strips, rows]
   float* col_part;             // [bands, cols]
   float* tile_part;            // [bands, strips]
-  int bands, strips;           // tiles of kWarps warp_rows rows and kStrip columns
-  int warp_rows;
+  int bands, strips;           // tiles of kWarps warp_rows rows and `strip` columns
+  int warp_rows, strip;
   int st;
-  int vec;                     // rows start on boundaries of a lane's 8 elements
+  int vec;                     // rows start on boundaries of a lane's vector
 };
 
 template <int N>
@@ -99,19 +100,22 @@ __device__ __forceinline__ uint2 load_codes(const uint8_t* v, int64_t i, int cou
   return u;
 }
 
-// The values of a lane's 8 codes added up, and to the columns.  By all lanes of a warp;
-// one that has none gives scale 0.
-__device__ __forceinline__ float add_codes(uint2 u, float scale, float2 (&col)[4]) {
-  float y[8];
-  decode_nonzero_second4(u.x, y);
-  decode_nonzero_second4(u.y, y + 4);
-  if (__any_sync(0xffffffffu, (zero_bytes(u.x) | zero_bytes(u.y)) != 0)) {
-    put_zeros4(u.x, y);
-    put_zeros4(u.y, y + 4);
+constexpr uint4 kNoCodes = {0x01010101u, 0x01010101u, 0x01010101u, 0x01010101u};
+
+// The values of a lane's 16 codes added up, and to the columns.  By all lanes of a warp;
+// one that has none gives kNoCodes and scale 0.
+__device__ __forceinline__ float add_codes(const uint4& u, float scale, float2 (&col)[8]) {
+  float y[16];
+#pragma unroll
+  for (int q = 0; q < 4; ++q) decode_nonzero_second4(word(u, q), y + 4 * q);
+  if (__any_sync(0xffffffffu, (zero_bytes(u.x) | zero_bytes(u.y) | zero_bytes(u.z) |
+                               zero_bytes(u.w)) != 0)) {
+#pragma unroll
+    for (int q = 0; q < 4; ++q) put_zeros4(word(u, q), y + 4 * q);
   }
   float2 s = {0.0f, 0.0f};
 #pragma unroll
-  for (int j = 0; j < 4; ++j) {
+  for (int j = 0; j < 8; ++j) {
     const float2 y2 = make_float2(y[2 * j], y[2 * j + 1]);
     col[j] = fma2(y2, pair(scale), col[j]);
     s = add2(s, y2);
@@ -119,20 +123,35 @@ __device__ __forceinline__ float add_codes(uint2 u, float scale, float2 (&col)[4
   return (s.x + s.y) * scale;
 }
 
-// A warp's rows r0 .. r0 + e.warp_rows of a tile: lane sums of the columns in col[], the
-// rows' sums to row_part.  Columns c0 + 8 lane + k, or of fp32 rows that start off a
-// lane's 32 bytes c0 + lane + 32 k.
-template <bool kEight, bool kVec>
+// The first `near` of 16 codes, the others 0.
+__device__ __forceinline__ uint4 first_codes(const uint4& u, int near) {
+  uint4 a;
+#pragma unroll
+  for (int q = 0; q < 4; ++q) {
+    const int n = near - 4 * q;
+    set_word(a, q, n >= 4 ? word(u, q) : n <= 0 ? 0u : word(u, q) & ((1u << (8 * n)) - 1u));
+  }
+  return a;
+}
+
+// A warp's rows r0 .. r0 + e.warp_rows of a tile: the rows' sums to row_part, and in col[]
+// the lane's columns c0 + kCols lane + k, or of fp32 rows that start off a lane's 32
+// bytes c0 + lane + 32 k.
+template <bool kEight, bool kVec, int kCols>
 __device__ __forceinline__ void take_rows(const Entry& e, int64_t r0, int64_t c0, float* row_part,
-                                          float (&col)[8]) {
+                                          float2 (&col)[kCols / 2]) {
   constexpr int kRows = kEight ? kRows8 : kRows32;
   const int lane = threadIdx.x & 31;
-  const int64_t r1 = min(e.rows, r0 + e.warp_rows);
-  const int64_t c = c0 + 8 * lane;
-  const int count = static_cast<int>(min(static_cast<int64_t>(8), e.cols - c));   // of the lane's
-  float2 col2[4] = {};
+  const int64_t c = c0 + kCols * lane;
+  const int cols = static_cast<int>(e.cols);
+  const int count = static_cast<int>(min(static_cast<int64_t>(kCols), e.cols - c));   // of the lane's
+  int left = static_cast<int>(min(e.rows - r0, static_cast<int64_t>(e.warp_rows)));
+#pragma unroll
+  for (int j = 0; j < kCols / 2; ++j) col[j] = {0.0f, 0.0f};
+  uint64_t i = static_cast<uint64_t>(r0) * cols + c;      // the lane's first element of a row
+  row_part += r0;
 #pragma unroll 1
-  for (int64_t r = r0; r < r1; r += kRows) {
+  for (; left > 0; left -= kRows, i += static_cast<uint64_t>(kRows) * cols, row_part += kRows) {
     float sums[kRows];
     if constexpr (!kEight) {
       uint32_t x[kRows][8];
@@ -140,14 +159,15 @@ __device__ __forceinline__ void take_rows(const Entry& e, int64_t r0, int64_t c0
       for (int k = 0; k < kRows; ++k) {
 #pragma unroll
         for (int j = 0; j < 8; ++j) x[k][j] = 0;
-        if (r + k >= r1) continue;
-        const float* row = static_cast<const float*>(e.v) + (r + k) * e.cols;
+        if (k >= left) continue;
+        const float* row = static_cast<const float*>(e.v) + (i + static_cast<uint64_t>(k) * cols);
         if (kVec) {
-          if (count > 0) load32(row + c, x[k]);
+          if (count > 0) load32(row, x[k]);
         } else {
+          row -= 8 * lane;
 #pragma unroll
           for (int j = 0; j < 8; ++j)
-            if (c0 + lane + 32 * j < e.cols) x[k][j] = __float_as_uint(row[c0 + lane + 32 * j]);
+            if (c0 + lane + 32 * j < cols) x[k][j] = __float_as_uint(row[lane + 32 * j]);
         }
       }
 #pragma unroll
@@ -156,97 +176,103 @@ __device__ __forceinline__ void take_rows(const Entry& e, int64_t r0, int64_t c0
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
           const float2 y = make_float2(__uint_as_float(x[k][2 * j]), __uint_as_float(x[k][2 * j + 1]));
-          col2[j] = add2(col2[j], y);
+          col[j] = add2(col[j], y);
           s = add2(s, y);
         }
         sums[k] = s.x + s.y;
       }
     } else if constexpr (kVec) {
-      uint2 u[kRows];
+      uint4 u[kRows];
       float sc[kRows];
 #pragma unroll
       for (int k = 0; k < kRows; ++k) {
-        u[k] = make_uint2(0x01010101u, 0x01010101u);
+        u[k] = kNoCodes;
         sc[k] = 0.0f;
-        if (r + k < r1 && count > 0) {
-          const uint64_t i = (r + k) * e.cols + c;
-          u[k] = *reinterpret_cast<const uint2*>(static_cast<const uint8_t*>(e.v) + i);
-          sc[k] = e.vs[i / kStateBlock];
+        if (k < left && count > 0) {
+          const uint64_t at = i + static_cast<uint64_t>(k) * cols;
+          u[k] = __ldcs(reinterpret_cast<const uint4*>(static_cast<const uint8_t*>(e.v) + at));
+          sc[k] = e.vs[at / kStateBlock];
         }
       }
 #pragma unroll
-      for (int k = 0; k < kRows; ++k) sums[k] = add_codes(u[k], sc[k], col2);
+      for (int k = 0; k < kRows; ++k) sums[k] = add_codes(u[k], sc[k], col);
     } else {
       const int64_t n = e.rows * e.cols;
+      const uint8_t* v = static_cast<const uint8_t*>(e.v);
 #pragma unroll
       for (int k = 0; k < kRows; ++k) {
-        uint2 u = make_uint2(0x01010101u, 0x01010101u), v = u;
+        uint4 u = kNoCodes, u2 = kNoCodes;
         float sc = 0.0f, sc2 = 0.0f;
-        if (r + k < r1 && count > 0) {
-          const uint64_t i = (r + k) * e.cols + c;
-          const int near = kStateBlock - static_cast<int>(i % kStateBlock);   // with the first scale
-          u = load_codes(static_cast<const uint8_t*>(e.v), i, count, n);
-          sc = e.vs[i / kStateBlock];
-          if (near < count) {                    // below 8 here
-            const uint32_t lo = near >= 4 ? 0xffffffffu : (1u << (8 * near)) - 1u;
-            const uint32_t hi = near <= 4 ? 0u : (1u << (8 * (near - 4))) - 1u;
-            v.x = u.x & ~lo;
-            v.y = u.y & ~hi;
-            u.x &= lo;
-            u.y &= hi;
-            sc2 = e.vs[i / kStateBlock + 1];
+        if (k < left && count > 0) {
+          const uint64_t at = i + static_cast<uint64_t>(k) * cols;
+          const uint2 a = load_codes(v, at, min(count, 8), n);
+          const uint2 b = count > 8 ? load_codes(v, at + 8, count - 8, n) : make_uint2(0, 0);
+          u = make_uint4(a.x, a.y, b.x, b.y);
+          const int near = kStateBlock - static_cast<int>(at % kStateBlock);   // with the first scale
+          sc = e.vs[at / kStateBlock];
+          if (near < count) {
+            const uint4 f = first_codes(u, near);
+            u2 = make_uint4(u.x ^ f.x, u.y ^ f.y, u.z ^ f.z, u.w ^ f.w);
+            u = f;
+            sc2 = e.vs[at / kStateBlock + 1];
           }
         }
-        sums[k] = add_codes(u, sc, col2);
-        if (__any_sync(0xffffffffu, sc2 != 0.0f)) sums[k] += add_codes(v, sc2, col2);
+        sums[k] = add_codes(u, sc, col);
+        if (__any_sync(0xffffffffu, sc2 != 0.0f)) sums[k] += add_codes(u2, sc2, col);
       }
     }
     const float t = sum_each(sums);
     const int k = lane / (32 / kRows);
-    if (lane % (32 / kRows) == 0 && r + k < r1) row_part[r + k] = t;
+    if (lane % (32 / kRows) == 0 && k < left) row_part[k] = t;
   }
+}
+
+// ... and the columns' sums of the warp to shared memory.
+template <bool kEight, bool kVec>
+__device__ __forceinline__ void take_tile(const Entry& e, int64_t r0, int64_t c0, float* row_part,
+                                          float* cols) {
+  constexpr int kCols = kEight ? kStrip8 / 32 : kStrip32 / 32;
+  const int lane = threadIdx.x & 31;
+  float2 col[kCols / 2];
+  take_rows<kEight, kVec, kCols>(e, r0, c0, row_part, col);
 #pragma unroll
-  for (int j = 0; j < 4; ++j) {
-    col[2 * j] = col2[j].x;
-    col[2 * j + 1] = col2[j].y;
-  }
+  for (int j = 0; j < kCols; ++j)
+    cols[kEight || kVec ? kCols * lane + j : lane + 32 * j] = j % 2 ? col[j / 2].y : col[j / 2].x;
 }
 
 template <int N>
 __global__ void __launch_bounds__(kThreads, kTileCtas) moment_tiles_kernel(
     const __grid_constant__ MomentParams<N> p) {
-  __shared__ float cols[kWarps][kStrip];
+  __shared__ float cols[kWarps][kStrip8];
   __shared__ float red[kWarps];
   const int at = find(p.tiles, p.n, blockIdx.x);
   const Entry& e = p.e[at];
   const uint32_t tile = blockIdx.x - p.tiles[at];
   griddep_wait();
   const int band = tile / e.strips, strip = tile % e.strips;
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int warp = threadIdx.x >> 5;
   const int64_t r0 = (static_cast<int64_t>(band) * kWarps + warp) * e.warp_rows;
-  const int64_t c0 = static_cast<int64_t>(strip) * kStrip;
+  const int64_t c0 = static_cast<int64_t>(strip) * e.strip;
   float* row_part = e.row_part + static_cast<int64_t>(strip) * e.rows;
-  float col[8];
   if (e.st == BERGSON_STATE_8BIT) {
-    if (e.vec) take_rows<true, true>(e, r0, c0, row_part, col);
-    else take_rows<true, false>(e, r0, c0, row_part, col);
+    if (e.vec) take_tile<true, true>(e, r0, c0, row_part, cols[warp]);
+    else take_tile<true, false>(e, r0, c0, row_part, cols[warp]);
   } else {
-    if (e.vec) take_rows<false, true>(e, r0, c0, row_part, col);
-    else take_rows<false, false>(e, r0, c0, row_part, col);
+    if (e.vec) take_tile<false, true>(e, r0, c0, row_part, cols[warp]);
+    else take_tile<false, false>(e, r0, c0, row_part, cols[warp]);
   }
-#pragma unroll
-  for (int j = 0; j < 8; ++j)
-    cols[warp][e.vec || e.st == BERGSON_STATE_8BIT ? 8 * lane + j : lane + 32 * j] = col[j];
   __syncthreads();
-  float x = 0.0f;
+  float all = 0.0f;
+  for (int k = threadIdx.x; k < e.strip; k += kThreads) {
+    float x = 0.0f;
 #pragma unroll
-  for (int w = 0; w < kWarps; ++w) x += cols[w][threadIdx.x];
-  const int64_t c = c0 + threadIdx.x;
-  if (c < e.cols) e.col_part[static_cast<int64_t>(band) * e.cols + c] = x;
-  x = block_sum(x, red);
-  if (threadIdx.x == 0) e.tile_part[tile] = x;
+    for (int w = 0; w < kWarps; ++w) x += cols[w][k];
+    if (c0 + k < e.cols) e.col_part[static_cast<int64_t>(band) * e.cols + c0 + k] = x;
+    all += x;
+  }
+  all = block_sum(all, red);
+  if (threadIdx.x == 0) e.tile_part[tile] = all;
 }
-static_assert(kStrip == kThreads, "a thread sums a column of the tile");
 
 template <int N>
 __global__ void __launch_bounds__(kThreads) moment_finish_kernel(
@@ -286,17 +312,20 @@ int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 // Rows a warp takes of a matrix, by its own size alone (so that its sums are the same
 // in any company): as many as leave kTilesWanted tiles.
 constexpr int64_t kTilesWanted = 64;
+int strip_of(const bergson_moment_matrix& m) {
+  return m.state_kind == BERGSON_STATE_8BIT ? kStrip8 : kStrip32;
+}
 int warp_rows_of(const bergson_moment_matrix& m) {
   int rows = kMostRows;
   while (rows > kLeastRows &&
-         ceil_div(m.d_out, kWarps * rows) * ceil_div(m.d_in, kStrip) < kTilesWanted)
+         ceil_div(m.d_out, kWarps * rows) * ceil_div(m.d_in, strip_of(m)) < kTilesWanted)
     rows /= 2;
   return rows;
 }
 
 size_t floats_of(const bergson_moment_matrix& m) {
   const size_t bands = ceil_div(m.d_out, kWarps * warp_rows_of(m));
-  const size_t strips = ceil_div(m.d_in, kStrip);
+  const size_t strips = ceil_div(m.d_in, strip_of(m));
   return strips * m.d_out + bands * m.d_in + bands * strips;
 }
 
@@ -322,7 +351,7 @@ cudaError_t run_moments(const bergson_moment_matrix* m, int n, double correction
   for (int i = 0; i < n; ++i) {
     const int warp_rows = warp_rows_of(m[i]);
     const int64_t bands = ceil_div(m[i].d_out, kWarps * warp_rows);
-    const int64_t strips = ceil_div(m[i].d_in, kStrip);
+    const int64_t strips = ceil_div(m[i].d_in, strip_of(m[i]));
     const int64_t outs = ceil_div(m[i].d_out + m[i].d_in, kThreads);
     if (k == N ||
         (k > 0 && (p.tiles[k] + bands * strips > INT32_MAX || p.outs[k] + outs > INT32_MAX))) {
@@ -337,8 +366,10 @@ cudaError_t run_moments(const bergson_moment_matrix* m, int n, double correction
     e.r = m[i].r;
     e.c = m[i].c;
     e.st = m[i].state_kind;
-    e.vec = m[i].d_in % 8 == 0 &&
-            reinterpret_cast<uintptr_t>(m[i].v) % (e.st == BERGSON_STATE_8BIT ? 8 : 32) == 0;
+    const bool eight = e.st == BERGSON_STATE_8BIT;
+    e.vec = m[i].d_in % (eight ? 16 : 8) == 0 &&
+            reinterpret_cast<uintptr_t>(m[i].v) % (eight ? 16 : 32) == 0;
+    e.strip = strip_of(m[i]);
     e.warp_rows = warp_rows;
     e.bands = static_cast<int>(bands);
     e.strips = static_cast<int>(strips);
