@@ -154,17 +154,27 @@ __device__ __forceinline__ unsigned count_bytes(const uint8_t* p, int64_t n) {
 
 // ---------------------------------------------------------------- policy
 
-constexpr int kSegment = 1024;                 // tokens of a row a warp takes
+// Tokens of a row a warp takes: the longer ones where they are enough for all SMs twice.
+constexpr int kSegment = 1024, kShortSegment = 256;
+constexpr int64_t kLongItems = 2 * 152 * 32;
 constexpr int kCountSegment = 4096;            // mask bytes a warp counts at once
 constexpr int kCountCtas = 1216;
 constexpr int kPolicyPerSm = 4;                // CTAs of the policy kernel an SM holds
 constexpr int kFinishCtas = 152;
-constexpr int kSmallItems = 512;               // (row, segment) items of the one-launch form
-constexpr int64_t kSmallTokens = 1 << 15;      // ... and its tokens: each CTA counts them all
+// The one-launch form: at most so many (row, segment) items and rows, of shorter segments.
+constexpr int kSmallItems = 512;
+constexpr int kSmallThreads = 512, kSmallWarps = kSmallThreads / 32;
+constexpr int kSmallCount = 2048;              // mask bytes a warp counts at once there
 
 struct Totals {
   Sum2 loss, kl;
   unsigned long long clipped = 0, valid = 0;
+  __device__ __forceinline__ void add(const float4& v) {  // a segment's sums
+    loss.add(v.x);
+    kl.add(v.y);
+    clipped += static_cast<unsigned>(v.z);
+    valid += static_cast<unsigned>(v.w);
+  }
   __device__ __forceinline__ void add(const Totals& o) {
     loss.add(o.loss);
     kl.add(o.kl);
@@ -183,6 +193,7 @@ __device__ __forceinline__ Totals totals_sum(const Totals& t) {
 
 struct PolicyParams {
   bergson_policy_args a;
+  int segment;                                 // tokens of a row a warp takes
   int64_t segments, count_segments;            // per row
   unsigned* counts;            // valid tokens: per CTA (TOKEN_MEAN) or [B, count_segments]
   int n_counts;                // CTAs that counted (TOKEN_MEAN)
@@ -279,10 +290,10 @@ __device__ __forceinline__ float4 policy_segment(const PolicyParams& p, int64_t 
   const float minus_we = -w * p.ent;
   float loss = 0.0f, kls = 0.0f;
   int clipped = 0, valid = 0;
-  int t0 = seg * kSegment;
+  int t0 = seg * p.segment;
   Mask<4> next = load_mask<4, kVec>(mask, t0, T);
 #pragma unroll 1
-  for (int left = min(T - t0, kSegment); left > 0; left -= 128, t0 += 128) {
+  for (int left = min(T - t0, p.segment); left > 0; left -= 128, t0 += 128) {
     const Mask<4> m = next;
     if (left > 128) next = load_mask<4, kVec>(mask, t0 + 128, T);
     float lp[4], old[4], adv[4], ref[4], ent[4], d[4], dh[4];
@@ -340,13 +351,7 @@ __device__ __forceinline__ void write_stats(const PolicyParams& p, const Totals&
 template <typename F>
 __device__ __forceinline__ Totals row_totals(int64_t segments, F part) {
   Totals r;
-  for (int64_t i = threadIdx.x & 31; i < segments; i += 32) {
-    const float4 v = part(i);
-    r.loss.add(v.x);
-    r.kl.add(v.y);
-    r.clipped += static_cast<unsigned>(v.z);
-    r.valid += static_cast<unsigned>(v.w);
-  }
+  for (int64_t i = threadIdx.x & 31; i < segments; i += 32) r.add(part(i));
   return totals_sum(r);
 }
 
@@ -397,25 +402,34 @@ __global__ void __launch_bounds__(kThreads) policy_finish_kernel(const PolicyPar
   if (lane == 0) write_stats(p, t);
 }
 
-// The whole of a small batch in one cluster: each CTA counts every row's valid tokens, takes
-// its share of the segments and leaves their sums with the first, which finishes.
+// The whole of a small batch in one cluster: the CTAs count the rows' valid tokens together,
+// each takes its share of the segments and leaves their sums with the first, which finishes.
 template <bool kVec>
-__global__ void __launch_bounds__(kThreads) policy_small_kernel(const PolicyParams p) {
+__global__ void __launch_bounds__(kSmallThreads) policy_small_kernel(const PolicyParams p) {
   __shared__ unsigned counts[kSmallItems];               // per row
   __shared__ float4 sums[kSmallItems];
-  __shared__ Totals red[kWarps];
-  const int parts = static_cast<int>(cluster_size());
+  __shared__ Totals red[kSmallWarps];
+  const int parts = static_cast<int>(cluster_size()), rank = static_cast<int>(blockIdx.x);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const int B = static_cast<int>(p.a.B), segments = static_cast<int>(p.segments);
-  unsigned total = 0;
+  const int B = static_cast<int>(p.a.B), T = static_cast<int>(p.a.T);
+  const int segments = static_cast<int>(p.segments);
+  const bool counted = p.a.reduction != BERGSON_POLICY_SUM_NORM;
+  for (int b = threadIdx.x; b < B; b += kSmallThreads)
+    counts[b] = p.a.mask == nullptr ? static_cast<unsigned>(T) : 0u;
+  cluster_sync();                                        // every CTA has started, with zeros
   griddep_wait();
-  if (p.a.reduction != BERGSON_POLICY_SUM_NORM) {
-    for (int b = warp; b < B; b += kWarps) {
-      const unsigned c = p.a.mask == nullptr ? static_cast<unsigned>(p.a.T)
-                                             : count_bytes(p.a.mask + b * p.a.ld_mask, p.a.T);
-      if (lane == 0) counts[b] = c;
+  unsigned total = 0;
+  if (counted) {
+    if (p.a.mask != nullptr) {
+      const int per = (T + kSmallCount - 1) / kSmallCount;
+      for (int i = rank * kSmallWarps + warp; i < B * per; i += parts * kSmallWarps) {
+        const int b = i / per, t = (i - b * per) * kSmallCount;
+        const unsigned c =
+            count_bytes(p.a.mask + b * p.a.ld_mask + t, min(T - t, kSmallCount));
+        if (lane < parts) add_cluster(&counts[b], lane, c);
+      }
+      cluster_sync();
     }
-    __syncthreads();
     if (p.a.reduction == BERGSON_POLICY_TOKEN_MEAN) {
       for (int b = lane; b < B; b += 32) total += counts[b];
       total = __reduce_add_sync(0xffffffffu, total);
@@ -424,8 +438,7 @@ __global__ void __launch_bounds__(kThreads) policy_small_kernel(const PolicyPara
   const auto weight = [&](int b) {
     return weight_of(p, p.a.reduction == BERGSON_POLICY_SEQ_MEAN ? counts[b] : total);
   };
-  if (parts > 1) cluster_sync();                         // the first CTA has started
-  for (int i = static_cast<int>(blockIdx.x) * kWarps + warp; i < B * segments; i += parts * kWarps) {
+  for (int i = rank * kSmallWarps + warp; i < B * segments; i += parts * kSmallWarps) {
     const int b = i / segments;
     const float4 s = policy_segment<kVec>(p, b, i - b * segments, weight(b));
     if (lane < 4) {
@@ -433,28 +446,34 @@ __global__ void __launch_bounds__(kThreads) policy_small_kernel(const PolicyPara
       st_cluster(reinterpret_cast<float*>(&sums[i]) + lane, 0, x);
     }
   }
-  if (parts > 1) cluster_sync(); else __syncthreads();
-  if (blockIdx.x != 0) return;
+  cluster_sync();
+  if (rank != 0) return;
   Totals t;
-  for (int b = threadIdx.x; b < B; b += kThreads) {      // a row a thread
-    Sum2 l;
-    for (int i = b * segments; i < (b + 1) * segments; ++i) {
-      const float4 v = sums[i];
-      l.add(v.x);
-      t.kl.add(v.y);
-      t.clipped += static_cast<unsigned>(v.z);
-      t.valid += static_cast<unsigned>(v.w);
-    }
-    const float x = l.value() * weight(b);
+  const auto take_row = [&](int b, Totals r) {
+    const float x = r.loss.value() * weight(b);
     if (p.a.seq_loss != nullptr) p.a.seq_loss[b] = x;
-    t.loss.add(x);
+    r.loss = Sum2();
+    r.loss.add(x);
+    t.add(r);
+  };
+  if (segments <= 4) {                                   // a row a thread
+    for (int b = threadIdx.x; b < B; b += kSmallThreads) {
+      Totals r;
+      for (int i = b * segments; i < (b + 1) * segments; ++i) r.add(sums[i]);
+      take_row(b, r);
+    }
+  } else {                                               // a row a warp
+    for (int b = warp; b < B; b += kSmallWarps) {
+      const Totals r = row_totals(segments, [&](int64_t i) { return sums[b * segments + i]; });
+      if (lane == 0) take_row(b, r);
+    }
   }
   t = totals_sum(t);
   if (lane == 0) red[warp] = t;
   __syncthreads();
   if (threadIdx.x == 0) {
     t = red[0];
-    for (int w = 1; w < kWarps; ++w) t.add(red[w]);
+    for (int w = 1; w < kSmallWarps; ++w) t.add(red[w]);
     write_stats(p, t);
   }
 }
@@ -466,6 +485,9 @@ constexpr int kPairWarps = kPairThreads / 32;
 constexpr int kPairPerSm = 5, kPairPerSmRef = 4;
 constexpr int kPairCtas = 2;                   // CTAs an SM up to which a pair is split,
 constexpr int64_t kPairTokens = 2048;          // into shares of more than half of this
+
+constexpr int64_t kManyPairs = 608;            // pairs from which on
+constexpr int64_t kShortPair = 512;            // ... those of so few tokens go to a warp each
 
 struct PreferenceParams {
   bergson_preference_args a;
@@ -489,12 +511,13 @@ __device__ __forceinline__ void preference_f(int kind, float x, float beta, floa
   }
 }
 
-// A CTA's sums over its share [t0, t1) of a pair's rows (both multiples of 256, but for T).
-template <int N, bool kVec, bool kRef>
+// The sums over [t0, t1) of a pair's rows (both multiples of 256, but for T) by a group of
+// kGroup warps: a warp by itself, or the CTA through red and counts.
+template <int N, bool kVec, bool kRef, int kGroup>
 __device__ __forceinline__ void pair_sums(const PreferenceParams& p, int64_t pair, int t0, int t1,
                                           Sum2 (*red)[2], int (*counts)[2], Sum2* sum, int* count) {
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  constexpr int kStride = 32 * N * kPairWarps;
+  const int lane = threadIdx.x & 31, warp = kGroup == 1 ? 0 : threadIdx.x >> 5;
+  constexpr int kStride = 32 * N * kGroup;
   const uint8_t* mask[2];
   const float* x[2];
   const float* ref[2];
@@ -541,18 +564,22 @@ __device__ __forceinline__ void pair_sums(const PreferenceParams& p, int64_t pai
   for (int k = 0; k < 2; ++k) {
     s[k] = warp_sum(s[k]);
     n[k] = __reduce_add_sync(0xffffffffu, n[k]);
-    if (lane == 0) {
+    if (kGroup == 1) {
+      sum[k] = s[k];
+      count[k] = n[k];
+    } else if (lane == 0) {
       red[warp][k] = s[k];
       counts[warp][k] = n[k];
     }
   }
+  if (kGroup == 1) return;
   __syncthreads();
 #pragma unroll
   for (int k = 0; k < 2; ++k) {
     sum[k] = red[0][k];
     count[k] = counts[0][k];
 #pragma unroll
-    for (int w = 1; w < kPairWarps; ++w) {
+    for (int w = 1; w < kGroup; ++w) {
       sum[k].add(red[w][k]);
       count[k] += counts[w][k];
     }
@@ -590,11 +617,11 @@ __device__ __forceinline__ PairGrad pair_grad(const bergson_preference_args& a, 
   return o;
 }
 
-template <int N, bool kVec>
+template <int N, bool kVec, int kGroup>
 __device__ __forceinline__ void write_pair(const PreferenceParams& p, int64_t pair, int t0, int t1,
                                            const float* d) {
-  const int warp = threadIdx.x >> 5;
-  constexpr int kStride = 32 * N * kPairWarps;
+  const int warp = kGroup == 1 ? 0 : threadIdx.x >> 5;
+  constexpr int kStride = 32 * N * kGroup;
   const uint8_t* mask[2];
   float* out[2];
 #pragma unroll
@@ -617,6 +644,29 @@ __device__ __forceinline__ void write_pair(const PreferenceParams& p, int64_t pa
   }
 }
 
+__device__ __forceinline__ void write_rewards(const bergson_preference_args& a, int64_t pair,
+                                              const PairGrad& g) {
+  a.pair_loss[pair] = g.loss;
+  if (a.rewards == nullptr) return;
+  a.rewards[pair] = g.reward[0];
+  a.rewards[pair + a.P] = g.reward[1];
+}
+
+// Many short pairs: one a warp.
+template <int N, bool kVec, bool kRef>
+__global__ void __launch_bounds__(kPairThreads) preference_warp_kernel(const PreferenceParams p) {
+  const int64_t pair = static_cast<int64_t>(blockIdx.x) * kPairWarps + (threadIdx.x >> 5);
+  griddep_wait();
+  if (pair >= p.a.P) return;
+  const int T = static_cast<int>(p.a.T);
+  Sum2 sum[2];
+  int count[2];
+  pair_sums<N, kVec, kRef, 1>(p, pair, 0, T, nullptr, nullptr, sum, count);
+  const PairGrad g = pair_grad(p.a, sum, count);
+  if ((threadIdx.x & 31) == 0) write_rewards(p.a, pair, g);
+  write_pair<N, kVec, 1>(p, pair, 0, T, g.d);
+}
+
 // kTogether: a pair a CTA, all of them in one cluster, whose first CTA adds the losses.
 // Else a pair a cluster, its CTAs each a share of the tokens.
 template <int N, bool kVec, bool kRef, bool kTogether>
@@ -635,7 +685,7 @@ __global__ void __launch_bounds__(kPairThreads, kRef ? kPairPerSmRef : kPairPerS
   Sum2 sum[2];
   int count[2] = {};
   griddep_wait();
-  if (live) pair_sums<N, kVec, kRef>(p, pair, t0, t1, red, counts, sum, count);
+  if (live) pair_sums<N, kVec, kRef, kPairWarps>(p, pair, t0, t1, red, counts, sum, count);
   if (!kTogether && parts > 1) {
     cluster_sync();                            // every CTA has started
     if (threadIdx.x < parts) {
@@ -662,16 +712,10 @@ __global__ void __launch_bounds__(kPairThreads, kRef ? kPairPerSmRef : kPairPerS
   PairGrad g = {};
   if (live) {
     g = pair_grad(p.a, sum, count);
-    if (threadIdx.x == 0 && (kTogether || rank == 0)) {
-      p.a.pair_loss[pair] = g.loss;
-      if (p.a.rewards != nullptr) {
-        p.a.rewards[pair] = g.reward[0];
-        p.a.rewards[pair + p.a.P] = g.reward[1];
-      }
-    }
+    if (threadIdx.x == 0 && (kTogether || rank == 0)) write_rewards(p.a, pair, g);
   }
 
-  if (live) write_pair<N, kVec>(p, pair, t0, t1, g.d);
+  if (live) write_pair<N, kVec, kPairWarps>(p, pair, t0, t1, g.d);
   if (kTogether) {
     cluster_sync();                            // every CTA has started
     if (threadIdx.x == 0) st_cluster(&shared[rank][0], 0, g.loss);
@@ -728,12 +772,12 @@ cudaError_t launch_cluster(K kernel, int64_t grid, int threads, int cluster, con
 
 template <bool kVec>
 cudaError_t run_policy(PolicyParams p, cudaStream_t s) {
-  const int64_t items = p.a.B * p.segments;
-  if (items <= kSmallItems && p.a.B <= kSmallItems && p.a.B * p.a.T <= kSmallTokens) {
+  if (p.a.B * ceil_div(p.a.T, kShortSegment) <= kSmallItems) {
     int parts = 1;
-    while (parts < 8 && parts * kWarps < items) parts *= 2;
-    return launch_cluster(policy_small_kernel<kVec>, parts, kThreads, parts, p, s);
+    while (parts < 8 && parts * kSmallWarps < p.a.B * p.segments) parts *= 2;
+    return launch_cluster(policy_small_kernel<kVec>, parts, kSmallThreads, parts, p, s);
   }
+  const int64_t items = p.a.B * p.segments;
   if (p.a.mask != nullptr && p.a.reduction != BERGSON_POLICY_SUM_NORM) {
     p.n_counts = static_cast<int>(
         std::min<int64_t>(kCountCtas, ceil_div(p.a.B * p.count_segments, kWarps)));
@@ -760,7 +804,13 @@ cudaError_t run_preference(const PreferenceParams& p, int sms, cudaStream_t s) {
   }
   int parts = 1;
   while (parts < 8 && P * parts < kPairCtas * sms && p.a.T / parts > kPairTokens) parts *= 2;
-  cudaError_t e = launch_cluster(preference_kernel<N, kVec, kRef, false>, P * parts, kPairThreads, parts, p, s);
+  cudaError_t e;
+  if (P >= kManyPairs && p.a.T <= kShortPair)
+    e = launch_dependent(preference_warp_kernel<N, kVec, kRef>,
+                         dim3(static_cast<unsigned>(ceil_div(P, kPairWarps))), dim3(kPairThreads), 0,
+                         s, p);
+  else
+    e = launch_cluster(preference_kernel<N, kVec, kRef, false>, P * parts, kPairThreads, parts, p, s);
   if (e != cudaSuccess) return e;
   return launch_dependent(preference_finish_kernel, dim3(1), dim3(1024), 0, s,
                           static_cast<const float*>(p.a.pair_loss), P, p.a.loss);
@@ -777,13 +827,14 @@ cudaError_t run_preference(const PreferenceParams& p, int sms, cudaStream_t s) {
 // counts, the totals and their ticket, the segments' sums
 size_t policy_workspace(int64_t B, int64_t T) {
   return counts_bytes(B, T) + align256(sizeof(Totals) * kFinishCtas) + 256 +
-         align256(sizeof(float4) * static_cast<size_t>(B) * static_cast<size_t>(ceil_div(T, kSegment)));
+         align256(sizeof(float4) * static_cast<size_t>(B) * static_cast<size_t>(ceil_div(T, kShortSegment)));
 }
 
 cudaError_t launch_policy_loss(const bergson_policy_args& a, void* ws, cudaStream_t s) {
   PolicyParams p;
   p.a = a;
-  p.segments = ceil_div(a.T, kSegment);
+  p.segment = a.B * ceil_div(a.T, kSegment) >= kLongItems ? kSegment : kShortSegment;
+  p.segments = ceil_div(a.T, p.segment);
   p.count_segments = ceil_div(a.T, kCountSegment);
   p.n_counts = 0;
   char* at = static_cast<char*>(ws);

@@ -168,6 +168,13 @@ __device__ __forceinline__ void st_cluster(float* p, uint32_t rank, float v) {
                : "memory");
 }
 
+// Adds to a word of the shared memory of the cluster's CTA `rank`.
+__device__ __forceinline__ void add_cluster(unsigned* p, uint32_t rank, unsigned v) {
+  asm volatile("red.relaxed.cluster.shared::cluster.add.u32 [%0], %1;" ::"r"(
+                   mapa_shared(smem_u32(p), rank)), "r"(v)
+               : "memory");
+}
+
 // Kahan-compensated running sum.
 struct CompensatedSum {
   float s = 0.0f, c = 0.0f;
