@@ -627,14 +627,21 @@ def bergson_debug_xgemm_plan(B: int, Q: int, K: int) -> dict:
 # ------------------------------------------------------------------ training side
 
 _DTYPES = {}
+_F32 = _I64 = _U8 = None
+
+
+def _load_dtypes() -> None:
+    global _F32, _I64, _U8
+    import torch
+    _F32, _I64, _U8 = torch.float32, torch.int64, torch.uint8
+    _DTYPES.update({torch.float32: BERGSON_F32, torch.bfloat16: BERGSON_BF16,
+                    torch.float16: BERGSON_F16})
 
 
 def _dtype(t) -> int:
     """The bergson_dtype of a torch tensor."""
     if not _DTYPES:
-        import torch
-        _DTYPES.update({torch.float32: BERGSON_F32, torch.bfloat16: BERGSON_BF16,
-                        torch.float16: BERGSON_F16})
+        _load_dtypes()
     code = _DTYPES.get(t.dtype)
     if code is None:
         raise TypeError(f"expected float32, bfloat16 or float16, got {t.dtype}")
@@ -649,40 +656,51 @@ def _rows(t, what: str) -> tuple[int, int]:
     return t.data_ptr(), ld if t.shape[0] > 1 else max(ld, t.shape[1])
 
 
-def _opt_rows(t, what: str) -> tuple[Optional[int], int]:
-    return (None, 0) if t is None else _rows(t, what)
+def _rows_like(t, what: str, dtype, shape) -> tuple[Optional[int], int]:
+    """_rows() of a matrix of this type and shape; None passes as NULL."""
+    if t is None:
+        return None, 0
+    if t.dtype is not dtype or t.shape != shape:
+        raise ValueError(f"{what} must be {dtype} of shape {tuple(shape)}, got {t.dtype} of "
+                         f"shape {tuple(t.shape)}")
+    return _rows(t, what)
 
 
-def _need(t, name: str, dtype: str, shape=None) -> None:
-    """Raises unless t has this torch dtype and, where given, this shape."""
-    if str(t.dtype) != dtype:
-        raise TypeError(f"{name} must be {dtype}, got {t.dtype}")
-    if shape is not None and tuple(t.shape) != tuple(shape):
-        raise ValueError(f"{name} must have shape {tuple(shape)}, got {tuple(t.shape)}")
+def _vector(t, what: str, dtype, n: int) -> Optional[int]:
+    """The device pointer of n consecutive elements; None passes as NULL."""
+    if t is None:
+        return None
+    if t.dtype is not dtype or t.numel() != n or not t.is_contiguous():
+        raise ValueError(f"{what} must be {dtype}, contiguous and of {n} elements, got {t.dtype} "
+                         f"of shape {tuple(t.shape)}")
+    return t.data_ptr()
 
 
 def bergson_token_logprobs(logits, targets, tau: float, logp, lse, entropy=None,
                            stream=None) -> None:
     """logp[r] = logits[r, targets[r]] / tau - lse[r] (and entropies); targets < 0 leave a row out."""
     rows, V = logits.shape
+    dtype = _dtype(logits)
     x, ld = _rows(logits, "logits")
-    _check(lib().bergson_token_logprobs(x, _dtype(logits), rows, V, ld, targets.data_ptr(), tau,
-                                        logp.data_ptr(), lse.data_ptr(), _ptr(entropy),
-                                        _stream(stream)))
+    _check(lib().bergson_token_logprobs(x, dtype, rows, V, ld,
+                                        _vector(targets, "targets", _I64, rows), tau,
+                                        _vector(logp, "logp", _F32, rows),
+                                        _vector(lse, "lse", _F32, rows),
+                                        _vector(entropy, "entropy", _F32, rows), _stream(stream)))
 
 
 def bergson_token_logprobs_backward(logits, targets, tau: float, lse, entropy, d_logp, d_entropy,
                                     d_logits, stream=None) -> None:
     """d_logits from the gradients at logp and entropy (either may be None)."""
     rows, V = logits.shape
+    dtype = _dtype(logits)
     x, ld = _rows(logits, "logits")
-    d, ld_d = _rows(d_logits, "d_logits")
-    if d_logits.dtype != logits.dtype or d_logits.shape != logits.shape:
-        raise ValueError("d_logits must have the logits' type and shape")
-    _check(lib().bergson_token_logprobs_backward(x, _dtype(logits), rows, V, ld,
-                                                 targets.data_ptr(), tau, lse.data_ptr(),
-                                                 _ptr(entropy), _ptr(d_logp), _ptr(d_entropy), d,
-                                                 ld_d, _stream(stream)))
+    d, ld_d = _rows_like(d_logits, "d_logits", logits.dtype, logits.shape)
+    _check(lib().bergson_token_logprobs_backward(
+        x, dtype, rows, V, ld, _vector(targets, "targets", _I64, rows), tau,
+        _vector(lse, "lse", _F32, rows), _vector(entropy, "entropy", _F32, rows),
+        _vector(d_logp, "d_logp", _F32, rows), _vector(d_entropy, "d_entropy", _F32, rows), d, ld_d,
+        _stream(stream)))
 
 
 def bergson_policy_loss_workspace(B: int, T: int) -> int:
@@ -699,20 +717,26 @@ def bergson_policy_loss(logp, old_logp, ref_logp, entropy, advantages, mask, cli
     sequences' shares, statistics and the gradients at logp and entropy.
     advantages: [B] (one a sequence) or [B, T]; ref_logp, entropy, mask,
     seq_loss, stats and d_entropy may be None."""
-    B, T = logp.shape
-    x, ld = _rows(logp, "logp")
-    old, ld_old = _rows(old_logp, "old_logp")
-    ref, ld_ref = _opt_rows(ref_logp, "ref_logp")
-    ent, ld_ent = _opt_rows(entropy, "entropy")
-    adv, ld_adv = (advantages.data_ptr(), 0) if advantages.dim() == 1 else _rows(advantages,
-                                                                                 "advantages")
-    on, ld_mask = _opt_rows(mask, "mask")
-    d, ld_d = _rows(d_logp, "d_logp")
-    de, ld_de = _opt_rows(d_entropy, "d_entropy")
+    if not _DTYPES:
+        _load_dtypes()
+    shape = logp.shape
+    B, T = shape
+    x, ld = _rows_like(logp, "logp", _F32, shape)
+    old, ld_old = _rows_like(old_logp, "old_logp", _F32, shape)
+    ref, ld_ref = _rows_like(ref_logp, "ref_logp", _F32, shape)
+    ent, ld_ent = _rows_like(entropy, "entropy", _F32, shape)
+    if advantages.dim() == 1:
+        adv, ld_adv = _vector(advantages, "advantages", _F32, B), 0
+    else:
+        adv, ld_adv = _rows_like(advantages, "advantages", _F32, shape)
+    on, ld_mask = _rows_like(mask, "mask", _U8, shape)
+    d, ld_d = _rows_like(d_logp, "d_logp", _F32, shape)
+    de, ld_de = _rows_like(d_entropy, "d_entropy", _F32, shape)
     args = bergson_policy_args(x, old, ref, ent, adv, on, ld, ld_old, ld_ref, ld_ent, ld_adv,
                                ld_mask, B, T, clip_low, clip_high, kl_coef, entropy_coef,
-                               norm_tokens, loss.data_ptr(), _ptr(seq_loss), _ptr(stats), d, de,
-                               ld_d, ld_de, reduction, 0)
+                               norm_tokens, _vector(loss, "loss", _F32, 1),
+                               _vector(seq_loss, "seq_loss", _F32, B),
+                               _vector(stats, "stats", _F32, 3), d, de, ld_d, ld_de, reduction, 0)
     _check(lib().bergson_policy_loss(args, workspace.data_ptr(),
                                      workspace.numel() * workspace.element_size(),
                                      _stream(stream)))
@@ -724,16 +748,22 @@ def bergson_preference_loss(logp, ref_logp, mask, kind: int, beta: float, margin
     """Preference loss over pairs (rows p and P + p of logp [2P, T]): the loss,
     the pairs' losses, rewards and the gradient at logp.  ref_logp, mask and
     rewards may be None."""
-    rows, T = logp.shape
+    if not _DTYPES:
+        _load_dtypes()
+    shape = logp.shape
+    rows, T = shape
     if rows % 2:
         raise ValueError("logp must have an even number of rows")
-    x, ld = _rows(logp, "logp")
-    ref, ld_ref = _opt_rows(ref_logp, "ref_logp")
-    on, ld_mask = _opt_rows(mask, "mask")
-    d, ld_d = _rows(d_logp, "d_logp")
-    args = bergson_preference_args(x, ref, on, ld, ld_ref, ld_mask, rows // 2, T, beta, margin,
-                                   label_smoothing, loss.data_ptr(), pair_loss.data_ptr(),
-                                   _ptr(rewards), d, ld_d, kind, 1 if mean_logp else 0)
+    P = rows // 2
+    x, ld = _rows_like(logp, "logp", _F32, shape)
+    ref, ld_ref = _rows_like(ref_logp, "ref_logp", _F32, shape)
+    on, ld_mask = _rows_like(mask, "mask", _U8, shape)
+    d, ld_d = _rows_like(d_logp, "d_logp", _F32, shape)
+    args = bergson_preference_args(x, ref, on, ld, ld_ref, ld_mask, P, T, beta, margin,
+                                   label_smoothing, _vector(loss, "loss", _F32, 1),
+                                   _vector(pair_loss, "pair_loss", _F32, P),
+                                   _vector(rewards, "rewards", _F32, rows), d, ld_d, kind,
+                                   1 if mean_logp else 0)
     _check(lib().bergson_preference_loss(args, _stream(stream)))
 
 
@@ -752,27 +782,22 @@ class AdamWTensor:
     weight_decay: float = 0.0
 
     def to_c(self) -> bergson_adamw_tensor:
+        if not _DTYPES:
+            _load_dtypes()
         n = self.param.numel()
         eight = self.m_scale is not None
         if eight != (self.v_scale is not None):
             raise ValueError("m_scale and v_scale must both be given or both be None")
-        blocks = (-(-n // BERGSON_STATE_BLOCK),)
-        state = "torch.uint8" if eight else "torch.float32"
-        for name, t, dtype, size in (
-                ("param", self.param, None, n), ("grad", self.grad, None, n),
-                ("master", self.master, "torch.float32", n), ("m", self.m, state, n),
-                ("v", self.v, state, n), ("m_scale", self.m_scale, "torch.float32", blocks[0]),
-                ("v_scale", self.v_scale, "torch.float32", blocks[0])):
-            if t is None:
-                continue
-            if dtype is not None:
-                _need(t, name, dtype)
-            if t.numel() != size or not t.is_contiguous():
-                raise ValueError(f"{name} must be contiguous and hold {size} elements")
+        blocks, state = -(-n // BERGSON_STATE_BLOCK), _U8 if eight else _F32
+        param = _vector(self.param, "param", self.param.dtype, n)
+        grad = _vector(self.grad, "grad", self.grad.dtype, n)
+        master = _vector(self.master, "master", _F32, n)
+        m, v = _vector(self.m, "m", state, n), _vector(self.v, "v", state, n)
+        ms = _vector(self.m_scale, "m_scale", _F32, blocks)
+        vs = _vector(self.v_scale, "v_scale", _F32, blocks)
         return bergson_adamw_tensor(
-            _ptr(self.param), _ptr(self.grad), _ptr(self.master), _ptr(self.m), _ptr(self.v),
-            _ptr(self.m_scale), _ptr(self.v_scale), n, float(self.lr_scale),
-            float(self.weight_decay), _dtype(self.param), _dtype(self.grad),
+            param, grad, master, m, v, ms, vs, n, float(self.lr_scale), float(self.weight_decay),
+            _dtype(self.param), _dtype(self.grad),
             BERGSON_STATE_8BIT if eight else BERGSON_STATE_F32, 0)
 
 
@@ -780,10 +805,7 @@ def _records(kind, items) -> "ctypes.Array":
     """The C array of a list of records; one that is an array already is returned."""
     if isinstance(items, ctypes.Array):
         return items
-    arr = (kind * len(items))()
-    for i, item in enumerate(items):
-        arr[i] = item if isinstance(item, kind) else item.to_c()
-    return arr
+    return (kind * len(items))(*[x if isinstance(x, kind) else x.to_c() for x in items])
 
 
 def bergson_adamw_tensors(tensors: Sequence) -> "ctypes.Array":
@@ -802,11 +824,12 @@ def bergson_adamw_step(tensors, lr: float, beta1: float, beta2: float, eps: floa
 
 def bergson_adamw_state_values(codes, scale, moment: int, out, stream=None) -> None:
     """out = the fp32 values of an 8-bit state (moment: BERGSON_MOMENT_FIRST or _SECOND)."""
+    if not _DTYPES:
+        _load_dtypes()
     n = codes.numel()
-    if out.numel() != n or scale.numel() < -(-n // BERGSON_STATE_BLOCK):
-        raise ValueError("out must hold a value per code and scale one per block of codes")
-    _check(lib().bergson_adamw_state_values(codes.data_ptr(), scale.data_ptr(), n, moment,
-                                            out.data_ptr(), _stream(stream)))
+    _check(lib().bergson_adamw_state_values(
+        _vector(codes, "codes", _U8, n), _vector(scale, "scale", _F32, -(-n // BERGSON_STATE_BLOCK)),
+        n, moment, _vector(out, "out", _F32, n), _stream(stream)))
 
 
 @dataclasses.dataclass
@@ -818,18 +841,15 @@ class MomentMatrix:
     v_scale: object = None
 
     def to_c(self) -> bergson_moment_matrix:
+        if not _DTYPES:
+            _load_dtypes()
         d_out, d_in = self.v.shape
-        _need(self.v, "v", "torch.float32" if self.v_scale is None else "torch.uint8")
-        _need(self.r, "r", "torch.float32", (d_out,))
-        _need(self.c, "c", "torch.float32", (d_in,))
-        if self.v_scale is not None:
-            _need(self.v_scale, "v_scale", "torch.float32",
-                  (-(-d_out * d_in // BERGSON_STATE_BLOCK),))
-        if not (self.v.is_contiguous() and self.r.is_contiguous() and self.c.is_contiguous()):
-            raise ValueError("v, r and c must be contiguous")
+        n = d_out * d_in
+        v = _vector(self.v, "v", _F32 if self.v_scale is None else _U8, n)
+        vs = _vector(self.v_scale, "v_scale", _F32, -(-n // BERGSON_STATE_BLOCK))
+        r, c = _vector(self.r, "r", _F32, d_out), _vector(self.c, "c", _F32, d_in)
         return bergson_moment_matrix(
-            _ptr(self.v), _ptr(self.v_scale), d_out, d_in, _ptr(self.r), _ptr(self.c),
-            BERGSON_STATE_F32 if self.v_scale is None else BERGSON_STATE_8BIT, 0)
+            v, vs, d_out, d_in, r, c, BERGSON_STATE_F32 if self.v_scale is None else BERGSON_STATE_8BIT, 0)
 
 
 def bergson_moment_matrices(mats: Sequence) -> "ctypes.Array":

@@ -334,3 +334,20 @@ def test_preference_nothing():
     assert run_preference(z, None, None)["loss"] == 0
     got = run_preference(np.zeros((4, 0), np.float32), None, None)
     np.testing.assert_allclose(got["pair"], np.log(2), rtol=1e-6)
+
+
+@pytest.mark.parametrize("reduction", REDUCTIONS)
+@pytest.mark.parametrize("B,T", [(512, 256), (513, 256), (512, 257), (2, 65_536), (1, 131_073),
+                                 (256, 300), (9800, 40), (20, 7000)])
+def test_policy_at_the_launches_limits(B, T, reduction):
+    """One launch of a cluster up to 512 segments of 256 tokens; longer segments from 9728 on."""
+    check_policy(policy_inputs(B, T, seed=B), reduction=reduction)
+
+
+@pytest.mark.parametrize("ref", [True, False])
+@pytest.mark.parametrize("P,T", [(607, 512), (608, 512), (608, 513), (700, 511), (1500, 1), (8, 4096),
+                                 (8, 4097), (9, 64), (2, 16_400)])
+def test_preference_at_the_launches_limits(P, T, ref):
+    """A warp a pair, a cluster of pairs, a CTA and a cluster a pair."""
+    logp, r, mask = preference_inputs(P, T, seed=P)
+    check_preference(logp, r if ref else None, mask)

@@ -297,3 +297,17 @@ def test_no_rows():
     bg.bergson_token_logprobs(x, torch.empty(0, dtype=torch.int64, device=DEV), 1.0, e, e, e)
     bg.bergson_token_logprobs_backward(x, torch.empty(0, dtype=torch.int64, device=DEV), 1.0, e, e,
                                        e, e, x)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("R,V", [(1300, 3001), (1217, 2561)])
+def test_many_rows_of_middling_length(R, V, dtype):
+    """Rows of 4 to 16 KB, enough of them to go to warps."""
+    x, t = logits(R, V, dtype, seed=V)
+    t[::7] = -1
+    check_forward(x, t, 0.9)
+    g = np.random.default_rng(R)
+    w = g.normal(size=R)
+    w[::5] = 0.0
+    check_backward(x, t, 0.9, w, None)
+    check_backward(x, t, 0.9, w, 0.1 * w)

@@ -260,15 +260,31 @@ def test_binding_refuses_what_it_cannot_pass_on():
     with pytest.raises(ValueError):                       # a scale per 256 elements
         u = torch.zeros(300, dtype=torch.uint8)
         bg.AdamWTensor(p, p, u, u, m_scale=torch.zeros(1), v_scale=torch.zeros(2)).to_c()
-    with pytest.raises(TypeError):
+    with pytest.raises(ValueError):
         bg.AdamWTensor(p, p, p.half(), p).to_c()
+    with pytest.raises(ValueError):                       # 32-bit indices
+        bg.bergson_token_logprobs(f, i.int(), 1.0, f[:, 0].contiguous(), f[:, 0].contiguous())
+    with pytest.raises(ValueError):
+        bg.bergson_token_logprobs(f, i, 1.0, p[:3], p[:4])
+    with pytest.raises(ValueError):                       # a mask of another shape, of another type
+        bg.bergson_preference_loss(f, None, torch.ones((4, 5), dtype=torch.uint8), 0, 0.1, 0.0, 0.0,
+                                   False, p[:1], p[:2], None, f)
+    with pytest.raises(ValueError):
+        bg.bergson_preference_loss(f, None, torch.ones((4, 6), dtype=torch.bool), 0, 0.1, 0.0, 0.0,
+                                   False, p[:1], p[:2], None, f)
+    with pytest.raises(ValueError):
+        bg.bergson_policy_loss(f, f[:3], None, None, p[:4], None, 0.2, 0.2, 0.0, 0.0, 0, 1.0, p[:1],
+                               None, None, f, None, p)
+    with pytest.raises(ValueError):
+        bg.bergson_policy_loss(f, f, None, None, p[:3], None, 0.2, 0.2, 0.0, 0.0, 0, 1.0, p[:1],
+                               None, None, f, None, p)
     with pytest.raises(ValueError):
         bg.AdamWTensor(p, p[:10], p, p).to_c()
     with pytest.raises(ValueError):
         bg.AdamWTensor(torch.zeros(600)[::2], p, p, p).to_c()
     with pytest.raises(ValueError):
         bg.MomentMatrix(torch.zeros(4, 6), torch.zeros(5), torch.zeros(6)).to_c()
-    with pytest.raises(TypeError):
+    with pytest.raises(ValueError):
         bg.MomentMatrix(torch.zeros(4, 6), torch.zeros(4), torch.zeros(6), torch.zeros(1)).to_c()
 
 
