@@ -35,7 +35,7 @@ struct Entry {
   float* vs;
   int64_t n;
   uint64_t key;                // start of the tensor's SplitMix64 sequence
-  float lr, wd;                // lr lr_scale, weight decay
+  float lr_c1, lr_wd;          // lr lr_scale / (1 - beta1^step), lr lr_scale weight_decay
   uint8_t pt, gt, st;
   uint8_t vec;                 // every pointer fits loads of 8 elements
   uint8_t pad[4];
@@ -43,7 +43,7 @@ struct Entry {
 
 struct StepScalars {
   float b1, b2, a1, a2;        // beta, 1 - beta
-  float c1, c2, eps;           // bias corrections 1 / (1 - beta^step)
+  float c2, eps;               // 1 / (1 - beta2^step)
   int n;                       // tensors
   const float* grad_scale;
 };
@@ -119,12 +119,12 @@ __device__ __forceinline__ float next_first(const StepScalars& s, float m, float
 __device__ __forceinline__ float next_second(const StepScalars& s, float v, float g) {
   return __fadd_rn(__fmul_rn(v, s.b2), __fmul_rn(__fmul_rn(g, g), s.a2));
 }
-// The root of a v below the normal range counts as that of the range's end, 1e-19.
+// w - lr (c1 m / (sqrt(c2 v) + eps) + wd w).  The root counts at least as that of the
+// normal range's end, 1e-19: 0 / 0 cannot arise.
 __device__ __forceinline__ float next_weight(const StepScalars& s, const Entry& e, float w, float m,
                                              float v) {
-  const float root = sqrt_approx(fmaxf(v * s.c2, 1.17549435e-38f));
-  const float up = m * s.c1 * rcp_approx(root + s.eps);
-  return w - e.lr * fmaf(e.wd, w, up);
+  const float root = sqrt_approx(fmaf(v, s.c2, 1.17549435e-38f));
+  return fmaf(-e.lr_c1 * m, rcp_approx(root + s.eps), fmaf(-e.lr_wd, w, w));
 }
 __device__ __forceinline__ float block_top(float top) {     // of the warp's lanes, NaN the largest
   return __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(top)));
@@ -282,7 +282,7 @@ __device__ __noinline__ void block_elements(const StepScalars& s, const Entry& e
 }
 
 template <int N>
-__global__ void __launch_bounds__(kThreads) adamw_kernel(const __grid_constant__ StepParams<N> p) {
+__global__ void __launch_bounds__(kThreads, 9) adamw_kernel(const __grid_constant__ StepParams<N> p) {
   int lo = 0, hi = p.s.n;                        // begin[lo] <= CTA < begin[hi]
   while (hi - lo > 1) {
     const int mid = (lo + hi) / 2;
@@ -347,7 +347,7 @@ cudaError_t run_adamw(const bergson_adamw_tensor* t, int n, const AdamwScalars& 
   p.s.b2 = static_cast<float>(a.beta2);
   p.s.a1 = static_cast<float>(1.0 - a.beta1);
   p.s.a2 = static_cast<float>(1.0 - a.beta2);
-  p.s.c1 = static_cast<float>(1.0 / (1.0 - std::pow(a.beta1, static_cast<double>(a.step))));
+  const double c1 = 1.0 / (1.0 - std::pow(a.beta1, static_cast<double>(a.step)));
   p.s.c2 = static_cast<float>(1.0 / (1.0 - std::pow(a.beta2, static_cast<double>(a.step))));
   p.s.eps = static_cast<float>(a.eps);
   p.s.grad_scale = a.grad_scale;
@@ -379,8 +379,8 @@ cudaError_t run_adamw(const bergson_adamw_tensor* t, int n, const AdamwScalars& 
     e.vs = t[i].v_scale;
     e.n = t[i].n;
     e.key = mix64(static_cast<uint64_t>(i) ^ base);
-    e.lr = static_cast<float>(a.lr * t[i].lr_scale);
-    e.wd = t[i].weight_decay;
+    e.lr_c1 = static_cast<float>(a.lr * t[i].lr_scale * c1);
+    e.lr_wd = static_cast<float>(a.lr * t[i].lr_scale * t[i].weight_decay);
     e.pt = static_cast<uint8_t>(t[i].param_dtype);
     e.gt = static_cast<uint8_t>(t[i].grad_dtype);
     e.st = static_cast<uint8_t>(t[i].state_kind);
