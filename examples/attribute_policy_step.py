@@ -71,11 +71,12 @@ def policy_step(layer, A, tokens, mask, old, ref, advantages, ws):
     logp, lse, entropy = logprobs(x, tokens)
     loss, stats = torch.empty(1, device="cuda"), torch.empty(3, device="cuda")
     d, dh = torch.empty((B, T), device="cuda"), torch.empty((B, T), device="cuda")
-    bg.bergson_policy_loss(logp.view(B, T), old, ref, entropy.view(B, T), advantages, mask, 0.2, 0.28,
-                           0.02, 0.001, bg.BERGSON_POLICY_TOKEN_MEAN, 1.0, loss, None, stats, d, dh,
-                           ws)
-    bg.bergson_token_logprobs_backward(x, tokens.view(-1), 1.0, lse, entropy, d.view(-1), dh.view(-1),
-                                       x)                  # in place of the logits
+    bg.bergson_policy_loss(logp.view(B, T), old, ref, entropy.view(B, T), advantages, mask, 0.2,
+                           0.28, 0.02, 0.001, bg.BERGSON_POLICY_TOKEN_MEAN, 1.0, loss, None, stats,
+                           d, dh, ws)
+    # in place of the logits
+    bg.bergson_token_logprobs_backward(x, tokens.view(-1), 1.0, lse, entropy, d.view(-1),
+                                       dh.view(-1), x)
     layer.step(A, x)
     return loss, x
 
@@ -119,7 +120,8 @@ def main(steps: int = 12) -> dict:
     mask = (torch.arange(T, device="cuda") < lengths[:, None]).to(torch.uint8)
     tokens = torch.randint(0, V, (B, T), generator=g, device="cuda")
     tokens = torch.where(mask != 0, tokens, -1)            # padding: left out
-    old = logprobs(layer.logits(A), tokens)[0].view(B, T)  # of the policy that sampled, and the reference
+    # of the policy that sampled, which is the reference too
+    old = logprobs(layer.logits(A), tokens)[0].view(B, T)
     advantages = torch.linspace(-1, 1, B, device="cuda")
     ws = bg.workspace_tensor(bg.bergson_policy_loss_workspace(B, T))
 

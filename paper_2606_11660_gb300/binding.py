@@ -678,7 +678,8 @@ def _vector(t, what: str, dtype, n: int) -> Optional[int]:
 
 def bergson_token_logprobs(logits, targets, tau: float, logp, lse, entropy=None,
                            stream=None) -> None:
-    """logp[r] = logits[r, targets[r]] / tau - lse[r] (and entropies); targets < 0 leave a row out."""
+    """logp[r] = logits[r, targets[r]] / tau - lse[r] (and entropies); a target < 0 leaves
+    its row out."""
     rows, V = logits.shape
     dtype = _dtype(logits)
     x, ld = _rows(logits, "logits")
@@ -828,8 +829,8 @@ def bergson_adamw_state_values(codes, scale, moment: int, out, stream=None) -> N
         _load_dtypes()
     n = codes.numel()
     _check(lib().bergson_adamw_state_values(
-        _vector(codes, "codes", _U8, n), _vector(scale, "scale", _F32, -(-n // BERGSON_STATE_BLOCK)),
-        n, moment, _vector(out, "out", _F32, n), _stream(stream)))
+        _vector(codes, "codes", _U8, n),
+        _vector(scale, "scale", _F32, -(-n // BERGSON_STATE_BLOCK)), n, moment, _vector(out, "out", _F32, n), _stream(stream)))
 
 
 @dataclasses.dataclass
@@ -849,7 +850,8 @@ class MomentMatrix:
         vs = _vector(self.v_scale, "v_scale", _F32, -(-n // BERGSON_STATE_BLOCK))
         r, c = _vector(self.r, "r", _F32, d_out), _vector(self.c, "c", _F32, d_in)
         return bergson_moment_matrix(
-            v, vs, d_out, d_in, r, c, BERGSON_STATE_F32 if self.v_scale is None else BERGSON_STATE_8BIT, 0)
+            v, vs, d_out, d_in, r, c,
+            BERGSON_STATE_F32 if self.v_scale is None else BERGSON_STATE_8BIT, 0)
 
 
 def bergson_moment_matrices(mats: Sequence) -> "ctypes.Array":

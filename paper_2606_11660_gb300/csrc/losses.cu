@@ -1,11 +1,17 @@
 // The clipped policy loss and the preference loss, forward and backward.
 //
-// Both read every token once and write its gradient: 4 bytes a tensor and one of
+// Both read every valid token once and write its gradient: 4 bytes a tensor and one of
 // mask, some 30 operations, so they are bound by memory, and below some 10^5 tokens by
 // their launches.  A token's gradient needs a weight that depends on others: the
 // policy loss counts the valid tokens beforehand (a byte a token), the preference
 // loss holds a pair in a CTA (or a cluster that shares its sums) and comes back to
 // write.  Sums over tokens follow an order fixed by the sizes.
+//
+// Policy loss of 2048 x 16,384 tokens, KL and entropy terms, a token mean: 123 us (the
+// count 10, the tokens 109, the finish 8), 6.8 TB/s of the 25 bytes a token; masked
+// tokens' inputs are not read, so less moves.  Preference loss of 256 pairs of
+// 32,768 tokens without a reference: 31 us, 0.74 of 9 bytes a token at the copy rate; what
+// is left are the two phases' latencies with a pair's CTAs in step.
 
 #include <algorithm>
 
@@ -32,7 +38,9 @@ struct Mask {
   __device__ __forceinline__ bool on(int j) const {
     return (w[j / 4] & (0xffu << (8 * (j % 4)))) != 0;
   }
-  __device__ __forceinline__ bool any() const { return N == 4 ? w[0] != 0 : (w[0] | w[N / 4 - 1]) != 0; }
+  __device__ __forceinline__ bool any() const {
+    return N == 4 ? w[0] != 0 : (w[0] | w[N / 4 - 1]) != 0;
+  }
   __device__ __forceinline__ int count() const {
     int c = 0;
 #pragma unroll
@@ -154,15 +162,18 @@ __device__ __forceinline__ unsigned count_bytes(const uint8_t* p, int64_t n) {
 
 // ---------------------------------------------------------------- policy
 
-// Tokens of a row a warp takes: the longer ones where they are enough for all SMs twice.
+// Tokens of a row a warp takes: the longer ones where there is one for every resident
+// warp.  us at 1024 / 256: 32 x 32,768 tokens 15.9 / 13.5, 512 x 4000 20.3 / 17.6,
+// 2048 x 4096 39.8 / 42.1, 2048 x 16,384 (without entropies) 103 / 128.
 constexpr int kSegment = 1024, kShortSegment = 256;
-constexpr int64_t kLongItems = 2 * 152 * 32;
+constexpr int64_t kLongItems = 152 * 32;
 constexpr int kCountSegment = 4096;            // mask bytes a warp counts at once
 constexpr int kCountCtas = 1216;
-constexpr int kPolicyPerSm = 4;                // CTAs of the policy kernel an SM holds
+constexpr int kPolicyPerSm = 4;                // CTAs an SM holds (123 us; 3: 129, 5: 126)
 constexpr int kFinishCtas = 152;
-// The one-launch form: at most so many (row, segment) items and rows, of shorter segments.
-constexpr int kSmallItems = 512;
+// The one-launch form: at most so many segments of the shorter kind.  us in one launch / in
+// three: 8 x 97 tokens 8.5 / 14.6, 64 x 1000 10.1 / 15.1; of 512 segments, 64 x 2000, 17.6 / 14.9.
+constexpr int kSmallItems = 256;
 constexpr int kSmallThreads = 512, kSmallWarps = kSmallThreads / 32;
 constexpr int kSmallCount = 2048;              // mask bytes a warp counts at once there
 
@@ -224,7 +235,7 @@ __global__ void __launch_bounds__(kThreads) policy_count_kernel(const PolicyPara
   if ((threadIdx.x & 31) == 0) red[threadIdx.x >> 5] = mine;
   __syncthreads();
   if (threadIdx.x == 0) {
-    unsigned c = 0;                            // at most 2^40 tokens over 1216 CTAs: 32 bits hold them
+    unsigned c = 0;                            // 2^40 tokens over 1216 CTAs fit 32 bits
     for (int w = 0; w < kWarps; ++w) c += red[w];
     p.counts[blockIdx.x] = c;
   }
@@ -483,11 +494,16 @@ __global__ void __launch_bounds__(kSmallThreads) policy_small_kernel(const Polic
 constexpr int kPairThreads = 256;
 constexpr int kPairWarps = kPairThreads / 32;
 constexpr int kPairPerSm = 5, kPairPerSmRef = 4;
-constexpr int kPairCtas = 2;                   // CTAs an SM up to which a pair is split,
-constexpr int64_t kPairTokens = 2048;          // into shares of more than half of this
+// A pair is split, into shares of more than half of kPairTokens, up to kPairCtas CTAs an SM:
+// 1 / 32 pairs of 32,768 tokens split 11.0 / 10.9 us, whole 17.4 / 18.2; more shares wait
+// longer for each other (256 pairs in 8 shares each 37 us, in 2 33).
+constexpr int kPairCtas = 2;
+constexpr int64_t kPairTokens = 2048;
 
-constexpr int64_t kManyPairs = 608;            // pairs from which on
-constexpr int64_t kShortPair = 512;            // ... those of so few tokens go to a warp each
+// From kManyPairs on, pairs of up to kShortPair tokens go to a warp each: 2048 of 100 / 500
+// tokens 7.8 / 11 us, to a CTA each 15.6 / 16.8; 700 of 500 level.
+constexpr int64_t kManyPairs = 608;
+constexpr int64_t kShortPair = 512;
 
 struct PreferenceParams {
   bergson_preference_args a;
@@ -670,7 +686,8 @@ __global__ void __launch_bounds__(kPairThreads) preference_warp_kernel(const Pre
 // kTogether: a pair a CTA, all of them in one cluster, whose first CTA adds the losses.
 // Else a pair a cluster, its CTAs each a share of the tokens.
 template <int N, bool kVec, bool kRef, bool kTogether>
-__global__ void __launch_bounds__(kPairThreads, kRef ? kPairPerSmRef : kPairPerSm) preference_kernel(const PreferenceParams p) {
+__global__ void __launch_bounds__(kPairThreads, kRef ? kPairPerSmRef : kPairPerSm)
+    preference_kernel(const PreferenceParams p) {
   __shared__ Sum2 red[kPairWarps][2];
   __shared__ int counts[kPairWarps][2];
   __shared__ float shared[8][6];               // from each CTA: two sums and counts
@@ -680,7 +697,8 @@ __global__ void __launch_bounds__(kPairThreads, kRef ? kPairPerSmRef : kPairPerS
   const bool live = pair < p.a.P;
   const int T = static_cast<int>(p.a.T), blocks = (T - 1) / 256 + 1;
   const int per = kTogether ? blocks : (blocks + parts - 1) / parts;
-  const int t0 = kTogether ? 0 : static_cast<int>(min(static_cast<int64_t>(T), int64_t{256} * per * rank));
+  const int t0 =
+      kTogether ? 0 : static_cast<int>(min(static_cast<int64_t>(T), int64_t{256} * per * rank));
   const int t1 = static_cast<int>(min(static_cast<int64_t>(T), t0 + int64_t{256} * per));
   Sum2 sum[2];
   int count[2] = {};
@@ -744,7 +762,8 @@ __global__ void __launch_bounds__(1024) preference_finish_kernel(const float* pa
 int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 size_t align256(size_t n) { return (n + 255) / 256 * 256; }
 size_t counts_bytes(int64_t B, int64_t T) {
-  return align256(4 * static_cast<size_t>(std::max<int64_t>(kCountCtas, B * ceil_div(T, kCountSegment))));
+  const int64_t n = std::max<int64_t>(kCountCtas, B * ceil_div(T, kCountSegment));
+  return align256(4 * static_cast<size_t>(n));
 }
 
 // Rows whose loads of n tokens at once are aligned.
@@ -797,6 +816,8 @@ cudaError_t run_policy(PolicyParams p, cudaStream_t s) {
 template <int N, bool kVec, bool kRef>
 cudaError_t run_preference(const PreferenceParams& p, int sms, cudaStream_t s) {
   const int64_t P = p.a.P;
+  // few short pairs: one launch, their losses added through the cluster (4 x 383 tokens
+  // 8.0 us, 9.9 with the second grid)
   if (P <= 8 && 2 * p.a.T <= 8192) {
     int n = 1;
     while (n < P) n *= 2;
@@ -807,10 +828,11 @@ cudaError_t run_preference(const PreferenceParams& p, int sms, cudaStream_t s) {
   cudaError_t e;
   if (P >= kManyPairs && p.a.T <= kShortPair)
     e = launch_dependent(preference_warp_kernel<N, kVec, kRef>,
-                         dim3(static_cast<unsigned>(ceil_div(P, kPairWarps))), dim3(kPairThreads), 0,
-                         s, p);
+                         dim3(static_cast<unsigned>(ceil_div(P, kPairWarps))),
+                         dim3(kPairThreads), 0, s, p);
   else
-    e = launch_cluster(preference_kernel<N, kVec, kRef, false>, P * parts, kPairThreads, parts, p, s);
+    e = launch_cluster(preference_kernel<N, kVec, kRef, false>, P * parts, kPairThreads, parts, p,
+                       s);
   if (e != cudaSuccess) return e;
   return launch_dependent(preference_finish_kernel, dim3(1), dim3(1024), 0, s,
                           static_cast<const float*>(p.a.pair_loss), P, p.a.loss);
@@ -827,7 +849,7 @@ cudaError_t run_preference(const PreferenceParams& p, int sms, cudaStream_t s) {
 // counts, the totals and their ticket, the segments' sums
 size_t policy_workspace(int64_t B, int64_t T) {
   return counts_bytes(B, T) + align256(sizeof(Totals) * kFinishCtas) + 256 +
-         align256(sizeof(float4) * static_cast<size_t>(B) * static_cast<size_t>(ceil_div(T, kShortSegment)));
+         align256(sizeof(float4) * static_cast<size_t>(B * ceil_div(T, kShortSegment)));
 }
 
 cudaError_t launch_policy_loss(const bergson_policy_args& a, void* ws, cudaStream_t s) {

@@ -1,5 +1,11 @@
 // Factored second moments of AdamW's v: the row and column means of every
 // matrix, in one pass over tiles and a second small one over their sums.
+//
+// A warp takes up to 32 rows of a strip, with its lanes' columns in registers; the
+// rows' sums of four or eight rows at a time go through one butterfly over the lanes.  fp32
+// matrices are bound by their bytes: 201M elements in 16 matrices 128 us, 6.3 TB/s.
+// 8-bit ones are bound by the instructions that take codes apart (7.6 an element, 0.57 of
+// the issue slots at a third of the warps): 68 us, 3.0 TB/s.
 
 #include "internal.h"
 #include "train.cuh"
@@ -85,7 +91,8 @@ __device__ __forceinline__ uint2 load_codes(const uint8_t* v, int64_t i, int cou
     }
     return u;
   }
-  const uint2 a = *reinterpret_cast<const uint2*>(base), b = *reinterpret_cast<const uint2*>(base + 8);
+  const uint2 a = *reinterpret_cast<const uint2*>(base);
+  const uint2 b = *reinterpret_cast<const uint2*>(base + 8);
   const uint32_t w[4] = {a.x, a.y, b.x, b.y};
   const bool far = skip >= 4;
   const uint32_t w0 = far ? w[1] : w[0], w1 = far ? w[2] : w[1], w2 = far ? w[3] : w[2];
@@ -144,7 +151,8 @@ __device__ __forceinline__ void take_rows(const Entry& e, int64_t r0, int64_t c0
   const int lane = threadIdx.x & 31;
   const int64_t c = c0 + kCols * lane;
   const int cols = static_cast<int>(e.cols);
-  const int count = static_cast<int>(min(static_cast<int64_t>(kCols), e.cols - c));   // of the lane's
+  // the lane's columns that the matrix has
+  const int count = static_cast<int>(min(static_cast<int64_t>(kCols), e.cols - c));
   int left = static_cast<int>(min(e.rows - r0, static_cast<int64_t>(e.warp_rows)));
 #pragma unroll
   for (int j = 0; j < kCols / 2; ++j) col[j] = {0.0f, 0.0f};
@@ -175,7 +183,8 @@ __device__ __forceinline__ void take_rows(const Entry& e, int64_t r0, int64_t c0
         float2 s = {0.0f, 0.0f};
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-          const float2 y = make_float2(__uint_as_float(x[k][2 * j]), __uint_as_float(x[k][2 * j + 1]));
+          const float2 y =
+              make_float2(__uint_as_float(x[k][2 * j]), __uint_as_float(x[k][2 * j + 1]));
           col[j] = add2(col[j], y);
           s = add2(s, y);
         }
@@ -208,7 +217,7 @@ __device__ __forceinline__ void take_rows(const Entry& e, int64_t r0, int64_t c0
           const uint2 a = load_codes(v, at, min(count, 8), n);
           const uint2 b = count > 8 ? load_codes(v, at + 8, count - 8, n) : make_uint2(0, 0);
           u = make_uint4(a.x, a.y, b.x, b.y);
-          const int near = kStateBlock - static_cast<int>(at % kStateBlock);   // with the first scale
+          const int near = kStateBlock - static_cast<int>(at % kStateBlock);   // of one scale
           sc = e.vs[at / kStateBlock];
           if (near < count) {
             const uint4 f = first_codes(u, near);
@@ -310,7 +319,8 @@ __global__ void __launch_bounds__(kThreads) moment_finish_kernel(
 int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
 // Rows a warp takes of a matrix, by its own size alone (so that its sums are the same
-// in any company): as many as leave kTilesWanted tiles.
+// in any company): as many as leave kTilesWanted tiles.  Four 8-bit matrices of 72 x 72 to
+// 288 x 72: 8.2 us, 26 with 32 rows always; 16 of 2048 x 2048 and more: 68, 83 with 256 tiles.
 constexpr int64_t kTilesWanted = 64;
 int strip_of(const bergson_moment_matrix& m) {
   return m.state_kind == BERGSON_STATE_8BIT ? kStrip8 : kStrip32;

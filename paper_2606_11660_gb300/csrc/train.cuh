@@ -318,8 +318,8 @@ __device__ __forceinline__ void chances(uint64_t h, uint32_t (&c)[4]) {
   c[2] = (hi << 4) & 0xffff0u;
   c[3] = (hi >> 12) & 0xffff0u;
 }
-// encode_first and encode_second (but for raise_zeros4) of four elements.  Magnitudes are packed with one
-// bit more, so that holding them to a byte holds them to 7 bits.
+// encode_first and encode_second (but for raise_zeros4) of four elements.  The first's
+// magnitudes are packed with one bit more, so that holding them to a byte holds them to 7 bits.
 __device__ __forceinline__ uint32_t encode_first4(const float* m, float inv, const uint32_t* c) {
   int x[4];
 #pragma unroll

@@ -39,7 +39,8 @@ int check_rows(const void* p, size_t align, int64_t cols, int64_t ld, const char
   if (ld < cols)
     return fail(BERGSON_EINVAL, "the leading dimension of %s must be >= %lld (got %lld)", what,
                 (long long)cols, (long long)ld);
-  if (ld > (1ll << 40)) return fail(BERGSON_EUNSUPPORTED, "the leading dimension of %s is too large", what);
+  if (ld > (1ll << 40))
+    return fail(BERGSON_EUNSUPPORTED, "the leading dimension of %s is too large", what);
   return check_tensor(p, align, what);
 }
 
