@@ -699,7 +699,7 @@ BERGSON_API int bergson_project_grads_noalloc(const bergson_layer* layers, int n
  *             logits are not read and its outputs are 0.  A target >= V makes
  *             the row's logp NaN and is recorded as BERGSON_EINVAL in the device
  *             status word.
- *   tau       > 0, finite.
+ *   tau       > 0, 1 / tau and 1.5 / tau in the normal range of fp32.
  *   logp, lse fp32 [rows];  entropy fp32 [rows] or NULL.
  * Sums are fp32, in an order fixed by the sizes.  rows in [0, 2^31), V < 2^31.
  * Errors: EINVAL, EALIGN, ECUDA.
@@ -868,6 +868,8 @@ typedef struct bergson_adamw_tensor {
  * 16 bits of chance of elements 4q .. 4q + 3 of tensor i are output q + 1 of the
  * SplitMix64 sequence that starts at mix(i ^ mix(seed ^ mix(step))).  A v > 0 below
  * the smallest code takes that code.  The parameters see m and v before rounding.
+ * A gradient that is infinite or NaN spoils its element (fp32 moments) or the
+ * moments of its block of 256 (8-bit ones).
  *
  *   tensors   HOST array of n_tensors (>= 0) records.
  *   step      >= 1: the number of this step.  beta1, beta2 in [0, 1), eps >= 0.

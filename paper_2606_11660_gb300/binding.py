@@ -663,7 +663,8 @@ def _rows_like(t, what: str, dtype, shape) -> tuple[Optional[int], int]:
     if t.dtype is not dtype or t.shape != shape:
         raise ValueError(f"{what} must be {dtype} of shape {tuple(shape)}, got {t.dtype} of "
                          f"shape {tuple(t.shape)}")
-    return _rows(t, what)
+    ld, col = t.stride()
+    return (t.data_ptr(), ld) if col == 1 and ld >= shape[1] else _rows(t, what)
 
 
 def _vector(t, what: str, dtype, n: int) -> Optional[int]:

@@ -58,9 +58,10 @@ int check_logits(const void* logits, int dtype, int64_t rows, int64_t V, int64_t
   if (size == 0) return fail(BERGSON_EINVAL, "unknown dtype %d", dtype);
   if (rows < 0 || rows > INT32_MAX) return fail(BERGSON_EINVAL, "rows must be in [0, 2^31)");
   if (V < 1 || V > INT32_MAX) return fail(BERGSON_EINVAL, "V must be in [1, 2^31)");
-  if (!(tau > 0.0) || !std::isfinite(tau) || !std::isfinite(static_cast<float>(1.0 / tau)) ||
-      static_cast<float>(1.0 / tau) == 0.0f)
-    return fail(BERGSON_EINVAL, "tau must be > 0 and finite");
+  // the kernels scale by 1 / tau and log2(e) / tau in fp32
+  if (!(tau > 0.0) || !std::isfinite(static_cast<float>(1.5 / tau)) ||
+      !(static_cast<float>(1.0 / tau) >= 1.17549435e-38f))
+    return fail(BERGSON_EINVAL, "tau must be > 0 and 1 / tau in the range of fp32");
   if (rows == 0) return BERGSON_OK;
   int st = check_rows(logits, size, V, ld, "logits");
   if (st == BERGSON_OK) st = check_tensor(targets, 8, "targets");

@@ -56,6 +56,7 @@ LOGITS_BAD = [
     (dict(tau=0.0), bg.BERGSON_EINVAL), (dict(tau=-1.0), bg.BERGSON_EINVAL),
     (dict(tau=NAN), bg.BERGSON_EINVAL), (dict(tau=INF), bg.BERGSON_EINVAL),
     (dict(tau=1e-50), bg.BERGSON_EINVAL), (dict(tau=1e60), bg.BERGSON_EINVAL),
+    (dict(tau=3e-39), bg.BERGSON_EINVAL),
     (dict(lse=None), bg.BERGSON_EINVAL), (dict(lse=FAKE + 2), bg.BERGSON_EALIGN),
 ]
 
