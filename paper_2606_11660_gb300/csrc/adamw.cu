@@ -7,8 +7,8 @@
 // bytes: 2 + 2 + 16 an element with 16-bit parameters and gradients and 32-bit
 // states, 2 + 2 + 2 + 4 with 8-bit ones, 8 more with a master copy (2 less read).  201M
 // elements with masters and 32-bit states: 796 us, 7.1 TB/s.  With 8-bit states
-// 73 instructions an element stand beside the bytes, half of them on the integer
-// pipe: 50M elements with masters 132 us (6.1 TB/s), without 136 (3.7 TB/s).
+// some 70 instructions an element stand beside the bytes, half of them on the integer
+// pipe: 50M elements with masters 127 us (6.4 TB/s), without 115 (4.4 TB/s).
 //
 // m and v are formed by multiplications and additions that are each rounded
 // (no fused multiply-add): the codes of an 8-bit state then follow from the
@@ -26,6 +26,13 @@ namespace {
 
 constexpr int kThreads = 128;
 constexpr int kWarps = kThreads / 32;
+// Tensors of a kind share a launch: fp32 states; 8-bit states without and with a master
+// copy.  A warp takes kRun blocks of them.  Without a master copy two blocks share what comes
+// before them (50M elements, 1 / 2 / 4 blocks: 136 / 115 / 121 us); with one the loop's
+// registers cost more (1 / 2: 127 / 138).
+enum class Kind { kWide, kEight, kEightMaster };
+template <Kind kKind>
+constexpr int kRun = kKind == Kind::kEight ? 2 : 1;
 constexpr int kFew = 24, kMany = 300;          // records a launch can take
 
 struct Entry {
@@ -134,14 +141,17 @@ __device__ __forceinline__ float block_top(float top) {     // of the warp's lan
 }
 
 // A whole block of a tensor whose pointers fit.
-template <bool kEight>
+template <Kind kKind>
 __device__ __forceinline__ void block_vectors(const StepScalars& s, const Entry& e, int64_t first,
                                               float gs) {
   const int lane = threadIdx.x & 31;
   const int64_t i = first + 8 * lane;
+  constexpr bool kEight = kKind != Kind::kWide;
+  const bool master =
+      kKind == Kind::kEightMaster || (kKind == Kind::kWide && e.master != nullptr);
   uint32_t rw[8], rg[8], rm[8], rv[8];
   load8(e.g, e.gt, i, rg);
-  if (e.master != nullptr) load32(e.master + i, rw); else load8(e.p, e.pt, i, rw);
+  if (master) load32(e.master + i, rw); else load8(e.p, e.pt, i, rw);
   float ms = 0.0f, vs = 0.0f;
   if (kEight) {
     const uint2 um = *reinterpret_cast<const uint2*>(static_cast<const uint8_t*>(e.m) + i);
@@ -156,7 +166,7 @@ __device__ __forceinline__ void block_vectors(const StepScalars& s, const Entry&
   }
   float g[8], w[8], m[8], v[8];
   to_floats(rg, e.gt, g);
-  to_floats(rw, e.master != nullptr ? BERGSON_F32 : e.pt, w);
+  to_floats(rw, master ? BERGSON_F32 : e.pt, w);
   if (kEight) {
 #pragma unroll
     for (int q = 0; q < 2; ++q) {
@@ -196,7 +206,7 @@ __device__ __forceinline__ void block_vectors(const StepScalars& s, const Entry&
     w[k] = next_weight(s, e, w[k], m[k], v[k]);
     w[k + 1] = next_weight(s, e, w[k + 1], m[k + 1], v[k + 1]);
   }
-  if (e.master != nullptr) store8(e.master, BERGSON_F32, i, w);
+  if (master) store8(e.master, BERGSON_F32, i, w);
   store8(e.p, e.pt, i, w);
   if (!kEight) {
     store8(e.m, BERGSON_F32, i, m);
@@ -284,8 +294,9 @@ __device__ __noinline__ void block_elements(const StepScalars& s, const Entry& e
   }
 }
 
-// Nine CTAs an SM: 56 registers (8: 138, 10, with spills: 150 us for 50M 8-bit elements).
-template <int N>
+// Nine CTAs an SM: 56 registers (10 spill: 134 against 127 us for 50M 8-bit elements with
+// masters).
+template <int N, Kind kKind>
 __global__ void __launch_bounds__(kThreads, 9) adamw_kernel(
     const __grid_constant__ StepParams<N> p) {
   int lo = 0, hi = p.s.n;                        // begin[lo] <= CTA < begin[hi]
@@ -296,12 +307,14 @@ __global__ void __launch_bounds__(kThreads, 9) adamw_kernel(
   const Entry& e = p.e[lo];
   griddep_wait();
   const float gs = p.s.grad_scale != nullptr ? *p.s.grad_scale : 1.0f;
-  const int64_t first =
-      (static_cast<int64_t>(blockIdx.x - p.begin[lo]) * kWarps + (threadIdx.x >> 5)) * kStateBlock;
-  if (first >= e.n) return;
-  if (!e.vec || first + kStateBlock > e.n) block_elements(p.s, e, first, gs);
-  else if (e.st == BERGSON_STATE_8BIT) block_vectors<true>(p.s, e, first, gs);
-  else block_vectors<false>(p.s, e, first, gs);
+  int64_t first = (static_cast<int64_t>(blockIdx.x - p.begin[lo]) * (kWarps * kRun<kKind>) +
+                   (threadIdx.x >> 5)) * kStateBlock;
+#pragma unroll 1
+  for (int k = 0; k < kRun<kKind>; ++k, first += kWarps * kStateBlock) {
+    if (first >= e.n) return;
+    if (!e.vec || first + kStateBlock > e.n) block_elements(p.s, e, first, gs);
+    else block_vectors<kKind>(p.s, e, first, gs);
+  }
 }
 
 // 8 codes a thread where the pointers allow it.
@@ -343,9 +356,16 @@ bool fits_vectors(const bergson_adamw_tensor& t) {
          on(t.v, state);
 }
 
+Kind kind_of(const bergson_adamw_tensor& t) {
+  return t.state_kind == BERGSON_STATE_F32 ? Kind::kWide
+         : t.master == nullptr             ? Kind::kEight
+                                           : Kind::kEightMaster;
+}
+
 int64_t blocks_of(int64_t n) { return (n + kStateBlock - 1) / kStateBlock; }
 
-template <int N>
+// The tensors of one kind.
+template <int N, Kind kKind>
 cudaError_t run_adamw(const bergson_adamw_tensor* t, int n, const AdamwScalars& a, cudaStream_t s) {
   StepParams<N> p;
   p.s.b1 = static_cast<float>(a.beta1);
@@ -357,6 +377,7 @@ cudaError_t run_adamw(const bergson_adamw_tensor* t, int n, const AdamwScalars& 
   p.s.eps = static_cast<float>(a.eps);
   p.s.grad_scale = a.grad_scale;
   const uint64_t base = mix64(a.seed ^ mix64(static_cast<uint64_t>(a.step)));
+  constexpr int64_t cta_blocks = kWarps * kRun<kKind>;
   constexpr int64_t kMaxCtas = INT32_MAX;       // of a launch
   int k = 0;
   p.begin[0] = 0;
@@ -365,11 +386,11 @@ cudaError_t run_adamw(const bergson_adamw_tensor* t, int n, const AdamwScalars& 
     p.s.n = k;
     const dim3 grid(p.begin[k]);
     k = 0;
-    return launch_dependent(adamw_kernel<N>, grid, dim3(kThreads), 0, s, p);
+    return launch_dependent(adamw_kernel<N, kKind>, grid, dim3(kThreads), 0, s, p);
   };
   for (int i = 0; i < n; ++i) {
-    if (t[i].n == 0) continue;
-    const int64_t ctas = (blocks_of(t[i].n) + kWarps - 1) / kWarps;
+    if (t[i].n == 0 || kind_of(t[i]) != kKind) continue;
+    const int64_t ctas = (blocks_of(t[i].n) + cta_blocks - 1) / cta_blocks;
     if (k == N || (k > 0 && p.begin[k] + ctas > kMaxCtas)) {
       const cudaError_t e = flush();
       if (e != cudaSuccess) return e;
@@ -396,11 +417,25 @@ cudaError_t run_adamw(const bergson_adamw_tensor* t, int n, const AdamwScalars& 
   return flush();
 }
 
+template <Kind kKind>
+cudaError_t run_kind(const bergson_adamw_tensor* t, int n, int count, const AdamwScalars& a,
+                     cudaStream_t s) {
+  if (count == 0) return cudaSuccess;
+  return count <= kFew ? run_adamw<kFew, kKind>(t, n, a, s) : run_adamw<kMany, kKind>(t, n, a, s);
+}
+
 }  // namespace
 
 cudaError_t launch_adamw(const bergson_adamw_tensor* t, int n, const AdamwScalars& a,
                          cudaStream_t s) {
-  return n <= kFew ? run_adamw<kFew>(t, n, a, s) : run_adamw<kMany>(t, n, a, s);
+  int count[3] = {0, 0, 0};
+  for (int i = 0; i < n; ++i) {
+    if (t[i].n > 0) ++count[static_cast<int>(kind_of(t[i]))];
+  }
+  cudaError_t e = run_kind<Kind::kWide>(t, n, count[0], a, s);
+  if (e == cudaSuccess) e = run_kind<Kind::kEight>(t, n, count[1], a, s);
+  if (e == cudaSuccess) e = run_kind<Kind::kEightMaster>(t, n, count[2], a, s);
+  return e;
 }
 
 cudaError_t launch_state_values(const uint8_t* codes, const float* scale, int64_t n, int moment,
