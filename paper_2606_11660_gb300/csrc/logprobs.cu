@@ -260,7 +260,7 @@ __global__ void __launch_bounds__(kThreads, kFwdCtas) logprobs_row_kernel(const 
       st_cluster(&ranks[part].s, 0, a.s);
       st_cluster(&ranks[part].w, 0, a.w);
     }
-    cluster_sync();
+    cluster_barrier();
     if (part != 0) return;
     if (threadIdx.x == 0) {
       a = ranks[0];

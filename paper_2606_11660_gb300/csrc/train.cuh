@@ -155,11 +155,18 @@ __device__ __forceinline__ uint32_t cluster_size() {
   asm volatile("mov.u32 %0, %%cluster_nctaid.x;" : "=r"(r));
   return r;
 }
-// The two halves of cluster_sync(), for work between them.
+// cluster_sync() after code in which a warp's lanes may have parted, and its two halves for
+// work between them (the barrier wants whole warps).
+__device__ __forceinline__ void cluster_barrier() {
+  __syncwarp();
+  cluster_sync();
+}
 __device__ __forceinline__ void cluster_arrive() {
+  __syncwarp();
   asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
 }
 __device__ __forceinline__ void cluster_wait() {
+  __syncwarp();
   asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
 // Stores to the shared memory of the cluster's CTA `rank`, at the address that `p` has here.
