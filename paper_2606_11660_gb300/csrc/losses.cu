@@ -29,8 +29,12 @@ constexpr int kWarps = kThreads / 32;
 //
 // A warp takes 32 N tokens of a row at a time, N (4 or 8) a lane: neighbours in one
 // load where the rows allow it (kVec), else 32 apart in loads of one.  Their mask
-// bytes stay in words; tokens past the end have mask 0.  Masked tokens are not read
+// bytes stay in words; tokens outside the row have mask 0.  Masked tokens are not read
 // (in a vector, where all of it is masked).
+//
+// Rows of any length start off a vector's boundary, but where the tensors' bases are
+// aligned and their leading dimensions the same modulo N, row b of each of them starts
+// s = b ld mod N elements past one.  A row is then taken from token -s on.
 
 template <int N>
 struct Mask {
@@ -55,10 +59,15 @@ __device__ __forceinline__ int token_of(int t0, int j) {
   const int lane = threadIdx.x & 31;
   return kVec ? t0 + N * lane + j : t0 + lane + 32 * j;
 }
-// Whether all of a lane's tokens lie before T, and in one vector.
+// Whether all of a lane's tokens lie in [0, T), and in one vector.
 template <int N, bool kVec>
 __device__ __forceinline__ bool whole(int t0, int T) {
-  return kVec && token_of<N, kVec>(t0, N - 1) < T;
+  return kVec && token_of<N, kVec>(t0, 0) >= 0 && token_of<N, kVec>(t0, N - 1) < T;
+}
+// How far past a vector's boundary row b starts.
+template <int N, bool kVec>
+__device__ __forceinline__ int shift_of(int64_t b, int64_t ld) {
+  return kVec ? static_cast<int>((b * ld) & (N - 1)) : 0;
 }
 
 template <int N, bool kVec>
@@ -172,7 +181,7 @@ constexpr int kCountCtas = 1216;
 constexpr int kPolicyPerSm = 4;                // CTAs an SM holds (123 us; 3: 129, 5: 126)
 constexpr int kFinishCtas = 152;
 // The one-launch form: at most so many segments of the shorter kind.  us in one launch / in
-// three: 8 x 97 tokens 8.5 / 14.6, 64 x 1000 10.1 / 15.1; of 512 segments, 64 x 2000, 17.6 / 14.9.
+// three: 8 x 97 tokens 9.1 / 12.9, 64 x 1000 10.1 / 13.5; of 512 segments, 64 x 2000, 17.6 / 12.9.
 constexpr int kSmallItems = 256;
 constexpr int kSmallThreads = 512, kSmallWarps = kSmallThreads / 32;
 constexpr int kSmallCount = 2048;              // mask bytes a warp counts at once there
@@ -306,7 +315,7 @@ __device__ __forceinline__ float4 policy_segment(const PolicyParams& p, int64_t 
   const float minus_we = -w * p.ent;
   float loss = 0.0f, kls = 0.0f;
   int clipped = 0, valid = 0;
-  int t0 = seg * p.segment;
+  int t0 = seg * p.segment - shift_of<4, kVec>(b, p.a.ld_logp);
   Mask<4> next = load_mask<4, kVec>(mask, t0, T);
 #pragma unroll 1
   for (int left = min(T - t0, p.segment); left > 0; left -= 128, t0 += 128) {
@@ -505,10 +514,11 @@ constexpr int kPairPerSm = 5, kPairPerSmRef = 4;
 constexpr int kPairCtas = 2;
 constexpr int64_t kPairTokens = 2048;
 
-// From kManyPairs on, pairs of up to kShortPair tokens go to a warp each: 2048 of 100 / 500
-// tokens 7.8 / 11 us, to a CTA each 15.6 / 16.8; 700 of 500 level.
+// From kManyPairs on, pairs of up to kShortPair tokens go to a warp each: 2048 of 100 / 600 /
+// 1000 tokens 7.8 / 9.4 / 13.4 us, to a CTA each 15.6 / 22.1 / 23.6; 700 of 1000 9.2 and 11.9,
+// of 2000 13.8 and 12.1.
 constexpr int64_t kManyPairs = 608;
-constexpr int64_t kShortPair = 512;
+constexpr int64_t kShortPair = 1024;
 
 struct PreferenceParams {
   bergson_preference_args a;
@@ -532,8 +542,9 @@ __device__ __forceinline__ void preference_f(int kind, float x, float beta, floa
   }
 }
 
-// The sums over [t0, t1) of a pair's rows (both multiples of 256, but for T) by a group of
-// kGroup warps: a warp by itself, or the CTA through red and counts.
+// The sums over places [t0, t1) of a pair's rows (token t of a row has place t + its shift;
+// t0 a multiple of 256) by a group of kGroup warps: a warp by itself, or the CTA
+// through red and counts.
 template <int N, bool kVec, bool kRef, int kGroup>
 __device__ __forceinline__ void pair_sums(const PreferenceParams& p, int64_t pair, int t0, int t1,
                                           Sum2 (*red)[2], int (*counts)[2], Sum2* sum, int* count) {
@@ -543,10 +554,12 @@ __device__ __forceinline__ void pair_sums(const PreferenceParams& p, int64_t pai
   const float* x[2];
   const float* ref[2];
   Sum2 s[2];
-  int n[2] = {0, 0};
+  int n[2] = {0, 0}, shift[2], end[2];
 #pragma unroll
   for (int k = 0; k < 2; ++k) {
     const int64_t r = pair + k * p.a.P;
+    shift[k] = shift_of<N, kVec>(r, p.a.ld_logp);
+    end[k] = min(static_cast<int>(p.a.T), t1 - shift[k]);
     mask[k] = p.a.mask == nullptr ? nullptr : p.a.mask + r * p.a.ld_mask;
     x[k] = p.a.logp + r * p.a.ld_logp;
     ref[k] = kRef ? p.a.ref_logp + r * p.a.ld_ref : nullptr;
@@ -554,22 +567,22 @@ __device__ __forceinline__ void pair_sums(const PreferenceParams& p, int64_t pai
   int t = t0 + 32 * N * warp, left = t1 - t;
   Mask<N> next[2];
   if (left > 0) {
-    next[0] = load_mask<N, kVec>(mask[0], t, t1);
-    next[1] = load_mask<N, kVec>(mask[1], t, t1);
+    next[0] = load_mask<N, kVec>(mask[0], t - shift[0], end[0]);
+    next[1] = load_mask<N, kVec>(mask[1], t - shift[1], end[1]);
   }
 #pragma unroll 1
   for (; left > 0; left -= kStride, t += kStride) {
     float v[2][N], u[2][N];
     const Mask<N> m[2] = {next[0], next[1]};
-    load_tokens<N, kVec>(x[0], t, t1, m[0], v[0]);
-    load_tokens<N, kVec>(x[1], t, t1, m[1], v[1]);
+    load_tokens<N, kVec>(x[0], t - shift[0], end[0], m[0], v[0]);
+    load_tokens<N, kVec>(x[1], t - shift[1], end[1], m[1], v[1]);
     if (kRef) {
-      load_tokens<N, kVec>(ref[0], t, t1, m[0], u[0]);
-      load_tokens<N, kVec>(ref[1], t, t1, m[1], u[1]);
+      load_tokens<N, kVec>(ref[0], t - shift[0], end[0], m[0], u[0]);
+      load_tokens<N, kVec>(ref[1], t - shift[1], end[1], m[1], u[1]);
     }
     if (left > kStride) {
-      next[0] = load_mask<N, kVec>(mask[0], t + kStride, t1);
-      next[1] = load_mask<N, kVec>(mask[1], t + kStride, t1);
+      next[0] = load_mask<N, kVec>(mask[0], t + kStride - shift[0], end[0]);
+      next[1] = load_mask<N, kVec>(mask[1], t + kStride - shift[1], end[1]);
     }
 #pragma unroll
     for (int k = 0; k < 2; ++k) {
@@ -645,22 +658,26 @@ __device__ __forceinline__ void write_pair(const PreferenceParams& p, int64_t pa
   constexpr int kStride = 32 * N * kGroup;
   const uint8_t* mask[2];
   float* out[2];
+  int shift[2], end[2];
 #pragma unroll
   for (int k = 0; k < 2; ++k) {
     const int64_t r = pair + k * p.a.P;
+    shift[k] = shift_of<N, kVec>(r, p.a.ld_logp);
+    end[k] = min(static_cast<int>(p.a.T), t1 - shift[k]);
     mask[k] = p.a.mask == nullptr ? nullptr : p.a.mask + r * p.a.ld_mask;
     out[k] = p.a.d_logp + r * p.a.ld_d;
   }
   int t = t0 + 32 * N * warp;
 #pragma unroll 2
   for (int left = t1 - t; left > 0; left -= kStride, t += kStride) {
-    const Mask<N> m[2] = {load_mask<N, kVec>(mask[0], t, t1), load_mask<N, kVec>(mask[1], t, t1)};
+    const Mask<N> m[2] = {load_mask<N, kVec>(mask[0], t - shift[0], end[0]),
+                          load_mask<N, kVec>(mask[1], t - shift[1], end[1])};
 #pragma unroll
     for (int k = 0; k < 2; ++k) {
       float x[N];
 #pragma unroll
       for (int j = 0; j < N; ++j) x[j] = m[k].on(j) ? d[k] : 0.0f;
-      store_tokens<N, kVec>(out[k], t, t1, x);
+      store_tokens<N, kVec>(out[k], t - shift[k], end[k], x);
     }
   }
 }
@@ -673,13 +690,19 @@ __device__ __forceinline__ void write_rewards(const bergson_preference_args& a, 
   a.rewards[pair + a.P] = g.reward[1];
 }
 
+// Places that the rows' tokens may have, whatever their shifts.
+template <int N>
+__device__ __forceinline__ int places(int64_t T) {
+  return T > 0 ? static_cast<int>(T) + N - 1 : 0;
+}
+
 // Many short pairs: one a warp.
 template <int N, bool kVec, bool kRef>
 __global__ void __launch_bounds__(kPairThreads) preference_warp_kernel(const PreferenceParams p) {
   const int64_t pair = static_cast<int64_t>(blockIdx.x) * kPairWarps + (threadIdx.x >> 5);
   griddep_wait();
   if (pair >= p.a.P) return;
-  const int T = static_cast<int>(p.a.T);
+  const int T = places<N>(p.a.T);
   Sum2 sum[2];
   int count[2];
   pair_sums<N, kVec, kRef, 1>(p, pair, 0, T, nullptr, nullptr, sum, count);
@@ -700,7 +723,7 @@ __global__ void __launch_bounds__(kPairThreads, kRef ? kPairPerSmRef : kPairPerS
   const int rank = static_cast<int>(blockIdx.x) % parts;
   const int64_t pair = kTogether ? blockIdx.x : blockIdx.x / parts;
   const bool live = pair < p.a.P;
-  const int T = static_cast<int>(p.a.T), blocks = (T - 1) / 256 + 1;
+  const int T = places<N>(p.a.T), blocks = (T - 1) / 256 + 1;
   const int per = kTogether ? blocks : (blocks + parts - 1) / parts;
   const int t0 =
       kTogether ? 0 : static_cast<int>(min(static_cast<int64_t>(T), int64_t{256} * per * rank));
@@ -771,9 +794,10 @@ size_t counts_bytes(int64_t B, int64_t T) {
   return align256(4 * static_cast<size_t>(n));
 }
 
-// Rows whose loads of n tokens at once are aligned.
-bool fits(const void* p, int64_t ld, size_t elem, int n) {
-  return p == nullptr || (reinterpret_cast<uintptr_t>(p) % (n * elem) == 0 && ld % n == 0);
+// Rows whose vectors of n tokens lie where those of a tensor of leading dimension ld0 do.
+bool fits(const void* p, int64_t ld, size_t elem, int n, int64_t ld0) {
+  return p == nullptr ||
+         (reinterpret_cast<uintptr_t>(p) % (n * elem) == 0 && (ld - ld0) % n == 0);
 }
 
 template <typename K, typename P>
@@ -796,7 +820,7 @@ cudaError_t launch_cluster(K kernel, int64_t grid, int threads, int cluster, con
 
 template <bool kVec>
 cudaError_t run_policy(PolicyParams p, cudaStream_t s) {
-  if (p.a.B * ceil_div(p.a.T, kShortSegment) <= kSmallItems) {
+  if (p.segment == kShortSegment && p.a.B * p.segments <= kSmallItems) {
     int parts = 1;
     while (parts < 8 && parts * kSmallWarps < p.a.B * p.segments) parts *= 2;
     return launch_cluster(policy_small_kernel<kVec>, parts, kSmallThreads, parts, p, s);
@@ -851,17 +875,19 @@ cudaError_t run_preference(const PreferenceParams& p, int sms, cudaStream_t s) {
 
 }  // namespace
 
+// Segments of a row, from its shift on.
+static int64_t segments_of(int64_t T, int segment) { return (T + 3 + segment - 1) / segment; }
+
 // counts, the totals and their ticket, the segments' sums
 size_t policy_workspace(int64_t B, int64_t T) {
   return counts_bytes(B, T) + align256(sizeof(Totals) * kFinishCtas) + 256 +
-         align256(sizeof(float4) * static_cast<size_t>(B * ceil_div(T, kShortSegment)));
+         align256(sizeof(float4) * static_cast<size_t>(B * segments_of(T, kShortSegment)));
 }
 
 cudaError_t launch_policy_loss(const bergson_policy_args& a, void* ws, cudaStream_t s) {
   PolicyParams p;
   p.a = a;
   p.segment = a.B * ceil_div(a.T, kSegment) >= kLongItems ? kSegment : kShortSegment;
-  p.segments = ceil_div(a.T, p.segment);
   p.count_segments = ceil_div(a.T, kCountSegment);
   p.n_counts = 0;
   char* at = static_cast<char*>(ws);
@@ -886,11 +912,16 @@ cudaError_t launch_policy_loss(const bergson_policy_args& a, void* ws, cudaStrea
       e = cudaMemsetAsync(a.seq_loss, 0, sizeof(float) * static_cast<size_t>(a.B), s);
     return e;
   }
-  const bool vec = fits(a.logp, a.ld_logp, 4, 4) && fits(a.old_logp, a.ld_old, 4, 4) &&
-                   fits(p.a.ref_logp, a.ld_ref, 4, 4) && fits(p.a.entropy, a.ld_entropy, 4, 4) &&
-                   (a.ld_adv == 0 || fits(a.advantages, a.ld_adv, 4, 4)) &&
-                   fits(a.mask, a.ld_mask, 1, 4) && fits(a.d_logp, a.ld_d, 4, 4) &&
-                   fits(a.d_entropy, a.ld_de, 4, 4);
+  const auto fit = [&](const void* x, int64_t ld, size_t elem) {
+    return fits(x, ld, elem, 4, a.ld_logp);
+  };
+  const bool vec = fit(a.logp, a.ld_logp, 4) && fit(a.old_logp, a.ld_old, 4) &&
+                   fit(p.a.ref_logp, a.ld_ref, 4) && fit(p.a.entropy, a.ld_entropy, 4) &&
+                   (a.ld_adv == 0 || fit(a.advantages, a.ld_adv, 4)) &&
+                   fit(a.mask, a.ld_mask, 1) && fit(a.d_logp, a.ld_d, 4) &&
+                   fit(a.d_entropy, a.ld_de, 4);
+  // rows that start on boundaries need no room for a shift
+  p.segments = vec && a.ld_logp % 4 != 0 ? segments_of(a.T, p.segment) : ceil_div(a.T, p.segment);
   return vec ? run_policy<true>(p, s) : run_policy<false>(p, s);
 }
 
@@ -902,8 +933,9 @@ cudaError_t launch_preference_loss(const bergson_preference_args& a, int sms, cu
   PreferenceParams p;
   p.a = a;
   const auto all_fit = [&](int n) {
-    return fits(a.logp, a.ld_logp, 4, n) && fits(a.ref_logp, a.ld_ref, 4, n) &&
-           fits(a.mask, a.ld_mask, 1, n) && fits(a.d_logp, a.ld_d, 4, n);
+    return fits(a.logp, a.ld_logp, 4, n, a.ld_logp) &&
+           fits(a.ref_logp, a.ld_ref, 4, n, a.ld_logp) &&
+           fits(a.mask, a.ld_mask, 1, n, a.ld_logp) && fits(a.d_logp, a.ld_d, 4, n, a.ld_logp);
   };
   if (all_fit(8)) return run_preference<8, true>(p, sms, s);
   return all_fit(4) ? run_preference<4, true>(p, sms, s) : run_preference<4, false>(p, sms, s);

@@ -346,8 +346,19 @@ def test_policy_at_the_launches_limits(B, T, reduction):
 
 @pytest.mark.parametrize("ref", [True, False])
 @pytest.mark.parametrize("P,T", [(607, 512), (608, 512), (608, 513), (700, 511), (1500, 1), (8, 4096),
-                                 (8, 4097), (9, 64), (2, 16_400)])
+                                 (8, 4097), (9, 64), (2, 16_400), (608, 1024), (608, 1025), (650, 1001),
+                                 (3, 30_003), (20, 12_349)])
 def test_preference_at_the_launches_limits(P, T, ref):
     """A warp a pair, a cluster of pairs, a CTA and a cluster a pair."""
     logp, r, mask = preference_inputs(P, T, seed=P)
     check_preference(logp, r if ref else None, mask)
+
+
+@pytest.mark.parametrize("T,pad", [(1001, 0), (997, 2), (4099, 4), (30, 1), (3, 0), (5, 2), (9, 7)])
+def test_rows_off_vector_boundaries(T, pad):
+    """Leading dimensions alike modulo 4 or 8: every row's vectors start elsewhere."""
+    for B in (6, 700):
+        check_policy(policy_inputs(B, T, seed=T), pad=pad)
+        logp, ref, mask = preference_inputs(B, T, seed=T)
+        check_preference(logp, ref, mask, pad=pad)
+        check_preference(logp, None, None, pad=pad)
