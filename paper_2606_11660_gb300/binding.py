@@ -731,6 +731,8 @@ def bergson_policy_loss(logp, old_logp, ref_logp, entropy, advantages, mask, cli
         adv, ld_adv = _vector(advantages, "advantages", _F32, B), 0
     else:
         adv, ld_adv = _rows_like(advantages, "advantages", _F32, shape)
+        if ld_adv == 0 and T > 0:             # to the C call: one a sequence, [B]
+            raise ValueError("advantages [B, T]: rows must not share their memory")
     on, ld_mask = _rows_like(mask, "mask", _U8, shape)
     d, ld_d = _rows_like(d_logp, "d_logp", _F32, shape)
     de, ld_de = _rows_like(d_entropy, "d_entropy", _F32, shape)

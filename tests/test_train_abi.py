@@ -295,3 +295,46 @@ def test_workspaces_grow_with_the_work():
     assert 0 < a < b and math.isfinite(b) and b < 4096 * 8192
     m = [bg.bergson_moment_matrix(FAKE, None, 4096, 4096, FAKE, FAKE, 0, 0)]
     assert 0 < bg.bergson_factor_moments_workspace(m) < 4096 * 4096 * 4 // 8
+
+
+class FakeTensor:
+    """What the binding asks of a device tensor, without a device."""
+    is_cuda = True
+
+    def __init__(self, shape, strides, dtype=torch.float32):
+        self.shape, self.strides, self.dtype = torch.Size(shape), strides, dtype
+
+    def stride(self):
+        return self.strides
+
+    def dim(self):
+        return len(self.shape)
+
+    def numel(self):
+        return math.prod(self.shape)
+
+    def element_size(self):
+        return self.dtype.itemsize
+
+    def is_contiguous(self):
+        return True
+
+    def data_ptr(self):
+        return FAKE
+
+
+@pytest.mark.parametrize("T,strides", [(6, (0, 1)), (1, (0, 1)), (1, (0, 0))])
+def test_advantages_that_sequences_share_are_refused(T, strides):
+    """One row for all sequences has leading dimension 0, which the C call takes for [B] advantages: it
+    would read past the row."""
+    x, one = FakeTensor((4, T), (T, 1)), FakeTensor((1,), (1,))
+    ws = FakeTensor((1 << 20,), (1,), torch.uint8)
+
+    def call(adv):
+        bg.bergson_policy_loss(x, x, None, None, adv, None, 0.2, 0.2, 0.0, 0.0, 0, 1.0, one, None,
+                               None, x, None, ws, stream=0)
+    with pytest.raises(ValueError, match="advantages"):
+        call(FakeTensor((4, T), strides))
+    for adv in (FakeTensor((4,), (1,)), x):
+        with pytest.raises(bg.BergsonError):          # the injected status: past the checks
+            call(adv)
