@@ -821,9 +821,13 @@ def bergson_adamw_tensors(tensors: Sequence) -> "ctypes.Array":
 def bergson_adamw_step(tensors, lr: float, beta1: float, beta2: float, eps: float, step: int,
                        seed: int = 0, grad_scale=None, stream=None) -> None:
     """One AdamW step over tensors (AdamWTensor list, or bergson_adamw_tensors' array)."""
+    if not _DTYPES:
+        _load_dtypes()
     arr = _records(bergson_adamw_tensor, tensors)
-    _check(lib().bergson_adamw_step(arr, len(arr), lr, beta1, beta2, eps, step, seed,
-                                    _ptr(grad_scale), _stream(stream)))
+    scale = (_vector(grad_scale, "grad_scale", _F32, 1) if hasattr(grad_scale, "data_ptr")
+             else _ptr(grad_scale))
+    _check(lib().bergson_adamw_step(arr, len(arr), lr, beta1, beta2, eps, step, seed, scale,
+                                    _stream(stream)))
 
 
 def bergson_adamw_state_values(codes, scale, moment: int, out, stream=None) -> None:

@@ -338,3 +338,17 @@ def test_advantages_that_sequences_share_are_refused(T, strides):
     for adv in (FakeTensor((4,), (1,)), x):
         with pytest.raises(bg.BergsonError):          # the injected status: past the checks
             call(adv)
+
+
+def test_gradient_scales_of_other_types_are_refused():
+    """They would be read as the bits of an fp32 number."""
+    def call(gs):
+        bg.bergson_adamw_step([], 1e-3, 0.9, 0.99, 1e-8, 1, grad_scale=gs, stream=0)
+    for dtype in (torch.float64, torch.bfloat16, torch.float16, torch.int32):
+        with pytest.raises(ValueError, match="grad_scale"):
+            call(FakeTensor((1,), (1,), dtype))
+    with pytest.raises(ValueError, match="grad_scale"):
+        call(FakeTensor((2,), (1,)))
+    for gs in (None, FAKE, FakeTensor((1,), (1,)), FakeTensor((), ())):
+        with pytest.raises(bg.BergsonError):          # the injected status: past the checks
+            call(gs)
