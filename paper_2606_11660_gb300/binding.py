@@ -648,11 +648,19 @@ def _dtype(t) -> int:
     return code
 
 
+def _host_tensor(t, what: str) -> None:
+    """Refuses a tensor that is not on a device, but for pinned host memory, which one can read."""
+    if t.numel() > 0 and not t.is_pinned():
+        raise ValueError(f"{what} must be on a CUDA device, got one on {t.device}")
+
+
 def _rows(t, what: str) -> tuple[int, int]:
     """(device pointer, leading dimension) of a matrix with consecutive columns."""
     ld, col = t.stride()
     if col != 1 and t.shape[1] > 1:
         raise ValueError(f"{what}: elements of a row must be consecutive")
+    if not t.is_cuda:
+        _host_tensor(t, what)
     return t.data_ptr(), ld if t.shape[0] > 1 else max(ld, t.shape[1])
 
 
@@ -663,6 +671,8 @@ def _rows_like(t, what: str, dtype, shape) -> tuple[Optional[int], int]:
     if t.dtype is not dtype or t.shape != shape:
         raise ValueError(f"{what} must be {dtype} of shape {tuple(shape)}, got {t.dtype} of "
                          f"shape {tuple(t.shape)}")
+    if not t.is_cuda:
+        _host_tensor(t, what)
     ld, col = t.stride()
     return (t.data_ptr(), ld) if col == 1 and ld >= shape[1] else _rows(t, what)
 
@@ -674,7 +684,16 @@ def _vector(t, what: str, dtype, n: int) -> Optional[int]:
     if t.dtype is not dtype or t.numel() != n or not t.is_contiguous():
         raise ValueError(f"{what} must be {dtype}, contiguous and of {n} elements, got {t.dtype} "
                          f"of shape {tuple(t.shape)}")
+    if not t.is_cuda:
+        _host_tensor(t, what)
     return t.data_ptr()
+
+
+def _scratch(t) -> tuple[int, int]:
+    """(device pointer, bytes) of a workspace."""
+    if not t.is_cuda:
+        _host_tensor(t, "workspace")
+    return t.data_ptr(), t.numel() * t.element_size()
 
 
 def bergson_token_logprobs(logits, targets, tau: float, logp, lse, entropy=None,
@@ -741,9 +760,7 @@ def bergson_policy_loss(logp, old_logp, ref_logp, entropy, advantages, mask, cli
                                norm_tokens, _vector(loss, "loss", _F32, 1),
                                _vector(seq_loss, "seq_loss", _F32, B),
                                _vector(stats, "stats", _F32, 3), d, de, ld_d, ld_de, reduction, 0)
-    _check(lib().bergson_policy_loss(args, workspace.data_ptr(),
-                                     workspace.numel() * workspace.element_size(),
-                                     _stream(stream)))
+    _check(lib().bergson_policy_loss(args, *_scratch(workspace), _stream(stream)))
 
 
 def bergson_preference_loss(logp, ref_logp, mask, kind: int, beta: float, margin: float,
@@ -876,8 +893,7 @@ def bergson_factor_moments_workspace(mats) -> int:
 def bergson_factor_moments(mats, correction: float, floor: float, workspace, stream=None) -> None:
     """r and c of every matrix (MomentMatrix list, or bergson_moment_matrices' array)."""
     arr = _records(bergson_moment_matrix, mats)
-    _check(lib().bergson_factor_moments(arr, len(arr), correction, floor, workspace.data_ptr(),
-                                        workspace.numel() * workspace.element_size(),
+    _check(lib().bergson_factor_moments(arr, len(arr), correction, floor, *_scratch(workspace),
                                         _stream(stream)))
 
 

@@ -352,3 +352,82 @@ def test_gradient_scales_of_other_types_are_refused():
     for gs in (None, FAKE, FakeTensor((1,), (1,)), FakeTensor((), ())):
         with pytest.raises(bg.BergsonError):          # the injected status: past the checks
             call(gs)
+
+
+class Host(FakeTensor):
+    """... of a tensor in host memory."""
+    is_cuda, device = False, "cpu"
+
+    def __init__(self, t, pinned=False):
+        super().__init__(t.shape, t.strides, t.dtype)
+        self.pinned = pinned
+
+    def is_pinned(self):
+        return self.pinned
+
+
+def _device_calls():
+    """Every training-side call of the binding as (its tensors by name, the call of them)."""
+    x, v, one, three = (FakeTensor(s, st) for s, st in (((4, 6), (6, 1)), ((4,), (1,)), ((1,), (1,)),
+                                                        ((3,), (1,))))
+    two = FakeTensor((2,), (1,))
+    idx, mask = FakeTensor((4,), (1,), torch.int64), FakeTensor((4, 6), (6, 1), torch.uint8)
+    ws = FakeTensor((1 << 20,), (1,), torch.uint8)
+    u = FakeTensor((4,), (1,), torch.uint8)
+    r, c = v, FakeTensor((6,), (1,))
+    return {
+        "logprobs": (dict(logits=x, targets=idx, logp=v, lse=v, entropy=v),
+                     lambda t: bg.bergson_token_logprobs(t["logits"], t["targets"], 1.0, t["logp"],
+                                                         t["lse"], t["entropy"], stream=0)),
+        "backward": (dict(logits=x, targets=idx, lse=v, entropy=v, d_logp=v, d_entropy=v, d_logits=x),
+                     lambda t: bg.bergson_token_logprobs_backward(
+                         t["logits"], t["targets"], 1.0, t["lse"], t["entropy"], t["d_logp"],
+                         t["d_entropy"], t["d_logits"], stream=0)),
+        "policy": (dict(logp=x, old_logp=x, ref_logp=x, entropy=x, advantages=v, mask=mask, loss=one,
+                        seq_loss=v, stats=three, d_logp=x, d_entropy=x, workspace=ws),
+                   lambda t: bg.bergson_policy_loss(
+                       t["logp"], t["old_logp"], t["ref_logp"], t["entropy"], t["advantages"], t["mask"],
+                       0.2, 0.2, 0.1, 0.1, 0, 1.0, t["loss"], t["seq_loss"], t["stats"], t["d_logp"],
+                       t["d_entropy"], t["workspace"], stream=0)),
+        "preference": (dict(logp=x, ref_logp=x, mask=mask, loss=one, pair_loss=two, rewards=v, d_logp=x),
+                       lambda t: bg.bergson_preference_loss(
+                           t["logp"], t["ref_logp"], t["mask"], 0, 0.1, 0.0, 0.0, False, t["loss"],
+                           t["pair_loss"], t["rewards"], t["d_logp"], stream=0)),
+        "adamw": (dict(param=v, grad=v, m=u, v=u, master=v, m_scale=one, v_scale=one, grad_scale=one),
+                  lambda t: bg.bergson_adamw_step(
+                      [bg.AdamWTensor(t["param"], t["grad"], t["m"], t["v"], t["master"], t["m_scale"],
+                                      t["v_scale"])], 1e-3, 0.9, 0.99, 1e-8, 1,
+                      grad_scale=t["grad_scale"], stream=0)),
+        "values": (dict(codes=u, scale=one, out=v),
+                   lambda t: bg.bergson_adamw_state_values(t["codes"], t["scale"], 0, t["out"], stream=0)),
+        "moments": (dict(v=x, r=r, c=c, workspace=ws),
+                    lambda t: bg.bergson_factor_moments([bg.MomentMatrix(t["v"], t["r"], t["c"])], 1.0,
+                                                        1e-12, t["workspace"], stream=0)),
+    }
+
+
+@pytest.mark.parametrize("name", list(_device_calls()))
+def test_tensors_in_host_memory_are_refused(name):
+    """A kernel would follow their addresses.  Pinned memory, which a device can read, passes."""
+    tensors, call = _device_calls()[name]
+    with pytest.raises(bg.BergsonError):              # the injected status: past the checks
+        call(tensors)
+    for what, t in tensors.items():
+        with pytest.raises(ValueError, match=f"^{what} must be on a CUDA device"):
+            call({**tensors, what: Host(t)})
+        with pytest.raises(bg.BergsonError):
+            call({**tensors, what: Host(t, pinned=True)})
+
+
+@pytest.mark.parametrize("name", list(_device_calls()))
+def test_device_tensors_of_other_sizes_are_refused_by_name(name):
+    tensors, call = _device_calls()[name]
+    first = next(iter(tensors))                       # the others' sizes follow from it
+    for what, t in tensors.items():
+        if what in (first, "workspace"):
+            continue
+        wrong = FakeTensor((t.shape[0] + 300, *t.shape[1:]), t.strides, t.dtype)
+        with pytest.raises(ValueError, match=f"^{what} must be "):
+            call({**tensors, what: wrong})
+        with pytest.raises((ValueError, TypeError)):
+            call({**tensors, what: FakeTensor(t.shape, t.strides, torch.float64)})
