@@ -719,9 +719,12 @@ BERGSON_API int bergson_token_logprobs(const void* logits, int dtype, int64_t ro
  *   lse, entropy   what the forward pass wrote (entropy only with d_entropy).
  *   d_logits  [rows, ld_d], ld_d >= V; may be `logits` itself with ld_d == ld.
  * A row whose target is negative, whose w and h are both 0, or whose lse is below
- * -1e30 (nothing but -inf or a type's lowest value, beside which lse cannot hold
- * log V) gets zeros and its logits are not read.  A target >= V makes the row NaN and
- * is recorded as BERGSON_EINVAL in the device status word.
+ * -1e30 (nothing but -inf or a type's lowest value) gets zeros and its logits are
+ * not read.  A target >= V makes the row NaN and is recorded as BERGSON_EINVAL in the
+ * device status word.  Where |lse| is 4096 or more (a large common offset, a finite
+ * mask over the whole row) fp32 holds too few digits of it: what it lacks is summed
+ * from the row's logits again, at some loss of speed.  Below, its rounding leaves p
+ * within 1.2e-4 (2^-25 |lse| and less).
  * Errors: EINVAL, EALIGN, ECUDA.
  */
 BERGSON_API int bergson_token_logprobs_backward(const void* logits, int dtype, int64_t rows,

@@ -12,6 +12,10 @@
 // the maximum are formed before anything is scaled, so that entries at a type's
 // lowest value take no other path.
 //
+// The backward pass takes p from x / tau - lse, where fp32 holds what lse has to say of the
+// sum; a row whose lse is far from 0 (logits at a large common offset, a finite mask over all
+// of them) is summed again about its largest element.
+//
 // Both passes are bound by the logits' bytes: 8192 x 131,072 bf16 with entropies 288 us
 // (6.7 TB/s, the measured copy rate; ex2 and the conversions fill half of the
 // issue slots), the gradients at 8192 x 65,536, half of whose rows are left out and only
@@ -31,8 +35,14 @@ constexpr int kUnroll = 4;                     // vectors a thread has on the wa
 // 64 registers hold them and their sums.  8192 x 131,072 bf16 with entropies, us:
 // 4 vectors at 3 / 4 CTAs an SM 320 / 290, 3 at 4: 311, 2 at 5 / 6: 319 / 317.
 constexpr int kFwdCtas = 4;
+// 48 registers, of which the rare second sum of a far row takes its share (1031 x 32,003 fp16 with
+// entropies at 5 / 6: 20.9 / 21.8 us).
+constexpr int kBwdCtas = 5;
 constexpr float kInf = __builtin_huge_valf();
 constexpr float kNoRow = -1e30f;               // a row's lse below this: it has no entries
+// From here on an fp32 lse says too little of the sum: its half unit, 1.2e-4 below 4096, is p's
+// relative error, and from 2^24 on log V is lost beside it.
+constexpr float kFarLse = 4096.0f;
 constexpr float kLog2e = 1.44269504f;
 constexpr float kLn2 = 0.693147181f;
 
@@ -155,8 +165,8 @@ __device__ __forceinline__ int64_t head_of(const T* row, int64_t V) {
 }
 
 // What thread `at` of `n` finds in its share of a row: every n-th vector of [first,
-// last), and the elements outside the vectors where `edges` is set.
-template <typename T, bool kEntropy>
+// last), kVecs of them on the way, and the elements outside the vectors where `edges` is set.
+template <typename T, bool kEntropy, int kVecs>
 __device__ __forceinline__ RowSums scan_row(const T* row, int64_t V, float c, int at, int n,
                                             int part, int parts) {
   constexpr int E = Vec16<T>::kElems;
@@ -167,19 +177,21 @@ __device__ __forceinline__ RowSums scan_row(const T* row, int64_t V, float c, in
   const uint4* body = reinterpret_cast<const uint4*>(row + head);
   Accumulator<T, kEntropy> a;
   int64_t i = per * part + at;
-  for (; i + (kUnroll - 1) * n < last; i += kUnroll * n) {
-    uint4 v[kUnroll];
+  for (; i + (kVecs - 1) * n < last; i += kVecs * n) {
+    uint4 v[kVecs];
 #pragma unroll
-    for (int k = 0; k < kUnroll; ++k) v[k] = __ldcs(body + i + k * n);
+    for (int k = 0; k < kVecs; ++k) v[k] = __ldcs(body + i + k * n);
     a.take(v, c);
   }
-  uint4 v[kUnroll - 1][1];
+  if constexpr (kVecs > 1) {
+    uint4 v[kVecs - 1][1];
 #pragma unroll
-  for (int k = 0; k < kUnroll - 1; ++k)
-    if (i + k * n < last) v[k][0] = __ldcs(body + i + k * n);
+    for (int k = 0; k < kVecs - 1; ++k)
+      if (i + k * n < last) v[k][0] = __ldcs(body + i + k * n);
 #pragma unroll
-  for (int k = 0; k < kUnroll - 1; ++k)
-    if (i + k * n < last) a.take(v[k], c);
+    for (int k = 0; k < kVecs - 1; ++k)
+      if (i + k * n < last) a.take(v[k], c);
+  }
   if (part == 0) {
     if (at < head) a.take_one(row[at], c);
     const int64_t tail = head + vecs * E + at;
@@ -243,7 +255,7 @@ __global__ void __launch_bounds__(kThreads, kFwdCtas) logprobs_row_kernel(const 
   }
   const T* row = static_cast<const T*>(p.x) + r * p.ld;
   if (parts > 1) cluster_arrive();
-  RowSums a = scan_row<T, kEntropy>(row, p.V, p.c, threadIdx.x, kThreads, part, parts);
+  RowSums a = scan_row<T, kEntropy, kUnroll>(row, p.V, p.c, threadIdx.x, kThreads, part, parts);
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) merge(a, shuffle(a, o), p.c);
   if ((threadIdx.x & 31) == 0) red[threadIdx.x >> 5] = a;
@@ -283,7 +295,7 @@ __global__ void __launch_bounds__(kThreads, kFwdCtas) logprobs_warp_kernel(const
     return;
   }
   const T* row = static_cast<const T*>(p.x) + r * p.ld;
-  RowSums a = scan_row<T, kEntropy>(row, p.V, p.c, lane, 32, 0, 1);
+  RowSums a = scan_row<T, kEntropy, kUnroll>(row, p.V, p.c, lane, 32, 0, 1);
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) merge(a, shuffle(a, o), p.c);
   if (lane == 0) write_row<T>(p, r, t, a);
@@ -295,7 +307,7 @@ struct BackwardParams {
   const void* x;
   int64_t rows, V, ld;
   const int64_t* targets;
-  float inv_tau;
+  float inv_tau, c;            // 1 / tau, log2(e) / tau
   const float* lse;
   const float* entropy;
   const float* d_logp;
@@ -306,10 +318,11 @@ struct BackwardParams {
   int* status;
 };
 
-// One row's constants.
+// One row's constants.  log p_v = q - rest, q = x_v / tau - lse; rest is 0 but for far rows.
 struct RowGrad {
   float inv_tau, lse;
-  float a, b;                  // dx_v = p_v (a + b log p_v) + [v = t] hit
+  float rest2;                 // -rest log2(e)
+  float a, b;                  // dx_v = p_v (a + b q) + [v = t] hit
   float hit;
 };
 
@@ -320,7 +333,7 @@ __device__ __forceinline__ float2 grad2(float2 x, const RowGrad& g) {
     q.x = fmaxf(q.x, -150.0f);
     q.y = fmaxf(q.y, -150.0f);
   }
-  const float2 u = mul2(q, pair(kLog2e));
+  const float2 u = fma2(q, pair(kLog2e), pair(g.rest2));
   const float2 e = make_float2(exp2_approx(u.x), exp2_approx(u.y));
   return kEntropy ? mul2(e, fma2(q, pair(g.b), pair(g.a))) : mul2(e, pair(g.a));
 }
@@ -349,25 +362,54 @@ __device__ __forceinline__ uint4 grad_vec(const uint4& x, const RowGrad& g, int6
   return o;
 }
 
-// Thread `at` of `n` takes its share of part `part` of a row.
-template <typename T, bool kEntropy>
-__device__ __forceinline__ void backward_row(const BackwardParams& p, int64_t r, int at, int n,
-                                             int part) {
+// What a far row's rounded lse leaves out: the row's largest element and sum once more, by a warp
+// or a CTA; the same in every thread, and none leaves before all have read the row.
+template <typename T, bool kWarp>
+__device__ __noinline__ float rest_of(const T* row, int64_t V, float c, float inv_tau, float lse) {
+  RowSums a = kWarp ? scan_row<T, false, 1>(row, V, c, threadIdx.x & 31, 32, 0, 1)
+                    : scan_row<T, false, 1>(row, V, c, threadIdx.x, kThreads, 0, 1);
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) merge(a, shuffle(a, o), c);
+  if (!kWarp) {
+    __shared__ RowSums red[kThreads / 32];
+    if ((threadIdx.x & 31) == 0) red[threadIdx.x >> 5] = a;
+    __syncthreads();
+    a = red[threadIdx.x & (kThreads / 32 - 1)];
+#pragma unroll
+    for (int o = kThreads / 64; o > 0; o >>= 1) merge(a, shuffle(a, o), c);
+  }
+  return fmaf(a.m, inv_tau, -lse) + log2f(a.s) * kLn2;
+}
+
+// Part `part` of a row, by a warp or a CTA.
+template <typename T, bool kEntropy, bool kWarp>
+__device__ __forceinline__ void backward_row(const BackwardParams& p, int64_t r, int part) {
   constexpr int E = Vec16<T>::kElems;
+  constexpr int n = kWarp ? 32 : kThreads;
+  const int at = kWarp ? threadIdx.x & 31 : threadIdx.x;
   const T* row = static_cast<const T*>(p.x) + r * p.ld;
   T* out = static_cast<T*>(p.dx) + r * p.ld_d;
   const int64_t t = p.targets[r];
   const float w = p.d_logp != nullptr ? p.d_logp[r] : 0.0f;
   const float h = p.d_entropy != nullptr ? p.d_entropy[r] : 0.0f;
   const float l = p.lse[r];
+  const bool nan = t >= p.V;
+  const bool none = nan || t < 0 || (w == 0.0f && h == 0.0f) || l < kNoRow;
+  float rest = 0.0f;
+  int slices = p.slices;
+  if (!none && fabsf(l) >= kFarLse) {
+    // by the row's first CTA alone: d_logits may be the logits
+    if (part != 0) return;
+    slices = 1;
+    rest = rest_of<T, kWarp>(row, p.V, p.c, p.inv_tau, l);
+  }
   const int64_t head = head_of(out, p.V);
   const int64_t vecs = (p.V - head) / E;
-  const int64_t per = (vecs + p.slices - 1) / p.slices;
+  const int64_t per = (vecs + slices - 1) / slices;
   const int64_t first = per * part, last = min(vecs, first + per);
   const int64_t tail = head + vecs * E + at;
   uint4* body = reinterpret_cast<uint4*>(out + head);
-  const bool nan = t >= p.V;
-  if (nan || t < 0 || (w == 0.0f && h == 0.0f) || l < kNoRow) {
+  if (none) {
     const float f = nan ? __int_as_float(0x7fffffff) : 0.0f;
     if (nan && part == 0 && at == 0 && p.status != nullptr)
       atomicCAS(p.status, 0, BERGSON_EINVAL);
@@ -384,8 +426,9 @@ __device__ __forceinline__ void backward_row(const BackwardParams& p, int64_t r,
   RowGrad g;
   g.inv_tau = p.inv_tau;
   g.lse = l;
-  g.a = -(w + (kEntropy ? h * p.entropy[r] : 0.0f)) * p.inv_tau;
+  g.rest2 = -kLog2e * rest;
   g.b = -h * p.inv_tau;
+  g.a = fmaf(-g.b, rest, -(w + (kEntropy ? h * p.entropy[r] : 0.0f)) * p.inv_tau);
   g.hit = w * p.inv_tau;
   if (((reinterpret_cast<uintptr_t>(row + head)) & 15) == 0) {
     const uint4* in = reinterpret_cast<const uint4*>(row + head);
@@ -417,17 +460,17 @@ __device__ __forceinline__ void backward_row(const BackwardParams& p, int64_t r,
 }
 
 template <typename T, bool kEntropy>
-__global__ void __launch_bounds__(kThreads) logprobs_backward_kernel(const BackwardParams p) {
+__global__ void __launch_bounds__(kThreads, kBwdCtas) logprobs_backward_kernel(const BackwardParams p) {
   griddep_wait();
-  backward_row<T, kEntropy>(p, blockIdx.x / p.slices, threadIdx.x, kThreads,
-                            static_cast<int>(blockIdx.x % p.slices));
+  backward_row<T, kEntropy, false>(p, blockIdx.x / p.slices,
+                                   static_cast<int>(blockIdx.x % p.slices));
 }
 
 template <typename T, bool kEntropy>
 __global__ void __launch_bounds__(kThreads) logprobs_backward_warp_kernel(const BackwardParams p) {
   griddep_wait();
   const int64_t r = static_cast<int64_t>(blockIdx.x) * (kThreads / 32) + (threadIdx.x >> 5);
-  if (r < p.rows) backward_row<T, kEntropy>(p, r, threadIdx.x & 31, 32, 0);
+  if (r < p.rows) backward_row<T, kEntropy, true>(p, r, 0);
 }
 
 // ------------------------------------------------------------------- host
@@ -478,8 +521,9 @@ cudaError_t run_forward(const LogprobArgs& a, cudaStream_t s) {
 
 template <typename T, bool kEntropy>
 cudaError_t run_backward(const LogprobGradArgs& a, cudaStream_t s) {
-  BackwardParams p{a.x, a.rows, a.V, a.ld, a.targets, static_cast<float>(1.0 / a.tau), a.lse,
-                   a.entropy, a.d_logp, a.d_entropy, a.dx, a.ld_d, 1, a.status};
+  BackwardParams p{a.x, a.rows, a.V, a.ld, a.targets, static_cast<float>(1.0 / a.tau),
+                   static_cast<float>(1.4426950408889634 / a.tau), a.lse, a.entropy, a.d_logp,
+                   a.d_entropy, a.dx, a.ld_d, 1, a.status};
   const int64_t bytes = a.V * static_cast<int64_t>(sizeof(T));
   if (rows_to_warps(a.rows, bytes)) {
     const int64_t grid = (a.rows + kThreads / 32 - 1) / (kThreads / 32);

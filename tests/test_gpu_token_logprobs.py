@@ -311,3 +311,60 @@ def test_many_rows_of_middling_length(R, V, dtype):
     w[::5] = 0.0
     check_backward(x, t, 0.9, w, None)
     check_backward(x, t, 0.9, w, 0.1 * w)
+
+
+def check_gradient_about_top(x, t, tau, w, h, in_place=False, pad=0):
+    """The backward pass where lse is far from 0: what counts are the differences from
+    the row's largest logit, so the bound goes by those and not by the logits' size."""
+    R, V = x.shape
+    ref = np64(x)
+    lse, ent = torch.empty(R, device=DEV), torch.empty(R, device=DEV)
+    bg.bergson_token_logprobs(x, t, tau, torch.empty(R, device=DEV), lse, ent)
+    dx = x if in_place else torch.full((R, V + pad), 7.0, dtype=x.dtype, device=DEV)[:, :V]
+    wd, hd = (None if y is None else torch.tensor(y, dtype=torch.float32, device=DEV) for y in (w, h))
+    bg.bergson_token_logprobs_backward(x, t, tau, lse, ent, wd, hd, dx)
+    assert bg.bergson_sync_status() == bg.BERGSON_OK, bg.bergson_last_error()
+    w64, h64 = (np.zeros(R) if y is None else np64(y) for y in (wd, hd))
+    # the fp64 oracle's own lse rounds at 2^-53 |z|, so it gets the rows about their tops
+    top = np.max(np.where(np.isfinite(ref), ref, -INF), axis=1, keepdims=True)
+    want = orc.token_logprobs_backward(ref - top, t.tolist(), tau, w64, h64)
+    z = (ref - top) / tau
+    p = np.exp(z) / np.exp(z).sum(1, keepdims=True)
+    logq = np.where(p > 0, np.abs(np.log(np.maximum(p, 1e-300))), 0.0)
+    p[np.arange(R), t.tolist()] += 1
+    tol = 1e-6 * (2 * np.where(p > 1e-30, np.abs(z), 0).max() + 8)
+    size = (np.abs(w64)[:, None] * p + np.abs(h64)[:, None] * p * (logq + 12)) / tau
+    bound = (tol + 4e-7) * size + HALF_UNIT[x.dtype] * np.abs(want) + SMALLEST[x.dtype]
+    got = np64(dx)
+    assert np.all(np.abs(got - want) <= bound), np.max(np.abs(got - want) / bound)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("V,pad", [(40, 0), (3000, 3), (70_001, 0), (70_000, 5)])
+def test_gradients_where_lse_cannot_hold_the_sum(V, pad, dtype):
+    """Rows of one large value, as a finite mask over all of them leaves (an even distribution), rows
+    at a large common offset, and a large top above others: lse's last digit is larger than log V."""
+    low = -6e4 if dtype == torch.float16 else -1e9
+    g = np.random.default_rng(V)
+    for in_place in (False, True):
+        for w, h in ((g.normal(size=6), None), (g.normal(size=6), 0.1 * g.normal(size=6))):
+            x, t = logits(6, V, dtype, seed=V)
+            x[0] = low
+            x[1] = -low
+            x[2] = low
+            x[2, V // 2:] = -INF
+            t[2] = 1
+            x[3] = -low / 4
+            x[3, ::3] = -low
+            x[4] = (torch.randn(V, device=DEV) * 3 + 9000).to(dtype)
+            check_gradient_about_top(x, t, 1.0, w, h, in_place, pad)
+            check_gradient_about_top(logits(6, V, dtype, seed=1)[0] * 0 + low / 2, t, 0.5, w, h)
+
+
+def test_many_rows_where_lse_cannot_hold_the_sum():
+    """... on warps, beside rows of ordinary size."""
+    x, t = logits(1300, 3001, torch.float32, seed=4)
+    x[::2] += 2.0 ** 20
+    w = np.random.default_rng(0).normal(size=1300)
+    check_gradient_about_top(x, t, 1.0, w, 0.1 * w)
+    check_gradient_about_top(x, t, 1.0, w, None, in_place=True)
