@@ -750,14 +750,15 @@ BERGSON_API int bergson_token_logprobs_backward(const void* logits, int dtype, i
  * hold there; a sequence, or a batch, without valid tokens has loss 0.
  *
  *   logp, old_logp   fp32 [B, ld] each.
- *   ref_logp  fp32 [B, ld_ref], NULL only with kl_coef == 0 (the term is then left out).
+ *   ref_logp  fp32 [B, ld_ref], NULL only with kl_coef == 0, which leaves the term out; k is
+ *             then taken for stats alone.
  *   entropy   fp32 [B, ld_entropy], NULL only with entropy_coef == 0.
  *   advantages  fp32: [B], one a sequence, with ld_adv == 0; else [B, ld_adv].
  *   mask      u8 [B, ld_mask] (nonzero = valid) or NULL (all valid).
  *   clip_low in [0, 1], clip_high >= 0, norm_tokens > 0 (SUM_NORM only).
  *   loss      fp32 [1];  seq_loss  fp32 [B] or NULL: the sequences' shares of it.
- *   stats     fp32 [3] or NULL: mean of k, share of tokens whose ratio is clipped
- *             (ratio A > clamped A), number of valid tokens.
+ *   stats     fp32 [3] or NULL: mean of k (0 where ref_logp is NULL), share of tokens
+ *             whose ratio is clipped (ratio A > clamped A), number of valid tokens.
  *   d_logp    fp32 [B, ld_d];  d_entropy  fp32 [B, ld_de] or NULL.
  *   workspace 256-byte aligned, contents on entry ignored.
  * Leading dimensions are >= T.  B, T >= 0, T <= 2^30, B * T <= 2^40.  Sums run in fp32 within 1024

@@ -67,9 +67,10 @@ def policy_loss(logp, old, ref, ent, adv, mask, low, high, kl_coef, ent_coef, re
     l = -np.minimum(free, held)
     grad = np.where(clip, 0.0, -free)
     k = z
-    if kl_coef:
+    if ref is not None:
         gap = np.where(mask, ref, 0.0) - lp
         k = np.expm1(gap) - gap
+    if kl_coef:
         l = l + kl_coef * k
         grad = grad - kl_coef * np.expm1(gap)
     if ent_coef:

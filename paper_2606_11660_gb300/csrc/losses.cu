@@ -344,9 +344,11 @@ __device__ __forceinline__ float4 policy_segment(const PolicyParams& p, int64_t 
       if (p.a.ref_logp != nullptr) {
         float k, up;
         kl_of(ref[j] - lp[j], &k, &up);
-        l = fmaf(p.kl, k, l);
-        grad = fmaf(-p.kl, up, grad);
         kls += k;
+        if (p.kl != 0.0f) {                    // 0: k is watched alone, also where it is infinite
+          l = fmaf(p.kl, k, l);
+          grad = fmaf(-p.kl, up, grad);
+        }
       }
       if (p.a.entropy != nullptr) l = fmaf(-p.ent, ent[j], l);
       loss += l;
@@ -902,7 +904,7 @@ cudaError_t launch_policy_loss(const bergson_policy_args& a, void* ws, cudaStrea
   p.kl = static_cast<float>(a.kl_coef);
   p.ent = static_cast<float>(a.entropy_coef);
   p.norm = static_cast<float>(1.0 / (static_cast<double>(a.B) * a.norm_tokens));
-  if (a.kl_coef == 0.0) p.a.ref_logp = nullptr;
+  if (a.kl_coef == 0.0 && a.stats == nullptr) p.a.ref_logp = nullptr;
   if (a.entropy_coef == 0.0) p.a.entropy = nullptr;
   if (a.B == 0 || a.T == 0) {                  // no token: zeros
     cudaError_t e = cudaMemsetAsync(a.loss, 0, sizeof(float), s);

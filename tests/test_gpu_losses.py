@@ -362,3 +362,20 @@ def test_rows_off_vector_boundaries(T, pad):
         logp, ref, mask = preference_inputs(B, T, seed=T)
         check_preference(logp, ref, mask, pad=pad)
         check_preference(logp, None, None, pad=pad)
+
+
+@pytest.mark.parametrize("reduction", REDUCTIONS)
+@pytest.mark.parametrize("B,T", [(6, 90), (300, 700)])
+def test_policy_watches_the_reference_without_the_term(B, T, reduction):
+    """kl_coef = 0 with a reference: the mean of k is reported, the loss and gradients are those without."""
+    logp, old, ref, ent, adv, mask = policy_inputs(B, T, seed=12)
+    got, want = check_policy((logp, old, ref, ent, adv, mask), kl=0.0, reduction=reduction)
+    assert want["stats"][0] > 0.01
+    none = run_policy(logp, old, None, ent, adv, mask, kl=0.0, reduction=reduction)
+    for k in ("loss", "seq", "d", "dh"):
+        assert np.array_equal(got[k], none[k])
+    ref[mask.nonzero()[0][0], mask.nonzero()[1][0]] = INF
+    spoilt = run_policy(logp, old, ref, ent, adv, mask, kl=0.0, reduction=reduction)
+    assert np.isnan(spoilt["stats"][0])           # exp(inf) - inf
+    for k in ("loss", "seq", "d", "dh"):
+        assert np.array_equal(spoilt[k], none[k])
