@@ -379,3 +379,22 @@ def test_policy_watches_the_reference_without_the_term(B, T, reduction):
     assert np.isnan(spoilt["stats"][0])           # exp(inf) - inf
     for k in ("loss", "seq", "d", "dh"):
         assert np.array_equal(spoilt[k], none[k])
+
+
+@pytest.mark.parametrize("pad", [0, 1])
+def test_policy_large_gaps_to_the_reference(pad):
+    """Gaps of a quarter to 60, exact in fp32, weights and coefficient powers of two: the gradient is
+    kl_coef (exp(gap) - 1) / n within exp's 2 units and three roundings."""
+    gap = np.concatenate([np.linspace(-60, 60, 3841), np.linspace(-4, 4, 255)])
+    gap = f32(np.round(gap * 1024) / 1024).reshape(4, 1024)
+    logp = f32(-np.round(np.random.default_rng(0).exponential(size=gap.shape) * 1024) / 1024)
+    ref = logp + gap
+    assert np.array_equal(ref - logp, gap)
+    got = run_policy(logp, logp, ref, None, f32(np.zeros(4)), None, kl=0.0625, ec=0.0, pad=pad)
+    up = np.expm1(gap.astype(np.float64))
+    big = np.abs(gap) >= 0.25
+    off = np.abs(got["d"] + 0.0625 * up / 4096)
+    assert np.all((off <= 7 * 2.0 ** -24 * (np.abs(up) + 1) * 0.0625 / 4096)[big])
+    k = up - gap
+    assert abs(got["stats"][0] - k.mean()) <= 2e-6 * k.mean()
+    assert abs(got["loss"][0] - 0.0625 * k.mean()) <= 2e-6 * 0.0625 * k.mean()
