@@ -865,6 +865,9 @@ typedef struct bergson_adamw_tensor {
  *   param <- param - lr lr_scale ( (m / (1 - beta1^step)) /
  *              (sqrt(v / (1 - beta2^step)) + eps) + weight_decay param ).
  *
+ * v / (1 - beta2^step) counts as 2^-126 at least, so that with eps = 0 a moment of 0 beside a
+ * v of 0 moves nothing.
+ *
  * 8-bit states hold code value * block scale, the scale such that the block's
  * largest magnitude takes the largest code.  m and v are rounded to a code up
  * or down by chance, so that on average no more than 2^-16 of a code's step is lost

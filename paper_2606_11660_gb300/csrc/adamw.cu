@@ -129,11 +129,11 @@ __device__ __forceinline__ float next_first(const StepScalars& s, float m, float
 __device__ __forceinline__ float next_second(const StepScalars& s, float v, float g) {
   return __fadd_rn(__fmul_rn(v, s.b2), __fmul_rn(__fmul_rn(g, g), s.a2));
 }
-// w - lr (c1 m / (sqrt(c2 v) + eps) + wd w).  The root counts at least as that of the
-// normal range's end, 1e-19: 0 / 0 cannot arise.
+// w - lr (c1 m / (sqrt(vc) + eps) + wd w), vc = c2 v.  It counts at least as the normal range's
+// end: 0 / 0 cannot arise.
 __device__ __forceinline__ float next_weight(const StepScalars& s, const Entry& e, float w, float m,
-                                             float v) {
-  const float root = sqrt_approx(fmaf(v, s.c2, 1.17549435e-38f));
+                                             float vc) {
+  const float root = sqrt_approx(at_least(vc, 1.17549435e-38f));
   return fmaf(-e.lr_c1 * m, rcp_approx(root + s.eps), fmaf(-e.lr_wd, w, w));
 }
 __device__ __forceinline__ float block_top(float top) {     // of the warp's lanes, NaN the largest
@@ -203,8 +203,9 @@ __device__ __forceinline__ void block_vectors(const StepScalars& s, const Entry&
     // one lane each: a sum of two lanes would be merged with the products before it
     m[k] = __fadd_rn(m2.x, mg.x); m[k + 1] = __fadd_rn(m2.y, mg.y);
     v[k] = __fadd_rn(v2.x, vg.x); v[k + 1] = __fadd_rn(v2.y, vg.y);
-    w[k] = next_weight(s, e, w[k], m[k], v[k]);
-    w[k + 1] = next_weight(s, e, w[k + 1], m[k + 1], v[k + 1]);
+    const float2 vc = mul2(make_float2(v[k], v[k + 1]), pair(s.c2));
+    w[k] = next_weight(s, e, w[k], m[k], vc.x);
+    w[k + 1] = next_weight(s, e, w[k + 1], m[k + 1], vc.y);
   }
   if (master) store8(e.master, BERGSON_F32, i, w);
   store8(e.p, e.pt, i, w);
@@ -273,7 +274,8 @@ __device__ __noinline__ void block_elements(const StepScalars& s, const Entry& e
     m[k] = next_first(s, m0, g);
     v[k] = next_second(s, v0, g);
     const float w = next_weight(
-        s, e, e.master != nullptr ? e.master[i] : load_as_f32(e.p, e.pt, i), m[k], v[k]);
+        s, e, e.master != nullptr ? e.master[i] : load_as_f32(e.p, e.pt, i), m[k],
+        v[k] * s.c2);
     if (e.master != nullptr) e.master[i] = w;
     store_from_f32(e.p, e.pt, i, w);
     if (!eight) {

@@ -141,6 +141,12 @@ __device__ __forceinline__ float max_nan(float a, float b) {
   asm("max.NaN.f32 %0, %1, %2;" : "=f"(y) : "f"(a), "f"(fabsf(b)));
   return y;
 }
+// The larger of two; NaN if one is.
+__device__ __forceinline__ float at_least(float a, float b) {
+  float y;
+  asm("max.NaN.f32 %0, %1, %2;" : "=f"(y) : "f"(a), "f"(b));
+  return y;
+}
 // Four bytes, x0 the lowest, of integers held to [0, 255].
 __device__ __forceinline__ uint32_t pack_bytes(int x0, int x1, int x2, int x3) {
   uint32_t hi, d;

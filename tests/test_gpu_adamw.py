@@ -325,3 +325,22 @@ def test_lowest_step_of_the_first_moment(power, offset):
     got = float(out[inner].double().mean())
     # 130,560 draws of 0 or 1.125 * 2^-15: half of that, over the root, is 1.4e-3 of it; 4 sigma
     assert abs(got - power) < 4 * 1.4e-3 * 1.125 * 2.0 ** -15, (got, power)
+
+
+@pytest.mark.parametrize("offset", [0, 1])
+def test_tiny_moments_without_eps(offset):
+    """eps = 0: the step is m / sqrt(v) down to the smallest normal v (5 roundings and the two
+    approximations' units: 1e-6), and 0 where both are 0."""
+    hyper = dict(lr=1.0, beta1=0.9, beta2=0.99, eps=0.0)
+    t = make(600, wd=0.0, offset=offset)
+    v = 10.0 ** np.linspace(-37, -20, 600)
+    t.v.copy_(torch.tensor(v)), t.m.copy_(torch.tensor(0.5 * np.sqrt(v)))
+    t.param.zero_(), t.grad.zero_()
+    t.m[7] = t.v[7] = 0.0
+    m32, v32 = n64(t.m), n64(t.v)
+    bg.bergson_adamw_step([t], step=100_000, **hyper)
+    got = n64(t.param)
+    assert got[7] == 0.0
+    keep = np.arange(600) != 7
+    want = -(0.9 * m32) / np.sqrt(0.99 * np.where(keep, v32, 1.0))
+    np.testing.assert_allclose(got[keep], want[keep], rtol=1e-6)
