@@ -797,7 +797,6 @@ int record_error(int code, const char* fmt, ...) {
 
 int injected_status() { return injected(); }
 int* device_status_word(int dev) { return status_word(dev); }
-int device_sm_count(int dev) { return sm_count(dev); }
 
 CUresult encode_tmap_2d(CUtensorMap* tm, CUtensorMapDataType dt, const void* ptr, int64_t inner,
                         int64_t outer, int64_t row_bytes, int box_inner, int box_outer) {

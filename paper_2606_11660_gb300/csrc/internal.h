@@ -189,9 +189,8 @@ struct ScoreParams {
 int record_error(int code, const char* fmt, ...);
 // The status a pending bergson_debug_inject_status() asks this call to return.
 int injected_status();
-// The device status word of `dev` (current), or nullptr; its SM count, or 0.
+// The device status word of `dev` (current), or nullptr.
 int* device_status_word(int dev);
-int device_sm_count(int dev);
 
 // Makes the device owning `ptr` current for the lifetime of the guard.
 struct DeviceGuard {

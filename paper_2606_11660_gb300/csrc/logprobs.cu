@@ -503,7 +503,7 @@ cudaError_t run_forward(const LogprobArgs& a, cudaStream_t s) {
   }
   // Few rows: the CTAs of a cluster share one.
   int parts = 1;
-  while (parts < 8 && a.rows * parts < 2 * a.sms && bytes / parts >= kPartBytes) parts *= 2;
+  while (parts < 8 && a.rows * parts < 2 * kPlanCTAs && bytes / parts >= kPartBytes) parts *= 2;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(static_cast<unsigned>(a.rows * parts));
   cfg.blockDim = dim3(kThreads);

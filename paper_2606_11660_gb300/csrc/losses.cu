@@ -846,7 +846,7 @@ cudaError_t run_policy(PolicyParams p, cudaStream_t s) {
 }
 
 template <int N, bool kVec, bool kRef>
-cudaError_t run_preference(const PreferenceParams& p, int sms, cudaStream_t s) {
+cudaError_t run_preference(const PreferenceParams& p, cudaStream_t s) {
   const int64_t P = p.a.P;
   // few short pairs: one launch, their losses added through the cluster (4 x 383 tokens
   // 8.0 us, 9.9 with the second grid)
@@ -856,7 +856,7 @@ cudaError_t run_preference(const PreferenceParams& p, int sms, cudaStream_t s) {
     return launch_cluster(preference_kernel<N, kVec, kRef, true>, n, kPairThreads, n, p, s);
   }
   int parts = 1;
-  while (parts < 8 && P * parts < kPairCtas * sms && p.a.T / parts > kPairTokens) parts *= 2;
+  while (parts < 8 && P * parts < kPairCtas * kPlanCTAs && p.a.T / parts > kPairTokens) parts *= 2;
   cudaError_t e;
   if (P >= kManyPairs && p.a.T <= kShortPair)
     e = launch_dependent(preference_warp_kernel<N, kVec, kRef>,
@@ -871,9 +871,9 @@ cudaError_t run_preference(const PreferenceParams& p, int sms, cudaStream_t s) {
 }
 
 template <int N, bool kVec>
-cudaError_t run_preference(const PreferenceParams& p, int sms, cudaStream_t s) {
-  return p.a.ref_logp != nullptr ? run_preference<N, kVec, true>(p, sms, s)
-                                 : run_preference<N, kVec, false>(p, sms, s);
+cudaError_t run_preference(const PreferenceParams& p, cudaStream_t s) {
+  return p.a.ref_logp != nullptr ? run_preference<N, kVec, true>(p, s)
+                                 : run_preference<N, kVec, false>(p, s);
 }
 
 }  // namespace
@@ -928,7 +928,7 @@ cudaError_t launch_policy_loss(const bergson_policy_args& a, void* ws, cudaStrea
   return vec ? run_policy<true>(p, s) : run_policy<false>(p, s);
 }
 
-cudaError_t launch_preference_loss(const bergson_preference_args& a, int sms, cudaStream_t s) {
+cudaError_t launch_preference_loss(const bergson_preference_args& a, cudaStream_t s) {
   if (a.P == 0) {
     preference_finish_kernel<<<1, 1024, 0, s>>>(a.pair_loss, 0, a.loss);
     return cudaGetLastError();
@@ -940,8 +940,8 @@ cudaError_t launch_preference_loss(const bergson_preference_args& a, int sms, cu
            fits(a.ref_logp, a.ld_ref, 4, n, a.ld_logp) &&
            fits(a.mask, a.ld_mask, 1, n, a.ld_logp) && fits(a.d_logp, a.ld_d, 4, n, a.ld_logp);
   };
-  if (all_fit(8)) return run_preference<8, true>(p, sms, s);
-  return all_fit(4) ? run_preference<4, true>(p, sms, s) : run_preference<4, false>(p, sms, s);
+  if (all_fit(8)) return run_preference<8, true>(p, s);
+  return all_fit(4) ? run_preference<4, true>(p, s) : run_preference<4, false>(p, s);
 }
 
 }  // namespace bergson

@@ -21,7 +21,6 @@ struct LogprobArgs {
   float* lse;
   float* entropy;
   int* status;
-  int sms;
 };
 cudaError_t launch_token_logprobs(const LogprobArgs& a, cudaStream_t s);
 
@@ -43,7 +42,7 @@ cudaError_t launch_token_logprobs_backward(const LogprobGradArgs& a, cudaStream_
 
 size_t policy_workspace(int64_t B, int64_t T);
 cudaError_t launch_policy_loss(const bergson_policy_args& a, void* ws, cudaStream_t s);
-cudaError_t launch_preference_loss(const bergson_preference_args& a, int sms, cudaStream_t s);
+cudaError_t launch_preference_loss(const bergson_preference_args& a, cudaStream_t s);
 
 struct AdamwScalars {
   double lr, beta1, beta2, eps;

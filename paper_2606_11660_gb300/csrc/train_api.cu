@@ -109,8 +109,7 @@ int bergson_token_logprobs(const void* logits, int dtype, int64_t rows, int64_t 
   if (dg.err != cudaSuccess) return fail_cuda(dg.err, "output device lookup");
   int* status = device_status_word(dg.dev);
   if (status == nullptr) return fail(BERGSON_ECUDA, "device status word unavailable");
-  const LogprobArgs a{logits, dtype, rows, V, ld, targets, tau, logp, lse, entropy, status,
-                      kPlanCTAs};
+  const LogprobArgs a{logits, dtype, rows, V, ld, targets, tau, logp, lse, entropy, status};
   const cudaError_t e = launch_token_logprobs(a, static_cast<cudaStream_t>(stream));
   if (e != cudaSuccess) return fail_cuda(e, "token log-probability launch");
   return BERGSON_OK;
@@ -229,7 +228,7 @@ int bergson_preference_loss(const bergson_preference_args* args, void* stream) {
   BERGSON_TRY(injected_status());
   DeviceGuard dg(a.loss);
   if (dg.err != cudaSuccess) return fail_cuda(dg.err, "output device lookup");
-  const cudaError_t e = launch_preference_loss(a, kPlanCTAs, static_cast<cudaStream_t>(stream));
+  const cudaError_t e = launch_preference_loss(a, static_cast<cudaStream_t>(stream));
   if (e != cudaSuccess) return fail_cuda(e, "preference loss launch");
   return BERGSON_OK;
 }
