@@ -870,9 +870,8 @@ typedef struct bergson_adamw_tensor {
  *
  * 8-bit states hold code value * block scale, the scale such that the block's
  * largest magnitude takes the largest code.  m and v are rounded to a code up
- * or down by chance, so that on average no more than 2^-16 of a code's step is lost
- * of a change, however small the moment (one that moves by 1% a step would never
- * leave its code otherwise); the
+ * or down by chance, so that on average no part of a small change is lost (a
+ * moment that moves by 1% a step would never leave its code otherwise); the
  * 16 bits of chance of elements 4q .. 4q + 3 of tensor i are output q + 1 of the
  * SplitMix64 sequence that starts at mix(i ^ mix(seed ^ mix(step))).  A v > 0 below
  * the smallest code takes that code.  The parameters see m and v before rounding.

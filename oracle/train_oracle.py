@@ -149,9 +149,8 @@ def code_values(second: bool):
 
 def quantise(x, second, rnd):
     """(codes, fp32 scales) of fp32 values x: with y = |x| / scale between two
-    codes' values (zero, of code 0, among a first moment's), the upper one is taken
-    if the part of the step above the lower one plus rnd / 2^16 reaches 1.  A second
-    moment above 0 takes code 1 at least."""
+    codes' values, the upper one is taken if the part of the step above the lower
+    one plus rnd / 2^16 reaches 1."""
     x = np.asarray(x, np.float32)
     n = x.size
     levels = np.float32(code_values(second)[:256 if second else 128])
@@ -168,8 +167,6 @@ def quantise(x, second, rnd):
         # as fractions of a binade: the codes' levels are evenly spaced in each
         e = np.floor(np.log2(np.maximum(y.astype(np.float64), 2.0 ** -140)))
         at = (e + (31 if second else 15)) * 8 + (y / 2.0 ** e - 1) * 8
-        if not second:
-            at = np.where(y < levels[1], y / np.float64(levels[1]), at)
         k = np.floor(at + rnd[part] / 65536.0).astype(np.int64)
         k = np.clip(k, 0, len(levels) - 1)
         if second:

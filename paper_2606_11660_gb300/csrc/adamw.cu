@@ -233,16 +233,9 @@ __device__ __forceinline__ void block_vectors(const StepScalars& s, const Entry&
     cm[q] = encode_first4(m + 4 * q, im, c);
     cv[q] = encode_second4(v + 4 * q, iv, c);
   }
-  // codes of 0 again
-  if (__any_sync(0xffffffffu, (zero_bytes(cm[0] & 0x7f7f7f7fu) | zero_bytes(cm[1] & 0x7f7f7f7fu) |
-                               zero_bytes(cv[0]) | zero_bytes(cv[1])) != 0)) {
-#pragma unroll
-    for (int q = 0; q < 2; ++q) {
-      uint32_t c[4];
-      chances(mix64(at + q * kSplitMixGamma), c);
-      cm[q] = raise_first4(cm[q], m + 4 * q, im, c);
-      cv[q] = raise_zeros4(cv[q], v + 4 * q);
-    }
+  if (__any_sync(0xffffffffu, (zero_bytes(cv[0]) | zero_bytes(cv[1])) != 0)) {
+    cv[0] = raise_zeros4(cv[0], v);
+    cv[1] = raise_zeros4(cv[1], v + 4);
   }
   *reinterpret_cast<uint2*>(static_cast<uint8_t*>(e.m) + i) = make_uint2(cm[0], cm[1]);
   *reinterpret_cast<uint2*>(static_cast<uint8_t*>(e.v) + i) = make_uint2(cv[0], cv[1]);

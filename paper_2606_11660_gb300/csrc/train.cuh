@@ -240,8 +240,7 @@ __device__ __forceinline__ F block_sum(F v, F* red) {
 
 // ---- 8-bit states.  A code is the top bits of a positive float below its sign,
 // less those of the smallest magnitude held: truncating the bits and adding chance
-// below the cut rounds up with a probability equal to the part cut off.  Code 0 is zero and not the
-// magnitude below code 1's: m takes code 1 from there with a probability of its share of that.
+// below the cut rounds up with a probability equal to the part cut off.
 constexpr int kCodeShift = 20;                 // three bits of mantissa stay
 constexpr int kFirstBase = 112 << 3;           // m: exponents 2^-15 .. 2^0 in 7 bits
 constexpr int kSecondBase = 96 << 3;           // v: exponents 2^-31 .. 2^0 in 8 bits
@@ -262,17 +261,11 @@ __device__ __forceinline__ float block_scale(float top) {
 __device__ __forceinline__ float block_inverse(float scale) {
   return scale > 0.0f ? __frcp_rn(scale) : 0.0f;
 }
-// Whether y, below code 1's value of 1.125 * 2^-15, takes that code: y / value + chance / 2^16 >= 1,
-// with `chance` as it stands below the cut (16 times as much).  Every term is exact.
-__device__ __forceinline__ bool takes_first_code(float y, uint32_t chance) {
-  return y * 0x1p35f >= 1.125f * static_cast<float>((1 << kCodeShift) - static_cast<int>(chance));
-}
 // `chance`: 16 random bits.
 __device__ __forceinline__ uint32_t encode_first(float m, float inv, uint32_t chance) {
   const float y = __fmul_rn(fabsf(m), inv);
   int code = ((__float_as_int(y) + static_cast<int>(chance << 4)) >> kCodeShift) - kFirstBase;
   code = min(max(code, 0), 127);
-  if (code == 0 && takes_first_code(y, chance << 4)) code = 1;
   return static_cast<uint32_t>(code) | (m < 0.0f ? 128u : 0u);
 }
 __device__ __forceinline__ uint32_t encode_second(float v, float inv, uint32_t chance) {
@@ -338,7 +331,7 @@ __device__ __forceinline__ void chances(uint64_t h, uint32_t (&c)[4]) {
   c[2] = (hi << 4) & 0xffff0u;
   c[3] = (hi >> 12) & 0xffff0u;
 }
-// encode_first and encode_second (but for raise_first4 and raise_zeros4) of four elements.  The first's
+// encode_first and encode_second (but for raise_zeros4) of four elements.  The first's
 // magnitudes are packed with one bit more, so that holding them to a byte holds them to 7 bits.
 __device__ __forceinline__ uint32_t encode_first4(const float* m, float inv, const uint32_t* c) {
   int x[4];
@@ -358,15 +351,6 @@ __device__ __forceinline__ uint32_t encode_second4(const float* v, float inv, co
     x[k] = (__float_as_int(__fmul_rn(v[k], inv)) + static_cast<int>(c[k]) -
             (kSecondBase << kCodeShift)) >> kCodeShift;
   return pack_bytes(x[0], x[1], x[2], x[3]);
-}
-// Code 1 where an m below its value takes it.
-__device__ __forceinline__ uint32_t raise_first4(uint32_t w, const float* m, float inv,
-                                                 const uint32_t* c) {
-#pragma unroll
-  for (int k = 0; k < 4; ++k)
-    if (((w >> (8 * k)) & 127u) == 0 && takes_first_code(__fmul_rn(fabsf(m[k]), inv), c[k]))
-      w |= 1u << (8 * k);
-  return w;
 }
 // Only a v of 0 takes code 0: others get the smallest.
 __device__ __forceinline__ uint32_t raise_zeros4(uint32_t w, const float* v) {

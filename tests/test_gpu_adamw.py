@@ -305,29 +305,6 @@ def test_every_code_has_its_value(second):
 
 
 @pytest.mark.parametrize("offset", [0, 1])
-@pytest.mark.parametrize("power", [2.0 ** -17, 2.0 ** -15, 1.06 * 2.0 ** -15, -2.0 ** -16])
-def test_lowest_step_of_the_first_moment(power, offset):
-    """Moments below the smallest code are held on average too: m takes it with the probability
-    that its mean is m."""
-    n = 256 * 512
-    t = make(n, eight=True, wd=0.0, offset=offset)
-    t.m.zero_(), t.v.zero_(), t.m_scale.zero_(), t.v_scale.zero_()
-    t.grad.fill_(power)
-    t.grad[::256] = 1.875                         # the scale is 1 within a unit
-    hyper = dict(HYPER, beta1=0.0)
-    o = snapshot(t)
-    bg.bergson_adamw_step([t], step=1, seed=3, **hyper)
-    check(t, o, 0, 1, seed=3, hyper=hyper)
-    out = torch.empty(n, device=DEV)
-    bg.bergson_adamw_state_values(t.m, t.m_scale, bg.BERGSON_MOMENT_FIRST, out)
-    inner = torch.ones(n, dtype=torch.bool, device=DEV)
-    inner[::256] = False
-    got = float(out[inner].double().mean())
-    # 130,560 draws of 0 or 1.125 * 2^-15: half of that, over the root, is 1.4e-3 of it; 4 sigma
-    assert abs(got - power) < 4 * 1.4e-3 * 1.125 * 2.0 ** -15, (got, power)
-
-
-@pytest.mark.parametrize("offset", [0, 1])
 def test_tiny_moments_without_eps(offset):
     """eps = 0: the step is m / sqrt(v) down to the smallest normal v (5 roundings and the two
     approximations' units: 1e-6), and 0 where both are 0."""

@@ -94,19 +94,3 @@ def test_factors_have_the_row_and_column_sums():
     want = 2 * v + 1e-3
     approx = r[:, None] * c[None]
     assert np.allclose(approx.sum(1), want.sum(1)) and np.allclose(approx.sum(0), want.sum(0))
-
-
-@pytest.mark.parametrize("y", [2.0 ** -17, 2.0 ** -15, 1.06 * 2.0 ** -15, 1.2 * 2.0 ** -15, 3.3 * 2.0 ** -15])
-def test_small_first_moments_are_unbiased(y):
-    """The mean over all 2^16 chances, below the smallest code (1.125 * 2^-15) and above it."""
-    x = np.full(256, y, np.float32)
-    x[0] = 1.875
-    mean = 0.0
-    for first in range(0, 65536, 255):
-        rnd = np.minimum(first + np.arange(-1, 255), 65535)
-        codes, scales = orc.quantise(x, False, rnd)
-        assert scales[0] == np.float32(np.float32(1.875) * np.float32(1 / 1.875))
-        live = (rnd >= first) & (first + np.arange(-1, 255) < 65536)
-        mean += orc.dequantise(codes, scales, False)[live].sum() / 65536
-    # 2^-16 of a code's step, and the scale's rounding
-    assert abs(mean - y) <= 1.125 * 2.0 ** -31 + 2.0 ** -22 * y
