@@ -871,12 +871,16 @@ typedef struct bergson_adamw_tensor {
  * 8-bit states hold code value * block scale, the scale such that the block's
  * largest magnitude takes the largest code.  m and v are rounded to a code up
  * or down by chance, so that on average no part of a small change is lost (a
- * moment that moves by 1% a step would never leave its code otherwise); the
- * 16 bits of chance of elements 4q .. 4q + 3 of tensor i are output q + 1 of the
- * SplitMix64 sequence that starts at mix(i ^ mix(seed ^ mix(step))).  A v > 0 below
- * the smallest code takes that code.  The parameters see m and v before rounding.
- * A gradient that is infinite or NaN spoils its element (fp32 moments) or the
- * moments of its block of 256 (8-bit ones).
+ * moment that moves by 1% a step would never leave its code otherwise) of moments
+ * from the smallest code's value on, 1.125 * 2^-15 of the scale for m and 1.125 *
+ * 2^-31 for v.  Below it, a v > 0 takes that code.  An |m| of up to 2^-15 of the scale
+ * becomes 0, and between the two it takes the smallest code with a probability that
+ * rises from 0 to 1: what is lost of an m is at most 2^-15 of the scale, 1.7e-5 of its
+ * block's largest.  The 16 bits of chance of elements 4q .. 4q + 3 of tensor i are output
+ * q + 1 of the SplitMix64 sequence that starts at mix(i ^ mix(seed ^ mix(step))).  The
+ * parameters see m and v before rounding.
+ * A gradient that is infinite or NaN, or whose square is, spoils its element (fp32
+ * moments) or the moments of its block of 256 (8-bit ones).
  *
  *   tensors   HOST array of n_tensors (>= 0) records.
  *   step      >= 1: the number of this step.  beta1, beta2 in [0, 1), eps >= 0.

@@ -240,7 +240,9 @@ __device__ __forceinline__ F block_sum(F v, F* red) {
 
 // ---- 8-bit states.  A code is the top bits of a positive float below its sign,
 // less those of the smallest magnitude held: truncating the bits and adding chance
-// below the cut rounds up with a probability equal to the part cut off.
+// below the cut rounds up with a probability equal to the part cut off.  Code 0 has the place of
+// the magnitude below code 1's but stands for zero: an m of up to 2^-15 of the scale is dropped, a
+// v > 0 takes code 1 at least.
 constexpr int kCodeShift = 20;                 // three bits of mantissa stay
 constexpr int kFirstBase = 112 << 3;           // m: exponents 2^-15 .. 2^0 in 7 bits
 constexpr int kSecondBase = 96 << 3;           // v: exponents 2^-31 .. 2^0 in 8 bits

@@ -321,3 +321,27 @@ def test_tiny_moments_without_eps(offset):
     keep = np.arange(600) != 7
     want = -(0.9 * m32) / np.sqrt(0.99 * np.where(keep, v32, 1.0))
     np.testing.assert_allclose(got[keep], want[keep], rtol=1e-6)
+
+
+@pytest.mark.parametrize("offset", [0, 1])
+@pytest.mark.parametrize("y", [2.0 ** -17, 2.0 ** -15, 1.06 * 2.0 ** -15, -1.2 * 2.0 ** -15])
+def test_small_first_moments_keep_the_stated_mean(y, offset):
+    """From the smallest code's value on, 1.125 * 2^-15 of the scale, m keeps its mean; 2^-15 and less
+    becomes 0, and between them the smallest code is taken with a probability that rises from 0 to 1."""
+    n = 256 * 512
+    t = make(n, eight=True, wd=0.0, offset=offset)
+    t.m.zero_(), t.v.zero_(), t.m_scale.zero_(), t.v_scale.zero_()
+    t.grad.fill_(y)
+    t.grad[::256] = 1.875                         # the scale is 1 within a unit
+    hyper = dict(HYPER, beta1=0.0)
+    o = snapshot(t)
+    bg.bergson_adamw_step([t], step=1, seed=3, **hyper)
+    check(t, o, 0, 1, seed=3, hyper=hyper)
+    out = torch.empty(n, device=DEV)
+    bg.bergson_adamw_state_values(t.m, t.m_scale, bg.BERGSON_MOMENT_FIRST, out)
+    inner = torch.ones(n, dtype=torch.bool, device=DEV)
+    inner[::256] = False
+    low, first = 2.0 ** -15, 1.125 * 2.0 ** -15
+    want = abs(y) if abs(y) >= first else first * max(0.0, (abs(y) - low) / (first - low))
+    # 130,560 draws of 0 or `first`: half of that, over the root, is 1.4e-3 of it; 4 sigma
+    assert abs(float(out[inner].double().mean()) - np.sign(y) * want) < 4 * 1.4e-3 * first

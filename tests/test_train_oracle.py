@@ -94,3 +94,26 @@ def test_factors_have_the_row_and_column_sums():
     want = 2 * v + 1e-3
     approx = r[:, None] * c[None]
     assert np.allclose(approx.sum(1), want.sum(1)) and np.allclose(approx.sum(0), want.sum(0))
+
+
+def lowest_step(y):
+    """The mean that a first moment of y (over the scale) keeps: code 0 is zero, but has the place of 2^-15."""
+    low, first = 2.0 ** -15, 1.125 * 2.0 ** -15
+    return y if y >= first else first * max(0.0, (y - low) / (first - low))
+
+
+@pytest.mark.parametrize("y", [2.0 ** -17, 2.0 ** -15, 1.06 * 2.0 ** -15, 1.2 * 2.0 ** -15, 3.3 * 2.0 ** -15])
+def test_small_first_moments(y):
+    """The mean over all 2^16 chances: unbiased from the smallest code (1.125 * 2^-15) on; below it at most
+    2^-15 is lost."""
+    x = np.full(256, y, np.float32)
+    x[0] = 1.875
+    mean = 0.0
+    for first in range(0, 65536, 255):
+        rnd = np.minimum(first + np.arange(-1, 255), 65535)
+        codes, scales = orc.quantise(x, False, rnd)
+        live = (rnd >= first) & (first + np.arange(-1, 255) < 65536)
+        mean += orc.dequantise(codes, scales, False)[live].sum() / 65536
+    # 2^-16 of a code's step, and the scale's rounding (of y, times 9 where the step is steep)
+    assert abs(mean - lowest_step(y)) <= 1.125 * 2.0 ** -31 + 9 * 2.0 ** -22 * y
+    assert 0 <= y - mean + 2.0 ** -22 * y <= 2.0 ** -15 * (1 + 2.0 ** -20)
