@@ -124,3 +124,12 @@ def test_projection_takes_them():
         assert bg.bergson_sync_status() == bg.BERGSON_OK
         outs.append(out)
     assert float((outs[0] - outs[1]).norm() / outs[1].norm()) < 1e-4
+
+
+@pytest.mark.parametrize("eight", [False, True])
+@pytest.mark.parametrize("o,i", [(4096, 2048), (4100, 2064), (4099, 2001), (16_411, 513), (1031, 8192)])
+def test_rows_of_several_turns(o, i, eight):
+    """Matrices whose warps take up to 32 rows each, in several turns of their loops."""
+    m = make(o, i, eight, seed=o)
+    run([m])
+    check(m)

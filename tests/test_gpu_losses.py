@@ -398,3 +398,14 @@ def test_policy_large_gaps_to_the_reference(pad):
     k = up - gap
     assert abs(got["stats"][0] - k.mean()) <= 2e-6 * k.mean()
     assert abs(got["loss"][0] - 0.0625 * k.mean()) <= 2e-6 * 0.0625 * k.mean()
+
+
+@pytest.mark.parametrize("reduction", REDUCTIONS)
+@pytest.mark.parametrize("B,T,pad", [(256, 256, 0), (257, 256, 0), (256, 1, 0), (257, 1, 0), (1, 65_536, 0),
+                                     (1, 65_537, 0), (85, 700, 2), (86, 700, 2), (2431, 1025, 0),
+                                     (2432, 1025, 0), (1650, 2500, 0), (2500, 1030, 1), (1621, 2049, 3),
+                                     (4864, 1000, 4)])
+def test_policy_forms_at_their_limits(B, T, pad, reduction):
+    """One launch up to 256 segments of 256 tokens; segments of 1024 tokens from 4864 of them on, several
+    a row, rows off 16-byte boundaries among them."""
+    check_policy(policy_inputs(B, T, seed=B + 1, token_adv=pad == 1), reduction=reduction, pad=pad)
