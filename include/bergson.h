@@ -682,7 +682,11 @@ BERGSON_API int bergson_project_grads_noalloc(const bergson_layer* layers, int n
  * of the gradient collection; Sec. 5.4's policy optimisation), token by token,
  * the optimiser step, and the second moments r, c that a layer takes (Fig. 1:
  * Adam and Adafactor normalisation).  Rows need no alignment beyond their
- * element type's.
+ * element type's.  Sums run in an order that follows from the sizes, the leading
+ * dimensions and where the tensors start within 32 bytes: a call gives the same bits
+ * every time, but a copy of its tensors at another alignment may give others.
+ * Host arguments (step, lr, seed, correction, coefficients) are taken at the call; a CUDA
+ * graph replays those it was captured with.
  */
 
 /*
@@ -701,7 +705,7 @@ BERGSON_API int bergson_project_grads_noalloc(const bergson_layer* layers, int n
  *             status word.
  *   tau       > 0, 1 / tau and 1.5 / tau in the normal range of fp32.
  *   logp, lse fp32 [rows];  entropy fp32 [rows] or NULL.
- * Sums are fp32, in an order fixed by the sizes.  rows in [0, 2^31), V < 2^31.
+ * Sums are fp32.  rows in [0, 2^31), V < 2^31.
  * Errors: EINVAL, EALIGN, ECUDA.
  */
 BERGSON_API int bergson_token_logprobs(const void* logits, int dtype, int64_t rows, int64_t V,
@@ -723,8 +727,8 @@ BERGSON_API int bergson_token_logprobs(const void* logits, int dtype, int64_t ro
  * not read.  A target >= V makes the row NaN and is recorded as BERGSON_EINVAL in the
  * device status word.  Where |lse| is 4096 or more (a large common offset, a finite
  * mask over the whole row) fp32 holds too few digits of it: what it lacks is summed
- * from the row's logits again, at some loss of speed.  Below, its rounding leaves p
- * within 1.2e-4 (2^-25 |lse| and less).
+ * from the row's logits again, at some loss of speed.  Below, the half of lse's last
+ * digit is in p: 1.2e-4 of it at most.
  * Errors: EINVAL, EALIGN, ECUDA.
  */
 BERGSON_API int bergson_token_logprobs_backward(const void* logits, int dtype, int64_t rows,
@@ -762,7 +766,7 @@ BERGSON_API int bergson_token_logprobs_backward(const void* logits, int dtype, i
  *   d_logp    fp32 [B, ld_d];  d_entropy  fp32 [B, ld_de] or NULL.
  *   workspace 256-byte aligned, contents on entry ignored.
  * Leading dimensions are >= T.  B, T >= 0, T <= 2^30, B * T <= 2^40.  Sums run in fp32 within 1024
- * tokens and in twice its bits above, in an order fixed by the sizes.
+ * tokens and in twice its bits above.
  * Errors: EINVAL, EALIGN, EUNSUPPORTED, EWORKSPACE, ECUDA.
  */
 typedef struct bergson_policy_args {
@@ -808,7 +812,6 @@ BERGSON_API int bergson_policy_loss(const bergson_policy_args* args, void* works
  *   beta > 0, label_smoothing in [0, 1].
  *   loss fp32 [1], pair_loss fp32 [P], rewards fp32 [2P] or NULL, d_logp fp32 [2P, ld_d].
  * Leading dimensions are >= T.  P, T >= 0, P < 2^30, T <= 2^30, 2 P T <= 2^40; P = 0 gives loss 0.
- * Sums over tokens and pairs run in an order fixed by the sizes.
  * Errors: EINVAL, EALIGN, EUNSUPPORTED, ECUDA.
  */
 typedef struct bergson_preference_args {
@@ -883,7 +886,9 @@ typedef struct bergson_adamw_tensor {
  * moments) or the moments of its block of 256 (8-bit ones).
  *
  *   tensors   HOST array of n_tensors (>= 0) records.
- *   step      >= 1: the number of this step.  beta1, beta2 in [0, 1), eps >= 0.
+ *   step      >= 1: the number of this step (a graph replays the one it was
+ *             captured with, its bias corrections and its chances: capture the step anew
+ *             each time, or leave it out).  beta1, beta2 in [0, 1), eps >= 0.
  *   seed      of the 8-bit states' rounding.
  *   grad_scale  device fp32 [1] or NULL (1), e.g. a clipping factor.
  * All tensors live on one device.
@@ -924,7 +929,7 @@ typedef struct bergson_moment_matrix {
  * floor > 0 keeps r and c positive where no gradient has arrived.
  *   mats      HOST array of n_mats (>= 0) records; d_out, d_in >= 1.
  *   workspace 256-byte aligned, contents on entry ignored.
- * Sums are fp32, in an order fixed by the sizes.
+ * Sums are fp32.
  * Errors: EINVAL, EALIGN, EUNSUPPORTED, EWORKSPACE, ECUDA.
  */
 BERGSON_API int bergson_factor_moments_workspace(const bergson_moment_matrix* mats, int n_mats,

@@ -5,7 +5,8 @@
 // their launches.  A token's gradient needs a weight that depends on others: the
 // policy loss counts the valid tokens beforehand (a byte a token), the preference
 // loss holds a pair in a CTA (or a cluster that shares its sums) and comes back to
-// write.  Sums over tokens follow an order fixed by the sizes.
+// write.  Sums over tokens follow an order fixed by the sizes, the leading dimensions and the
+// tensors' alignment.
 //
 // Policy loss of 2048 x 16,384 tokens, KL and entropy terms, a token mean: 123 us (the
 // count 10, the tokens 109, the finish 8), 6.8 TB/s of the 25 bytes a token; masked
