@@ -6,9 +6,10 @@
 // state; a lane has 8 of them, in loads of 8 to 32 bytes.  The step is bound by its
 // bytes: 2 + 2 + 16 an element with 16-bit parameters and gradients and 32-bit
 // states, 2 + 2 + 2 + 4 with 8-bit ones, 8 more with a master copy (2 less read).  201M
-// elements with masters and 32-bit states: 796 us, 7.1 TB/s.  With 8-bit states
+// elements with masters and 32-bit states: 798 us, 7.1 TB/s.  With 8-bit states
 // some 70 instructions an element stand beside the bytes, half of them on the integer
-// pipe: 50M elements with masters 127 us (6.4 TB/s), without 115 (4.4 TB/s).
+// pipe: 50M elements with masters 128 us (6.3 TB/s, two thirds of the issue slots), without 116
+// (4.4 TB/s, three quarters of them).
 //
 // m and v are formed by multiplications and additions that are each rounded
 // (no fused multiply-add): the codes of an 8-bit state then follow from the
