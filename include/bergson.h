@@ -725,10 +725,10 @@ BERGSON_API int bergson_token_logprobs(const void* logits, int dtype, int64_t ro
  * A row whose target is negative, whose w and h are both 0, or whose lse is below
  * -1e30 (nothing but -inf or a type's lowest value) gets zeros and its logits are
  * not read.  A target >= V makes the row NaN and is recorded as BERGSON_EINVAL in the
- * device status word.  Where |lse| is 4096 or more (a large common offset, a finite
+ * device status word.  Where |lse| is 512 or more (a large common offset, a finite
  * mask over the whole row) fp32 holds too few digits of it: what it lacks is summed
  * from the row's logits again, at some loss of speed.  Below, the half of lse's last
- * digit is in p: 1.2e-4 of it at most.
+ * digit is in p: 1.5e-5 of it at most.
  * Errors: EINVAL, EALIGN, ECUDA.
  */
 BERGSON_API int bergson_token_logprobs_backward(const void* logits, int dtype, int64_t rows,

@@ -368,3 +368,13 @@ def test_many_rows_where_lse_cannot_hold_the_sum():
     w = np.random.default_rng(0).normal(size=1300)
     check_gradient_about_top(x, t, 1.0, w, 0.1 * w)
     check_gradient_about_top(x, t, 1.0, w, None, in_place=True)
+
+
+@pytest.mark.parametrize("V", [301, 20_001])
+def test_rows_at_moderate_offsets(V):
+    """Offsets of 600 to 3000, where half of lse's last digit, up to 1.2e-4, would be p's error."""
+    x, t = logits(120, V, torch.float32, seed=V)
+    x += torch.linspace(600, 3000, 120, device=DEV)[:, None]
+    w = np.random.default_rng(0).normal(size=120)
+    check_gradient_about_top(x, t, 1.0, w, None)
+    check_gradient_about_top(x, t, 1.0, w, 0.1 * w)
