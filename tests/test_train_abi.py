@@ -431,3 +431,25 @@ def test_device_tensors_of_other_sizes_are_refused_by_name(name):
             call({**tensors, what: wrong})
         with pytest.raises((ValueError, TypeError)):
             call({**tensors, what: FakeTensor(t.shape, t.strides, torch.float64)})
+
+
+@pytest.mark.parametrize("kind,record", [("bergson_policy_args", "_POLICY_RECORD"),
+                                         ("bergson_preference_args", "_PREFERENCE_RECORD")])
+def test_packed_records_have_the_fields_places(kind, record):
+    from paper_2606_11660_gb300 import binding
+    kind, record = getattr(bg, kind), getattr(binding, record)
+    fields = kind._fields_
+    values = [k + 1.5 if t is ctypes.c_double else k + 1 for k, (_, t) in enumerate(fields)]
+    assert record.size == ctypes.sizeof(kind)
+    packed = kind.from_buffer_copy(record.pack(*values))
+    assert [getattr(packed, name) for name, _ in fields] == values
+
+
+@pytest.mark.parametrize("name,missing", [("policy", ("old_logp", "loss", "d_logp")),
+                                          ("preference", ("loss", "pair_loss", "d_logp"))])
+def test_missing_tensors_are_the_librarys_to_refuse(name, missing):
+    tensors, call = _device_calls()[name]
+    bg.bergson_debug_inject_status(0, 0)
+    for what in missing:
+        with pytest.raises(bg.BergsonError, match="EINVAL"):
+            call({**tensors, what: None})
