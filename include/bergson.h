@@ -110,6 +110,11 @@ typedef enum {
   BERGSON_MOMENT_SECOND = 1       /* v: 5 bits of exponent, 3 of mantissa */
 } bergson_moment;
 
+typedef enum {
+  BERGSON_NORM_LAYER = 0,         /* of a row less its mean */
+  BERGSON_NORM_RMS = 1            /* of the row itself */
+} bergson_norm_kind;
+
 #define BERGSON_STATE_BLOCK 256   /* elements that share a scale of an 8-bit state */
 
 /*
@@ -937,6 +942,51 @@ BERGSON_API int bergson_factor_moments_workspace(const bergson_moment_matrix* ma
 BERGSON_API int bergson_factor_moments(const bergson_moment_matrix* mats, int n_mats,
                                        double correction, double floor, void* workspace,
                                        size_t ws_bytes, void* stream);
+
+/*
+ * Layer norm (BERGSON_NORM_LAYER) of every row of x, or its form without a mean
+ * (BERGSON_NORM_RMS: mu = 0), what stands before the linear layers whose inputs
+ * bergson_layer takes:
+ *
+ *   mu = mean_j x_j,   rstd = (mean_j (x_j - mu)^2 + eps)^-1/2,
+ *   y_j = (x_j - mu) rstd weight_j + bias_j.
+ *
+ *   x         [rows, ld_x] of `dtype` (bergson_dtype), ld_x >= d >= 1.
+ *   weight, bias   [d] of w_dtype, each or NULL (ones, zeros).
+ *   eps       >= 0.  With eps = 0 a row without variance is NaN.
+ *   y         [rows, ld_y] of `dtype`; may be x itself with ld_y == ld_x.
+ *   mean, rstd  fp32 [rows], what the backward pass reads, each or NULL; mean is not
+ *             written without a mean.
+ * Sums are fp32, about the row's mean.  A row that holds NaN or an infinity is NaN; the
+ * others keep their values.  rows in [0, 2^31), d <= 2^24.
+ * Errors: EINVAL, EALIGN, EUNSUPPORTED, ECUDA.
+ */
+BERGSON_API int bergson_norm(const void* x, int dtype, int64_t rows, int64_t d, int64_t ld_x,
+                             const void* weight, const void* bias, int w_dtype, int kind,
+                             double eps, void* y, int64_t ld_y, float* mean, float* rstd,
+                             void* stream);
+
+/*
+ * The backward pass: with n = (x - mu) rstd and h = dy weight,
+ *
+ *   dx = rstd (h - mean_j h - n mean_j (h n))       (no mean_j h without a mean),
+ *   d_weight = sum_r dy n,   d_bias = sum_r dy.
+ *
+ *   mean, rstd   what the forward pass wrote (mean only with BERGSON_NORM_LAYER).
+ *   dy        [rows, ld_dy] of `dtype`.
+ *   dx        [rows, ld_dx] of `dtype`; may be x or dy itself with its leading dimension.
+ *   d_weight, d_bias   fp32 [d], each or NULL; zeros where rows is 0.
+ *   workspace 256-byte aligned, contents on entry ignored.
+ * Sums are fp32.
+ * Errors: EINVAL, EALIGN, EUNSUPPORTED, EWORKSPACE, ECUDA.
+ */
+BERGSON_API int bergson_norm_backward_workspace(int64_t rows, int64_t d, size_t* ws_bytes);
+BERGSON_API int bergson_norm_backward(const void* x, int dtype, int64_t rows, int64_t d,
+                                      int64_t ld_x, const void* weight, int w_dtype, int kind,
+                                      const float* mean, const float* rstd, const void* dy,
+                                      int64_t ld_dy, void* dx, int64_t ld_dx, float* d_weight,
+                                      float* d_bias, void* workspace, size_t ws_bytes,
+                                      void* stream);
 
 #ifdef __cplusplus
 }

@@ -54,6 +54,9 @@ BERGSON_STATE_F32 = 0
 BERGSON_STATE_8BIT = 1
 BERGSON_STATE_BLOCK = 256
 
+BERGSON_NORM_LAYER = 0
+BERGSON_NORM_RMS = 1
+
 BERGSON_MOMENT_FIRST = 0
 BERGSON_MOMENT_SECOND = 1
 
@@ -83,6 +86,7 @@ EXPORTED = (
     "bergson_token_logprobs", "bergson_token_logprobs_backward", "bergson_policy_loss_workspace",
     "bergson_policy_loss", "bergson_preference_loss", "bergson_adamw_step",
     "bergson_adamw_state_values", "bergson_factor_moments_workspace", "bergson_factor_moments",
+    "bergson_norm", "bergson_norm_backward_workspace", "bergson_norm_backward",
 )
 
 
@@ -233,6 +237,10 @@ def lib() -> ctypes.CDLL:
                                                    szp]),
         "bergson_factor_moments": (i32, [ctypes.POINTER(bergson_moment_matrix), i32, f64, f64, vp,
                                          ctypes.c_size_t, vp]),
+        "bergson_norm": (i32, [vp, i32, i64, i64, i64, vp, vp, i32, i32, f64, vp, i64, vp, vp, vp]),
+        "bergson_norm_backward_workspace": (i32, [i64, i64, szp]),
+        "bergson_norm_backward": (i32, [vp, i32, i64, i64, i64, vp, i32, i32, vp, vp, vp, i64, vp, i64,
+                                        vp, vp, vp, ctypes.c_size_t, vp]),
     }
     for name, (res, args) in sig.items():
         fn = getattr(L, name)
@@ -900,6 +908,50 @@ def bergson_factor_moments(mats, correction: float, floor: float, workspace, str
     arr = _records(bergson_moment_matrix, mats)
     _check(lib().bergson_factor_moments(arr, len(arr), correction, floor, *_scratch(workspace),
                                         _stream(stream)))
+
+
+def _weights(weight, bias, d: int):
+    """(weight's pointer, bias's pointer, their dtype); None passes as NULL."""
+    one = weight if weight is not None else bias
+    if one is None:
+        return None, None, BERGSON_F32
+    return (_vector(weight, "weight", one.dtype, d), _vector(bias, "bias", one.dtype, d),
+            _dtype(one))
+
+
+def bergson_norm(x, weight, bias, kind: int, eps: float, y, mean=None, rstd=None,
+                 stream=None) -> None:
+    """y = layer norm of the rows of x (kind: BERGSON_NORM_LAYER, or BERGSON_NORM_RMS without a
+    mean), and the rows' mean and rstd; weight and bias may be None."""
+    rows, d = x.shape
+    dtype = _dtype(x)
+    px, ld = _rows(x, "x")
+    py, ld_y = _rows_like(y, "y", x.dtype, x.shape)
+    _check(lib().bergson_norm(px, dtype, rows, d, ld, *_weights(weight, bias, d), kind, eps, py, ld_y,
+                              _vector(mean, "mean", _F32, rows), _vector(rstd, "rstd", _F32, rows),
+                              _stream(stream)))
+
+
+def bergson_norm_backward_workspace(rows: int, d: int) -> int:
+    n = ctypes.c_size_t()
+    _check(lib().bergson_norm_backward_workspace(int(rows), int(d), ctypes.byref(n)))
+    return n.value
+
+
+def bergson_norm_backward(x, weight, kind: int, mean, rstd, dy, dx, d_weight, d_bias, workspace,
+                          stream=None) -> None:
+    """dx, d_weight and d_bias (either may be None) from the gradient at y."""
+    rows, d = x.shape
+    dtype = _dtype(x)
+    px, ld = _rows(x, "x")
+    pdy, ld_dy = _rows_like(dy, "dy", x.dtype, x.shape)
+    pdx, ld_dx = _rows_like(dx, "dx", x.dtype, x.shape)
+    w, _, w_dtype = _weights(weight, None, d)
+    _check(lib().bergson_norm_backward(
+        px, dtype, rows, d, ld, w, w_dtype, kind, _vector(mean, "mean", _F32, rows),
+        _vector(rstd, "rstd", _F32, rows), pdy, ld_dy, pdx, ld_dx,
+        _vector(d_weight, "d_weight", _F32, d), _vector(d_bias, "d_bias", _F32, d),
+        *_scratch(workspace), _stream(stream)))
 
 
 # ------------------------------------------------------------------ helpers

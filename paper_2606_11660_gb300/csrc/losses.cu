@@ -792,7 +792,6 @@ __global__ void __launch_bounds__(1024) preference_finish_kernel(const float* pa
 
 // ------------------------------------------------------------------- host
 
-int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 size_t align256(size_t n) { return (n + 255) / 256 * 256; }
 size_t counts_bytes(int64_t B, int64_t T) {
   const int64_t n = std::max<int64_t>(kCountCtas, B * ceil_div(T, kCountSegment));

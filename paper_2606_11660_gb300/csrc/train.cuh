@@ -1,5 +1,5 @@
-// Device helpers of the training-side operators: element types, block sums and
-// the codes of 8-bit optimiser states.
+// Device helpers of the training-side operators: element types, a thread's part of
+// a row, block sums and the codes of 8-bit optimiser states.
 #pragma once
 
 #include <cuda_bf16.h>
@@ -113,6 +113,103 @@ __device__ __forceinline__ H2 vec_max2(const uint4& v) {
   const H2* h = reinterpret_cast<const H2*>(&v);
   return __hmax2(__hmax2(h[0], h[1]), __hmax2(h[2], h[3]));
 }
+
+// Host helpers of the launchers.
+inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
+// Rows of a matrix that can be accessed 16 bytes at a time.
+inline bool on16(const void* p, int64_t ld, size_t size) {
+  return reinterpret_cast<uintptr_t>(p) % 16 == 0 && ld * size % 16 == 0;
+}
+
+__device__ __forceinline__ float load_any(const void* p, int type, int64_t i) {
+  if (type == BERGSON_BF16) return __bfloat162float(static_cast<const __nv_bfloat16*>(p)[i]);
+  if (type == BERGSON_F16) return __half2float(static_cast<const __half*>(p)[i]);
+  return static_cast<const float*>(p)[i];
+}
+
+// A thread's columns of a row and how they lie in it: kPer vectors of E elements, vector k at column
+// E (t + k G) for thread t of the G that share the row.
+template <typename T, bool kVec, int C>
+struct RowPart {
+  static constexpr int E = kVec ? Vec16<T>::kElems : 1;
+  static constexpr int kPer = C / E;
+  // As they lie in memory.
+  static constexpr int kWords = kVec ? 4 * kPer : kPer;
+  uint32_t raw[kWords];
+
+  __device__ __forceinline__ static int col(int t, int G, int k) { return E * (t + k * G); }
+
+  __device__ __forceinline__ void load(const T* row, int d, int t, int G) {
+#pragma unroll
+    for (int k = 0; k < kPer; ++k) {
+      const int c = col(t, G, k);
+      if constexpr (kVec) {
+        uint4 v = make_uint4(0, 0, 0, 0);
+        if (c + E <= d) {
+          v = *reinterpret_cast<const uint4*>(row + c);
+        } else if (c < d) {
+          __align__(16) T part[E];
+#pragma unroll
+          for (int i = 0; i < E; ++i) part[i] = c + i < d ? row[c + i] : T(0.0f);
+          v = *reinterpret_cast<const uint4*>(part);
+        }
+        raw[4 * k] = v.x; raw[4 * k + 1] = v.y; raw[4 * k + 2] = v.z; raw[4 * k + 3] = v.w;
+      } else {
+        raw[k] = 0;
+        if (c < d) {
+          if constexpr (sizeof(T) == 2) raw[k] = *reinterpret_cast<const uint16_t*>(row + c);
+          else raw[k] = __float_as_uint(row[c]);
+        }
+      }
+    }
+  }
+  __device__ __forceinline__ void floats(float (&x)[C]) const {
+#pragma unroll
+    for (int k = 0; k < kPer; ++k) {
+      if constexpr (kVec) {
+        const uint4 v = make_uint4(raw[4 * k], raw[4 * k + 1], raw[4 * k + 2], raw[4 * k + 3]);
+#pragma unroll
+        for (int i = 0; i < E / 2; ++i) {
+          const float2 f = unpack2(v, i, static_cast<const T*>(nullptr));
+          x[E * k + 2 * i] = f.x;
+          x[E * k + 2 * i + 1] = f.y;
+        }
+      } else if constexpr (sizeof(T) == 2) {
+        const uint16_t u = static_cast<uint16_t>(raw[k]);
+        x[k] = to_f32(*reinterpret_cast<const T*>(&u));
+      } else {
+        x[k] = __uint_as_float(raw[k]);
+      }
+    }
+  }
+  __device__ __forceinline__ static void store(T* row, int d, int t, int G, const float (&x)[C]) {
+#pragma unroll
+    for (int k = 0; k < kPer; ++k) {
+      const int c = col(t, G, k);
+      if constexpr (kVec) {
+        uint4 v;
+#pragma unroll
+        for (int i = 0; i < E / 2; ++i)
+          pack2(v, i, make_float2(x[E * k + 2 * i], x[E * k + 2 * i + 1]),
+                static_cast<const T*>(nullptr));
+        if (c + E <= d) {
+          *reinterpret_cast<uint4*>(row + c) = v;
+        } else if (c < d) {
+          const T* part = reinterpret_cast<const T*>(&v);
+#pragma unroll
+          for (int i = 0; i < E; ++i)
+            if (c + i < d) row[c + i] = part[i];
+        }
+      } else if (c < d) {
+        row[c] = from_f32<T>(x[k]);
+      }
+    }
+  }
+  // The column of element i of the thread's C.
+  __device__ __forceinline__ static int column(int t, int G, int i) {
+    return col(t, G, i / E) + i % E;
+  }
+};
 
 // 32 bytes at once, from and to 32-byte boundaries.
 __device__ __forceinline__ void load32(const void* p, uint32_t (&r)[8]) {

@@ -1,5 +1,5 @@
 // Arguments and launchers of the training-side operators (token
-// log-probabilities, losses, AdamW, factored moments).
+// log-probabilities, losses, AdamW, factored moments, norms).
 #pragma once
 
 #include <cuda_runtime.h>
@@ -58,5 +58,40 @@ cudaError_t launch_state_values(const uint8_t* codes, const float* scale, int64_
 size_t moments_workspace(const bergson_moment_matrix* m, int n);
 cudaError_t launch_factor_moments(const bergson_moment_matrix* m, int n, double correction,
                                   double floor, void* ws, cudaStream_t s);
+
+struct NormArgs {
+  const void* x;               // [rows, ld_x] of dtype
+  int dtype;
+  int64_t rows, d, ld_x;
+  const void* weight;          // [d] of w_dtype, or nullptr: ones
+  const void* bias;            // [d] of w_dtype, or nullptr: zeros
+  int w_dtype;
+  int kind;                    // bergson_norm_kind
+  double eps;
+  void* y;                     // [rows, ld_y]
+  int64_t ld_y;
+  float* mean;                 // [rows], or nullptr; layer norm only
+  float* rstd;                 // [rows], or nullptr
+};
+cudaError_t launch_norm(const NormArgs& a, cudaStream_t s);
+
+struct NormGradArgs {
+  const void* x;
+  int dtype;
+  int64_t rows, d, ld_x;
+  const void* weight;
+  int w_dtype;
+  int kind;
+  const float* mean;           // layer norm only
+  const float* rstd;
+  const void* dy;              // [rows, ld_dy]
+  int64_t ld_dy;
+  void* dx;                    // [rows, ld_dx]
+  int64_t ld_dx;
+  float* dw;                   // [d], or nullptr
+  float* db;                   // [d], or nullptr
+};
+size_t norm_backward_workspace(int64_t rows, int64_t d);
+cudaError_t launch_norm_backward(const NormGradArgs& a, void* ws, cudaStream_t s);
 
 }  // namespace bergson

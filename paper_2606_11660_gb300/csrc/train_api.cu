@@ -85,6 +85,33 @@ int check_policy_sizes(int64_t B, int64_t T) {
   return BERGSON_OK;
 }
 
+int check_norm_sizes(int64_t rows, int64_t d) {
+  if (rows < 0 || rows > INT32_MAX) return fail(BERGSON_EINVAL, "rows must be in [0, 2^31)");
+  if (d < 1) return fail(BERGSON_EINVAL, "d must be >= 1");
+  if (d > (1ll << 24)) return fail(BERGSON_EUNSUPPORTED, "d must be <= 2^24");
+  return BERGSON_OK;
+}
+
+int check_norm(int dtype, int64_t rows, int64_t d, const void* weight, const void* bias,
+               int w_dtype, int kind) {
+  BERGSON_TRY(check_norm_sizes(rows, d));
+  if (dtype_size(dtype) == 0 || dtype_size(w_dtype) == 0)
+    return fail(BERGSON_EINVAL, "unknown dtype (x %d, weight %d)", dtype, w_dtype);
+  if (kind != BERGSON_NORM_LAYER && kind != BERGSON_NORM_RMS)
+    return fail(BERGSON_EINVAL, "unknown kind %d", kind);
+  if (!aligned(weight, dtype_size(w_dtype)) || !aligned(bias, dtype_size(w_dtype)))
+    return fail(BERGSON_EALIGN, "weight and bias must be aligned to their elements");
+  return BERGSON_OK;
+}
+
+// An output in the place of an input needs its leading dimension.
+int check_in_place(const void* out, int64_t ld_out, const void* in, int64_t ld_in,
+                   const char* what) {
+  if (out == in && ld_out != ld_in)
+    return fail(BERGSON_EINVAL, "%s in place needs its input's leading dimension", what);
+  return BERGSON_OK;
+}
+
 bool probability(double x) { return x >= 0.0 && x <= 1.0; }
 
 }  // namespace
@@ -347,6 +374,65 @@ int bergson_factor_moments(const bergson_moment_matrix* mats, int n_mats, double
   const cudaError_t e = launch_factor_moments(mats, n_mats, correction, floor, workspace,
                                               static_cast<cudaStream_t>(stream));
   if (e != cudaSuccess) return fail_cuda(e, "factored moment launch");
+  return BERGSON_OK;
+}
+
+int bergson_norm(const void* x, int dtype, int64_t rows, int64_t d, int64_t ld_x,
+                 const void* weight, const void* bias, int w_dtype, int kind, double eps, void* y,
+                 int64_t ld_y, float* mean, float* rstd, void* stream) {
+  BERGSON_TRY(check_norm(dtype, rows, d, weight, bias, w_dtype, kind));
+  if (!(eps >= 0.0) || !std::isfinite(static_cast<float>(eps)))
+    return fail(BERGSON_EINVAL, "eps must be >= 0 and finite");
+  if (rows > 0) {
+    BERGSON_TRY(check_rows(x, dtype_size(dtype), d, ld_x, "x"));
+    BERGSON_TRY(check_rows(y, dtype_size(dtype), d, ld_y, "y"));
+    BERGSON_TRY(check_in_place(y, ld_y, x, ld_x, "y"));
+    if (mean != nullptr) BERGSON_TRY(check_tensor(mean, 4, "mean"));
+    if (rstd != nullptr) BERGSON_TRY(check_tensor(rstd, 4, "rstd"));
+  }
+  BERGSON_TRY(injected_status());
+  if (rows == 0) return BERGSON_OK;
+  DeviceGuard dg(y);
+  if (dg.err != cudaSuccess) return fail_cuda(dg.err, "output device lookup");
+  const NormArgs a{x, dtype, rows, d, ld_x, weight, bias, w_dtype, kind, eps, y, ld_y, mean, rstd};
+  const cudaError_t e = launch_norm(a, static_cast<cudaStream_t>(stream));
+  if (e != cudaSuccess) return fail_cuda(e, "norm launch");
+  return BERGSON_OK;
+}
+
+int bergson_norm_backward_workspace(int64_t rows, int64_t d, size_t* ws_bytes) {
+  if (ws_bytes == nullptr) return fail(BERGSON_EINVAL, "ws_bytes is NULL");
+  BERGSON_TRY(check_norm_sizes(rows, d));
+  *ws_bytes = norm_backward_workspace(rows, d);
+  return BERGSON_OK;
+}
+
+int bergson_norm_backward(const void* x, int dtype, int64_t rows, int64_t d, int64_t ld_x,
+                          const void* weight, int w_dtype, int kind, const float* mean,
+                          const float* rstd, const void* dy, int64_t ld_dy, void* dx,
+                          int64_t ld_dx, float* d_weight, float* d_bias, void* workspace,
+                          size_t ws_bytes, void* stream) {
+  BERGSON_TRY(check_norm(dtype, rows, d, weight, nullptr, w_dtype, kind));
+  const size_t size = dtype_size(dtype);
+  if (rows > 0) {
+    BERGSON_TRY(check_rows(x, size, d, ld_x, "x"));
+    BERGSON_TRY(check_rows(dy, size, d, ld_dy, "dy"));
+    BERGSON_TRY(check_rows(dx, size, d, ld_dx, "dx"));
+    BERGSON_TRY(check_in_place(dx, ld_dx, x, ld_x, "dx"));
+    BERGSON_TRY(check_in_place(dx, ld_dx, dy, ld_dy, "dx"));
+    if (kind == BERGSON_NORM_LAYER) BERGSON_TRY(check_tensor(mean, 4, "mean"));
+    BERGSON_TRY(check_tensor(rstd, 4, "rstd"));
+  }
+  if (d_weight != nullptr) BERGSON_TRY(check_tensor(d_weight, 4, "d_weight"));
+  if (d_bias != nullptr) BERGSON_TRY(check_tensor(d_bias, 4, "d_bias"));
+  BERGSON_TRY(check_workspace(workspace, ws_bytes, norm_backward_workspace(rows, d)));
+  BERGSON_TRY(injected_status());
+  DeviceGuard dg(workspace);
+  if (dg.err != cudaSuccess) return fail_cuda(dg.err, "workspace device lookup");
+  const NormGradArgs a{x,    dtype, rows, d,     ld_x, weight, w_dtype,  kind,
+                       mean, rstd,  dy,   ld_dy, dx,   ld_dx,  d_weight, d_bias};
+  const cudaError_t e = launch_norm_backward(a, workspace, static_cast<cudaStream_t>(stream));
+  if (e != cudaSuccess) return fail_cuda(e, "norm backward launch");
   return BERGSON_OK;
 }
 

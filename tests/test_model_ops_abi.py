@@ -1,0 +1,94 @@
+"""Host-side checks of the entry points around a model's linear layers that need no GPU:
+refusals of arguments, workspace sizes, records."""
+import pytest
+
+import paper_2606_11660_gb300 as bg
+
+FAKE = 0x7F0000000000  # aligned, never dereferenced: validation fails first or no device
+NAN, INF = float("nan"), float("inf")
+
+
+@pytest.fixture(scope="module", autouse=True)
+def built_library():
+    from paper_2606_11660_gb300 import _build
+    _build.build()
+    yield
+
+
+def accepted(st):
+    """Past validation: without a device the pointers' lookup fails."""
+    return st == bg.BERGSON_ECUDA
+
+
+@pytest.fixture(autouse=True)
+def no_launch():
+    """What passes validation returns an injected status and enqueues nothing."""
+    bg.bergson_debug_inject_status(bg.BERGSON_ECUDA, 1 << 20)
+    yield
+    bg.bergson_debug_inject_status(0, 0)
+
+
+def norm(**kw):
+    a = dict(x=FAKE, dtype=bg.BERGSON_BF16, rows=4, d=100, ld_x=100, w=FAKE, b=FAKE, wt=0, kind=0,
+             eps=1e-5, y=FAKE + 4096, ld_y=100, mean=FAKE, rstd=FAKE)
+    a.update(kw)
+    return bg.lib().bergson_norm(*a.values(), None)
+
+
+def dnorm(ws=FAKE, ws_bytes=1 << 24, **kw):
+    a = dict(x=FAKE, dtype=bg.BERGSON_BF16, rows=4, d=100, ld_x=100, w=FAKE, wt=0, kind=0, mean=FAKE,
+             rstd=FAKE, dy=FAKE + 4096, ld_dy=100, dx=FAKE + 8192, ld_dx=100, dw=FAKE, db=FAKE)
+    a.update(kw)
+    return bg.lib().bergson_norm_backward(*a.values(), ws, ws_bytes, None)
+
+
+NORM_BAD = [
+    (dict(dtype=3), bg.BERGSON_EINVAL), (dict(wt=-1), bg.BERGSON_EINVAL),
+    (dict(rows=-1), bg.BERGSON_EINVAL), (dict(rows=1 << 31), bg.BERGSON_EINVAL),
+    (dict(d=0), bg.BERGSON_EINVAL), (dict(d=(1 << 24) + 1, ld_x=1 << 25), bg.BERGSON_EUNSUPPORTED),
+    (dict(ld_x=99), bg.BERGSON_EINVAL), (dict(ld_x=1 << 41), bg.BERGSON_EUNSUPPORTED),
+    (dict(x=None), bg.BERGSON_EINVAL), (dict(x=FAKE + 1), bg.BERGSON_EALIGN),
+    (dict(dtype=0, x=FAKE + 2), bg.BERGSON_EALIGN), (dict(w=FAKE + 2), bg.BERGSON_EALIGN),
+    (dict(kind=2), bg.BERGSON_EINVAL), (dict(mean=FAKE + 2), bg.BERGSON_EALIGN),
+    (dict(rstd=FAKE + 1), bg.BERGSON_EALIGN),
+]
+
+
+@pytest.mark.parametrize("kw,code", NORM_BAD + [
+    (dict(eps=-1e-9), bg.BERGSON_EINVAL), (dict(eps=NAN), bg.BERGSON_EINVAL),
+    (dict(eps=INF), bg.BERGSON_EINVAL), (dict(eps=1e60), bg.BERGSON_EINVAL),
+    (dict(y=None), bg.BERGSON_EINVAL), (dict(y=FAKE + 1), bg.BERGSON_EALIGN),
+    (dict(ld_y=99), bg.BERGSON_EINVAL), (dict(y=FAKE, ld_y=104), bg.BERGSON_EINVAL),
+    (dict(b=FAKE + 2), bg.BERGSON_EALIGN)])
+def test_norm_refusals(kw, code):
+    assert norm(**kw) == code and bg.bergson_last_error() != ""
+
+
+@pytest.mark.parametrize("kw,code", NORM_BAD + [
+    (dict(mean=None), bg.BERGSON_EINVAL), (dict(rstd=None), bg.BERGSON_EINVAL),
+    (dict(dy=None), bg.BERGSON_EINVAL), (dict(ld_dy=99), bg.BERGSON_EINVAL),
+    (dict(dx=None), bg.BERGSON_EINVAL), (dict(ld_dx=-1), bg.BERGSON_EINVAL),
+    (dict(dx=FAKE, ld_dx=104), bg.BERGSON_EINVAL), (dict(dx=FAKE + 4096, ld_dx=104), bg.BERGSON_EINVAL),
+    (dict(dw=FAKE + 2), bg.BERGSON_EALIGN), (dict(db=FAKE + 2), bg.BERGSON_EALIGN),
+    (dict(ws=None), bg.BERGSON_EINVAL), (dict(ws=FAKE + 16), bg.BERGSON_EALIGN),
+    (dict(ws_bytes=64), bg.BERGSON_EWORKSPACE)])
+def test_norm_backward_refusals(kw, code):
+    assert dnorm(**kw) == code and bg.bergson_last_error() != ""
+
+
+def test_norm_calls_that_pass():
+    need = bg.bergson_norm_backward_workspace(4, 100)
+    assert need > 0 and need % 256 == 0
+    for st in (norm(), norm(w=None, b=None), norm(mean=None, rstd=None), norm(y=FAKE), norm(eps=0.0),
+               norm(x=FAKE + 2, ld_x=101), norm(rows=0, x=None, y=None), norm(kind=1, mean=None),
+               dnorm(), dnorm(ws_bytes=need), dnorm(dw=None, db=None), dnorm(kind=1, mean=None),
+               dnorm(dx=FAKE), dnorm(dx=FAKE + 4096), dnorm(w=None),
+               dnorm(rows=0, x=None, dy=None, dx=None, mean=None, rstd=None)):
+        assert accepted(st), bg.bergson_last_error()
+    assert bg.lib().bergson_norm_backward_workspace(4, 4, None) == bg.BERGSON_EINVAL
+    for rows, d in ((-1, 4), (4, 0), (1 << 31, 4)):
+        with pytest.raises(bg.BergsonError):
+            bg.bergson_norm_backward_workspace(rows, d)
+    # a row of dw and db a CTA at most
+    assert all(bg.bergson_norm_backward_workspace(1 << 30, d) <= 152 * 8 * 2 * 4 * max(d, 512)
+               for d in (1, 24, 512, 513, 2048, 8192, 16_384, 16_385, 1 << 20))

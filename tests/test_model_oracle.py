@@ -1,0 +1,30 @@
+"""The fp64 definitions of the operators around the linear layers against differences (CPU)."""
+import numpy as np
+import pytest
+
+from oracle import model_oracle as orc
+
+
+def along(f, eps=1e-6):
+    return (f(eps) - f(-eps)) / (2 * eps)
+
+
+@pytest.mark.parametrize("layer", [True, False])
+def test_norm_gradients(layer):
+    r = np.random.default_rng(0)
+    x, dy, u = (r.normal(size=(5, 12)) + 0.5 for _ in range(3))
+    w, b, uw, ub = (r.normal(size=12) for _ in range(4))
+
+    def f(e):
+        return (orc.norm(x + e * u, w + e * uw, b + e * ub, layer, 1e-3)[0] * dy).sum()
+    _, mean, rstd = orc.norm(x, w, b, layer, 1e-3)
+    dx, dw, db = orc.norm_backward(x, w, layer, mean, rstd, dy)
+    assert abs(along(f) - (dx * u).sum() - (dw * uw).sum() - (db * ub).sum()) < 1e-7
+
+
+def test_norm_closed_forms():
+    x = np.array([[1.0, 3.0], [2.0, 2.0]])
+    y, mean, rstd = orc.norm(x, None, None, True, 0.0 + 1e-300)
+    assert np.allclose(y[0], [-1, 1]) and np.allclose(mean, [2, 2]) and rstd[0] == 1
+    y, _, rstd = orc.norm(x, None, None, False, 0.0)
+    assert np.allclose((y ** 2).mean(1), 1) and np.allclose(rstd[1], 0.5)
