@@ -988,6 +988,47 @@ BERGSON_API int bergson_norm_backward(const void* x, int dtype, int64_t rows, in
                                       float* d_bias, void* workspace, size_t ws_bytes,
                                       void* stream);
 
+/*
+ * Embedding lookup with a scale: out[r] = scale table[ids[r]], rounded once.
+ *
+ *   table     [V, ld_t] of `dtype` (bergson_dtype), V >= 1, ld_t >= d >= 1.
+ *   ids       int64 [rows].  A negative id (padding) gives a row of zeros.  An id >= V gives
+ *             a row of NaN and is recorded as BERGSON_EINVAL in the device status word.
+ *   scale     finite, e.g. sqrt(d).
+ *   out       [rows, ld_o] of `dtype`; shares no memory with table.
+ * rows, V in [0, 2^31), d <= 2^24.
+ * Errors: EINVAL, EALIGN, EUNSUPPORTED, ECUDA.
+ */
+BERGSON_API int bergson_embedding(const void* table, int dtype, int64_t V, int64_t d, int64_t ld_t,
+                                  const int64_t* ids, int64_t rows, double scale, void* out,
+                                  int64_t ld_o, void* stream);
+
+/*
+ * The table's gradient from dy, the gradient at the lookups,
+ *
+ *   d_table[v] = scale sum_{r: ids[r] = v} dy_r        (add == 0: all V rows are written)
+ *   d_table[v] += scale sum_{r: ids[r] = v} dy_r       (add != 0: rows without an id are not touched)
+ *
+ * add != 0 is for weights tied to the output layer, whose gradient is there already.
+ *
+ *   dy        [rows, ld_dy] of `dtype`.
+ *   ids       int64 [rows]; a negative id leaves its row out, whatever dy holds there.  An id >= V
+ *             does too and is recorded as BERGSON_EINVAL in the device status word.
+ *   d_table   [V, ld_t] of t_dtype; shares no memory with dy.
+ *   workspace 256-byte aligned, contents on entry ignored.
+ * Sums are fp32, without atomics, in an order that follows from the ids and sizes alone; with
+ * add != 0 the sum is rounded to t_dtype once, after the addition.
+ * rows, V in [0, 2^31), d <= 2^24.
+ * Errors: EINVAL, EALIGN, EUNSUPPORTED, EWORKSPACE, ECUDA.
+ */
+BERGSON_API int bergson_embedding_backward_workspace(int64_t rows, int64_t V, int64_t d,
+                                                     size_t* ws_bytes);
+BERGSON_API int bergson_embedding_backward(const void* dy, int dtype, int64_t rows, int64_t d,
+                                           int64_t ld_dy, const int64_t* ids, double scale,
+                                           void* d_table, int t_dtype, int64_t V, int64_t ld_t,
+                                           int add, void* workspace, size_t ws_bytes,
+                                           void* stream);
+
 #ifdef __cplusplus
 }
 #endif

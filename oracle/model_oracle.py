@@ -29,3 +29,20 @@ def norm_backward(x, w, layer, mean, rstd, dy):
     if layer:
         dx = dx - h.mean(1, keepdims=True)
     return dx * rstd[:, None], (dy * n).sum(0), dy.sum(0)
+
+
+# ------------------------------------------------------------------ embedding
+
+def embedding(table, ids, scale):
+    """scale table[id] of fp64 rows; a negative id gives zeros."""
+    return np.stack([scale * table[i] if i >= 0 else np.zeros(table.shape[1]) for i in ids])
+
+
+def embedding_backward(dy, ids, scale, V):
+    """(the table's gradient [V, d], the same of magnitudes)."""
+    out = np.zeros((2, V, dy.shape[1]))
+    for r, i in enumerate(ids):
+        if 0 <= i < V:
+            out[0, i] += scale * dy[r]
+            out[1, i] += abs(scale) * np.abs(dy[r])
+    return out[0], out[1]

@@ -87,6 +87,7 @@ EXPORTED = (
     "bergson_policy_loss", "bergson_preference_loss", "bergson_adamw_step",
     "bergson_adamw_state_values", "bergson_factor_moments_workspace", "bergson_factor_moments",
     "bergson_norm", "bergson_norm_backward_workspace", "bergson_norm_backward",
+    "bergson_embedding", "bergson_embedding_backward_workspace", "bergson_embedding_backward",
 )
 
 
@@ -241,6 +242,10 @@ def lib() -> ctypes.CDLL:
         "bergson_norm_backward_workspace": (i32, [i64, i64, szp]),
         "bergson_norm_backward": (i32, [vp, i32, i64, i64, i64, vp, i32, i32, vp, vp, vp, i64, vp, i64,
                                         vp, vp, vp, ctypes.c_size_t, vp]),
+        "bergson_embedding": (i32, [vp, i32, i64, i64, i64, vp, i64, f64, vp, i64, vp]),
+        "bergson_embedding_backward_workspace": (i32, [i64, i64, i64, szp]),
+        "bergson_embedding_backward": (i32, [vp, i32, i64, i64, i64, vp, f64, vp, i32, i64, i64, i32, vp,
+                                             ctypes.c_size_t, vp]),
     }
     for name, (res, args) in sig.items():
         fn = getattr(L, name)
@@ -952,6 +957,37 @@ def bergson_norm_backward(x, weight, kind: int, mean, rstd, dy, dx, d_weight, d_
         _vector(rstd, "rstd", _F32, rows), pdy, ld_dy, pdx, ld_dx,
         _vector(d_weight, "d_weight", _F32, d), _vector(d_bias, "d_bias", _F32, d),
         *_scratch(workspace), _stream(stream)))
+
+
+def bergson_embedding(table, ids, scale: float, out, stream=None) -> None:
+    """out[r] = scale table[ids[r]]; a negative id gives zeros."""
+    V, d = table.shape
+    dtype = _dtype(table)
+    t, ld = _rows(table, "table")
+    rows = ids.numel()
+    po, ld_o = _rows_like(out, "out", table.dtype, (rows, d))
+    _check(lib().bergson_embedding(t, dtype, V, d, ld, _vector(ids, "ids", _I64, rows), rows, scale, po,
+                                   ld_o, _stream(stream)))
+
+
+def bergson_embedding_backward_workspace(rows: int, V: int, d: int) -> int:
+    n = ctypes.c_size_t()
+    _check(lib().bergson_embedding_backward_workspace(int(rows), int(V), int(d), ctypes.byref(n)))
+    return n.value
+
+
+def bergson_embedding_backward(dy, ids, scale: float, d_table, add: bool, workspace,
+                               stream=None) -> None:
+    """The table's gradient from the gradient at the lookups, in place of d_table's values or
+    (add) on top of them."""
+    rows, d = dy.shape
+    V = d_table.shape[0]
+    dtype = _dtype(dy)
+    g, ld = _rows(dy, "dy")
+    t, ld_t = _rows_like(d_table, "d_table", d_table.dtype, (V, d))
+    _check(lib().bergson_embedding_backward(
+        g, dtype, rows, d, ld, _vector(ids, "ids", _I64, rows), scale, t, _dtype(d_table), V, ld_t,
+        1 if add else 0, *_scratch(workspace), _stream(stream)))
 
 
 # ------------------------------------------------------------------ helpers

@@ -1,0 +1,733 @@
+// Embedding lookup with a scale, and its gradient.
+//
+//   forward   out_r = s table[id_r]
+//   backward  dT[v] = s sum_{r: id_r = v} dy_r   (+ dT[v])
+//
+// Both are bound by their bytes.  The gradient is summed in fp32 and without
+// atomics, so that it has the same bits every time: the rows are put in the order of
+// their tokens, and what shares a token is added up in the order of the rows.
+//
+// Up to kFewRows rows, one launch: the CTA of a token's first row finds the
+// others by comparing tokens, and CTAs of their own write zeros to the rest of the
+// table.  Above, a radix sort of (token, row), 9 bits a pass: counts per tile
+// of rows, then every tile places its rows behind those of the tiles before it.
+// The sorted rows are added up kRun at a time: a token whose rows all lie within such a run
+// is done there; what it has of the tokens that cross its ends goes to the workspace and is
+// joined by a last kernel.  No run is longer than another, however often a token comes.
+
+#include <algorithm>
+
+#include "internal.h"
+#include "train.cuh"
+
+namespace bergson {
+
+namespace {
+
+// ------------------------------------------------------------------ forward
+
+constexpr int kLookupThreads = 128;
+constexpr int kLookupCols = 32;                // columns a lane of a lookup
+
+struct LookupParams {
+  const void* table;
+  const int64_t* ids;
+  void* out;
+  int64_t V, rows, ld_t, ld_o;
+  int d, slabs;
+  float scale;
+  int* status;
+};
+
+// A warp takes 32 * C columns of a row.
+template <typename T, bool kVec>
+__global__ void __launch_bounds__(kLookupThreads) lookup_kernel(
+    const __grid_constant__ LookupParams p) {
+  constexpr int C = kVec ? 4 * Vec16<T>::kElems : 8;
+  using R = RowPart<T, kVec, C>;
+  const int lane = threadIdx.x & 31;
+  const int64_t unit = static_cast<int64_t>(blockIdx.x) * (kLookupThreads / 32) + (threadIdx.x >> 5);
+  const int64_t r = unit / p.slabs;
+  const int c0 = static_cast<int>(unit % p.slabs) * 32 * C;
+  griddep_wait();
+  if (r >= p.rows) return;
+  const int64_t id = p.ids[r];
+  const int d = min(p.d - c0, 32 * C);
+  float x[C];
+  if (id < 0 || id >= p.V) {
+    if (id >= p.V && lane == 0 && c0 == 0) raise_device_error(p.status, nullptr, BERGSON_EINVAL);
+    const float v = id < 0 ? 0.0f : __int_as_float(0x7fffffff);
+#pragma unroll
+    for (int i = 0; i < C; ++i) x[i] = v;
+  } else {
+    R row;
+    row.load(static_cast<const T*>(p.table) + id * p.ld_t + c0, d, lane, 32);
+    row.floats(x);
+#pragma unroll
+    for (int i = 0; i < C; ++i) x[i] *= p.scale;
+  }
+  R::store(static_cast<T*>(p.out) + r * p.ld_o + c0, d, lane, 32, x);
+}
+
+// ------------------------------------------------------------------ backward
+
+constexpr int kFewRows = 2048;                 // up to here one launch does it all
+constexpr int kFewThreads = 512;
+constexpr int kFewZeros = 512;                 // rows of the table a CTA of zeros looks after
+constexpr int kRun = 32;                       // sorted rows added up by one CTA
+constexpr int kSumThreads = 128;
+constexpr int kCols = 8;                       // columns a thread
+constexpr int kAhead = 8;                      // rows on their way
+constexpr int kJoinRuns = 16;                  // runs whose last token a CTA joins
+constexpr int kJoinThreads = 256;
+constexpr int kJoinCols = 128;
+constexpr int kSortThreads = 1024;
+constexpr int kSortItems = 2048;               // items of a step of the sort
+constexpr int kDigitBits = 9;
+constexpr int kBins = 1 << kDigitBits;
+constexpr int kMaxTiles = 128;
+constexpr int kMaxPasses = 4;
+
+struct GradOut {
+  void* table;                 // [V, ld]
+  int64_t ld;
+  int type;
+  int vec;                     // its rows take 16-byte accesses
+  int add;
+  float scale;
+};
+
+// E (1, 4 or 8) neighbouring columns of the table's row v: their sum times the scale.
+template <int E>
+__device__ __forceinline__ void put_columns(const GradOut& o, int64_t v, int col, int d,
+                                            const float* sum) {
+  const int64_t at = v * o.ld + col;
+  float x[E];
+  const bool whole = E > 1 && o.vec && col + E <= d;
+  if (!whole) {
+#pragma unroll
+    for (int i = 0; i < E; ++i) {
+      if (col + i >= d) return;
+      float y = sum[i] * o.scale;
+      if (o.add) y += load_any(o.table, o.type, at + i);
+      if (o.type == BERGSON_BF16) static_cast<__nv_bfloat16*>(o.table)[at + i] = __float2bfloat16_rn(y);
+      else if (o.type == BERGSON_F16) static_cast<__half*>(o.table)[at + i] = __float2half_rn(y);
+      else static_cast<float*>(o.table)[at + i] = y;
+    }
+    return;
+  }
+  if constexpr (E > 1) {
+#pragma unroll
+    for (int i = 0; i < E; ++i) x[i] = sum[i] * o.scale;
+    if (o.type == BERGSON_F32) {
+      float4* t = reinterpret_cast<float4*>(static_cast<float*>(o.table) + at);
+#pragma unroll
+      for (int k = 0; k < E / 4; ++k) {
+        float4 y = make_float4(x[4 * k], x[4 * k + 1], x[4 * k + 2], x[4 * k + 3]);
+        if (o.add) {
+          const float4 z = t[k];
+          y.x += z.x; y.y += z.y; y.z += z.z; y.w += z.w;
+        }
+        t[k] = y;
+      }
+      return;
+    }
+    uint2* t = reinterpret_cast<uint2*>(static_cast<uint16_t*>(o.table) + at);
+    uint2 u[E / 4];
+#pragma unroll
+    for (int k = 0; k < E / 4; ++k) {
+      uint4 w = make_uint4(0, 0, 0, 0);
+      if (o.add) {
+        const uint2 z = t[k];
+        w.x = z.x;
+        w.y = z.y;
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          const float2 f = o.type == BERGSON_BF16
+                               ? unpack2(w, h, static_cast<const __nv_bfloat16*>(nullptr))
+                               : unpack2(w, h, static_cast<const __half*>(nullptr));
+          x[4 * k + 2 * h] += f.x;
+          x[4 * k + 2 * h + 1] += f.y;
+        }
+      }
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const float2 f = make_float2(x[4 * k + 2 * h], x[4 * k + 2 * h + 1]);
+        if (o.type == BERGSON_BF16) pack2(w, h, f, static_cast<const __nv_bfloat16*>(nullptr));
+        else pack2(w, h, f, static_cast<const __half*>(nullptr));
+      }
+      u[k] = make_uint2(w.x, w.y);
+    }
+    if constexpr (E == 8)
+      *reinterpret_cast<uint4*>(t) = make_uint4(u[0].x, u[0].y, u[1].x, u[1].y);
+    else
+      *t = u[0];
+  }
+}
+
+// A thread's columns of a slab of the table's row v.
+template <typename R>
+__device__ __forceinline__ void put_row(const GradOut& o, int64_t v, int c0, int d, int t, int G,
+                                        const float (&sum)[kCols]) {
+#pragma unroll
+  for (int k = 0; k < R::kPer; ++k)
+    if (c0 + R::col(t, G, k) < d) put_columns<R::E>(o, v, c0 + R::col(t, G, k), d, sum + R::E * k);
+}
+
+// Zeros in the table's row v, by `n` threads of which this is the t-th.
+__device__ __forceinline__ void zero_row(const GradOut& o, int64_t v, int d, int t, int n) {
+  const int64_t size = o.type == BERGSON_F32 ? 4 : 2;
+  uint8_t* row = static_cast<uint8_t*>(o.table) + v * o.ld * size;
+  const int64_t bytes = d * size;
+  const int64_t vecs = o.vec ? bytes / 16 : 0;
+  for (int64_t i = t; i < vecs; i += n) reinterpret_cast<uint4*>(row)[i] = make_uint4(0, 0, 0, 0);
+  for (int64_t i = 8 * vecs + t; i < bytes / 2; i += n) reinterpret_cast<uint16_t*>(row)[i] = 0;
+}
+
+struct FewParams {
+  const void* dy;
+  const int64_t* ids;
+  GradOut out;
+  int64_t V, ld_dy;
+  int rows, d, slabs, group;   // threads of a row's slab
+  int* status;
+};
+
+// CTA r * slabs + k: the token whose first row is r, slab k.  The CTAs behind: zeros.
+template <typename T, bool kVec>
+__global__ void __launch_bounds__(kFewThreads) few_rows_kernel(
+    const __grid_constant__ FewParams p) {
+  using R = RowPart<T, kVec, kCols>;
+  __shared__ uint16_t list[kFewRows];
+  __shared__ int counts[kFewThreads / 32];
+  __shared__ float joined[kFewThreads * kCols];
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  griddep_wait();
+  const int n_sum = p.rows * p.slabs;
+  if (static_cast<int>(blockIdx.x) >= n_sum) {
+    uint8_t* touched = reinterpret_cast<uint8_t*>(list);
+    for (int i = tid; i < kFewZeros; i += kFewThreads) touched[i] = 0;
+    __syncthreads();
+    const int64_t v0 = static_cast<int64_t>(blockIdx.x - n_sum) * kFewZeros;
+    for (int j = tid; j < p.rows; j += kFewThreads) {
+      const int64_t at = p.ids[j] - v0;
+      if (at >= 0 && at < kFewZeros) touched[at] = 1;
+    }
+    __syncthreads();
+    for (int i = warp; i < kFewZeros && v0 + i < p.V; i += kFewThreads / 32)
+      if (!touched[i]) zero_row(p.out, v0 + i, p.d, lane, 32);
+    return;
+  }
+  const int r = blockIdx.x / p.slabs, slab = blockIdx.x % p.slabs;
+  const int64_t id = p.ids[r];
+  if (id < 0) return;
+  if (id >= p.V) {
+    if (tid == 0 && slab == 0) raise_device_error(p.status, nullptr, BERGSON_EINVAL);
+    return;
+  }
+  int before = 0;
+  for (int j = tid; j < r; j += kFewThreads) before |= p.ids[j] == id ? 1 : 0;
+  if (__syncthreads_or(before)) return;
+  int n = 0;
+  for (int j0 = r; j0 < p.rows; j0 += kFewThreads) {
+    const bool mine = j0 + tid < p.rows && p.ids[j0 + tid] == id;
+    const unsigned votes = __ballot_sync(0xffffffffu, mine);
+    if (lane == 0) counts[warp] = __popc(votes);
+    __syncthreads();
+    const int c = lane < kFewThreads / 32 ? counts[lane] : 0;
+    const int below = __reduce_add_sync(0xffffffffu, lane < warp ? c : 0);
+    const int all = __reduce_add_sync(0xffffffffu, c);
+    if (mine) list[n + below + __popc(votes & ((1u << lane) - 1))] = static_cast<uint16_t>(j0 + tid);
+    n += all;
+    __syncthreads();
+  }
+  // `groups` of threads take parts of the list, joined in order
+  const int groups = kFewThreads / p.group, g = tid / p.group, t = tid % p.group;
+  const int per = (n + groups - 1) / groups;
+  const int c0 = slab * p.group * kCols;
+  float sum[kCols];
+#pragma unroll
+  for (int i = 0; i < kCols; ++i) sum[i] = 0.0f;
+  if (g < groups) {
+    const int end = min(n, (g + 1) * per);
+    for (int k0 = g * per; k0 < end; k0 += kAhead) {
+      R row[kAhead];
+#pragma unroll
+      for (int k = 0; k < kAhead; ++k) {
+        const int64_t at = k0 + k < end ? list[k0 + k] : 0;
+        row[k].load(static_cast<const T*>(p.dy) + at * p.ld_dy + c0, k0 + k < end ? p.d - c0 : 0, t,
+                    p.group);
+      }
+#pragma unroll
+      for (int k = 0; k < kAhead; ++k) {
+        if (k0 + k >= end) break;
+        float x[kCols];
+        row[k].floats(x);
+#pragma unroll
+        for (int i = 0; i < kCols; ++i) sum[i] += x[i];
+      }
+    }
+  }
+  if (n > 1) {
+#pragma unroll
+    for (int i = 0; i < kCols; ++i) joined[i * kFewThreads + tid] = sum[i];
+    __syncthreads();
+    if (g == 0) {
+      for (int k = 1; k < groups && k * per < n; ++k) {
+#pragma unroll
+        for (int i = 0; i < kCols; ++i) sum[i] += joined[i * kFewThreads + k * p.group + t];
+      }
+    }
+  }
+  if (g == 0) put_row<R>(p.out, id, c0, p.d, t, p.group, sum);
+}
+
+// ---- the sort.  Keys are tokens; rows that take no part have V, behind all others.
+
+struct SortParams {
+  const int64_t* ids;
+  const uint32_t* key_in;      // nullptr: ids, of rows 0, 1, ..
+  const int* row_in;
+  uint32_t* key_out;
+  int* row_out;
+  int* table;                  // [tiles, kBins] of this pass
+  int* next_table;             // of the next pass, or nullptr: the last one
+  uint8_t* touched;            // [V]
+  int64_t V, rows;
+  int64_t tile;                // rows of a tile, a multiple of kSortItems
+  int tiles, shift, next_shift;
+  int64_t clear_words;         // of next tables, 4-byte words from clear on
+  int* clear;
+  int* status;
+};
+
+__device__ __forceinline__ uint32_t sort_key(const SortParams& p, int64_t i) {
+  if (p.key_in != nullptr) return p.key_in[i];
+  const int64_t id = p.ids[i];
+  return static_cast<uint32_t>(id >= 0 && id < p.V ? id : p.V);
+}
+
+// The first pass's counts per tile; also clears the later passes' and the marks of touched rows.
+__global__ void __launch_bounds__(kSortThreads) sort_count_kernel(
+    const __grid_constant__ SortParams p) {
+  __shared__ int bins[kBins];
+  griddep_wait();
+  const int64_t step = static_cast<int64_t>(gridDim.x) * kSortThreads;
+  const int64_t me = static_cast<int64_t>(blockIdx.x) * kSortThreads + threadIdx.x;
+  for (int64_t i = me; i < p.clear_words; i += step) p.clear[i] = 0;
+  if (static_cast<int>(blockIdx.x) >= p.tiles) return;
+  if (threadIdx.x < kBins) bins[threadIdx.x] = 0;
+  __syncthreads();
+  const int64_t end = min((blockIdx.x + 1) * p.tile, p.rows);
+  for (int64_t i = blockIdx.x * p.tile + threadIdx.x; i < end; i += kSortThreads) {
+    if (p.ids[i] >= p.V) raise_device_error(p.status, nullptr, BERGSON_EINVAL);
+    atomicAdd(&bins[(sort_key(p, i) >> p.shift) & (kBins - 1)], 1);
+  }
+  __syncthreads();
+  if (threadIdx.x < kBins) p.table[blockIdx.x * kBins + threadIdx.x] = bins[threadIdx.x];
+}
+
+// Places a tile's items: behind those of smaller digits and those of the tiles before it.
+__global__ void __launch_bounds__(kSortThreads) sort_place_kernel(
+    const __grid_constant__ SortParams p) {
+  constexpr int kWarps = kSortThreads / 32;
+  constexpr int kRounds = kSortItems / kSortThreads;
+  __shared__ uint16_t hist[kWarps][kBins];
+  __shared__ int base[kBins];
+  __shared__ int part[2][2][kBins];
+  __shared__ int scan[kBins / 32];
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  griddep_wait();
+  {
+    // what stands before this tile and in all: two halves of the tiles a digit
+    const int digit = tid & (kBins - 1), half = tid / kBins;
+    int before = 0, all = 0;
+    for (int t = half; t < p.tiles; t += kSortThreads / kBins) {
+      const int c = p.table[t * kBins + digit];
+      all += c;
+      before += t < static_cast<int>(blockIdx.x) ? c : 0;
+    }
+    part[half][0][digit] = before;
+    part[half][1][digit] = all;
+    __syncthreads();
+    int total = 0, incl = 0;
+    if (tid < kBins) {
+      before = part[0][0][tid] + part[1][0][tid];
+      total = part[0][1][tid] + part[1][1][tid];
+      incl = total;
+#pragma unroll
+      for (int o = 1; o < 32; o <<= 1) {
+        const int v = __shfl_up_sync(0xffffffffu, incl, o);
+        if (lane >= o) incl += v;
+      }
+      if (lane == 31) scan[warp] = incl;
+    }
+    __syncthreads();
+    if (tid < kBins) {
+      for (int w = 0; w < warp; ++w) incl += scan[w];
+      base[tid] = incl - total + before;
+    }
+  }
+  const int64_t begin = blockIdx.x * p.tile, end = min(begin + p.tile, p.rows);
+  for (int64_t i0 = begin; i0 < end; i0 += kSortItems) {
+    for (int i = tid; i < kWarps * kBins / 2; i += kSortThreads)
+      reinterpret_cast<uint32_t*>(hist)[i] = 0;
+    __syncthreads();
+    uint32_t key[kRounds];
+    unsigned same[kRounds];
+#pragma unroll
+    for (int k = 0; k < kRounds; ++k) {
+      const int64_t i = i0 + (warp * kRounds + k) * 32 + lane;
+      key[k] = i < end ? sort_key(p, i) : 0;
+      // an item past the end has a digit of its own
+      const uint32_t digit = i < end ? (key[k] >> p.shift) & (kBins - 1) : kBins;
+      same[k] = __match_any_sync(0xffffffffu, digit);
+      if (i < end && lane == __ffs(same[k]) - 1) hist[warp][digit] += __popc(same[k]);
+      __syncwarp();
+    }
+    __syncthreads();
+    int sum = 0;
+    if (tid < kBins) {
+      for (int w = 0; w < kWarps; ++w) {
+        const int c = hist[w][tid];
+        hist[w][tid] = static_cast<uint16_t>(sum);
+        sum += c;
+      }
+    }
+    __syncthreads();
+#pragma unroll
+    for (int k = 0; k < kRounds; ++k) {
+      const int64_t i = i0 + (warp * kRounds + k) * 32 + lane;
+      const uint32_t digit = (key[k] >> p.shift) & (kBins - 1);
+      int at = 0;
+      if (i < end) at = base[digit] + hist[warp][digit] + __popc(same[k] & ((1u << lane) - 1));
+      __syncwarp();
+      if (i < end) {
+        if (lane == __ffs(same[k]) - 1) hist[warp][digit] += __popc(same[k]);
+        p.key_out[at] = key[k];
+        p.row_out[at] = p.row_in != nullptr ? p.row_in[i] : static_cast<int>(i);
+        if (p.next_table != nullptr)
+          atomicAdd(&p.next_table[at / p.tile * kBins + ((key[k] >> p.next_shift) & (kBins - 1))], 1);
+        else if (p.touched != nullptr && key[k] < p.V)
+          p.touched[key[k]] = 1;
+      }
+      __syncwarp();
+    }
+    __syncthreads();
+    if (tid < kBins) base[tid] += sum;
+  }
+}
+
+// ---- sums of the sorted rows
+
+struct SumParams {
+  const void* dy;
+  const uint32_t* key;
+  const int* row;
+  const uint8_t* touched;      // nullptr: no zeros
+  float* part;                 // [runs, 2, ld_part]
+  GradOut out;
+  int64_t V, rows, ld_dy, ld_part;
+  int64_t runs;
+  int64_t n_sum;               // CTAs that add
+  int d, slabs;
+};
+
+template <typename T, bool kVec>
+__global__ void __launch_bounds__(kSumThreads) sum_kernel(const __grid_constant__ SumParams p) {
+  using R = RowPart<T, kVec, kCols>;
+  __shared__ uint32_t keys[kRun + 2];            // one before, one behind
+  __shared__ int rows[kRun];
+  const int tid = threadIdx.x, G = blockDim.x;
+  griddep_wait();
+  if (blockIdx.x >= p.n_sum) {
+    const int64_t step = static_cast<int64_t>(gridDim.x - p.n_sum) * (G / 32);
+    for (int64_t v = (blockIdx.x - p.n_sum) * (G / 32) + (tid >> 5); v < p.V; v += step)
+      if (!p.touched[v]) zero_row(p.out, v, p.d, tid & 31, 32);
+    return;
+  }
+  const uint32_t none = static_cast<uint32_t>(p.V);
+  const int64_t run = blockIdx.x / p.slabs, p0 = run * kRun;
+  const int c0 = static_cast<int>(blockIdx.x % p.slabs) * G * kCols;
+  for (int i = tid; i < kRun + 2; i += G) {
+    const int64_t at = p0 + i - 1;
+    keys[i] = at >= 0 && at < p.rows ? p.key[at] : none;
+    if (i < kRun) rows[i] = p0 + i < p.rows ? p.row[p0 + i] : 0;
+  }
+  __syncthreads();
+  bool open = keys[0] == keys[1];                // the first token began before
+  float sum[kCols];
+#pragma unroll
+  for (int i = 0; i < kCols; ++i) sum[i] = 0.0f;
+  for (int j0 = 0; j0 < kRun; j0 += kAhead) {
+    if (keys[j0 + 1] == none) break;
+    R row[kAhead];
+#pragma unroll
+    for (int k = 0; k < kAhead; ++k)
+      row[k].load(static_cast<const T*>(p.dy) + rows[j0 + k] * p.ld_dy + c0,
+                  keys[j0 + k + 1] != none ? p.d - c0 : 0, tid, G);
+#pragma unroll
+    for (int k = 0; k < kAhead; ++k) {
+      const int j = j0 + k;
+      const uint32_t v = keys[j + 1];
+      if (v == none) break;
+      float x[kCols];
+      row[k].floats(x);
+#pragma unroll
+      for (int i = 0; i < kCols; ++i) sum[i] += x[i];
+      const bool ends = keys[j + 2] != v;
+      if (!ends && j < kRun - 1) continue;
+      if (open || !ends) {
+        float* part = p.part + (2 * run + (open ? 0 : 1)) * p.ld_part;
+#pragma unroll
+        for (int i = 0; i < kCols; ++i) {
+          const int c = c0 + R::column(tid, G, i);
+          if (c < p.d) part[c] = sum[i];
+        }
+      } else {
+        put_row<R>(p.out, v, c0, p.d, tid, G, sum);
+      }
+      open = false;
+#pragma unroll
+      for (int i = 0; i < kCols; ++i) sum[i] = 0.0f;
+    }
+  }
+}
+
+// The tokens that cross ends of runs: the CTA of the run where a token begins adds
+// what that run and the next ones have of it, eight warps a part each, joined in order.
+__global__ void __launch_bounds__(kJoinThreads) join_kernel(const __grid_constant__ SumParams p) {
+  constexpr int kWarps = kJoinThreads / 32;
+  constexpr int kE = kJoinCols / 32;
+  static_assert(kE == 4, "a lane takes 16 bytes of a sum");
+  __shared__ float red[kWarps][kJoinCols];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int c0 = blockIdx.y * kJoinCols;
+  const uint32_t none = static_cast<uint32_t>(p.V);
+  griddep_wait();
+  for (int k = 0; k < kJoinRuns; ++k) {
+    const int64_t run = static_cast<int64_t>(blockIdx.x) * kJoinRuns + k;
+    const int64_t last = run * kRun + kRun - 1;
+    if (last + 1 >= p.rows) return;
+    const uint32_t v = p.key[last];
+    if (v == none) return;
+    if (p.key[last + 1] != v || (run > 0 && p.key[run * kRun - 1] == v)) continue;
+    int64_t n = 1;                               // runs behind that hold some of it
+    for (;; n += 32) {
+      const int64_t at = (run + n + 1 + lane) * kRun;   // does run + n + lane + 1 hold some too?
+      const unsigned votes = __ballot_sync(0xffffffffu, at < p.rows && p.key[at] == v);
+      if (votes != 0xffffffffu) {
+        n += __ffs(~votes) - 1;
+        break;
+      }
+    }
+    // part 0 is this run's second sum, part q the first of run + q
+    const int64_t per = (n + 1 + kWarps - 1) / kWarps;
+    const int64_t begin = warp * per, end = min(begin + per, n + 1);
+    float sum[kE];
+#pragma unroll
+    for (int i = 0; i < kE; ++i) sum[i] = 0.0f;
+#pragma unroll 4
+    for (int64_t q = begin; q < end; ++q) {
+      const float* part = p.part + (2 * (run + q) + (q == 0 ? 1 : 0)) * p.ld_part + c0;
+      if (c0 + kE * lane < p.ld_part) {
+        const float4 x = *reinterpret_cast<const float4*>(part + kE * lane);
+        sum[0] += x.x; sum[1] += x.y; sum[2] += x.z; sum[3] += x.w;
+      }
+    }
+    __syncthreads();                             // the last token's sums have been read
+#pragma unroll
+    for (int i = 0; i < kE; ++i) red[warp][kE * lane + i] = sum[i];
+    __syncthreads();
+    if (warp == 0) {
+      for (int w = 1; w < kWarps; ++w) {
+#pragma unroll
+        for (int i = 0; i < kE; ++i) sum[i] += red[w][kE * lane + i];
+      }
+      const int c = c0 + kE * lane;
+      if (c < p.d) put_columns<kE>(p.out, v, c, p.d, sum);
+    }
+  }
+}
+
+size_t round256(size_t n) { return (n + 255) / 256 * 256; }
+
+// Threads of a row's slab: 8 columns each.
+int slab_threads(int64_t d) {
+  return static_cast<int>(std::min<int64_t>(kSumThreads, ceil_div(ceil_div(d, kCols), 32) * 32));
+}
+
+struct SortPlan {
+  int passes = 1, tiles = 1;
+  int64_t tile = kSortItems, runs = 0, ld_part = 0;
+  size_t table = 0, touched = 0, key[2] = {0, 0}, row[2] = {0, 0}, part = 0, total = 0;
+  int64_t clear_words = 0;     // from the second pass's table to the end of `touched`
+};
+
+SortPlan sort_plan(int64_t rows, int64_t V, int64_t d) {
+  SortPlan s;
+  int bits = 1;
+  while ((V >> bits) != 0) ++bits;             // keys are 0 .. V
+  s.passes = static_cast<int>(ceil_div(bits, kDigitBits));
+  s.tile = ceil_div(ceil_div(rows, kMaxTiles), kSortItems) * kSortItems;
+  s.tiles = static_cast<int>(ceil_div(rows, s.tile));
+  s.runs = ceil_div(rows, kRun);
+  s.ld_part = ceil_div(d, 8) * 8;
+  size_t at = 0;
+  const auto take = [&](size_t bytes) {
+    const size_t here = at;
+    at += round256(bytes);
+    return here;
+  };
+  const size_t one = static_cast<size_t>(s.tiles) * kBins * sizeof(int);
+  s.table = take(one * s.passes);
+  s.touched = take(static_cast<size_t>(V));
+  s.clear_words = static_cast<int64_t>((at - s.table - one) / 4);
+  for (int i = 0; i < 2; ++i) {
+    s.key[i] = take(static_cast<size_t>(rows) * 4);
+    s.row[i] = take(static_cast<size_t>(rows) * 4);
+  }
+  s.part = take(static_cast<size_t>(s.runs) * 2 * s.ld_part * sizeof(float));
+  s.total = at;
+  return s;
+}
+
+template <typename T, bool kVec>
+cudaError_t run_few(const EmbeddingGradArgs& a, const GradOut& out, cudaStream_t s) {
+  FewParams p = {};
+  p.dy = a.dy;
+  p.ids = a.ids;
+  p.out = out;
+  p.V = a.V;
+  p.ld_dy = a.ld_dy;
+  p.rows = static_cast<int>(a.rows);
+  p.d = static_cast<int>(a.d);
+  p.group = slab_threads(a.d);
+  p.slabs = static_cast<int>(ceil_div(a.d, p.group * kCols));
+  p.status = a.status;
+  const int64_t grid = a.rows * p.slabs + (a.add ? 0 : ceil_div(a.V, kFewZeros));
+  return launch_dependent(few_rows_kernel<T, kVec>, dim3(static_cast<unsigned>(grid)),
+                          dim3(kFewThreads), 0, s, p);
+}
+
+template <typename T, bool kVec>
+cudaError_t run_sums(const EmbeddingGradArgs& a, SumParams p, cudaStream_t s) {
+  const int threads = slab_threads(a.d);
+  p.slabs = static_cast<int>(ceil_div(a.d, threads * kCols));
+  p.n_sum = p.runs * p.slabs;
+  const int64_t zeros =
+      a.add ? 0 : std::min<int64_t>(ceil_div(a.V, threads / 32), 4 * kPlanCTAs);
+  return launch_dependent(sum_kernel<T, kVec>, dim3(static_cast<unsigned>(p.n_sum + zeros)),
+                          dim3(threads), 0, s, p);
+}
+
+cudaError_t run_sorted(const EmbeddingGradArgs& a, const GradOut& out, bool vec, uint8_t* ws,
+                       cudaStream_t s) {
+  const SortPlan plan = sort_plan(a.rows, a.V, a.d);
+  SortParams p = {};
+  p.ids = a.ids;
+  p.table = reinterpret_cast<int*>(ws + plan.table);
+  p.V = a.V;
+  p.rows = a.rows;
+  p.tile = plan.tile;
+  p.tiles = plan.tiles;
+  p.clear = p.table + plan.tiles * kBins;
+  p.clear_words = a.add ? static_cast<int64_t>(plan.passes - 1) * plan.tiles * kBins
+                        : plan.clear_words;
+  p.status = a.status;
+  const int64_t ctas =
+      std::max<int64_t>(plan.tiles, std::min<int64_t>(kPlanCTAs, p.clear_words / 8192));
+  cudaError_t e = launch_dependent(sort_count_kernel, dim3(static_cast<unsigned>(ctas)),
+                                   dim3(kSortThreads), 0, s, p);
+  for (int k = 0; k < plan.passes && e == cudaSuccess; ++k) {
+    const bool last = k == plan.passes - 1;
+    p.key_in = k == 0 ? nullptr : p.key_out;
+    p.row_in = k == 0 ? nullptr : p.row_out;
+    p.key_out = reinterpret_cast<uint32_t*>(ws + plan.key[k & 1]);
+    p.row_out = reinterpret_cast<int*>(ws + plan.row[k & 1]);
+    p.table = reinterpret_cast<int*>(ws + plan.table) + k * plan.tiles * kBins;
+    p.next_table = last ? nullptr : p.table + plan.tiles * kBins;
+    p.shift = k * kDigitBits;
+    p.next_shift = p.shift + kDigitBits;
+    p.touched = a.add ? nullptr : ws + plan.touched;
+    e = launch_dependent(sort_place_kernel, dim3(static_cast<unsigned>(plan.tiles)),
+                         dim3(kSortThreads), 0, s, p);
+  }
+  if (e != cudaSuccess) return e;
+  SumParams q = {};
+  q.dy = a.dy;
+  q.key = p.key_out;
+  q.row = p.row_out;
+  q.touched = p.touched;
+  q.part = reinterpret_cast<float*>(ws + plan.part);
+  q.out = out;
+  q.V = a.V;
+  q.rows = a.rows;
+  q.ld_dy = a.ld_dy;
+  q.ld_part = plan.ld_part;
+  q.runs = plan.runs;
+  q.d = static_cast<int>(a.d);
+  if (a.dtype == BERGSON_BF16)
+    e = vec ? run_sums<__nv_bfloat16, true>(a, q, s) : run_sums<__nv_bfloat16, false>(a, q, s);
+  else if (a.dtype == BERGSON_F16)
+    e = vec ? run_sums<__half, true>(a, q, s) : run_sums<__half, false>(a, q, s);
+  else
+    e = vec ? run_sums<float, true>(a, q, s) : run_sums<float, false>(a, q, s);
+  if (e != cudaSuccess) return e;
+  const dim3 grid(static_cast<unsigned>(ceil_div(plan.runs, kJoinRuns)),
+                  static_cast<unsigned>(ceil_div(a.d, kJoinCols)));
+  return launch_dependent(join_kernel, grid, dim3(kJoinThreads), 0, s, q);
+}
+
+template <typename T>
+cudaError_t run_lookup(const EmbeddingArgs& a, cudaStream_t s) {
+  const bool vec = on16(a.table, a.ld_t, sizeof(T)) && on16(a.out, a.ld_o, sizeof(T));
+  LookupParams p = {};
+  p.table = a.table;
+  p.ids = a.ids;
+  p.out = a.out;
+  p.V = a.V;
+  p.rows = a.rows;
+  p.ld_t = a.ld_t;
+  p.ld_o = a.ld_o;
+  p.d = static_cast<int>(a.d);
+  p.slabs = static_cast<int>(ceil_div(a.d, 32 * (vec ? 4 * Vec16<T>::kElems : 8)));
+  p.scale = static_cast<float>(a.scale);
+  p.status = a.status;
+  const int64_t grid = ceil_div(a.rows * p.slabs, kLookupThreads / 32);
+  if (grid > INT32_MAX) return cudaErrorInvalidConfiguration;
+  const auto kernel = vec ? lookup_kernel<T, true> : lookup_kernel<T, false>;
+  return launch_dependent(kernel, dim3(static_cast<unsigned>(grid)), dim3(kLookupThreads), 0, s, p);
+}
+
+}  // namespace
+
+cudaError_t launch_embedding(const EmbeddingArgs& a, cudaStream_t s) {
+  if (a.dtype == BERGSON_BF16) return run_lookup<__nv_bfloat16>(a, s);
+  if (a.dtype == BERGSON_F16) return run_lookup<__half>(a, s);
+  return run_lookup<float>(a, s);
+}
+
+size_t embedding_backward_workspace(int64_t rows, int64_t V, int64_t d) {
+  return rows <= kFewRows ? 256 : sort_plan(rows, V, d).total;
+}
+
+cudaError_t launch_embedding_backward(const EmbeddingGradArgs& a, void* ws, cudaStream_t s) {
+  GradOut out = {};
+  out.table = a.d_table;
+  out.ld = a.ld_t;
+  out.type = a.t_dtype;
+  out.vec = on16(a.d_table, a.ld_t, a.t_dtype == BERGSON_F32 ? 4 : 2) ? 1 : 0;
+  out.add = a.add ? 1 : 0;
+  out.scale = static_cast<float>(a.scale);
+  const bool vec = on16(a.dy, a.ld_dy, a.dtype == BERGSON_F32 ? 4 : 2);
+  if (a.rows > kFewRows) return run_sorted(a, out, vec, static_cast<uint8_t*>(ws), s);
+  if (a.rows == 0 && a.add) return cudaSuccess;
+  if (a.dtype == BERGSON_BF16)
+    return vec ? run_few<__nv_bfloat16, true>(a, out, s) : run_few<__nv_bfloat16, false>(a, out, s);
+  if (a.dtype == BERGSON_F16)
+    return vec ? run_few<__half, true>(a, out, s) : run_few<__half, false>(a, out, s);
+  return vec ? run_few<float, true>(a, out, s) : run_few<float, false>(a, out, s);
+}
+
+}  // namespace bergson

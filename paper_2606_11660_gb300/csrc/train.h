@@ -1,5 +1,6 @@
 // Arguments and launchers of the training-side operators (token
-// log-probabilities, losses, AdamW, factored moments, norms).
+// log-probabilities, losses, AdamW, factored moments, norms,
+// embedding).
 #pragma once
 
 #include <cuda_runtime.h>
@@ -93,5 +94,33 @@ struct NormGradArgs {
 };
 size_t norm_backward_workspace(int64_t rows, int64_t d);
 cudaError_t launch_norm_backward(const NormGradArgs& a, void* ws, cudaStream_t s);
+
+struct EmbeddingArgs {
+  const void* table;           // [V, ld_t] of dtype
+  int dtype;
+  int64_t V, d, ld_t;
+  const int64_t* ids;          // [rows]
+  int64_t rows;
+  double scale;
+  void* out;                   // [rows, ld_o]
+  int64_t ld_o;
+  int* status;
+};
+cudaError_t launch_embedding(const EmbeddingArgs& a, cudaStream_t s);
+
+struct EmbeddingGradArgs {
+  const void* dy;              // [rows, ld_dy] of dtype
+  int dtype;
+  int64_t rows, d, ld_dy;
+  const int64_t* ids;          // [rows]
+  double scale;
+  void* d_table;               // [V, ld_t] of t_dtype
+  int t_dtype;
+  int64_t V, ld_t;
+  bool add;
+  int* status;
+};
+size_t embedding_backward_workspace(int64_t rows, int64_t V, int64_t d);
+cudaError_t launch_embedding_backward(const EmbeddingGradArgs& a, void* ws, cudaStream_t s);
 
 }  // namespace bergson

@@ -112,6 +112,15 @@ int check_in_place(const void* out, int64_t ld_out, const void* in, int64_t ld_i
   return BERGSON_OK;
 }
 
+int check_embedding(int64_t rows, int64_t V, int64_t d) {
+  if (rows < 0 || rows > INT32_MAX) return fail(BERGSON_EINVAL, "rows must be in [0, 2^31)");
+  if (V < 1 || V > INT32_MAX) return fail(BERGSON_EINVAL, "V must be in [1, 2^31)");
+  if (d < 1) return fail(BERGSON_EINVAL, "d must be >= 1");
+  if (d > (1ll << 24)) return fail(BERGSON_EUNSUPPORTED, "d must be <= 2^24");
+  if (rows * ((d + 255) / 256) > INT32_MAX) return fail(BERGSON_EUNSUPPORTED, "rows*d too large");
+  return BERGSON_OK;
+}
+
 bool probability(double x) { return x >= 0.0 && x <= 1.0; }
 
 }  // namespace
@@ -433,6 +442,67 @@ int bergson_norm_backward(const void* x, int dtype, int64_t rows, int64_t d, int
                        mean, rstd,  dy,   ld_dy, dx,   ld_dx,  d_weight, d_bias};
   const cudaError_t e = launch_norm_backward(a, workspace, static_cast<cudaStream_t>(stream));
   if (e != cudaSuccess) return fail_cuda(e, "norm backward launch");
+  return BERGSON_OK;
+}
+
+int bergson_embedding(const void* table, int dtype, int64_t V, int64_t d, int64_t ld_t,
+                      const int64_t* ids, int64_t rows, double scale, void* out, int64_t ld_o,
+                      void* stream) {
+  BERGSON_TRY(check_embedding(rows, V, d));
+  const size_t size = dtype_size(dtype);
+  if (size == 0) return fail(BERGSON_EINVAL, "unknown dtype %d", dtype);
+  if (!std::isfinite(static_cast<float>(scale)))
+    return fail(BERGSON_EINVAL, "scale must be finite");
+  if (rows > 0) {
+    BERGSON_TRY(check_rows(table, size, d, ld_t, "table"));
+    BERGSON_TRY(check_tensor(ids, 8, "ids"));
+    BERGSON_TRY(check_rows(out, size, d, ld_o, "out"));
+  }
+  BERGSON_TRY(injected_status());
+  if (rows == 0) return BERGSON_OK;
+  DeviceGuard dg(out);
+  if (dg.err != cudaSuccess) return fail_cuda(dg.err, "output device lookup");
+  int* status = device_status_word(dg.dev);
+  if (status == nullptr) return fail(BERGSON_ECUDA, "device status word unavailable");
+  const EmbeddingArgs a{table, dtype, V, d, ld_t, ids, rows, scale, out, ld_o, status};
+  const cudaError_t e = launch_embedding(a, static_cast<cudaStream_t>(stream));
+  if (e != cudaSuccess) return fail_cuda(e, "embedding launch");
+  return BERGSON_OK;
+}
+
+int bergson_embedding_backward_workspace(int64_t rows, int64_t V, int64_t d, size_t* ws_bytes) {
+  if (ws_bytes == nullptr) return fail(BERGSON_EINVAL, "ws_bytes is NULL");
+  BERGSON_TRY(check_embedding(rows, V, d));
+  *ws_bytes = embedding_backward_workspace(rows, V, d);
+  return BERGSON_OK;
+}
+
+int bergson_embedding_backward(const void* dy, int dtype, int64_t rows, int64_t d, int64_t ld_dy,
+                               const int64_t* ids, double scale, void* d_table, int t_dtype,
+                               int64_t V, int64_t ld_t, int add, void* workspace, size_t ws_bytes,
+                               void* stream) {
+  BERGSON_TRY(check_embedding(rows, V, d));
+  const size_t size = dtype_size(dtype), t_size = dtype_size(t_dtype);
+  if (size == 0 || t_size == 0)
+    return fail(BERGSON_EINVAL, "unknown dtype (dy %d, d_table %d)", dtype, t_dtype);
+  if (!std::isfinite(static_cast<float>(scale)))
+    return fail(BERGSON_EINVAL, "scale must be finite");
+  if (rows > 0) {
+    BERGSON_TRY(check_rows(dy, size, d, ld_dy, "dy"));
+    BERGSON_TRY(check_tensor(ids, 8, "ids"));
+  }
+  BERGSON_TRY(check_rows(d_table, t_size, d, ld_t, "d_table"));
+  BERGSON_TRY(check_workspace(workspace, ws_bytes, embedding_backward_workspace(rows, V, d)));
+  BERGSON_TRY(injected_status());
+  DeviceGuard dg(d_table);
+  if (dg.err != cudaSuccess) return fail_cuda(dg.err, "output device lookup");
+  int* status = device_status_word(dg.dev);
+  if (status == nullptr) return fail(BERGSON_ECUDA, "device status word unavailable");
+  const EmbeddingGradArgs a{dy,      dtype,   rows, d,    ld_dy,    ids,   scale,
+                            d_table, t_dtype, V,    ld_t, add != 0, status};
+  const cudaError_t e =
+      launch_embedding_backward(a, workspace, static_cast<cudaStream_t>(stream));
+  if (e != cudaSuccess) return fail_cuda(e, "embedding backward launch");
   return BERGSON_OK;
 }
 

@@ -92,3 +92,58 @@ def test_norm_calls_that_pass():
     # a row of dw and db a CTA at most
     assert all(bg.bergson_norm_backward_workspace(1 << 30, d) <= 152 * 8 * 2 * 4 * max(d, 512)
                for d in (1, 24, 512, 513, 2048, 8192, 16_384, 16_385, 1 << 20))
+
+
+def embed(**kw):
+    a = dict(table=FAKE, dtype=bg.BERGSON_BF16, V=50, d=100, ld_t=100, ids=FAKE, rows=4, scale=1.0,
+             out=FAKE + 65_536, ld_o=100)
+    a.update(kw)
+    return bg.lib().bergson_embedding(*a.values(), None)
+
+
+def dembed(ws=FAKE, ws_bytes=1 << 30, **kw):
+    a = dict(dy=FAKE, dtype=bg.BERGSON_BF16, rows=4, d=100, ld_dy=100, ids=FAKE, scale=1.0,
+             dt=FAKE + 65_536, tt=0, V=50, ld_t=100, add=0)
+    a.update(kw)
+    return bg.lib().bergson_embedding_backward(*a.values(), ws, ws_bytes, None)
+
+
+EMBED_BAD = [
+    (dict(dtype=7), bg.BERGSON_EINVAL), (dict(rows=-1), bg.BERGSON_EINVAL),
+    (dict(rows=1 << 31), bg.BERGSON_EINVAL), (dict(V=0), bg.BERGSON_EINVAL),
+    (dict(V=1 << 31), bg.BERGSON_EINVAL), (dict(d=0), bg.BERGSON_EINVAL),
+    (dict(d=1 << 25), bg.BERGSON_EUNSUPPORTED), (dict(rows=1 << 30, d=1024), bg.BERGSON_EUNSUPPORTED),
+    (dict(scale=INF), bg.BERGSON_EINVAL), (dict(scale=NAN), bg.BERGSON_EINVAL),
+    (dict(scale=1e39), bg.BERGSON_EINVAL), (dict(ids=None), bg.BERGSON_EINVAL),
+    (dict(ids=FAKE + 4), bg.BERGSON_EALIGN), (dict(ld_t=99), bg.BERGSON_EINVAL),
+]
+
+
+@pytest.mark.parametrize("kw,code", EMBED_BAD + [
+    (dict(table=None), bg.BERGSON_EINVAL), (dict(table=FAKE + 1), bg.BERGSON_EALIGN),
+    (dict(out=None), bg.BERGSON_EINVAL), (dict(out=FAKE + 1), bg.BERGSON_EALIGN),
+    (dict(ld_o=99), bg.BERGSON_EINVAL)])
+def test_embedding_refusals(kw, code):
+    assert embed(**kw) == code and bg.bergson_last_error() != ""
+
+
+@pytest.mark.parametrize("kw,code", EMBED_BAD + [
+    (dict(tt=3), bg.BERGSON_EINVAL), (dict(dy=None), bg.BERGSON_EINVAL),
+    (dict(dy=FAKE + 1), bg.BERGSON_EALIGN), (dict(ld_dy=99), bg.BERGSON_EINVAL),
+    (dict(dt=None), bg.BERGSON_EINVAL), (dict(dt=FAKE + 2), bg.BERGSON_EALIGN),
+    (dict(ws=None), bg.BERGSON_EINVAL), (dict(ws=FAKE + 128), bg.BERGSON_EALIGN),
+    (dict(ws_bytes=1), bg.BERGSON_EWORKSPACE)])
+def test_embedding_backward_refusals(kw, code):
+    assert dembed(**kw) == code and bg.bergson_last_error() != ""
+
+
+def test_embedding_calls_that_pass():
+    for st in (embed(), embed(table=FAKE + 2, ld_t=101), embed(rows=0, table=None, ids=None, out=None),
+               embed(scale=-2.0), dembed(), dembed(add=1, tt=1), dembed(rows=0, dy=None, ids=None),
+               dembed(rows=5000, ws_bytes=bg.bergson_embedding_backward_workspace(5000, 50, 100))):
+        assert accepted(st), bg.bergson_last_error()
+    assert dembed(rows=5000, ws_bytes=4096) == bg.BERGSON_EWORKSPACE
+    assert bg.lib().bergson_embedding_backward_workspace(4, 4, 4, None) == bg.BERGSON_EINVAL
+    for sizes in ((0, 1, 1), (2048, 50_000, 64), (2049, 50_000, 64), (1 << 20, 1 << 18, 100)):
+        need = bg.bergson_embedding_backward_workspace(*sizes)
+        assert need > 0 and need % 256 == 0

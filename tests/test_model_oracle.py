@@ -28,3 +28,15 @@ def test_norm_closed_forms():
     assert np.allclose(y[0], [-1, 1]) and np.allclose(mean, [2, 2]) and rstd[0] == 1
     y, _, rstd = orc.norm(x, None, None, False, 0.0)
     assert np.allclose((y ** 2).mean(1), 1) and np.allclose(rstd[1], 0.5)
+
+
+def test_embedding_gradient():
+    r = np.random.default_rng(1)
+    table, u, dy = r.normal(size=(7, 4)), r.normal(size=(7, 4)), r.normal(size=(6, 4))
+    ids = [3, 0, -1, 3, 6, 0]
+
+    def f(e):
+        return (orc.embedding(table + e * u, ids, 1.7) * dy).sum()
+    d, size = orc.embedding_backward(dy, ids, 1.7, 7)
+    assert abs(along(f) - (d * u).sum()) < 1e-8
+    assert np.all(d[[1, 2, 4, 5]] == 0) and np.all(size >= np.abs(d))
