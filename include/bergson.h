@@ -1029,6 +1029,62 @@ BERGSON_API int bergson_embedding_backward(const void* dy, int dtype, int64_t ro
                                            int add, void* workspace, size_t ws_bytes,
                                            void* stream);
 
+/*
+ * One matrix of a Muon step.
+ *   param     [rows, cols] of param_dtype, contiguous, updated in place.
+ *   grad      [rows, cols] of grad_dtype, contiguous.
+ *   master    fp32 [rows, cols] or NULL.  With it the step is taken on `master` and param
+ *             receives its rounding; without, on param.
+ *   m         fp32 [rows, cols], the momentum, updated in place; zeros before the first step.
+ *   lr_scale  multiplies the call's lr;  ortho_scale  the orthogonalised update (e.g. 0.2
+ *             sqrt(max(rows, cols)));  weight_decay  decoupled.
+ * rows, cols in [1, 2^20], the smaller of them <= 2^16.  Matrices share no memory.
+ */
+typedef struct bergson_muon_tensor {
+  void* param;
+  const void* grad;
+  float* master;
+  float* m;
+  int64_t rows;
+  int64_t cols;
+  float lr_scale;
+  float ortho_scale;
+  float weight_decay;
+  int32_t param_dtype, grad_dtype;   /* bergson_dtype */
+  int32_t reserved;                  /* 0 */
+} bergson_muon_tensor;
+
+/*
+ * One Muon step over many matrices: with g the gradient times *grad_scale,
+ *
+ *   m <- beta m + (1 - beta) g,   u = m, or beta m + (1 - beta) g with nesterov != 0,
+ *   X = u / |u|_F;  per (a, b, c) of coefficients:  A = X X^T,  X <- (a I + b A + c A^2) X,
+ *   param <- param - lr lr_scale (ortho_scale X + weight_decay param)
+ *
+ * (X^T X and from the right where rows > cols, which is the same).  The iteration drives X's
+ * singular values toward 1.  An update of zeros has X = 0; one that holds NaN or an infinity
+ * spoils its matrix, and no other.
+ *
+ *   tensors   HOST array of n_tensors (>= 0) records, of any shapes; matrices of one shape run
+ *             together.
+ *   coefficients  HOST array [n_iterations, 3], n_iterations in [1, 64].  From |X|_F = 1 they must
+ *             hold |X|, |A| and |b A + c A^2| to 48 (EUNSUPPORTED; a bound by the polynomials alone).
+ *   products  3: the products' operands hold 22 bits (X is off by some 1e-6 |X| an iteration).
+ *             1: they hold fp16's 11 (some 1e-3), at a third of the work: for weights without a
+ *             master copy, whose own rounding is larger.
+ *   grad_scale  device fp32 [1] or NULL (1).
+ *   workspace 256-byte aligned, contents on entry ignored; its size follows from the shapes and
+ *             products.
+ * All tensors live on one device.  Sums are fp32; the same call gives the same bits.
+ * Errors: EINVAL, EALIGN, EUNSUPPORTED, EWORKSPACE, ECUDA.
+ */
+BERGSON_API int bergson_muon_step_workspace(const bergson_muon_tensor* tensors, int n_tensors,
+                                            int products, size_t* ws_bytes);
+BERGSON_API int bergson_muon_step(const bergson_muon_tensor* tensors, int n_tensors, double lr,
+                                  double beta, int nesterov, const double* coefficients,
+                                  int n_iterations, int products, const float* grad_scale,
+                                  void* workspace, size_t ws_bytes, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -46,3 +46,28 @@ def embedding_backward(dy, ids, scale, V):
             out[0, i] += scale * dy[r]
             out[1, i] += abs(scale) * np.abs(dy[r])
     return out[0], out[1]
+
+
+# ------------------------------------------------------------------ Muon
+
+def newton_schulz(u, coefficients, hold=lambda x: x, product=lambda x: x):
+    """The iteration on u / |u|_F in fp64.  hold rounds what an operand holds, product what a
+    product gives: the identity by default."""
+    n = np.linalg.norm(u)
+    x = hold(u / n if n > 0 else np.zeros_like(u))
+    tall = u.shape[0] > u.shape[1]
+    for a, b, c in coefficients:
+        y = x.T if tall else x
+        g = hold(product(y @ y.T))
+        q = hold(b * g + c * product(g @ g))
+        x = a * x + product(x @ q if tall else q @ x)
+        x = hold(x)
+    return x
+
+
+def muon_step(w, g, m, lr, beta, nesterov, coefficients, ortho_scale, weight_decay):
+    """(w, m, X) after the step, all fp64."""
+    m = beta * m + (1 - beta) * g
+    u = beta * m + (1 - beta) * g if nesterov else m
+    x = newton_schulz(u, coefficients)
+    return w - lr * (ortho_scale * x + weight_decay * w), m, x

@@ -88,6 +88,7 @@ EXPORTED = (
     "bergson_adamw_state_values", "bergson_factor_moments_workspace", "bergson_factor_moments",
     "bergson_norm", "bergson_norm_backward_workspace", "bergson_norm_backward",
     "bergson_embedding", "bergson_embedding_backward_workspace", "bergson_embedding_backward",
+    "bergson_muon_step_workspace", "bergson_muon_step",
 )
 
 
@@ -149,6 +150,14 @@ class bergson_moment_matrix(ctypes.Structure):
         ("d_in", ctypes.c_int64), ("r", ctypes.c_void_p), ("c", ctypes.c_void_p),
         ("state_kind", ctypes.c_int32), ("reserved", ctypes.c_int32),
     ]
+
+
+class bergson_muon_tensor(ctypes.Structure):
+    _fields_ = (
+        [(n, ctypes.c_void_p) for n in ("param", "grad", "master", "m")]
+        + [("rows", ctypes.c_int64), ("cols", ctypes.c_int64)]
+        + [(n, ctypes.c_float) for n in ("lr_scale", "ortho_scale", "weight_decay")]
+        + [(n, ctypes.c_int32) for n in ("param_dtype", "grad_dtype", "reserved")])
 
 
 _LIB = None
@@ -246,6 +255,9 @@ def lib() -> ctypes.CDLL:
         "bergson_embedding_backward_workspace": (i32, [i64, i64, i64, szp]),
         "bergson_embedding_backward": (i32, [vp, i32, i64, i64, i64, vp, f64, vp, i32, i64, i64, i32, vp,
                                              ctypes.c_size_t, vp]),
+        "bergson_muon_step_workspace": (i32, [ctypes.POINTER(bergson_muon_tensor), i32, i32, szp]),
+        "bergson_muon_step": (i32, [ctypes.POINTER(bergson_muon_tensor), i32, f64, f64, i32,
+                                    ctypes.POINTER(f64), i32, i32, vp, vp, ctypes.c_size_t, vp]),
     }
     for name, (res, args) in sig.items():
         fn = getattr(L, name)
@@ -988,6 +1000,66 @@ def bergson_embedding_backward(dy, ids, scale: float, d_table, add: bool, worksp
     _check(lib().bergson_embedding_backward(
         g, dtype, rows, d, ld, _vector(ids, "ids", _I64, rows), scale, t, _dtype(d_table), V, ld_t,
         1 if add else 0, *_scratch(workspace), _stream(stream)))
+
+
+@dataclasses.dataclass
+class MuonTensor:
+    """One matrix of a Muon step (see bergson_muon_tensor).  Contiguous tensors [rows, cols], which
+    share no memory."""
+    param: object
+    grad: object
+    m: object
+    master: object = None
+    ortho_scale: float = 1.0
+    weight_decay: float = 0.0
+    lr_scale: float = 1.0
+
+    def to_c(self) -> bergson_muon_tensor:
+        if not _DTYPES:
+            _load_dtypes()
+        rows, cols = shape = self.param.shape
+        for what in ("grad", "m", "master"):
+            t = getattr(self, what)
+            if t is not None and t.shape != shape:
+                raise ValueError(f"{what} must have param's shape {tuple(shape)}, got "
+                                 f"{tuple(t.shape)}")
+        n = rows * cols
+        return bergson_muon_tensor(
+            _vector(self.param, "param", self.param.dtype, n),
+            _vector(self.grad, "grad", self.grad.dtype, n), _vector(self.master, "master", _F32, n),
+            _vector(self.m, "m", _F32, n), rows, cols, float(self.lr_scale),
+            float(self.ortho_scale), float(self.weight_decay), _dtype(self.param),
+            _dtype(self.grad), 0)
+
+
+def bergson_muon_tensors(tensors: Sequence) -> "ctypes.Array":
+    """The record array of bergson_muon_step, to be kept from step to step.  It holds
+    addresses: keep the tensors alive and in place."""
+    return _records(bergson_muon_tensor, tensors)
+
+
+def bergson_muon_step_workspace(tensors, products: int) -> int:
+    arr = _records(bergson_muon_tensor, tensors)
+    n = ctypes.c_size_t()
+    _check(lib().bergson_muon_step_workspace(arr, len(arr), int(products), ctypes.byref(n)))
+    return n.value
+
+
+def bergson_muon_step(tensors, lr: float, beta: float, nesterov: bool, coefficients, products: int,
+                      workspace, grad_scale=None, stream=None) -> None:
+    """One Muon step over matrices (MuonTensor list, or bergson_muon_tensors' array); coefficients:
+    (a, b, c) an iteration."""
+    if not _DTYPES:
+        _load_dtypes()
+    arr = _records(bergson_muon_tensor, tensors)
+    flat = [float(x) for abc in coefficients for x in abc]
+    if len(flat) != 3 * len(coefficients):
+        raise ValueError("coefficients must be triples (a, b, c)")
+    scale = (_vector(grad_scale, "grad_scale", _F32, 1) if hasattr(grad_scale, "data_ptr")
+             else _ptr(grad_scale))
+    _check(lib().bergson_muon_step(arr, len(arr), lr, beta, 1 if nesterov else 0,
+                                   (ctypes.c_double * len(flat))(*flat), len(coefficients), products,
+                                   scale, *_scratch(workspace), _stream(stream)))
 
 
 # ------------------------------------------------------------------ helpers

@@ -411,4 +411,9 @@ CUresult encode_tmap_2d(CUtensorMap* tm, CUtensorMapDataType dt, const void* ptr
 CUresult encode_tmap_planes(CUtensorMap* tm, const void* ptr, int64_t inner, int64_t outer,
                             int64_t ld, int box_inner, int box_outer);
 
+// 3-D tiled tensor map over `planes` stacked fp16 matrices [outer, ld], box {64, box_outer, 1},
+// 128-byte swizzle.
+CUresult encode_tmap_stack(CUtensorMap* tm, const void* ptr, int64_t inner, int64_t outer,
+                           int64_t planes, int64_t ld, int box_outer);
+
 }  // namespace bergson

@@ -1,0 +1,977 @@
+// One Muon step over many matrices: momentum, orthogonalisation of the update by
+// Newton-Schulz products, weight update.
+//
+//   m <- beta m + (1 - beta) g,   u = m, or beta m + (1 - beta) g,   X = u / |u|_F,
+//   per iteration (a, b, c):  A = X X^T,  B = b A + c A^2,  X <- a X + B X,
+//   w <- w - lr (ortho_scale X + weight_decay w)
+//
+// for the short side first; a matrix with more rows than columns takes A = X^T X and
+// X <- a X + X B, and none is ever transposed.
+//
+// The products run on the tensor cores with fp16 operands and fp32 sums.  An
+// operand is held as one fp16 plane (products = 1) or as the sum of two, hi = fp16(v), lo = fp16(v - hi)
+// (products = 3: hi hi + hi lo + lo hi; what is left out is below 2^-22), in 1024
+// times its value: entries are 1 / 32768 and smaller at first, of the size of
+// 1 / sqrt(columns) later, and stay clear of fp16's subnormals by that.
+//
+// Matrices of one shape form a group, their planes stacked in the workspace under one
+// tensor map; each product of an iteration is one launch over the tiles of all
+// groups, by persistent CTA pairs with 256-row tiles, longest products first.  An
+// operand is read with its rows as they lie (K-major) or across (MN-major) by the tensor cores'
+// own descriptors.  A and B are symmetric: only tiles on and below the diagonal are
+// computed and stored, and a read above it takes the mirror image across.  The last
+// product's epilogue updates the weights.
+
+#include <algorithm>
+#include <cmath>
+#include <vector>
+
+#include "internal.h"
+#include "train.cuh"
+
+namespace bergson {
+
+namespace {
+
+constexpr float kPlaneScale = 1024.0f;         // of what the planes hold
+constexpr int kMaxGroups = 24;                 // shapes of a batch of matrices
+constexpr int kMaxMats = 300;                  // matrices of a batch
+constexpr int64_t kBatchElements = 1ll << 29;  // where a batch ends: bounds the workspace
+
+int64_t round_to(int64_t n, int64_t to) { return (n + to - 1) / to * to; }
+
+// ------------------------------------------------------------------ momentum
+
+constexpr int kMomentThreads = 256;
+constexpr int64_t kMomentChunk = 8 * kMomentThreads;   // elements of a CTA's turn
+constexpr float kUp = 0x1p50f, kDown = 0x1p-50f;
+
+struct MomentEntry {
+  const void* g;
+  float* m;
+  __half* x;                   // planes
+  int64_t n, plane;            // elements; planes apart
+  int32_t cols, ld;
+  int32_t gt;
+  int32_t vec;                 // g and m take vectors of 8
+};
+
+template <int N>
+struct MomentParams {
+  float beta, alpha;           // alpha = 1 - beta
+  int nesterov;
+  int n;
+  const float* grad_scale;
+  float2* part;                // a CTA's sums of squares
+  int64_t chunk;               // elements a CTA
+  uint32_t begin[N + 1];       // first CTA of each matrix
+  MomentEntry e[N];
+};
+
+template <int N>
+__device__ __forceinline__ int entry_of(const MomentParams<N>& p) {
+  int lo = 0, hi = p.n;
+  while (hi - lo > 1) {
+    const int mid = (lo + hi) / 2;
+    if (p.begin[mid] <= blockIdx.x) lo = mid; else hi = mid;
+  }
+  return lo;
+}
+
+// 8 elements from i on as floats; those from n on are 0.
+__device__ __forceinline__ void load_eight(const void* p, int type, bool vec, int64_t i, int64_t n,
+                                           float (&x)[8]) {
+  if (vec && i + 8 <= n) {
+    if (type == BERGSON_F32) {
+      uint32_t r[8];
+      load32(static_cast<const float*>(p) + i, r);
+#pragma unroll
+      for (int k = 0; k < 8; ++k) x[k] = __uint_as_float(r[k]);
+      return;
+    }
+    const uint4 u = *reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(p) + i);
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      const float2 f = type == BERGSON_BF16 ? unpack2(u, k, static_cast<const __nv_bfloat16*>(nullptr))
+                                            : unpack2(u, k, static_cast<const __half*>(nullptr));
+      x[2 * k] = f.x;
+      x[2 * k + 1] = f.y;
+    }
+    return;
+  }
+#pragma unroll
+  for (int k = 0; k < 8; ++k) x[k] = i + k < n ? load_any(p, type, i + k) : 0.0f;
+}
+
+// m's update and the sums of u's squares, of 2^50 u and of 2^-50 u: one of them holds the norm
+// of any u that fp32 does.
+template <int N>
+__global__ void __launch_bounds__(kMomentThreads) moment_kernel(
+    const __grid_constant__ MomentParams<N> p) {
+  __shared__ float red[2][32];
+  const int k = entry_of(p);
+  const MomentEntry& e = p.e[k];
+  griddep_wait();
+  const float gs = p.grad_scale != nullptr ? *p.grad_scale : 1.0f;
+  const int64_t begin = static_cast<int64_t>(blockIdx.x - p.begin[k]) * p.chunk;
+  const int64_t end = min(begin + p.chunk, e.n);
+  CompensatedSum up, down;
+  for (int64_t i = begin + 8 * threadIdx.x; i < end; i += kMomentChunk) {
+    float g[8], m[8];
+    load_eight(e.g, e.gt, e.vec, i, e.n, g);
+    load_eight(e.m, BERGSON_F32, e.vec, i, e.n, m);
+    float su = 0.0f, sd = 0.0f;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const float a = p.alpha * (g[j] * gs);
+      m[j] = fmaf(p.beta, m[j], a);
+      const float u = p.nesterov ? fmaf(p.beta, m[j], a) : m[j];
+      su = fmaf(u * kUp, u * kUp, su);
+      sd = fmaf(u * kDown, u * kDown, sd);
+    }
+    up.add(su);
+    down.add(sd);
+    if (e.vec && i + 8 <= e.n) {
+      uint32_t r[8];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) r[j] = __float_as_uint(m[j]);
+      store32(e.m + i, r);
+    } else {
+#pragma unroll
+      for (int j = 0; j < 8; ++j)
+        if (i + j < e.n) e.m[i + j] = m[j];
+    }
+  }
+  const float a = block_sum(up.s, red[0]), b = block_sum(down.s, red[1]);
+  if (threadIdx.x == 0) p.part[blockIdx.x] = make_float2(a, b);
+}
+
+// The planes of 1024 u / |u|_F.  A matrix of zeros stays one.
+template <int N, int P>
+__global__ void __launch_bounds__(kMomentThreads) planes_kernel(
+    const __grid_constant__ MomentParams<N> p) {
+  __shared__ float red[2][32];
+  const int k = entry_of(p);
+  const MomentEntry& e = p.e[k];
+  griddep_wait();
+  float a = 0.0f, b = 0.0f;
+  for (uint32_t i = p.begin[k] + threadIdx.x; i < p.begin[k + 1]; i += kMomentThreads) {
+    const float2 s = p.part[i];
+    a += s.x;
+    b += s.y;
+  }
+  a = block_sum(a, red[0]);
+  b = block_sum(b, red[1]);
+  const float norm = a - a == 0.0f ? __fsqrt_rn(a) * kDown : __fsqrt_rn(b) * kUp;
+  const float scale = norm == 0.0f ? 0.0f : kPlaneScale * __frcp_rn(norm);
+  const float gs = p.grad_scale != nullptr ? *p.grad_scale : 1.0f;
+  const int64_t begin = static_cast<int64_t>(blockIdx.x - p.begin[k]) * p.chunk;
+  const int64_t end = min(begin + p.chunk, e.n);
+  for (int64_t i = begin + 8 * threadIdx.x; i < end; i += kMomentChunk) {
+    float u[8];
+    load_eight(e.m, BERGSON_F32, e.vec, i, e.n, u);
+    if (p.nesterov) {
+      float g[8];
+      load_eight(e.g, e.gt, e.vec, i, e.n, g);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) u[j] = fmaf(p.beta, u[j], p.alpha * (g[j] * gs));
+    }
+    __half hi[8], lo[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const float v = u[j] * scale;
+      hi[j] = __float2half_rn(v);
+      lo[j] = __float2half_rn(v - __half2float(hi[j]));
+    }
+    int64_t row = i / e.cols;
+    int col = static_cast<int>(i - row * e.cols);
+    if (e.cols % 8 == 0) {                       // the eight are of one row
+      __half* x = e.x + row * e.ld + col;
+      uint4 w;
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        set_word(w, j, static_cast<uint32_t>(__half_as_ushort(hi[2 * j])) |
+                           static_cast<uint32_t>(__half_as_ushort(hi[2 * j + 1])) << 16);
+      *reinterpret_cast<uint4*>(x) = w;
+      if (P == 2) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+          set_word(w, j, static_cast<uint32_t>(__half_as_ushort(lo[2 * j])) |
+                             static_cast<uint32_t>(__half_as_ushort(lo[2 * j + 1])) << 16);
+        *reinterpret_cast<uint4*>(x + e.plane) = w;
+      }
+      continue;
+    }
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      if (i + j >= e.n) break;
+      __half* x = e.x + row * e.ld + col;
+      *x = hi[j];
+      if (P == 2) x[e.plane] = lo[j];
+      if (++col == e.cols) {
+        col = 0;
+        ++row;
+      }
+    }
+  }
+}
+
+// ------------------------------------------------------------------ products
+
+constexpr int kTileM = 256;                    // rows of a pair's tile, 128 a CTA
+constexpr int kTileN = 256;                    // columns, at most
+constexpr int kTileK = 64;                     // a stage: one 128-byte row of fp16
+constexpr int kBox = 64;                       // rows of a box
+constexpr int kBoxBytes = kBox * 128;
+constexpr int kPlaneBytes = 2 * kBoxBytes;     // of an operand's plane in a stage, per CTA
+constexpr int kThreads = 64 + 256;             // producer, MMA, 8 epilogue warps
+constexpr int kBarBytes = 256;
+constexpr int kTmemCols = 2 * kTileN;          // two accumulators
+constexpr uint64_t kDrainTimeoutNs = 2000000000ull;
+
+template <int P>
+struct ProdCfg {
+  static constexpr int kStageBytes = 2 * P * kPlaneBytes;
+  static constexpr int kStages = P == 2 ? 3 : 6;
+  static constexpr int kSmemBytes = 1024 + kStages * kStageBytes + kBarBytes;
+};
+
+// How an operand [rows, K] of a product lies in memory.
+enum : int { kRowMajor = 0, kAcross = 1, kSymmetric = 2 };
+
+struct ProdGroup {
+  int begin;                   // first tile
+  int per_mat;                 // tiles of a matrix
+  int n_mt, n_nt, tn;          // tiles of tn columns
+  int M, N, K;                 // of D [M, N]
+  int a_kind, b_kind;
+  int lower;                   // only tiles that reach the diagonal or lie below
+  int first_mat;
+  int src_ld, dst_ld;
+  float alpha, beta;           // D' = alpha acc + beta src
+  const __half* src;           // planes, or nullptr
+  __half* dst;                 // planes, or nullptr: the weights
+  int64_t src_plane, dst_plane;
+};
+
+struct WeightEntry {
+  void* p;
+  float* master;
+  float lr_ortho, lr_decay;    // lr lr_scale ortho_scale / 1024, lr lr_scale weight_decay
+  int32_t pt;
+  int32_t vec;                 // rows and pointers take vectors of 16
+};
+
+template <int G, int N>
+struct ProdParams {
+  CUtensorMap a[G], b[G];
+  ProdGroup g[G];
+  WeightEntry w[N];
+  int n;
+  int n_tiles;
+  int* status;
+  uint64_t timeout_ns;
+};
+
+struct Tile {
+  int group, mat, mt, nt;
+};
+
+template <int G, int N>
+__device__ __forceinline__ Tile tile_of(const ProdParams<G, N>& p, int t) {
+  Tile o;
+  o.group = 0;
+  while (o.group + 1 < p.n && p.g[o.group + 1].begin <= t) ++o.group;
+  const ProdGroup& g = p.g[o.group];
+  t -= g.begin;
+  o.mat = t / g.per_mat;
+  t -= o.mat * g.per_mat;
+  if (g.lower) {
+    o.mt = 0;
+    for (;;) {
+      const int n = (min((o.mt + 1) * kTileM, g.N) + g.tn - 1) / g.tn;
+      if (t < n) break;
+      t -= n;
+      ++o.mt;
+    }
+    o.nt = t;
+    return o;
+  }
+  constexpr int kSide = 8;                       // near-square blocks of tiles share panels in L2
+  const int per = kSide * g.n_nt, block = t / per, r = t - block * per;
+  const int rows = min(kSide, g.n_mt - block * kSide);
+  o.mt = block * kSide + r % rows;
+  o.nt = r / rows;
+  return o;
+}
+
+// The tile of a cluster's i-th turn: there and back over the clusters, so that tiles that
+// fall in length come out even.  -1: none.
+__device__ __forceinline__ int tile_index(int i, int cid, int n_cl, int n_tiles) {
+  const int t = i * n_cl + ((i & 1) ? n_cl - 1 - cid : cid);
+  return t < n_tiles ? t : -1;
+}
+
+// Whether the operand rows from row0 on (a tile's first) are read across at column k0.
+__device__ __forceinline__ bool across(int kind, int row0, int k0) {
+  return kind == kAcross || (kind == kSymmetric && (k0 / kTileM) > (row0 / kTileM));
+}
+
+__device__ __forceinline__ void tma_load_box_pair(uint32_t dst, const void* tmap, uint32_t bar,
+                                                  int c0, int c1, int c2, uint64_t policy) {
+  asm volatile(
+      "cp.async.bulk.tensor.3d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes"
+      ".L2::cache_hint [%0], [%1, {%3, %4, %5}], [%2], %6;" ::"r"(dst),
+      "l"(tmap), "r"(bar), "r"(c0), "r"(c1), "r"(c2), "l"(policy)
+      : "memory");
+}
+
+// Descriptor of an operand read across: 64 of its rows side by side in 128 bytes (128-byte
+// swizzle), 8 columns of K every 1024 bytes, the next 64 rows a box further.
+__device__ __forceinline__ uint64_t across_desc(uint32_t saddr) {
+  return static_cast<uint64_t>((saddr & 0x3FFFFu) >> 4) |
+         (static_cast<uint64_t>(kBoxBytes >> 4) << 16) |
+         (static_cast<uint64_t>(1024 >> 4) << 32) | (static_cast<uint64_t>(1) << 46) |
+         (static_cast<uint64_t>(2) << 61);
+}
+
+__device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity, uint64_t tmo,
+                                          const volatile int* abort_flag) {
+  bool ok = true;
+  if ((threadIdx.x & 31) == 0) ok = mbar_wait_inline(bar, parity, tmo, abort_flag);
+  return __shfl_sync(0xffffffffu, ok ? 1 : 0, 0) != 0;
+}
+
+// 16 fp16 elements from 32-byte boundaries.
+__device__ __forceinline__ void add_plane(const __half* p, float (&x)[16]) {
+  uint32_t r[8];
+  load32(p, r);
+#pragma unroll
+  for (int k = 0; k < 8; ++k) {
+    const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&r[k]));
+    x[2 * k] += f.x;
+    x[2 * k + 1] += f.y;
+  }
+}
+
+// 16 columns of a row: D' to its planes or into the weights.
+template <int P>
+__device__ __forceinline__ void finish(const ProdGroup& g, const WeightEntry& w, int mat, int row,
+                                       int col, const float* acc) {
+  float v[16];
+#pragma unroll
+  for (int k = 0; k < 16; ++k) v[k] = 0.0f;
+  if (g.src != nullptr) {
+    const __half* s = g.src + static_cast<int64_t>(mat) * P * g.src_plane +
+                      static_cast<int64_t>(row) * g.src_ld + col;
+    add_plane(s, v);
+    if (P == 2) add_plane(s + g.src_plane, v);
+  }
+#pragma unroll
+  for (int k = 0; k < 16; ++k) v[k] = fmaf(g.alpha, acc[k], g.beta * v[k]);
+  if (g.dst != nullptr) {
+    __half* d = g.dst + static_cast<int64_t>(mat) * P * g.dst_plane +
+                static_cast<int64_t>(row) * g.dst_ld + col;
+    uint32_t hi[8], lo[8];
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      const __half2 h = __floats2half2_rn(v[2 * k], v[2 * k + 1]);
+      const float2 f = __half22float2(h);
+      const __half2 l = __floats2half2_rn(v[2 * k] - f.x, v[2 * k + 1] - f.y);
+      hi[k] = *reinterpret_cast<const uint32_t*>(&h);
+      lo[k] = *reinterpret_cast<const uint32_t*>(&l);
+    }
+    store32(d, hi);
+    if (P == 2) store32(d + g.dst_plane, lo);
+    return;
+  }
+  const int64_t at = static_cast<int64_t>(row) * g.N + col;
+  if (w.vec) {
+    float x[16];
+    if (w.master != nullptr || w.pt == BERGSON_F32) {
+      float* f = w.master != nullptr ? w.master : static_cast<float*>(w.p);
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        uint32_t r[8];
+        load32(f + at + 8 * h, r);
+#pragma unroll
+        for (int k = 0; k < 8; ++k) x[8 * h + k] = __uint_as_float(r[k]);
+      }
+    } else {
+      uint32_t r[8];
+      load32(static_cast<uint16_t*>(w.p) + at, r);
+#pragma unroll
+      for (int k = 0; k < 8; ++k) {
+        const uint4 u = make_uint4(r[k], 0, 0, 0);
+        const float2 f = w.pt == BERGSON_BF16 ? unpack2(u, 0, static_cast<__nv_bfloat16*>(nullptr))
+                                              : unpack2(u, 0, static_cast<__half*>(nullptr));
+        x[2 * k] = f.x;
+        x[2 * k + 1] = f.y;
+      }
+    }
+#pragma unroll
+    for (int k = 0; k < 16; ++k) x[k] = fmaf(-w.lr_ortho, v[k], fmaf(-w.lr_decay, x[k], x[k]));
+    if (w.master != nullptr || w.pt == BERGSON_F32) {
+      float* f = w.master != nullptr ? w.master : static_cast<float*>(w.p);
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        uint32_t r[8];
+#pragma unroll
+        for (int k = 0; k < 8; ++k) r[k] = __float_as_uint(x[8 * h + k]);
+        store32(f + at + 8 * h, r);
+        if (w.master != nullptr && w.pt == BERGSON_F32)
+          store32(static_cast<float*>(w.p) + at + 8 * h, r);
+      }
+    }
+    if (w.pt != BERGSON_F32) {
+      uint32_t r[8];
+#pragma unroll
+      for (int k = 0; k < 8; ++k) {
+        uint4 u = make_uint4(0, 0, 0, 0);
+        const float2 f = make_float2(x[2 * k], x[2 * k + 1]);
+        if (w.pt == BERGSON_BF16) pack2(u, 0, f, static_cast<__nv_bfloat16*>(nullptr));
+        else pack2(u, 0, f, static_cast<__half*>(nullptr));
+        r[k] = u.x;
+      }
+      store32(static_cast<uint16_t*>(w.p) + at, r);
+    }
+    return;
+  }
+#pragma unroll
+  for (int k = 0; k < 16; ++k) {
+    if (col + k >= g.N) return;
+    float x = w.master != nullptr ? w.master[at + k] : load_any(w.p, w.pt, at + k);
+    x = fmaf(-w.lr_ortho, v[k], fmaf(-w.lr_decay, x, x));
+    if (w.master != nullptr) w.master[at + k] = x;
+    if (w.pt == BERGSON_BF16) static_cast<__nv_bfloat16*>(w.p)[at + k] = __float2bfloat16_rn(x);
+    else if (w.pt == BERGSON_F16) static_cast<__half*>(w.p)[at + k] = __float2half_rn(x);
+    else static_cast<float*>(w.p)[at + k] = x;
+  }
+}
+
+// D[i, j] = alpha <a_i, b_j> + beta src[i, j] over persistent CTA pairs, synchronised
+// as the other pair kernels: the odd CTA's loads complete on the even CTA's `full`, the
+// even CTA's MMA thread frees a stage in both CTAs and hands accumulators to both
+// epilogues by multicast commits, and every epilogue warp of both CTAs releases an
+// accumulator on the even CTA's `tempty`.  Every wait is bounded.
+//
+// The tensor cores' fp32 sums round toward zero.  With two planes, an accumulation chain is
+// one stage (12 MMAs, its smallest terms first) and the epilogue adds the chains in registers while the
+// next one runs; with one plane the operands' own rounding is 2^-12 and a tile is one chain.
+template <int P, int G, int N>
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
+    product_kernel(const __grid_constant__ ProdParams<G, N> p) {
+  using C = ProdCfg<P>;
+  extern __shared__ uint8_t smem_raw[];
+  uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) &
+                                             ~static_cast<uintptr_t>(1023));
+  const uint32_t sbase = smem_u32(smem);
+  uint64_t* full = reinterpret_cast<uint64_t*>(smem + C::kStages * C::kStageBytes);
+  uint64_t* empty = full + C::kStages;
+  uint64_t* tfull = empty + C::kStages;
+  uint64_t* tempty = tfull + 2;
+  uint64_t* drain = tempty + 2;
+  uint32_t* s_tmem = reinterpret_cast<uint32_t*>(drain + 1);
+  volatile int* s_abort = reinterpret_cast<volatile int*>(s_tmem + 1);
+
+  const int rank = static_cast<int>(cluster_ctarank());
+  const int cid = blockIdx.x >> 1;
+  const int n_cl = gridDim.x >> 1;
+  const int warp = threadIdx.x >> 5;
+  const int lane = threadIdx.x & 31;
+  griddep_launch_dependents();   // the next grid sets itself up and waits for this one to end
+  if (threadIdx.x == 0) {
+    for (int s = 0; s < C::kStages; ++s) {
+      mbar_init(smem_u32(&full[s]), 1);
+      mbar_init(smem_u32(&empty[s]), 1);
+    }
+    for (int i = 0; i < 2; ++i) {
+      mbar_init(smem_u32(&tfull[i]), 1);
+      mbar_init(smem_u32(&tempty[i]), 16);           // 8 epilogue warps of each CTA
+    }
+    mbar_init(smem_u32(drain), 1);
+    *s_abort = 0;
+    fence_barrier_init();
+  }
+  if (warp == 1) {
+    tmem_alloc_pair(smem_u32(s_tmem), kTmemCols);
+    tmem_relinquish_pair();
+  }
+  griddep_wait();                // the operands come from earlier grids
+  tc_fence_before();
+  cluster_sync();
+  tc_fence_after();
+  const uint32_t tmem = *s_tmem;
+  const uint64_t tmo = p.timeout_ns;
+
+  if (warp == 0) {
+    // ------------------------------------------------------------ producer
+    if (lane == 0) {
+      const uint64_t pol = policy_evict_normal();
+      int stage = 0;
+      uint32_t ph = 0;
+      uint32_t issued = 0, issued_par = 0;
+      bool ok = true;
+      for (int i = 0, t; ok && (t = tile_index(i, cid, n_cl, p.n_tiles)) >= 0; ++i) {
+        const Tile o = tile_of(p, t);
+        const ProdGroup& g = p.g[o.group];
+        const void* ta = &p.a[o.group];
+        const void* tb = &p.b[o.group];
+        const int z = o.mat * P;
+        const int boxes_b = (g.tn / 2 + kBox - 1) / kBox;
+        const int a0 = o.mt * kTileM, b0 = o.nt * g.tn;
+        const int ar = a0 + rank * (kTileM / 2), br = b0 + rank * (g.tn / 2);
+        for (int k0 = 0; k0 < g.K; k0 += kTileK) {
+          if (!mbar_wait(smem_u32(&empty[stage]), ph ^ 1, tmo, s_abort)) { ok = false; break; }
+          const uint32_t fb_local = smem_u32(&full[stage]);
+          const uint32_t fb = mapa_shared(fb_local, 0);
+          if (rank == 0) mbar_arrive_expect_tx(fb_local, 2 * P * (2 + boxes_b) * kBoxBytes);
+          const uint32_t dst = sbase + stage * C::kStageBytes;
+          const bool xa = across(g.a_kind, a0, k0), xb = across(g.b_kind, b0, k0);
+#pragma unroll
+          for (int q = 0; q < P; ++q) {
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+              const int r = ar + h * kBox;
+              tma_load_box_pair(dst + q * kPlaneBytes + h * kBoxBytes, ta, fb, xa ? r : k0,
+                                xa ? k0 : r, z + q, pol);
+            }
+            for (int h = 0; h < boxes_b; ++h) {
+              const int r = br + h * kBox;
+              tma_load_box_pair(dst + (P + q) * kPlaneBytes + h * kBoxBytes, tb, fb, xb ? r : k0,
+                                xb ? k0 : r, z + q, pol);
+            }
+          }
+          issued |= 1u << stage;
+          issued_par = (issued_par & ~(1u << stage)) | (ph << stage);
+          if (++stage == C::kStages) { stage = 0; ph ^= 1; }
+        }
+      }
+      if (!ok) {
+        raise_device_error(p.status, s_abort, kStatusTimeout);
+        if (rank == 0) {
+          for (int s = 0; s < C::kStages; ++s)
+            if (issued >> s & 1)
+              mbar_wait(smem_u32(&full[s]), (issued_par >> s) & 1, kDrainTimeoutNs, nullptr);
+        } else {
+          const uint64_t t0 = global_timer_ns();      // its loads complete on the other CTA's barrier
+          while (global_timer_ns() - t0 < 1000000ull) {
+          }
+        }
+      }
+    }
+    __syncwarp();
+  } else if (warp == 1) {
+    // ------------------------------------------------------------ MMA issuer (even CTA)
+    if (rank == 0 && lane == 0) {
+      int stage = 0;
+      uint32_t ph = 0;
+      int ab = 0;
+      uint32_t aph = 0;
+      bool ok = true;
+      for (int i = 0, t; ok && (t = tile_index(i, cid, n_cl, p.n_tiles)) >= 0; ++i) {
+        const Tile o = tile_of(p, t);
+        const ProdGroup& g = p.g[o.group];
+        const int a0 = o.mt * kTileM, b0 = o.nt * g.tn;
+        const uint32_t base_desc = make_idesc_f16(kTileM, g.tn, false);
+        bool fresh = true;                           // the accumulator holds nothing yet
+        for (int k0 = 0; k0 < g.K; k0 += kTileK) {
+          if (!mbar_wait(smem_u32(&full[stage]), ph, tmo, s_abort)) { ok = false; break; }
+          if (fresh && !mbar_wait(smem_u32(&tempty[ab]), aph ^ 1, tmo, s_abort)) { ok = false; break; }
+          tc_fence_after();
+          const bool xa = across(g.a_kind, a0, k0), xb = across(g.b_kind, b0, k0);
+          const uint32_t sa = sbase + stage * C::kStageBytes, sb = sa + P * kPlaneBytes;
+          const uint64_t da = xa ? across_desc(sa) : sw128_desc(sa);
+          const uint64_t db = xb ? across_desc(sb) : sw128_desc(sb);
+          // 16 columns of K: 32 bytes of a row, or 16 rows of 128 bytes
+          const uint32_t step_a = xa ? 128 : 2, step_b = xb ? 128 : 2;
+          const uint32_t idesc = base_desc | (xa ? 1u << 15 : 0u) | (xb ? 1u << 16 : 0u);
+          const uint32_t d = tmem + ab * kTileN;
+          constexpr int kTerms = P == 2 ? 3 : 1;
+          constexpr uint32_t kPlane = kPlaneBytes / 16;
+#pragma unroll
+          for (int q = 0; q < kTerms; ++q) {         // lo hi, hi lo, hi hi
+            const uint64_t at = da + (P == 2 && q == 0 ? kPlane : 0);
+            const uint64_t bt = db + (P == 2 && q == 1 ? kPlane : 0);
+#pragma unroll
+            for (int kk = 0; kk < kTileK / 16; ++kk)
+              umma_f16_pair(d, at + kk * step_a, bt + kk * step_b, idesc,
+                            !fresh || q != 0 || kk != 0);
+          }
+          umma_commit_pair(smem_u32(&empty[stage]), 0x3);
+          fresh = P == 2 || k0 + kTileK >= g.K;
+          if (fresh) {
+            umma_commit_pair(smem_u32(&tfull[ab]), 0x3);
+            if (++ab == 2) { ab = 0; aph ^= 1; }
+          }
+          if (++stage == C::kStages) { stage = 0; ph ^= 1; }
+        }
+      }
+      if (!ok) raise_device_error(p.status, s_abort, kStatusTimeout);
+      umma_commit_pair(smem_u32(drain), 0x1);
+      mbar_wait(smem_u32(drain), 0, kDrainTimeoutNs, nullptr);
+    }
+    __syncwarp();
+  } else {
+    // ------------------------------------------------------------ epilogue
+    // Thread = a row of this CTA's half (TMEM lane) and half of the tile's columns.
+    const int quarter = warp & 3;
+    const int half = (warp - 2) >> 2;
+    int ab = 0;
+    uint32_t aph = 0;
+    bool aborted = false;
+    for (int i = 0, t; !aborted && (t = tile_index(i, cid, n_cl, p.n_tiles)) >= 0; ++i) {
+      const Tile o = tile_of(p, t);
+      const ProdGroup& g = p.g[o.group];
+      const WeightEntry& w = p.w[min(g.first_mat + o.mat, N - 1)];
+      const int cols = g.tn / 2;
+      const int row = o.mt * kTileM + rank * (kTileM / 2) + 32 * quarter + lane;
+      const int col0 = o.nt * g.tn + half * cols;
+      const int chains = P == 2 ? (g.K + kTileK - 1) / kTileK : 1;
+      constexpr int kAcc = P == 2 ? kTileN / 2 : 16;
+      float acc[kAcc];
+      if constexpr (P == 2) {
+#pragma unroll
+        for (int j = 0; j < kAcc; ++j) acc[j] = 0.0f;
+      }
+      for (int ch = 0; ch < chains; ++ch) {
+        if (!warp_wait(smem_u32(&tfull[ab]), aph, tmo, s_abort)) {
+          raise_device_error(p.status, s_abort, kStatusTimeout);
+          aborted = true;
+          break;
+        }
+        tc_fence_after();
+        const uint32_t tb = tmem + (static_cast<uint32_t>(32 * quarter) << 16) + ab * kTileN +
+                            half * cols;
+        if constexpr (P == 2) {
+#pragma unroll
+          for (int c = 0; c < kAcc; c += 16) {
+            if (c < cols) {
+              float v[16];
+              tmem_ld16(tb + c, v);
+#pragma unroll
+              for (int j = 0; j < 16; ++j) acc[c + j] += v[j];
+            }
+          }
+        } else {
+#pragma unroll 1
+          for (int c = 0; c < cols; c += 16) {
+            tmem_ld16(tb + c, acc);
+            if (row < g.M && col0 + c < g.N) finish<P>(g, w, o.mat, row, col0 + c, acc);
+            __syncwarp();
+          }
+        }
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive_remote(mapa_shared(smem_u32(&tempty[ab]), 0));
+        if (++ab == 2) { ab = 0; aph ^= 1; }
+      }
+      if (aborted) break;
+      if constexpr (P == 2) {
+#pragma unroll
+        for (int c = 0; c < kAcc; c += 16)
+          if (c < cols && row < g.M && col0 + c < g.N)
+            finish<P>(g, w, o.mat, row, col0 + c, acc + c);
+        __syncwarp();
+      }
+    }
+  }
+
+  tc_fence_before();
+  cluster_sync();              // no MMA, commit or remote arrival is still in flight
+  if (warp == 1) {
+    tc_fence_after();
+    tmem_dealloc_pair(tmem, kTmemCols);
+  }
+}
+
+// ------------------------------------------------------------------ host
+
+struct Shape {
+  int64_t rows, cols;
+  std::vector<int> mats;       // indices into the caller's array
+};
+
+// The tensors by their shape, the longest products first, cut into batches.
+struct Batch {
+  std::vector<Shape> shapes;
+  int mats = 0;
+  int64_t elements = 0;
+};
+
+std::vector<Batch> batches_of(const bergson_muon_tensor* t, int n) {
+  std::vector<Shape> shapes;
+  for (int i = 0; i < n; ++i) {
+    size_t k = 0;
+    while (k < shapes.size() && (shapes[k].rows != t[i].rows || shapes[k].cols != t[i].cols)) ++k;
+    if (k == shapes.size()) shapes.push_back({t[i].rows, t[i].cols, {}});
+    shapes[k].mats.push_back(i);
+  }
+  std::stable_sort(shapes.begin(), shapes.end(), [](const Shape& a, const Shape& b) {
+    return std::max(a.rows, a.cols) > std::max(b.rows, b.cols);
+  });
+  std::vector<Batch> out;
+  for (const Shape& s : shapes) {
+    const int64_t each = s.rows * s.cols;
+    bool open = false;                           // the shape is the last of the last batch
+    for (int i : s.mats) {
+      if (out.empty() || out.back().mats == kMaxMats ||
+          (out.back().mats > 0 && out.back().elements + each > kBatchElements) ||
+          (!open && out.back().shapes.size() == kMaxGroups)) {
+        out.emplace_back();
+        open = false;
+      }
+      Batch& b = out.back();
+      if (!open) b.shapes.push_back({s.rows, s.cols, {}});
+      open = true;
+      b.shapes.back().mats.push_back(i);
+      ++b.mats;
+      b.elements += each;
+    }
+  }
+  return out;
+}
+
+int64_t leading(int64_t cols) { return round_to(cols, 16); }
+
+// Where a shape's planes stand in the workspace: X twice, A and B.
+struct Planes {
+  size_t x[2], a, b;
+  int64_t x_ld, x_plane, s_ld, s_plane;
+};
+
+struct BatchLayout {
+  std::vector<Planes> shapes;
+  size_t part = 0, total = 0;
+  int64_t chunk = 0, ctas = 0;
+};
+
+BatchLayout layout_of(const Batch& b, int P) {
+  BatchLayout l;
+  size_t at = 0;
+  const auto take = [&](int64_t bytes) {
+    const size_t here = at;
+    at += static_cast<size_t>(round_to(bytes, 256));
+    return here;
+  };
+  l.chunk = std::max(2 * kMomentChunk,
+                     round_to(ceil_div(b.elements, kPlanCTAs * 16), kMomentChunk));
+  for (const Shape& s : b.shapes)
+    l.ctas += ceil_div(s.rows * s.cols, l.chunk) * static_cast<int64_t>(s.mats.size());
+  l.part = take(l.ctas * static_cast<int64_t>(sizeof(float2)));
+  for (const Shape& s : b.shapes) {
+    Planes p;
+    const int64_t m = std::min(s.rows, s.cols), n = static_cast<int64_t>(s.mats.size()) * P * 2;
+    p.x_ld = leading(s.cols);
+    p.x_plane = s.rows * p.x_ld;
+    p.s_ld = leading(m);
+    p.s_plane = m * p.s_ld;
+    p.x[0] = take(n * p.x_plane);
+    p.x[1] = take(n * p.x_plane);
+    p.a = take(n * p.s_plane);
+    p.b = take(n * p.s_plane);
+    l.shapes.push_back(p);
+  }
+  l.total = at;
+  return l;
+}
+
+// Columns of a tile: what wastes least of the last one.  A tile pays some 40 columns' time
+// beside its own.
+int tile_columns(int64_t n) {
+  int best = kTileN;
+  int64_t cost = INT64_MAX;
+  for (int tn = kTileN; tn >= 128; tn -= 32) {
+    const int64_t c = ceil_div(n, tn) * (tn + 40);
+    if (c < cost) {
+      cost = c;
+      best = tn;
+    }
+  }
+  return best;
+}
+
+template <int N>
+cudaError_t run_moments(const bergson_muon_tensor* t, const Batch& b, const BatchLayout& l,
+                        const MuonScalars& a, uint8_t* ws, cudaStream_t s) {
+  const int P = a.products == 3 ? 2 : 1;
+  MomentParams<N> p;
+  p.beta = static_cast<float>(a.beta);
+  p.alpha = static_cast<float>(1.0 - a.beta);
+  p.nesterov = a.nesterov ? 1 : 0;
+  p.n = b.mats;
+  p.grad_scale = a.grad_scale;
+  p.part = reinterpret_cast<float2*>(ws + l.part);
+  p.chunk = l.chunk;
+  p.begin[0] = 0;
+  int k = 0;
+  for (size_t g = 0; g < b.shapes.size(); ++g) {
+    const Shape& sh = b.shapes[g];
+    const Planes& pl = l.shapes[g];
+    for (size_t z = 0; z < sh.mats.size(); ++z, ++k) {
+      const bergson_muon_tensor& x = t[sh.mats[z]];
+      MomentEntry& e = p.e[k];
+      e.g = x.grad;
+      e.m = x.m;
+      e.x = reinterpret_cast<__half*>(ws + pl.x[0]) + static_cast<int64_t>(z) * P * pl.x_plane;
+      e.n = sh.rows * sh.cols;
+      e.plane = pl.x_plane;
+      e.cols = static_cast<int32_t>(sh.cols);
+      e.ld = static_cast<int32_t>(pl.x_ld);
+      e.gt = x.grad_dtype;
+      e.vec = on16(x.grad, 0, 1) && reinterpret_cast<uintptr_t>(x.m) % 32 == 0 &&
+              (x.grad_dtype != BERGSON_F32 || reinterpret_cast<uintptr_t>(x.grad) % 32 == 0);
+      p.begin[k + 1] = p.begin[k] + static_cast<uint32_t>(ceil_div(e.n, l.chunk));
+    }
+  }
+  const dim3 grid(p.begin[k]), block(kMomentThreads);
+  cudaError_t e = launch_dependent(moment_kernel<N>, grid, block, 0, s, p);
+  if (e != cudaSuccess) return e;
+  return P == 2 ? launch_dependent(planes_kernel<N, 2>, grid, block, 0, s, p)
+                : launch_dependent(planes_kernel<N, 1>, grid, block, 0, s, p);
+}
+
+struct Maps {
+  CUtensorMap x[2], a, b;
+};
+
+template <int P, int G, int N>
+cudaError_t run_products(const bergson_muon_tensor* t, const Batch& b, const BatchLayout& l,
+                         const MuonScalars& a, uint8_t* ws, int* status, int sms, cudaStream_t s) {
+  std::vector<Maps> maps(b.shapes.size());
+  ProdParams<G, N> p = {};
+  p.n = static_cast<int>(b.shapes.size());
+  p.status = status;
+  p.timeout_ns = kWaitTimeoutNs;
+  int first = 0;
+  for (int k = 0; k < p.n; ++k) {
+    const Shape& sh = b.shapes[k];
+    const Planes& pl = l.shapes[k];
+    const int64_t m = std::min(sh.rows, sh.cols), n = static_cast<int64_t>(sh.mats.size()) * P;
+    Maps& mp = maps[k];
+    if (encode_tmap_stack(&mp.x[0], ws + pl.x[0], sh.cols, sh.rows, n, pl.x_ld, kBox) != CUDA_SUCCESS ||
+        encode_tmap_stack(&mp.x[1], ws + pl.x[1], sh.cols, sh.rows, n, pl.x_ld, kBox) != CUDA_SUCCESS ||
+        encode_tmap_stack(&mp.a, ws + pl.a, m, m, n, pl.s_ld, kBox) != CUDA_SUCCESS ||
+        encode_tmap_stack(&mp.b, ws + pl.b, m, m, n, pl.s_ld, kBox) != CUDA_SUCCESS)
+      return cudaErrorInvalidValue;
+    p.g[k].first_mat = first;
+    for (int i : sh.mats) {
+      const bergson_muon_tensor& x = t[i];
+      WeightEntry& w = p.w[first++];
+      w.p = x.param;
+      w.master = x.master;
+      const double lr = a.lr * x.lr_scale;
+      w.lr_ortho = static_cast<float>(lr * x.ortho_scale / kPlaneScale);
+      w.lr_decay = static_cast<float>(lr * x.weight_decay);
+      w.pt = x.param_dtype;
+      w.vec = sh.cols % 16 == 0 && reinterpret_cast<uintptr_t>(x.param) % 32 == 0 &&
+              reinterpret_cast<uintptr_t>(x.master) % 32 == 0;
+    }
+  }
+  const auto kernel = product_kernel<P, G, N>;
+  static PerDeviceOnce attr;
+  cudaError_t e = smem_attr_once(attr, kernel, ProdCfg<P>::kSmemBytes);
+  if (e != cudaSuccess) return e;
+  const auto run = [&]() {
+    int64_t tiles = 0;
+    for (int k = 0; k < p.n; ++k) {
+      ProdGroup& g = p.g[k];
+      g.tn = tile_columns(g.N);
+      g.n_mt = static_cast<int>(ceil_div(g.M, kTileM));
+      g.n_nt = static_cast<int>(ceil_div(g.N, g.tn));
+      g.per_mat = 0;
+      for (int mt = 0; mt < g.n_mt; ++mt)
+        g.per_mat += g.lower ? static_cast<int>(ceil_div(std::min((mt + 1) * kTileM, g.N), g.tn))
+                             : g.n_nt;
+      g.begin = static_cast<int>(tiles);
+      tiles += static_cast<int64_t>(g.per_mat) * static_cast<int64_t>(b.shapes[k].mats.size());
+    }
+    p.n_tiles = static_cast<int>(tiles);
+    const int64_t clusters = std::max<int64_t>(1, std::min<int64_t>(sms / 2, tiles));
+    return launch_dependent(kernel, dim3(static_cast<unsigned>(2 * clusters)), dim3(kThreads),
+                            ProdCfg<P>::kSmemBytes, s, p);
+  };
+  for (int it = 0; it < a.iterations; ++it) {
+    const double* c = a.coefficients + 3 * it;
+    const int cur = it & 1;
+    const bool last = it == a.iterations - 1;
+    for (int part = 0; part < 3; ++part) {       // A = X X^T, B = b A + c A^2, X' = a X + B X
+      for (int k = 0; k < p.n; ++k) {
+        const Shape& sh = b.shapes[k];
+        const Planes& pl = l.shapes[k];
+        const bool tall = sh.rows > sh.cols;
+        const int m = static_cast<int>(std::min(sh.rows, sh.cols));
+        ProdGroup& g = p.g[k];
+        g.M = part == 2 ? static_cast<int>(sh.rows) : m;
+        g.N = part == 2 ? static_cast<int>(sh.cols) : m;
+        g.K = part == 0 ? static_cast<int>(std::max(sh.rows, sh.cols)) : m;
+        g.lower = part < 2 ? 1 : 0;
+        const auto at = [&](size_t off) { return reinterpret_cast<__half*>(ws + off); };
+        if (part == 0) {
+          p.a[k] = p.b[k] = maps[k].x[cur];
+          g.a_kind = g.b_kind = tall ? kAcross : kRowMajor;
+          g.src = nullptr;
+          g.dst = at(pl.a);
+          g.alpha = 1.0f / kPlaneScale;
+          g.beta = 0.0f;
+        } else if (part == 1) {
+          p.a[k] = p.b[k] = maps[k].a;
+          g.a_kind = g.b_kind = kSymmetric;
+          g.src = at(pl.a);
+          g.dst = at(pl.b);
+          g.alpha = static_cast<float>(c[2] / kPlaneScale);
+          g.beta = static_cast<float>(c[1]);
+        } else {
+          p.a[k] = tall ? maps[k].x[cur] : maps[k].b;
+          p.b[k] = tall ? maps[k].b : maps[k].x[cur];
+          g.a_kind = tall ? kRowMajor : kSymmetric;
+          g.b_kind = tall ? kSymmetric : kAcross;
+          g.src = at(pl.x[cur]);
+          g.dst = last ? nullptr : at(pl.x[cur ^ 1]);
+          g.alpha = 1.0f / kPlaneScale;
+          g.beta = static_cast<float>(c[0]);
+        }
+        g.src_ld = static_cast<int>(part == 2 ? pl.x_ld : pl.s_ld);
+        g.src_plane = part == 2 ? pl.x_plane : pl.s_plane;
+        g.dst_ld = g.src_ld;
+        g.dst_plane = g.src_plane;
+      }
+      e = run();
+      if (e != cudaSuccess) return e;
+    }
+  }
+  return cudaSuccess;
+}
+
+constexpr int kFewGroups = 4, kFewMats = 48;
+
+}  // namespace
+
+size_t muon_workspace(const bergson_muon_tensor* t, int n, int products) {
+  size_t most = 256;
+  for (const Batch& b : batches_of(t, n))
+    most = std::max(most, layout_of(b, products == 3 ? 2 : 1).total);
+  return most;
+}
+
+cudaError_t launch_muon(const bergson_muon_tensor* t, int n, const MuonScalars& a, void* ws,
+                        int* status, int sms, cudaStream_t s) {
+  uint8_t* w = static_cast<uint8_t*>(ws);
+  for (const Batch& b : batches_of(t, n)) {
+    const BatchLayout l = layout_of(b, a.products == 3 ? 2 : 1);
+    const bool few = b.mats <= kFewMats && b.shapes.size() <= kFewGroups;
+    cudaError_t e = few ? run_moments<kFewMats>(t, b, l, a, w, s)
+                        : run_moments<kMaxMats>(t, b, l, a, w, s);
+    if (e != cudaSuccess) return e;
+    if (a.products == 3)
+      e = few ? run_products<2, kFewGroups, kFewMats>(t, b, l, a, w, status, sms, s)
+              : run_products<2, kMaxGroups, kMaxMats>(t, b, l, a, w, status, sms, s);
+    else
+      e = few ? run_products<1, kFewGroups, kFewMats>(t, b, l, a, w, status, sms, s)
+              : run_products<1, kMaxGroups, kMaxMats>(t, b, l, a, w, status, sms, s);
+    if (e != cudaSuccess) return e;
+  }
+  return cudaSuccess;
+}
+
+}  // namespace bergson

@@ -1,6 +1,6 @@
 // Arguments and launchers of the training-side operators (token
 // log-probabilities, losses, AdamW, factored moments, norms,
-// embedding).
+// embedding, Muon).
 #pragma once
 
 #include <cuda_runtime.h>
@@ -122,5 +122,17 @@ struct EmbeddingGradArgs {
 };
 size_t embedding_backward_workspace(int64_t rows, int64_t V, int64_t d);
 cudaError_t launch_embedding_backward(const EmbeddingGradArgs& a, void* ws, cudaStream_t s);
+
+struct MuonScalars {
+  double lr, beta;
+  bool nesterov;
+  const double* coefficients;  // [iterations, 3]
+  int iterations;
+  int products;                // 1 or 3
+  const float* grad_scale;     // device, or nullptr
+};
+size_t muon_workspace(const bergson_muon_tensor* t, int n, int products);
+cudaError_t launch_muon(const bergson_muon_tensor* t, int n, const MuonScalars& a, void* ws,
+                        int* status, int sms, cudaStream_t s);
 
 }  // namespace bergson

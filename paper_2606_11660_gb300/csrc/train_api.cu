@@ -1,7 +1,9 @@
 // Host side of the training-side operators' entry points: argument validation
 // and error mapping.
 
+#include <algorithm>
 #include <cmath>
+#include <new>
 
 #include "bergson.h"
 #include "internal.h"
@@ -118,6 +120,77 @@ int check_embedding(int64_t rows, int64_t V, int64_t d) {
   if (d < 1) return fail(BERGSON_EINVAL, "d must be >= 1");
   if (d > (1ll << 24)) return fail(BERGSON_EUNSUPPORTED, "d must be <= 2^24");
   if (rows * ((d + 255) / 256) > INT32_MAX) return fail(BERGSON_EUNSUPPORTED, "rows*d too large");
+  return BERGSON_OK;
+}
+
+int check_muon_matrices(const bergson_muon_tensor* tensors, int n_tensors, int products,
+                        bool pointers) {
+  if (n_tensors < 0) return fail(BERGSON_EINVAL, "n_tensors must be >= 0");
+  if (n_tensors > 0 && tensors == nullptr) return fail(BERGSON_EINVAL, "tensors is NULL");
+  if (products != 1 && products != 3) return fail(BERGSON_EINVAL, "products must be 1 or 3");
+  for (int i = 0; i < n_tensors; ++i) {
+    const bergson_muon_tensor& t = tensors[i];
+    const size_t ps = dtype_size(t.param_dtype), gs = dtype_size(t.grad_dtype);
+    if (ps == 0 || gs == 0)
+      return fail(BERGSON_EINVAL, "tensor %d: unknown dtype (param %d, grad %d)", i, t.param_dtype,
+                  t.grad_dtype);
+    if (t.reserved != 0) return fail(BERGSON_EINVAL, "tensor %d: reserved must be 0", i);
+    if (t.rows < 1 || t.cols < 1)
+      return fail(BERGSON_EINVAL, "tensor %d: rows and cols must be >= 1", i);
+    if (std::max(t.rows, t.cols) > (1 << 20) || std::min(t.rows, t.cols) > (1 << 16))
+      return fail(BERGSON_EUNSUPPORTED, "tensor %d: too large", i);
+    if (!std::isfinite(t.lr_scale) || !std::isfinite(t.ortho_scale) ||
+        !std::isfinite(t.weight_decay))
+      return fail(BERGSON_EINVAL, "tensor %d: lr_scale, ortho_scale and weight_decay must be finite",
+                  i);
+    if (!pointers) continue;
+    if (t.param == nullptr || t.grad == nullptr || t.m == nullptr)
+      return fail(BERGSON_EINVAL, "tensor %d: a pointer is NULL", i);
+    if (!aligned(t.param, ps) || !aligned(t.grad, gs) || !aligned(t.master, 4) || !aligned(t.m, 4))
+      return fail(BERGSON_EALIGN, "tensor %d: a pointer is not aligned to its elements", i);
+  }
+  return BERGSON_OK;
+}
+
+// The largest |p(y)| x^odd of polynomials in y = x^2 on [0, top]: at the ends, or where the
+// derivative is 0.  odd: of a x + b x^3 + c x^5, else of b y + c y^2.
+double largest(double a, double b, double c, bool odd, double top) {
+  const auto f = [&](double y) {
+    return odd ? std::sqrt(y) * std::fabs(a + y * (b + y * c)) : std::fabs(y * (b + y * c));
+  };
+  double most = f(top * top);
+  const auto at = [&](double y) {
+    if (y > 0.0 && y < top * top) most = std::max(most, f(y));
+  };
+  if (!odd) {
+    if (c != 0.0) at(-b / (2.0 * c));
+    return most;
+  }
+  const double d = 9.0 * b * b - 20.0 * a * c;             // a + 3 b y + 5 c y^2 = 0
+  if (c == 0.0) {
+    if (b != 0.0) at(-a / (3.0 * b));
+  } else if (d >= 0.0) {
+    at((-3.0 * b + std::sqrt(d)) / (10.0 * c));
+    at((-3.0 * b - std::sqrt(d)) / (10.0 * c));
+  }
+  return most;
+}
+
+// The planes hold 1024 times X, A and B in fp16: up to 48 of them, 64 and more are infinite.
+int check_coefficients(const double* k, int n) {
+  constexpr double kMost = 48.0;
+  if (n < 1 || n > 64) return fail(BERGSON_EINVAL, "n_iterations must be in [1, 64]");
+  if (k == nullptr) return fail(BERGSON_EINVAL, "coefficients is NULL");
+  double top = 1.01;                                       // of X's singular values, with room for roundings
+  for (int i = 0; i < n; ++i, k += 3) {
+    if (!std::isfinite(k[0]) || !std::isfinite(k[1]) || !std::isfinite(k[2]))
+      return fail(BERGSON_EINVAL, "coefficients must be finite");
+    const double next = 1.01 * largest(k[0], k[1], k[2], true, top);
+    if (!(top * top <= kMost) || !(largest(0.0, k[1], k[2], false, top) <= kMost) ||
+        !(next <= kMost))
+      return fail(BERGSON_EUNSUPPORTED, "iteration %d: the coefficients let X, A or B pass 48", i);
+    top = next;
+  }
   return BERGSON_OK;
 }
 
@@ -503,6 +576,48 @@ int bergson_embedding_backward(const void* dy, int dtype, int64_t rows, int64_t 
   const cudaError_t e =
       launch_embedding_backward(a, workspace, static_cast<cudaStream_t>(stream));
   if (e != cudaSuccess) return fail_cuda(e, "embedding backward launch");
+  return BERGSON_OK;
+}
+
+int bergson_muon_step_workspace(const bergson_muon_tensor* tensors, int n_tensors, int products,
+                                size_t* ws_bytes) {
+  if (ws_bytes == nullptr) return fail(BERGSON_EINVAL, "ws_bytes is NULL");
+  BERGSON_TRY(check_muon_matrices(tensors, n_tensors, products, false));
+  try {
+    *ws_bytes = muon_workspace(tensors, n_tensors, products);
+  } catch (const std::bad_alloc&) {
+    return fail(BERGSON_EUNSUPPORTED, "out of host memory");
+  }
+  return BERGSON_OK;
+}
+
+int bergson_muon_step(const bergson_muon_tensor* tensors, int n_tensors, double lr, double beta,
+                      int nesterov, const double* coefficients, int n_iterations, int products,
+                      const float* grad_scale, void* workspace, size_t ws_bytes, void* stream) {
+  BERGSON_TRY(check_muon_matrices(tensors, n_tensors, products, true));
+  if (!std::isfinite(lr)) return fail(BERGSON_EINVAL, "lr must be finite");
+  if (!(beta >= 0.0 && beta < 1.0)) return fail(BERGSON_EINVAL, "beta must be in [0, 1)");
+  BERGSON_TRY(check_coefficients(coefficients, n_iterations));
+  if (grad_scale != nullptr) BERGSON_TRY(check_tensor(grad_scale, 4, "grad_scale"));
+  try {
+    BERGSON_TRY(check_workspace(workspace, ws_bytes, muon_workspace(tensors, n_tensors, products)));
+    BERGSON_TRY(injected_status());
+    if (n_tensors == 0) return BERGSON_OK;
+    DeviceGuard dg(workspace);
+    if (dg.err != cudaSuccess) return fail_cuda(dg.err, "workspace device lookup");
+    int* status = device_status_word(dg.dev);
+    if (status == nullptr) return fail(BERGSON_ECUDA, "device status word unavailable");
+    int sms = 0;
+    cudaError_t e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dg.dev);
+    const MuonScalars a{lr,           beta,     nesterov != 0, coefficients,
+                        n_iterations, products, grad_scale};
+    if (e == cudaSuccess)
+      e = launch_muon(tensors, n_tensors, a, workspace, status, sms,
+                      static_cast<cudaStream_t>(stream));
+    if (e != cudaSuccess) return fail_cuda(e, "Muon launch");
+  } catch (const std::bad_alloc&) {
+    return fail(BERGSON_EUNSUPPORTED, "out of host memory");
+  }
   return BERGSON_OK;
 }
 

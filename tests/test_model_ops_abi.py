@@ -1,5 +1,7 @@
 """Host-side checks of the entry points around a model's linear layers that need no GPU:
 refusals of arguments, workspace sizes, records."""
+import ctypes
+
 import pytest
 
 import paper_2606_11660_gb300 as bg
@@ -147,3 +149,69 @@ def test_embedding_calls_that_pass():
     for sizes in ((0, 1, 1), (2048, 50_000, 64), (2049, 50_000, 64), (1 << 20, 1 << 18, 100)):
         need = bg.bergson_embedding_backward_workspace(*sizes)
         assert need > 0 and need % 256 == 0
+
+
+QUINTIC = (3.4445, -4.7750, 2.0315)
+
+
+def muon(ws=FAKE, ws_bytes=1 << 40, n=1, lr=1e-3, beta=0.9, k=(QUINTIC,) * 5, products=3, gs=None,
+         **kw):
+    a = dict(param=FAKE, grad=FAKE, master=FAKE, m=FAKE, rows=64, cols=100, lr_scale=1.0, ortho_scale=1.0,
+             weight_decay=0.1, param_dtype=1, grad_dtype=1, reserved=0)
+    a.update(kw)
+    rec = (bg.bergson_muon_tensor * max(n, 1))(*[bg.bergson_muon_tensor(**a)] * max(n, 1))
+    flat = [x for abc in k for x in abc] if k is not None else []
+    c = (ctypes.c_double * len(flat))(*flat) if k is not None else None
+    return bg.lib().bergson_muon_step(rec if n is not None else None, n, lr, beta, 1, c,
+                                      len(flat) // 3 if k is not None else 1, products, gs, ws, ws_bytes,
+                                      None)
+
+
+@pytest.mark.parametrize("kw,code", [
+    (dict(n=-1), bg.BERGSON_EINVAL), (dict(lr=INF), bg.BERGSON_EINVAL), (dict(beta=1.0), bg.BERGSON_EINVAL),
+    (dict(beta=-0.1), bg.BERGSON_EINVAL), (dict(beta=NAN), bg.BERGSON_EINVAL),
+    (dict(products=2), bg.BERGSON_EINVAL), (dict(k=()), bg.BERGSON_EINVAL), (dict(k=None), bg.BERGSON_EINVAL),
+    (dict(k=(QUINTIC,) * 65), bg.BERGSON_EINVAL), (dict(k=((NAN, 0, 0),)), bg.BERGSON_EINVAL),
+    (dict(k=((60.0, 0.0, 0.0),)), bg.BERGSON_EUNSUPPORTED),
+    (dict(k=((3.0, 0.0, 0.0),) * 4), bg.BERGSON_EUNSUPPORTED),
+    (dict(k=((0.0, 400.0, -399.0),)), bg.BERGSON_EUNSUPPORTED), (dict(gs=FAKE + 2), bg.BERGSON_EALIGN),
+    (dict(ws=None), bg.BERGSON_EINVAL), (dict(ws=FAKE + 64), bg.BERGSON_EALIGN),
+    (dict(ws_bytes=4096), bg.BERGSON_EWORKSPACE), (dict(param=None), bg.BERGSON_EINVAL),
+    (dict(grad=None), bg.BERGSON_EINVAL), (dict(m=None), bg.BERGSON_EINVAL),
+    (dict(param=FAKE + 1), bg.BERGSON_EALIGN), (dict(grad=FAKE + 1), bg.BERGSON_EALIGN),
+    (dict(m=FAKE + 2), bg.BERGSON_EALIGN), (dict(master=FAKE + 2), bg.BERGSON_EALIGN),
+    (dict(rows=0), bg.BERGSON_EINVAL), (dict(cols=-1), bg.BERGSON_EINVAL),
+    (dict(cols=(1 << 20) + 1), bg.BERGSON_EUNSUPPORTED),
+    (dict(rows=(1 << 16) + 1, cols=(1 << 16) + 1), bg.BERGSON_EUNSUPPORTED),
+    (dict(param_dtype=3), bg.BERGSON_EINVAL), (dict(grad_dtype=-1), bg.BERGSON_EINVAL),
+    (dict(reserved=1), bg.BERGSON_EINVAL), (dict(lr_scale=INF), bg.BERGSON_EINVAL),
+    (dict(ortho_scale=NAN), bg.BERGSON_EINVAL), (dict(weight_decay=INF), bg.BERGSON_EINVAL),
+])
+def test_muon_refusals(kw, code):
+    assert muon(**kw) == code and bg.bergson_last_error() != ""
+
+
+def test_muon_calls_that_pass():
+    for st in (muon(), muon(master=None), muon(n=0), muon(products=1), muon(k=(QUINTIC,) * 64),
+               muon(k=((1.5, -0.5, 0.0),) * 20), muon(k=((1.0, 0.0, 0.0),)), muon(gs=FAKE),
+               muon(rows=1, cols=1), muon(param_dtype=0, grad_dtype=2), muon(n=700),
+               muon(k=((40.0, 0.0, 0.0),))):
+        assert accepted(st), bg.bergson_last_error()
+
+
+def test_muon_workspace():
+    def need(shapes, products):
+        recs = [bg.bergson_muon_tensor(rows=r, cols=c, param_dtype=1, grad_dtype=1) for r, c in shapes]
+        return bg.bergson_muon_step_workspace((bg.bergson_muon_tensor * len(recs))(*recs), products)
+    one = need([(64, 100)], 3)
+    assert one % 256 == 0 and one > need([(64, 100)], 1) > 0
+    assert need([], 3) > 0
+    # two planes of X twice, of A and of B: 16 bytes an element of a square matrix, and no more
+    # than a batch's however many matrices there are
+    assert need([(1024, 1024)] * 4, 3) <= 16 * 4 * 1024 ** 2 + 65_536
+    many = need([(4096, 4096)] * 300, 3)
+    assert many <= 16 * 2 ** 29 + 65_536
+    assert need([(1 + i, 300 - i) for i in range(200)], 3) >= one
+    assert bg.lib().bergson_muon_step_workspace(None, 0, 3, None) == bg.BERGSON_EINVAL
+    with pytest.raises(bg.BergsonError):
+        need([(64, 0)], 3)

@@ -40,3 +40,24 @@ def test_embedding_gradient():
     d, size = orc.embedding_backward(dy, ids, 1.7, 7)
     assert abs(along(f) - (d * u).sum()) < 1e-8
     assert np.all(d[[1, 2, 4, 5]] == 0) and np.all(size >= np.abs(d))
+
+
+@pytest.mark.parametrize("shape", [(6, 6), (5, 11), (11, 5)])
+def test_newton_schulz_is_a_polynomial_in_the_singular_values(shape):
+    r = np.random.default_rng(2)
+    u = r.normal(size=shape)
+    k = [(3.4445, -4.7750, 2.0315), (2.0, -1.5, 0.5), (1.5, -0.5, 0.0)]
+    left, s, right = np.linalg.svd(u, full_matrices=False)
+    s = s / np.linalg.norm(s)
+    for a, b, c in k:
+        s = a * s + b * s ** 3 + c * s ** 5
+    assert np.allclose(orc.newton_schulz(u, k), (left * s) @ right, atol=1e-12)
+    assert not orc.newton_schulz(np.zeros(shape), k).any()
+    x = orc.newton_schulz(u, [(1.5, -0.5, 0.0)] * 40)
+    assert np.allclose(x @ x.T if shape[0] <= shape[1] else x.T @ x, np.eye(min(shape)))
+
+
+def test_muon_step_closed_form():
+    w, m, x = orc.muon_step(np.array([[2.0]]), np.array([[-3.0]]), np.zeros((1, 1)), 0.1, 0.9, True,
+                            [(1.0, 0.0, 0.0)], 2.0, 0.5)
+    assert np.allclose([w, m, x], [[[2.0 - 0.1 * (-2.0 + 1.0)]], [[-0.3]], [[-1.0]]])
