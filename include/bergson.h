@@ -1067,8 +1067,9 @@ typedef struct bergson_muon_tensor {
  *
  *   tensors   HOST array of n_tensors (>= 0) records, of any shapes; matrices of one shape run
  *             together.
- *   coefficients  HOST array [n_iterations, 3], n_iterations in [1, 64].  From |X|_F = 1 they must
- *             hold |X|, |A| and |b A + c A^2| to 48 (EUNSUPPORTED; a bound by the polynomials alone).
+ *   coefficients  HOST array [n_iterations, 3], n_iterations in [1, 64].  From |X|_F = 1 on,
+ *             |X|, |a I + b A + c A^2| and, where c is not 0, |A + b / 2c| and b^2 / 4c have to stay
+ *             within 48 (else EUNSUPPORTED; judged by the polynomials alone).
  *   products  3: the products' operands hold 22 bits (X is off by some 1e-6 |X| an iteration).
  *             1: they hold fp16's 11 (some 1e-3), at a third of the work: for weights without a
  *             master copy, whose own rounding is larger.

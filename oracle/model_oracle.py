@@ -50,18 +50,15 @@ def embedding_backward(dy, ids, scale, V):
 
 # ------------------------------------------------------------------ Muon
 
-def newton_schulz(u, coefficients, hold=lambda x: x, product=lambda x: x):
-    """The iteration on u / |u|_F in fp64.  hold rounds what an operand holds, product what a
-    product gives: the identity by default."""
+def newton_schulz(u, coefficients):
+    """The iteration on u / |u|_F, short side first."""
     n = np.linalg.norm(u)
-    x = hold(u / n if n > 0 else np.zeros_like(u))
-    tall = u.shape[0] > u.shape[1]
+    x = u / n if n > 0 else np.zeros_like(u)
+    if u.shape[0] > u.shape[1]:
+        return newton_schulz(u.T, coefficients).T
     for a, b, c in coefficients:
-        y = x.T if tall else x
-        g = hold(product(y @ y.T))
-        q = hold(b * g + c * product(g @ g))
-        x = a * x + product(x @ q if tall else q @ x)
-        x = hold(x)
+        g = x @ x.T
+        x = a * x + (b * g + c * g @ g) @ x
     return x
 
 

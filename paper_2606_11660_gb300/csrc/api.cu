@@ -819,14 +819,30 @@ CUresult encode_tmap_planes(CUtensorMap* tm, const void* ptr, int64_t inner, int
 }
 
 CUresult encode_tmap_stack(CUtensorMap* tm, const void* ptr, int64_t inner, int64_t outer,
-                           int64_t planes, int64_t ld, int box_outer) {
+                           int64_t planes, int64_t ld, int box_outer, int box_planes) {
   if (encode_fn() == nullptr) return CUDA_ERROR_NOT_SUPPORTED;
   cuuint64_t dims[3] = {static_cast<cuuint64_t>(inner), static_cast<cuuint64_t>(outer),
                         static_cast<cuuint64_t>(planes)};
   cuuint64_t strides[2] = {static_cast<cuuint64_t>(ld * 2), static_cast<cuuint64_t>(outer * ld * 2)};
-  cuuint32_t box[3] = {64, static_cast<cuuint32_t>(box_outer), 1};
+  cuuint32_t box[3] = {64, static_cast<cuuint32_t>(box_outer), static_cast<cuuint32_t>(box_planes)};
   cuuint32_t es[3] = {1, 1, 1};
   return encode_fn()(tm, CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 3, const_cast<void*>(ptr), dims, strides,
+                     box, es, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+                     CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+}
+
+CUresult encode_tmap_across(CUtensorMap* tm, const void* ptr, int64_t inner, int64_t outer,
+                            int64_t planes, int64_t ld, int box_planes, int chunks) {
+  if (encode_fn() == nullptr) return CUDA_ERROR_NOT_SUPPORTED;
+  cuuint64_t dims[4] = {static_cast<cuuint64_t>(chunks > 0 ? 64 : inner),
+                        static_cast<cuuint64_t>(outer), static_cast<cuuint64_t>(planes),
+                        static_cast<cuuint64_t>(chunks > 0 ? (inner + 63) / 64 : 1)};
+  cuuint64_t strides[3] = {static_cast<cuuint64_t>(ld * 2), static_cast<cuuint64_t>(outer * ld * 2),
+                           128};
+  cuuint32_t box[4] = {64, 64, static_cast<cuuint32_t>(box_planes),
+                       static_cast<cuuint32_t>(chunks > 0 ? chunks : 1)};
+  cuuint32_t es[4] = {1, 1, 1, 1};
+  return encode_fn()(tm, CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 4, const_cast<void*>(ptr), dims, strides,
                      box, es, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
                      CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
 }

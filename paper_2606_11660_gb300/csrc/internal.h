@@ -411,9 +411,13 @@ CUresult encode_tmap_2d(CUtensorMap* tm, CUtensorMapDataType dt, const void* ptr
 CUresult encode_tmap_planes(CUtensorMap* tm, const void* ptr, int64_t inner, int64_t outer,
                             int64_t ld, int box_inner, int box_outer);
 
-// 3-D tiled tensor map over `planes` stacked fp16 matrices [outer, ld], box {64, box_outer, 1},
-// 128-byte swizzle.
+// Tensor maps over `planes` stacked fp16 matrices [outer, ld], 128-byte swizzle.  The first: boxes
+// of 64 columns, box_outer rows and box_planes planes.  The second, with dimensions (column, row,
+// plane, chunk): boxes of 64 rows, box_planes planes and `chunks` chunks of 64 columns each, the box's slowest
+// dimension (rows are whole chunks: 64 | ld); chunks = 0: of 64 columns from any on.
 CUresult encode_tmap_stack(CUtensorMap* tm, const void* ptr, int64_t inner, int64_t outer,
-                           int64_t planes, int64_t ld, int box_outer);
+                           int64_t planes, int64_t ld, int box_outer, int box_planes);
+CUresult encode_tmap_across(CUtensorMap* tm, const void* ptr, int64_t inner, int64_t outer,
+                            int64_t planes, int64_t ld, int box_planes, int chunks);
 
 }  // namespace bergson

@@ -2,11 +2,15 @@
 // Newton-Schulz products, weight update.
 //
 //   m <- beta m + (1 - beta) g,   u = m, or beta m + (1 - beta) g,   X = u / |u|_F,
-//   per iteration (a, b, c):  A = X X^T,  B = b A + c A^2,  X <- a X + B X,
+//   per iteration (a, b, c):  A = X X^T,  X <- (a I + b A + c A^2) X,
 //   w <- w - lr (ortho_scale X + weight_decay w)
 //
 // for the short side first; a matrix with more rows than columns takes A = X^T X and
-// X <- a X + X B, and none is ever transposed.
+// X <- X (..), and none is ever transposed.  The polynomial is taken as
+//
+//   A' = A + h I,   B = c A'^2 + (a - c h^2) I,   X <- B X,     h = b / 2c
+//
+// (c = 0: B = b A + a I at once), so that no product reads anything but its two operands.
 //
 // The products run on the tensor cores with fp16 operands and fp32 sums.  An
 // operand is held as one fp16 plane (products = 1) or as the sum of two, hi = fp16(v), lo = fp16(v - hi)
@@ -219,20 +223,26 @@ __global__ void __launch_bounds__(kMomentThreads) planes_kernel(
 // ------------------------------------------------------------------ products
 
 constexpr int kTileM = 256;                    // rows of a pair's tile, 128 a CTA
-constexpr int kTileN = 256;                    // columns, at most
+constexpr int kTileN = 256;                    // columns of an accumulator, at most
 constexpr int kTileK = 64;                     // a stage: one 128-byte row of fp16
-constexpr int kBox = 64;                       // rows of a box
-constexpr int kBoxBytes = kBox * 128;
-constexpr int kPlaneBytes = 2 * kBoxBytes;     // of an operand's plane in a stage, per CTA
-constexpr int kThreads = 64 + 256;             // producer, MMA, 8 epilogue warps
+constexpr int kBoxBytes = 64 * 128;
+constexpr int kPlaneBytes = 2 * kBoxBytes;     // of 128 rows of an operand's plane in a stage
+constexpr int kEpilogueWarps = 16;             // four to a quarter of the rows: 64 columns a thread
+constexpr int kThreads = 32 * (3 + kEpilogueWarps);    // A's loads, MMA, B's loads, epilogue
+constexpr int kChain = 4;                      // stages of an accumulation chain with two planes
 constexpr int kBarBytes = 256;
 constexpr int kTmemCols = 2 * kTileN;          // two accumulators
 constexpr uint64_t kDrainTimeoutNs = 2000000000ull;
 
+// With one plane a tile is two accumulators wide: a stage's loads (48 KB a CTA for 8 MMAs of 128
+// cycles) then keep up with the MMAs, which those of one (32 KB for 4) do not, at some 2.4
+// cycles a row of 128 bytes.  With two planes an accumulator has 12 MMAs for 64 KB.
 template <int P>
 struct ProdCfg {
-  static constexpr int kStageBytes = 2 * P * kPlaneBytes;
-  static constexpr int kStages = P == 2 ? 3 : 6;
+  static constexpr int kSub = P == 2 ? 1 : 2;
+  static constexpr int kABytes = P * kPlaneBytes;
+  static constexpr int kStageBytes = kABytes + kSub * P * kPlaneBytes;
+  static constexpr int kStages = P == 2 ? 3 : 4;
   static constexpr int kSmemBytes = 1024 + kStages * kStageBytes + kBarBytes;
 };
 
@@ -242,16 +252,16 @@ enum : int { kRowMajor = 0, kAcross = 1, kSymmetric = 2 };
 struct ProdGroup {
   int begin;                   // first tile
   int per_mat;                 // tiles of a matrix
-  int n_mt, n_nt, tn;          // tiles of tn columns
+  int n_mt, n_nt, tn;          // tiles of ProdCfg::kSub times tn columns
   int M, N, K;                 // of D [M, N]
   int a_kind, b_kind;
+  int chunks_b;                // 64-row chunks of a box of B's across; 0: one each, tn % 128 != 0
   int lower;                   // only tiles that reach the diagonal or lie below
   int first_mat;
-  int src_ld, dst_ld;
-  float alpha, beta;           // D' = alpha acc + beta src
-  const __half* src;           // planes, or nullptr
+  int dst_ld;
+  float alpha, gamma;          // D' = alpha acc + gamma I
   __half* dst;                 // planes, or nullptr: the weights
-  int64_t src_plane, dst_plane;
+  int64_t dst_plane;
 };
 
 struct WeightEntry {
@@ -264,7 +274,8 @@ struct WeightEntry {
 
 template <int G, int N>
 struct ProdParams {
-  CUtensorMap a[G], b[G];
+  CUtensorMap a[G], b[G];      // boxes of rows as they lie
+  CUtensorMap ax[G], bx[G];    // and across
   ProdGroup g[G];
   WeightEntry w[N];
   int n;
@@ -275,10 +286,12 @@ struct ProdParams {
 
 struct Tile {
   int group, mat, mt, nt;
+  int subs;                    // accumulators that are needed: columns within D and not above the diagonal
 };
 
-template <int G, int N>
+template <int P, int G, int N>
 __device__ __forceinline__ Tile tile_of(const ProdParams<G, N>& p, int t) {
+  constexpr int kSub = ProdCfg<P>::kSub;
   Tile o;
   o.group = 0;
   while (o.group + 1 < p.n && p.g[o.group + 1].begin <= t) ++o.group;
@@ -286,22 +299,25 @@ __device__ __forceinline__ Tile tile_of(const ProdParams<G, N>& p, int t) {
   t -= g.begin;
   o.mat = t / g.per_mat;
   t -= o.mat * g.per_mat;
+  int width = g.N;                               // of the tile's row of tiles
   if (g.lower) {
     o.mt = 0;
     for (;;) {
-      const int n = (min((o.mt + 1) * kTileM, g.N) + g.tn - 1) / g.tn;
+      width = min((o.mt + 1) * kTileM, g.N);
+      const int n = (width + kSub * g.tn - 1) / (kSub * g.tn);
       if (t < n) break;
       t -= n;
       ++o.mt;
     }
     o.nt = t;
-    return o;
+  } else {
+    constexpr int kSide = 8;                     // near-square blocks of tiles share panels in L2
+    const int per = kSide * g.n_nt, block = t / per, r = t - block * per;
+    const int rows = min(kSide, g.n_mt - block * kSide);
+    o.mt = block * kSide + r % rows;
+    o.nt = r / rows;
   }
-  constexpr int kSide = 8;                       // near-square blocks of tiles share panels in L2
-  const int per = kSide * g.n_nt, block = t / per, r = t - block * per;
-  const int rows = min(kSide, g.n_mt - block * kSide);
-  o.mt = block * kSide + r % rows;
-  o.nt = r / rows;
+  o.subs = kSub == 1 ? 1 : min(kSub, (width - o.nt * kSub * g.tn + g.tn - 1) / g.tn);
   return o;
 }
 
@@ -312,27 +328,123 @@ __device__ __forceinline__ int tile_index(int i, int cid, int n_cl, int n_tiles)
   return t < n_tiles ? t : -1;
 }
 
-// Whether the operand rows from row0 on (a tile's first) are read across at column k0.
-__device__ __forceinline__ bool across(int kind, int row0, int k0) {
-  return kind == kAcross || (kind == kSymmetric && (k0 / kTileM) > (row0 / kTileM));
+// The stage from which on the operand rows from row0 on (a tile's first) are read across.
+__device__ __forceinline__ int across_from(int kind, int row0) {
+  return kind == kRowMajor ? INT32_MAX
+         : kind == kAcross ? 0
+                           : (row0 / kTileM + 1) * (kTileM / kTileK);
 }
 
-__device__ __forceinline__ void tma_load_box_pair(uint32_t dst, const void* tmap, uint32_t bar,
-                                                  int c0, int c1, int c2, uint64_t policy) {
+__device__ __forceinline__ void tma_load_rows(uint32_t dst, const void* tmap, uint32_t bar, int k,
+                                              int row, int plane, uint64_t policy) {
   asm volatile(
       "cp.async.bulk.tensor.3d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes"
       ".L2::cache_hint [%0], [%1, {%3, %4, %5}], [%2], %6;" ::"r"(dst),
-      "l"(tmap), "r"(bar), "r"(c0), "r"(c1), "r"(c2), "l"(policy)
+      "l"(tmap), "r"(bar), "r"(k), "r"(row), "r"(plane), "l"(policy)
+      : "memory");
+}
+__device__ __forceinline__ void tma_load_across(uint32_t dst, const void* tmap, uint32_t bar,
+                                                int row, int k, int plane, int chunk,
+                                                uint64_t policy) {
+  asm volatile(
+      "cp.async.bulk.tensor.4d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes"
+      ".L2::cache_hint [%0], [%1, {%3, %4, %5, %6}], [%2], %7;" ::"r"(dst),
+      "l"(tmap), "r"(bar), "r"(row), "r"(k), "r"(plane), "r"(chunk), "l"(policy)
       : "memory");
 }
 
-// Descriptor of an operand read across: 64 of its rows side by side in 128 bytes (128-byte
-// swizzle), 8 columns of K every 1024 bytes, the next 64 rows a box further.
-__device__ __forceinline__ uint64_t across_desc(uint32_t saddr) {
-  return static_cast<uint64_t>((saddr & 0x3FFFFu) >> 4) |
-         (static_cast<uint64_t>(kBoxBytes >> 4) << 16) |
-         (static_cast<uint64_t>(1024 >> 4) << 32) | (static_cast<uint64_t>(1) << 46) |
-         (static_cast<uint64_t>(2) << 61);
+// Shared-memory descriptors of the two ways, 128-byte swizzle, as their low words (the upper one is
+// the same: 1024 bytes from one group of 8 to the next).  Rows as they lie: 128 bytes of K each, 8
+// rows a group.  Across: 64 rows side by side in 128 bytes, 8 columns of K a group; a chunk's P
+// planes come one after the other, the next 64 rows behind them.
+constexpr uint32_t kDescHigh = (1024u >> 4) | (1u << 14) | (2u << 29);
+template <int P>
+__device__ __forceinline__ uint32_t desc_low(uint32_t saddr, bool x) {
+  return (saddr >> 4) | (x ? static_cast<uint32_t>(P * kBoxBytes >> 4) : 1u) << 16;
+}
+__device__ __forceinline__ void umma_pair_low(uint32_t d_tmem, uint32_t a_low, uint32_t b_low,
+                                              uint32_t idesc, uint32_t accumulate) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t.reg .b64 a, b;\n\t"
+      "setp.ne.b32 p, %5, 0;\n\t"
+      "mov.b64 a, {%1, %3};\n\tmov.b64 b, {%2, %3};\n\t"
+      "tcgen05.mma.cta_group::2.kind::f16 [%0], a, b, %4, p;\n\t}" ::"r"(d_tmem),
+      "r"(a_low), "r"(b_low), "r"(kDescHigh), "r"(idesc), "r"(accumulate)
+      : "memory");
+}
+// True in one lane of a whole warp, the same each time.
+__device__ __forceinline__ bool elect_lane() {
+  uint32_t r;
+  asm volatile(
+      "{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}"
+      : "=r"(r));
+  return r != 0;
+}
+
+// One side's loads of all the tiles of a CTA, by one thread.
+template <int P, bool kSideB, int G, int N>
+__device__ __forceinline__ void load_side(const ProdParams<G, N>& p, int rank, int cid, int n_cl,
+                                          uint32_t sbase, uint64_t* full, uint64_t* empty,
+                                          volatile int* s_abort) {
+  using C = ProdCfg<P>;
+  const uint64_t tmo = p.timeout_ns;
+  const uint64_t pol = policy_evict_normal();
+  int stage = 0;
+  uint32_t ph = 0;
+  uint32_t issued = 0, issued_par = 0;
+  bool ok = true;
+  for (int i = 0, t; ok && (t = tile_index(i, cid, n_cl, p.n_tiles)) >= 0; ++i) {
+    const Tile o = tile_of<P>(p, t);
+    const ProdGroup& g = p.g[o.group];
+    const void* rows_map = kSideB ? &p.b[o.group] : &p.a[o.group];
+    const void* across_map = kSideB ? &p.bx[o.group] : &p.ax[o.group];
+    const int kind = kSideB ? g.b_kind : g.a_kind;
+    const int z = o.mat * P;
+    const int subs = kSideB ? o.subs : 1;
+    const int wide = kSideB ? g.tn : kTileM;       // rows over the pair
+    const int half = wide / 2;
+    const int first = kSideB ? o.nt * C::kSub * g.tn : o.mt * kTileM;
+    const int chunks = kSideB ? g.chunks_b : 2;
+    const int boxes = (half + 63) / 64;            // without whole chunks
+    const int x_from = across_from(kind, first), inner = g.K;
+    for (int k0 = 0; k0 < inner; k0 += kTileK) {
+      if (!mbar_wait(smem_u32(&empty[stage]), ph ^ 1, tmo, s_abort)) { ok = false; break; }
+      const bool x = k0 / kTileK >= x_from;
+      const uint32_t fb_local = smem_u32(&full[stage]);
+      const uint32_t fb = mapa_shared(fb_local, 0);
+      if (rank == 0) {
+        const uint32_t bytes = x ? (chunks > 0 ? chunks : boxes) * P * kBoxBytes : half * 128 * P;
+        mbar_arrive_expect_tx(fb_local, 2 * subs * bytes);
+      }
+      uint32_t dst = sbase + stage * C::kStageBytes + (kSideB ? C::kABytes : 0);
+      int r = first + rank * half;
+      for (int h = 0; h < subs; ++h, r += wide, dst += P * kPlaneBytes) {
+        if (!x) {
+          tma_load_rows(dst, rows_map, fb, k0, r, z, pol);
+        } else if (chunks > 0) {
+          tma_load_across(dst, across_map, fb, 0, k0, z, r / 64, pol);
+        } else {
+          for (int q = 0; q < boxes; ++q)
+            tma_load_across(dst + q * P * kBoxBytes, across_map, fb, r + 64 * q, k0, z, 0, pol);
+        }
+      }
+      issued |= 1u << stage;
+      issued_par = (issued_par & ~(1u << stage)) | (ph << stage);
+      if (++stage == C::kStages) { stage = 0; ph ^= 1; }
+    }
+  }
+  if (!ok) {
+    raise_device_error(p.status, s_abort, kStatusTimeout);
+    if (rank == 0) {
+      for (int s = 0; s < C::kStages; ++s)
+        if (issued >> s & 1)
+          mbar_wait(smem_u32(&full[s]), (issued_par >> s) & 1, kDrainTimeoutNs, nullptr);
+    } else {
+      const uint64_t t0 = global_timer_ns();      // its loads complete on the other CTA's barrier
+      while (global_timer_ns() - t0 < 1000000ull) {
+      }
+    }
+  }
 }
 
 __device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity, uint64_t tmo,
@@ -342,114 +454,78 @@ __device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity, uint64_
   return __shfl_sync(0xffffffffu, ok ? 1 : 0, 0) != 0;
 }
 
-// 16 fp16 elements from 32-byte boundaries.
-__device__ __forceinline__ void add_plane(const __half* p, float (&x)[16]) {
-  uint32_t r[8];
-  load32(p, r);
-#pragma unroll
-  for (int k = 0; k < 8; ++k) {
-    const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&r[k]));
-    x[2 * k] += f.x;
-    x[2 * k + 1] += f.y;
-  }
-}
-
-// 16 columns of a row: D' to its planes or into the weights.
-template <int P>
-__device__ __forceinline__ void finish(const ProdGroup& g, const WeightEntry& w, int mat, int row,
-                                       int col, const float* acc) {
-  float v[16];
-#pragma unroll
-  for (int k = 0; k < 16; ++k) v[k] = 0.0f;
-  if (g.src != nullptr) {
-    const __half* s = g.src + static_cast<int64_t>(mat) * P * g.src_plane +
-                      static_cast<int64_t>(row) * g.src_ld + col;
-    add_plane(s, v);
-    if (P == 2) add_plane(s + g.src_plane, v);
-  }
-#pragma unroll
-  for (int k = 0; k < 16; ++k) v[k] = fmaf(g.alpha, acc[k], g.beta * v[k]);
-  if (g.dst != nullptr) {
-    __half* d = g.dst + static_cast<int64_t>(mat) * P * g.dst_plane +
-                static_cast<int64_t>(row) * g.dst_ld + col;
-    uint32_t hi[8], lo[8];
-#pragma unroll
-    for (int k = 0; k < 8; ++k) {
-      const __half2 h = __floats2half2_rn(v[2 * k], v[2 * k + 1]);
-      const float2 f = __half22float2(h);
-      const __half2 l = __floats2half2_rn(v[2 * k] - f.x, v[2 * k + 1] - f.y);
-      hi[k] = *reinterpret_cast<const uint32_t*>(&h);
-      lo[k] = *reinterpret_cast<const uint32_t*>(&l);
-    }
-    store32(d, hi);
-    if (P == 2) store32(d + g.dst_plane, lo);
-    return;
-  }
-  const int64_t at = static_cast<int64_t>(row) * g.N + col;
+// Sets 16 values of a row as the step leaves them: w - lr (ortho_scale X + weight_decay w).
+__device__ __forceinline__ void update_weights(const WeightEntry& w, float ortho, int64_t at, int left,
+                                               const float* v) {
+  const bool wide = w.master != nullptr || w.pt == BERGSON_F32;
+  float* f = w.master != nullptr ? w.master : static_cast<float*>(w.p);
   if (w.vec) {
-    float x[16];
-    if (w.master != nullptr || w.pt == BERGSON_F32) {
-      float* f = w.master != nullptr ? w.master : static_cast<float*>(w.p);
 #pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        uint32_t r[8];
-        load32(f + at + 8 * h, r);
-#pragma unroll
-        for (int k = 0; k < 8; ++k) x[8 * h + k] = __uint_as_float(r[k]);
-      }
-    } else {
-      uint32_t r[8];
-      load32(static_cast<uint16_t*>(w.p) + at, r);
-#pragma unroll
-      for (int k = 0; k < 8; ++k) {
-        const uint4 u = make_uint4(r[k], 0, 0, 0);
-        const float2 f = w.pt == BERGSON_BF16 ? unpack2(u, 0, static_cast<__nv_bfloat16*>(nullptr))
-                                              : unpack2(u, 0, static_cast<__half*>(nullptr));
-        x[2 * k] = f.x;
-        x[2 * k + 1] = f.y;
-      }
-    }
-#pragma unroll
-    for (int k = 0; k < 16; ++k) x[k] = fmaf(-w.lr_ortho, v[k], fmaf(-w.lr_decay, x[k], x[k]));
-    if (w.master != nullptr || w.pt == BERGSON_F32) {
-      float* f = w.master != nullptr ? w.master : static_cast<float*>(w.p);
-#pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        uint32_t r[8];
-#pragma unroll
-        for (int k = 0; k < 8; ++k) r[k] = __float_as_uint(x[8 * h + k]);
-        store32(f + at + 8 * h, r);
-        if (w.master != nullptr && w.pt == BERGSON_F32)
-          store32(static_cast<float*>(w.p) + at + 8 * h, r);
-      }
-    }
-    if (w.pt != BERGSON_F32) {
+    for (int h = 0; h < 16; h += 8) {
+      float x[8];
+      load_eight(wide ? f : w.p, wide ? BERGSON_F32 : w.pt, true, at + h, at + h + 8, x);
       uint32_t r[8];
 #pragma unroll
       for (int k = 0; k < 8; ++k) {
-        uint4 u = make_uint4(0, 0, 0, 0);
-        const float2 f = make_float2(x[2 * k], x[2 * k + 1]);
-        if (w.pt == BERGSON_BF16) pack2(u, 0, f, static_cast<__nv_bfloat16*>(nullptr));
-        else pack2(u, 0, f, static_cast<__half*>(nullptr));
-        r[k] = u.x;
+        x[k] = fmaf(-ortho, v[h + k], fmaf(-w.lr_decay, x[k], x[k]));
+        r[k] = __float_as_uint(x[k]);
       }
-      store32(static_cast<uint16_t*>(w.p) + at, r);
+      if (wide) store32(f + at + h, r);
+      if (w.pt == BERGSON_F32) {
+        if (w.master != nullptr) store32(static_cast<float*>(w.p) + at + h, r);
+        continue;
+      }
+      uint4 u;
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const float2 y = make_float2(x[2 * k], x[2 * k + 1]);
+        if (w.pt == BERGSON_BF16) pack2(u, k, y, static_cast<__nv_bfloat16*>(nullptr));
+        else pack2(u, k, y, static_cast<__half*>(nullptr));
+      }
+      *reinterpret_cast<uint4*>(static_cast<uint16_t*>(w.p) + at + h) = u;
     }
     return;
   }
 #pragma unroll
   for (int k = 0; k < 16; ++k) {
-    if (col + k >= g.N) return;
-    float x = w.master != nullptr ? w.master[at + k] : load_any(w.p, w.pt, at + k);
-    x = fmaf(-w.lr_ortho, v[k], fmaf(-w.lr_decay, x, x));
-    if (w.master != nullptr) w.master[at + k] = x;
+    if (k >= left) return;
+    float x = wide ? f[at + k] : load_any(w.p, w.pt, at + k);
+    x = fmaf(-ortho, v[k], fmaf(-w.lr_decay, x, x));
+    if (wide) f[at + k] = x;
     if (w.pt == BERGSON_BF16) static_cast<__nv_bfloat16*>(w.p)[at + k] = __float2bfloat16_rn(x);
     else if (w.pt == BERGSON_F16) static_cast<__half*>(w.p)[at + k] = __float2half_rn(x);
-    else static_cast<float*>(w.p)[at + k] = x;
+    else if (w.master != nullptr) static_cast<float*>(w.p)[at + k] = x;
   }
 }
 
-// D[i, j] = alpha <a_i, b_j> + beta src[i, j] over persistent CTA pairs, synchronised
+// The weights that update_weights() will read, on their way to L2 while the product runs.
+__device__ __forceinline__ void prefetch_weights(const WeightEntry& w, int64_t at, int n) {
+  const bool wide = w.master != nullptr || w.pt == BERGSON_F32;
+  const int size = wide ? 4 : 2;
+  const uint8_t* p = (w.master != nullptr ? reinterpret_cast<const uint8_t*>(w.master)
+                                          : static_cast<const uint8_t*>(w.p)) + at * size;
+  for (int i = 0; i < n * size; i += 128) asm volatile("prefetch.global.L2 [%0];" ::"l"(p + i));
+}
+
+// 16 columns of a row: D' to its planes.
+template <int P>
+__device__ __forceinline__ void put_planes(const ProdGroup& g, __half* d, const float* v) {
+  uint32_t hi[8], lo[8];
+#pragma unroll
+  for (int k = 0; k < 8; ++k) {
+    const __half2 h = __floats2half2_rn(v[2 * k], v[2 * k + 1]);
+    hi[k] = *reinterpret_cast<const uint32_t*>(&h);
+    if (P == 2) {
+      const float2 f = __half22float2(h);
+      const __half2 l = __floats2half2_rn(v[2 * k] - f.x, v[2 * k + 1] - f.y);
+      lo[k] = *reinterpret_cast<const uint32_t*>(&l);
+    }
+  }
+  store32(d, hi);
+  if (P == 2) store32(d + g.dst_plane, lo);
+}
+
+// D[i, j] = alpha <a_i, b_j> + gamma [i == j] over persistent CTA pairs, synchronised
 // as the other pair kernels: the odd CTA's loads complete on the even CTA's `full`, the
 // even CTA's MMA thread frees a stage in both CTAs and hands accumulators to both
 // epilogues by multicast commits, and every epilogue warp of both CTAs releases an
@@ -482,12 +558,12 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
   griddep_launch_dependents();   // the next grid sets itself up and waits for this one to end
   if (threadIdx.x == 0) {
     for (int s = 0; s < C::kStages; ++s) {
-      mbar_init(smem_u32(&full[s]), 1);
+      mbar_init(smem_u32(&full[s]), 2);              // A's and B's loads
       mbar_init(smem_u32(&empty[s]), 1);
     }
     for (int i = 0; i < 2; ++i) {
       mbar_init(smem_u32(&tfull[i]), 1);
-      mbar_init(smem_u32(&tempty[i]), 16);           // 8 epilogue warps of each CTA
+      mbar_init(smem_u32(&tempty[i]), 2 * kEpilogueWarps);     // of both CTAs
     }
     mbar_init(smem_u32(drain), 1);
     *s_abort = 0;
@@ -505,173 +581,158 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
   const uint64_t tmo = p.timeout_ns;
 
   if (warp == 0) {
-    // ------------------------------------------------------------ producer
-    if (lane == 0) {
-      const uint64_t pol = policy_evict_normal();
-      int stage = 0;
-      uint32_t ph = 0;
-      uint32_t issued = 0, issued_par = 0;
-      bool ok = true;
-      for (int i = 0, t; ok && (t = tile_index(i, cid, n_cl, p.n_tiles)) >= 0; ++i) {
-        const Tile o = tile_of(p, t);
-        const ProdGroup& g = p.g[o.group];
-        const void* ta = &p.a[o.group];
-        const void* tb = &p.b[o.group];
-        const int z = o.mat * P;
-        const int boxes_b = (g.tn / 2 + kBox - 1) / kBox;
-        const int a0 = o.mt * kTileM, b0 = o.nt * g.tn;
-        const int ar = a0 + rank * (kTileM / 2), br = b0 + rank * (g.tn / 2);
-        for (int k0 = 0; k0 < g.K; k0 += kTileK) {
-          if (!mbar_wait(smem_u32(&empty[stage]), ph ^ 1, tmo, s_abort)) { ok = false; break; }
-          const uint32_t fb_local = smem_u32(&full[stage]);
-          const uint32_t fb = mapa_shared(fb_local, 0);
-          if (rank == 0) mbar_arrive_expect_tx(fb_local, 2 * P * (2 + boxes_b) * kBoxBytes);
-          const uint32_t dst = sbase + stage * C::kStageBytes;
-          const bool xa = across(g.a_kind, a0, k0), xb = across(g.b_kind, b0, k0);
-#pragma unroll
-          for (int q = 0; q < P; ++q) {
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-              const int r = ar + h * kBox;
-              tma_load_box_pair(dst + q * kPlaneBytes + h * kBoxBytes, ta, fb, xa ? r : k0,
-                                xa ? k0 : r, z + q, pol);
-            }
-            for (int h = 0; h < boxes_b; ++h) {
-              const int r = br + h * kBox;
-              tma_load_box_pair(dst + (P + q) * kPlaneBytes + h * kBoxBytes, tb, fb, xb ? r : k0,
-                                xb ? k0 : r, z + q, pol);
-            }
-          }
-          issued |= 1u << stage;
-          issued_par = (issued_par & ~(1u << stage)) | (ph << stage);
-          if (++stage == C::kStages) { stage = 0; ph ^= 1; }
-        }
-      }
-      if (!ok) {
-        raise_device_error(p.status, s_abort, kStatusTimeout);
-        if (rank == 0) {
-          for (int s = 0; s < C::kStages; ++s)
-            if (issued >> s & 1)
-              mbar_wait(smem_u32(&full[s]), (issued_par >> s) & 1, kDrainTimeoutNs, nullptr);
-        } else {
-          const uint64_t t0 = global_timer_ns();      // its loads complete on the other CTA's barrier
-          while (global_timer_ns() - t0 < 1000000ull) {
-          }
-        }
-      }
-    }
+    if (lane == 0) load_side<P, false>(p, rank, cid, n_cl, sbase, full, empty, s_abort);
+    __syncwarp();
+  } else if (warp == 2) {
+    if (lane == 0) load_side<P, true>(p, rank, cid, n_cl, sbase, full, empty, s_abort);
     __syncwarp();
   } else if (warp == 1) {
     // ------------------------------------------------------------ MMA issuer (even CTA)
-    if (rank == 0 && lane == 0) {
+    // The whole warp goes through the loop and one lane issues: descriptors then are the warp's
+    // own, and an MMA takes 18 cycles to issue instead of 62 in a branch of one lane.
+    if (rank == 0) {
+      const bool lead = elect_lane();
       int stage = 0;
       uint32_t ph = 0;
-      int ab = 0;
+      int ab = 0;                                    // the tile's first accumulator, its round's parity
       uint32_t aph = 0;
       bool ok = true;
       for (int i = 0, t; ok && (t = tile_index(i, cid, n_cl, p.n_tiles)) >= 0; ++i) {
-        const Tile o = tile_of(p, t);
+        const Tile o = tile_of<P>(p, t);
         const ProdGroup& g = p.g[o.group];
-        const int a0 = o.mt * kTileM, b0 = o.nt * g.tn;
-        const uint32_t base_desc = make_idesc_f16(kTileM, g.tn, false);
-        bool fresh = true;                           // the accumulator holds nothing yet
-        for (int k0 = 0; k0 < g.K; k0 += kTileK) {
-          if (!mbar_wait(smem_u32(&full[stage]), ph, tmo, s_abort)) { ok = false; break; }
-          if (fresh && !mbar_wait(smem_u32(&tempty[ab]), aph ^ 1, tmo, s_abort)) { ok = false; break; }
-          tc_fence_after();
-          const bool xa = across(g.a_kind, a0, k0), xb = across(g.b_kind, b0, k0);
-          const uint32_t sa = sbase + stage * C::kStageBytes, sb = sa + P * kPlaneBytes;
-          const uint64_t da = xa ? across_desc(sa) : sw128_desc(sa);
-          const uint64_t db = xb ? across_desc(sb) : sw128_desc(sb);
+        const int subs = o.subs, tn = g.tn, stages = (g.K + kTileK - 1) / kTileK;
+        // stages from which on an operand is read across
+        const int xa_from = across_from(g.a_kind, o.mt * kTileM);
+        const int xb_from = across_from(g.b_kind, o.nt * C::kSub * tn);
+        const uint32_t base_idesc = make_idesc_f16(kTileM, tn, false);
+        bool fresh = true;                           // the accumulators hold nothing yet
+        for (int kc = 0; kc < stages; ++kc) {
+          ok = warp_wait(smem_u32(&full[stage]), ph, tmo, s_abort);
+          if (!ok) break;
+          const bool xa = kc >= xa_from, xb = kc >= xb_from;
+          const uint32_t sa = sbase + stage * C::kStageBytes;
+          const uint32_t da = desc_low<P>(sa, xa);
           // 16 columns of K: 32 bytes of a row, or 16 rows of 128 bytes
           const uint32_t step_a = xa ? 128 : 2, step_b = xb ? 128 : 2;
-          const uint32_t idesc = base_desc | (xa ? 1u << 15 : 0u) | (xb ? 1u << 16 : 0u);
-          const uint32_t d = tmem + ab * kTileN;
-          constexpr int kTerms = P == 2 ? 3 : 1;
-          constexpr uint32_t kPlane = kPlaneBytes / 16;
+          const uint32_t plane_a = (xa ? kBoxBytes : kPlaneBytes) / 16;
+          const uint32_t plane_b = (xb ? kBoxBytes : tn / 2 * 128) / 16;
+          const uint32_t idesc = base_idesc | (xa ? 1u << 15 : 0u) | (xb ? 1u << 16 : 0u);
+          const bool ends = kc + 1 == stages || (P == 2 && kc % kChain == kChain - 1);
+          int cab = ab;
+          uint32_t caph = aph;
 #pragma unroll
-          for (int q = 0; q < kTerms; ++q) {         // lo hi, hi lo, hi hi
-            const uint64_t at = da + (P == 2 && q == 0 ? kPlane : 0);
-            const uint64_t bt = db + (P == 2 && q == 1 ? kPlane : 0);
+          for (int h = 0; h < C::kSub; ++h) {
+            if (h >= subs) break;
+            if (fresh) {
+              ok = warp_wait(smem_u32(&tempty[cab]), caph ^ 1, tmo, s_abort);
+              if (!ok) break;
+            }
+            tc_fence_after();
+            if (lead) {
+              const uint32_t db = desc_low<P>(sa + C::kABytes + h * P * kPlaneBytes, xb);
+              const uint32_t d = tmem + cab * kTileN;
+              constexpr int kTerms = P == 2 ? 3 : 1;
 #pragma unroll
-            for (int kk = 0; kk < kTileK / 16; ++kk)
-              umma_f16_pair(d, at + kk * step_a, bt + kk * step_b, idesc,
-                            !fresh || q != 0 || kk != 0);
+              for (int q = 0; q < kTerms; ++q) {     // lo hi, hi lo, hi hi
+                const uint32_t at = da + (P == 2 && q == 0 ? plane_a : 0);
+                const uint32_t bt = db + (P == 2 && q == 1 ? plane_b : 0);
+#pragma unroll
+                for (int kk = 0; kk < kTileK / 16; ++kk)
+                  umma_pair_low(d, at + kk * step_a, bt + kk * step_b, idesc,
+                                !fresh || q != 0 || kk != 0);
+              }
+              if (ends) umma_commit_pair(smem_u32(&tfull[cab]), 0x3);
+              if (h == subs - 1) umma_commit_pair(smem_u32(&empty[stage]), 0x3);
+            }
+            __syncwarp();
+            if (++cab == 2) { cab = 0; caph ^= 1; }
           }
-          umma_commit_pair(smem_u32(&empty[stage]), 0x3);
-          fresh = P == 2 || k0 + kTileK >= g.K;
-          if (fresh) {
-            umma_commit_pair(smem_u32(&tfull[ab]), 0x3);
-            if (++ab == 2) { ab = 0; aph ^= 1; }
-          }
+          if (!ok) break;
+          fresh = ends;
+          if (ends) { ab = cab; aph = caph; }
           if (++stage == C::kStages) { stage = 0; ph ^= 1; }
         }
       }
-      if (!ok) raise_device_error(p.status, s_abort, kStatusTimeout);
-      umma_commit_pair(smem_u32(drain), 0x1);
-      mbar_wait(smem_u32(drain), 0, kDrainTimeoutNs, nullptr);
+      if (lead) {
+        if (!ok) raise_device_error(p.status, s_abort, kStatusTimeout);
+        umma_commit_pair(smem_u32(drain), 0x1);
+        mbar_wait(smem_u32(drain), 0, kDrainTimeoutNs, nullptr);
+      }
     }
     __syncwarp();
   } else {
     // ------------------------------------------------------------ epilogue
-    // Thread = a row of this CTA's half (TMEM lane) and half of the tile's columns.
+    // Thread = a row of this CTA's half (TMEM lane) and up to 64 of an accumulator's columns: summed up
+    // in registers, so that the accumulator is free again before anything is written.  A thread
+    // writes whole 32-byte sectors of its row.
+    const int ew = warp - 3;
     const int quarter = warp & 3;
-    const int half = (warp - 2) >> 2;
     int ab = 0;
     uint32_t aph = 0;
     bool aborted = false;
     for (int i = 0, t; !aborted && (t = tile_index(i, cid, n_cl, p.n_tiles)) >= 0; ++i) {
-      const Tile o = tile_of(p, t);
+      const Tile o = tile_of<P>(p, t);
       const ProdGroup& g = p.g[o.group];
       const WeightEntry& w = p.w[min(g.first_mat + o.mat, N - 1)];
-      const int cols = g.tn / 2;
+      const int pieces = g.tn / 16, first = pieces * (ew >> 2) / 4;      // of 16 columns
+      const int mine = pieces * ((ew >> 2) + 1) / 4 - first;             // up to 4
       const int row = o.mt * kTileM + rank * (kTileM / 2) + 32 * quarter + lane;
-      const int col0 = o.nt * g.tn + half * cols;
-      const int chains = P == 2 ? (g.K + kTileK - 1) / kTileK : 1;
-      constexpr int kAcc = P == 2 ? kTileN / 2 : 16;
-      float acc[kAcc];
-      if constexpr (P == 2) {
+      const int chains = P == 2 ? (g.K + kTileK * kChain - 1) / (kTileK * kChain) : 1;
+      for (int h = 0; h < o.subs && !aborted; ++h) {
+        const int col0 = (o.nt * C::kSub + h) * g.tn + 16 * first;
+        const int left = row < g.M ? min(16 * mine, g.N - col0) : 0;     // columns to write
+        const int64_t at = static_cast<int64_t>(row) * g.N + col0;
+        if (g.dst == nullptr && left > 0) prefetch_weights(w, at, left);
+        constexpr int kAcc = kTileN / 4;
+        float acc[kAcc];
 #pragma unroll
-        for (int j = 0; j < kAcc; ++j) acc[j] = 0.0f;
-      }
-      for (int ch = 0; ch < chains; ++ch) {
-        if (!warp_wait(smem_u32(&tfull[ab]), aph, tmo, s_abort)) {
-          raise_device_error(p.status, s_abort, kStatusTimeout);
-          aborted = true;
-          break;
-        }
-        tc_fence_after();
-        const uint32_t tb = tmem + (static_cast<uint32_t>(32 * quarter) << 16) + ab * kTileN +
-                            half * cols;
-        if constexpr (P == 2) {
+        for (int j = 0; j < kAcc; ++j) acc[j] = 0.0f;    // 0 + v = v: the first chain lands unchanged
+        for (int ch = 0; ch < chains; ++ch) {
+          if (!warp_wait(smem_u32(&tfull[ab]), aph, tmo, s_abort)) {
+            raise_device_error(p.status, s_abort, kStatusTimeout);
+            aborted = true;
+            break;
+          }
+          tc_fence_after();
+          const uint32_t tb = tmem + (static_cast<uint32_t>(32 * quarter) << 16) + ab * kTileN +
+                              16 * first;
 #pragma unroll
-          for (int c = 0; c < kAcc; c += 16) {
-            if (c < cols) {
+          for (int u = 0; u < 4; ++u) {
+            if (u < mine) {
               float v[16];
-              tmem_ld16(tb + c, v);
+              tmem_ld16(tb + 16 * u, v);
 #pragma unroll
-              for (int j = 0; j < 16; ++j) acc[c + j] += v[j];
+              for (int j = 0; j < 16; ++j) acc[16 * u + j] += v[j];
             }
           }
+          tc_fence_before();
+          __syncwarp();
+          if (lane == 0) mbar_arrive_remote(mapa_shared(smem_u32(&tempty[ab]), 0));
+          if (++ab == 2) { ab = 0; aph ^= 1; }
+        }
+        if (aborted) break;
+        if (g.dst != nullptr) {
+          __half* d = g.dst + static_cast<int64_t>(o.mat) * P * g.dst_plane +
+                      static_cast<int64_t>(row) * g.dst_ld + col0;
+          const float gamma = g.gamma, alpha = g.alpha;
+#pragma unroll
+          for (int u = 0; u < 4; ++u) {
+            if (16 * u >= left) break;
+#pragma unroll
+            for (int j = 0; j < 16; ++j) {
+              acc[16 * u + j] *= alpha;
+              if (gamma != 0.0f && row == col0 + 16 * u + j) acc[16 * u + j] += gamma;
+            }
+            put_planes<P>(g, d + 16 * u, acc + 16 * u);
+          }
         } else {
-#pragma unroll 1
-          for (int c = 0; c < cols; c += 16) {
-            tmem_ld16(tb + c, acc);
-            if (row < g.M && col0 + c < g.N) finish<P>(g, w, o.mat, row, col0 + c, acc);
-            __syncwarp();
+          const float ortho = w.lr_ortho * g.alpha;
+#pragma unroll
+          for (int u = 0; u < 4; ++u) {
+            if (16 * u >= left) break;
+            update_weights(w, ortho, at + 16 * u, left - 16 * u, acc + 16 * u);
           }
         }
-        tc_fence_before();
-        __syncwarp();
-        if (lane == 0) mbar_arrive_remote(mapa_shared(smem_u32(&tempty[ab]), 0));
-        if (++ab == 2) { ab = 0; aph ^= 1; }
-      }
-      if (aborted) break;
-      if constexpr (P == 2) {
-#pragma unroll
-        for (int c = 0; c < kAcc; c += 16)
-          if (c < cols && row < g.M && col0 + c < g.N)
-            finish<P>(g, w, o.mat, row, col0 + c, acc + c);
         __syncwarp();
       }
     }
@@ -732,7 +793,8 @@ std::vector<Batch> batches_of(const bergson_muon_tensor* t, int n) {
   return out;
 }
 
-int64_t leading(int64_t cols) { return round_to(cols, 16); }
+// Rows are whole chunks of 64 columns.
+int64_t leading(int64_t cols) { return round_to(cols, 64); }
 
 // Where a shape's planes stand in the workspace: X twice, A and B.
 struct Planes {
@@ -776,12 +838,12 @@ BatchLayout layout_of(const Batch& b, int P) {
   return l;
 }
 
-// Columns of a tile: what wastes least of the last one.  A tile pays some 40 columns' time
-// beside its own.
-int tile_columns(int64_t n) {
+// Columns of an accumulator: what wastes least of the last one.  One pays some 40 columns' time
+// beside its own.  With one plane they are whole chunks.
+int tile_columns(int64_t n, int P) {
   int best = kTileN;
   int64_t cost = INT64_MAX;
-  for (int tn = kTileN; tn >= 128; tn -= 32) {
+  for (int tn = kTileN; tn >= 128; tn -= P == 2 ? 32 : 128) {
     const int64_t c = ceil_div(n, tn) * (tn + 40);
     if (c < cost) {
       cost = c;
@@ -831,9 +893,21 @@ cudaError_t run_moments(const bergson_muon_tensor* t, const Batch& b, const Batc
                 : launch_dependent(planes_kernel<N, 1>, grid, block, 0, s, p);
 }
 
-struct Maps {
-  CUtensorMap x[2], a, b;
+// An operand's boxes: of the rows as they lie, and across.
+struct Side {
+  CUtensorMap rows, across;
 };
+// Of a group: the first product's operands (by X's buffer), the square's, and the last one's, B and X.
+struct Maps {
+  Side gram_a[2], gram_b[2], square_a, square_b, last_s, last_x[2];
+};
+
+// rows: of a box of rows; chunks: of a box across (0: a chunk at any row).
+bool encode_side(Side* s, const void* ptr, int64_t cols, int64_t rows, int64_t planes, int64_t ld,
+                 int P, int box_rows, int chunks) {
+  return encode_tmap_stack(&s->rows, ptr, cols, rows, planes, ld, box_rows, P) == CUDA_SUCCESS &&
+         encode_tmap_across(&s->across, ptr, cols, rows, planes, ld, P, chunks) == CUDA_SUCCESS;
+}
 
 template <int P, int G, int N>
 cudaError_t run_products(const bergson_muon_tensor* t, const Batch& b, const BatchLayout& l,
@@ -849,11 +923,26 @@ cudaError_t run_products(const bergson_muon_tensor* t, const Batch& b, const Bat
     const Planes& pl = l.shapes[k];
     const int64_t m = std::min(sh.rows, sh.cols), n = static_cast<int64_t>(sh.mats.size()) * P;
     Maps& mp = maps[k];
-    if (encode_tmap_stack(&mp.x[0], ws + pl.x[0], sh.cols, sh.rows, n, pl.x_ld, kBox) != CUDA_SUCCESS ||
-        encode_tmap_stack(&mp.x[1], ws + pl.x[1], sh.cols, sh.rows, n, pl.x_ld, kBox) != CUDA_SUCCESS ||
-        encode_tmap_stack(&mp.a, ws + pl.a, m, m, n, pl.s_ld, kBox) != CUDA_SUCCESS ||
-        encode_tmap_stack(&mp.b, ws + pl.b, m, m, n, pl.s_ld, kBox) != CUDA_SUCCESS)
-      return cudaErrorInvalidValue;
+    const int tn_s = tile_columns(m, P), tn_x = tile_columns(sh.cols, P);
+    const auto chunks = [](int tn) { return tn % 128 == 0 ? tn / 128 : 0; };
+    bool good = true;
+    for (int i = 0; i < 2; ++i) {
+      const auto x = [&](Side* side, int rows, int ch) {
+        good = good && encode_side(side, ws + pl.x[i], sh.cols, sh.rows, n, pl.x_ld, P, rows, ch);
+      };
+      x(&mp.gram_a[i], kTileM / 2, 2);
+      x(&mp.gram_b[i], tn_s / 2, chunks(tn_s));
+      if (sh.rows > sh.cols) x(&mp.last_x[i], kTileM / 2, 2);
+      else x(&mp.last_x[i], tn_x / 2, chunks(tn_x));
+    }
+    const auto sym = [&](Side* side, size_t at, int rows, int ch) {
+      good = good && encode_side(side, ws + at, m, m, n, pl.s_ld, P, rows, ch);
+    };
+    sym(&mp.square_a, pl.a, kTileM / 2, 2);
+    sym(&mp.square_b, pl.a, tn_s / 2, chunks(tn_s));
+    if (sh.rows > sh.cols) sym(&mp.last_s, pl.b, tn_x / 2, chunks(tn_x));
+    else sym(&mp.last_s, pl.b, kTileM / 2, 2);
+    if (!good) return cudaErrorInvalidValue;
     p.g[k].first_mat = first;
     for (int i : sh.mats) {
       const bergson_muon_tensor& x = t[i];
@@ -876,12 +965,14 @@ cudaError_t run_products(const bergson_muon_tensor* t, const Batch& b, const Bat
     int64_t tiles = 0;
     for (int k = 0; k < p.n; ++k) {
       ProdGroup& g = p.g[k];
-      g.tn = tile_columns(g.N);
+      g.tn = tile_columns(g.N, P);
+      g.chunks_b = g.tn % 128 == 0 ? g.tn / 128 : 0;
+      const int width = ProdCfg<P>::kSub * g.tn;
       g.n_mt = static_cast<int>(ceil_div(g.M, kTileM));
-      g.n_nt = static_cast<int>(ceil_div(g.N, g.tn));
+      g.n_nt = static_cast<int>(ceil_div(g.N, width));
       g.per_mat = 0;
       for (int mt = 0; mt < g.n_mt; ++mt)
-        g.per_mat += g.lower ? static_cast<int>(ceil_div(std::min((mt + 1) * kTileM, g.N), g.tn))
+        g.per_mat += g.lower ? static_cast<int>(ceil_div(std::min((mt + 1) * kTileM, g.N), width))
                              : g.n_nt;
       g.begin = static_cast<int>(tiles);
       tiles += static_cast<int64_t>(g.per_mat) * static_cast<int64_t>(b.shapes[k].mats.size());
@@ -895,7 +986,10 @@ cudaError_t run_products(const bergson_muon_tensor* t, const Batch& b, const Bat
     const double* c = a.coefficients + 3 * it;
     const int cur = it & 1;
     const bool last = it == a.iterations - 1;
-    for (int part = 0; part < 3; ++part) {       // A = X X^T, B = b A + c A^2, X' = a X + B X
+    const double ca = c[0], cb = c[1], cc = c[2];
+    const double h = cc != 0.0 ? cb / (2.0 * cc) : 0.0;
+    for (int part = 0; part < 3; ++part) {       // A' = X X^T + h I, B = c A'^2 + .., X' = B X
+      if (part == 1 && cc == 0.0) continue;
       for (int k = 0; k < p.n; ++k) {
         const Shape& sh = b.shapes[k];
         const Planes& pl = l.shapes[k];
@@ -906,35 +1000,37 @@ cudaError_t run_products(const bergson_muon_tensor* t, const Batch& b, const Bat
         g.N = part == 2 ? static_cast<int>(sh.cols) : m;
         g.K = part == 0 ? static_cast<int>(std::max(sh.rows, sh.cols)) : m;
         g.lower = part < 2 ? 1 : 0;
+        g.dst_ld = static_cast<int>(part == 2 ? pl.x_ld : pl.s_ld);
+        g.dst_plane = part == 2 ? pl.x_plane : pl.s_plane;
         const auto at = [&](size_t off) { return reinterpret_cast<__half*>(ws + off); };
+        const auto set = [&](double alpha, double gamma, __half* dst) {
+          g.alpha = static_cast<float>(alpha / kPlaneScale);
+          g.gamma = static_cast<float>(gamma * kPlaneScale);
+          g.dst = dst;
+        };
+        const Maps& mp = maps[k];
+        const auto sides = [&](const Side& a_side, const Side& b_side) {
+          p.a[k] = a_side.rows;
+          p.ax[k] = a_side.across;
+          p.b[k] = b_side.rows;
+          p.bx[k] = b_side.across;
+        };
         if (part == 0) {
-          p.a[k] = p.b[k] = maps[k].x[cur];
+          sides(mp.gram_a[cur], mp.gram_b[cur]);
           g.a_kind = g.b_kind = tall ? kAcross : kRowMajor;
-          g.src = nullptr;
-          g.dst = at(pl.a);
-          g.alpha = 1.0f / kPlaneScale;
-          g.beta = 0.0f;
+          if (cc != 0.0) set(1.0, h, at(pl.a));
+          else set(cb, ca, at(pl.b));
         } else if (part == 1) {
-          p.a[k] = p.b[k] = maps[k].a;
+          sides(mp.square_a, mp.square_b);
           g.a_kind = g.b_kind = kSymmetric;
-          g.src = at(pl.a);
-          g.dst = at(pl.b);
-          g.alpha = static_cast<float>(c[2] / kPlaneScale);
-          g.beta = static_cast<float>(c[1]);
+          set(cc, ca - cc * h * h, at(pl.b));
         } else {
-          p.a[k] = tall ? maps[k].x[cur] : maps[k].b;
-          p.b[k] = tall ? maps[k].b : maps[k].x[cur];
+          if (tall) sides(mp.last_x[cur], mp.last_s);
+          else sides(mp.last_s, mp.last_x[cur]);
           g.a_kind = tall ? kRowMajor : kSymmetric;
           g.b_kind = tall ? kSymmetric : kAcross;
-          g.src = at(pl.x[cur]);
-          g.dst = last ? nullptr : at(pl.x[cur ^ 1]);
-          g.alpha = 1.0f / kPlaneScale;
-          g.beta = static_cast<float>(c[0]);
+          set(1.0, 0.0, last ? nullptr : at(pl.x[cur ^ 1]));
         }
-        g.src_ld = static_cast<int>(part == 2 ? pl.x_ld : pl.s_ld);
-        g.src_plane = part == 2 ? pl.x_plane : pl.s_plane;
-        g.dst_ld = g.src_ld;
-        g.dst_plane = g.src_plane;
       }
       e = run();
       if (e != cudaSuccess) return e;

@@ -152,43 +152,43 @@ int check_muon_matrices(const bergson_muon_tensor* tensors, int n_tensors, int p
   return BERGSON_OK;
 }
 
-// The largest |p(y)| x^odd of polynomials in y = x^2 on [0, top]: at the ends, or where the
-// derivative is 0.  odd: of a x + b x^3 + c x^5, else of b y + c y^2.
+// The largest sqrt(y)^odd |a + b y + c y^2| on [0, top]: at an end, or where the derivative is 0.
 double largest(double a, double b, double c, bool odd, double top) {
-  const auto f = [&](double y) {
-    return odd ? std::sqrt(y) * std::fabs(a + y * (b + y * c)) : std::fabs(y * (b + y * c));
-  };
-  double most = f(top * top);
+  const auto f = [&](double y) { return (odd ? std::sqrt(y) : 1.0) * std::fabs(a + y * (b + y * c)); };
+  double most = std::max(f(0.0), f(top));
   const auto at = [&](double y) {
-    if (y > 0.0 && y < top * top) most = std::max(most, f(y));
+    if (y > 0.0 && y < top) most = std::max(most, f(y));
   };
   if (!odd) {
     if (c != 0.0) at(-b / (2.0 * c));
-    return most;
-  }
-  const double d = 9.0 * b * b - 20.0 * a * c;             // a + 3 b y + 5 c y^2 = 0
-  if (c == 0.0) {
+  } else if (c == 0.0) {                                   // a + 3 b y = 0
     if (b != 0.0) at(-a / (3.0 * b));
-  } else if (d >= 0.0) {
-    at((-3.0 * b + std::sqrt(d)) / (10.0 * c));
-    at((-3.0 * b - std::sqrt(d)) / (10.0 * c));
+  } else if (9.0 * b * b >= 20.0 * a * c) {                // a + 3 b y + 5 c y^2 = 0
+    const double root = std::sqrt(9.0 * b * b - 20.0 * a * c);
+    at((-3.0 * b + root) / (10.0 * c));
+    at((-3.0 * b - root) / (10.0 * c));
   }
   return most;
 }
 
-// The planes hold 1024 times X, A and B in fp16: up to 48 of them, 64 and more are infinite.
+// What the planes hold, 1024 times X, A + h I and a I + b A + c A^2 (h = b / 2c), in fp16: up to
+// 48 of them; 64 and more would be infinite.  c h^2 is what the completed square takes off
+// and must not be large either.
 int check_coefficients(const double* k, int n) {
   constexpr double kMost = 48.0;
   if (n < 1 || n > 64) return fail(BERGSON_EINVAL, "n_iterations must be in [1, 64]");
   if (k == nullptr) return fail(BERGSON_EINVAL, "coefficients is NULL");
   double top = 1.01;                                       // of X's singular values, with room for roundings
   for (int i = 0; i < n; ++i, k += 3) {
-    if (!std::isfinite(k[0]) || !std::isfinite(k[1]) || !std::isfinite(k[2]))
+    const double a = k[0], b = k[1], c = k[2], h = c != 0.0 ? b / (2.0 * c) : 0.0;
+    if (!std::isfinite(a) || !std::isfinite(b) || !std::isfinite(c))
       return fail(BERGSON_EINVAL, "coefficients must be finite");
-    const double next = 1.01 * largest(k[0], k[1], k[2], true, top);
-    if (!(top * top <= kMost) || !(largest(0.0, k[1], k[2], false, top) <= kMost) ||
+    const double next = 1.01 * largest(a, b, c, true, top * top);
+    if (!(std::max(std::fabs(h), std::fabs(top * top + h)) <= kMost) ||
+        !(std::fabs(c * h * h) <= kMost) || !(largest(a, b, c, false, top * top) <= kMost) ||
         !(next <= kMost))
-      return fail(BERGSON_EUNSUPPORTED, "iteration %d: the coefficients let X, A or B pass 48", i);
+      return fail(BERGSON_EUNSUPPORTED,
+                  "iteration %d: the coefficients let X or a polynomial of A pass 48", i);
     top = next;
   }
   return BERGSON_OK;

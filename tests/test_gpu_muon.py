@@ -1,14 +1,16 @@
 """GPU parity of the Muon step with the fp64 oracle.
 
 Tolerances of the orthogonalised update X.  How roundings grow over the iterations
-follows from the singular values, so the oracle carries them: it repeats the
-iteration with what an operand holds rounded as the kernels round it (one fp16 plane,
-or two, of 1024 times the value), with every product in fp32 (whose random roundings are
-those of sums of any order), and with every product lowered by the most that sums
-rounded toward zero lose: a chain of 12 MMAs of 16 products each, 2^-23 each with two
-planes; K / 16 of them with one.  The three deviations from the exact X, added, are
-allowed four times over in the Frobenius norm, and that norm's eight times the share of an
-entry in any entry.  m takes two roundings; a weight two more and half a unit of its type.
+follows from the singular values, so they are carried through the iteration as the kernels
+take it (A + h I, c (..)^2 + (a - c h^2) I with h = b / 2c, times X): with what an operand holds
+rounded as the kernels round it (one fp16 plane, or two, of 1024 times the value), with
+every product in fp32 (whose random roundings are those of sums of any order), and with
+every product lowered by what sums rounded toward zero lose: n MMAs one after the
+other round partial sums, half of the whole on average, by up to 2^-23 each, and n is 12 a
+stage of 64 columns and 48 at most with two planes, 4 a stage with one.  The deviations
+from the exact X, added, are allowed four times over in the Frobenius norm, and that norm's
+eight times the share of an entry in any entry.  m takes two roundings; a weight two more and
+half a unit of its type.
 """
 import numpy as np
 import pytest
@@ -50,14 +52,34 @@ def hold(planes):
     return f
 
 
+def carried(u, k, hold=lambda x, inner=0: x, product=lambda p, inner: p):
+    n = np.linalg.norm(u)
+    x = hold(u / n if n > 0 else np.zeros_like(u))
+    tall, one = u.shape[0] > u.shape[1], np.eye(min(u.shape))
+    for a, b, c in k:
+        y = x.T if tall else x
+        g = product(y @ y.T, y.shape[1])
+        h = b / (2 * c) if c != 0 else 0.0
+        if c != 0:
+            s = hold(g + h * one)
+            q = hold(c * product(s @ s, len(s)) + (a - c * h * h) * one)
+        else:
+            q = hold(b * g + a * one)
+        x = hold(product(x @ q if tall else q @ x, len(q)))
+    return x
+
+
 def x_error(u, k, products):
     """(X, its allowed deviation in the Frobenius norm)."""
     x = orc.newton_schulz(u, k)
     planes = 2 if products == 3 else 1
-    lost = (12 if planes == 2 else 12 + max(u.shape) / 16) * 2.0 ** -23
-    e = [np.linalg.norm(orc.newton_schulz(u, k, **kw) - x) for kw in (
-        dict(hold=hold(planes)), dict(product=lambda p: p.astype(np.float32).astype(np.float64)),
-        dict(product=lambda p: p * (1 - lost)))]
+
+    def lowered(p, inner):
+        stages = -(-inner // 64)
+        return p * (1 - 0.5 * (min(12 * stages, 48) if planes == 2 else 4 * stages) * 2.0 ** -23)
+    e = [np.linalg.norm(carried(u, k, **kw) - x) for kw in (
+        dict(hold=hold(planes)), dict(product=lambda p, _: p.astype(np.float32).astype(np.float64)),
+        dict(product=lowered))]
     n = np.linalg.norm(u)
     xf = (u / n if n > 0 else u).astype(np.float32)
     for a, b, c in np.float32(k):
