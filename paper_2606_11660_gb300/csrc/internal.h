@@ -419,5 +419,8 @@ CUresult encode_tmap_stack(CUtensorMap* tm, const void* ptr, int64_t inner, int6
                            int64_t planes, int64_t ld, int box_outer, int box_planes);
 CUresult encode_tmap_across(CUtensorMap* tm, const void* ptr, int64_t inner, int64_t outer,
                             int64_t planes, int64_t ld, int box_planes, int chunks);
+// Of stores to them: boxes of 32 columns and rows, 64-byte swizzle.
+CUresult encode_tmap_out(CUtensorMap* tm, const void* ptr, int64_t inner, int64_t outer,
+                         int64_t planes, int64_t ld);
 
 }  // namespace bergson

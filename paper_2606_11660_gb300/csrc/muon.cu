@@ -230,6 +230,7 @@ constexpr int kPlaneBytes = 2 * kBoxBytes;     // of 128 rows of an operand's pl
 constexpr int kEpilogueWarps = 16;             // four to a quarter of the rows: 64 columns a thread
 constexpr int kThreads = 32 * (3 + kEpilogueWarps);    // A's loads, MMA, B's loads, epilogue
 constexpr int kChain = 4;                      // stages of an accumulation chain with two planes
+constexpr int kOutTile = 32 * 64;              // bytes
 constexpr int kBarBytes = 256;
 constexpr int kTmemCols = 2 * kTileN;          // two accumulators
 constexpr uint64_t kDrainTimeoutNs = 2000000000ull;
@@ -243,7 +244,9 @@ struct ProdCfg {
   static constexpr int kABytes = P * kPlaneBytes;
   static constexpr int kStageBytes = kABytes + kSub * P * kPlaneBytes;
   static constexpr int kStages = P == 2 ? 3 : 4;
-  static constexpr int kSmemBytes = 1024 + kStages * kStageBytes + kBarBytes;
+  // one plane: a warp's 32 rows and columns on their way out
+  static constexpr int kOutBytes = P == 2 ? 0 : kEpilogueWarps * kOutTile;
+  static constexpr int kSmemBytes = 1024 + kStages * kStageBytes + kOutBytes + kBarBytes;
 };
 
 // How an operand [rows, K] of a product lies in memory.
@@ -276,6 +279,7 @@ template <int G, int N>
 struct ProdParams {
   CUtensorMap a[G], b[G];      // boxes of rows as they lie
   CUtensorMap ax[G], bx[G];    // and across
+  CUtensorMap out[G];          // D', boxes of 32 rows and columns (one plane)
   ProdGroup g[G];
   WeightEntry w[N];
   int n;
@@ -459,18 +463,36 @@ __device__ __forceinline__ void update_weights(const WeightEntry& w, float ortho
                                                const float* v) {
   const bool wide = w.master != nullptr || w.pt == BERGSON_F32;
   float* f = w.master != nullptr ? w.master : static_cast<float*>(w.p);
+  if (w.vec && !wide) {
+    uint32_t r[8];
+    uint16_t* q = static_cast<uint16_t*>(w.p) + at;
+    load32(q, r);
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      uint4 u = make_uint4(r[k], 0, 0, 0);
+      float2 y = w.pt == BERGSON_BF16 ? unpack2(u, 0, static_cast<__nv_bfloat16*>(nullptr))
+                                      : unpack2(u, 0, static_cast<__half*>(nullptr));
+      y.x = fmaf(-ortho, v[2 * k], fmaf(-w.lr_decay, y.x, y.x));
+      y.y = fmaf(-ortho, v[2 * k + 1], fmaf(-w.lr_decay, y.y, y.y));
+      if (w.pt == BERGSON_BF16) pack2(u, 0, y, static_cast<__nv_bfloat16*>(nullptr));
+      else pack2(u, 0, y, static_cast<__half*>(nullptr));
+      r[k] = u.x;
+    }
+    store32(q, r);
+    return;
+  }
   if (w.vec) {
 #pragma unroll
     for (int h = 0; h < 16; h += 8) {
       float x[8];
-      load_eight(wide ? f : w.p, wide ? BERGSON_F32 : w.pt, true, at + h, at + h + 8, x);
+      load_eight(f, BERGSON_F32, true, at + h, at + h + 8, x);
       uint32_t r[8];
 #pragma unroll
       for (int k = 0; k < 8; ++k) {
         x[k] = fmaf(-ortho, v[h + k], fmaf(-w.lr_decay, x[k], x[k]));
         r[k] = __float_as_uint(x[k]);
       }
-      if (wide) store32(f + at + h, r);
+      store32(f + at + h, r);
       if (w.pt == BERGSON_F32) {
         if (w.master != nullptr) store32(static_cast<float*>(w.p) + at + h, r);
         continue;
@@ -507,22 +529,19 @@ __device__ __forceinline__ void prefetch_weights(const WeightEntry& w, int64_t a
   for (int i = 0; i < n * size; i += 128) asm volatile("prefetch.global.L2 [%0];" ::"l"(p + i));
 }
 
-// 16 columns of a row: D' to its planes.
-template <int P>
-__device__ __forceinline__ void put_planes(const ProdGroup& g, __half* d, const float* v) {
+// 16 columns of a row to their two planes.
+__device__ __forceinline__ void put_planes(__half* d, int64_t plane, const float* v) {
   uint32_t hi[8], lo[8];
 #pragma unroll
   for (int k = 0; k < 8; ++k) {
     const __half2 h = __floats2half2_rn(v[2 * k], v[2 * k + 1]);
+    const float2 f = __half22float2(h);
+    const __half2 l = __floats2half2_rn(v[2 * k] - f.x, v[2 * k + 1] - f.y);
     hi[k] = *reinterpret_cast<const uint32_t*>(&h);
-    if (P == 2) {
-      const float2 f = __half22float2(h);
-      const __half2 l = __floats2half2_rn(v[2 * k] - f.x, v[2 * k + 1] - f.y);
-      lo[k] = *reinterpret_cast<const uint32_t*>(&l);
-    }
+    lo[k] = *reinterpret_cast<const uint32_t*>(&l);
   }
   store32(d, hi);
-  if (P == 2) store32(d + g.dst_plane, lo);
+  store32(d + plane, lo);
 }
 
 // D[i, j] = alpha <a_i, b_j> + gamma [i == j] over persistent CTA pairs, synchronised
@@ -542,7 +561,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) &
                                              ~static_cast<uintptr_t>(1023));
   const uint32_t sbase = smem_u32(smem);
-  uint64_t* full = reinterpret_cast<uint64_t*>(smem + C::kStages * C::kStageBytes);
+  uint64_t* full =
+      reinterpret_cast<uint64_t*>(smem + C::kStages * C::kStageBytes + C::kOutBytes);
   uint64_t* empty = full + C::kStages;
   uint64_t* tfull = empty + C::kStages;
   uint64_t* tempty = tfull + 2;
@@ -606,18 +626,11 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
         const int xb_from = across_from(g.b_kind, o.nt * C::kSub * tn);
         const uint32_t base_idesc = make_idesc_f16(kTileM, tn, false);
         bool fresh = true;                           // the accumulators hold nothing yet
-        for (int kc = 0; kc < stages; ++kc) {
-          ok = warp_wait(smem_u32(&full[stage]), ph, tmo, s_abort);
-          if (!ok) break;
-          const bool xa = kc >= xa_from, xb = kc >= xb_from;
-          const uint32_t sa = sbase + stage * C::kStageBytes;
-          const uint32_t da = desc_low<P>(sa, xa);
-          // 16 columns of K: 32 bytes of a row, or 16 rows of 128 bytes
-          const uint32_t step_a = xa ? 128 : 2, step_b = xb ? 128 : 2;
-          const uint32_t plane_a = (xa ? kBoxBytes : kPlaneBytes) / 16;
-          const uint32_t plane_b = (xb ? kBoxBytes : tn / 2 * 128) / 16;
-          const uint32_t idesc = base_idesc | (xa ? 1u << 15 : 0u) | (xb ? 1u << 16 : 0u);
-          const bool ends = kc + 1 == stages || (P == 2 && kc % kChain == kChain - 1);
+        // A tile of two accumulators begins with a ring of stages for the first and then for the
+        // second, which the epilogue is still reading at that time.
+        for (int kb = 0, len; ok && kb < stages; kb += len) {
+          len = C::kSub == 2 && kb == 0 && subs == 2 ? min(C::kStages, stages) : 1;
+          const bool ends = kb + len == stages || (P == 2 && kb % kChain == kChain - 1);
           int cab = ab;
           uint32_t caph = aph;
 #pragma unroll
@@ -627,30 +640,51 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
               ok = warp_wait(smem_u32(&tempty[cab]), caph ^ 1, tmo, s_abort);
               if (!ok) break;
             }
-            tc_fence_after();
-            if (lead) {
-              const uint32_t db = desc_low<P>(sa + C::kABytes + h * P * kPlaneBytes, xb);
-              const uint32_t d = tmem + cab * kTileN;
-              constexpr int kTerms = P == 2 ? 3 : 1;
-#pragma unroll
-              for (int q = 0; q < kTerms; ++q) {     // lo hi, hi lo, hi hi
-                const uint32_t at = da + (P == 2 && q == 0 ? plane_a : 0);
-                const uint32_t bt = db + (P == 2 && q == 1 ? plane_b : 0);
-#pragma unroll
-                for (int kk = 0; kk < kTileK / 16; ++kk)
-                  umma_pair_low(d, at + kk * step_a, bt + kk * step_b, idesc,
-                                !fresh || q != 0 || kk != 0);
+            int st = stage;
+            uint32_t sph = ph;
+            for (int kc = kb; kc < kb + len; ++kc) {
+              if (h == 0) {
+                ok = warp_wait(smem_u32(&full[st]), sph, tmo, s_abort);
+                if (!ok) break;
               }
-              if (ends) umma_commit_pair(smem_u32(&tfull[cab]), 0x3);
-              if (h == subs - 1) umma_commit_pair(smem_u32(&empty[stage]), 0x3);
+              const bool xa = kc >= xa_from, xb = kc >= xb_from;
+              tc_fence_after();
+              if (lead) {
+                const uint32_t sa = sbase + st * C::kStageBytes;
+                const uint32_t da = desc_low<P>(sa, xa);
+                const uint32_t db = desc_low<P>(sa + C::kABytes + h * P * kPlaneBytes, xb);
+                // 16 columns of K: 32 bytes of a row, or 16 rows of 128 bytes
+                const uint32_t step_a = xa ? 128 : 2, step_b = xb ? 128 : 2;
+                const uint32_t plane_a = (xa ? kBoxBytes : kPlaneBytes) / 16;
+                const uint32_t plane_b = (xb ? kBoxBytes : tn / 2 * 128) / 16;
+                const uint32_t idesc = base_idesc | (xa ? 1u << 15 : 0u) | (xb ? 1u << 16 : 0u);
+                const uint32_t d = tmem + cab * kTileN;
+                const bool first = fresh && kc == kb;
+                constexpr int kTerms = P == 2 ? 3 : 1;
+#pragma unroll
+                for (int q = 0; q < kTerms; ++q) {   // lo hi, hi lo, hi hi
+                  const uint32_t at = da + (P == 2 && q == 0 ? plane_a : 0);
+                  const uint32_t bt = db + (P == 2 && q == 1 ? plane_b : 0);
+#pragma unroll
+                  for (int kk = 0; kk < kTileK / 16; ++kk)
+                    umma_pair_low(d, at + kk * step_a, bt + kk * step_b, idesc,
+                                  !first || q != 0 || kk != 0);
+                }
+                // a commit stands with its MMAs, in the branch of the lane that issued them
+                if (ends && kc == kb + len - 1) umma_commit_pair(smem_u32(&tfull[cab]), 0x3);
+                if (h == subs - 1) umma_commit_pair(smem_u32(&empty[st]), 0x3);
+              }
+              __syncwarp();
+              if (++st == C::kStages) { st = 0; sph ^= 1; }
             }
-            __syncwarp();
+            if (!ok) break;
             if (++cab == 2) { cab = 0; caph ^= 1; }
           }
           if (!ok) break;
           fresh = ends;
           if (ends) { ab = cab; aph = caph; }
-          if (++stage == C::kStages) { stage = 0; ph ^= 1; }
+          stage += len;
+          if (stage >= C::kStages) { stage -= C::kStages; ph ^= 1; }
         }
       }
       if (lead) {
@@ -667,6 +701,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
     // writes whole 32-byte sectors of its row.
     const int ew = warp - 3;
     const int quarter = warp & 3;
+    uint8_t* out = smem + C::kStages * C::kStageBytes + ew * kOutTile;
     int ab = 0;
     uint32_t aph = 0;
     bool aborted = false;
@@ -685,8 +720,10 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
         if (g.dst == nullptr && left > 0) prefetch_weights(w, at, left);
         constexpr int kAcc = kTileN / 4;
         float acc[kAcc];
+        if constexpr (P == 2) {
 #pragma unroll
-        for (int j = 0; j < kAcc; ++j) acc[j] = 0.0f;    // 0 + v = v: the first chain lands unchanged
+          for (int j = 0; j < kAcc; ++j) acc[j] = 0.0f;  // 0 + v = v: the first chain lands unchanged
+        }
         for (int ch = 0; ch < chains; ++ch) {
           if (!warp_wait(smem_u32(&tfull[ab]), aph, tmo, s_abort)) {
             raise_device_error(p.status, s_abort, kStatusTimeout);
@@ -696,13 +733,22 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
           tc_fence_after();
           const uint32_t tb = tmem + (static_cast<uint32_t>(32 * quarter) << 16) + ab * kTileN +
                               16 * first;
+          if constexpr (P == 1) {                    // 32 columns or 64
+            tmem_ld64(tb, acc);
+          } else {
 #pragma unroll
-          for (int u = 0; u < 4; ++u) {
-            if (u < mine) {
-              float v[16];
-              tmem_ld16(tb + 16 * u, v);
+            for (int u = 0; u < 4; u += 2) {
+              if (u < mine) {                        // 16 columns more than asked for at most
+                float v[32];
+                tmem_ld32(tb + 16 * u, v);
 #pragma unroll
-              for (int j = 0; j < 16; ++j) acc[16 * u + j] += v[j];
+                for (int j = 0; j < 32; j += 2) {
+                  const float2 x = add2(make_float2(acc[16 * u + j], acc[16 * u + j + 1]),
+                                        make_float2(v[j], v[j + 1]));
+                  acc[16 * u + j] = x.x;
+                  acc[16 * u + j + 1] = x.y;
+                }
+              }
             }
           }
           tc_fence_before();
@@ -712,18 +758,53 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
         }
         if (aborted) break;
         if (g.dst != nullptr) {
-          __half* d = g.dst + static_cast<int64_t>(o.mat) * P * g.dst_plane +
-                      static_cast<int64_t>(row) * g.dst_ld + col0;
-          const float gamma = g.gamma, alpha = g.alpha;
+          const float2 alpha = pair(g.alpha);
 #pragma unroll
-          for (int u = 0; u < 4; ++u) {
-            if (16 * u >= left) break;
+          for (int j = 0; j < kAcc; j += 2) {
+            const float2 x = mul2(make_float2(acc[j], acc[j + 1]), alpha);
+            acc[j] = x.x;
+            acc[j + 1] = x.y;
+          }
+          const int row0 = row - lane;
+          if (g.gamma != 0.0f && row0 < col0 + kAcc && row0 + 32 > col0) {     // on the diagonal
+            const float gamma = g.gamma;
 #pragma unroll
-            for (int j = 0; j < 16; ++j) {
-              acc[16 * u + j] *= alpha;
-              if (gamma != 0.0f && row == col0 + 16 * u + j) acc[16 * u + j] += gamma;
+            for (int j = 0; j < kAcc; ++j) acc[j] += row == col0 + j ? gamma : 0.0f;
+          }
+          if constexpr (P == 1) {
+#pragma unroll
+            for (int u = 0; u < 4; u += 2) {
+              if (u >= mine) break;
+              if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
+              __syncwarp();
+#pragma unroll
+              for (int c = 0; c < 4; ++c) {          // 8 columns each, 64-byte swizzle
+                uint4 v;
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                  pack2(v, j, make_float2(acc[16 * u + 8 * c + 2 * j], acc[16 * u + 8 * c + 2 * j + 1]),
+                        static_cast<const __half*>(nullptr));
+                *reinterpret_cast<uint4*>(out + 64 * lane + 16 * (c ^ ((lane >> 1) & 3))) = v;
+              }
+              fence_proxy_async_smem();
+              __syncwarp();
+              if (lane == 0 && row0 < g.M && col0 + 16 * u < g.N) {
+                asm volatile(
+                    "cp.async.bulk.tensor.3d.global.shared::cta.bulk_group [%0, {%2, %3, %4}], [%1];"
+                    ::"l"(&p.out[o.group]), "r"(smem_u32(out)), "r"(col0 + 16 * u), "r"(row0),
+                      "r"(o.mat)
+                    : "memory");
+                asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+              }
             }
-            put_planes<P>(g, d + 16 * u, acc + 16 * u);
+          } else {
+            __half* d = g.dst + static_cast<int64_t>(o.mat) * P * g.dst_plane +
+                        static_cast<int64_t>(row) * g.dst_ld + col0;
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+              if (16 * u >= left) break;
+              put_planes(d + 16 * u, g.dst_plane, acc + 16 * u);
+            }
           }
         } else {
           const float ortho = w.lr_ortho * g.alpha;
@@ -736,6 +817,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
         __syncwarp();
       }
     }
+    if (P == 1 && lane == 0) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
+    __syncwarp();
   }
 
   tc_fence_before();
@@ -838,13 +921,16 @@ BatchLayout layout_of(const Batch& b, int P) {
   return l;
 }
 
-// Columns of an accumulator: what wastes least of the last one.  One pays some 40 columns' time
-// beside its own.  With one plane they are whole chunks.
-int tile_columns(int64_t n, int P) {
+// Columns of an accumulator for D [m, n] (lower: the tiles that reach the diagonal or lie below):
+// what computes least that is not needed.  An accumulator pays some 40 columns' time beside its
+// own.  With one plane they are whole chunks.
+int tile_columns(int64_t m, int64_t n, bool lower, int P) {
   int best = kTileN;
   int64_t cost = INT64_MAX;
   for (int tn = kTileN; tn >= 128; tn -= P == 2 ? 32 : 128) {
-    const int64_t c = ceil_div(n, tn) * (tn + 40);
+    int64_t c = 0;
+    for (int64_t r = kTileM; r < m + kTileM; r += kTileM)
+      c += ceil_div(lower ? std::min(r, n) : n, tn) * (tn + 40);
     if (c < cost) {
       cost = c;
       best = tn;
@@ -900,6 +986,7 @@ struct Side {
 // Of a group: the first product's operands (by X's buffer), the square's, and the last one's, B and X.
 struct Maps {
   Side gram_a[2], gram_b[2], square_a, square_b, last_s, last_x[2];
+  CUtensorMap x_out[2], a_out, b_out;
 };
 
 // rows: of a box of rows; chunks: of a box across (0: a chunk at any row).
@@ -923,13 +1010,15 @@ cudaError_t run_products(const bergson_muon_tensor* t, const Batch& b, const Bat
     const Planes& pl = l.shapes[k];
     const int64_t m = std::min(sh.rows, sh.cols), n = static_cast<int64_t>(sh.mats.size()) * P;
     Maps& mp = maps[k];
-    const int tn_s = tile_columns(m, P), tn_x = tile_columns(sh.cols, P);
+    const int tn_s = tile_columns(m, m, true, P), tn_x = tile_columns(sh.rows, sh.cols, false, P);
     const auto chunks = [](int tn) { return tn % 128 == 0 ? tn / 128 : 0; };
     bool good = true;
     for (int i = 0; i < 2; ++i) {
       const auto x = [&](Side* side, int rows, int ch) {
         good = good && encode_side(side, ws + pl.x[i], sh.cols, sh.rows, n, pl.x_ld, P, rows, ch);
       };
+      good = good && encode_tmap_out(&mp.x_out[i], ws + pl.x[i], sh.cols, sh.rows, n, pl.x_ld) ==
+                         CUDA_SUCCESS;
       x(&mp.gram_a[i], kTileM / 2, 2);
       x(&mp.gram_b[i], tn_s / 2, chunks(tn_s));
       if (sh.rows > sh.cols) x(&mp.last_x[i], kTileM / 2, 2);
@@ -942,6 +1031,8 @@ cudaError_t run_products(const bergson_muon_tensor* t, const Batch& b, const Bat
     sym(&mp.square_b, pl.a, tn_s / 2, chunks(tn_s));
     if (sh.rows > sh.cols) sym(&mp.last_s, pl.b, tn_x / 2, chunks(tn_x));
     else sym(&mp.last_s, pl.b, kTileM / 2, 2);
+    good = good && encode_tmap_out(&mp.a_out, ws + pl.a, m, m, n, pl.s_ld) == CUDA_SUCCESS &&
+           encode_tmap_out(&mp.b_out, ws + pl.b, m, m, n, pl.s_ld) == CUDA_SUCCESS;
     if (!good) return cudaErrorInvalidValue;
     p.g[k].first_mat = first;
     for (int i : sh.mats) {
@@ -965,7 +1056,7 @@ cudaError_t run_products(const bergson_muon_tensor* t, const Batch& b, const Bat
     int64_t tiles = 0;
     for (int k = 0; k < p.n; ++k) {
       ProdGroup& g = p.g[k];
-      g.tn = tile_columns(g.N, P);
+      g.tn = tile_columns(g.M, g.N, g.lower != 0, P);
       g.chunks_b = g.tn % 128 == 0 ? g.tn / 128 : 0;
       const int width = ProdCfg<P>::kSub * g.tn;
       g.n_mt = static_cast<int>(ceil_div(g.M, kTileM));
@@ -1017,14 +1108,17 @@ cudaError_t run_products(const bergson_muon_tensor* t, const Batch& b, const Bat
         };
         if (part == 0) {
           sides(mp.gram_a[cur], mp.gram_b[cur]);
+          p.out[k] = cc != 0.0 ? mp.a_out : mp.b_out;
           g.a_kind = g.b_kind = tall ? kAcross : kRowMajor;
           if (cc != 0.0) set(1.0, h, at(pl.a));
           else set(cb, ca, at(pl.b));
         } else if (part == 1) {
           sides(mp.square_a, mp.square_b);
+          p.out[k] = mp.b_out;
           g.a_kind = g.b_kind = kSymmetric;
           set(cc, ca - cc * h * h, at(pl.b));
         } else {
+          p.out[k] = mp.x_out[cur ^ 1];
           if (tall) sides(mp.last_x[cur], mp.last_s);
           else sides(mp.last_s, mp.last_x[cur]);
           g.a_kind = tall ? kRowMajor : kSymmetric;
