@@ -23,8 +23,7 @@
 // groups, by persistent CTA pairs with 256-row tiles, longest products first.  An
 // operand is read with its rows as they lie (K-major) or across (MN-major) by the tensor cores'
 // own descriptors.  A and B are symmetric: only tiles on and below the diagonal are
-// computed and stored, and a read above it takes the mirror image across.  The last
-// product's epilogue updates the weights.
+// computed and stored, and a read above it takes the mirror image across.
 
 #include <algorithm>
 #include <cmath>
@@ -57,7 +56,17 @@ struct MomentEntry {
   int64_t n, plane;            // elements; planes apart
   int32_t cols, ld;
   int32_t gt;
-  int32_t vec;                 // g and m take vectors of 8
+  int32_t vec;                 // g and m take vectors of 8, and rows are whole ones
+};
+struct WeightEntry {
+  void* p;
+  float* master;
+  const __half* x;
+  int64_t n, plane;
+  int32_t cols, ld;
+  float lr_ortho, lr_decay;    // lr lr_scale ortho_scale / 1024, lr lr_scale weight_decay
+  int32_t pt;
+  int32_t vec;
 };
 
 template <int N>
@@ -71,9 +80,16 @@ struct MomentParams {
   uint32_t begin[N + 1];       // first CTA of each matrix
   MomentEntry e[N];
 };
-
 template <int N>
-__device__ __forceinline__ int entry_of(const MomentParams<N>& p) {
+struct WeightParams {
+  int n;
+  int64_t chunk;
+  uint32_t begin[N + 1];
+  WeightEntry e[N];
+};
+
+template <typename Params>
+__device__ __forceinline__ int entry_of(const Params& p) {
   int lo = 0, hi = p.n;
   while (hi - lo > 1) {
     const int mid = (lo + hi) / 2;
@@ -107,6 +123,29 @@ __device__ __forceinline__ void load_eight(const void* p, int type, bool vec, in
   for (int k = 0; k < 8; ++k) x[k] = i + k < n ? load_any(p, type, i + k) : 0.0f;
 }
 
+// Where a thread's 8 elements of a CTA's 2048 stand: side by side in vectors, else 256 apart, so that
+// neighbouring threads take neighbouring elements.
+__device__ __forceinline__ int64_t place(bool vec, int64_t at, int k) {
+  return vec ? at + 8 * threadIdx.x + k : at + threadIdx.x + static_cast<int64_t>(kMomentThreads) * k;
+}
+__device__ __forceinline__ void load_turn(const void* p, int type, bool vec, int64_t at, int64_t n,
+                                          float (&x)[8]) {
+  if (vec) {
+    load_eight(p, type, true, place(true, at, 0), n, x);
+    return;
+  }
+#pragma unroll
+  for (int k = 0; k < 8; ++k) {
+    const int64_t i = place(false, at, k);
+    x[k] = i < n ? load_any(p, type, i) : 0.0f;
+  }
+}
+// Where element i of a matrix stands in its planes.
+__device__ __forceinline__ int64_t in_plane(int64_t i, int cols, int ld) {
+  const int64_t row = i <= INT32_MAX ? static_cast<uint32_t>(i) / static_cast<uint32_t>(cols) : i / cols;
+  return row * ld + (i - row * cols);
+}
+
 // m's update and the sums of u's squares, of 2^50 u and of 2^-50 u: one of them holds the norm
 // of any u that fp32 does.
 template <int N>
@@ -120,10 +159,10 @@ __global__ void __launch_bounds__(kMomentThreads) moment_kernel(
   const int64_t begin = static_cast<int64_t>(blockIdx.x - p.begin[k]) * p.chunk;
   const int64_t end = min(begin + p.chunk, e.n);
   CompensatedSum up, down;
-  for (int64_t i = begin + 8 * threadIdx.x; i < end; i += kMomentChunk) {
+  for (int64_t at = begin; at < end; at += kMomentChunk) {
     float g[8], m[8];
-    load_eight(e.g, e.gt, e.vec, i, e.n, g);
-    load_eight(e.m, BERGSON_F32, e.vec, i, e.n, m);
+    load_turn(e.g, e.gt, e.vec, at, end, g);
+    load_turn(e.m, BERGSON_F32, e.vec, at, end, m);
     float su = 0.0f, sd = 0.0f;
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
@@ -135,15 +174,17 @@ __global__ void __launch_bounds__(kMomentThreads) moment_kernel(
     }
     up.add(su);
     down.add(sd);
-    if (e.vec && i + 8 <= e.n) {
-      uint32_t r[8];
+    if (e.vec) {
+      if (place(true, at, 0) < end) {
+        uint32_t r[8];
 #pragma unroll
-      for (int j = 0; j < 8; ++j) r[j] = __float_as_uint(m[j]);
-      store32(e.m + i, r);
+        for (int j = 0; j < 8; ++j) r[j] = __float_as_uint(m[j]);
+        store32(e.m + place(true, at, 0), r);
+      }
     } else {
 #pragma unroll
       for (int j = 0; j < 8; ++j)
-        if (i + j < e.n) e.m[i + j] = m[j];
+        if (place(false, at, j) < end) e.m[place(false, at, j)] = m[j];
     }
   }
   const float a = block_sum(up.s, red[0]), b = block_sum(down.s, red[1]);
@@ -171,51 +212,110 @@ __global__ void __launch_bounds__(kMomentThreads) planes_kernel(
   const float gs = p.grad_scale != nullptr ? *p.grad_scale : 1.0f;
   const int64_t begin = static_cast<int64_t>(blockIdx.x - p.begin[k]) * p.chunk;
   const int64_t end = min(begin + p.chunk, e.n);
-  for (int64_t i = begin + 8 * threadIdx.x; i < end; i += kMomentChunk) {
+  for (int64_t at = begin; at < end; at += kMomentChunk) {
     float u[8];
-    load_eight(e.m, BERGSON_F32, e.vec, i, e.n, u);
+    load_turn(e.m, BERGSON_F32, e.vec, at, end, u);
     if (p.nesterov) {
       float g[8];
-      load_eight(e.g, e.gt, e.vec, i, e.n, g);
+      load_turn(e.g, e.gt, e.vec, at, end, g);
 #pragma unroll
       for (int j = 0; j < 8; ++j) u[j] = fmaf(p.beta, u[j], p.alpha * (g[j] * gs));
     }
-    __half hi[8], lo[8];
+    if (e.vec) {                                 // the eight are of one row
+      const int64_t i = place(true, at, 0);
+      if (i >= end) continue;
+      uint4 hi, lo;
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      const float v = u[j] * scale;
-      hi[j] = __float2half_rn(v);
-      lo[j] = __float2half_rn(v - __half2float(hi[j]));
-    }
-    int64_t row = i / e.cols;
-    int col = static_cast<int>(i - row * e.cols);
-    if (e.cols % 8 == 0) {                       // the eight are of one row
-      __half* x = e.x + row * e.ld + col;
-      uint4 w;
-#pragma unroll
-      for (int j = 0; j < 4; ++j)
-        set_word(w, j, static_cast<uint32_t>(__half_as_ushort(hi[2 * j])) |
-                           static_cast<uint32_t>(__half_as_ushort(hi[2 * j + 1])) << 16);
-      *reinterpret_cast<uint4*>(x) = w;
-      if (P == 2) {
-#pragma unroll
-        for (int j = 0; j < 4; ++j)
-          set_word(w, j, static_cast<uint32_t>(__half_as_ushort(lo[2 * j])) |
-                             static_cast<uint32_t>(__half_as_ushort(lo[2 * j + 1])) << 16);
-        *reinterpret_cast<uint4*>(x + e.plane) = w;
+      for (int j = 0; j < 4; ++j) {
+        const float2 v = make_float2(u[2 * j] * scale, u[2 * j + 1] * scale);
+        pack2(hi, j, v, static_cast<const __half*>(nullptr));
+        const float2 h = unpack2(hi, j, static_cast<const __half*>(nullptr));
+        pack2(lo, j, make_float2(v.x - h.x, v.y - h.y), static_cast<const __half*>(nullptr));
       }
+      __half* x = e.x + in_plane(i, e.cols, e.ld);
+      *reinterpret_cast<uint4*>(x) = hi;
+      if (P == 2) *reinterpret_cast<uint4*>(x + e.plane) = lo;
       continue;
     }
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
-      if (i + j >= e.n) break;
-      __half* x = e.x + row * e.ld + col;
-      *x = hi[j];
-      if (P == 2) x[e.plane] = lo[j];
-      if (++col == e.cols) {
-        col = 0;
-        ++row;
+      const int64_t i = place(false, at, j);
+      if (i >= end) break;
+      const float v = u[j] * scale;
+      const __half hi = __float2half_rn(v);
+      __half* x = e.x + in_plane(i, e.cols, e.ld);
+      *x = hi;
+      if (P == 2) x[e.plane] = __float2half_rn(v - __half2float(hi));
+    }
+  }
+}
+
+// w <- w - lr (ortho_scale X + weight_decay w).  In a pass of its own: in the last product's epilogue
+// the scattered rows of a tile cost as much (49M elements with masters: 100 us either way).
+template <int N, int P>
+__global__ void __launch_bounds__(kMomentThreads) weights_kernel(
+    const __grid_constant__ WeightParams<N> p) {
+  const int k = entry_of(p);
+  const WeightEntry& e = p.e[k];
+  griddep_wait();
+  const int64_t begin = static_cast<int64_t>(blockIdx.x - p.begin[k]) * p.chunk;
+  const int64_t end = min(begin + p.chunk, e.n);
+  const void* from = e.master != nullptr ? e.master : e.p;
+  const int type = e.master != nullptr ? static_cast<int>(BERGSON_F32) : e.pt;
+  for (int64_t at = begin; at < end; at += kMomentChunk) {
+    float w[8], x[8];
+    load_turn(from, type, e.vec, at, end, w);
+    const int64_t i0 = place(true, at, 0);
+    if (e.vec) {
+      if (i0 >= end) continue;
+      const __half* s = e.x + in_plane(i0, e.cols, e.ld);
+      load_eight(s, BERGSON_F16, true, 0, 8, x);
+      if (P == 2) {
+        float lo[8];
+        load_eight(s + e.plane, BERGSON_F16, true, 0, 8, lo);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) x[j] += lo[j];
       }
+    } else {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        const int64_t i = place(false, at, j);
+        x[j] = 0.0f;
+        if (i >= end) continue;
+        const __half* s = e.x + in_plane(i, e.cols, e.ld);
+        x[j] = __half2float(*s);
+        if (P == 2) x[j] += __half2float(s[e.plane]);
+      }
+    }
+#pragma unroll
+    for (int j = 0; j < 8; ++j) w[j] = fmaf(-e.lr_ortho, x[j], fmaf(-e.lr_decay, w[j], w[j]));
+    if (e.vec) {
+      uint32_t r[8];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) r[j] = __float_as_uint(w[j]);
+      if (e.master != nullptr) store32(e.master + i0, r);
+      if (e.pt == BERGSON_F32) {
+        store32(static_cast<float*>(e.p) + i0, r);
+        continue;
+      }
+      uint4 u;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const float2 y = make_float2(w[2 * j], w[2 * j + 1]);
+        if (e.pt == BERGSON_BF16) pack2(u, j, y, static_cast<__nv_bfloat16*>(nullptr));
+        else pack2(u, j, y, static_cast<__half*>(nullptr));
+      }
+      *reinterpret_cast<uint4*>(static_cast<uint16_t*>(e.p) + i0) = u;
+      continue;
+    }
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const int64_t i = place(false, at, j);
+      if (i >= end) break;
+      if (e.master != nullptr) e.master[i] = w[j];
+      if (e.pt == BERGSON_BF16) static_cast<__nv_bfloat16*>(e.p)[i] = __float2bfloat16_rn(w[j]);
+      else if (e.pt == BERGSON_F16) static_cast<__half*>(e.p)[i] = __float2half_rn(w[j]);
+      else static_cast<float*>(e.p)[i] = w[j];
     }
   }
 }
@@ -260,28 +360,18 @@ struct ProdGroup {
   int a_kind, b_kind;
   int chunks_b;                // 64-row chunks of a box of B's across; 0: one each, tn % 128 != 0
   int lower;                   // only tiles that reach the diagonal or lie below
-  int first_mat;
   int dst_ld;
   float alpha, gamma;          // D' = alpha acc + gamma I
-  __half* dst;                 // planes, or nullptr: the weights
+  __half* dst;                 // planes
   int64_t dst_plane;
 };
 
-struct WeightEntry {
-  void* p;
-  float* master;
-  float lr_ortho, lr_decay;    // lr lr_scale ortho_scale / 1024, lr lr_scale weight_decay
-  int32_t pt;
-  int32_t vec;                 // rows and pointers take vectors of 16
-};
-
-template <int G, int N>
+template <int G>
 struct ProdParams {
   CUtensorMap a[G], b[G];      // boxes of rows as they lie
   CUtensorMap ax[G], bx[G];    // and across
   CUtensorMap out[G];          // D', boxes of 32 rows and columns (one plane)
   ProdGroup g[G];
-  WeightEntry w[N];
   int n;
   int n_tiles;
   int* status;
@@ -293,8 +383,8 @@ struct Tile {
   int subs;                    // accumulators that are needed: columns within D and not above the diagonal
 };
 
-template <int P, int G, int N>
-__device__ __forceinline__ Tile tile_of(const ProdParams<G, N>& p, int t) {
+template <int P, int G>
+__device__ __forceinline__ Tile tile_of(const ProdParams<G>& p, int t) {
   constexpr int kSub = ProdCfg<P>::kSub;
   Tile o;
   o.group = 0;
@@ -386,8 +476,8 @@ __device__ __forceinline__ bool elect_lane() {
 }
 
 // One side's loads of all the tiles of a CTA, by one thread.
-template <int P, bool kSideB, int G, int N>
-__device__ __forceinline__ void load_side(const ProdParams<G, N>& p, int rank, int cid, int n_cl,
+template <int P, bool kSideB, int G>
+__device__ __forceinline__ void load_side(const ProdParams<G>& p, int rank, int cid, int n_cl,
                                           uint32_t sbase, uint64_t* full, uint64_t* empty,
                                           volatile int* s_abort) {
   using C = ProdCfg<P>;
@@ -458,77 +548,6 @@ __device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity, uint64_
   return __shfl_sync(0xffffffffu, ok ? 1 : 0, 0) != 0;
 }
 
-// Sets 16 values of a row as the step leaves them: w - lr (ortho_scale X + weight_decay w).
-__device__ __forceinline__ void update_weights(const WeightEntry& w, float ortho, int64_t at, int left,
-                                               const float* v) {
-  const bool wide = w.master != nullptr || w.pt == BERGSON_F32;
-  float* f = w.master != nullptr ? w.master : static_cast<float*>(w.p);
-  if (w.vec && !wide) {
-    uint32_t r[8];
-    uint16_t* q = static_cast<uint16_t*>(w.p) + at;
-    load32(q, r);
-#pragma unroll
-    for (int k = 0; k < 8; ++k) {
-      uint4 u = make_uint4(r[k], 0, 0, 0);
-      float2 y = w.pt == BERGSON_BF16 ? unpack2(u, 0, static_cast<__nv_bfloat16*>(nullptr))
-                                      : unpack2(u, 0, static_cast<__half*>(nullptr));
-      y.x = fmaf(-ortho, v[2 * k], fmaf(-w.lr_decay, y.x, y.x));
-      y.y = fmaf(-ortho, v[2 * k + 1], fmaf(-w.lr_decay, y.y, y.y));
-      if (w.pt == BERGSON_BF16) pack2(u, 0, y, static_cast<__nv_bfloat16*>(nullptr));
-      else pack2(u, 0, y, static_cast<__half*>(nullptr));
-      r[k] = u.x;
-    }
-    store32(q, r);
-    return;
-  }
-  if (w.vec) {
-#pragma unroll
-    for (int h = 0; h < 16; h += 8) {
-      float x[8];
-      load_eight(f, BERGSON_F32, true, at + h, at + h + 8, x);
-      uint32_t r[8];
-#pragma unroll
-      for (int k = 0; k < 8; ++k) {
-        x[k] = fmaf(-ortho, v[h + k], fmaf(-w.lr_decay, x[k], x[k]));
-        r[k] = __float_as_uint(x[k]);
-      }
-      store32(f + at + h, r);
-      if (w.pt == BERGSON_F32) {
-        if (w.master != nullptr) store32(static_cast<float*>(w.p) + at + h, r);
-        continue;
-      }
-      uint4 u;
-#pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        const float2 y = make_float2(x[2 * k], x[2 * k + 1]);
-        if (w.pt == BERGSON_BF16) pack2(u, k, y, static_cast<__nv_bfloat16*>(nullptr));
-        else pack2(u, k, y, static_cast<__half*>(nullptr));
-      }
-      *reinterpret_cast<uint4*>(static_cast<uint16_t*>(w.p) + at + h) = u;
-    }
-    return;
-  }
-#pragma unroll
-  for (int k = 0; k < 16; ++k) {
-    if (k >= left) return;
-    float x = wide ? f[at + k] : load_any(w.p, w.pt, at + k);
-    x = fmaf(-ortho, v[k], fmaf(-w.lr_decay, x, x));
-    if (wide) f[at + k] = x;
-    if (w.pt == BERGSON_BF16) static_cast<__nv_bfloat16*>(w.p)[at + k] = __float2bfloat16_rn(x);
-    else if (w.pt == BERGSON_F16) static_cast<__half*>(w.p)[at + k] = __float2half_rn(x);
-    else if (w.master != nullptr) static_cast<float*>(w.p)[at + k] = x;
-  }
-}
-
-// The weights that update_weights() will read, on their way to L2 while the product runs.
-__device__ __forceinline__ void prefetch_weights(const WeightEntry& w, int64_t at, int n) {
-  const bool wide = w.master != nullptr || w.pt == BERGSON_F32;
-  const int size = wide ? 4 : 2;
-  const uint8_t* p = (w.master != nullptr ? reinterpret_cast<const uint8_t*>(w.master)
-                                          : static_cast<const uint8_t*>(w.p)) + at * size;
-  for (int i = 0; i < n * size; i += 128) asm volatile("prefetch.global.L2 [%0];" ::"l"(p + i));
-}
-
 // 16 columns of a row to their two planes.
 __device__ __forceinline__ void put_planes(__half* d, int64_t plane, const float* v) {
   uint32_t hi[8], lo[8];
@@ -553,9 +572,9 @@ __device__ __forceinline__ void put_planes(__half* d, int64_t plane, const float
 // The tensor cores' fp32 sums round toward zero.  With two planes, an accumulation chain is
 // one stage (12 MMAs, its smallest terms first) and the epilogue adds the chains in registers while the
 // next one runs; with one plane the operands' own rounding is 2^-12 and a tile is one chain.
-template <int P, int G, int N>
+template <int P, int G>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
-    product_kernel(const __grid_constant__ ProdParams<G, N> p) {
+    product_kernel(const __grid_constant__ ProdParams<G> p) {
   using C = ProdCfg<P>;
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) &
@@ -708,7 +727,6 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
     for (int i = 0, t; !aborted && (t = tile_index(i, cid, n_cl, p.n_tiles)) >= 0; ++i) {
       const Tile o = tile_of<P>(p, t);
       const ProdGroup& g = p.g[o.group];
-      const WeightEntry& w = p.w[min(g.first_mat + o.mat, N - 1)];
       const int pieces = g.tn / 16, first = pieces * (ew >> 2) / 4;      // of 16 columns
       const int mine = pieces * ((ew >> 2) + 1) / 4 - first;             // up to 4
       const int row = o.mt * kTileM + rank * (kTileM / 2) + 32 * quarter + lane;
@@ -716,8 +734,6 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
       for (int h = 0; h < o.subs && !aborted; ++h) {
         const int col0 = (o.nt * C::kSub + h) * g.tn + 16 * first;
         const int left = row < g.M ? min(16 * mine, g.N - col0) : 0;     // columns to write
-        const int64_t at = static_cast<int64_t>(row) * g.N + col0;
-        if (g.dst == nullptr && left > 0) prefetch_weights(w, at, left);
         constexpr int kAcc = kTileN / 4;
         float acc[kAcc];
         if constexpr (P == 2) {
@@ -737,12 +753,12 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
             tmem_ld64(tb, acc);
           } else {
 #pragma unroll
-            for (int u = 0; u < 4; u += 2) {
-              if (u < mine) {                        // 16 columns more than asked for at most
-                float v[32];
-                tmem_ld32(tb + 16 * u, v);
+            for (int u = 0; u < 4; ++u) {
+              if (u < mine) {
+                float v[16];
+                tmem_ld16(tb + 16 * u, v);
 #pragma unroll
-                for (int j = 0; j < 32; j += 2) {
+                for (int j = 0; j < 16; j += 2) {
                   const float2 x = add2(make_float2(acc[16 * u + j], acc[16 * u + j + 1]),
                                         make_float2(v[j], v[j + 1]));
                   acc[16 * u + j] = x.x;
@@ -757,61 +773,52 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
           if (++ab == 2) { ab = 0; aph ^= 1; }
         }
         if (aborted) break;
-        if (g.dst != nullptr) {
-          const float2 alpha = pair(g.alpha);
+        const float2 alpha = pair(g.alpha);
 #pragma unroll
-          for (int j = 0; j < kAcc; j += 2) {
-            const float2 x = mul2(make_float2(acc[j], acc[j + 1]), alpha);
-            acc[j] = x.x;
-            acc[j + 1] = x.y;
-          }
-          const int row0 = row - lane;
-          if (g.gamma != 0.0f && row0 < col0 + kAcc && row0 + 32 > col0) {     // on the diagonal
-            const float gamma = g.gamma;
+        for (int j = 0; j < kAcc; j += 2) {
+          const float2 x = mul2(make_float2(acc[j], acc[j + 1]), alpha);
+          acc[j] = x.x;
+          acc[j + 1] = x.y;
+        }
+        const int row0 = row - lane;
+        if (g.gamma != 0.0f && row0 < col0 + kAcc && row0 + 32 > col0) {     // on the diagonal
+          const float gamma = g.gamma;
 #pragma unroll
-            for (int j = 0; j < kAcc; ++j) acc[j] += row == col0 + j ? gamma : 0.0f;
-          }
-          if constexpr (P == 1) {
+          for (int j = 0; j < kAcc; ++j) acc[j] += row == col0 + j ? gamma : 0.0f;
+        }
+        if constexpr (P == 1) {
 #pragma unroll
-            for (int u = 0; u < 4; u += 2) {
-              if (u >= mine) break;
-              if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
-              __syncwarp();
+          for (int u = 0; u < 4; u += 2) {
+            if (u >= mine) break;
+            if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
+            __syncwarp();
 #pragma unroll
-              for (int c = 0; c < 4; ++c) {          // 8 columns each, 64-byte swizzle
-                uint4 v;
+            for (int c = 0; c < 4; ++c) {          // 8 columns each, 64-byte swizzle
+              uint4 v;
 #pragma unroll
-                for (int j = 0; j < 4; ++j)
-                  pack2(v, j, make_float2(acc[16 * u + 8 * c + 2 * j], acc[16 * u + 8 * c + 2 * j + 1]),
-                        static_cast<const __half*>(nullptr));
-                *reinterpret_cast<uint4*>(out + 64 * lane + 16 * (c ^ ((lane >> 1) & 3))) = v;
-              }
-              fence_proxy_async_smem();
-              __syncwarp();
-              if (lane == 0 && row0 < g.M && col0 + 16 * u < g.N) {
-                asm volatile(
-                    "cp.async.bulk.tensor.3d.global.shared::cta.bulk_group [%0, {%2, %3, %4}], [%1];"
-                    ::"l"(&p.out[o.group]), "r"(smem_u32(out)), "r"(col0 + 16 * u), "r"(row0),
-                      "r"(o.mat)
-                    : "memory");
-                asm volatile("cp.async.bulk.commit_group;" ::: "memory");
-              }
+              for (int j = 0; j < 4; ++j)
+                pack2(v, j, make_float2(acc[16 * u + 8 * c + 2 * j], acc[16 * u + 8 * c + 2 * j + 1]),
+                      static_cast<const __half*>(nullptr));
+              *reinterpret_cast<uint4*>(out + 64 * lane + 16 * (c ^ ((lane >> 1) & 3))) = v;
             }
-          } else {
-            __half* d = g.dst + static_cast<int64_t>(o.mat) * P * g.dst_plane +
-                        static_cast<int64_t>(row) * g.dst_ld + col0;
-#pragma unroll
-            for (int u = 0; u < 4; ++u) {
-              if (16 * u >= left) break;
-              put_planes(d + 16 * u, g.dst_plane, acc + 16 * u);
+            fence_proxy_async_smem();
+            __syncwarp();
+            if (lane == 0 && row0 < g.M && col0 + 16 * u < g.N) {
+              asm volatile(
+                  "cp.async.bulk.tensor.3d.global.shared::cta.bulk_group [%0, {%2, %3, %4}], [%1];"
+                  ::"l"(&p.out[o.group]), "r"(smem_u32(out)), "r"(col0 + 16 * u), "r"(row0),
+                    "r"(o.mat)
+                  : "memory");
+              asm volatile("cp.async.bulk.commit_group;" ::: "memory");
             }
           }
         } else {
-          const float ortho = w.lr_ortho * g.alpha;
+          __half* d = g.dst + static_cast<int64_t>(o.mat) * P * g.dst_plane +
+                      static_cast<int64_t>(row) * g.dst_ld + col0;
 #pragma unroll
           for (int u = 0; u < 4; ++u) {
             if (16 * u >= left) break;
-            update_weights(w, ortho, at + 16 * u, left - 16 * u, acc + 16 * u);
+            put_planes(d + 16 * u, g.dst_plane, acc + 16 * u);
           }
         }
         __syncwarp();
@@ -921,19 +928,60 @@ BatchLayout layout_of(const Batch& b, int P) {
   return l;
 }
 
-// Columns of an accumulator for D [m, n] (lower: the tiles that reach the diagonal or lie below):
-// what computes least that is not needed.  An accumulator pays some 40 columns' time beside its
-// own.  With one plane they are whole chunks.
-int tile_columns(int64_t m, int64_t n, bool lower, int P) {
-  int best = kTileN;
+// Columns of an accumulator for D [m, n] (lower: the tiles that reach the diagonal or lie below),
+// at most `most`: what computes least that is not needed.  An accumulator pays some 40 columns'
+// time beside its own.  With one plane they are whole chunks.
+struct Columns {
+  int tn;
+  int64_t accs;                // accumulators of a matrix
+};
+Columns tile_columns(int64_t m, int64_t n, bool lower, int P, int most) {
+  Columns best{most, 0};
   int64_t cost = INT64_MAX;
-  for (int tn = kTileN; tn >= 128; tn -= P == 2 ? 32 : 128) {
+  for (int tn = most; tn >= std::min(128, most); tn -= P == 2 ? 32 : 128) {
     int64_t c = 0;
     for (int64_t r = kTileM; r < m + kTileM; r += kTileM)
-      c += ceil_div(lower ? std::min(r, n) : n, tn) * (tn + 40);
-    if (c < cost) {
-      cost = c;
-      best = tn;
+      c += ceil_div(lower ? std::min(r, n) : n, tn);
+    if (c * (tn + 40) < cost) {
+      cost = c * (tn + 40);
+      best = {tn, c};
+    }
+  }
+  return best;
+}
+
+// The D of a shape's product: 0 A', 1 B, 2 X'.
+struct Dims {
+  int64_t m, n, k;
+};
+Dims dims_of(const Shape& s, int part) {
+  const int64_t m = std::min(s.rows, s.cols);
+  return part == 2 ? Dims{s.rows, s.cols, m} : Dims{m, m, part == 0 ? std::max(s.rows, s.cols) : m};
+}
+
+// The same for all shapes of a launch, with the width that leaves the clusters least time: wide
+// tiles read less for a product, narrow ones are more.  In cycles: MMAs of 1 / 2 a column and 57
+// at least, loads of 2.6 a 128-byte row, 4000 a tile.
+std::vector<int> launch_columns(const Batch& b, int part, int P, int clusters) {
+  std::vector<int> best(b.shapes.size()), now(b.shapes.size());
+  double least = INFINITY;
+  for (int most : {256, 128, 64}) {
+    if (P == 1 && most < 128) break;
+    double all = 0.0, longest = 0.0;
+    for (size_t i = 0; i < b.shapes.size(); ++i) {
+      const Dims d = dims_of(b.shapes[i], part);
+      const Columns c = tile_columns(d.m, d.n, part < 2, P, most);
+      now[i] = c.tn;
+      const double mma = (P == 2 ? 12 : 4) * std::max(57.0, c.tn / 2.0);
+      const double load = 2.6 * P * (128 + c.tn / 2);
+      const double tile = 4000.0 + static_cast<double>(ceil_div(d.k, kTileK)) * std::max(mma, load);
+      all += tile * static_cast<double>(c.accs) * static_cast<double>(b.shapes[i].mats.size());
+      longest = std::max(longest, tile);
+    }
+    const double time = std::max(all / clusters, longest);
+    if (time < 0.97 * least) {
+      least = time;
+      best = now;
     }
   }
   return best;
@@ -967,7 +1015,7 @@ cudaError_t run_moments(const bergson_muon_tensor* t, const Batch& b, const Batc
       e.cols = static_cast<int32_t>(sh.cols);
       e.ld = static_cast<int32_t>(pl.x_ld);
       e.gt = x.grad_dtype;
-      e.vec = on16(x.grad, 0, 1) && reinterpret_cast<uintptr_t>(x.m) % 32 == 0 &&
+      e.vec = sh.cols % 8 == 0 && on16(x.grad, 0, 1) && reinterpret_cast<uintptr_t>(x.m) % 32 == 0 &&
               (x.grad_dtype != BERGSON_F32 || reinterpret_cast<uintptr_t>(x.grad) % 32 == 0);
       p.begin[k + 1] = p.begin[k] + static_cast<uint32_t>(ceil_div(e.n, l.chunk));
     }
@@ -977,6 +1025,43 @@ cudaError_t run_moments(const bergson_muon_tensor* t, const Batch& b, const Batc
   if (e != cudaSuccess) return e;
   return P == 2 ? launch_dependent(planes_kernel<N, 2>, grid, block, 0, s, p)
                 : launch_dependent(planes_kernel<N, 1>, grid, block, 0, s, p);
+}
+
+template <int N>
+cudaError_t run_weights(const bergson_muon_tensor* t, const Batch& b, const BatchLayout& l,
+                        const MuonScalars& a, uint8_t* ws, cudaStream_t s) {
+  const int P = a.products == 3 ? 2 : 1;
+  WeightParams<N> p;
+  p.n = b.mats;
+  p.chunk = l.chunk;
+  p.begin[0] = 0;
+  int k = 0;
+  for (size_t g = 0; g < b.shapes.size(); ++g) {
+    const Shape& sh = b.shapes[g];
+    const Planes& pl = l.shapes[g];
+    for (size_t z = 0; z < sh.mats.size(); ++z, ++k) {
+      const bergson_muon_tensor& x = t[sh.mats[z]];
+      WeightEntry& e = p.e[k];
+      e.p = x.param;
+      e.master = x.master;
+      e.x = reinterpret_cast<const __half*>(ws + pl.x[a.iterations & 1]) +
+            static_cast<int64_t>(z) * P * pl.x_plane;
+      e.n = sh.rows * sh.cols;
+      e.plane = pl.x_plane;
+      e.cols = static_cast<int32_t>(sh.cols);
+      e.ld = static_cast<int32_t>(pl.x_ld);
+      const double lr = a.lr * x.lr_scale;
+      e.lr_ortho = static_cast<float>(lr * x.ortho_scale / kPlaneScale);
+      e.lr_decay = static_cast<float>(lr * x.weight_decay);
+      e.pt = x.param_dtype;
+      e.vec = sh.cols % 8 == 0 && reinterpret_cast<uintptr_t>(x.master) % 32 == 0 &&
+              reinterpret_cast<uintptr_t>(x.param) % (x.param_dtype == BERGSON_F32 ? 32 : 16) == 0;
+      p.begin[k + 1] = p.begin[k] + static_cast<uint32_t>(ceil_div(e.n, l.chunk));
+    }
+  }
+  const dim3 grid(p.begin[k]), block(kMomentThreads);
+  return P == 2 ? launch_dependent(weights_kernel<N, 2>, grid, block, 0, s, p)
+                : launch_dependent(weights_kernel<N, 1>, grid, block, 0, s, p);
 }
 
 // An operand's boxes: of the rows as they lie, and across.
@@ -996,21 +1081,24 @@ bool encode_side(Side* s, const void* ptr, int64_t cols, int64_t rows, int64_t p
          encode_tmap_across(&s->across, ptr, cols, rows, planes, ld, P, chunks) == CUDA_SUCCESS;
 }
 
-template <int P, int G, int N>
-cudaError_t run_products(const bergson_muon_tensor* t, const Batch& b, const BatchLayout& l,
+template <int P, int G>
+cudaError_t run_products(const Batch& b, const BatchLayout& l,
                          const MuonScalars& a, uint8_t* ws, int* status, int sms, cudaStream_t s) {
   std::vector<Maps> maps(b.shapes.size());
-  ProdParams<G, N> p = {};
+  const int most_clusters = std::max(1, sms / 2);
+  std::vector<int> columns[3];
+  for (int part = 0; part < 3; ++part)
+    columns[part] = launch_columns(b, part, P, most_clusters);
+  ProdParams<G> p = {};
   p.n = static_cast<int>(b.shapes.size());
   p.status = status;
   p.timeout_ns = kWaitTimeoutNs;
-  int first = 0;
   for (int k = 0; k < p.n; ++k) {
     const Shape& sh = b.shapes[k];
     const Planes& pl = l.shapes[k];
     const int64_t m = std::min(sh.rows, sh.cols), n = static_cast<int64_t>(sh.mats.size()) * P;
     Maps& mp = maps[k];
-    const int tn_s = tile_columns(m, m, true, P), tn_x = tile_columns(sh.rows, sh.cols, false, P);
+    const int tn_g = columns[0][k], tn_s = columns[1][k], tn_x = columns[2][k];
     const auto chunks = [](int tn) { return tn % 128 == 0 ? tn / 128 : 0; };
     bool good = true;
     for (int i = 0; i < 2; ++i) {
@@ -1020,7 +1108,7 @@ cudaError_t run_products(const bergson_muon_tensor* t, const Batch& b, const Bat
       good = good && encode_tmap_out(&mp.x_out[i], ws + pl.x[i], sh.cols, sh.rows, n, pl.x_ld) ==
                          CUDA_SUCCESS;
       x(&mp.gram_a[i], kTileM / 2, 2);
-      x(&mp.gram_b[i], tn_s / 2, chunks(tn_s));
+      x(&mp.gram_b[i], tn_g / 2, chunks(tn_g));
       if (sh.rows > sh.cols) x(&mp.last_x[i], kTileM / 2, 2);
       else x(&mp.last_x[i], tn_x / 2, chunks(tn_x));
     }
@@ -1034,29 +1122,16 @@ cudaError_t run_products(const bergson_muon_tensor* t, const Batch& b, const Bat
     good = good && encode_tmap_out(&mp.a_out, ws + pl.a, m, m, n, pl.s_ld) == CUDA_SUCCESS &&
            encode_tmap_out(&mp.b_out, ws + pl.b, m, m, n, pl.s_ld) == CUDA_SUCCESS;
     if (!good) return cudaErrorInvalidValue;
-    p.g[k].first_mat = first;
-    for (int i : sh.mats) {
-      const bergson_muon_tensor& x = t[i];
-      WeightEntry& w = p.w[first++];
-      w.p = x.param;
-      w.master = x.master;
-      const double lr = a.lr * x.lr_scale;
-      w.lr_ortho = static_cast<float>(lr * x.ortho_scale / kPlaneScale);
-      w.lr_decay = static_cast<float>(lr * x.weight_decay);
-      w.pt = x.param_dtype;
-      w.vec = sh.cols % 16 == 0 && reinterpret_cast<uintptr_t>(x.param) % 32 == 0 &&
-              reinterpret_cast<uintptr_t>(x.master) % 32 == 0;
-    }
   }
-  const auto kernel = product_kernel<P, G, N>;
+  const auto kernel = product_kernel<P, G>;
   static PerDeviceOnce attr;
   cudaError_t e = smem_attr_once(attr, kernel, ProdCfg<P>::kSmemBytes);
   if (e != cudaSuccess) return e;
-  const auto run = [&]() {
+  const auto run = [&](int part) {
     int64_t tiles = 0;
     for (int k = 0; k < p.n; ++k) {
       ProdGroup& g = p.g[k];
-      g.tn = tile_columns(g.M, g.N, g.lower != 0, P);
+      g.tn = columns[part][k];
       g.chunks_b = g.tn % 128 == 0 ? g.tn / 128 : 0;
       const int width = ProdCfg<P>::kSub * g.tn;
       g.n_mt = static_cast<int>(ceil_div(g.M, kTileM));
@@ -1069,14 +1144,13 @@ cudaError_t run_products(const bergson_muon_tensor* t, const Batch& b, const Bat
       tiles += static_cast<int64_t>(g.per_mat) * static_cast<int64_t>(b.shapes[k].mats.size());
     }
     p.n_tiles = static_cast<int>(tiles);
-    const int64_t clusters = std::max<int64_t>(1, std::min<int64_t>(sms / 2, tiles));
+    const int64_t clusters = std::max<int64_t>(1, std::min<int64_t>(most_clusters, tiles));
     return launch_dependent(kernel, dim3(static_cast<unsigned>(2 * clusters)), dim3(kThreads),
                             ProdCfg<P>::kSmemBytes, s, p);
   };
   for (int it = 0; it < a.iterations; ++it) {
     const double* c = a.coefficients + 3 * it;
     const int cur = it & 1;
-    const bool last = it == a.iterations - 1;
     const double ca = c[0], cb = c[1], cc = c[2];
     const double h = cc != 0.0 ? cb / (2.0 * cc) : 0.0;
     for (int part = 0; part < 3; ++part) {       // A' = X X^T + h I, B = c A'^2 + .., X' = B X
@@ -1085,11 +1159,11 @@ cudaError_t run_products(const bergson_muon_tensor* t, const Batch& b, const Bat
         const Shape& sh = b.shapes[k];
         const Planes& pl = l.shapes[k];
         const bool tall = sh.rows > sh.cols;
-        const int m = static_cast<int>(std::min(sh.rows, sh.cols));
+        const Dims d = dims_of(sh, part);
         ProdGroup& g = p.g[k];
-        g.M = part == 2 ? static_cast<int>(sh.rows) : m;
-        g.N = part == 2 ? static_cast<int>(sh.cols) : m;
-        g.K = part == 0 ? static_cast<int>(std::max(sh.rows, sh.cols)) : m;
+        g.M = static_cast<int>(d.m);
+        g.N = static_cast<int>(d.n);
+        g.K = static_cast<int>(d.k);
         g.lower = part < 2 ? 1 : 0;
         g.dst_ld = static_cast<int>(part == 2 ? pl.x_ld : pl.s_ld);
         g.dst_plane = part == 2 ? pl.x_plane : pl.s_plane;
@@ -1123,10 +1197,10 @@ cudaError_t run_products(const bergson_muon_tensor* t, const Batch& b, const Bat
           else sides(mp.last_s, mp.last_x[cur]);
           g.a_kind = tall ? kRowMajor : kSymmetric;
           g.b_kind = tall ? kSymmetric : kAcross;
-          set(1.0, 0.0, last ? nullptr : at(pl.x[cur ^ 1]));
+          set(1.0, 0.0, at(pl.x[cur ^ 1]));
         }
       }
-      e = run();
+      e = run(part);
       if (e != cudaSuccess) return e;
     }
   }
@@ -1154,11 +1228,13 @@ cudaError_t launch_muon(const bergson_muon_tensor* t, int n, const MuonScalars& 
                         : run_moments<kMaxMats>(t, b, l, a, w, s);
     if (e != cudaSuccess) return e;
     if (a.products == 3)
-      e = few ? run_products<2, kFewGroups, kFewMats>(t, b, l, a, w, status, sms, s)
-              : run_products<2, kMaxGroups, kMaxMats>(t, b, l, a, w, status, sms, s);
+      e = few ? run_products<2, kFewGroups>(b, l, a, w, status, sms, s)
+              : run_products<2, kMaxGroups>(b, l, a, w, status, sms, s);
     else
-      e = few ? run_products<1, kFewGroups, kFewMats>(t, b, l, a, w, status, sms, s)
-              : run_products<1, kMaxGroups, kMaxMats>(t, b, l, a, w, status, sms, s);
+      e = few ? run_products<1, kFewGroups>(b, l, a, w, status, sms, s)
+              : run_products<1, kMaxGroups>(b, l, a, w, status, sms, s);
+    if (e != cudaSuccess) return e;
+    e = few ? run_weights<kFewMats>(t, b, l, a, w, s) : run_weights<kMaxMats>(t, b, l, a, w, s);
     if (e != cudaSuccess) return e;
   }
   return cudaSuccess;
