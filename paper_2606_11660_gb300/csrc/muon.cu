@@ -612,10 +612,16 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
     tmem_alloc_pair(smem_u32(s_tmem), kTmemCols);
     tmem_relinquish_pair();
   }
-  griddep_wait();                // the operands come from earlier grids
+  if (lane == 0 && (warp == 0 || warp == 2) && tile_index(0, cid, n_cl, p.n_tiles) >= 0) {
+    const int group = tile_of<P>(p, tile_index(0, cid, n_cl, p.n_tiles)).group;
+    prefetch_tmap(warp == 0 ? &p.a[group] : &p.b[group]);
+    prefetch_tmap(warp == 0 ? &p.ax[group] : &p.bx[group]);
+  }
+  __syncwarp();
   tc_fence_before();
   cluster_sync();
   tc_fence_after();
+  griddep_wait();                // the operands come from earlier grids
   const uint32_t tmem = *s_tmem;
   const uint64_t tmo = p.timeout_ns;
 
