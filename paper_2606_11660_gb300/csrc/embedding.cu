@@ -78,9 +78,9 @@ constexpr int kRun = 32;                       // sorted rows added up by one CT
 constexpr int kSumThreads = 128;
 constexpr int kCols = 8;                       // columns a thread
 constexpr int kAhead = 8;                      // rows on their way
-constexpr int kJoinRuns = 16;                  // runs whose last token a CTA joins
-constexpr int kJoinThreads = 256;
+constexpr int kJoinThreads = 256;               // a warp joins the token that a run ends in
 constexpr int kJoinCols = 128;
+constexpr int kShortParts = 32;                // of so many runs
 constexpr int kSortThreads = 1024;
 constexpr int kSortItems = 2048;               // items of a step of the sort
 constexpr int kDigitBits = 9;
@@ -342,6 +342,7 @@ __global__ void __launch_bounds__(kSortThreads) sort_place_kernel(
     // what stands before this tile and in all: two halves of the tiles a digit
     const int digit = tid & (kBins - 1), half = tid / kBins;
     int before = 0, all = 0;
+#pragma unroll 8
     for (int t = half; t < p.tiles; t += kSortThreads / kBins) {
       const int c = p.table[t * kBins + digit];
       all += c;
@@ -388,6 +389,7 @@ __global__ void __launch_bounds__(kSortThreads) sort_place_kernel(
     __syncthreads();
     int sum = 0;
     if (tid < kBins) {
+#pragma unroll 8
       for (int w = 0; w < kWarps; ++w) {
         const int c = hist[w][tid];
         hist[w][tid] = static_cast<uint16_t>(sum);
@@ -494,58 +496,75 @@ __global__ void __launch_bounds__(kSumThreads) sum_kernel(const __grid_constant_
   }
 }
 
-// The tokens that cross ends of runs: the CTA of the run where a token begins adds
-// what that run and the next ones have of it, eight warps a part each, joined in order.
+// The part sums [begin, end) of a token that begins in `run`: 0 is that run's second sum, q the
+// first of run + q.  Four columns a lane.
+__device__ __forceinline__ float4 add_parts(const SumParams& p, int64_t run, int64_t begin,
+                                            int64_t end, int col) {
+  float4 sum = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+#pragma unroll 16
+  for (int64_t q = begin; q < end; ++q) {
+    const float4 x = *reinterpret_cast<const float4*>(
+        p.part + (2 * (run + q) + (q == 0 ? 1 : 0)) * p.ld_part + col);
+    sum.x += x.x; sum.y += x.y; sum.z += x.z; sum.w += x.w;
+  }
+  return sum;
+}
+
+// The tokens that cross ends of runs: the warp of the run where a token begins adds what that
+// run and the next ones have of it.  What more than kShortParts runs have is added by all the CTA's
+// warps, a stretch each, joined in order.
 __global__ void __launch_bounds__(kJoinThreads) join_kernel(const __grid_constant__ SumParams p) {
   constexpr int kWarps = kJoinThreads / 32;
-  constexpr int kE = kJoinCols / 32;
-  static_assert(kE == 4, "a lane takes 16 bytes of a sum");
-  __shared__ float red[kWarps][kJoinCols];
+  __shared__ float4 red[kWarps][32];
+  __shared__ int64_t parts[kWarps];              // of the warps' tokens that are left
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  const int c0 = blockIdx.y * kJoinCols;
+  const int col = static_cast<int>(blockIdx.y) * kJoinCols + 4 * lane;
+  const bool mine = col < p.ld_part;
   const uint32_t none = static_cast<uint32_t>(p.V);
   griddep_wait();
-  for (int k = 0; k < kJoinRuns; ++k) {
-    const int64_t run = static_cast<int64_t>(blockIdx.x) * kJoinRuns + k;
-    const int64_t last = run * kRun + kRun - 1;
-    if (last + 1 >= p.rows) return;
-    const uint32_t v = p.key[last];
-    if (v == none) return;
-    if (p.key[last + 1] != v || (run > 0 && p.key[run * kRun - 1] == v)) continue;
-    int64_t n = 1;                               // runs behind that hold some of it
-    for (;; n += 32) {
-      const int64_t at = (run + n + 1 + lane) * kRun;   // does run + n + lane + 1 hold some too?
-      const unsigned votes = __ballot_sync(0xffffffffu, at < p.rows && p.key[at] == v);
-      if (votes != 0xffffffffu) {
-        n += __ffs(~votes) - 1;
-        break;
+  const int64_t run0 = static_cast<int64_t>(blockIdx.x) * kWarps, run = run0 + warp;
+  const int64_t last = run * kRun + kRun - 1;
+  int64_t n = 0;                                 // part sums, if a token that goes on begins here
+  uint32_t v = none;
+  if (last + 1 < p.rows) {
+    v = p.key[last];
+    const uint32_t next = p.key[last + 1];
+    const uint32_t before = run > 0 ? p.key[run * kRun - 1] : none;
+    if (v != none && next == v && before != v) {
+      for (n = 2;; n += 32) {
+        const int64_t at = (run + n + lane) * kRun;        // does run + n + lane hold some too?
+        const unsigned votes = __ballot_sync(0xffffffffu, at < p.rows && p.key[at] == v);
+        if (votes != 0xffffffffu) {
+          n += __ffs(~votes) - 1;
+          break;
+        }
       }
     }
-    // part 0 is this run's second sum, part q the first of run + q
-    const int64_t per = (n + 1 + kWarps - 1) / kWarps;
-    const int64_t begin = warp * per, end = min(begin + per, n + 1);
-    float sum[kE];
-#pragma unroll
-    for (int i = 0; i < kE; ++i) sum[i] = 0.0f;
-#pragma unroll 4
-    for (int64_t q = begin; q < end; ++q) {
-      const float* part = p.part + (2 * (run + q) + (q == 0 ? 1 : 0)) * p.ld_part + c0;
-      if (c0 + kE * lane < p.ld_part) {
-        const float4 x = *reinterpret_cast<const float4*>(part + kE * lane);
-        sum[0] += x.x; sum[1] += x.y; sum[2] += x.z; sum[3] += x.w;
-      }
-    }
+  }
+  const bool many = n > kShortParts;
+  if (n > 0 && !many && mine) {
+    const float4 s = add_parts(p, run, 0, n, col);
+    const float sum[4] = {s.x, s.y, s.z, s.w};
+    if (col < p.d) put_columns<4>(p.out, v, col, p.d, sum);
+  }
+  if (lane == 0) parts[warp] = many ? n : 0;
+  if (!__syncthreads_or(many)) return;
+  for (int k = 0; k < kWarps; ++k) {
+    const int64_t all = parts[k];
+    if (all == 0) continue;
+    const int64_t per = (all + kWarps - 1) / kWarps;
+    const int64_t begin = min(warp * per, all), end = min(begin + per, all);
     __syncthreads();                             // the last token's sums have been read
-#pragma unroll
-    for (int i = 0; i < kE; ++i) red[warp][kE * lane + i] = sum[i];
+    if (mine) red[warp][lane] = add_parts(p, run0 + k, begin, end, col);
     __syncthreads();
-    if (warp == 0) {
+    if (warp == 0 && col < p.d) {
+      float4 s = red[0][lane];
       for (int w = 1; w < kWarps; ++w) {
-#pragma unroll
-        for (int i = 0; i < kE; ++i) sum[i] += red[w][kE * lane + i];
+        const float4 x = red[w][lane];
+        s.x += x.x; s.y += x.y; s.z += x.z; s.w += x.w;
       }
-      const int c = c0 + kE * lane;
-      if (c < p.d) put_columns<kE>(p.out, v, c, p.d, sum);
+      const float sum[4] = {s.x, s.y, s.z, s.w};
+      put_columns<4>(p.out, p.key[(run0 + k) * kRun + kRun - 1], col, p.d, sum);
     }
   }
 }
@@ -674,7 +693,7 @@ cudaError_t run_sorted(const EmbeddingGradArgs& a, const GradOut& out, bool vec,
   else
     e = vec ? run_sums<float, true>(a, q, s) : run_sums<float, false>(a, q, s);
   if (e != cudaSuccess) return e;
-  const dim3 grid(static_cast<unsigned>(ceil_div(plan.runs, kJoinRuns)),
+  const dim3 grid(static_cast<unsigned>(ceil_div(plan.runs, kJoinThreads / 32)),
                   static_cast<unsigned>(ceil_div(a.d, kJoinCols)));
   return launch_dependent(join_kernel, grid, dim3(kJoinThreads), 0, s, q);
 }

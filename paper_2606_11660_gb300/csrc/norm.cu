@@ -12,6 +12,7 @@
 // of both a CTA goes to the workspace, and a second kernel adds these up in order.
 
 #include <algorithm>
+#include <atomic>
 #include <cmath>
 
 #include "internal.h"
@@ -30,27 +31,118 @@ constexpr int kMaxCols = 16384;                // up to here a row stays in regi
 constexpr int kLoopThreads = 512;              // of the kernels for longer rows
 constexpr int kSlabRows = 512;                 // rows of a CTA that sums columns of such rows
 
-// Sums over the threads that share a row, in each of them: G lanes side by side, or the
-// CTA by way of `red` (32 values each, not in use by the row before or after).
+// Sums of one value or two over the threads that share a row, in each of them: G lanes side by
+// side, or the CTA by way of `red` (N values for each of 32 warps, not in use by the row before or
+// after, zeros at first).  Two go through the warp as one: its halves take one each after the first step.
 template <bool kCta, int N>
 __device__ __forceinline__ void row_sums(float (&v)[N], int G, float* red) {
+  static_assert(N == 1 || N == 2, "one value or two");
   if constexpr (!kCta) {
     for (int o = G >> 1; o > 0; o >>= 1) {
 #pragma unroll
       for (int i = 0; i < N; ++i) v[i] += __shfl_xor_sync(0xffffffffu, v[i], o);
     }
   } else {
-#pragma unroll
-    for (int i = 0; i < N; ++i) v[i] = warp_sum(v[i]);
-    const int lane = threadIdx.x & 31, warps = blockDim.x >> 5;
-    if (lane == 0) {
-#pragma unroll
-      for (int i = 0; i < N; ++i) red[32 * i + (threadIdx.x >> 5)] = v[i];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
+    float s;
+    if constexpr (N == 2) {
+      const bool upper = lane >= 16;
+      s = upper ? v[1] : v[0];
+      s += __shfl_xor_sync(0xffffffffu, upper ? v[0] : v[1], 16);
+    } else {
+      s = v[0] + __shfl_xor_sync(0xffffffffu, v[0], 16);
     }
-    __syncthreads();
 #pragma unroll
-    for (int i = 0; i < N; ++i) v[i] = warp_sum(lane < warps ? red[32 * i + lane] : 0.0f);
+    for (int o = 8; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
+    if (lane % (32 / N) == 0) red[N * warp + lane / (32 / N)] = s;
+    __syncthreads();
+    // four at a time; what stands behind the last warp's is 0
+    float4 t = *reinterpret_cast<const float4*>(red);
+    for (int w = 4; w < N * warps; w += 4) {
+      const float4 y = *reinterpret_cast<const float4*>(red + w);
+      t.x += y.x; t.y += y.y; t.z += y.z; t.w += y.w;
+    }
+    if constexpr (N == 1) {
+      v[0] = (t.x + t.y) + (t.z + t.w);
+    } else {
+      v[0] = t.x + t.z;
+      v[1] = t.y + t.w;
+    }
   }
+}
+// Clears the places of row_sums.
+__device__ __forceinline__ void clear_sums(float* red, int n) {
+  for (int i = threadIdx.x; i < n; i += blockDim.x) red[i] = 0.0f;
+  __syncthreads();
+}
+
+// Rows on their way to a thread.  In vectors: by asynchronous copies to places of its own in
+// shared memory, kSlots rows ahead, so that no thread waits for another and no register is
+// held (a row at a time in registers: too few bytes in flight, 65,536 x 2048 at 4.1 TB/s with 6 CTAs an SM).  A
+// vector past the end copies what there is and zeros.  Else: one row ahead, in registers.
+template <typename T, bool kVec, int C, int kSlots>
+struct Feed {
+  using R = RowPart<T, kVec, C>;
+  static constexpr int kBytes = kVec ? R::kPer * 16 : 0;     // of a row, a thread
+  uint32_t base;
+  int slot = 0;
+  int bytes[kVec ? R::kPer : 1];                 // of the thread's vectors that are within a row
+  R row;
+  __device__ __forceinline__ Feed(const void* smem, int part, int d, int t, int G)
+      : base(kVec ? smem_u32(smem) + part * kSlots * kBytes * blockDim.x + 16 * threadIdx.x : 0) {
+    if constexpr (kVec) {
+#pragma unroll
+      for (int k = 0; k < R::kPer; ++k)
+        bytes[k] = max(0, min(16, (d - R::col(t, G, k)) * static_cast<int>(sizeof(T))));
+    }
+  }
+  __device__ __forceinline__ uint32_t at(int k) const {
+    return base + (slot * R::kPer + k) * 16 * blockDim.x;
+  }
+  // Sends for row r, which starts at p, into the slot that was read last (in: it is a row at all).
+  __device__ __forceinline__ void send(const T* first, int64_t r, int64_t ld, bool in, int d, int t,
+                                       int G) {
+    const T* p = in ? first + r * ld : first;
+    if constexpr (kVec) {
+      p += R::E * t;
+#pragma unroll
+      for (int k = 0; k < R::kPer; ++k) {
+        const int n = in ? bytes[k] : 0;
+        asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(at(k)),
+                     "l"(n > 0 ? p + k * R::E * G : first), "r"(n)
+                     : "memory");
+      }
+    } else {
+      row.load(p, in ? d : 0, t, G);
+    }
+  }
+  __device__ __forceinline__ void next() { slot = slot + 1 == kSlots ? 0 : slot + 1; }
+  // The values of the slot's row (which must have arrived).
+  __device__ __forceinline__ void take(float2 (&x)[C / 2]) {
+    if constexpr (kVec) {
+#pragma unroll
+      for (int k = 0; k < R::kPer; ++k) {
+        uint32_t* r = row.raw + 4 * k;
+        asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];"
+                     : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3])
+                     : "r"(at(k))
+                     : "memory");
+      }
+    }
+    row.pairs(x);
+  }
+};
+template <bool kVec>
+__device__ __forceinline__ void feed_commit() {
+  if constexpr (kVec) asm volatile("cp.async.commit_group;" ::: "memory");
+}
+template <bool kVec>
+__device__ __forceinline__ void feed_end() {
+  if constexpr (kVec) asm volatile("cp.async.wait_group 0;" ::: "memory");
+}
+template <bool kVec, int kSlots>
+__device__ __forceinline__ void feed_wait() {
+  if constexpr (kVec) asm volatile("cp.async.wait_group %0;" ::"n"(kSlots - 1) : "memory");
 }
 
 // The rows of a thread: its first one, and how far apart they are.  All lanes of a warp make
@@ -95,55 +187,81 @@ struct NormParams {
   float eps, inv_d;
 };
 
+constexpr int kForwardSlots = 3, kBackwardSlots = 2;
+
 template <typename T, bool kVec, bool kCta, bool kWide, int C>
 __global__ void __launch_bounds__(kWide ? 1024 : kCta ? 512 : 32 * kWarps)
     norm_kernel(const __grid_constant__ NormParams p) {
   using R = RowPart<T, kVec, C>;
-  __shared__ float red[2][2][32];
+  constexpr int kSlots = kVec ? kForwardSlots : 1;
+  constexpr int H = C / 2;
+  extern __shared__ __align__(16) uint8_t slots[];
+  __shared__ __align__(16) float red[2][2][32];
   const Turns u = turns<kCta>(p.lanes);
   const int G = u.G, t = u.t, d = static_cast<int>(p.d);
+  const bool whole = R::column(t, G, C - 1) < d;       // all of the thread's columns are
+  if (kCta) clear_sums(&red[0][0][0], 128);
   griddep_wait();
-  float w[C], b[C];
+  const T* xs = static_cast<const T*>(p.x);
+  Feed<T, kVec, C, kSlots> feed(slots, 0, d, t, G);
+  const auto send = [&](int64_t r) {
+    feed.send(xs, r, p.ld_x, r < p.rows, d, t, G);
+    feed_commit<kVec>();
+  };
+#pragma unroll
+  for (int k = 0; k < kSlots; ++k) {
+    send(u.first + k * u.step + u.sub);
+    feed.next();
+  }
+  float2 w[H], b[H];
 #pragma unroll
   for (int i = 0; i < C; ++i) {
     const int c = R::column(t, G, i);
-    w[i] = p.w != nullptr && c < d ? load_any(p.w, p.wt, c) : 1.0f;
-    b[i] = p.b != nullptr && c < d ? load_any(p.b, p.wt, c) : 0.0f;
+    const float wi = p.w != nullptr && c < d ? load_any(p.w, p.wt, c) : 1.0f;
+    const float bi = p.b != nullptr && c < d ? load_any(p.b, p.wt, c) : 0.0f;
+    (i % 2 == 0 ? w[i / 2].x : w[i / 2].y) = wi;
+    (i % 2 == 0 ? b[i / 2].x : b[i / 2].y) = bi;
   }
-  const T* xs = static_cast<const T*>(p.x);
-  R next;
-  const auto fetch = [&](int64_t r) { next.load(xs + r * p.ld_x, r < p.rows ? d : 0, t, G); };
-  fetch(u.first + u.sub);
   int turn = 0;
   for (int64_t first = u.first; first < p.rows; first += u.step, turn ^= 1) {
     const int64_t r = first + u.sub;
-    const R row = next;
-    fetch(r + u.step);
-    float x[C];
-    row.floats(x);
+    float2 x[H];
+    feed_wait<kVec, kSlots>();
+    feed.take(x);
+    send(r + kSlots * u.step);
+    feed.next();
     float mean = 0.0f;
     if (p.layer) {
-      float s[1] = {0.0f};
+      float2 s2 = x[0];
 #pragma unroll
-      for (int i = 0; i < C; ++i) s[0] += x[i];
+      for (int i = 1; i < H; ++i) s2 = add2(s2, x[i]);
+      float s[1] = {s2.x + s2.y};
       row_sums<kCta>(s, G, red[turn][0]);
       mean = s[0] * p.inv_d;
+      const float2 less = pair(-mean);
 #pragma unroll
-      for (int i = 0; i < C; ++i) x[i] = R::column(t, G, i) < d ? x[i] - mean : 0.0f;
+      for (int i = 0; i < H; ++i) x[i] = add2(x[i], less);
+      if (!whole) {
+#pragma unroll
+        for (int i = 0; i < C; ++i)
+          if (R::column(t, G, i) >= d) (i % 2 == 0 ? x[i / 2].x : x[i / 2].y) = 0.0f;
+      }
     }
-    float q[1] = {0.0f};
+    float2 q2 = mul2(x[0], x[0]);
 #pragma unroll
-    for (int i = 0; i < C; ++i) q[0] = fmaf(x[i], x[i], q[0]);
+    for (int i = 1; i < H; ++i) q2 = fma2(x[i], x[i], q2);
+    float q[1] = {q2.x + q2.y};
     row_sums<kCta>(q, G, red[turn][1]);
     const float rstd = __frcp_rn(__fsqrt_rn(fmaf(q[0], p.inv_d, p.eps)));
 #pragma unroll
-    for (int i = 0; i < C; ++i) x[i] = fmaf(x[i] * rstd, w[i], b[i]);
-    R::store(static_cast<T*>(p.y) + r * p.ld_y, r < p.rows ? d : 0, t, G, x);
+    for (int i = 0; i < H; ++i) x[i] = fma2(mul2(x[i], pair(rstd)), w[i], b[i]);
+    R::store_pairs(static_cast<T*>(p.y) + r * p.ld_y, r < p.rows ? d : 0, t, G, x);
     if (t == 0 && r < p.rows) {
       if (p.mean != nullptr && p.layer) p.mean[r] = mean;
       if (p.rstd != nullptr) p.rstd[r] = rstd;
     }
   }
+  feed_end<kVec>();
 }
 
 // Rows too long for registers: a CTA a row, read once a sum and once more.
@@ -203,96 +321,137 @@ template <typename T, bool kVec, bool kCta, bool kWide, int C>
 __global__ void __launch_bounds__(kWide ? 1024 : kCta ? 512 : 32 * kWarps)
     norm_backward_kernel(const __grid_constant__ GradParams p) {
   using R = RowPart<T, kVec, C>;
-  __shared__ float red[2][64];
-  extern __shared__ float wide[];              // kWide: weights, dw, db; warps of rows: [2, d] to add up
+  // kWide: the rows are read as they are needed
+  constexpr bool kFed = kVec && !kWide;
+  constexpr int kSlots = kFed ? kBackwardSlots : 1;
+  constexpr int H = C / 2;
+  __shared__ __align__(16) float red[2][64];
+  // kWide: weights, dw, db; else the rows on their way, and at the end [2, d] of a CTA's warps to add up
+  extern __shared__ __align__(16) float wide[];
   const Turns u = turns<kCta>(p.lanes);
   const int G = u.G, t = u.t, d = static_cast<int>(p.d);
+  if (kCta) clear_sums(&red[0][0], 128);
   griddep_wait();
-  // where thread t's value i stands in shared memory: neighbouring threads side by side
+  // where thread t's pair i stands in shared memory: neighbouring threads side by side
+  float2* wide2 = reinterpret_cast<float2*>(wide);
   const auto at = [&](int i) { return i * G + t; };
-  const int n = C * G;
-  float w[kWide ? 1 : C], dw[kWide ? 1 : C], db[kWide ? 1 : C];
-#pragma unroll
-  for (int i = 0; i < C; ++i) {
-    const int c = R::column(t, G, i);
-    const float v = p.w != nullptr && c < d ? load_any(p.w, p.wt, c) : 1.0f;
-    if constexpr (kWide) {
-      wide[at(i)] = v;
-      wide[n + at(i)] = wide[2 * n + at(i)] = 0.0f;
-    } else {
-      w[i] = v;
-      dw[i] = db[i] = 0.0f;
-    }
-  }
+  const int n = H * G;
+  float2 w[kWide ? 1 : H], dw[kWide ? 1 : H], db[kWide ? 1 : H];
   const T* xs = static_cast<const T*>(p.x);
   const T* dys = static_cast<const T*>(p.dy);
-  R nx, ny;
-  float mean_next = 0.0f, rstd_next = 0.0f;
-  const auto fetch = [&](int64_t row) {
+  Feed<T, kVec, C, kSlots> nx(wide, 0, d, t, G), ny(wide, 1, d, t, G);
+  RowPart<T, kVec, C> rx, ry;                  // kWide
+  float mean_next[kSlots], rstd_next[kSlots];
+  const auto send = [&](int k, int64_t row) {
     const bool in = row < p.rows;
-    nx.load(xs + row * p.ld_x, in ? d : 0, t, G);
-    ny.load(dys + row * p.ld_dy, in ? d : 0, t, G);
-    if (p.layer) mean_next = in ? p.mean[row] : 0.0f;
-    rstd_next = in ? p.rstd[row] : 0.0f;
+    if constexpr (kWide) {
+      rx.load(xs + (in ? row * p.ld_x : 0), in ? d : 0, t, G);
+      ry.load(dys + (in ? row * p.ld_dy : 0), in ? d : 0, t, G);
+    } else {
+      nx.send(xs, row, p.ld_x, in, d, t, G);
+      ny.send(dys, row, p.ld_dy, in, d, t, G);
+    }
+    feed_commit<kFed>();
+    mean_next[k] = p.layer && in ? p.mean[row] : 0.0f;
+    rstd_next[k] = in ? p.rstd[row] : 0.0f;
   };
-  fetch(u.first + u.sub);
+#pragma unroll
+  for (int k = 0; k < kSlots; ++k) {
+    send(k, u.first + k * u.step + u.sub);
+    nx.next();
+    ny.next();
+  }
+#pragma unroll
+  for (int i = 0; i < H; ++i) {
+    float2 v;
+    const int c0 = R::column(t, G, 2 * i), c1 = R::column(t, G, 2 * i + 1);
+    v.x = p.w != nullptr && c0 < d ? load_any(p.w, p.wt, c0) : 1.0f;
+    v.y = p.w != nullptr && c1 < d ? load_any(p.w, p.wt, c1) : 1.0f;
+    if constexpr (kWide) {
+      wide2[at(i)] = v;
+      wide2[n + at(i)] = wide2[2 * n + at(i)] = pair(0.0f);
+    } else {
+      w[i] = v;
+      dw[i] = db[i] = pair(0.0f);
+    }
+  }
   int turn = 0;
   for (int64_t first = u.first; first < p.rows; first += u.step, turn ^= 1) {
     const int64_t r = first + u.sub;
-    float x[C], g[C];
-    nx.floats(x);
-    ny.floats(g);
-    const float mean = mean_next, rstd = rstd_next;
-    if constexpr (!kWide) fetch(r + u.step);
-    float s[2] = {0.0f, 0.0f};                 // of h n and h
-#pragma unroll
-    for (int i = 0; i < C; ++i) {
-      x[i] = R::column(t, G, i) < d ? (x[i] - mean) * rstd : 0.0f;
-      if constexpr (kWide) {
-        wide[n + at(i)] = fmaf(g[i], x[i], wide[n + at(i)]);
-        wide[2 * n + at(i)] += g[i];
-        g[i] *= wide[at(i)];
-      } else {
-        dw[i] = fmaf(g[i], x[i], dw[i]);
-        db[i] += g[i];
-        g[i] *= w[i];
-      }
-      s[0] = fmaf(g[i], x[i], s[0]);
-      s[1] += g[i];
+    float2 x[H], g[H];
+    feed_wait<kFed, kSlots>();
+    if constexpr (kWide) {
+      rx.pairs(x);
+      ry.pairs(g);
+    } else {
+      nx.take(x);
+      ny.take(g);
     }
-    row_sums<kCta>(s, G, red[turn]);
-    const float along = s[0] * p.inv_d, level = p.layer ? s[1] * p.inv_d : 0.0f;
+    const float mean = mean_next[0], rstd = rstd_next[0];
 #pragma unroll
-    for (int i = 0; i < C; ++i) x[i] = rstd * (g[i] - fmaf(x[i], along, level));
-    R::store(static_cast<T*>(p.dx) + r * p.ld_dx, r < p.rows ? d : 0, t, G, x);
-    if constexpr (kWide) fetch(r + u.step);
+    for (int k = 1; k < kSlots; ++k) {
+      mean_next[k - 1] = mean_next[k];
+      rstd_next[k - 1] = rstd_next[k];
+    }
+    if constexpr (!kWide) {
+      send(kSlots - 1, r + kSlots * u.step);
+      nx.next();
+      ny.next();
+    }
+    // past the row's end dy is 0: nothing there counts
+    float2 along2 = pair(0.0f), level2 = pair(0.0f);
+#pragma unroll
+    for (int i = 0; i < H; ++i) {
+      x[i] = mul2(add2(x[i], pair(-mean)), pair(rstd));
+      if constexpr (kWide) {
+        wide2[n + at(i)] = fma2(g[i], x[i], wide2[n + at(i)]);
+        wide2[2 * n + at(i)] = add2(wide2[2 * n + at(i)], g[i]);
+        g[i] = mul2(g[i], wide2[at(i)]);
+      } else {
+        dw[i] = fma2(g[i], x[i], dw[i]);
+        db[i] = add2(db[i], g[i]);
+        g[i] = mul2(g[i], w[i]);
+      }
+      along2 = fma2(g[i], x[i], along2);
+      level2 = add2(level2, g[i]);
+    }
+    float s[2] = {along2.x + along2.y, level2.x + level2.y};
+    row_sums<kCta>(s, G, red[turn]);
+    const float2 along = pair(-s[0] * p.inv_d), level = pair(p.layer ? -s[1] * p.inv_d : 0.0f);
+#pragma unroll
+    for (int i = 0; i < H; ++i) x[i] = mul2(add2(fma2(x[i], along, g[i]), level), pair(rstd));
+    R::store_pairs(static_cast<T*>(p.dx) + r * p.ld_dx, r < p.rows ? d : 0, t, G, x);
+    if constexpr (kWide) send(0, r + u.step);
   }
+  feed_end<kFed>();
   if (p.part == nullptr) return;
   float* part = p.part + static_cast<int64_t>(blockIdx.x) * 2 * d;
+  const auto put = [&](float* to, int i, const float2& v) {
+    const int c0 = R::column(t, G, 2 * i), c1 = R::column(t, G, 2 * i + 1);
+    if (c0 < d) to[c0] = v.x;
+    if (c1 < d) to[c1] = v.y;
+  };
   if constexpr (kWide) {
 #pragma unroll
-    for (int i = 0; i < C; ++i) {
-      const int c = R::column(t, G, i);
-      if (c < d) {
-        part[c] = wide[n + at(i)];
-        part[d + c] = wide[2 * n + at(i)];
-      }
+    for (int i = 0; i < H; ++i) {
+      put(part, i, wide2[n + at(i)]);
+      put(part + d, i, wide2[2 * n + at(i)]);
     }
   } else if constexpr (kCta) {
 #pragma unroll
-    for (int i = 0; i < C; ++i) {
-      const int c = R::column(t, G, i);
-      if (c < d) {
-        part[c] = dw[i];
-        part[d + c] = db[i];
-      }
+    for (int i = 0; i < H; ++i) {
+      put(part, i, dw[i]);
+      put(part + d, i, db[i]);
     }
   } else {
+    __syncthreads();                           // the slots are free
     for (int o = G; o < 32; o <<= 1) {         // the warp's rows
 #pragma unroll
-      for (int i = 0; i < C; ++i) {
-        dw[i] += __shfl_xor_sync(0xffffffffu, dw[i], o);
-        db[i] += __shfl_xor_sync(0xffffffffu, db[i], o);
+      for (int i = 0; i < H; ++i) {
+        dw[i].x += __shfl_xor_sync(0xffffffffu, dw[i].x, o);
+        dw[i].y += __shfl_xor_sync(0xffffffffu, dw[i].y, o);
+        db[i].x += __shfl_xor_sync(0xffffffffu, db[i].x, o);
+        db[i].y += __shfl_xor_sync(0xffffffffu, db[i].y, o);
       }
     }
     const int warp = threadIdx.x >> 5;         // one warp after the other: a fixed order
@@ -302,8 +461,10 @@ __global__ void __launch_bounds__(kWide ? 1024 : kCta ? 512 : 32 * kWarps)
         for (int i = 0; i < C; ++i) {
           const int c = R::column(t, G, i);
           if (c < d) {
-            wide[c] = k == 0 ? dw[i] : wide[c] + dw[i];
-            wide[d + c] = k == 0 ? db[i] : wide[d + c] + db[i];
+            const float vw = i % 2 == 0 ? dw[i / 2].x : dw[i / 2].y;
+            const float vb = i % 2 == 0 ? db[i / 2].x : db[i / 2].y;
+            wide[c] = k == 0 ? vw : wide[c] + vw;
+            wide[d + c] = k == 0 ? vb : wide[d + c] + vb;
           }
         }
       }
@@ -363,29 +524,27 @@ __global__ void __launch_bounds__(128) norm_columns_kernel(const __grid_constant
   part[p.d + c] = db.s;
 }
 
-// dw and db from the CTAs' sums: 32 columns a CTA, its 8 warps every eighth of them.
-__global__ void __launch_bounds__(256) norm_parts_kernel(const float* __restrict__ part, int n,
-                                                         int64_t d, float* dw, float* db) {
-  __shared__ float red[8][32];
+// dw and db from the CTAs' sums: 32 columns a CTA, a warp every 32nd of them.
+constexpr int kPartWarps = 32;
+__global__ void __launch_bounds__(32 * kPartWarps) norm_parts_kernel(
+    const float* __restrict__ part, int n, int64_t d, float* dw, float* db) {
+  __shared__ float red[kPartWarps][33];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  const int64_t c = static_cast<int64_t>(blockIdx.x) * 32 + lane;
+  const int64_t c0 = static_cast<int64_t>(blockIdx.x) * 32;
   float* out = blockIdx.y == 0 ? dw : db;
   griddep_wait();
   if (out == nullptr) return;
-  const float* p = part + blockIdx.y * d + c;
+  const float* p = part + blockIdx.y * d + c0 + lane;
   float s = 0.0f;
-  if (c < d) {
+  if (c0 + lane < d) {
 #pragma unroll 8
-    for (int k = warp; k < n; k += 8) s += p[2 * d * k];
+    for (int k = warp; k < n; k += kPartWarps) s += p[2 * d * k];
   }
   red[warp][lane] = s;
   __syncthreads();
-  if (warp == 0 && c < d) {
-    float t = red[0][lane];
-#pragma unroll
-    for (int k = 1; k < 8; ++k) t += red[k][lane];
-    out[c] = t;
-  }
+  // column `warp`, its 32 sums across the lanes
+  s = warp_sum(red[lane][warp]);
+  if (lane == 0 && c0 + warp < d) out[c0 + warp] = s;
 }
 
 // Threads that share a row of the CTA kernels.
@@ -398,33 +557,59 @@ int row_lanes(int64_t d) {
   return lanes;
 }
 
-// CTAs of the kernels whose CTAs go over the rows: as many as are resident.
-int64_t forward_ctas(int64_t rows, int64_t d) {
-  if (d <= kWarpCols)
-    return std::min(ceil_div(rows, kWarps * 32 / row_lanes(d)), int64_t{kPlanCTAs} * 8);
-  const int g = row_threads(d);
-  return std::min(rows, kPlanCTAs * std::max<int64_t>(1, 896 / g));
+// CTAs of the forward kernels, which go over the rows: as many as are resident (one more than that
+// would wait for all of another's rows: 65,536 x 2048 at 7 CTAs an SM where 6 fit 160 us, not 103).
+template <typename Kernel>
+cudaError_t resident_ctas(std::atomic<int>* known, Kernel kernel, int threads, size_t smem,
+                          int64_t* ctas) {
+  int n = known[threads / 32].load(std::memory_order_relaxed);
+  if (n == 0) {
+    const cudaError_t e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&n, kernel, threads, smem);
+    if (e != cudaSuccess) return e;
+    known[threads / 32].store(n, std::memory_order_relaxed);
+  }
+  *ctas = static_cast<int64_t>(kPlanCTAs) * std::max(1, n);
+  return cudaSuccess;
 }
+
+// The backward pass takes three rows a CTA at least: a CTA's sums cost about as much as a row.
 int64_t backward_ctas(int64_t rows, int64_t d) {
   if (d <= kWarpCols)
-    return std::min(ceil_div(rows, kWarps * 32 / row_lanes(d)), int64_t{kPlanCTAs} * 5);
+    return std::min(ceil_div(rows, 3 * kWarps * 32 / row_lanes(d)), int64_t{kPlanCTAs} * 5);
   const int g = row_threads(d);
-  return std::min(rows, kPlanCTAs * std::max<int64_t>(1, 512 / g));
+  return std::min(ceil_div(rows, 3), kPlanCTAs * std::max<int64_t>(1, 512 / g));
 }
 int64_t column_slabs(int64_t rows) { return std::min<int64_t>(ceil_div(rows, kSlabRows), 64); }
 
+// Bytes of a kernel's rows on their way, and the most that a kernel of C columns a thread takes.
+template <typename T, bool kVec, int C, int kSlots>
+constexpr size_t slot_bytes(int threads, int parts) {
+  return static_cast<size_t>(parts) * kSlots * Feed<T, kVec, C, kSlots>::kBytes * threads;
+}
+
+template <typename T, bool kVec, bool kCta, bool kWide, int C>
+cudaError_t run_norm_rows(const NormParams& p, int threads, int64_t units, cudaStream_t s) {
+  static std::atomic<int> known[33];
+  static PerDeviceOnce attr;
+  const auto kernel = norm_kernel<T, kVec, kCta, kWide, C>;
+  constexpr int kMost = kWide ? 1024 : kCta ? 512 : 32 * kWarps;
+  const size_t smem = slot_bytes<T, kVec, C, kForwardSlots>(threads, 1);
+  cudaError_t e = smem_attr_once(
+      attr, kernel, static_cast<int>(slot_bytes<T, kVec, C, kForwardSlots>(kMost, 1)));
+  int64_t ctas = 0;
+  if (e == cudaSuccess) e = resident_ctas(known, kernel, threads, smem, &ctas);
+  if (e != cudaSuccess) return e;
+  return launch_dependent(kernel, dim3(static_cast<unsigned>(std::min(units, ctas))), dim3(threads),
+                          smem, s, p);
+}
+
 template <typename T, bool kVec>
 cudaError_t run_norm(const NormParams& p, cudaStream_t s) {
-  const dim3 grid(static_cast<unsigned>(forward_ctas(p.rows, p.d)));
-  if (p.d <= kShortCols)
-    return launch_dependent(norm_kernel<T, kVec, false, false, 8>, grid, dim3(32 * kWarps), 0, s,
-                            p);
-  if (p.d <= kWarpCols)
-    return launch_dependent(norm_kernel<T, kVec, false, false, kCols>, grid, dim3(32 * kWarps), 0,
-                            s, p);
-  const auto kernel = p.d <= kMidCols ? norm_kernel<T, kVec, true, false, kCols>
-                                      : norm_kernel<T, kVec, true, true, kCols>;
-  return launch_dependent(kernel, grid, dim3(row_threads(p.d)), 0, s, p);
+  const int64_t units = p.d <= kWarpCols ? ceil_div(p.rows, kWarps * 32 / p.lanes) : p.rows;
+  if (p.d <= kShortCols) return run_norm_rows<T, kVec, false, false, 8>(p, 32 * kWarps, units, s);
+  if (p.d <= kWarpCols) return run_norm_rows<T, kVec, false, false, kCols>(p, 32 * kWarps, units, s);
+  if (p.d <= kMidCols) return run_norm_rows<T, kVec, true, false, kCols>(p, row_threads(p.d), units, s);
+  return run_norm_rows<T, kVec, true, true, kCols>(p, row_threads(p.d), units, s);
 }
 
 template <typename T>
@@ -437,30 +622,28 @@ cudaError_t run_norm_any(const NormParams& p, cudaStream_t s) {
   return vec ? run_norm<T, true>(p, s) : run_norm<T, false>(p, s);
 }
 
-template <typename T, bool kVec, bool kWide>
-cudaError_t run_backward_cta(const GradParams& p, dim3 grid, size_t smem, cudaStream_t s) {
-  const auto kernel = norm_backward_kernel<T, kVec, true, kWide, kCols>;
-  if (kWide) {
-    static PerDeviceOnce attr;
-    const cudaError_t e = smem_attr_once(attr, kernel, 3 * kMaxCols * sizeof(float));
-    if (e != cudaSuccess) return e;
-  }
-  return launch_dependent(kernel, grid, dim3(row_threads(p.d)), smem, s, p);
+template <typename T, bool kVec, bool kCta, bool kWide, int C>
+cudaError_t run_backward_rows(const GradParams& p, dim3 grid, int threads, cudaStream_t s) {
+  const auto kernel = norm_backward_kernel<T, kVec, kCta, kWide, C>;
+  constexpr int kMost = kWide ? 1024 : kCta ? 512 : 32 * kWarps;
+  const auto bytes = [](int n) {
+    if (kWide) return 3 * kCols * sizeof(float) * n;
+    const size_t sums = kCta ? 0 : 2 * kWarpCols * sizeof(float);
+    return std::max(sums, slot_bytes<T, kVec, C, kBackwardSlots>(n, 2));
+  };
+  static PerDeviceOnce attr;
+  const cudaError_t e = smem_attr_once(attr, kernel, static_cast<int>(bytes(kMost)));
+  if (e != cudaSuccess) return e;
+  return launch_dependent(kernel, grid, dim3(threads), bytes(threads), s, p);
 }
 
 template <typename T, bool kVec>
 cudaError_t run_backward(const GradParams& p, int64_t ctas, cudaStream_t s) {
   const dim3 grid(static_cast<unsigned>(ctas));
-  const size_t sums = 2 * p.d * sizeof(float);
-  if (p.d <= kShortCols)
-    return launch_dependent(norm_backward_kernel<T, kVec, false, false, 8>, grid,
-                            dim3(32 * kWarps), sums, s, p);
-  if (p.d <= kWarpCols)
-    return launch_dependent(norm_backward_kernel<T, kVec, false, false, kCols>, grid,
-                            dim3(32 * kWarps), sums, s, p);
-  if (p.d <= kMidCols) return run_backward_cta<T, kVec, false>(p, grid, 0, s);
-  return run_backward_cta<T, kVec, true>(
-      p, grid, 3 * kCols * static_cast<size_t>(row_threads(p.d)) * sizeof(float), s);
+  if (p.d <= kShortCols) return run_backward_rows<T, kVec, false, false, 8>(p, grid, 32 * kWarps, s);
+  if (p.d <= kWarpCols) return run_backward_rows<T, kVec, false, false, kCols>(p, grid, 32 * kWarps, s);
+  if (p.d <= kMidCols) return run_backward_rows<T, kVec, true, false, kCols>(p, grid, row_threads(p.d), s);
+  return run_backward_rows<T, kVec, true, true, kCols>(p, grid, row_threads(p.d), s);
 }
 
 template <typename T>
@@ -545,7 +728,7 @@ cudaError_t launch_norm_backward(const NormGradArgs& a, void* ws, cudaStream_t s
                                            : run_backward_any<float>(p, parts, s);
   if (e != cudaSuccess || !sums) return e;
   const dim3 grid(static_cast<unsigned>(ceil_div(a.d, 32)), 2);
-  return launch_dependent(norm_parts_kernel, grid, dim3(256), 0, s,
+  return launch_dependent(norm_parts_kernel, grid, dim3(32 * kPartWarps), 0, s,
                           static_cast<const float*>(ws), static_cast<int>(parts), a.d, a.dw, a.db);
 }
 

@@ -138,76 +138,99 @@ struct RowPart {
   uint32_t raw[kWords];
 
   __device__ __forceinline__ static int col(int t, int G, int k) { return E * (t + k * G); }
+  // The column of element i of the thread's C.
+  __device__ __forceinline__ static int column(int t, int G, int i) {
+    return col(t, G, i / E) + i % E;
+  }
 
   __device__ __forceinline__ void load(const T* row, int d, int t, int G) {
+    const T* p = row + E * t;
+    const int left = d - E * t, step = E * G;    // columns from the thread's first one on
 #pragma unroll
-    for (int k = 0; k < kPer; ++k) {
-      const int c = col(t, G, k);
+    for (int k = 0; k < kPer; ++k, p += step) {
+      const int n = left - k * step;
       if constexpr (kVec) {
         uint4 v = make_uint4(0, 0, 0, 0);
-        if (c + E <= d) {
-          v = *reinterpret_cast<const uint4*>(row + c);
-        } else if (c < d) {
+        if (n >= E) {
+          v = *reinterpret_cast<const uint4*>(p);
+        } else if (n > 0) {
           __align__(16) T part[E];
 #pragma unroll
-          for (int i = 0; i < E; ++i) part[i] = c + i < d ? row[c + i] : T(0.0f);
+          for (int i = 0; i < E; ++i) part[i] = i < n ? p[i] : T(0.0f);
           v = *reinterpret_cast<const uint4*>(part);
         }
         raw[4 * k] = v.x; raw[4 * k + 1] = v.y; raw[4 * k + 2] = v.z; raw[4 * k + 3] = v.w;
       } else {
         raw[k] = 0;
-        if (c < d) {
-          if constexpr (sizeof(T) == 2) raw[k] = *reinterpret_cast<const uint16_t*>(row + c);
-          else raw[k] = __float_as_uint(row[c]);
+        if (n > 0) {
+          if constexpr (sizeof(T) == 2) raw[k] = *reinterpret_cast<const uint16_t*>(p);
+          else raw[k] = __float_as_uint(*p);
         }
       }
     }
   }
-  __device__ __forceinline__ void floats(float (&x)[C]) const {
+  // Pairs of neighbours among the thread's C.
+  __device__ __forceinline__ void pairs(float2 (&x)[C / 2]) const {
+    if constexpr (kVec) {
 #pragma unroll
-    for (int k = 0; k < kPer; ++k) {
-      if constexpr (kVec) {
+      for (int k = 0; k < kPer; ++k) {
         const uint4 v = make_uint4(raw[4 * k], raw[4 * k + 1], raw[4 * k + 2], raw[4 * k + 3]);
 #pragma unroll
-        for (int i = 0; i < E / 2; ++i) {
-          const float2 f = unpack2(v, i, static_cast<const T*>(nullptr));
-          x[E * k + 2 * i] = f.x;
-          x[E * k + 2 * i + 1] = f.y;
+        for (int i = 0; i < E / 2; ++i)
+          x[E / 2 * k + i] = unpack2(v, i, static_cast<const T*>(nullptr));
+      }
+    } else {
+#pragma unroll
+      for (int k = 0; k < C / 2; ++k) x[k] = make_float2(one(raw[2 * k]), one(raw[2 * k + 1]));
+    }
+  }
+  __device__ __forceinline__ static float one(uint32_t w) {
+    if constexpr (sizeof(T) == 2) {
+      const uint16_t u = static_cast<uint16_t>(w);
+      return to_f32(*reinterpret_cast<const T*>(&u));
+    } else {
+      return __uint_as_float(w);
+    }
+  }
+  __device__ __forceinline__ void floats(float (&x)[C]) const {
+    float2 y[C / 2];
+    pairs(y);
+#pragma unroll
+    for (int i = 0; i < C / 2; ++i) {
+      x[2 * i] = y[i].x;
+      x[2 * i + 1] = y[i].y;
+    }
+  }
+  __device__ __forceinline__ static void store_pairs(T* row, int d, int t, int G,
+                                                     const float2 (&x)[C / 2]) {
+    T* p = row + E * t;
+    const int left = d - E * t, step = E * G;
+#pragma unroll
+    for (int k = 0; k < kPer; ++k, p += step) {
+      const int n = left - k * step;
+      if constexpr (kVec) {
+        uint4 v;
+#pragma unroll
+        for (int i = 0; i < E / 2; ++i) pack2(v, i, x[E / 2 * k + i], static_cast<const T*>(nullptr));
+        if (n >= E) {
+          *reinterpret_cast<uint4*>(p) = v;
+        } else if (n > 0) {
+#pragma unroll
+          for (int i = 0; i < E; ++i) {
+            const float2 y = x[E / 2 * k + i / 2];
+            if (i < n) p[i] = from_f32<T>(i % 2 == 0 ? y.x : y.y);
+          }
         }
-      } else if constexpr (sizeof(T) == 2) {
-        const uint16_t u = static_cast<uint16_t>(raw[k]);
-        x[k] = to_f32(*reinterpret_cast<const T*>(&u));
-      } else {
-        x[k] = __uint_as_float(raw[k]);
+      } else if (n > 0) {
+        *p = from_f32<T>(k % 2 == 0 ? x[k / 2].x : x[k / 2].y);
       }
     }
   }
   __device__ __forceinline__ static void store(T* row, int d, int t, int G, const float (&x)[C]) {
+    float2 y[C / 2];
 #pragma unroll
-    for (int k = 0; k < kPer; ++k) {
-      const int c = col(t, G, k);
-      if constexpr (kVec) {
-        uint4 v;
-#pragma unroll
-        for (int i = 0; i < E / 2; ++i)
-          pack2(v, i, make_float2(x[E * k + 2 * i], x[E * k + 2 * i + 1]),
-                static_cast<const T*>(nullptr));
-        if (c + E <= d) {
-          *reinterpret_cast<uint4*>(row + c) = v;
-        } else if (c < d) {
-          const T* part = reinterpret_cast<const T*>(&v);
-#pragma unroll
-          for (int i = 0; i < E; ++i)
-            if (c + i < d) row[c + i] = part[i];
-        }
-      } else if (c < d) {
-        row[c] = from_f32<T>(x[k]);
-      }
-    }
-  }
-  // The column of element i of the thread's C.
-  __device__ __forceinline__ static int column(int t, int G, int i) {
-    return col(t, G, i / E) + i % E;
+    for (int i = 0; i < C / 2; ++i) y[i] = make_float2(x[2 * i], x[2 * i + 1]);
+    store_pairs(row, d, t, G, y);
   }
 };
 
