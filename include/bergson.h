@@ -961,10 +961,21 @@ BERGSON_API int bergson_factor_moments(const bergson_moment_matrix* mats, int n_
  * others keep their values.  rows in [0, 2^31), d <= 2^24.
  * Errors: EINVAL, EALIGN, EUNSUPPORTED, ECUDA.
  */
-BERGSON_API int bergson_norm(const void* x, int dtype, int64_t rows, int64_t d, int64_t ld_x,
-                             const void* weight, const void* bias, int w_dtype, int kind,
-                             double eps, void* y, int64_t ld_y, float* mean, float* rstd,
-                             void* stream);
+typedef struct bergson_norm_args {
+  const void* x;
+  const void* weight;
+  const void* bias;
+  void* y;
+  float* mean;
+  float* rstd;
+  int64_t rows, d, ld_x, ld_y;
+  double eps;
+  int32_t dtype, w_dtype;         /* bergson_dtype */
+  int32_t kind;                   /* bergson_norm_kind */
+  int32_t reserved;               /* 0 */
+} bergson_norm_args;
+
+BERGSON_API int bergson_norm(const bergson_norm_args* args, void* stream);
 
 /*
  * The backward pass: with n = (x - mu) rstd and h = dy weight,
@@ -980,13 +991,24 @@ BERGSON_API int bergson_norm(const void* x, int dtype, int64_t rows, int64_t d, 
  * Sums are fp32.
  * Errors: EINVAL, EALIGN, EUNSUPPORTED, EWORKSPACE, ECUDA.
  */
+typedef struct bergson_norm_grad_args {
+  const void* x;
+  const void* weight;
+  const float* mean;
+  const float* rstd;
+  const void* dy;
+  void* dx;
+  float* d_weight;
+  float* d_bias;
+  int64_t rows, d, ld_x, ld_dy, ld_dx;
+  int32_t dtype, w_dtype;         /* bergson_dtype */
+  int32_t kind;                   /* bergson_norm_kind */
+  int32_t reserved;               /* 0 */
+} bergson_norm_grad_args;
+
 BERGSON_API int bergson_norm_backward_workspace(int64_t rows, int64_t d, size_t* ws_bytes);
-BERGSON_API int bergson_norm_backward(const void* x, int dtype, int64_t rows, int64_t d,
-                                      int64_t ld_x, const void* weight, int w_dtype, int kind,
-                                      const float* mean, const float* rstd, const void* dy,
-                                      int64_t ld_dy, void* dx, int64_t ld_dx, float* d_weight,
-                                      float* d_bias, void* workspace, size_t ws_bytes,
-                                      void* stream);
+BERGSON_API int bergson_norm_backward(const bergson_norm_grad_args* args, void* workspace,
+                                      size_t ws_bytes, void* stream);
 
 /*
  * Embedding lookup with a scale: out[r] = scale table[ids[r]], rounded once.
@@ -999,9 +1021,17 @@ BERGSON_API int bergson_norm_backward(const void* x, int dtype, int64_t rows, in
  * rows, V in [0, 2^31), d <= 2^24.
  * Errors: EINVAL, EALIGN, EUNSUPPORTED, ECUDA.
  */
-BERGSON_API int bergson_embedding(const void* table, int dtype, int64_t V, int64_t d, int64_t ld_t,
-                                  const int64_t* ids, int64_t rows, double scale, void* out,
-                                  int64_t ld_o, void* stream);
+typedef struct bergson_embedding_args {
+  const void* table;
+  const int64_t* ids;
+  void* out;
+  int64_t V, d, rows, ld_t, ld_o;
+  double scale;
+  int32_t dtype;                  /* bergson_dtype */
+  int32_t reserved;               /* 0 */
+} bergson_embedding_args;
+
+BERGSON_API int bergson_embedding(const bergson_embedding_args* args, void* stream);
 
 /*
  * The table's gradient from dy, the gradient at the lookups,
@@ -1021,13 +1051,21 @@ BERGSON_API int bergson_embedding(const void* table, int dtype, int64_t V, int64
  * rows, V in [0, 2^31), d <= 2^24.
  * Errors: EINVAL, EALIGN, EUNSUPPORTED, EWORKSPACE, ECUDA.
  */
+typedef struct bergson_embedding_grad_args {
+  const void* dy;
+  const int64_t* ids;
+  void* d_table;
+  int64_t V, d, rows, ld_dy, ld_t;
+  double scale;
+  int32_t dtype, t_dtype;         /* bergson_dtype */
+  int32_t add;
+  int32_t reserved;               /* 0 */
+} bergson_embedding_grad_args;
+
 BERGSON_API int bergson_embedding_backward_workspace(int64_t rows, int64_t V, int64_t d,
                                                      size_t* ws_bytes);
-BERGSON_API int bergson_embedding_backward(const void* dy, int dtype, int64_t rows, int64_t d,
-                                           int64_t ld_dy, const int64_t* ids, double scale,
-                                           void* d_table, int t_dtype, int64_t V, int64_t ld_t,
-                                           int add, void* workspace, size_t ws_bytes,
-                                           void* stream);
+BERGSON_API int bergson_embedding_backward(const bergson_embedding_grad_args* args,
+                                           void* workspace, size_t ws_bytes, void* stream);
 
 /*
  * One matrix of a Muon step.

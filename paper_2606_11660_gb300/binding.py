@@ -132,9 +132,13 @@ class bergson_preference_args(ctypes.Structure):
         + [("ld_d", ctypes.c_int64), ("kind", ctypes.c_int32), ("mean_logp", ctypes.c_int32)])
 
 
-# The two records' fields, packed at once: as arguments of the ctypes classes they take twice the time.
+# The records' fields, packed at once: as arguments of the ctypes classes they take twice the time.
 _POLICY_RECORD = struct.Struct("=6Q8q5d5Q2q2i")
 _PREFERENCE_RECORD = struct.Struct("=3Q5q3d4Qq2i")
+_NORM_RECORD = struct.Struct("=6Q4qd4i")
+_NORM_GRAD_RECORD = struct.Struct("=8Q5q4i")
+_EMBEDDING_RECORD = struct.Struct("=3Q5qd2i")
+_EMBEDDING_GRAD_RECORD = struct.Struct("=3Q5qd4i")
 
 
 class bergson_adamw_tensor(ctypes.Structure):
@@ -247,14 +251,13 @@ def lib() -> ctypes.CDLL:
                                                    szp]),
         "bergson_factor_moments": (i32, [ctypes.POINTER(bergson_moment_matrix), i32, f64, f64, vp,
                                          ctypes.c_size_t, vp]),
-        "bergson_norm": (i32, [vp, i32, i64, i64, i64, vp, vp, i32, i32, f64, vp, i64, vp, vp, vp]),
+        # records, as bytes
+        "bergson_norm": (i32, [ctypes.c_char_p, vp]),
         "bergson_norm_backward_workspace": (i32, [i64, i64, szp]),
-        "bergson_norm_backward": (i32, [vp, i32, i64, i64, i64, vp, i32, i32, vp, vp, vp, i64, vp, i64,
-                                        vp, vp, vp, ctypes.c_size_t, vp]),
-        "bergson_embedding": (i32, [vp, i32, i64, i64, i64, vp, i64, f64, vp, i64, vp]),
+        "bergson_norm_backward": (i32, [ctypes.c_char_p, vp, ctypes.c_size_t, vp]),
+        "bergson_embedding": (i32, [ctypes.c_char_p, vp]),
         "bergson_embedding_backward_workspace": (i32, [i64, i64, i64, szp]),
-        "bergson_embedding_backward": (i32, [vp, i32, i64, i64, i64, vp, f64, vp, i32, i64, i64, i32, vp,
-                                             ctypes.c_size_t, vp]),
+        "bergson_embedding_backward": (i32, [ctypes.c_char_p, vp, ctypes.c_size_t, vp]),
         "bergson_muon_step_workspace": (i32, [ctypes.POINTER(bergson_muon_tensor), i32, i32, szp]),
         "bergson_muon_step": (i32, [ctypes.POINTER(bergson_muon_tensor), i32, f64, f64, i32,
                                     ctypes.POINTER(f64), i32, i32, vp, vp, ctypes.c_size_t, vp]),
@@ -927,26 +930,43 @@ def bergson_factor_moments(mats, correction: float, floor: float, workspace, str
                                         _stream(stream)))
 
 
-def _weights(weight, bias, d: int):
-    """(weight's pointer, bias's pointer, their dtype); None passes as NULL."""
-    one = weight if weight is not None else bias
-    if one is None:
-        return None, None, BERGSON_F32
-    return (_vector(weight, "weight", one.dtype, d), _vector(bias, "bias", one.dtype, d),
-            _dtype(one))
+def _matrix(t, what: str) -> tuple:
+    """(device pointer, shape, leading dimension, torch's and the library's dtype) of a matrix."""
+    shape, dtype = t.shape, t.dtype
+    code = _DTYPES.get(dtype)
+    if code is None:
+        code = _dtype(t)
+    ld, col = t.stride()
+    if col == 1 and ld >= shape[1] and t.is_cuda:
+        return t.data_ptr(), shape, ld, dtype, code
+    x, ld = _rows(t, what)
+    return x, shape, ld, dtype, code
+
+
+def _array(t, what: str, dtype, n: int) -> int:
+    """_vector() where None passes as 0."""
+    if t is None:
+        return 0
+    if t.dtype is dtype and t.is_cuda and t.numel() == n and t.is_contiguous():
+        return t.data_ptr()
+    return _vector(t, what, dtype, n)
 
 
 def bergson_norm(x, weight, bias, kind: int, eps: float, y, mean=None, rstd=None,
                  stream=None) -> None:
     """y = layer norm of the rows of x (kind: BERGSON_NORM_LAYER, or BERGSON_NORM_RMS without a
     mean), and the rows' mean and rstd; weight and bias may be None."""
-    rows, d = x.shape
-    dtype = _dtype(x)
-    px, ld = _rows(x, "x")
-    py, ld_y = _rows_like(y, "y", x.dtype, x.shape)
-    _check(lib().bergson_norm(px, dtype, rows, d, ld, *_weights(weight, bias, d), kind, eps, py, ld_y,
-                              _vector(mean, "mean", _F32, rows), _vector(rstd, "rstd", _F32, rows),
-                              _stream(stream)))
+    px, shape, ld, dtype, code = _matrix(x, "x")
+    py, ld_y = _rows_like(y, "y", dtype, shape)
+    rows, d = shape
+    one = weight if weight is not None else bias
+    wt, w_code = (_F32, BERGSON_F32) if one is None else (one.dtype, _dtype(one))
+    status = (_LIB or lib()).bergson_norm(_NORM_RECORD.pack(
+        px, _array(weight, "weight", wt, d), _array(bias, "bias", wt, d), py,
+        _array(mean, "mean", _F32, rows), _array(rstd, "rstd", _F32, rows), rows, d, ld, ld_y, eps, code,
+        w_code, kind, 0), _stream(stream))
+    if status:
+        _check(status)
 
 
 def bergson_norm_backward_workspace(rows: int, d: int) -> int:
@@ -958,28 +978,29 @@ def bergson_norm_backward_workspace(rows: int, d: int) -> int:
 def bergson_norm_backward(x, weight, kind: int, mean, rstd, dy, dx, d_weight, d_bias, workspace,
                           stream=None) -> None:
     """dx, d_weight and d_bias (either may be None) from the gradient at y."""
-    rows, d = x.shape
-    dtype = _dtype(x)
-    px, ld = _rows(x, "x")
-    pdy, ld_dy = _rows_like(dy, "dy", x.dtype, x.shape)
-    pdx, ld_dx = _rows_like(dx, "dx", x.dtype, x.shape)
-    w, _, w_dtype = _weights(weight, None, d)
-    _check(lib().bergson_norm_backward(
-        px, dtype, rows, d, ld, w, w_dtype, kind, _vector(mean, "mean", _F32, rows),
-        _vector(rstd, "rstd", _F32, rows), pdy, ld_dy, pdx, ld_dx,
-        _vector(d_weight, "d_weight", _F32, d), _vector(d_bias, "d_bias", _F32, d),
-        *_scratch(workspace), _stream(stream)))
+    px, shape, ld, dtype, code = _matrix(x, "x")
+    pdy, ld_dy = _rows_like(dy, "dy", dtype, shape)
+    pdx, ld_dx = _rows_like(dx, "dx", dtype, shape)
+    rows, d = shape
+    wt, w_code = (_F32, BERGSON_F32) if weight is None else (weight.dtype, _dtype(weight))
+    status = (_LIB or lib()).bergson_norm_backward(_NORM_GRAD_RECORD.pack(
+        px, _array(weight, "weight", wt, d), _array(mean, "mean", _F32, rows),
+        _array(rstd, "rstd", _F32, rows), pdy, pdx, _array(d_weight, "d_weight", _F32, d),
+        _array(d_bias, "d_bias", _F32, d), rows, d, ld, ld_dy, ld_dx, code, w_code, kind, 0),
+        *_scratch(workspace), _stream(stream))
+    if status:
+        _check(status)
 
 
 def bergson_embedding(table, ids, scale: float, out, stream=None) -> None:
     """out[r] = scale table[ids[r]]; a negative id gives zeros."""
-    V, d = table.shape
-    dtype = _dtype(table)
-    t, ld = _rows(table, "table")
+    t, (V, d), ld, dtype, code = _matrix(table, "table")
     rows = ids.numel()
-    po, ld_o = _rows_like(out, "out", table.dtype, (rows, d))
-    _check(lib().bergson_embedding(t, dtype, V, d, ld, _vector(ids, "ids", _I64, rows), rows, scale, po,
-                                   ld_o, _stream(stream)))
+    po, ld_o = _rows_like(out, "out", dtype, (rows, d))
+    status = (_LIB or lib()).bergson_embedding(_EMBEDDING_RECORD.pack(
+        t, _array(ids, "ids", _I64, rows), po, V, d, rows, ld, ld_o, scale, code, 0), _stream(stream))
+    if status:
+        _check(status)
 
 
 def bergson_embedding_backward_workspace(rows: int, V: int, d: int) -> int:
@@ -992,14 +1013,15 @@ def bergson_embedding_backward(dy, ids, scale: float, d_table, add: bool, worksp
                                stream=None) -> None:
     """The table's gradient from the gradient at the lookups, in place of d_table's values or
     (add) on top of them."""
-    rows, d = dy.shape
-    V = d_table.shape[0]
-    dtype = _dtype(dy)
-    g, ld = _rows(dy, "dy")
-    t, ld_t = _rows_like(d_table, "d_table", d_table.dtype, (V, d))
-    _check(lib().bergson_embedding_backward(
-        g, dtype, rows, d, ld, _vector(ids, "ids", _I64, rows), scale, t, _dtype(d_table), V, ld_t,
-        1 if add else 0, *_scratch(workspace), _stream(stream)))
+    g, (rows, d), ld, _, code = _matrix(dy, "dy")
+    t, (V, d_t), ld_t, _, t_code = _matrix(d_table, "d_table")
+    if d_t != d:
+        raise ValueError(f"d_table must have {d} columns, got {d_t}")
+    status = (_LIB or lib()).bergson_embedding_backward(_EMBEDDING_GRAD_RECORD.pack(
+        g, _array(ids, "ids", _I64, rows), t, V, d, rows, ld, ld_t, scale, code, t_code, 1 if add else 0, 0),
+        *_scratch(workspace), _stream(stream))
+    if status:
+        _check(status)
 
 
 @dataclasses.dataclass

@@ -612,7 +612,8 @@ SortPlan sort_plan(int64_t rows, int64_t V, int64_t d) {
 }
 
 template <typename T, bool kVec>
-cudaError_t run_few(const EmbeddingGradArgs& a, const GradOut& out, cudaStream_t s) {
+cudaError_t run_few(const bergson_embedding_grad_args& a, const GradOut& out, int* status,
+                    cudaStream_t s) {
   FewParams p = {};
   p.dy = a.dy;
   p.ids = a.ids;
@@ -623,14 +624,14 @@ cudaError_t run_few(const EmbeddingGradArgs& a, const GradOut& out, cudaStream_t
   p.d = static_cast<int>(a.d);
   p.group = slab_threads(a.d);
   p.slabs = static_cast<int>(ceil_div(a.d, p.group * kCols));
-  p.status = a.status;
+  p.status = status;
   const int64_t grid = a.rows * p.slabs + (a.add ? 0 : ceil_div(a.V, kFewZeros));
   return launch_dependent(few_rows_kernel<T, kVec>, dim3(static_cast<unsigned>(grid)),
                           dim3(kFewThreads), 0, s, p);
 }
 
 template <typename T, bool kVec>
-cudaError_t run_sums(const EmbeddingGradArgs& a, SumParams p, cudaStream_t s) {
+cudaError_t run_sums(const bergson_embedding_grad_args& a, SumParams p, cudaStream_t s) {
   const int threads = slab_threads(a.d);
   p.slabs = static_cast<int>(ceil_div(a.d, threads * kCols));
   p.n_sum = p.runs * p.slabs;
@@ -640,8 +641,8 @@ cudaError_t run_sums(const EmbeddingGradArgs& a, SumParams p, cudaStream_t s) {
                           dim3(threads), 0, s, p);
 }
 
-cudaError_t run_sorted(const EmbeddingGradArgs& a, const GradOut& out, bool vec, uint8_t* ws,
-                       cudaStream_t s) {
+cudaError_t run_sorted(const bergson_embedding_grad_args& a, const GradOut& out, bool vec,
+                       uint8_t* ws, int* status, cudaStream_t s) {
   const SortPlan plan = sort_plan(a.rows, a.V, a.d);
   SortParams p = {};
   p.ids = a.ids;
@@ -653,7 +654,7 @@ cudaError_t run_sorted(const EmbeddingGradArgs& a, const GradOut& out, bool vec,
   p.clear = p.table + plan.tiles * kBins;
   p.clear_words = a.add ? static_cast<int64_t>(plan.passes - 1) * plan.tiles * kBins
                         : plan.clear_words;
-  p.status = a.status;
+  p.status = status;
   const int64_t ctas =
       std::max<int64_t>(plan.tiles, std::min<int64_t>(kPlanCTAs, p.clear_words / 8192));
   cudaError_t e = launch_dependent(sort_count_kernel, dim3(static_cast<unsigned>(ctas)),
@@ -699,7 +700,7 @@ cudaError_t run_sorted(const EmbeddingGradArgs& a, const GradOut& out, bool vec,
 }
 
 template <typename T>
-cudaError_t run_lookup(const EmbeddingArgs& a, cudaStream_t s) {
+cudaError_t run_lookup(const bergson_embedding_args& a, int* status, cudaStream_t s) {
   const bool vec = on16(a.table, a.ld_t, sizeof(T)) && on16(a.out, a.ld_o, sizeof(T));
   LookupParams p = {};
   p.table = a.table;
@@ -712,7 +713,7 @@ cudaError_t run_lookup(const EmbeddingArgs& a, cudaStream_t s) {
   p.d = static_cast<int>(a.d);
   p.slabs = static_cast<int>(ceil_div(a.d, 32 * (vec ? 4 * Vec16<T>::kElems : 8)));
   p.scale = static_cast<float>(a.scale);
-  p.status = a.status;
+  p.status = status;
   const int64_t grid = ceil_div(a.rows * p.slabs, kLookupThreads / 32);
   if (grid > INT32_MAX) return cudaErrorInvalidConfiguration;
   const auto kernel = vec ? lookup_kernel<T, true> : lookup_kernel<T, false>;
@@ -721,17 +722,18 @@ cudaError_t run_lookup(const EmbeddingArgs& a, cudaStream_t s) {
 
 }  // namespace
 
-cudaError_t launch_embedding(const EmbeddingArgs& a, cudaStream_t s) {
-  if (a.dtype == BERGSON_BF16) return run_lookup<__nv_bfloat16>(a, s);
-  if (a.dtype == BERGSON_F16) return run_lookup<__half>(a, s);
-  return run_lookup<float>(a, s);
+cudaError_t launch_embedding(const bergson_embedding_args& a, int* status, cudaStream_t s) {
+  if (a.dtype == BERGSON_BF16) return run_lookup<__nv_bfloat16>(a, status, s);
+  if (a.dtype == BERGSON_F16) return run_lookup<__half>(a, status, s);
+  return run_lookup<float>(a, status, s);
 }
 
 size_t embedding_backward_workspace(int64_t rows, int64_t V, int64_t d) {
   return rows <= kFewRows ? 256 : sort_plan(rows, V, d).total;
 }
 
-cudaError_t launch_embedding_backward(const EmbeddingGradArgs& a, void* ws, cudaStream_t s) {
+cudaError_t launch_embedding_backward(const bergson_embedding_grad_args& a, void* ws, int* status,
+                                      cudaStream_t s) {
   GradOut out = {};
   out.table = a.d_table;
   out.ld = a.ld_t;
@@ -740,13 +742,15 @@ cudaError_t launch_embedding_backward(const EmbeddingGradArgs& a, void* ws, cuda
   out.add = a.add ? 1 : 0;
   out.scale = static_cast<float>(a.scale);
   const bool vec = on16(a.dy, a.ld_dy, a.dtype == BERGSON_F32 ? 4 : 2);
-  if (a.rows > kFewRows) return run_sorted(a, out, vec, static_cast<uint8_t*>(ws), s);
+  if (a.rows > kFewRows) return run_sorted(a, out, vec, static_cast<uint8_t*>(ws), status, s);
   if (a.rows == 0 && a.add) return cudaSuccess;
   if (a.dtype == BERGSON_BF16)
-    return vec ? run_few<__nv_bfloat16, true>(a, out, s) : run_few<__nv_bfloat16, false>(a, out, s);
+    return vec ? run_few<__nv_bfloat16, true>(a, out, status, s)
+               : run_few<__nv_bfloat16, false>(a, out, status, s);
   if (a.dtype == BERGSON_F16)
-    return vec ? run_few<__half, true>(a, out, s) : run_few<__half, false>(a, out, s);
-  return vec ? run_few<float, true>(a, out, s) : run_few<float, false>(a, out, s);
+    return vec ? run_few<__half, true>(a, out, status, s)
+               : run_few<__half, false>(a, out, status, s);
+  return vec ? run_few<float, true>(a, out, status, s) : run_few<float, false>(a, out, status, s);
 }
 
 }  // namespace bergson

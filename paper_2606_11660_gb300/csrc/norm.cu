@@ -670,7 +670,7 @@ int64_t backward_parts(int64_t rows, int64_t d) {
 
 }  // namespace
 
-cudaError_t launch_norm(const NormArgs& a, cudaStream_t s) {
+cudaError_t launch_norm(const bergson_norm_args& a, cudaStream_t s) {
   NormParams p = {};
   p.x = a.x;
   p.w = a.weight;
@@ -697,12 +697,12 @@ size_t norm_backward_workspace(int64_t rows, int64_t d) {
   return std::max<size_t>(256, (bytes + 255) / 256 * 256);
 }
 
-cudaError_t launch_norm_backward(const NormGradArgs& a, void* ws, cudaStream_t s) {
-  const bool sums = a.dw != nullptr || a.db != nullptr;
+cudaError_t launch_norm_backward(const bergson_norm_grad_args& a, void* ws, cudaStream_t s) {
+  const bool sums = a.d_weight != nullptr || a.d_bias != nullptr;
   if (a.rows == 0) {
     cudaError_t e = cudaSuccess;
-    if (a.dw != nullptr) e = cudaMemsetAsync(a.dw, 0, a.d * sizeof(float), s);
-    if (e == cudaSuccess && a.db != nullptr) e = cudaMemsetAsync(a.db, 0, a.d * sizeof(float), s);
+    if (a.d_weight != nullptr) e = cudaMemsetAsync(a.d_weight, 0, a.d * sizeof(float), s);
+    if (e == cudaSuccess && a.d_bias != nullptr) e = cudaMemsetAsync(a.d_bias, 0, a.d * sizeof(float), s);
     return e;
   }
   const int64_t parts = backward_parts(a.rows, a.d);
@@ -729,7 +729,7 @@ cudaError_t launch_norm_backward(const NormGradArgs& a, void* ws, cudaStream_t s
   if (e != cudaSuccess || !sums) return e;
   const dim3 grid(static_cast<unsigned>(ceil_div(a.d, 32)), 2);
   return launch_dependent(norm_parts_kernel, grid, dim3(32 * kPartWarps), 0, s,
-                          static_cast<const float*>(ws), static_cast<int>(parts), a.d, a.dw, a.db);
+                          static_cast<const float*>(ws), static_cast<int>(parts), a.d, a.d_weight, a.d_bias);
 }
 
 }  // namespace bergson

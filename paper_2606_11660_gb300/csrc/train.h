@@ -60,68 +60,14 @@ size_t moments_workspace(const bergson_moment_matrix* m, int n);
 cudaError_t launch_factor_moments(const bergson_moment_matrix* m, int n, double correction,
                                   double floor, void* ws, cudaStream_t s);
 
-struct NormArgs {
-  const void* x;               // [rows, ld_x] of dtype
-  int dtype;
-  int64_t rows, d, ld_x;
-  const void* weight;          // [d] of w_dtype, or nullptr: ones
-  const void* bias;            // [d] of w_dtype, or nullptr: zeros
-  int w_dtype;
-  int kind;                    // bergson_norm_kind
-  double eps;
-  void* y;                     // [rows, ld_y]
-  int64_t ld_y;
-  float* mean;                 // [rows], or nullptr; layer norm only
-  float* rstd;                 // [rows], or nullptr
-};
-cudaError_t launch_norm(const NormArgs& a, cudaStream_t s);
-
-struct NormGradArgs {
-  const void* x;
-  int dtype;
-  int64_t rows, d, ld_x;
-  const void* weight;
-  int w_dtype;
-  int kind;
-  const float* mean;           // layer norm only
-  const float* rstd;
-  const void* dy;              // [rows, ld_dy]
-  int64_t ld_dy;
-  void* dx;                    // [rows, ld_dx]
-  int64_t ld_dx;
-  float* dw;                   // [d], or nullptr
-  float* db;                   // [d], or nullptr
-};
+cudaError_t launch_norm(const bergson_norm_args& a, cudaStream_t s);
 size_t norm_backward_workspace(int64_t rows, int64_t d);
-cudaError_t launch_norm_backward(const NormGradArgs& a, void* ws, cudaStream_t s);
+cudaError_t launch_norm_backward(const bergson_norm_grad_args& a, void* ws, cudaStream_t s);
 
-struct EmbeddingArgs {
-  const void* table;           // [V, ld_t] of dtype
-  int dtype;
-  int64_t V, d, ld_t;
-  const int64_t* ids;          // [rows]
-  int64_t rows;
-  double scale;
-  void* out;                   // [rows, ld_o]
-  int64_t ld_o;
-  int* status;
-};
-cudaError_t launch_embedding(const EmbeddingArgs& a, cudaStream_t s);
-
-struct EmbeddingGradArgs {
-  const void* dy;              // [rows, ld_dy] of dtype
-  int dtype;
-  int64_t rows, d, ld_dy;
-  const int64_t* ids;          // [rows]
-  double scale;
-  void* d_table;               // [V, ld_t] of t_dtype
-  int t_dtype;
-  int64_t V, ld_t;
-  bool add;
-  int* status;
-};
+cudaError_t launch_embedding(const bergson_embedding_args& a, int* status, cudaStream_t s);
 size_t embedding_backward_workspace(int64_t rows, int64_t V, int64_t d);
-cudaError_t launch_embedding_backward(const EmbeddingGradArgs& a, void* ws, cudaStream_t s);
+cudaError_t launch_embedding_backward(const bergson_embedding_grad_args& a, void* ws, int* status,
+                                      cudaStream_t s);
 
 struct MuonScalars {
   double lr, beta;

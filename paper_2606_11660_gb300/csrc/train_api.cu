@@ -95,8 +95,9 @@ int check_norm_sizes(int64_t rows, int64_t d) {
 }
 
 int check_norm(int dtype, int64_t rows, int64_t d, const void* weight, const void* bias,
-               int w_dtype, int kind) {
+               int w_dtype, int kind, int reserved) {
   BERGSON_TRY(check_norm_sizes(rows, d));
+  if (reserved != 0) return fail(BERGSON_EINVAL, "reserved must be 0");
   if (dtype_size(dtype) == 0 || dtype_size(w_dtype) == 0)
     return fail(BERGSON_EINVAL, "unknown dtype (x %d, weight %d)", dtype, w_dtype);
   if (kind != BERGSON_NORM_LAYER && kind != BERGSON_NORM_RMS)
@@ -114,7 +115,10 @@ int check_in_place(const void* out, int64_t ld_out, const void* in, int64_t ld_i
   return BERGSON_OK;
 }
 
-int check_embedding(int64_t rows, int64_t V, int64_t d) {
+int check_embedding(int64_t rows, int64_t V, int64_t d, double scale, int reserved) {
+  if (reserved != 0) return fail(BERGSON_EINVAL, "reserved must be 0");
+  if (!std::isfinite(static_cast<float>(scale)))
+    return fail(BERGSON_EINVAL, "scale must be finite");
   if (rows < 0 || rows > INT32_MAX) return fail(BERGSON_EINVAL, "rows must be in [0, 2^31)");
   if (V < 1 || V > INT32_MAX) return fail(BERGSON_EINVAL, "V must be in [1, 2^31)");
   if (d < 1) return fail(BERGSON_EINVAL, "d must be >= 1");
@@ -459,24 +463,24 @@ int bergson_factor_moments(const bergson_moment_matrix* mats, int n_mats, double
   return BERGSON_OK;
 }
 
-int bergson_norm(const void* x, int dtype, int64_t rows, int64_t d, int64_t ld_x,
-                 const void* weight, const void* bias, int w_dtype, int kind, double eps, void* y,
-                 int64_t ld_y, float* mean, float* rstd, void* stream) {
-  BERGSON_TRY(check_norm(dtype, rows, d, weight, bias, w_dtype, kind));
-  if (!(eps >= 0.0) || !std::isfinite(static_cast<float>(eps)))
+int bergson_norm(const bergson_norm_args* args, void* stream) {
+  if (args == nullptr) return fail(BERGSON_EINVAL, "args is NULL");
+  const bergson_norm_args& a = *args;
+  BERGSON_TRY(check_norm(a.dtype, a.rows, a.d, a.weight, a.bias, a.w_dtype, a.kind, a.reserved));
+  if (!(a.eps >= 0.0) || !std::isfinite(static_cast<float>(a.eps)))
     return fail(BERGSON_EINVAL, "eps must be >= 0 and finite");
-  if (rows > 0) {
-    BERGSON_TRY(check_rows(x, dtype_size(dtype), d, ld_x, "x"));
-    BERGSON_TRY(check_rows(y, dtype_size(dtype), d, ld_y, "y"));
-    BERGSON_TRY(check_in_place(y, ld_y, x, ld_x, "y"));
-    if (mean != nullptr) BERGSON_TRY(check_tensor(mean, 4, "mean"));
-    if (rstd != nullptr) BERGSON_TRY(check_tensor(rstd, 4, "rstd"));
+  const size_t size = dtype_size(a.dtype);
+  if (a.rows > 0) {
+    BERGSON_TRY(check_rows(a.x, size, a.d, a.ld_x, "x"));
+    BERGSON_TRY(check_rows(a.y, size, a.d, a.ld_y, "y"));
+    BERGSON_TRY(check_in_place(a.y, a.ld_y, a.x, a.ld_x, "y"));
+    if (a.mean != nullptr) BERGSON_TRY(check_tensor(a.mean, 4, "mean"));
+    if (a.rstd != nullptr) BERGSON_TRY(check_tensor(a.rstd, 4, "rstd"));
   }
   BERGSON_TRY(injected_status());
-  if (rows == 0) return BERGSON_OK;
-  DeviceGuard dg(y);
+  if (a.rows == 0) return BERGSON_OK;
+  DeviceGuard dg(a.y);
   if (dg.err != cudaSuccess) return fail_cuda(dg.err, "output device lookup");
-  const NormArgs a{x, dtype, rows, d, ld_x, weight, bias, w_dtype, kind, eps, y, ld_y, mean, rstd};
   const cudaError_t e = launch_norm(a, static_cast<cudaStream_t>(stream));
   if (e != cudaSuccess) return fail_cuda(e, "norm launch");
   return BERGSON_OK;
@@ -489,92 +493,82 @@ int bergson_norm_backward_workspace(int64_t rows, int64_t d, size_t* ws_bytes) {
   return BERGSON_OK;
 }
 
-int bergson_norm_backward(const void* x, int dtype, int64_t rows, int64_t d, int64_t ld_x,
-                          const void* weight, int w_dtype, int kind, const float* mean,
-                          const float* rstd, const void* dy, int64_t ld_dy, void* dx,
-                          int64_t ld_dx, float* d_weight, float* d_bias, void* workspace,
-                          size_t ws_bytes, void* stream) {
-  BERGSON_TRY(check_norm(dtype, rows, d, weight, nullptr, w_dtype, kind));
-  const size_t size = dtype_size(dtype);
-  if (rows > 0) {
-    BERGSON_TRY(check_rows(x, size, d, ld_x, "x"));
-    BERGSON_TRY(check_rows(dy, size, d, ld_dy, "dy"));
-    BERGSON_TRY(check_rows(dx, size, d, ld_dx, "dx"));
-    BERGSON_TRY(check_in_place(dx, ld_dx, x, ld_x, "dx"));
-    BERGSON_TRY(check_in_place(dx, ld_dx, dy, ld_dy, "dx"));
-    if (kind == BERGSON_NORM_LAYER) BERGSON_TRY(check_tensor(mean, 4, "mean"));
-    BERGSON_TRY(check_tensor(rstd, 4, "rstd"));
+int bergson_norm_backward(const bergson_norm_grad_args* args, void* workspace, size_t ws_bytes,
+                          void* stream) {
+  if (args == nullptr) return fail(BERGSON_EINVAL, "args is NULL");
+  const bergson_norm_grad_args& a = *args;
+  BERGSON_TRY(check_norm(a.dtype, a.rows, a.d, a.weight, nullptr, a.w_dtype, a.kind, a.reserved));
+  const size_t size = dtype_size(a.dtype);
+  if (a.rows > 0) {
+    BERGSON_TRY(check_rows(a.x, size, a.d, a.ld_x, "x"));
+    BERGSON_TRY(check_rows(a.dy, size, a.d, a.ld_dy, "dy"));
+    BERGSON_TRY(check_rows(a.dx, size, a.d, a.ld_dx, "dx"));
+    BERGSON_TRY(check_in_place(a.dx, a.ld_dx, a.x, a.ld_x, "dx"));
+    BERGSON_TRY(check_in_place(a.dx, a.ld_dx, a.dy, a.ld_dy, "dx"));
+    if (a.kind == BERGSON_NORM_LAYER) BERGSON_TRY(check_tensor(a.mean, 4, "mean"));
+    BERGSON_TRY(check_tensor(a.rstd, 4, "rstd"));
   }
-  if (d_weight != nullptr) BERGSON_TRY(check_tensor(d_weight, 4, "d_weight"));
-  if (d_bias != nullptr) BERGSON_TRY(check_tensor(d_bias, 4, "d_bias"));
-  BERGSON_TRY(check_workspace(workspace, ws_bytes, norm_backward_workspace(rows, d)));
+  if (a.d_weight != nullptr) BERGSON_TRY(check_tensor(a.d_weight, 4, "d_weight"));
+  if (a.d_bias != nullptr) BERGSON_TRY(check_tensor(a.d_bias, 4, "d_bias"));
+  BERGSON_TRY(check_workspace(workspace, ws_bytes, norm_backward_workspace(a.rows, a.d)));
   BERGSON_TRY(injected_status());
   DeviceGuard dg(workspace);
   if (dg.err != cudaSuccess) return fail_cuda(dg.err, "workspace device lookup");
-  const NormGradArgs a{x,    dtype, rows, d,     ld_x, weight, w_dtype,  kind,
-                       mean, rstd,  dy,   ld_dy, dx,   ld_dx,  d_weight, d_bias};
   const cudaError_t e = launch_norm_backward(a, workspace, static_cast<cudaStream_t>(stream));
   if (e != cudaSuccess) return fail_cuda(e, "norm backward launch");
   return BERGSON_OK;
 }
 
-int bergson_embedding(const void* table, int dtype, int64_t V, int64_t d, int64_t ld_t,
-                      const int64_t* ids, int64_t rows, double scale, void* out, int64_t ld_o,
-                      void* stream) {
-  BERGSON_TRY(check_embedding(rows, V, d));
-  const size_t size = dtype_size(dtype);
-  if (size == 0) return fail(BERGSON_EINVAL, "unknown dtype %d", dtype);
-  if (!std::isfinite(static_cast<float>(scale)))
-    return fail(BERGSON_EINVAL, "scale must be finite");
-  if (rows > 0) {
-    BERGSON_TRY(check_rows(table, size, d, ld_t, "table"));
-    BERGSON_TRY(check_tensor(ids, 8, "ids"));
-    BERGSON_TRY(check_rows(out, size, d, ld_o, "out"));
+int bergson_embedding(const bergson_embedding_args* args, void* stream) {
+  if (args == nullptr) return fail(BERGSON_EINVAL, "args is NULL");
+  const bergson_embedding_args& a = *args;
+  BERGSON_TRY(check_embedding(a.rows, a.V, a.d, a.scale, a.reserved));
+  const size_t size = dtype_size(a.dtype);
+  if (size == 0) return fail(BERGSON_EINVAL, "unknown dtype %d", a.dtype);
+  if (a.rows > 0) {
+    BERGSON_TRY(check_rows(a.table, size, a.d, a.ld_t, "table"));
+    BERGSON_TRY(check_tensor(a.ids, 8, "ids"));
+    BERGSON_TRY(check_rows(a.out, size, a.d, a.ld_o, "out"));
   }
   BERGSON_TRY(injected_status());
-  if (rows == 0) return BERGSON_OK;
-  DeviceGuard dg(out);
+  if (a.rows == 0) return BERGSON_OK;
+  DeviceGuard dg(a.out);
   if (dg.err != cudaSuccess) return fail_cuda(dg.err, "output device lookup");
   int* status = device_status_word(dg.dev);
   if (status == nullptr) return fail(BERGSON_ECUDA, "device status word unavailable");
-  const EmbeddingArgs a{table, dtype, V, d, ld_t, ids, rows, scale, out, ld_o, status};
-  const cudaError_t e = launch_embedding(a, static_cast<cudaStream_t>(stream));
+  const cudaError_t e = launch_embedding(a, status, static_cast<cudaStream_t>(stream));
   if (e != cudaSuccess) return fail_cuda(e, "embedding launch");
   return BERGSON_OK;
 }
 
 int bergson_embedding_backward_workspace(int64_t rows, int64_t V, int64_t d, size_t* ws_bytes) {
   if (ws_bytes == nullptr) return fail(BERGSON_EINVAL, "ws_bytes is NULL");
-  BERGSON_TRY(check_embedding(rows, V, d));
+  BERGSON_TRY(check_embedding(rows, V, d, 1.0, 0));
   *ws_bytes = embedding_backward_workspace(rows, V, d);
   return BERGSON_OK;
 }
 
-int bergson_embedding_backward(const void* dy, int dtype, int64_t rows, int64_t d, int64_t ld_dy,
-                               const int64_t* ids, double scale, void* d_table, int t_dtype,
-                               int64_t V, int64_t ld_t, int add, void* workspace, size_t ws_bytes,
-                               void* stream) {
-  BERGSON_TRY(check_embedding(rows, V, d));
-  const size_t size = dtype_size(dtype), t_size = dtype_size(t_dtype);
+int bergson_embedding_backward(const bergson_embedding_grad_args* args, void* workspace,
+                               size_t ws_bytes, void* stream) {
+  if (args == nullptr) return fail(BERGSON_EINVAL, "args is NULL");
+  const bergson_embedding_grad_args& a = *args;
+  BERGSON_TRY(check_embedding(a.rows, a.V, a.d, a.scale, a.reserved));
+  const size_t size = dtype_size(a.dtype), t_size = dtype_size(a.t_dtype);
   if (size == 0 || t_size == 0)
-    return fail(BERGSON_EINVAL, "unknown dtype (dy %d, d_table %d)", dtype, t_dtype);
-  if (!std::isfinite(static_cast<float>(scale)))
-    return fail(BERGSON_EINVAL, "scale must be finite");
-  if (rows > 0) {
-    BERGSON_TRY(check_rows(dy, size, d, ld_dy, "dy"));
-    BERGSON_TRY(check_tensor(ids, 8, "ids"));
+    return fail(BERGSON_EINVAL, "unknown dtype (dy %d, d_table %d)", a.dtype, a.t_dtype);
+  if (a.rows > 0) {
+    BERGSON_TRY(check_rows(a.dy, size, a.d, a.ld_dy, "dy"));
+    BERGSON_TRY(check_tensor(a.ids, 8, "ids"));
   }
-  BERGSON_TRY(check_rows(d_table, t_size, d, ld_t, "d_table"));
-  BERGSON_TRY(check_workspace(workspace, ws_bytes, embedding_backward_workspace(rows, V, d)));
+  BERGSON_TRY(check_rows(a.d_table, t_size, a.d, a.ld_t, "d_table"));
+  BERGSON_TRY(check_workspace(workspace, ws_bytes, embedding_backward_workspace(a.rows, a.V, a.d)));
   BERGSON_TRY(injected_status());
-  DeviceGuard dg(d_table);
+  DeviceGuard dg(a.d_table);
   if (dg.err != cudaSuccess) return fail_cuda(dg.err, "output device lookup");
   int* status = device_status_word(dg.dev);
   if (status == nullptr) return fail(BERGSON_ECUDA, "device status word unavailable");
-  const EmbeddingGradArgs a{dy,      dtype,   rows, d,    ld_dy,    ids,   scale,
-                            d_table, t_dtype, V,    ld_t, add != 0, status};
   const cudaError_t e =
-      launch_embedding_backward(a, workspace, static_cast<cudaStream_t>(stream));
+      launch_embedding_backward(a, workspace, status, static_cast<cudaStream_t>(stream));
   if (e != cudaSuccess) return fail_cuda(e, "embedding backward launch");
   return BERGSON_OK;
 }

@@ -1,6 +1,7 @@
 """Host-side checks of the entry points around a model's linear layers that need no GPU:
 refusals of arguments, workspace sizes, records."""
 import ctypes
+import struct
 
 import pytest
 
@@ -30,18 +31,23 @@ def no_launch():
     bg.bergson_debug_inject_status(0, 0)
 
 
+def pack(layout, **values):
+    """A C record of 8-byte pointers and integers, doubles, and 32-bit integers, in that order."""
+    return struct.pack(layout, *[0 if v is None else v for v in values.values()])
+
+
 def norm(**kw):
-    a = dict(x=FAKE, dtype=bg.BERGSON_BF16, rows=4, d=100, ld_x=100, w=FAKE, b=FAKE, wt=0, kind=0,
-             eps=1e-5, y=FAKE + 4096, ld_y=100, mean=FAKE, rstd=FAKE)
+    a = dict(x=FAKE, w=FAKE, b=FAKE, y=FAKE + 4096, mean=FAKE, rstd=FAKE, rows=4, d=100, ld_x=100,
+             ld_y=100, eps=1e-5, dtype=bg.BERGSON_BF16, wt=0, kind=0, reserved=0)
     a.update(kw)
-    return bg.lib().bergson_norm(*a.values(), None)
+    return bg.lib().bergson_norm(pack("=6Q4qd4i", **a), None)
 
 
 def dnorm(ws=FAKE, ws_bytes=1 << 24, **kw):
-    a = dict(x=FAKE, dtype=bg.BERGSON_BF16, rows=4, d=100, ld_x=100, w=FAKE, wt=0, kind=0, mean=FAKE,
-             rstd=FAKE, dy=FAKE + 4096, ld_dy=100, dx=FAKE + 8192, ld_dx=100, dw=FAKE, db=FAKE)
+    a = dict(x=FAKE, w=FAKE, mean=FAKE, rstd=FAKE, dy=FAKE + 4096, dx=FAKE + 8192, dw=FAKE, db=FAKE, rows=4,
+             d=100, ld_x=100, ld_dy=100, ld_dx=100, dtype=bg.BERGSON_BF16, wt=0, kind=0, reserved=0)
     a.update(kw)
-    return bg.lib().bergson_norm_backward(*a.values(), ws, ws_bytes, None)
+    return bg.lib().bergson_norm_backward(pack("=8Q5q4i", **a), ws, ws_bytes, None)
 
 
 NORM_BAD = [
@@ -52,7 +58,7 @@ NORM_BAD = [
     (dict(x=None), bg.BERGSON_EINVAL), (dict(x=FAKE + 1), bg.BERGSON_EALIGN),
     (dict(dtype=0, x=FAKE + 2), bg.BERGSON_EALIGN), (dict(w=FAKE + 2), bg.BERGSON_EALIGN),
     (dict(kind=2), bg.BERGSON_EINVAL), (dict(mean=FAKE + 2), bg.BERGSON_EALIGN),
-    (dict(rstd=FAKE + 1), bg.BERGSON_EALIGN),
+    (dict(rstd=FAKE + 1), bg.BERGSON_EALIGN), (dict(reserved=1), bg.BERGSON_EINVAL),
 ]
 
 
@@ -87,6 +93,8 @@ def test_norm_calls_that_pass():
                dnorm(dx=FAKE), dnorm(dx=FAKE + 4096), dnorm(w=None),
                dnorm(rows=0, x=None, dy=None, dx=None, mean=None, rstd=None)):
         assert accepted(st), bg.bergson_last_error()
+    assert bg.lib().bergson_norm(None, None) == bg.BERGSON_EINVAL
+    assert bg.lib().bergson_norm_backward(None, FAKE, 1 << 20, None) == bg.BERGSON_EINVAL
     assert bg.lib().bergson_norm_backward_workspace(4, 4, None) == bg.BERGSON_EINVAL
     for rows, d in ((-1, 4), (4, 0), (1 << 31, 4)):
         with pytest.raises(bg.BergsonError):
@@ -97,17 +105,17 @@ def test_norm_calls_that_pass():
 
 
 def embed(**kw):
-    a = dict(table=FAKE, dtype=bg.BERGSON_BF16, V=50, d=100, ld_t=100, ids=FAKE, rows=4, scale=1.0,
-             out=FAKE + 65_536, ld_o=100)
+    a = dict(table=FAKE, ids=FAKE, out=FAKE + 65_536, V=50, d=100, rows=4, ld_t=100, ld_o=100, scale=1.0,
+             dtype=bg.BERGSON_BF16, reserved=0)
     a.update(kw)
-    return bg.lib().bergson_embedding(*a.values(), None)
+    return bg.lib().bergson_embedding(pack("=3Q5qd2i", **a), None)
 
 
 def dembed(ws=FAKE, ws_bytes=1 << 30, **kw):
-    a = dict(dy=FAKE, dtype=bg.BERGSON_BF16, rows=4, d=100, ld_dy=100, ids=FAKE, scale=1.0,
-             dt=FAKE + 65_536, tt=0, V=50, ld_t=100, add=0)
+    a = dict(dy=FAKE, ids=FAKE, dt=FAKE + 65_536, V=50, d=100, rows=4, ld_dy=100, ld_t=100, scale=1.0,
+             dtype=bg.BERGSON_BF16, tt=0, add=0, reserved=0)
     a.update(kw)
-    return bg.lib().bergson_embedding_backward(*a.values(), ws, ws_bytes, None)
+    return bg.lib().bergson_embedding_backward(pack("=3Q5qd4i", **a), ws, ws_bytes, None)
 
 
 EMBED_BAD = [
@@ -118,6 +126,7 @@ EMBED_BAD = [
     (dict(scale=INF), bg.BERGSON_EINVAL), (dict(scale=NAN), bg.BERGSON_EINVAL),
     (dict(scale=1e39), bg.BERGSON_EINVAL), (dict(ids=None), bg.BERGSON_EINVAL),
     (dict(ids=FAKE + 4), bg.BERGSON_EALIGN), (dict(ld_t=99), bg.BERGSON_EINVAL),
+    (dict(reserved=1), bg.BERGSON_EINVAL),
 ]
 
 
@@ -145,6 +154,8 @@ def test_embedding_calls_that_pass():
                dembed(rows=5000, ws_bytes=bg.bergson_embedding_backward_workspace(5000, 50, 100))):
         assert accepted(st), bg.bergson_last_error()
     assert dembed(rows=5000, ws_bytes=4096) == bg.BERGSON_EWORKSPACE
+    assert bg.lib().bergson_embedding(None, None) == bg.BERGSON_EINVAL
+    assert bg.lib().bergson_embedding_backward(None, FAKE, 1 << 20, None) == bg.BERGSON_EINVAL
     assert bg.lib().bergson_embedding_backward_workspace(4, 4, 4, None) == bg.BERGSON_EINVAL
     for sizes in ((0, 1, 1), (2048, 50_000, 64), (2049, 50_000, 64), (1 << 20, 1 << 18, 100)):
         need = bg.bergson_embedding_backward_workspace(*sizes)
