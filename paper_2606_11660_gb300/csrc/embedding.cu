@@ -80,7 +80,7 @@ constexpr int kCols = 8;                       // columns a thread
 constexpr int kAhead = 8;                      // rows on their way
 constexpr int kJoinThreads = 256;               // a warp joins the token that a run ends in
 constexpr int kJoinCols = 128;
-constexpr int kShortParts = 32;                // of so many runs
+constexpr int kShortParts = 16;                // of so many runs
 constexpr int kSortThreads = 1024;
 constexpr int kSortItems = 2048;               // items of a step of the sort
 constexpr int kDigitBits = 9;
@@ -501,11 +501,21 @@ __global__ void __launch_bounds__(kSumThreads) sum_kernel(const __grid_constant_
 __device__ __forceinline__ float4 add_parts(const SumParams& p, int64_t run, int64_t begin,
                                             int64_t end, int col) {
   float4 sum = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-#pragma unroll 16
-  for (int64_t q = begin; q < end; ++q) {
-    const float4 x = *reinterpret_cast<const float4*>(
-        p.part + (2 * (run + q) + (q == 0 ? 1 : 0)) * p.ld_part + col);
-    sum.x += x.x; sum.y += x.y; sum.z += x.z; sum.w += x.w;
+  constexpr int kParts = 8;                      // on their way
+  for (int64_t q0 = begin; q0 < end; q0 += kParts) {
+    float4 x[kParts];
+#pragma unroll
+    for (int k = 0; k < kParts; ++k) {
+      const int64_t q = q0 + k;
+      x[k] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+      if (q < end)
+        x[k] = *reinterpret_cast<const float4*>(
+            p.part + (2 * (run + q) + (q == 0 ? 1 : 0)) * p.ld_part + col);
+    }
+#pragma unroll
+    for (int k = 0; k < kParts; ++k) {
+      sum.x += x[k].x; sum.y += x[k].y; sum.z += x[k].z; sum.w += x[k].w;
+    }
   }
   return sum;
 }
