@@ -537,8 +537,16 @@ __global__ void __launch_bounds__(32 * kPartWarps) norm_parts_kernel(
   const float* p = part + blockIdx.y * d + c0 + lane;
   float s = 0.0f;
   if (c0 + lane < d) {
-#pragma unroll 8
-    for (int k = warp; k < n; k += kPartWarps) s += p[2 * d * k];
+    for (int k0 = warp; k0 < n; k0 += 8 * kPartWarps) {
+      float x[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const int k = k0 + i * kPartWarps;
+        x[i] = k < n ? p[2 * d * k] : 0.0f;
+      }
+#pragma unroll
+      for (int i = 0; i < 8; ++i) s += x[i];
+    }
   }
   red[warp][lane] = s;
   __syncthreads();

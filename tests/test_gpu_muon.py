@@ -138,13 +138,24 @@ def test_shapes_together(products):
         check_x(np64(x), np64(g), FIVE, products)
 
 
+@pytest.mark.parametrize("products", [3, 1])
 @pytest.mark.parametrize("shapes,count", [(6, 2), (30, 1), (3, 130)])
-def test_many_matrices(shapes, count):
+def test_many_matrices(shapes, count, products):
     """More shapes and matrices than a launch takes."""
     grads = [gradient(20 + 7 * s, 60 + s, c) for c in range(count) for s in range(shapes)]
-    got = orthogonalised(grads, FIVE, 3)
+    got = orthogonalised(grads, FIVE, products)
     for x, g in list(zip(got, grads))[::1 if shapes != 3 else 29]:
-        check_x(np64(x), np64(g), FIVE, 3)
+        check_x(np64(x), np64(g), FIVE, products)
+
+
+@pytest.mark.parametrize("products", [3, 1])
+@pytest.mark.parametrize("o,i", [(8, 70_000), (70_000, 8), (1100, 1300), (1300, 1100)])
+def test_long_and_wide(o, i, products):
+    """Sums over many stages; several rows of tiles, the last ones short."""
+    g = gradient(o, i)
+    k = [QUINTIC] * (2 if min(o, i) > 1000 else 5)
+    x, = orthogonalised([g], k, products)
+    check_x(np64(x), np64(g), k, products)
 
 
 def test_other_coefficients():
