@@ -158,6 +158,26 @@ def test_long_and_wide(o, i, products):
     check_x(np64(x), np64(g), k, products)
 
 
+@pytest.mark.parametrize("products", [3, 1])
+@pytest.mark.parametrize("o,i,count", [(1024, 1280, 10), (1290, 1030, 10), (700, 2000, 16)])
+def test_enough_to_fill_the_device(o, i, count, products):
+    """So many that tiles are at their widest, and a CTA pair has several."""
+    grads = [gradient(o, i, c) for c in range(count)]
+    k = [QUINTIC] * 2
+    got = orthogonalised(grads, k, products)
+    for z in (0, count - 1):
+        check_x(np64(got[z]), np64(grads[z]), k, products)
+    # the others against torch's products in 64 bits, to the bound of the last
+    _, tol = x_error(np64(grads[-1]), k, products)
+    for x, g in zip(got, grads):
+        y = g.double() / torch.linalg.matrix_norm(g.double())
+        y = y.t() if o > i else y
+        for a, b, c in k:
+            s = y @ y.t()
+            y = a * y + (b * s + c * s @ s) @ y
+        assert float(torch.linalg.matrix_norm(x.double() - (y.t() if o > i else y))) <= tol
+
+
 def test_other_coefficients():
     g = gradient(200, 333)
     for k in ([(1.5, -0.5, 0.0)] * 12, [(2.0, -1.5, 0.5)] * 8, [QUINTIC, (2.0, -1.5, 0.5), (1.875, -1.25, 0.375)],
