@@ -37,7 +37,7 @@ namespace bergson {
 namespace {
 
 constexpr float kPlaneScale = 1024.0f;         // of what the planes hold
-constexpr int kMaxGroups = 24;                 // shapes of a batch of matrices
+constexpr int kMaxGroups = 8;                  // shapes of a batch of matrices
 constexpr int kMaxMats = 300;                  // matrices of a batch
 constexpr int64_t kBatchElements = 1ll << 29;  // where a batch ends: bounds the workspace
 
@@ -76,6 +76,7 @@ struct MomentParams {
   int n;
   const float* grad_scale;
   float2* part;                // a CTA's sums of squares
+  int* counters;               // of the products: cleared by the first CTA
   int64_t chunk;               // elements a CTA
   uint32_t begin[N + 1];       // first CTA of each matrix
   MomentEntry e[N];
@@ -155,6 +156,8 @@ __global__ void __launch_bounds__(kMomentThreads) moment_kernel(
   const int k = entry_of(p);
   const MomentEntry& e = p.e[k];
   griddep_wait();
+  if (blockIdx.x == 0)
+    for (int i = threadIdx.x; i <= p.n; i += kMomentThreads) p.counters[i] = 0;
   const float gs = p.grad_scale != nullptr ? *p.grad_scale : 1.0f;
   const int64_t begin = static_cast<int64_t>(blockIdx.x - p.begin[k]) * p.chunk;
   const int64_t end = min(begin + p.chunk, e.n);
@@ -328,7 +331,8 @@ constexpr int kTileK = 64;                     // a stage: one 128-byte row of f
 constexpr int kBoxBytes = 64 * 128;
 constexpr int kPlaneBytes = 2 * kBoxBytes;     // of 128 rows of an operand's plane in a stage
 constexpr int kEpilogueWarps = 16;             // four to a quarter of the rows: 64 columns a thread
-constexpr int kThreads = 32 * (3 + kEpilogueWarps);    // A's loads, MMA, B's loads, epilogue
+constexpr int kFirstEpilogue = 4;              // warps: A's loads, MMA, B's loads, schedule, epilogue
+constexpr int kThreads = 32 * (kFirstEpilogue + kEpilogueWarps);
 constexpr int kChain = 4;                      // stages of an accumulation chain with two planes
 constexpr int kOutTile = 32 * 64;              // bytes
 constexpr int kBarBytes = 256;
@@ -352,44 +356,72 @@ struct ProdCfg {
 // How an operand [rows, K] of a product lies in memory.
 enum : int { kRowMajor = 0, kAcross = 1, kSymmetric = 2 };
 
-struct ProdGroup {
-  int begin;                   // first tile
+// The three products of an iteration: A' = X X^T + h I, B = c A'^2 + .., X' = B X.
+constexpr int kParts = 3;
+
+struct ProdGroup {             // of a shape's product
+  int begin;                   // first tile of the shape within the product's step
   int per_mat;                 // tiles of a matrix
   int n_mt, n_nt, tn;          // tiles of ProdCfg::kSub times tn columns
   int M, N, K;                 // of D [M, N]
   int a_kind, b_kind;
   int chunks_b;                // 64-row chunks of a box of B's across; 0: one each, tn % 128 != 0
   int lower;                   // only tiles that reach the diagonal or lie below
-  int dst_ld;
+};
+struct ShapeInfo {
+  ProdGroup part[kParts];
+  int first_mat;
+  int ld[2];                   // of X's planes, and of A' and B's
+  int64_t plane[2];
+  __half* buf[4];              // X, X', A', B
+};
+// An operand's boxes: of the rows as they lie, and across.
+struct Side {
+  CUtensorMap rows, across;
+};
+struct ShapeMaps {
+  Side a[5], b[5];             // of the first product by X's buffer, the second, the third by X's buffer
+  CUtensorMap out[4];          // of buf, boxes of 32 rows and columns (one plane)
+};
+__host__ __device__ constexpr int side_of(int part, int cur) {
+  return part == 0 ? cur : part == 1 ? 2 : 3 + cur;
+}
+struct Step {
+  int begin;                   // first tile
   float alpha, gamma;          // D' = alpha acc + gamma I
-  __half* dst;                 // planes
-  int64_t dst_plane;
+  uint8_t part, cur, dst;      // product, X's buffer, buf it writes
+  uint8_t before[kParts];      // steps before this one, by product
+  uint8_t pad[2];
 };
 
-template <int G>
+template <int G, int S>
 struct ProdParams {
-  CUtensorMap a[G], b[G];      // boxes of rows as they lie
-  CUtensorMap ax[G], bx[G];    // and across
-  CUtensorMap out[G];          // D', boxes of 32 rows and columns (one plane)
-  ProdGroup g[G];
-  int n;
-  int n_tiles;
+  ShapeMaps maps[G];
+  ShapeInfo info[G];
+  Step step[S];
+  int n, n_steps, n_tiles;
+  int* counters;               // tiles handed out; then per matrix, epilogue warps that are through with a tile
   int* status;
   uint64_t timeout_ns;
 };
 
 struct Tile {
-  int group, mat, mt, nt;
+  int step, group, mat, mt, nt;
   int subs;                    // accumulators that are needed: columns within D and not above the diagonal
 };
 
-template <int P, int G>
-__device__ __forceinline__ Tile tile_of(const ProdParams<G>& p, int t) {
+// Tile t, which is of step `step` or a later one.
+template <int P, int G, int S>
+__device__ __forceinline__ Tile tile_of(const ProdParams<G, S>& p, int t, int step) {
   constexpr int kSub = ProdCfg<P>::kSub;
   Tile o;
+  while (step + 1 < p.n_steps && p.step[step + 1].begin <= t) ++step;
+  o.step = step;
+  const int part = p.step[step].part;
+  t -= p.step[step].begin;
   o.group = 0;
-  while (o.group + 1 < p.n && p.g[o.group + 1].begin <= t) ++o.group;
-  const ProdGroup& g = p.g[o.group];
+  while (o.group + 1 < p.n && p.info[o.group + 1].part[part].begin <= t) ++o.group;
+  const ProdGroup& g = p.info[o.group].part[part];
   t -= g.begin;
   o.mat = t / g.per_mat;
   t -= o.mat * g.per_mat;
@@ -415,11 +447,72 @@ __device__ __forceinline__ Tile tile_of(const ProdParams<G>& p, int t) {
   return o;
 }
 
-// The tile of a cluster's i-th turn: there and back over the clusters, so that tiles that
-// fall in length come out even.  -1: none.
-__device__ __forceinline__ int tile_index(int i, int cid, int n_cl, int n_tiles) {
-  const int t = i * n_cl + ((i & 1) ? n_cl - 1 - cid : cid);
-  return t < n_tiles ? t : -1;
+// ---- The schedule.  Tiles are handed out in order, step by step, to pairs as they become free: a
+// warp of each pair takes the next one and passes it to the pair's others through a ring in shared
+// memory.  A matrix's tiles wait for all tiles of its earlier steps, which were handed out before:
+// whichever pairs run, the first unfinished tile can proceed, so that no pair needs another to be
+// resident.
+constexpr int kSlots = 2;
+constexpr int kTakers = 2 * (2 + kEpilogueWarps) + 1;    // loads and epilogue of both CTAs, MMA
+
+struct Ring {                  // in each CTA; `empty` counts in the even one
+  uint64_t full[kSlots], empty[kSlots];
+  int tile[kSlots];
+};
+
+__device__ __forceinline__ void store_remote(uint32_t cluster_addr, int v) {
+  asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(cluster_addr), "r"(v) : "memory");
+}
+
+// Hands out tiles, from one thread of the even CTA.
+__device__ __forceinline__ bool hand_out(Ring* ring, int* counter, int n_tiles, uint64_t tmo,
+                                         const volatile int* abort_flag) {
+  uint32_t ph = 0;
+  for (int slot = 0;;) {
+    if (!mbar_wait_cluster(smem_u32(&ring->empty[slot]), ph ^ 1, tmo, abort_flag)) return false;
+    const int t = atomicAdd(counter, 1);
+    const int tile = t < n_tiles ? t : -1;
+    for (uint32_t r = 0; r < 2; ++r) {
+      store_remote(mapa_shared(smem_u32(&ring->tile[slot]), r), tile);
+      mbar_arrive_cluster(mapa_shared(smem_u32(&ring->full[slot]), r));
+    }
+    if (tile < 0) return true;
+    if (++slot == kSlots) { slot = 0; ph ^= 1; }
+  }
+}
+
+// A taker's place in the ring; next() is called by one lane: the tile, -1 at the end, -2 when it gave up.
+struct Taker {
+  int slot = 0;
+  uint32_t ph = 0;
+  __device__ __forceinline__ int next(Ring* ring, uint64_t tmo, const volatile int* abort_flag) {
+    if (!mbar_wait_cluster(smem_u32(&ring->full[slot]), ph, tmo, abort_flag)) return -2;
+    const int t = *reinterpret_cast<volatile int*>(&ring->tile[slot]);
+    mbar_arrive_cluster(mapa_shared(smem_u32(&ring->empty[slot]), 0));
+    if (++slot == kSlots) { slot = 0; ph ^= 1; }
+    return t;
+  }
+  __device__ __forceinline__ int next_warp(Ring* ring, uint64_t tmo, const volatile int* abort_flag) {
+    int t = 0;
+    if ((threadIdx.x & 31) == 0) t = next(ring, tmo, abort_flag);
+    return __shfl_sync(0xffffffffu, t, 0);
+  }
+};
+
+// Waits until `need` epilogue warps are through with the matrix's earlier steps, whose planes
+// may be loaded then.
+__device__ __forceinline__ bool wait_matrix(const int* done, int need, uint64_t tmo,
+                                            const volatile int* abort_flag) {
+  const uint64_t t0 = global_timer_ns();
+  for (uint32_t it = 0;; ++it) {
+    int v;
+    asm volatile("ld.acquire.gpu.global.s32 %0, [%1];" : "=r"(v) : "l"(done) : "memory");
+    if (v >= need) break;
+    if (abort_flag != nullptr && *abort_flag) return false;
+    if (it == (1u << 30) || global_timer_ns() - t0 > tmo) return false;
+  }
+  asm volatile("fence.proxy.async;" ::: "memory");
+  return true;
 }
 
 // The stage from which on the operand rows from row0 on (a tile's first) are read across.
@@ -476,22 +569,42 @@ __device__ __forceinline__ bool elect_lane() {
 }
 
 // One side's loads of all the tiles of a CTA, by one thread.
-template <int P, bool kSideB, int G>
-__device__ __forceinline__ void load_side(const ProdParams<G>& p, int rank, int cid, int n_cl,
+template <int P, bool kSideB, int G, int S>
+__device__ __forceinline__ void load_side(const ProdParams<G, S>& p, int rank, Ring* ring,
                                           uint32_t sbase, uint64_t* full, uint64_t* empty,
                                           volatile int* s_abort) {
   using C = ProdCfg<P>;
   const uint64_t tmo = p.timeout_ns;
   const uint64_t pol = policy_evict_normal();
-  int stage = 0;
+  Taker taker;
+  int stage = 0, step = 0;
   uint32_t ph = 0;
   uint32_t issued = 0, issued_par = 0;
   bool ok = true;
-  for (int i = 0, t; ok && (t = tile_index(i, cid, n_cl, p.n_tiles)) >= 0; ++i) {
-    const Tile o = tile_of<P>(p, t);
-    const ProdGroup& g = p.g[o.group];
-    const void* rows_map = kSideB ? &p.b[o.group] : &p.a[o.group];
-    const void* across_map = kSideB ? &p.bx[o.group] : &p.ax[o.group];
+  while (ok) {
+    const int t = taker.next(ring, tmo, s_abort);
+    if (t < 0) {
+      ok = t == -1;
+      break;
+    }
+    const Tile o = tile_of<P>(p, t, step);
+    step = o.step;
+    const Step& st = p.step[step];
+    const ShapeInfo& info = p.info[o.group];
+    const ProdGroup& g = info.part[st.part];
+    int need = 0;
+#pragma unroll
+    for (int k = 0; k < kParts; ++k)
+      need += st.before[k] * info.part[k].per_mat * (2 * kEpilogueWarps);
+    if (need > 0 &&
+        !wait_matrix(p.counters + 1 + info.first_mat + o.mat, need, tmo, s_abort)) {
+      ok = false;
+      break;
+    }
+    const ShapeMaps& maps = p.maps[o.group];
+    const Side& side = kSideB ? maps.b[side_of(st.part, st.cur)] : maps.a[side_of(st.part, st.cur)];
+    const void* rows_map = &side.rows;
+    const void* across_map = &side.across;
     const int kind = kSideB ? g.b_kind : g.a_kind;
     const int z = o.mat * P;
     const int subs = kSideB ? o.subs : 1;
@@ -572,9 +685,9 @@ __device__ __forceinline__ void put_planes(__half* d, int64_t plane, const float
 // The tensor cores' fp32 sums round toward zero.  With two planes, an accumulation chain is
 // one stage (12 MMAs, its smallest terms first) and the epilogue adds the chains in registers while the
 // next one runs; with one plane the operands' own rounding is 2^-12 and a tile is one chain.
-template <int P, int G>
+template <int P, int G, int S>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
-    product_kernel(const __grid_constant__ ProdParams<G> p) {
+    products_kernel(const __grid_constant__ ProdParams<G, S> p) {
   using C = ProdCfg<P>;
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) &
@@ -586,12 +699,11 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
   uint64_t* tfull = empty + C::kStages;
   uint64_t* tempty = tfull + 2;
   uint64_t* drain = tempty + 2;
-  uint32_t* s_tmem = reinterpret_cast<uint32_t*>(drain + 1);
+  Ring* ring = reinterpret_cast<Ring*>(drain + 1);
+  uint32_t* s_tmem = reinterpret_cast<uint32_t*>(ring + 1);
   volatile int* s_abort = reinterpret_cast<volatile int*>(s_tmem + 1);
 
   const int rank = static_cast<int>(cluster_ctarank());
-  const int cid = blockIdx.x >> 1;
-  const int n_cl = gridDim.x >> 1;
   const int warp = threadIdx.x >> 5;
   const int lane = threadIdx.x & 31;
   griddep_launch_dependents();   // the next grid sets itself up and waits for this one to end
@@ -604,6 +716,10 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
       mbar_init(smem_u32(&tfull[i]), 1);
       mbar_init(smem_u32(&tempty[i]), 2 * kEpilogueWarps);     // of both CTAs
     }
+    for (int i = 0; i < kSlots; ++i) {
+      mbar_init(smem_u32(&ring->full[i]), 1);
+      mbar_init(smem_u32(&ring->empty[i]), kTakers);
+    }
     mbar_init(smem_u32(drain), 1);
     *s_abort = 0;
     fence_barrier_init();
@@ -611,11 +727,6 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
   if (warp == 1) {
     tmem_alloc_pair(smem_u32(s_tmem), kTmemCols);
     tmem_relinquish_pair();
-  }
-  if (lane == 0 && (warp == 0 || warp == 2) && tile_index(0, cid, n_cl, p.n_tiles) >= 0) {
-    const int group = tile_of<P>(p, tile_index(0, cid, n_cl, p.n_tiles)).group;
-    prefetch_tmap(warp == 0 ? &p.a[group] : &p.b[group]);
-    prefetch_tmap(warp == 0 ? &p.ax[group] : &p.bx[group]);
   }
   __syncwarp();
   tc_fence_before();
@@ -626,10 +737,14 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
   const uint64_t tmo = p.timeout_ns;
 
   if (warp == 0) {
-    if (lane == 0) load_side<P, false>(p, rank, cid, n_cl, sbase, full, empty, s_abort);
+    if (lane == 0) load_side<P, false>(p, rank, ring, sbase, full, empty, s_abort);
     __syncwarp();
   } else if (warp == 2) {
-    if (lane == 0) load_side<P, true>(p, rank, cid, n_cl, sbase, full, empty, s_abort);
+    if (lane == 0) load_side<P, true>(p, rank, ring, sbase, full, empty, s_abort);
+    __syncwarp();
+  } else if (warp == 3) {
+    if (rank == 0 && lane == 0 && !hand_out(ring, p.counters, p.n_tiles, tmo, s_abort))
+      raise_device_error(p.status, s_abort, kStatusTimeout);
     __syncwarp();
   } else if (warp == 1) {
     // ------------------------------------------------------------ MMA issuer (even CTA)
@@ -642,9 +757,17 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
       int ab = 0;                                    // the tile's first accumulator, its round's parity
       uint32_t aph = 0;
       bool ok = true;
-      for (int i = 0, t; ok && (t = tile_index(i, cid, n_cl, p.n_tiles)) >= 0; ++i) {
-        const Tile o = tile_of<P>(p, t);
-        const ProdGroup& g = p.g[o.group];
+      Taker taker;
+      int step = 0;
+      while (ok) {
+        const int t = taker.next_warp(ring, tmo, s_abort);
+        if (t < 0) {
+          ok = t == -1;
+          break;
+        }
+        const Tile o = tile_of<P>(p, t, step);
+        step = o.step;
+        const ProdGroup& g = p.info[o.group].part[p.step[step].part];
         const int subs = o.subs, tn = g.tn, stages = (g.K + kTileK - 1) / kTileK;
         // stages from which on an operand is read across
         const int xa_from = across_from(g.a_kind, o.mt * kTileM);
@@ -724,15 +847,26 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
     // Thread = a row of this CTA's half (TMEM lane) and up to 64 of an accumulator's columns: summed up
     // in registers, so that the accumulator is free again before anything is written.  A thread
     // writes whole 32-byte sectors of its row.
-    const int ew = warp - 3;
+    const int ew = warp - kFirstEpilogue;
     const int quarter = warp & 3;
     uint8_t* out = smem + C::kStages * C::kStageBytes + ew * kOutTile;
     int ab = 0;
     uint32_t aph = 0;
     bool aborted = false;
-    for (int i = 0, t; !aborted && (t = tile_index(i, cid, n_cl, p.n_tiles)) >= 0; ++i) {
-      const Tile o = tile_of<P>(p, t);
-      const ProdGroup& g = p.g[o.group];
+    Taker taker;
+    int step = 0;
+    while (!aborted) {
+      const int t = taker.next_warp(ring, tmo, s_abort);
+      if (t < 0) {
+        if (t != -1) raise_device_error(p.status, s_abort, kStatusTimeout);
+        break;
+      }
+      const Tile o = tile_of<P>(p, t, step);
+      step = o.step;
+      const Step& st = p.step[step];
+      const ShapeInfo& info = p.info[o.group];
+      const ProdGroup& g = info.part[st.part];
+      const int which = st.part == 2 ? 0 : 1;        // planes of X's, or of A' and B's
       const int pieces = g.tn / 16, first = pieces * (ew >> 2) / 4;      // of 16 columns
       const int mine = pieces * ((ew >> 2) + 1) / 4 - first;             // up to 4
       const int row = o.mt * kTileM + rank * (kTileM / 2) + 32 * quarter + lane;
@@ -779,7 +913,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
           if (++ab == 2) { ab = 0; aph ^= 1; }
         }
         if (aborted) break;
-        const float2 alpha = pair(g.alpha);
+        const float2 alpha = pair(st.alpha);
 #pragma unroll
         for (int j = 0; j < kAcc; j += 2) {
           const float2 x = mul2(make_float2(acc[j], acc[j + 1]), alpha);
@@ -787,8 +921,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
           acc[j + 1] = x.y;
         }
         const int row0 = row - lane;
-        if (g.gamma != 0.0f && row0 < col0 + kAcc && row0 + 32 > col0) {     // on the diagonal
-          const float gamma = g.gamma;
+        if (st.gamma != 0.0f && row0 < col0 + kAcc && row0 + 32 > col0) {     // on the diagonal
+          const float gamma = st.gamma;
 #pragma unroll
           for (int j = 0; j < kAcc; ++j) acc[j] += row == col0 + j ? gamma : 0.0f;
         }
@@ -812,25 +946,34 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
             if (lane == 0 && row0 < g.M && col0 + 16 * u < g.N) {
               asm volatile(
                   "cp.async.bulk.tensor.3d.global.shared::cta.bulk_group [%0, {%2, %3, %4}], [%1];"
-                  ::"l"(&p.out[o.group]), "r"(smem_u32(out)), "r"(col0 + 16 * u), "r"(row0),
+                  ::"l"(&p.maps[o.group].out[st.dst]), "r"(smem_u32(out)), "r"(col0 + 16 * u), "r"(row0),
                     "r"(o.mat)
                   : "memory");
               asm volatile("cp.async.bulk.commit_group;" ::: "memory");
             }
           }
         } else {
-          __half* d = g.dst + static_cast<int64_t>(o.mat) * P * g.dst_plane +
-                      static_cast<int64_t>(row) * g.dst_ld + col0;
+          __half* d = info.buf[st.dst] + static_cast<int64_t>(o.mat) * P * info.plane[which] +
+                      static_cast<int64_t>(row) * info.ld[which] + col0;
 #pragma unroll
           for (int u = 0; u < 4; ++u) {
             if (16 * u >= left) break;
-            put_planes(d + 16 * u, g.dst_plane, acc + 16 * u);
+            put_planes(d + 16 * u, info.plane[which], acc + 16 * u);
           }
         }
         __syncwarp();
       }
+      if (aborted) break;
+      // through with the tile: its planes may be loaded, by whoever sees the count
+      if (P == 1 && lane == 0) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
+      asm volatile("fence.proxy.async;" ::: "memory");
+      __threadfence();
+      __syncwarp();
+      if (lane == 0)
+        asm volatile("red.release.gpu.global.add.s32 [%0], 1;" ::"l"(p.counters + 1 + info.first_mat +
+                                                                    o.mat)
+                     : "memory");
     }
-    if (P == 1 && lane == 0) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
     __syncwarp();
   }
 
@@ -900,7 +1043,7 @@ struct Planes {
 
 struct BatchLayout {
   std::vector<Planes> shapes;
-  size_t part = 0, total = 0;
+  size_t part = 0, counters = 0, total = 0;
   int64_t chunk = 0, ctas = 0;
 };
 
@@ -917,6 +1060,7 @@ BatchLayout layout_of(const Batch& b, int P) {
   for (const Shape& s : b.shapes)
     l.ctas += ceil_div(s.rows * s.cols, l.chunk) * static_cast<int64_t>(s.mats.size());
   l.part = take(l.ctas * static_cast<int64_t>(sizeof(float2)));
+  l.counters = take((1 + b.mats) * static_cast<int64_t>(sizeof(int)));
   for (const Shape& s : b.shapes) {
     Planes p;
     const int64_t m = std::min(s.rows, s.cols), n = static_cast<int64_t>(s.mats.size()) * P * 2;
@@ -1004,6 +1148,7 @@ cudaError_t run_moments(const bergson_muon_tensor* t, const Batch& b, const Batc
   p.n = b.mats;
   p.grad_scale = a.grad_scale;
   p.part = reinterpret_cast<float2*>(ws + l.part);
+  p.counters = reinterpret_cast<int*>(ws + l.counters);
   p.chunk = l.chunk;
   p.begin[0] = 0;
   int k = 0;
@@ -1070,16 +1215,6 @@ cudaError_t run_weights(const bergson_muon_tensor* t, const Batch& b, const Batc
                 : launch_dependent(weights_kernel<N, 1>, grid, block, 0, s, p);
 }
 
-// An operand's boxes: of the rows as they lie, and across.
-struct Side {
-  CUtensorMap rows, across;
-};
-// Of a group: the first product's operands (by X's buffer), the square's, and the last one's, B and X.
-struct Maps {
-  Side gram_a[2], gram_b[2], square_a, square_b, last_s, last_x[2];
-  CUtensorMap x_out[2], a_out, b_out;
-};
-
 // rows: of a box of rows; chunks: of a box across (0: a chunk at any row).
 bool encode_side(Side* s, const void* ptr, int64_t cols, int64_t rows, int64_t planes, int64_t ld,
                  int P, int box_rows, int chunks) {
@@ -1087,56 +1222,52 @@ bool encode_side(Side* s, const void* ptr, int64_t cols, int64_t rows, int64_t p
          encode_tmap_across(&s->across, ptr, cols, rows, planes, ld, P, chunks) == CUDA_SUCCESS;
 }
 
-template <int P, int G>
-cudaError_t run_products(const Batch& b, const BatchLayout& l,
-                         const MuonScalars& a, uint8_t* ws, int* status, int sms, cudaStream_t s) {
-  std::vector<Maps> maps(b.shapes.size());
+template <int P, int G, int S>
+cudaError_t run_products(const Batch& b, const BatchLayout& l, const MuonScalars& a, uint8_t* ws,
+                         int* status, int sms, cudaStream_t s) {
   const int most_clusters = std::max(1, sms / 2);
-  std::vector<int> columns[3];
-  for (int part = 0; part < 3; ++part)
+  std::vector<int> columns[kParts];
+  for (int part = 0; part < kParts; ++part)
     columns[part] = launch_columns(b, part, P, most_clusters);
-  ProdParams<G> p = {};
+  static_assert(sizeof(ProdParams<G, S>) <= 32'000, "a launch's parameters");
+  ProdParams<G, S> p = {};
   p.n = static_cast<int>(b.shapes.size());
+  p.counters = reinterpret_cast<int*>(ws + l.counters);
   p.status = status;
   p.timeout_ns = kWaitTimeoutNs;
+  int first = 0;
+  int64_t tiles[kParts] = {0, 0, 0};             // of a step
   for (int k = 0; k < p.n; ++k) {
     const Shape& sh = b.shapes[k];
     const Planes& pl = l.shapes[k];
     const int64_t m = std::min(sh.rows, sh.cols), n = static_cast<int64_t>(sh.mats.size()) * P;
-    Maps& mp = maps[k];
-    const int tn_g = columns[0][k], tn_s = columns[1][k], tn_x = columns[2][k];
-    const auto chunks = [](int tn) { return tn % 128 == 0 ? tn / 128 : 0; };
+    const bool tall = sh.rows > sh.cols;
+    ShapeInfo& info = p.info[k];
+    ShapeMaps& maps = p.maps[k];
+    info.first_mat = first;
+    first += static_cast<int>(sh.mats.size());
+    info.ld[0] = static_cast<int>(pl.x_ld);
+    info.ld[1] = static_cast<int>(pl.s_ld);
+    info.plane[0] = pl.x_plane;
+    info.plane[1] = pl.s_plane;
+    const size_t at[4] = {pl.x[0], pl.x[1], pl.a, pl.b};
     bool good = true;
-    for (int i = 0; i < 2; ++i) {
-      const auto x = [&](Side* side, int rows, int ch) {
-        good = good && encode_side(side, ws + pl.x[i], sh.cols, sh.rows, n, pl.x_ld, P, rows, ch);
-      };
-      good = good && encode_tmap_out(&mp.x_out[i], ws + pl.x[i], sh.cols, sh.rows, n, pl.x_ld) ==
-                         CUDA_SUCCESS;
-      x(&mp.gram_a[i], kTileM / 2, 2);
-      x(&mp.gram_b[i], tn_g / 2, chunks(tn_g));
-      if (sh.rows > sh.cols) x(&mp.last_x[i], kTileM / 2, 2);
-      else x(&mp.last_x[i], tn_x / 2, chunks(tn_x));
+    for (int i = 0; i < 4; ++i) {
+      info.buf[i] = reinterpret_cast<__half*>(ws + at[i]);
+      good = good && encode_tmap_out(&maps.out[i], ws + at[i], i < 2 ? sh.cols : m,
+                                     i < 2 ? sh.rows : m, n, i < 2 ? pl.x_ld : pl.s_ld) == CUDA_SUCCESS;
     }
-    const auto sym = [&](Side* side, size_t at, int rows, int ch) {
-      good = good && encode_side(side, ws + at, m, m, n, pl.s_ld, P, rows, ch);
-    };
-    sym(&mp.square_a, pl.a, kTileM / 2, 2);
-    sym(&mp.square_b, pl.a, tn_s / 2, chunks(tn_s));
-    if (sh.rows > sh.cols) sym(&mp.last_s, pl.b, tn_x / 2, chunks(tn_x));
-    else sym(&mp.last_s, pl.b, kTileM / 2, 2);
-    good = good && encode_tmap_out(&mp.a_out, ws + pl.a, m, m, n, pl.s_ld) == CUDA_SUCCESS &&
-           encode_tmap_out(&mp.b_out, ws + pl.b, m, m, n, pl.s_ld) == CUDA_SUCCESS;
-    if (!good) return cudaErrorInvalidValue;
-  }
-  const auto kernel = product_kernel<P, G>;
-  static PerDeviceOnce attr;
-  cudaError_t e = smem_attr_once(attr, kernel, ProdCfg<P>::kSmemBytes);
-  if (e != cudaSuccess) return e;
-  const auto run = [&](int part) {
-    int64_t tiles = 0;
-    for (int k = 0; k < p.n; ++k) {
-      ProdGroup& g = p.g[k];
+    for (int part = 0; part < kParts; ++part) {
+      const Dims d = dims_of(sh, part);
+      ProdGroup& g = info.part[part];
+      g.M = static_cast<int>(d.m);
+      g.N = static_cast<int>(d.n);
+      g.K = static_cast<int>(d.k);
+      g.lower = part < 2 ? 1 : 0;
+      g.a_kind = part == 1 ? kSymmetric : part == 0 ? (tall ? kAcross : kRowMajor)
+                                                    : (tall ? kRowMajor : kSymmetric);
+      g.b_kind = part == 1 ? kSymmetric : part == 0 ? (tall ? kAcross : kRowMajor)
+                                                    : (tall ? kSymmetric : kAcross);
       g.tn = columns[part][k];
       g.chunks_b = g.tn % 128 == 0 ? g.tn / 128 : 0;
       const int width = ProdCfg<P>::kSub * g.tn;
@@ -1146,74 +1277,56 @@ cudaError_t run_products(const Batch& b, const BatchLayout& l,
       for (int mt = 0; mt < g.n_mt; ++mt)
         g.per_mat += g.lower ? static_cast<int>(ceil_div(std::min((mt + 1) * kTileM, g.N), width))
                              : g.n_nt;
-      g.begin = static_cast<int>(tiles);
-      tiles += static_cast<int64_t>(g.per_mat) * static_cast<int64_t>(b.shapes[k].mats.size());
-    }
-    p.n_tiles = static_cast<int>(tiles);
-    const int64_t clusters = std::max<int64_t>(1, std::min<int64_t>(most_clusters, tiles));
-    return launch_dependent(kernel, dim3(static_cast<unsigned>(2 * clusters)), dim3(kThreads),
-                            ProdCfg<P>::kSmemBytes, s, p);
-  };
-  for (int it = 0; it < a.iterations; ++it) {
-    const double* c = a.coefficients + 3 * it;
-    const int cur = it & 1;
-    const double ca = c[0], cb = c[1], cc = c[2];
-    const double h = cc != 0.0 ? cb / (2.0 * cc) : 0.0;
-    for (int part = 0; part < 3; ++part) {       // A' = X X^T + h I, B = c A'^2 + .., X' = B X
-      if (part == 1 && cc == 0.0) continue;
-      for (int k = 0; k < p.n; ++k) {
-        const Shape& sh = b.shapes[k];
-        const Planes& pl = l.shapes[k];
-        const bool tall = sh.rows > sh.cols;
-        const Dims d = dims_of(sh, part);
-        ProdGroup& g = p.g[k];
-        g.M = static_cast<int>(d.m);
-        g.N = static_cast<int>(d.n);
-        g.K = static_cast<int>(d.k);
-        g.lower = part < 2 ? 1 : 0;
-        g.dst_ld = static_cast<int>(part == 2 ? pl.x_ld : pl.s_ld);
-        g.dst_plane = part == 2 ? pl.x_plane : pl.s_plane;
-        const auto at = [&](size_t off) { return reinterpret_cast<__half*>(ws + off); };
-        const auto set = [&](double alpha, double gamma, __half* dst) {
-          g.alpha = static_cast<float>(alpha / kPlaneScale);
-          g.gamma = static_cast<float>(gamma * kPlaneScale);
-          g.dst = dst;
+      g.begin = static_cast<int>(tiles[part]);
+      tiles[part] += static_cast<int64_t>(g.per_mat) * static_cast<int64_t>(sh.mats.size());
+      // the operands: X [rows, cols] or the symmetric A', B [m, m]
+      for (int cur = 0; cur < (part == 1 ? 1 : 2); ++cur) {
+        const auto operand = [&](Side* side, bool x, int rows, int chunks) {
+          const size_t from = x ? pl.x[cur] : part == 1 ? pl.a : pl.b;
+          good = good && encode_side(side, ws + from, x ? sh.cols : m, x ? sh.rows : m, n,
+                                     x ? pl.x_ld : pl.s_ld, P, rows, chunks);
         };
-        const Maps& mp = maps[k];
-        const auto sides = [&](const Side& a_side, const Side& b_side) {
-          p.a[k] = a_side.rows;
-          p.ax[k] = a_side.across;
-          p.b[k] = b_side.rows;
-          p.bx[k] = b_side.across;
-        };
-        if (part == 0) {
-          sides(mp.gram_a[cur], mp.gram_b[cur]);
-          p.out[k] = cc != 0.0 ? mp.a_out : mp.b_out;
-          g.a_kind = g.b_kind = tall ? kAcross : kRowMajor;
-          if (cc != 0.0) set(1.0, h, at(pl.a));
-          else set(cb, ca, at(pl.b));
-        } else if (part == 1) {
-          sides(mp.square_a, mp.square_b);
-          p.out[k] = mp.b_out;
-          g.a_kind = g.b_kind = kSymmetric;
-          set(cc, ca - cc * h * h, at(pl.b));
-        } else {
-          p.out[k] = mp.x_out[cur ^ 1];
-          if (tall) sides(mp.last_x[cur], mp.last_s);
-          else sides(mp.last_s, mp.last_x[cur]);
-          g.a_kind = tall ? kRowMajor : kSymmetric;
-          g.b_kind = tall ? kSymmetric : kAcross;
-          set(1.0, 0.0, at(pl.x[cur ^ 1]));
-        }
+        operand(&maps.a[side_of(part, cur)], g.a_kind != kSymmetric, kTileM / 2, 2);
+        operand(&maps.b[side_of(part, cur)], g.b_kind != kSymmetric, g.tn / 2, g.chunks_b);
       }
-      e = run(part);
-      if (e != cudaSuccess) return e;
+    }
+    if (!good) return cudaErrorInvalidValue;
+  }
+  int64_t total = 0;
+  int before[kParts] = {0, 0, 0};
+  for (int it = 0; it < a.iterations; ++it) {
+    const double ca = a.coefficients[3 * it], cb = a.coefficients[3 * it + 1],
+                 cc = a.coefficients[3 * it + 2];
+    const double h = cc != 0.0 ? cb / (2.0 * cc) : 0.0;
+    for (int part = 0; part < kParts; ++part) {
+      if (part == 1 && cc == 0.0) continue;
+      const double alpha = part == 0 ? (cc != 0.0 ? 1.0 : cb) : part == 1 ? cc : 1.0;
+      const double gamma = part == 0 ? (cc != 0.0 ? h : ca) : part == 1 ? ca - cc * h * h : 0.0;
+      Step& st = p.step[p.n_steps++];
+      st.begin = static_cast<int>(total);
+      st.alpha = static_cast<float>(alpha / kPlaneScale);
+      st.gamma = static_cast<float>(gamma * kPlaneScale);
+      st.part = static_cast<uint8_t>(part);
+      st.cur = static_cast<uint8_t>(it & 1);
+      st.dst = static_cast<uint8_t>(part == 2 ? (it & 1) ^ 1 : part == 0 && cc != 0.0 ? 2 : 3);
+      for (int k = 0; k < kParts; ++k) st.before[k] = static_cast<uint8_t>(before[k]);
+      ++before[part];
+      total += tiles[part];
     }
   }
-  return cudaSuccess;
+  if (total > INT32_MAX / (4 * kEpilogueWarps)) return cudaErrorInvalidConfiguration;
+  p.n_tiles = static_cast<int>(total);
+  const int64_t widest = std::max(tiles[0], std::max(tiles[1], tiles[2]));
+  const int64_t clusters = std::max<int64_t>(1, std::min<int64_t>(most_clusters, widest));
+  const auto kernel = products_kernel<P, G, S>;
+  static PerDeviceOnce attr;
+  const cudaError_t e = smem_attr_once(attr, kernel, ProdCfg<P>::kSmemBytes);
+  if (e != cudaSuccess) return e;
+  return launch_dependent(kernel, dim3(static_cast<unsigned>(2 * clusters)), dim3(kThreads),
+                          ProdCfg<P>::kSmemBytes, s, p);
 }
 
-constexpr int kFewGroups = 4, kFewMats = 48;
+constexpr int kFewGroups = 4, kFewMats = 48, kFewSteps = 24, kMaxSteps = 3 * 64;
 
 }  // namespace
 
@@ -1229,16 +1342,17 @@ cudaError_t launch_muon(const bergson_muon_tensor* t, int n, const MuonScalars& 
   uint8_t* w = static_cast<uint8_t*>(ws);
   for (const Batch& b : batches_of(t, n)) {
     const BatchLayout l = layout_of(b, a.products == 3 ? 2 : 1);
-    const bool few = b.mats <= kFewMats && b.shapes.size() <= kFewGroups;
+    const bool few = b.mats <= kFewMats;
     cudaError_t e = few ? run_moments<kFewMats>(t, b, l, a, w, s)
                         : run_moments<kMaxMats>(t, b, l, a, w, s);
     if (e != cudaSuccess) return e;
+    const bool short_run = b.shapes.size() <= kFewGroups && 3 * a.iterations <= kFewSteps;
     if (a.products == 3)
-      e = few ? run_products<2, kFewGroups>(b, l, a, w, status, sms, s)
-              : run_products<2, kMaxGroups>(b, l, a, w, status, sms, s);
+      e = short_run ? run_products<2, kFewGroups, kFewSteps>(b, l, a, w, status, sms, s)
+                    : run_products<2, kMaxGroups, kMaxSteps>(b, l, a, w, status, sms, s);
     else
-      e = few ? run_products<1, kFewGroups>(b, l, a, w, status, sms, s)
-              : run_products<1, kMaxGroups>(b, l, a, w, status, sms, s);
+      e = short_run ? run_products<1, kFewGroups, kFewSteps>(b, l, a, w, status, sms, s)
+                    : run_products<1, kMaxGroups, kMaxSteps>(b, l, a, w, status, sms, s);
     if (e != cudaSuccess) return e;
     e = few ? run_weights<kFewMats>(t, b, l, a, w, s) : run_weights<kMaxMats>(t, b, l, a, w, s);
     if (e != cudaSuccess) return e;
