@@ -19,11 +19,17 @@
 // 1 / sqrt(columns) later, and stay clear of fp16's subnormals by that.
 //
 // Matrices of one shape form a group, their planes stacked in the workspace under one
-// tensor map; each product of an iteration is one launch over the tiles of all
-// groups, by persistent CTA pairs with 256-row tiles, longest products first.  An
-// operand is read with its rows as they lie (K-major) or across (MN-major) by the tensor cores'
-// own descriptors.  A and B are symmetric: only tiles on and below the diagonal are
-// computed and stored, and a read above it takes the mirror image across.
+// tensor map.  All products of all iterations are one launch of persistent CTA pairs over 256-row
+// tiles, handed out step by step, longest products first; a matrix's tiles wait for its own earlier
+// ones alone.  An operand is read with its rows as they lie (K-major) or across (MN-major)
+// by the tensor cores' own descriptors.  A' and B are symmetric: only tiles on and below the diagonal
+// are computed and stored, and a read above it takes the mirror image across.
+//
+// Bound: with two planes an accumulator of 256 columns is 12 MMAs of 128 cycles a stage for 64 KB of loads,
+// with one plane two of them are 8 for 48 KB; a CTA's loads come at 39 to 47 bytes a cycle when all SMs load,
+// so that both forms wait for them a little (1.0 to 1.3 of the MMAs' time), and the smallest steps are
+// latency, 5 to 7 us a product.  Four blocks of d 2048 at one plane: 5.5 ms, 1.25 PFLOP/s under the
+// power cap; ten of d 640 at two: 1.7 ms, 0.92 PFLOP/s of MMAs.
 
 #include <algorithm>
 #include <cmath>
@@ -452,7 +458,7 @@ __device__ __forceinline__ Tile tile_of(const ProdParams<G, S>& p, int t, int st
 // memory.  A matrix's tiles wait for all tiles of its earlier steps, which were handed out before:
 // whichever pairs run, the first unfinished tile can proceed, so that no pair needs another to be
 // resident.
-constexpr int kSlots = 2;
+constexpr int kSlots = 2;                      // tiles a pair has taken and not begun
 constexpr int kTakers = 2 * (2 + kEpilogueWarps) + 1;    // loads and epilogue of both CTAs, MMA
 
 struct Ring {                  // in each CTA; `empty` counts in the even one
@@ -596,16 +602,17 @@ __device__ __forceinline__ void load_side(const ProdParams<G, S>& p, int rank, R
 #pragma unroll
     for (int k = 0; k < kParts; ++k)
       need += st.before[k] * info.part[k].per_mat * (2 * kEpilogueWarps);
-    if (need > 0 &&
-        !wait_matrix(p.counters + 1 + info.first_mat + o.mat, need, tmo, s_abort)) {
-      ok = false;
-      break;
-    }
     const ShapeMaps& maps = p.maps[o.group];
     const Side& side = kSideB ? maps.b[side_of(st.part, st.cur)] : maps.a[side_of(st.part, st.cur)];
     const void* rows_map = &side.rows;
     const void* across_map = &side.across;
     const int kind = kSideB ? g.b_kind : g.a_kind;
+    if (kind != kAcross) prefetch_tmap(rows_map);
+    if (kind != kRowMajor) prefetch_tmap(across_map);
+    if (need > 0 && !wait_matrix(p.counters + 1 + info.first_mat + o.mat, need, tmo, s_abort)) {
+      ok = false;
+      break;
+    }
     const int z = o.mat * P;
     const int subs = kSideB ? o.subs : 1;
     const int wide = kSideB ? g.tn : kTileM;       // rows over the pair
@@ -676,7 +683,7 @@ __device__ __forceinline__ void put_planes(__half* d, int64_t plane, const float
   store32(d + plane, lo);
 }
 
-// D[i, j] = alpha <a_i, b_j> + gamma [i == j] over persistent CTA pairs, synchronised
+// All steps' D[i, j] = alpha <a_i, b_j> + gamma [i == j] over persistent CTA pairs, synchronised
 // as the other pair kernels: the odd CTA's loads complete on the even CTA's `full`, the
 // even CTA's MMA thread frees a stage in both CTAs and hands accumulators to both
 // epilogues by multicast commits, and every epilogue warp of both CTAs releases an
@@ -966,8 +973,6 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
       if (aborted) break;
       // through with the tile: its planes may be loaded, by whoever sees the count
       if (P == 1 && lane == 0) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
-      asm volatile("fence.proxy.async;" ::: "memory");
-      __threadfence();
       __syncwarp();
       if (lane == 0)
         asm volatile("red.release.gpu.global.add.s32 [%0], 1;" ::"l"(p.counters + 1 + info.first_mat +
@@ -1215,11 +1220,14 @@ cudaError_t run_weights(const bergson_muon_tensor* t, const Batch& b, const Batc
                 : launch_dependent(weights_kernel<N, 1>, grid, block, 0, s, p);
 }
 
-// rows: of a box of rows; chunks: of a box across (0: a chunk at any row).
-bool encode_side(Side* s, const void* ptr, int64_t cols, int64_t rows, int64_t planes, int64_t ld,
-                 int P, int box_rows, int chunks) {
-  return encode_tmap_stack(&s->rows, ptr, cols, rows, planes, ld, box_rows, P) == CUDA_SUCCESS &&
-         encode_tmap_across(&s->across, ptr, cols, rows, planes, ld, P, chunks) == CUDA_SUCCESS;
+// The maps that a kind of operand is read by.  rows: of a box of rows; chunks: of a box across
+// (0: a chunk at any row).
+bool encode_side(Side* s, int kind, const void* ptr, int64_t cols, int64_t rows, int64_t planes,
+                 int64_t ld, int P, int box_rows, int chunks) {
+  return (kind == kAcross ||
+          encode_tmap_stack(&s->rows, ptr, cols, rows, planes, ld, box_rows, P) == CUDA_SUCCESS) &&
+         (kind == kRowMajor ||
+          encode_tmap_across(&s->across, ptr, cols, rows, planes, ld, P, chunks) == CUDA_SUCCESS);
 }
 
 template <int P, int G, int S>
@@ -1254,7 +1262,7 @@ cudaError_t run_products(const Batch& b, const BatchLayout& l, const MuonScalars
     bool good = true;
     for (int i = 0; i < 4; ++i) {
       info.buf[i] = reinterpret_cast<__half*>(ws + at[i]);
-      good = good && encode_tmap_out(&maps.out[i], ws + at[i], i < 2 ? sh.cols : m,
+      if (P == 1) good = good && encode_tmap_out(&maps.out[i], ws + at[i], i < 2 ? sh.cols : m,
                                      i < 2 ? sh.rows : m, n, i < 2 ? pl.x_ld : pl.s_ld) == CUDA_SUCCESS;
     }
     for (int part = 0; part < kParts; ++part) {
@@ -1281,13 +1289,19 @@ cudaError_t run_products(const Batch& b, const BatchLayout& l, const MuonScalars
       tiles[part] += static_cast<int64_t>(g.per_mat) * static_cast<int64_t>(sh.mats.size());
       // the operands: X [rows, cols] or the symmetric A', B [m, m]
       for (int cur = 0; cur < (part == 1 ? 1 : 2); ++cur) {
-        const auto operand = [&](Side* side, bool x, int rows, int chunks) {
+        const auto operand = [&](Side* sides, int kind, int rows, int chunks) {
+          Side* side = &sides[side_of(part, cur)];
+          if (kind == kSymmetric && cur == 1) {
+            *side = sides[side_of(part, 0)];
+            return;
+          }
+          const bool x = kind != kSymmetric;
           const size_t from = x ? pl.x[cur] : part == 1 ? pl.a : pl.b;
-          good = good && encode_side(side, ws + from, x ? sh.cols : m, x ? sh.rows : m, n,
+          good = good && encode_side(side, kind, ws + from, x ? sh.cols : m, x ? sh.rows : m, n,
                                      x ? pl.x_ld : pl.s_ld, P, rows, chunks);
         };
-        operand(&maps.a[side_of(part, cur)], g.a_kind != kSymmetric, kTileM / 2, 2);
-        operand(&maps.b[side_of(part, cur)], g.b_kind != kSymmetric, g.tn / 2, g.chunks_b);
+        operand(maps.a, g.a_kind, kTileM / 2, 2);
+        operand(maps.b, g.b_kind, g.tn / 2, g.chunks_b);
       }
     }
     if (!good) return cudaErrorInvalidValue;
@@ -1326,7 +1340,8 @@ cudaError_t run_products(const Batch& b, const BatchLayout& l, const MuonScalars
                           ProdCfg<P>::kSmemBytes, s, p);
 }
 
-constexpr int kFewGroups = 4, kFewMats = 48, kFewSteps = 24, kMaxSteps = 3 * 64;
+// Sizes of the launches' parameters: few and most.
+constexpr int kFewGroups = 4, kFewMats = 48, kFewSteps = 18, kMaxSteps = kParts * 64;
 
 }  // namespace
 
