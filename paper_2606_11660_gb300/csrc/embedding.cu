@@ -7,7 +7,7 @@
 // atomics, so that it has the same bits every time: the rows are put in the order of
 // their tokens, and what shares a token is added up in the order of the rows.
 //
-// Up to kFewRows rows, one launch: the CTA of a token's first row finds the
+// Up to 4096 rows, one launch: the CTA of a token's first row finds the
 // others by comparing tokens, and CTAs of their own write zeros to the rest of the
 // table.  Above, a radix sort of (token, row), 9 bits a pass: counts per tile
 // of rows, then every tile places its rows behind those of the tiles before it.
@@ -71,13 +71,14 @@ __global__ void __launch_bounds__(kLookupThreads) lookup_kernel(
 
 // ------------------------------------------------------------------ backward
 
-constexpr int kFewRows = 2048;                 // up to here one launch does it all
+constexpr int kFewRows = 4096;                 // up to here one launch does it all
 constexpr int kFewThreads = 512;
-constexpr int kFewZeros = 512;                 // rows of the table a CTA of zeros looks after
+constexpr int kFewZeros = 512;                 // rows of the table a CTA of zeros looks after, at most,
+constexpr int64_t kZeroBytes = 64 << 10;       //   and what they hold, about
 constexpr int kRun = 32;                       // sorted rows added up by one CTA
 constexpr int kSumThreads = 128;
 constexpr int kCols = 8;                       // columns a thread
-constexpr int kAhead = 8;                      // rows on their way
+constexpr int kFewAhead = 4;                   // rows on their way
 constexpr int kJoinThreads = 256;               // a warp joins the token that a run ends in
 constexpr int kJoinCols = 128;
 constexpr int kShortParts = 16;                // of so many runs
@@ -97,91 +98,117 @@ struct GradOut {
   float scale;
 };
 
-// E (1, 4 or 8) neighbouring columns of the table's row v: their sum times the scale.
+// E (1, 4 or 8) neighbouring columns of the table's row v, as they are.
 template <int E>
-__device__ __forceinline__ void put_columns(const GradOut& o, int64_t v, int col, int d,
-                                            const float* sum) {
+__device__ __forceinline__ void get_columns(const GradOut& o, int64_t v, int col, int d, float* x) {
   const int64_t at = v * o.ld + col;
-  float x[E];
-  const bool whole = E > 1 && o.vec && col + E <= d;
-  if (!whole) {
+  if (E == 1 || !o.vec || col + E > d) {
 #pragma unroll
-    for (int i = 0; i < E; ++i) {
-      if (col + i >= d) return;
-      float y = sum[i] * o.scale;
-      if (o.add) y += load_any(o.table, o.type, at + i);
-      if (o.type == BERGSON_BF16) static_cast<__nv_bfloat16*>(o.table)[at + i] = __float2bfloat16_rn(y);
-      else if (o.type == BERGSON_F16) static_cast<__half*>(o.table)[at + i] = __float2half_rn(y);
-      else static_cast<float*>(o.table)[at + i] = y;
-    }
+    for (int i = 0; i < E; ++i) x[i] = col + i < d ? load_any(o.table, o.type, at + i) : 0.0f;
     return;
   }
   if constexpr (E > 1) {
 #pragma unroll
-    for (int i = 0; i < E; ++i) x[i] = sum[i] * o.scale;
-    if (o.type == BERGSON_F32) {
-      float4* t = reinterpret_cast<float4*>(static_cast<float*>(o.table) + at);
-#pragma unroll
-      for (int k = 0; k < E / 4; ++k) {
-        float4 y = make_float4(x[4 * k], x[4 * k + 1], x[4 * k + 2], x[4 * k + 3]);
-        if (o.add) {
-          const float4 z = t[k];
-          y.x += z.x; y.y += z.y; y.z += z.z; y.w += z.w;
-        }
-        t[k] = y;
-      }
-      return;
-    }
-    uint2* t = reinterpret_cast<uint2*>(static_cast<uint16_t*>(o.table) + at);
-    uint2 u[E / 4];
-#pragma unroll
     for (int k = 0; k < E / 4; ++k) {
-      uint4 w = make_uint4(0, 0, 0, 0);
-      if (o.add) {
-        const uint2 z = t[k];
-        w.x = z.x;
-        w.y = z.y;
+      if (o.type == BERGSON_F32) {
+        const float4 z = reinterpret_cast<const float4*>(static_cast<const float*>(o.table) + at)[k];
+        x[4 * k] = z.x; x[4 * k + 1] = z.y; x[4 * k + 2] = z.z; x[4 * k + 3] = z.w;
+      } else {
+        const uint2 z = reinterpret_cast<const uint2*>(static_cast<const uint16_t*>(o.table) + at)[k];
+        const uint4 w = make_uint4(z.x, z.y, 0, 0);
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
           const float2 f = o.type == BERGSON_BF16
                                ? unpack2(w, h, static_cast<const __nv_bfloat16*>(nullptr))
                                : unpack2(w, h, static_cast<const __half*>(nullptr));
-          x[4 * k + 2 * h] += f.x;
-          x[4 * k + 2 * h + 1] += f.y;
+          x[4 * k + 2 * h] = f.x;
+          x[4 * k + 2 * h + 1] = f.y;
         }
       }
-#pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        const float2 f = make_float2(x[4 * k + 2 * h], x[4 * k + 2 * h + 1]);
-        if (o.type == BERGSON_BF16) pack2(w, h, f, static_cast<const __nv_bfloat16*>(nullptr));
-        else pack2(w, h, f, static_cast<const __half*>(nullptr));
-      }
-      u[k] = make_uint2(w.x, w.y);
     }
-    if constexpr (E == 8)
-      *reinterpret_cast<uint4*>(t) = make_uint4(u[0].x, u[0].y, u[1].x, u[1].y);
-    else
-      *t = u[0];
   }
+}
+// Sets them to x.
+template <int E>
+__device__ __forceinline__ void set_columns(const GradOut& o, int64_t v, int col, int d,
+                                            const float* x) {
+  const int64_t at = v * o.ld + col;
+  if (E == 1 || !o.vec || col + E > d) {
+#pragma unroll
+    for (int i = 0; i < E; ++i) {
+      if (col + i >= d) return;
+      if (o.type == BERGSON_BF16)
+        static_cast<__nv_bfloat16*>(o.table)[at + i] = __float2bfloat16_rn(x[i]);
+      else if (o.type == BERGSON_F16) static_cast<__half*>(o.table)[at + i] = __float2half_rn(x[i]);
+      else static_cast<float*>(o.table)[at + i] = x[i];
+    }
+    return;
+  }
+  if constexpr (E > 1) {
+    if (o.type == BERGSON_F32) {
+      float4* t = reinterpret_cast<float4*>(static_cast<float*>(o.table) + at);
+#pragma unroll
+      for (int k = 0; k < E / 4; ++k)
+        t[k] = make_float4(x[4 * k], x[4 * k + 1], x[4 * k + 2], x[4 * k + 3]);
+      return;
+    }
+    uint4 w;
+#pragma unroll
+    for (int h = 0; h < E / 2; ++h) {
+      const float2 f = make_float2(x[2 * h], x[2 * h + 1]);
+      if (o.type == BERGSON_BF16) pack2(w, h, f, static_cast<const __nv_bfloat16*>(nullptr));
+      else pack2(w, h, f, static_cast<const __half*>(nullptr));
+    }
+    uint16_t* t = static_cast<uint16_t*>(o.table) + at;
+    if constexpr (E == 8) *reinterpret_cast<uint4*>(t) = w;
+    else *reinterpret_cast<uint2*>(t) = make_uint2(w.x, w.y);
+  }
+}
+// Their sum times the scale, added to what is there with o.add.
+template <int E>
+__device__ __forceinline__ void put_columns(const GradOut& o, int64_t v, int col, int d,
+                                            const float* sum) {
+  float x[E];
+#pragma unroll
+  for (int i = 0; i < E; ++i) x[i] = 0.0f;
+  if (o.add) get_columns<E>(o, v, col, d, x);
+#pragma unroll
+  for (int i = 0; i < E; ++i) x[i] = fmaf(sum[i], o.scale, x[i]);
+  set_columns<E>(o, v, col, d, x);
 }
 
 // A thread's columns of a slab of the table's row v.
 template <typename R>
-__device__ __forceinline__ void put_row(const GradOut& o, int64_t v, int c0, int d, int t, int G,
-                                        const float (&sum)[kCols]) {
+__device__ __forceinline__ void get_row(const GradOut& o, int64_t v, int c0, int d, int t, int G,
+                                        float (&x)[kCols]) {
 #pragma unroll
   for (int k = 0; k < R::kPer; ++k)
-    if (c0 + R::col(t, G, k) < d) put_columns<R::E>(o, v, c0 + R::col(t, G, k), d, sum + R::E * k);
+    if (c0 + R::col(t, G, k) < d) get_columns<R::E>(o, v, c0 + R::col(t, G, k), d, x + R::E * k);
+}
+// Sets them to the sum times the scale on top of `old`.
+template <typename R>
+__device__ __forceinline__ void put_row(const GradOut& o, int64_t v, int c0, int d, int t, int G,
+                                        const float (&sum)[kCols], const float (&old)[kCols]) {
+  float x[kCols];
+#pragma unroll
+  for (int i = 0; i < kCols; ++i) x[i] = fmaf(sum[i], o.scale, old[i]);
+#pragma unroll
+  for (int k = 0; k < R::kPer; ++k)
+    if (c0 + R::col(t, G, k) < d) set_columns<R::E>(o, v, c0 + R::col(t, G, k), d, x + R::E * k);
 }
 
-// Zeros in the table's row v, by `n` threads of which this is the t-th.
+// Zeros in the table's row v, by `n` threads of which this is the t-th: 16 bytes at a time between
+// the row's first and last 16-byte boundaries.
 __device__ __forceinline__ void zero_row(const GradOut& o, int64_t v, int d, int t, int n) {
   const int64_t size = o.type == BERGSON_F32 ? 4 : 2;
   uint8_t* row = static_cast<uint8_t*>(o.table) + v * o.ld * size;
   const int64_t bytes = d * size;
-  const int64_t vecs = o.vec ? bytes / 16 : 0;
-  for (int64_t i = t; i < vecs; i += n) reinterpret_cast<uint4*>(row)[i] = make_uint4(0, 0, 0, 0);
-  for (int64_t i = 8 * vecs + t; i < bytes / 2; i += n) reinterpret_cast<uint16_t*>(row)[i] = 0;
+  const int64_t head = min(bytes, static_cast<int64_t>(-reinterpret_cast<uintptr_t>(row) & 15));
+  const int64_t vecs = (bytes - head) / 16, tail = head + 16 * vecs;
+  uint4* whole = reinterpret_cast<uint4*>(row + head);
+  for (int64_t i = t; i < vecs; i += n) whole[i] = make_uint4(0, 0, 0, 0);
+  if (2 * t < head) reinterpret_cast<uint16_t*>(row)[t] = 0;
+  if (2 * t < bytes - tail) reinterpret_cast<uint16_t*>(row + tail)[t] = 0;
 }
 
 struct FewParams {
@@ -190,12 +217,13 @@ struct FewParams {
   GradOut out;
   int64_t V, ld_dy;
   int rows, d, slabs, group;   // threads of a row's slab
+  int zeros;                   // rows of the table a CTA of zeros looks after
   int* status;
 };
 
 // CTA r * slabs + k: the token whose first row is r, slab k.  The CTAs behind: zeros.
 template <typename T, bool kVec>
-__global__ void __launch_bounds__(kFewThreads) few_rows_kernel(
+__global__ void __launch_bounds__(kFewThreads, 3) few_rows_kernel(
     const __grid_constant__ FewParams p) {
   using R = RowPart<T, kVec, kCols>;
   __shared__ uint16_t list[kFewRows];
@@ -206,15 +234,20 @@ __global__ void __launch_bounds__(kFewThreads) few_rows_kernel(
   const int n_sum = p.rows * p.slabs;
   if (static_cast<int>(blockIdx.x) >= n_sum) {
     uint8_t* touched = reinterpret_cast<uint8_t*>(list);
-    for (int i = tid; i < kFewZeros; i += kFewThreads) touched[i] = 0;
+    for (int i = tid; i < p.zeros; i += kFewThreads) touched[i] = 0;
     __syncthreads();
-    const int64_t v0 = static_cast<int64_t>(blockIdx.x - n_sum) * kFewZeros;
+    const int64_t v0 = static_cast<int64_t>(blockIdx.x - n_sum) * p.zeros;
     for (int j = tid; j < p.rows; j += kFewThreads) {
-      const int64_t at = p.ids[j] - v0;
-      if (at >= 0 && at < kFewZeros) touched[at] = 1;
+      const int64_t id = p.ids[j];
+      if (id >= v0 && id < v0 + p.zeros) touched[id - v0] = 1;
     }
     __syncthreads();
-    for (int i = warp; i < kFewZeros && v0 + i < p.V; i += kFewThreads / 32)
+    if (p.zeros < kFewThreads / 32) {              // few wide rows: all threads for each
+      for (int i = 0; i < p.zeros && v0 + i < p.V; ++i)
+        if (!touched[i]) zero_row(p.out, v0 + i, p.d, tid, kFewThreads);
+      return;
+    }
+    for (int i = warp; i < p.zeros && v0 + i < p.V; i += kFewThreads / 32)
       if (!touched[i]) zero_row(p.out, v0 + i, p.d, lane, 32);
     return;
   }
@@ -225,9 +258,8 @@ __global__ void __launch_bounds__(kFewThreads) few_rows_kernel(
     if (tid == 0 && slab == 0) raise_device_error(p.status, nullptr, BERGSON_EINVAL);
     return;
   }
-  int before = 0;
-  for (int j = tid; j < r; j += kFewThreads) before |= p.ids[j] == id ? 1 : 0;
-  if (__syncthreads_or(before)) return;
+  for (int j0 = 0; j0 < r; j0 += kFewThreads)      // frequent tokens end early
+    if (__syncthreads_or(j0 + tid < r && p.ids[j0 + tid] == id)) return;
   int n = 0;
   for (int j0 = r; j0 < p.rows; j0 += kFewThreads) {
     const bool mine = j0 + tid < p.rows && p.ids[j0 + tid] == id;
@@ -245,21 +277,25 @@ __global__ void __launch_bounds__(kFewThreads) few_rows_kernel(
   const int groups = kFewThreads / p.group, g = tid / p.group, t = tid % p.group;
   const int per = (n + groups - 1) / groups;
   const int c0 = slab * p.group * kCols;
+  float old[kCols];
+#pragma unroll
+  for (int i = 0; i < kCols; ++i) old[i] = 0.0f;
+  if (p.out.add && g == 0) get_row<R>(p.out, id, c0, p.d, t, p.group, old);
   float sum[kCols];
 #pragma unroll
   for (int i = 0; i < kCols; ++i) sum[i] = 0.0f;
   if (g < groups) {
     const int end = min(n, (g + 1) * per);
-    for (int k0 = g * per; k0 < end; k0 += kAhead) {
-      R row[kAhead];
+    for (int k0 = g * per; k0 < end; k0 += kFewAhead) {
+      R row[kFewAhead];
 #pragma unroll
-      for (int k = 0; k < kAhead; ++k) {
+      for (int k = 0; k < kFewAhead; ++k) {
         const int64_t at = k0 + k < end ? list[k0 + k] : 0;
         row[k].load(static_cast<const T*>(p.dy) + at * p.ld_dy + c0, k0 + k < end ? p.d - c0 : 0, t,
                     p.group);
       }
 #pragma unroll
-      for (int k = 0; k < kAhead; ++k) {
+      for (int k = 0; k < kFewAhead; ++k) {
         if (k0 + k >= end) break;
         float x[kCols];
         row[k].floats(x);
@@ -279,7 +315,7 @@ __global__ void __launch_bounds__(kFewThreads) few_rows_kernel(
       }
     }
   }
-  if (g == 0) put_row<R>(p.out, id, c0, p.d, t, p.group, sum);
+  if (g == 0) put_row<R>(p.out, id, c0, p.d, t, p.group, sum, old);
 }
 
 // ---- the sort.  Keys are tokens; rows that take no part have V, behind all others.
@@ -435,8 +471,10 @@ struct SumParams {
   int d, slabs;
 };
 
-template <typename T, bool kVec>
+// kAdd: the table's rows that are done here come with the rows that are added to them.
+template <typename T, bool kVec, bool kAdd>
 __global__ void __launch_bounds__(kSumThreads) sum_kernel(const __grid_constant__ SumParams p) {
+  constexpr int kAhead = kAdd ? 4 : 8;           // rows on their way
   using R = RowPart<T, kVec, kCols>;
   __shared__ uint32_t keys[kRun + 2];            // one before, one behind
   __shared__ int rows[kRun];
@@ -464,10 +502,18 @@ __global__ void __launch_bounds__(kSumThreads) sum_kernel(const __grid_constant_
   for (int j0 = 0; j0 < kRun; j0 += kAhead) {
     if (keys[j0 + 1] == none) break;
     R row[kAhead];
+    float old[kAdd ? kAhead : 1][kCols];
 #pragma unroll
-    for (int k = 0; k < kAhead; ++k)
-      row[k].load(static_cast<const T*>(p.dy) + rows[j0 + k] * p.ld_dy + c0,
-                  keys[j0 + k + 1] != none ? p.d - c0 : 0, tid, G);
+    for (int k = 0; k < kAhead; ++k) {
+      const uint32_t v = keys[j0 + k + 1];
+      row[k].load(static_cast<const T*>(p.dy) + rows[j0 + k] * p.ld_dy + c0, v != none ? p.d - c0 : 0,
+                  tid, G);
+      if constexpr (kAdd) {
+        // a token that ends here and did not begin before the run
+        if (v != none && keys[j0 + k + 2] != v && v != keys[0])
+          get_row<R>(p.out, v, c0, p.d, tid, G, old[k]);
+      }
+    }
 #pragma unroll
     for (int k = 0; k < kAhead; ++k) {
       const int j = j0 + k;
@@ -487,7 +533,11 @@ __global__ void __launch_bounds__(kSumThreads) sum_kernel(const __grid_constant_
           if (c < p.d) part[c] = sum[i];
         }
       } else {
-        put_row<R>(p.out, v, c0, p.d, tid, G, sum);
+        float zero[kCols];
+#pragma unroll
+        for (int i = 0; i < kCols; ++i) zero[i] = 0.0f;
+        if constexpr (kAdd) put_row<R>(p.out, v, c0, p.d, tid, G, sum, old[k]);
+        else put_row<R>(p.out, v, c0, p.d, tid, G, sum, zero);
       }
       open = false;
 #pragma unroll
@@ -635,7 +685,9 @@ cudaError_t run_few(const bergson_embedding_grad_args& a, const GradOut& out, in
   p.group = slab_threads(a.d);
   p.slabs = static_cast<int>(ceil_div(a.d, p.group * kCols));
   p.status = status;
-  const int64_t grid = a.rows * p.slabs + (a.add ? 0 : ceil_div(a.V, kFewZeros));
+  const int64_t row_bytes = a.d * (a.t_dtype == BERGSON_F32 ? 4 : 2);
+  p.zeros = static_cast<int>(std::max<int64_t>(1, std::min<int64_t>(kFewZeros, kZeroBytes / row_bytes)));
+  const int64_t grid = a.rows * p.slabs + (a.add ? 0 : ceil_div(a.V, p.zeros));
   return launch_dependent(few_rows_kernel<T, kVec>, dim3(static_cast<unsigned>(grid)),
                           dim3(kFewThreads), 0, s, p);
 }
@@ -647,8 +699,9 @@ cudaError_t run_sums(const bergson_embedding_grad_args& a, SumParams p, cudaStre
   p.n_sum = p.runs * p.slabs;
   const int64_t zeros =
       a.add ? 0 : std::min<int64_t>(ceil_div(a.V, threads / 32), 4 * kPlanCTAs);
-  return launch_dependent(sum_kernel<T, kVec>, dim3(static_cast<unsigned>(p.n_sum + zeros)),
-                          dim3(threads), 0, s, p);
+  const auto kernel = a.add ? sum_kernel<T, kVec, true> : sum_kernel<T, kVec, false>;
+  return launch_dependent(kernel, dim3(static_cast<unsigned>(p.n_sum + zeros)), dim3(threads), 0, s,
+                          p);
 }
 
 cudaError_t run_sorted(const bergson_embedding_grad_args& a, const GradOut& out, bool vec,

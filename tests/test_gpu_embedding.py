@@ -107,12 +107,12 @@ def test_lookup(R, V, d, dtype, scale, pad, offset):
                                       (torch.float32, torch.bfloat16), (torch.float16, torch.float32)])
 @pytest.mark.parametrize("add", [False, True])
 @pytest.mark.parametrize("R,V,d", [(1, 1, 1), (1, 700, 40), (97, 600, 24), (776, 1500, 768), (300, 96, 1100),
-                                   (2048, 500, 65), (2049, 500, 65), (5000, 3000, 96), (4100, 96, 1032)])
+                                   (4096, 500, 65), (4097, 500, 65), (5000, 3000, 96), (4100, 96, 1032)])
 def test_gradient(R, V, d, dtype, tt, add):
     check_gradient(tokens(R, V, seed=R), V, d, dtype, tt, add, scale=1.0 if d % 2 else 3.3, poison=True)
 
 
-@pytest.mark.parametrize("R", [400, 3000])
+@pytest.mark.parametrize("R", [400, 5000])
 @pytest.mark.parametrize("pad,offset", [(3, 0), (8, 8), (0, 1)])
 @pytest.mark.parametrize("d", [40, 1027])
 @pytest.mark.parametrize("tt", DTYPES)
@@ -121,7 +121,7 @@ def test_rows_apart(R, d, pad, offset, tt):
         check_gradient(tokens(R, 200), 200, d, torch.bfloat16, tt, add, 0.5, pad, offset)
 
 
-@pytest.mark.parametrize("R", [64, 2048, 2100, 6000, 9000])
+@pytest.mark.parametrize("R", [64, 2048, 4100, 6000, 9000])
 @pytest.mark.parametrize("kind", ["one", "two", "apart", "none", "last", "falling"])
 def test_orders_of_tokens(R, kind):
     """One token for all, tokens that come once, none at all, runs that end at their limits."""
@@ -134,8 +134,8 @@ def test_orders_of_tokens(R, kind):
         check_gradient(ids, V, 72, torch.bfloat16, torch.float32, add)
 
 
-@pytest.mark.parametrize("R,V", [(3000, 511), (3000, 512), (3000, 513), (3000, 262_143), (3000, 262_144),
-                                 (300_000, 3000)])
+@pytest.mark.parametrize("R,V", [(5000, 511), (5000, 512), (5000, 513), (5000, 262_143), (5000, 262_144),
+                                 (300_000, 5000)])
 def test_sort_passes(R, V):
     """The digits' borders, and tiles of several steps."""
     check_gradient(tokens(R, V, skewed=False), V, 8, torch.float32, torch.float32, False)
@@ -143,7 +143,7 @@ def test_sort_passes(R, V):
 
 def test_wide_vocabulary():
     """Three passes of the sort; a table of 2^27 rows and one column."""
-    V, R = 1 << 27, 4000
+    V, R = 1 << 27, 5000
     ids = torch.randint(0, V, (R,), device=DEV)
     ids[:3] = torch.tensor([0, V - 1, V - 1], device=DEV)
     dy = torch.randn((R, 1), device=DEV)
@@ -162,7 +162,7 @@ def test_ids_out_of_range():
     bg.bergson_embedding(table, ids, 1.0, out)
     assert bg.bergson_sync_status() == bg.BERGSON_EINVAL
     assert bool(out[1].isnan().all()) and not bool(out[2].any()) and torch.equal(out[3], table[9])
-    for R in (4, 3000):
+    for R in (4, 5000):
         many = ids.repeat(R // 4)
         dy = torch.ones((len(many), 64), device=DEV)
         ws = bg.workspace_tensor(bg.bergson_embedding_backward_workspace(len(many), 10, 64), DEV)
@@ -212,6 +212,6 @@ def test_refused_tensors():
     with pytest.raises(TypeError):
         bg.bergson_embedding_backward(t[:4], ids, 1.0, t.long(), False, ws)
     with pytest.raises(bg.BergsonError) as e:
-        bg.bergson_embedding_backward(torch.zeros((4000, 64), device=DEV), ids.repeat(1000), 1.0, t,
+        bg.bergson_embedding_backward(torch.zeros((5000, 64), device=DEV), ids.repeat(1250), 1.0, t,
                                       False, ws)
     assert e.value.status == bg.BERGSON_EWORKSPACE

@@ -92,7 +92,7 @@ class Model:
         return dict(dE=E.grad, dW=W.grad, dw1=w1.grad, db1=b1.grad, dw2=w2.grad)
 
 
-@pytest.mark.parametrize("R,V,d", [(37, 61, 48), (300, 500, 264), (2500, 1000, 520)])
+@pytest.mark.parametrize("R,V,d", [(37, 61, 48), (300, 500, 264), (4500, 1000, 520)])
 def test_gradients_of_a_model(R, V, d):
     m = Model(R, V, d)
     m.gradients()
@@ -111,7 +111,7 @@ def test_steps_run():
     assert bg.bergson_sync_status() == bg.BERGSON_OK and all(x == x for x in losses)
 
 
-@pytest.mark.parametrize("R,V,d", [(37, 61, 48), (2500, 1000, 264)])
+@pytest.mark.parametrize("R,V,d", [(37, 61, 48), (4500, 1000, 264)])
 def test_graph_of_a_step(R, V, d):
     one, two = Model(R, V, d), Model(R, V, d)
     one.step()

@@ -157,7 +157,7 @@ def test_embedding_calls_that_pass():
     assert bg.lib().bergson_embedding(None, None) == bg.BERGSON_EINVAL
     assert bg.lib().bergson_embedding_backward(None, FAKE, 1 << 20, None) == bg.BERGSON_EINVAL
     assert bg.lib().bergson_embedding_backward_workspace(4, 4, 4, None) == bg.BERGSON_EINVAL
-    for sizes in ((0, 1, 1), (2048, 50_000, 64), (2049, 50_000, 64), (1 << 20, 1 << 18, 100)):
+    for sizes in ((0, 1, 1), (4096, 50_000, 64), (4097, 50_000, 64), (1 << 20, 1 << 18, 100)):
         need = bg.bergson_embedding_backward_workspace(*sizes)
         assert need > 0 and need % 256 == 0
 
