@@ -373,7 +373,19 @@ __global__ void __launch_bounds__(kSortThreads) sort_place_kernel(
   __shared__ int part[2][2][kBins];
   __shared__ int scan[kBins / 32];
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const int64_t begin = blockIdx.x * p.tile, end = min(begin + p.tile, p.rows);
   griddep_wait();
+  uint32_t key[kRounds];
+  int row[kRounds];
+  const auto fetch = [&](int64_t i0) {
+#pragma unroll
+    for (int k = 0; k < kRounds; ++k) {
+      const int64_t i = i0 + (warp * kRounds + k) * 32 + lane;
+      key[k] = i < end ? sort_key(p, i) : 0;
+      row[k] = p.row_in != nullptr && i < end ? p.row_in[i] : static_cast<int>(i);
+    }
+  };
+  fetch(begin);
   {
     // what stands before this tile and in all: two halves of the tiles a digit
     const int digit = tid & (kBins - 1), half = tid / kBins;
@@ -405,17 +417,14 @@ __global__ void __launch_bounds__(kSortThreads) sort_place_kernel(
       base[tid] = incl - total + before;
     }
   }
-  const int64_t begin = blockIdx.x * p.tile, end = min(begin + p.tile, p.rows);
   for (int64_t i0 = begin; i0 < end; i0 += kSortItems) {
     for (int i = tid; i < kWarps * kBins / 2; i += kSortThreads)
       reinterpret_cast<uint32_t*>(hist)[i] = 0;
     __syncthreads();
-    uint32_t key[kRounds];
     unsigned same[kRounds];
 #pragma unroll
     for (int k = 0; k < kRounds; ++k) {
       const int64_t i = i0 + (warp * kRounds + k) * 32 + lane;
-      key[k] = i < end ? sort_key(p, i) : 0;
       // an item past the end has a digit of its own
       const uint32_t digit = i < end ? (key[k] >> p.shift) & (kBins - 1) : kBins;
       same[k] = __match_any_sync(0xffffffffu, digit);
@@ -443,7 +452,7 @@ __global__ void __launch_bounds__(kSortThreads) sort_place_kernel(
       if (i < end) {
         if (lane == __ffs(same[k]) - 1) hist[warp][digit] += __popc(same[k]);
         p.key_out[at] = key[k];
-        p.row_out[at] = p.row_in != nullptr ? p.row_in[i] : static_cast<int>(i);
+        p.row_out[at] = row[k];
         if (p.next_table != nullptr)
           atomicAdd(&p.next_table[at / p.tile * kBins + ((key[k] >> p.next_shift) & (kBins - 1))], 1);
         else if (p.touched != nullptr && key[k] < p.V)
@@ -453,6 +462,7 @@ __global__ void __launch_bounds__(kSortThreads) sort_place_kernel(
     }
     __syncthreads();
     if (tid < kBins) base[tid] += sum;
+    if (i0 + kSortItems < end) fetch(i0 + kSortItems);
   }
 }
 
@@ -591,11 +601,22 @@ __global__ void __launch_bounds__(kJoinThreads) join_kernel(const __grid_constan
     const uint32_t next = p.key[last + 1];
     const uint32_t before = run > 0 ? p.key[run * kRun - 1] : none;
     if (v != none && next == v && before != v) {
-      for (n = 2;; n += 32) {
-        const int64_t at = (run + n + lane) * kRun;        // does run + n + lane hold some too?
-        const unsigned votes = __ballot_sync(0xffffffffu, at < p.rows && p.key[at] == v);
-        if (votes != 0xffffffffu) {
-          n += __ffs(~votes) - 1;
+      // does run + n hold some too?  128 runs a step
+      for (n = 2;; n += 128) {
+        uint32_t first[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          const int64_t at = (run + n + 32 * k + lane) * kRun;
+          first[k] = at < p.rows ? p.key[at] : none;
+        }
+        int more = 0;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          const unsigned votes = __ballot_sync(0xffffffffu, first[k] == v);
+          if (more == 32 * k) more += votes == 0xffffffffu ? 32 : __ffs(~votes) - 1;
+        }
+        if (more < 128) {
+          n += more;
           break;
         }
       }
