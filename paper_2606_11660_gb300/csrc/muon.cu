@@ -29,7 +29,8 @@
 // with one plane two of them are 8 for 48 KB; a CTA's loads come at 39 to 47 bytes a cycle when all SMs load,
 // so that both forms wait for them a little (1.0 to 1.3 of the MMAs' time), and the smallest steps are
 // latency, 5 to 7 us a product.  Four blocks of d 2048 at one plane: 5.5 ms, 1.25 PFLOP/s under the
-// power cap; ten of d 640 at two: 1.7 ms, 0.92 PFLOP/s of MMAs.
+// power cap; ten of d 640 at two: 1.8 ms, 0.87 PFLOP/s of MMAs (six of 2048 rows: 84% of the tensor
+// pipe's cycles, 69% at one plane).
 
 #include <algorithm>
 #include <cmath>
@@ -825,7 +826,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
                     umma_pair_low(d, at + kk * step_a, bt + kk * step_b, idesc,
                                   !first || q != 0 || kk != 0);
                 }
-                // a commit stands with its MMAs, in the branch of the lane that issued them
+                // a commit stands with its MMAs, in the branch of the lane that issued them: in a branch of
+                // its own behind the warp's barrier it did not arrive
                 if (ends && kc == kb + len - 1) umma_commit_pair(smem_u32(&tfull[cab]), 0x3);
                 if (h == subs - 1) umma_commit_pair(smem_u32(&empty[st]), 0x3);
               }

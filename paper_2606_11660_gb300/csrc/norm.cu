@@ -6,10 +6,12 @@
 //
 // (mu = 0 and no mean of h without a mean).  Both are bound by their bytes: a
 // row is read once, stays in the registers of the 4 .. 32 lanes (up to 512 columns)
-// or the CTA that have it, 8 or 16 columns a thread, and the next row's loads are on their way while this
+// or the CTA that have it, 8 or 16 columns a thread, and the next rows are on their way while this
 // one is reduced.  A thread keeps its columns from row to row, so that weights are
 // loaded once a CTA and the backward pass sums dw and db in registers; one row
 // of both a CTA goes to the workspace, and a second kernel adds these up in order.
+// 65,536 x 2048 bf16: 95 us forward (5.7 TB/s) and 142 backward (138 and 4; 5.8 TB/s); the forward pass
+// fills 68% of the issue slots, and did so at 77% in 127 us before its arithmetic went in pairs.
 
 #include <algorithm>
 #include <atomic>
