@@ -957,8 +957,8 @@ BERGSON_API int bergson_factor_moments(const bergson_moment_matrix* mats, int n_
  *   y         [rows, ld_y] of `dtype`; may be x itself with ld_y == ld_x.
  *   mean, rstd  fp32 [rows], what the backward pass reads, each or NULL; mean is not
  *             written without a mean.
- * Sums are fp32, about the row's mean.  A row that holds NaN or an infinity is NaN; the
- * others keep their values.  rows in [0, 2^31), d <= 2^24.
+ * Sums and squares are fp32, about the row's mean (values above some 1e18 overflow them).  A row
+ * that holds NaN or an infinity is NaN; the others keep their values.  rows in [0, 2^31), d <= 2^24.
  * Errors: EINVAL, EALIGN, EUNSUPPORTED, ECUDA.
  */
 typedef struct bergson_norm_args {
@@ -1018,7 +1018,7 @@ BERGSON_API int bergson_norm_backward(const bergson_norm_grad_args* args, void* 
  *             a row of NaN and is recorded as BERGSON_EINVAL in the device status word.
  *   scale     finite, e.g. sqrt(d).
  *   out       [rows, ld_o] of `dtype`; shares no memory with table.
- * rows, V in [0, 2^31), d <= 2^24.
+ * rows, V in [0, 2^31), d <= 2^20.
  * Errors: EINVAL, EALIGN, EUNSUPPORTED, ECUDA.
  */
 typedef struct bergson_embedding_args {
@@ -1048,7 +1048,7 @@ BERGSON_API int bergson_embedding(const bergson_embedding_args* args, void* stre
  *   workspace 256-byte aligned, contents on entry ignored.
  * Sums are fp32, without atomics, in an order that follows from the ids and sizes alone; with
  * add != 0 the sum is rounded to t_dtype once, after the addition.
- * rows, V in [0, 2^31), d <= 2^24.
+ * rows, V in [0, 2^31), d <= 2^20.
  * Errors: EINVAL, EALIGN, EUNSUPPORTED, EWORKSPACE, ECUDA.
  */
 typedef struct bergson_embedding_grad_args {
@@ -1107,7 +1107,7 @@ typedef struct bergson_muon_tensor {
  *             together.
  *   coefficients  HOST array [n_iterations, 3], n_iterations in [1, 64].  From |X|_F = 1 on,
  *             |X|, |a I + b A + c A^2| and, where c is not 0, |A + b / 2c| and b^2 / 4c have to stay
- *             within 48 (else EUNSUPPORTED; judged by the polynomials alone).
+ *             within 48 (else EUNSUPPORTED; by the polynomials alone).
  *   products  3: the products' operands hold 22 bits (X is off by some 1e-6 |X| an iteration).
  *             1: they hold fp16's 11 (some 1e-3), at a third of the work: for weights without a
  *             master copy, whose own rounding is larger.

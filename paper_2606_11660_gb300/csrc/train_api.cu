@@ -122,7 +122,7 @@ int check_embedding(int64_t rows, int64_t V, int64_t d, double scale, int reserv
   if (rows < 0 || rows > INT32_MAX) return fail(BERGSON_EINVAL, "rows must be in [0, 2^31)");
   if (V < 1 || V > INT32_MAX) return fail(BERGSON_EINVAL, "V must be in [1, 2^31)");
   if (d < 1) return fail(BERGSON_EINVAL, "d must be >= 1");
-  if (d > (1ll << 24)) return fail(BERGSON_EUNSUPPORTED, "d must be <= 2^24");
+  if (d > (1ll << 20)) return fail(BERGSON_EUNSUPPORTED, "d must be <= 2^20");
   if (rows * ((d + 255) / 256) > INT32_MAX) return fail(BERGSON_EUNSUPPORTED, "rows*d too large");
   return BERGSON_OK;
 }
