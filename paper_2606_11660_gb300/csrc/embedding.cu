@@ -46,7 +46,7 @@ template <typename T, bool kVec>
 __global__ void __launch_bounds__(kLookupThreads) lookup_kernel(
     const __grid_constant__ LookupParams p) {
   constexpr int C = kVec ? 4 * Vec16<T>::kElems : 8;
-  using R = RowPart<T, kVec, C>;
+  using R = RowPart<T, kVec ? 16 : 0, C>;
   const int lane = threadIdx.x & 31;
   const int64_t unit = static_cast<int64_t>(blockIdx.x) * (kLookupThreads / 32) + (threadIdx.x >> 5);
   const int64_t r = unit / p.slabs;
@@ -227,7 +227,7 @@ struct FewParams {
 template <typename T, bool kVec>
 __global__ void __launch_bounds__(kFewThreads, 3) few_rows_kernel(
     const __grid_constant__ FewParams p) {
-  using R = RowPart<T, kVec, kCols>;
+  using R = RowPart<T, kVec ? 16 : 0, kCols>;
   __shared__ uint16_t list[kFewRows];
   __shared__ int counts[kFewThreads / 32];
   __shared__ float joined[kFewThreads * kCols];
@@ -487,7 +487,7 @@ struct SumParams {
 template <typename T, bool kVec, bool kAdd>
 __global__ void __launch_bounds__(kSumThreads) sum_kernel(const __grid_constant__ SumParams p) {
   constexpr int kAhead = kAdd ? 4 : 8;           // rows on their way
-  using R = RowPart<T, kVec, kCols>;
+  using R = RowPart<T, kVec ? 16 : 0, kCols>;
   __shared__ uint32_t keys[kRun + 2];            // one before, one behind
   __shared__ int rows[kRun];
   const int tid = threadIdx.x, G = blockDim.x;

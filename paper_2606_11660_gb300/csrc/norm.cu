@@ -81,25 +81,26 @@ __device__ __forceinline__ void clear_sums(float* red, int n) {
 // Rows on their way to a thread.  In vectors: by asynchronous copies to places of its own in
 // shared memory, kSlots rows ahead, so that no thread waits for another and no register is
 // held (a row at a time in registers: too few bytes in flight, 65,536 x 2048 at 4.1 TB/s with 6 CTAs an SM).  A
-// vector past the end copies what there is and zeros.  Else: one row ahead, in registers.
-template <typename T, bool kVec, int C, int kSlots>
+// vector past the end copies what there is and zeros.  By elements: one row ahead, in registers.
+template <typename T, int kB, int C, int kSlots>
 struct Feed {
-  using R = RowPart<T, kVec, C>;
-  static constexpr int kBytes = kVec ? R::kPer * 16 : 0;     // of a row, a thread
+  using R = RowPart<T, kB, C>;
+  static constexpr bool kVec = kB > 0;
+  static constexpr int kBytes = R::kPer * kB;    // of a row, a thread
   uint32_t base;
   int slot = 0;
   int bytes[kVec ? R::kPer : 1];                 // of the thread's vectors that are within a row
   R row;
   __device__ __forceinline__ Feed(const void* smem, int part, int d, int t, int G)
-      : base(kVec ? smem_u32(smem) + part * kSlots * kBytes * blockDim.x + 16 * threadIdx.x : 0) {
+      : base(kVec ? smem_u32(smem) + part * kSlots * kBytes * blockDim.x + kB * threadIdx.x : 0) {
     if constexpr (kVec) {
 #pragma unroll
       for (int k = 0; k < R::kPer; ++k)
-        bytes[k] = max(0, min(16, (d - R::col(t, G, k)) * static_cast<int>(sizeof(T))));
+        bytes[k] = max(0, min(kB, (d - R::col(t, G, k)) * static_cast<int>(sizeof(T))));
     }
   }
   __device__ __forceinline__ uint32_t at(int k) const {
-    return base + (slot * R::kPer + k) * 16 * blockDim.x;
+    return base + (slot * R::kPer + k) * kB * blockDim.x;
   }
   // Sends for row r, which starts at p, into the slot that was read last (in: it is a row at all).
   __device__ __forceinline__ void send(const T* first, int64_t r, int64_t ld, bool in, int d, int t,
@@ -110,9 +111,13 @@ struct Feed {
 #pragma unroll
       for (int k = 0; k < R::kPer; ++k) {
         const int n = in ? bytes[k] : 0;
-        asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(at(k)),
-                     "l"(n > 0 ? p + k * R::E * G : first), "r"(n)
-                     : "memory");
+        const T* from = n > 0 ? p + k * R::E * G : first;
+        if constexpr (kB == 16)
+          asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(at(k)), "l"(from), "r"(n)
+                       : "memory");
+        else
+          asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(at(k)), "l"(from), "r"(n)
+                       : "memory");
       }
     } else {
       row.load(p, in ? d : 0, t, G);
@@ -124,11 +129,15 @@ struct Feed {
     if constexpr (kVec) {
 #pragma unroll
       for (int k = 0; k < R::kPer; ++k) {
-        uint32_t* r = row.raw + 4 * k;
-        asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];"
-                     : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3])
-                     : "r"(at(k))
-                     : "memory");
+        if constexpr (kB == 16) {
+          uint32_t* r = row.raw + 4 * k;
+          asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];"
+                       : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3])
+                       : "r"(at(k))
+                       : "memory");
+        } else {
+          asm volatile("ld.shared.b32 %0, [%1];" : "=r"(row.raw[k]) : "r"(at(k)) : "memory");
+        }
       }
     }
     row.pairs(x);
@@ -191,10 +200,11 @@ struct NormParams {
 
 constexpr int kForwardSlots = 3, kBackwardSlots = 2;
 
-template <typename T, bool kVec, bool kCta, bool kWide, int C>
+template <typename T, int kB, bool kCta, bool kWide, int C>
 __global__ void __launch_bounds__(kWide ? 1024 : kCta ? 512 : 32 * kWarps)
     norm_kernel(const __grid_constant__ NormParams p) {
-  using R = RowPart<T, kVec, C>;
+  using R = RowPart<T, kB, C>;
+  constexpr bool kVec = kB > 0;
   constexpr int kSlots = kVec ? kForwardSlots : 1;
   constexpr int H = C / 2;
   extern __shared__ __align__(16) uint8_t slots[];
@@ -205,7 +215,7 @@ __global__ void __launch_bounds__(kWide ? 1024 : kCta ? 512 : 32 * kWarps)
   if (kCta) clear_sums(&red[0][0][0], 128);
   griddep_wait();
   const T* xs = static_cast<const T*>(p.x);
-  Feed<T, kVec, C, kSlots> feed(slots, 0, d, t, G);
+  Feed<T, kB, C, kSlots> feed(slots, 0, d, t, G);
   const auto send = [&](int64_t r) {
     feed.send(xs, r, p.ld_x, r < p.rows, d, t, G);
     feed_commit<kVec>();
@@ -319,12 +329,12 @@ struct GradParams {
 
 // kWide: 8192 < d <= 16384, 1024 threads of 64 registers: dw, db and the weights stand
 // in shared memory (192 KB at the longest), and no row is read ahead.
-template <typename T, bool kVec, bool kCta, bool kWide, int C>
+template <typename T, int kB, bool kCta, bool kWide, int C>
 __global__ void __launch_bounds__(kWide ? 1024 : kCta ? 512 : 32 * kWarps)
     norm_backward_kernel(const __grid_constant__ GradParams p) {
-  using R = RowPart<T, kVec, C>;
+  using R = RowPart<T, kB, C>;
   // kWide: the rows are read as they are needed
-  constexpr bool kFed = kVec && !kWide;
+  constexpr bool kFed = kB > 0 && !kWide;
   constexpr int kSlots = kFed ? kBackwardSlots : 1;
   constexpr int H = C / 2;
   __shared__ __align__(16) float red[2][64];
@@ -341,8 +351,8 @@ __global__ void __launch_bounds__(kWide ? 1024 : kCta ? 512 : 32 * kWarps)
   float2 w[kWide ? 1 : H], dw[kWide ? 1 : H], db[kWide ? 1 : H];
   const T* xs = static_cast<const T*>(p.x);
   const T* dys = static_cast<const T*>(p.dy);
-  Feed<T, kVec, C, kSlots> nx(wide, 0, d, t, G), ny(wide, 1, d, t, G);
-  RowPart<T, kVec, C> rx, ry;                  // kWide
+  Feed<T, kB, C, kSlots> nx(wide, 0, d, t, G), ny(wide, 1, d, t, G);
+  RowPart<T, kB, C> rx, ry;                  // kWide
   float mean_next[kSlots], rstd_next[kSlots];
   const auto send = [&](int k, int64_t row) {
     const bool in = row < p.rows;
@@ -582,30 +592,32 @@ cudaError_t resident_ctas(std::atomic<int>* known, Kernel kernel, int threads, s
   return cudaSuccess;
 }
 
-// The backward pass takes three rows a CTA at least: a CTA's sums cost about as much as a row.
+// The most CTAs of the backward pass, which launches as many of them as are resident (65,536 x 512:
+// 51 us; 5 an SM for every length 68).  It takes three rows a CTA at least: a CTA's sums cost about
+// as much as a row.
 int64_t backward_ctas(int64_t rows, int64_t d) {
   if (d <= kWarpCols)
-    return std::min(ceil_div(rows, 3 * kWarps * 32 / row_lanes(d)), int64_t{kPlanCTAs} * 5);
+    return std::min(ceil_div(rows, 3 * kWarps * 32 / row_lanes(d)), int64_t{kPlanCTAs} * 7);
   const int g = row_threads(d);
   return std::min(ceil_div(rows, 3), kPlanCTAs * std::max<int64_t>(1, 512 / g));
 }
 int64_t column_slabs(int64_t rows) { return std::min<int64_t>(ceil_div(rows, kSlabRows), 64); }
 
 // Bytes of a kernel's rows on their way, and the most that a kernel of C columns a thread takes.
-template <typename T, bool kVec, int C, int kSlots>
+template <typename T, int kB, int C, int kSlots>
 constexpr size_t slot_bytes(int threads, int parts) {
-  return static_cast<size_t>(parts) * kSlots * Feed<T, kVec, C, kSlots>::kBytes * threads;
+  return static_cast<size_t>(parts) * kSlots * Feed<T, kB, C, kSlots>::kBytes * threads;
 }
 
-template <typename T, bool kVec, bool kCta, bool kWide, int C>
+template <typename T, int kB, bool kCta, bool kWide, int C>
 cudaError_t run_norm_rows(const NormParams& p, int threads, int64_t units, cudaStream_t s) {
   static std::atomic<int> known[33];
   static PerDeviceOnce attr;
-  const auto kernel = norm_kernel<T, kVec, kCta, kWide, C>;
+  const auto kernel = norm_kernel<T, kB, kCta, kWide, C>;
   constexpr int kMost = kWide ? 1024 : kCta ? 512 : 32 * kWarps;
-  const size_t smem = slot_bytes<T, kVec, C, kForwardSlots>(threads, 1);
+  const size_t smem = slot_bytes<T, kB, C, kForwardSlots>(threads, 1);
   cudaError_t e = smem_attr_once(
-      attr, kernel, static_cast<int>(slot_bytes<T, kVec, C, kForwardSlots>(kMost, 1)));
+      attr, kernel, static_cast<int>(slot_bytes<T, kB, C, kForwardSlots>(kMost, 1)));
   int64_t ctas = 0;
   if (e == cudaSuccess) e = resident_ctas(known, kernel, threads, smem, &ctas);
   if (e != cudaSuccess) return e;
@@ -613,13 +625,14 @@ cudaError_t run_norm_rows(const NormParams& p, int threads, int64_t units, cudaS
                           smem, s, p);
 }
 
-template <typename T, bool kVec>
+template <typename T, int kB>
 cudaError_t run_norm(const NormParams& p, cudaStream_t s) {
   const int64_t units = p.d <= kWarpCols ? ceil_div(p.rows, kWarps * 32 / p.lanes) : p.rows;
-  if (p.d <= kShortCols) return run_norm_rows<T, kVec, false, false, 8>(p, 32 * kWarps, units, s);
-  if (p.d <= kWarpCols) return run_norm_rows<T, kVec, false, false, kCols>(p, 32 * kWarps, units, s);
-  if (p.d <= kMidCols) return run_norm_rows<T, kVec, true, false, kCols>(p, row_threads(p.d), units, s);
-  return run_norm_rows<T, kVec, true, true, kCols>(p, row_threads(p.d), units, s);
+  if constexpr (kB != 4)
+    if (p.d <= kShortCols) return run_norm_rows<T, kB, false, false, 8>(p, 32 * kWarps, units, s);
+  if (p.d <= kWarpCols) return run_norm_rows<T, kB, false, false, kCols>(p, 32 * kWarps, units, s);
+  if (p.d <= kMidCols) return run_norm_rows<T, kB, true, false, kCols>(p, row_threads(p.d), units, s);
+  return run_norm_rows<T, kB, true, true, kCols>(p, row_threads(p.d), units, s);
 }
 
 template <typename T>
@@ -628,40 +641,52 @@ cudaError_t run_norm_any(const NormParams& p, cudaStream_t s) {
     return launch_dependent(norm_loop_kernel<T>,
                             dim3(static_cast<unsigned>(std::min<int64_t>(p.rows, 4 * kPlanCTAs))),
                             dim3(kLoopThreads), 0, s, p);
-  const bool vec = on16(p.x, p.ld_x, sizeof(T)) && on16(p.y, p.ld_y, sizeof(T));
-  return vec ? run_norm<T, true>(p, s) : run_norm<T, false>(p, s);
+  const auto fits = [&](size_t n) {
+    return on_bytes(p.x, p.ld_x, sizeof(T), n) && on_bytes(p.y, p.ld_y, sizeof(T), n);
+  };
+  if (fits(16)) return run_norm<T, 16>(p, s);
+  // Two 16-bit elements at once: 20,000 x 4090 82 us, by elements 121; up to 256 columns no faster
+  // (100,000 x 90 26 us, by elements 23).
+  if constexpr (sizeof(T) == 2)
+    if (p.d > kShortCols && fits(4)) return run_norm<T, 4>(p, s);
+  return run_norm<T, 0>(p, s);
 }
 
-template <typename T, bool kVec, bool kCta, bool kWide, int C>
-cudaError_t run_backward_rows(const GradParams& p, dim3 grid, int threads, cudaStream_t s) {
-  const auto kernel = norm_backward_kernel<T, kVec, kCta, kWide, C>;
+template <typename T, int kB, bool kCta, bool kWide, int C>
+cudaError_t run_backward_rows(const GradParams& p, int64_t* parts, int threads, cudaStream_t s) {
+  const auto kernel = norm_backward_kernel<T, kB, kCta, kWide, C>;
   constexpr int kMost = kWide ? 1024 : kCta ? 512 : 32 * kWarps;
   const auto bytes = [](int n) {
     if (kWide) return 3 * kCols * sizeof(float) * n;
     const size_t sums = kCta ? 0 : 2 * kWarpCols * sizeof(float);
-    return std::max(sums, slot_bytes<T, kVec, C, kBackwardSlots>(n, 2));
+    return std::max(sums, slot_bytes<T, kB, C, kBackwardSlots>(n, 2));
   };
+  static std::atomic<int> known[33];
   static PerDeviceOnce attr;
-  const cudaError_t e = smem_attr_once(attr, kernel, static_cast<int>(bytes(kMost)));
+  cudaError_t e = smem_attr_once(attr, kernel, static_cast<int>(bytes(kMost)));
+  int64_t ctas = 0;
+  if (e == cudaSuccess) e = resident_ctas(known, kernel, threads, bytes(threads), &ctas);
   if (e != cudaSuccess) return e;
-  return launch_dependent(kernel, grid, dim3(threads), bytes(threads), s, p);
+  *parts = std::min(*parts, ctas);
+  return launch_dependent(kernel, dim3(static_cast<unsigned>(*parts)), dim3(threads), bytes(threads),
+                          s, p);
 }
 
-template <typename T, bool kVec>
-cudaError_t run_backward(const GradParams& p, int64_t ctas, cudaStream_t s) {
-  const dim3 grid(static_cast<unsigned>(ctas));
-  if (p.d <= kShortCols) return run_backward_rows<T, kVec, false, false, 8>(p, grid, 32 * kWarps, s);
-  if (p.d <= kWarpCols) return run_backward_rows<T, kVec, false, false, kCols>(p, grid, 32 * kWarps, s);
-  if (p.d <= kMidCols) return run_backward_rows<T, kVec, true, false, kCols>(p, grid, row_threads(p.d), s);
-  return run_backward_rows<T, kVec, true, true, kCols>(p, grid, row_threads(p.d), s);
+template <typename T, int kB>
+cudaError_t run_backward(const GradParams& p, int64_t* parts, cudaStream_t s) {
+  if constexpr (kB != 4)
+    if (p.d <= kShortCols) return run_backward_rows<T, kB, false, false, 8>(p, parts, 32 * kWarps, s);
+  if (p.d <= kWarpCols) return run_backward_rows<T, kB, false, false, kCols>(p, parts, 32 * kWarps, s);
+  if (p.d <= kMidCols) return run_backward_rows<T, kB, true, false, kCols>(p, parts, row_threads(p.d), s);
+  return run_backward_rows<T, kB, true, true, kCols>(p, parts, row_threads(p.d), s);
 }
 
 template <typename T>
-cudaError_t run_backward_any(const GradParams& p, int64_t parts, cudaStream_t s) {
+cudaError_t run_backward_any(const GradParams& p, int64_t* parts, cudaStream_t s) {
   if (p.d > kMaxCols) {
     // the column sums first: dx may take the place of x or dy
     if (p.part != nullptr) {
-      const dim3 grid(static_cast<unsigned>(ceil_div(p.d, 128)), static_cast<unsigned>(parts));
+      const dim3 grid(static_cast<unsigned>(ceil_div(p.d, 128)), static_cast<unsigned>(*parts));
       const cudaError_t e = launch_dependent(norm_columns_kernel<T>, grid, dim3(128), 0, s, p);
       if (e != cudaSuccess) return e;
     }
@@ -669,9 +694,15 @@ cudaError_t run_backward_any(const GradParams& p, int64_t parts, cudaStream_t s)
                             dim3(static_cast<unsigned>(std::min<int64_t>(p.rows, 4 * kPlanCTAs))),
                             dim3(kLoopThreads), 0, s, p);
   }
-  const bool vec = on16(p.x, p.ld_x, sizeof(T)) && on16(p.dy, p.ld_dy, sizeof(T)) &&
-                   on16(p.dx, p.ld_dx, sizeof(T));
-  return vec ? run_backward<T, true>(p, parts, s) : run_backward<T, false>(p, parts, s);
+  const auto fits = [&](size_t n) {
+    return on_bytes(p.x, p.ld_x, sizeof(T), n) && on_bytes(p.dy, p.ld_dy, sizeof(T), n) &&
+           on_bytes(p.dx, p.ld_dx, sizeof(T), n);
+  };
+  if (fits(16)) return run_backward<T, 16>(p, parts, s);
+  // as the forward pass: 5000 x 10,002 119 us, by elements 146; 100,000 x 90 35, by elements 31
+  if constexpr (sizeof(T) == 2)
+    if (p.d > kShortCols && fits(4)) return run_backward<T, 4>(p, parts, s);
+  return run_backward<T, 0>(p, parts, s);
 }
 
 int64_t backward_parts(int64_t rows, int64_t d) {
@@ -715,7 +746,7 @@ cudaError_t launch_norm_backward(const bergson_norm_grad_args& a, void* ws, cuda
     if (e == cudaSuccess && a.d_bias != nullptr) e = cudaMemsetAsync(a.d_bias, 0, a.d * sizeof(float), s);
     return e;
   }
-  const int64_t parts = backward_parts(a.rows, a.d);
+  int64_t parts = backward_parts(a.rows, a.d);
   GradParams p = {};
   p.x = a.x;
   p.w = a.weight;
@@ -733,9 +764,9 @@ cudaError_t launch_norm_backward(const bergson_norm_grad_args& a, void* ws, cuda
   p.wt = a.w_dtype;
   p.layer = a.kind == BERGSON_NORM_LAYER ? 1 : 0;
   p.inv_d = static_cast<float>(1.0 / static_cast<double>(a.d));
-  cudaError_t e = a.dtype == BERGSON_BF16  ? run_backward_any<__nv_bfloat16>(p, parts, s)
-                  : a.dtype == BERGSON_F16 ? run_backward_any<__half>(p, parts, s)
-                                           : run_backward_any<float>(p, parts, s);
+  cudaError_t e = a.dtype == BERGSON_BF16  ? run_backward_any<__nv_bfloat16>(p, &parts, s)
+                  : a.dtype == BERGSON_F16 ? run_backward_any<__half>(p, &parts, s)
+                                           : run_backward_any<float>(p, &parts, s);
   if (e != cudaSuccess || !sums) return e;
   const dim3 grid(static_cast<unsigned>(ceil_div(a.d, 32)), 2);
   return launch_dependent(norm_parts_kernel, grid, dim3(32 * kPartWarps), 0, s,

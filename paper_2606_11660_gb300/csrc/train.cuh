@@ -116,10 +116,11 @@ __device__ __forceinline__ H2 vec_max2(const uint4& v) {
 
 // Host helpers of the launchers.
 inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
-// Rows of a matrix that can be accessed 16 bytes at a time.
-inline bool on16(const void* p, int64_t ld, size_t size) {
-  return reinterpret_cast<uintptr_t>(p) % 16 == 0 && ld * size % 16 == 0;
+// Rows of a matrix that can be accessed 16 (4) bytes at a time.
+inline bool on_bytes(const void* p, int64_t ld, size_t size, size_t n) {
+  return reinterpret_cast<uintptr_t>(p) % n == 0 && ld * size % n == 0;
 }
+inline bool on16(const void* p, int64_t ld, size_t size) { return on_bytes(p, ld, size, 16); }
 
 __device__ __forceinline__ float load_any(const void* p, int type, int64_t i) {
   if (type == BERGSON_BF16) return __bfloat162float(static_cast<const __nv_bfloat16*>(p)[i]);
@@ -127,11 +128,13 @@ __device__ __forceinline__ float load_any(const void* p, int type, int64_t i) {
   return static_cast<const float*>(p)[i];
 }
 
-// A thread's columns of a row and how they lie in it: kPer vectors of E elements, vector k at column
-// E (t + k G) for thread t of the G that share the row.
-template <typename T, bool kVec, int C>
+// A thread's columns of a row and how they lie in it: kPer vectors of kB bytes (16; 4, of two 16-bit
+// elements; 0: an element), vector k at column E (t + k G) for thread t of the G that share the row.
+template <typename T, int kB, int C>
 struct RowPart {
-  static constexpr int E = kVec ? Vec16<T>::kElems : 1;
+  static_assert(kB == 16 || (kB == 4 && sizeof(T) == 2) || kB == 0, "vectors of 16 or 4 bytes");
+  static constexpr bool kVec = kB == 16;
+  static constexpr int E = kB == 0 ? 1 : kB / static_cast<int>(sizeof(T));
   static constexpr int kPer = C / E;
   // As they lie in memory.
   static constexpr int kWords = kVec ? 4 * kPer : kPer;
@@ -160,6 +163,9 @@ struct RowPart {
           v = *reinterpret_cast<const uint4*>(part);
         }
         raw[4 * k] = v.x; raw[4 * k + 1] = v.y; raw[4 * k + 2] = v.z; raw[4 * k + 3] = v.w;
+      } else if constexpr (kB == 4) {
+        raw[k] = n >= 2 ? *reinterpret_cast<const uint32_t*>(p)
+                 : n == 1 ? *reinterpret_cast<const uint16_t*>(p) : 0;
       } else {
         raw[k] = 0;
         if (n > 0) {
@@ -179,6 +185,10 @@ struct RowPart {
         for (int i = 0; i < E / 2; ++i)
           x[E / 2 * k + i] = unpack2(v, i, static_cast<const T*>(nullptr));
       }
+    } else if constexpr (kB == 4) {
+#pragma unroll
+      for (int k = 0; k < kPer; ++k)
+        x[k] = unpack2(make_uint4(raw[k], 0, 0, 0), 0, static_cast<const T*>(nullptr));
     } else {
 #pragma unroll
       for (int k = 0; k < C / 2; ++k) x[k] = make_float2(one(raw[2 * k]), one(raw[2 * k + 1]));
@@ -221,6 +231,11 @@ struct RowPart {
             if (i < n) p[i] = from_f32<T>(i % 2 == 0 ? y.x : y.y);
           }
         }
+      } else if constexpr (kB == 4) {
+        uint4 v = make_uint4(0, 0, 0, 0);
+        pack2(v, 0, x[k], static_cast<const T*>(nullptr));
+        if (n >= 2) *reinterpret_cast<uint32_t*>(p) = v.x;
+        else if (n == 1) *p = from_f32<T>(x[k].x);
       } else if (n > 0) {
         *p = from_f32<T>(k % 2 == 0 ? x[k / 2].x : x[k / 2].y);
       }

@@ -133,6 +133,22 @@ def test_rows_apart(d, pad, offset, dtype):
         assert bool((f == 7.0).all())
 
 
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("d,pad,offset", [(41, 1, 0), (40, 2, 2), (250, 4, 6), (257, 5, 4), (777, 1, 10),
+                                          (1030, 4, 0), (8191, 1, 2), (9001, 1, 4), (16383, 3, 2)])
+def test_rows_of_whole_words(d, pad, offset, dtype):
+    """Rows at even elements, no multiple of 16 bytes apart or not on one, odd and even lengths."""
+    R = 7
+    x, dy, w, b = inputs(R, d, dtype, dtype, pad, offset, seed=d)
+    flat, y = matrix(R, d, dtype, pad, offset)
+    _, mean, rstd = check_forward(x, w, b, LAYER, y=y)
+    flat2, dx = matrix(R, d, dtype, pad, offset)
+    check_backward(x, dy, w, LAYER, mean, rstd, dx)
+    for f, m in ((flat, y), (flat2, dx)):
+        m.fill_(7.0)
+        assert bool((f == 7.0).all())
+
+
 @pytest.mark.parametrize("R,d", [(4000, 24), (5000, 300), (3000, 1100), (700, 8192), (400, 10_000),
                                  (700, 17_000)])
 def test_many_rows(R, d):

@@ -122,7 +122,8 @@ EMBED_BAD = [
     (dict(dtype=7), bg.BERGSON_EINVAL), (dict(rows=-1), bg.BERGSON_EINVAL),
     (dict(rows=1 << 31), bg.BERGSON_EINVAL), (dict(V=0), bg.BERGSON_EINVAL),
     (dict(V=1 << 31), bg.BERGSON_EINVAL), (dict(d=0), bg.BERGSON_EINVAL),
-    (dict(d=1 << 25), bg.BERGSON_EUNSUPPORTED), (dict(rows=1 << 30, d=1024), bg.BERGSON_EUNSUPPORTED),
+    (dict(d=1 << 25), bg.BERGSON_EUNSUPPORTED), (dict(d=(1 << 20) + 1), bg.BERGSON_EUNSUPPORTED),
+    (dict(rows=1 << 30, d=1024), bg.BERGSON_EUNSUPPORTED),
     (dict(scale=INF), bg.BERGSON_EINVAL), (dict(scale=NAN), bg.BERGSON_EINVAL),
     (dict(scale=1e39), bg.BERGSON_EINVAL), (dict(ids=None), bg.BERGSON_EINVAL),
     (dict(ids=FAKE + 4), bg.BERGSON_EALIGN), (dict(ld_t=99), bg.BERGSON_EINVAL),
