@@ -981,6 +981,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
                                                                     o.mat)
                      : "memory");
     }
+    // one that gave up may have copies out of shared memory on their way
+    if (P == 1 && aborted && lane == 0) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
     __syncwarp();
   }
 
