@@ -11,7 +11,7 @@
 // others by comparing tokens, and CTAs of their own write zeros to the rest of the
 // table.  Above, a radix sort of (token, row), 9 bits a pass: counts per tile
 // of rows, then every tile places its rows behind those of the tiles before it.
-// The sorted rows are added up kRun at a time: a token whose rows all lie within such a run
+// The sorted rows are added up 8 to 64 at a time, a run: a token whose rows all lie within such a run
 // is done there; what it has of the tokens that cross its ends goes to the workspace and is
 // joined by a last kernel.  No run is longer than another, however often a token comes.
 // 65,536 x 4096 bf16 lookups 111 us (6.2 TB/s); the gradient of 65,536 x 2048 into 50,304 rows 114 us:
@@ -77,7 +77,8 @@ constexpr int kFewRows = 4096;                 // up to here one launch does it 
 constexpr int kFewThreads = 512;
 constexpr int kFewZeros = 512;                 // rows of the table a CTA of zeros looks after, at most,
 constexpr int64_t kZeroBytes = 64 << 10;       //   and what they hold, about
-constexpr int kRun = 32;                       // sorted rows added up by one CTA
+constexpr int kMinRun = 8, kMaxRun = 64;       // sorted rows added up by one CTA
+constexpr int64_t kManyRuns = 1000;            // CTAs that are worth longer runs
 constexpr int kSumThreads = 128;
 constexpr int kCols = 8;                       // columns a thread
 constexpr int kFewAhead = 4;                   // rows on their way
@@ -481,6 +482,7 @@ struct SumParams {
   int64_t runs;
   int64_t n_sum;               // CTAs that add
   int d, slabs;
+  int run;                     // rows of a run, a multiple of 8
 };
 
 // kAdd: the table's rows that are done here come with the rows that are added to them.
@@ -488,9 +490,9 @@ template <typename T, bool kVec, bool kAdd>
 __global__ void __launch_bounds__(kSumThreads) sum_kernel(const __grid_constant__ SumParams p) {
   constexpr int kAhead = kAdd ? 4 : 8;           // rows on their way
   using R = RowPart<T, kVec ? 16 : 0, kCols>;
-  __shared__ uint32_t keys[kRun + 2];            // one before, one behind
-  __shared__ int rows[kRun];
-  const int tid = threadIdx.x, G = blockDim.x;
+  __shared__ uint32_t keys[kMaxRun + 2];         // one before, one behind
+  __shared__ int rows[kMaxRun];
+  const int tid = threadIdx.x, G = blockDim.x, length = p.run;
   griddep_wait();
   if (blockIdx.x >= p.n_sum) {
     const int64_t step = static_cast<int64_t>(gridDim.x - p.n_sum) * (G / 32);
@@ -499,19 +501,19 @@ __global__ void __launch_bounds__(kSumThreads) sum_kernel(const __grid_constant_
     return;
   }
   const uint32_t none = static_cast<uint32_t>(p.V);
-  const int64_t run = blockIdx.x / p.slabs, p0 = run * kRun;
+  const int64_t run = blockIdx.x / p.slabs, p0 = run * length;
   const int c0 = static_cast<int>(blockIdx.x % p.slabs) * G * kCols;
-  for (int i = tid; i < kRun + 2; i += G) {
+  for (int i = tid; i < length + 2; i += G) {
     const int64_t at = p0 + i - 1;
     keys[i] = at >= 0 && at < p.rows ? p.key[at] : none;
-    if (i < kRun) rows[i] = p0 + i < p.rows ? p.row[p0 + i] : 0;
+    if (i < length) rows[i] = p0 + i < p.rows ? p.row[p0 + i] : 0;
   }
   __syncthreads();
   bool open = keys[0] == keys[1];                // the first token began before
   float sum[kCols];
 #pragma unroll
   for (int i = 0; i < kCols; ++i) sum[i] = 0.0f;
-  for (int j0 = 0; j0 < kRun; j0 += kAhead) {
+  for (int j0 = 0; j0 < length; j0 += kAhead) {
     if (keys[j0 + 1] == none) break;
     R row[kAhead];
     float old[kAdd ? kAhead : 1][kCols];
@@ -536,7 +538,7 @@ __global__ void __launch_bounds__(kSumThreads) sum_kernel(const __grid_constant_
 #pragma unroll
       for (int i = 0; i < kCols; ++i) sum[i] += x[i];
       const bool ends = keys[j + 2] != v;
-      if (!ends && j < kRun - 1) continue;
+      if (!ends && j < length - 1) continue;
       if (open || !ends) {
         float* part = p.part + (2 * run + (open ? 0 : 1)) * p.ld_part;
 #pragma unroll
@@ -595,20 +597,20 @@ __global__ void __launch_bounds__(kJoinThreads) join_kernel(const __grid_constan
   const uint32_t none = static_cast<uint32_t>(p.V);
   griddep_wait();
   const int64_t run0 = static_cast<int64_t>(blockIdx.x) * kWarps, run = run0 + warp;
-  const int64_t last = run * kRun + kRun - 1;
+  const int64_t last = run * p.run + p.run - 1;
   int64_t n = 0;                                 // part sums, if a token that goes on begins here
   uint32_t v = none;
   if (last + 1 < p.rows) {
     v = p.key[last];
     const uint32_t next = p.key[last + 1];
-    const uint32_t before = run > 0 ? p.key[run * kRun - 1] : none;
+    const uint32_t before = run > 0 ? p.key[run * p.run - 1] : none;
     if (v != none && next == v && before != v) {
       // does run + n hold some too?  128 runs a step
       for (n = 2;; n += 128) {
         uint32_t first[4];
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
-          const int64_t at = (run + n + 32 * k + lane) * kRun;
+          const int64_t at = (run + n + 32 * k + lane) * p.run;
           first[k] = at < p.rows ? p.key[at] : none;
         }
         int more = 0;
@@ -647,7 +649,7 @@ __global__ void __launch_bounds__(kJoinThreads) join_kernel(const __grid_constan
         s.x += x.x; s.y += x.y; s.z += x.z; s.w += x.w;
       }
       const float sum[4] = {s.x, s.y, s.z, s.w};
-      put_columns<4>(p.out, p.key[(run0 + k) * kRun + kRun - 1], col, p.d, sum);
+      put_columns<4>(p.out, p.key[(run0 + k + 1) * p.run - 1], col, p.d, sum);
     }
   }
 }
@@ -660,20 +662,32 @@ int slab_threads(int64_t d) {
 }
 
 struct SortPlan {
-  int passes = 1, tiles = 1;
+  int passes = 1, tiles = 1, run = kMinRun;
   int64_t tile = kSortItems, runs = 0, ld_part = 0;
   size_t table = 0, touched = 0, key[2] = {0, 0}, row[2] = {0, 0}, part = 0, total = 0;
   int64_t clear_words = 0;     // from the second pass's table to the end of `touched`
 };
 
-SortPlan sort_plan(int64_t rows, int64_t V, int64_t d) {
+// Long runs have less to join, short ones more rows on their way when there are few: 32 rows a run
+// for all had 5009 x 437 at 41 us and 33,799 x 5463 at 146; by this rule 32 and 129.  With rows
+// of the table beside them (add) a run takes twice the turns.
+int run_rows(int64_t rows, int64_t d, bool add) {
+  const int64_t ctas = rows * ceil_div(d, slab_threads(d) * kCols);      // of runs of one row
+  const int64_t many = add ? 2 * kManyRuns : kManyRuns;
+  int run = kMinRun;
+  while (run < (add ? kMaxRun / 2 : kMaxRun) && ctas >= 2 * run * many) run *= 2;
+  return run;
+}
+
+SortPlan sort_plan(int64_t rows, int64_t V, int64_t d, bool add) {
   SortPlan s;
   int bits = 1;
   while ((V >> bits) != 0) ++bits;             // keys are 0 .. V
   s.passes = static_cast<int>(ceil_div(bits, kDigitBits));
   s.tile = ceil_div(ceil_div(rows, kMaxTiles), kSortItems) * kSortItems;
   s.tiles = static_cast<int>(ceil_div(rows, s.tile));
-  s.runs = ceil_div(rows, kRun);
+  s.run = run_rows(rows, d, add);
+  s.runs = ceil_div(rows, s.run);
   s.ld_part = ceil_div(d, 8) * 8;
   size_t at = 0;
   const auto take = [&](size_t bytes) {
@@ -729,7 +743,7 @@ cudaError_t run_sums(const bergson_embedding_grad_args& a, SumParams p, cudaStre
 
 cudaError_t run_sorted(const bergson_embedding_grad_args& a, const GradOut& out, bool vec,
                        uint8_t* ws, int* status, cudaStream_t s) {
-  const SortPlan plan = sort_plan(a.rows, a.V, a.d);
+  const SortPlan plan = sort_plan(a.rows, a.V, a.d, a.add != 0);
   SortParams p = {};
   p.ids = a.ids;
   p.table = reinterpret_cast<int*>(ws + plan.table);
@@ -772,6 +786,7 @@ cudaError_t run_sorted(const bergson_embedding_grad_args& a, const GradOut& out,
   q.ld_dy = a.ld_dy;
   q.ld_part = plan.ld_part;
   q.runs = plan.runs;
+  q.run = plan.run;
   q.d = static_cast<int>(a.d);
   if (a.dtype == BERGSON_BF16)
     e = vec ? run_sums<__nv_bfloat16, true>(a, q, s) : run_sums<__nv_bfloat16, false>(a, q, s);
@@ -815,7 +830,7 @@ cudaError_t launch_embedding(const bergson_embedding_args& a, int* status, cudaS
 }
 
 size_t embedding_backward_workspace(int64_t rows, int64_t V, int64_t d) {
-  return rows <= kFewRows ? 256 : sort_plan(rows, V, d).total;
+  return rows <= kFewRows ? 256 : sort_plan(rows, V, d, true).total;
 }
 
 cudaError_t launch_embedding_backward(const bergson_embedding_grad_args& a, void* ws, int* status,

@@ -134,6 +134,19 @@ def test_orders_of_tokens(R, kind):
         check_gradient(ids, V, 72, torch.bfloat16, torch.float32, add)
 
 
+@pytest.mark.parametrize("R", [17_000, 40_000, 70_001])
+@pytest.mark.parametrize("kind", ["one", "apart", "last", "falling", "skewed"])
+def test_orders_of_many_tokens(R, kind):
+    """The longer runs, and tokens that cross their ends or fill them."""
+    V = 4000
+    i = torch.arange(R, device=DEV)
+    ids = {"one": torch.full_like(i, 5), "apart": (i * 7919) % V,
+           "last": torch.where(i % 64 < 63, i % (V - 1), V - 1), "falling": ((R - 1 - i) // 64) % V,
+           "skewed": tokens(R, V, seed=R)}[kind]
+    for add in (False, True):
+        check_gradient(ids, V, 24, torch.bfloat16, torch.float32, add)
+
+
 @pytest.mark.parametrize("R,V", [(5000, 511), (5000, 512), (5000, 513), (5000, 262_143), (5000, 262_144),
                                  (300_000, 5000)])
 def test_sort_passes(R, V):
