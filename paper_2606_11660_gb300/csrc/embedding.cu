@@ -14,8 +14,8 @@
 // The sorted rows are added up 8 to 64 at a time, a run: a token whose rows all lie within such a run
 // is done there; what it has of the tokens that cross its ends goes to the workspace and is
 // joined by a last kernel.  No run is longer than another, however often a token comes.
-// 65,536 x 4096 bf16 lookups 111 us (6.2 TB/s); the gradient of 65,536 x 2048 into 50,304 rows 114 us:
-// the sort 20 (latency), sums and zeros 80 (5.7 TB/s), joining 13.
+// 65,536 x 4096 bf16 lookups 111 us (6.2 TB/s); the gradient of 65,536 x 2048 into 50,304 rows 110 us:
+// the sort 25 (latency), sums and zeros 75 (6.0 TB/s), joining 11.
 
 #include <algorithm>
 

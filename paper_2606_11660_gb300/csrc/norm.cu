@@ -5,12 +5,12 @@
 //             dx = rstd (h - mean h - n mean (h n)),  dw = sum_r dy n,  db = sum_r dy
 //
 // (mu = 0 and no mean of h without a mean).  Both are bound by their bytes: a
-// row is read once, stays in the registers of the 4 .. 32 lanes (up to 512 columns)
-// or the CTA that have it, 8 or 16 columns a thread, and the next rows are on their way while this
+// row is read once, stays in the registers of the 4 .. 32 lanes (up to 512 columns;
+// forward up to 1024) or the CTA that have it, 8 to 32 columns a thread, and the next rows are on their way while this
 // one is reduced.  A thread keeps its columns from row to row, so that weights are
 // loaded once a CTA and the backward pass sums dw and db in registers; one row
 // of both a CTA goes to the workspace, and a second kernel adds these up in order.
-// 65,536 x 2048 bf16: 95 us forward (5.7 TB/s) and 142 backward (138 and 4; 5.8 TB/s); the forward pass
+// 65,536 x 2048 bf16: 91 us forward (5.9 TB/s) and 139 backward (135 and 4; 6.0 TB/s); the forward pass
 // fills 68% of the issue slots, and did so at 77% in 127 us before its arithmetic went in pairs.
 
 #include <algorithm>
@@ -26,7 +26,8 @@ namespace {
 
 constexpr int kCols = 16;                      // columns a thread
 constexpr int kShortCols = 32 * 8;             // up to here 8 columns a lane, as few lanes as do
-constexpr int kWarpCols = 32 * kCols;          // up to here a warp takes a row
+constexpr int kWarpCols = 32 * kCols;          // up to here a warp takes a row, 16 columns a lane
+constexpr int kLongCols = 64 * kCols;          // forward, with vectors, up to here, 32 columns a lane
 constexpr int kWarps = 4;                      // warps of such a CTA
 constexpr int kMidCols = 8192;                 // up to here dw, db and the next row stay in registers
 constexpr int kMaxCols = 16384;                // up to here a row stays in registers
@@ -627,12 +628,17 @@ cudaError_t run_norm_rows(const NormParams& p, int threads, int64_t units, cudaS
 
 template <typename T, int kB>
 cudaError_t run_norm(const NormParams& p, cudaStream_t s) {
-  const int64_t units = p.d <= kWarpCols ? ceil_div(p.rows, kWarps * 32 / p.lanes) : p.rows;
+  const int64_t units = ceil_div(p.rows, kWarps * 32 / p.lanes);       // of kernels without kCta
   if constexpr (kB != 4)
     if (p.d <= kShortCols) return run_norm_rows<T, kB, false, false, 8>(p, 32 * kWarps, units, s);
   if (p.d <= kWarpCols) return run_norm_rows<T, kB, false, false, kCols>(p, 32 * kWarps, units, s);
-  if (p.d <= kMidCols) return run_norm_rows<T, kB, true, false, kCols>(p, row_threads(p.d), units, s);
-  return run_norm_rows<T, kB, true, true, kCols>(p, row_threads(p.d), units, s);
+  // No barrier a row: 65,536 x 768 52 us, by CTAs 56; 65,536 x 640 38 and 44.  The backward
+  // pass has no registers for it (32,768 x 1024 fp32 88 us, by CTAs 74).
+  if constexpr (kB == 16)
+    if (p.d <= kLongCols)
+      return run_norm_rows<T, kB, false, false, 2 * kCols>(p, 32 * kWarps, units, s);
+  if (p.d <= kMidCols) return run_norm_rows<T, kB, true, false, kCols>(p, row_threads(p.d), p.rows, s);
+  return run_norm_rows<T, kB, true, true, kCols>(p, row_threads(p.d), p.rows, s);
 }
 
 template <typename T>
@@ -658,7 +664,7 @@ cudaError_t run_backward_rows(const GradParams& p, int64_t* parts, int threads, 
   constexpr int kMost = kWide ? 1024 : kCta ? 512 : 32 * kWarps;
   const auto bytes = [](int n) {
     if (kWide) return 3 * kCols * sizeof(float) * n;
-    const size_t sums = kCta ? 0 : 2 * kWarpCols * sizeof(float);
+    const size_t sums = kCta ? 0 : 2 * 32 * C * sizeof(float);
     return std::max(sums, slot_bytes<T, kB, C, kBackwardSlots>(n, 2));
   };
   static std::atomic<int> known[33];

@@ -158,6 +158,19 @@ def test_many_rows(R, d):
     check_backward(x, dy, w, LAYER, mean, rstd)
 
 
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("R,d,pad", [(1, 520, 0), (7, 520, 8), (4001, 776, 0), (6003, 1001, 7), (9, 1017, 7),
+                                     (2500, 1024, 8)])
+def test_medium_rows(R, d, pad, dtype):
+    """Rows that end inside a vector, of a warp's last turn alone or of many turns."""
+    x, dy, w, b = inputs(R, d, dtype, dtype, pad, 8, seed=R)
+    flat, y = matrix(R, d, dtype, pad, 8)
+    _, mean, rstd = check_forward(x, w, b, LAYER, y=y)
+    check_backward(x, dy, w, LAYER, mean, rstd)
+    y.fill_(7.0)
+    assert bool((flat == 7.0).all())
+
+
 @pytest.mark.parametrize("d", [100, 1000, 9000, 17_000])
 def test_in_place_and_optional(d):
     x, dy, w, b = inputs(40, d, torch.bfloat16, torch.float32, seed=d)
