@@ -1100,8 +1100,11 @@ typedef struct bergson_muon_tensor {
  *   param <- param - lr lr_scale (ortho_scale X + weight_decay param)
  *
  * (X^T X and from the right where rows > cols, which is the same).  The iteration drives X's
- * singular values toward 1.  An update of zeros has X = 0; one that holds NaN or an infinity
- * spoils its matrix, and no other.
+ * singular values toward 1, whatever the size of u: every finite u of fp32 that is not all zeros has its
+ * X, subnormal ones too, and nothing is added to |u|_F.  A matrix whose gradients stop keeps taking steps of
+ * full length along the momentum that is left, until that is 0: leave it out of the call, or set its
+ * ortho_scale to 0.  An update of zeros has X = 0; one that holds NaN or an infinity spoils its
+ * matrix, and no other.
  *
  *   tensors   HOST array of n_tensors (>= 0) records, of any shapes; matrices of one shape run
  *             together.

@@ -54,7 +54,7 @@ int64_t round_to(int64_t n, int64_t to) { return (n + to - 1) / to * to; }
 
 constexpr int kMomentThreads = 256;
 constexpr int64_t kMomentChunk = 8 * kMomentThreads;   // elements of a CTA's turn
-constexpr float kUp = 0x1p50f, kDown = 0x1p-50f;
+constexpr float kUp = 0x1p100f, kDown = 0x1p-100f;
 
 struct MomentEntry {
   const void* g;
@@ -82,7 +82,7 @@ struct MomentParams {
   int nesterov;
   int n;
   const float* grad_scale;
-  float2* part;                // a CTA's sums of squares
+  float3* part;                // a CTA's sums of squares
   int* counters;               // of the products: cleared by the first CTA
   int64_t chunk;               // elements a CTA
   uint32_t begin[N + 1];       // first CTA of each matrix
@@ -154,8 +154,9 @@ __device__ __forceinline__ int64_t in_plane(int64_t i, int cols, int ld) {
   return row * ld + (i - row * cols);
 }
 
-// m's update and the sums of u's squares, of 2^50 u and of 2^-50 u: one of them holds the norm
-// of any u that fp32 does.
+// m's update and the sums of the squares of 2^100 u, u and 2^-100 u.  The first that is finite holds the
+// norm of any u that fp32 does, with all its digits: the smallest u, 2^-149, has a square of 2^-98 in the first
+// sum, and where a sum of up to 2^36 squares passed 2^128, the largest is 2^-108 or more in the next one.
 template <int N>
 __global__ void __launch_bounds__(kMomentThreads) moment_kernel(
     const __grid_constant__ MomentParams<N> p) {
@@ -168,21 +169,23 @@ __global__ void __launch_bounds__(kMomentThreads) moment_kernel(
   const float gs = p.grad_scale != nullptr ? *p.grad_scale : 1.0f;
   const int64_t begin = static_cast<int64_t>(blockIdx.x - p.begin[k]) * p.chunk;
   const int64_t end = min(begin + p.chunk, e.n);
-  CompensatedSum up, down;
+  CompensatedSum up, mid, down;
   for (int64_t at = begin; at < end; at += kMomentChunk) {
     float g[8], m[8];
     load_turn(e.g, e.gt, e.vec, at, end, g);
     load_turn(e.m, BERGSON_F32, e.vec, at, end, m);
-    float su = 0.0f, sd = 0.0f;
+    float su = 0.0f, sm = 0.0f, sd = 0.0f;
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
       const float a = p.alpha * (g[j] * gs);
       m[j] = fmaf(p.beta, m[j], a);
       const float u = p.nesterov ? fmaf(p.beta, m[j], a) : m[j];
       su = fmaf(u * kUp, u * kUp, su);
+      sm = fmaf(u, u, sm);
       sd = fmaf(u * kDown, u * kDown, sd);
     }
     up.add(su);
+    mid.add(sm);
     down.add(sd);
     if (e.vec) {
       if (place(true, at, 0) < end) {
@@ -197,11 +200,13 @@ __global__ void __launch_bounds__(kMomentThreads) moment_kernel(
         if (place(false, at, j) < end) e.m[place(false, at, j)] = m[j];
     }
   }
-  const float a = block_sum(up.s, red[0]), b = block_sum(down.s, red[1]);
-  if (threadIdx.x == 0) p.part[blockIdx.x] = make_float2(a, b);
+  const float a = block_sum(up.s, red[0]), b = block_sum(mid.s, red[1]), c = block_sum(down.s, red[0]);
+  if (threadIdx.x == 0) p.part[blockIdx.x] = make_float3(a, b, c);
 }
 
-// The planes of 1024 u / |u|_F.  A matrix of zeros stays one.
+// The planes of 1024 u / |u|_F, as (2^k u) (1024 / |2^k u|_F) with the k of the sum that holds the norm:
+// 1024 / |u|_F alone would pass fp32 below 3e-36, and the norm itself above 3.4e38.  A matrix of
+// zeros stays one; one that holds NaN or an infinity is NaN.
 template <int N, int P>
 __global__ void __launch_bounds__(kMomentThreads) planes_kernel(
     const __grid_constant__ MomentParams<N> p) {
@@ -209,16 +214,21 @@ __global__ void __launch_bounds__(kMomentThreads) planes_kernel(
   const int k = entry_of(p);
   const MomentEntry& e = p.e[k];
   griddep_wait();
-  float a = 0.0f, b = 0.0f;
+  float a = 0.0f, b = 0.0f, c = 0.0f;
   for (uint32_t i = p.begin[k] + threadIdx.x; i < p.begin[k + 1]; i += kMomentThreads) {
-    const float2 s = p.part[i];
+    const float3 s = p.part[i];
     a += s.x;
     b += s.y;
+    c += s.z;
   }
   a = block_sum(a, red[0]);
   b = block_sum(b, red[1]);
-  const float norm = a - a == 0.0f ? __fsqrt_rn(a) * kDown : __fsqrt_rn(b) * kUp;
-  const float scale = norm == 0.0f ? 0.0f : kPlaneScale * __frcp_rn(norm);
+  c = block_sum(c, red[0]);
+  const bool small = a - a == 0.0f, medium = b - b == 0.0f;
+  const float shift = small ? kUp : medium ? 1.0f : kDown, square = small ? a : medium ? b : c;
+  const float scale = square - square != 0.0f ? __int_as_float(0x7fffffff)
+                      : square == 0.0f        ? 0.0f
+                                              : kPlaneScale * __frcp_rn(__fsqrt_rn(square));
   const float gs = p.grad_scale != nullptr ? *p.grad_scale : 1.0f;
   const int64_t begin = static_cast<int64_t>(blockIdx.x - p.begin[k]) * p.chunk;
   const int64_t end = min(begin + p.chunk, e.n);
@@ -237,7 +247,7 @@ __global__ void __launch_bounds__(kMomentThreads) planes_kernel(
       uint4 hi, lo;
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
-        const float2 v = make_float2(u[2 * j] * scale, u[2 * j + 1] * scale);
+        const float2 v = make_float2(u[2 * j] * shift * scale, u[2 * j + 1] * shift * scale);
         pack2(hi, j, v, static_cast<const __half*>(nullptr));
         const float2 h = unpack2(hi, j, static_cast<const __half*>(nullptr));
         pack2(lo, j, make_float2(v.x - h.x, v.y - h.y), static_cast<const __half*>(nullptr));
@@ -251,7 +261,7 @@ __global__ void __launch_bounds__(kMomentThreads) planes_kernel(
     for (int j = 0; j < 8; ++j) {
       const int64_t i = place(false, at, j);
       if (i >= end) break;
-      const float v = u[j] * scale;
+      const float v = u[j] * shift * scale;
       const __half hi = __float2half_rn(v);
       __half* x = e.x + in_plane(i, e.cols, e.ld);
       *x = hi;
@@ -1068,7 +1078,7 @@ BatchLayout layout_of(const Batch& b, int P) {
                      round_to(ceil_div(b.elements, kPlanCTAs * 16), kMomentChunk));
   for (const Shape& s : b.shapes)
     l.ctas += ceil_div(s.rows * s.cols, l.chunk) * static_cast<int64_t>(s.mats.size());
-  l.part = take(l.ctas * static_cast<int64_t>(sizeof(float2)));
+  l.part = take(l.ctas * static_cast<int64_t>(sizeof(float3)));
   l.counters = take((1 + b.mats) * static_cast<int64_t>(sizeof(int)));
   for (const Shape& s : b.shapes) {
     Planes p;
@@ -1156,7 +1166,7 @@ cudaError_t run_moments(const bergson_muon_tensor* t, const Batch& b, const Batc
   p.nesterov = a.nesterov ? 1 : 0;
   p.n = b.mats;
   p.grad_scale = a.grad_scale;
-  p.part = reinterpret_cast<float2*>(ws + l.part);
+  p.part = reinterpret_cast<float3*>(ws + l.part);
   p.counters = reinterpret_cast<int*>(ws + l.counters);
   p.chunk = l.chunk;
   p.begin[0] = 0;
