@@ -957,8 +957,10 @@ BERGSON_API int bergson_factor_moments(const bergson_moment_matrix* mats, int n_
  *   y         [rows, ld_y] of `dtype`; may be x itself with ld_y == ld_x.
  *   mean, rstd  fp32 [rows], what the backward pass reads, each or NULL; mean is not
  *             written without a mean.
- * Sums and squares are fp32, about the row's mean (values above some 1e18 overflow them).  A row
- * that holds NaN or an infinity is NaN; the others keep their values.  rows in [0, 2^31), d <= 2^24.
+ * Sums and squares are fp32, about the row's mean.  A row that holds NaN or an infinity, or whose
+ * squares pass fp32 (values above some 1e18), is NaN, its rstd with it; the others keep their values.
+ * With eps = 0, rows of values below some 1e-18 lose digits of their squares (below 1e-23 all of
+ * them).  rows in [0, 2^31), d <= 2^24.
  * Errors: EINVAL, EALIGN, EUNSUPPORTED, ECUDA.
  */
 typedef struct bergson_norm_args {

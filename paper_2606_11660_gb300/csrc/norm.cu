@@ -73,6 +73,11 @@ __device__ __forceinline__ void row_sums(float (&v)[N], int G, float* red) {
     }
   }
 }
+// rstd of a mean square with eps added: NaN where that is infinite, so that a row which holds an infinity
+// is NaN without a mean too (1 / sqrt(inf) = 0 would make its other entries zeros).
+__device__ __forceinline__ float inverse_root(float square) {
+  return __frcp_rn(__fsqrt_rn(square)) + (square - square);
+}
 // Clears the places of row_sums.
 __device__ __forceinline__ void clear_sums(float* red, int n) {
   for (int i = threadIdx.x; i < n; i += blockDim.x) red[i] = 0.0f;
@@ -265,7 +270,7 @@ __global__ void __launch_bounds__(kWide ? 1024 : kCta ? 512 : 32 * kWarps)
     for (int i = 1; i < H; ++i) q2 = fma2(x[i], x[i], q2);
     float q[1] = {q2.x + q2.y};
     row_sums<kCta>(q, G, red[turn][1]);
-    const float rstd = __frcp_rn(__fsqrt_rn(fmaf(q[0], p.inv_d, p.eps)));
+    const float rstd = inverse_root(fmaf(q[0], p.inv_d, p.eps));
 #pragma unroll
     for (int i = 0; i < H; ++i) x[i] = fma2(mul2(x[i], pair(rstd)), w[i], b[i]);
     R::store_pairs(static_cast<T*>(p.y) + r * p.ld_y, r < p.rows ? d : 0, t, G, x);
@@ -297,7 +302,7 @@ __global__ void __launch_bounds__(kLoopThreads) norm_loop_kernel(
       const float v = to_f32(x[c]) - mean;
       q.add(v * v);
     }
-    const float rstd = __frcp_rn(__fsqrt_rn(fmaf(block_sum(q.s, red[1]), p.inv_d, p.eps)));
+    const float rstd = inverse_root(fmaf(block_sum(q.s, red[1]), p.inv_d, p.eps));
     for (int64_t c = threadIdx.x; c < p.d; c += kLoopThreads) {
       const float w = p.w != nullptr ? load_any(p.w, p.wt, c) : 1.0f;
       const float b = p.b != nullptr ? load_any(p.b, p.wt, c) : 0.0f;
