@@ -1342,7 +1342,15 @@ cudaError_t run_products(const Batch& b, const BatchLayout& l, const MuonScalars
       total += tiles[part];
     }
   }
-  if (total > INT32_MAX / (4 * kEpilogueWarps)) return cudaErrorInvalidConfiguration;
+  // the counters: tiles handed out (one past the last a pair), and a matrix's epilogue warps
+  bool counted = total <= INT32_MAX - most_clusters;
+  for (int k = 0; k < p.n; ++k) {
+    int64_t of_mat = 0;
+    for (int part = 0; part < kParts; ++part)
+      of_mat += static_cast<int64_t>(before[part]) * p.info[k].part[part].per_mat;
+    counted = counted && of_mat <= INT32_MAX / (2 * kEpilogueWarps);
+  }
+  if (!counted) return cudaErrorInvalidConfiguration;
   p.n_tiles = static_cast<int>(total);
   const int64_t widest = std::max(tiles[0], std::max(tiles[1], tiles[2]));
   const int64_t clusters = std::max<int64_t>(1, std::min<int64_t>(most_clusters, widest));

@@ -1,4 +1,4 @@
-"""Muon steps on updates of any size that fp32 holds.
+"""Muon steps on updates of any size that fp32 holds, and over more tiles than one count of all takes.
 
 Tolerances are test_gpu_muon's: an update's size drops out of X = u / |u|_F, so that they hold at
 every size.  u is read back from m (beta 0, or no new gradient), so that the roundings of small
@@ -72,6 +72,25 @@ def test_momentum_that_fades(o, i, rank, products, nesterov):
             continue
         check_x(np64(w), u, FIVE, products)
     assert 20 < turn < 59 and not bool(w.any())
+
+
+def test_many_thin_matrices():
+    """264 rows of 2^20, 64 iterations: 34 million tiles, counted matrix by matrix.
+
+    Rows are their own singular direction.  The iteration has its fixed point at 1, but for what A's sum
+    loses: 65,536 products are added one after the other and lose up to 2^-23 each, 0.8%, which raises the
+    fixed point by half of that; X's entries and B round to 11 bits."""
+    n, length = 264, 1 << 20
+    gen = torch.Generator(device=DEV).manual_seed(1)
+    g = torch.randn((n, length), generator=gen, device=DEV).bfloat16()
+    w, m = torch.zeros((n, length), device=DEV), torch.zeros((n, length), device=DEV)
+    step([bg.MuonTensor(w[k:k + 1], g[k:k + 1], m[k:k + 1]) for k in range(n)], -1.0, 0.0, False,
+         [(1.5, -0.5, 0.0)] * 64, 1)
+    for k in range(0, n, 8):
+        x = g[k:k + 8].double()
+        x = x / x.norm(dim=1, keepdim=True)
+        off = (w[k:k + 8].double() - x).abs() - (2.0 ** -8 + 3 * 2.0 ** -11) * x.abs()
+        assert float(off.max()) <= 2.0 ** -34
 
 
 def test_oracle_at_the_ends():
