@@ -46,7 +46,7 @@ namespace {
 constexpr float kPlaneScale = 1024.0f;         // of what the planes hold
 constexpr int kMaxGroups = 8;                  // shapes of a batch of matrices
 constexpr int kMaxMats = 300;                  // matrices of a batch
-constexpr int64_t kBatchElements = 1ll << 29;  // where a batch ends: bounds the workspace
+constexpr int64_t kBatchElements = 1ll << 29;  // of an X plane, where a batch ends: bounds the workspace
 
 int64_t round_to(int64_t n, int64_t to) { return (n + to - 1) / to * to; }
 
@@ -1015,8 +1015,11 @@ struct Shape {
 struct Batch {
   std::vector<Shape> shapes;
   int mats = 0;
-  int64_t elements = 0;
+  int64_t elements = 0, held = 0;                // of the matrices, and of an X plane of each
 };
+
+// Rows of a plane are whole chunks of 64 columns.
+int64_t leading(int64_t cols) { return round_to(cols, 64); }
 
 std::vector<Batch> batches_of(const bergson_muon_tensor* t, int n) {
   std::vector<Shape> shapes;
@@ -1031,11 +1034,12 @@ std::vector<Batch> batches_of(const bergson_muon_tensor* t, int n) {
   });
   std::vector<Batch> out;
   for (const Shape& s : shapes) {
-    const int64_t each = s.rows * s.cols;
+    // A' and B take no more than X: their short side squared, padded alike
+    const int64_t each = s.rows * s.cols, held = s.rows * leading(s.cols);
     bool open = false;                           // the shape is the last of the last batch
     for (int i : s.mats) {
       if (out.empty() || out.back().mats == kMaxMats ||
-          (out.back().mats > 0 && out.back().elements + each > kBatchElements) ||
+          (out.back().mats > 0 && out.back().held + held > kBatchElements) ||
           (!open && out.back().shapes.size() == kMaxGroups)) {
         out.emplace_back();
         open = false;
@@ -1046,13 +1050,11 @@ std::vector<Batch> batches_of(const bergson_muon_tensor* t, int n) {
       b.shapes.back().mats.push_back(i);
       ++b.mats;
       b.elements += each;
+      b.held += held;
     }
   }
   return out;
 }
-
-// Rows are whole chunks of 64 columns.
-int64_t leading(int64_t cols) { return round_to(cols, 64); }
 
 // Where a shape's planes stand in the workspace: X twice, A and B.
 struct Planes {

@@ -93,6 +93,16 @@ def test_many_thin_matrices():
         assert float(off.max()) <= 2.0 ** -34
 
 
+@pytest.mark.parametrize("products", [3, 1])
+def test_columns_in_several_batches(products):
+    """Rows of one element take 64 in the planes: eight such matrices are a batch."""
+    grads = [update(1 << 20, 1, 1e-3, seed=k) for k in range(10)] + [update(40, 50, 1e-3)]
+    w = [torch.zeros_like(g) for g in grads]
+    step([bg.MuonTensor(a, g, torch.zeros_like(g)) for a, g in zip(w, grads)], -1.0, 0.0, False, FIVE, products)
+    for k in (0, 7, 8, 9, 10):
+        check_x(np64(w[k]), np64(grads[k]), FIVE, products)
+
+
 def test_oracle_at_the_ends():
     """The oracle's own X does not depend on the update's size."""
     u = np64(update(30, 40, 1.0))
