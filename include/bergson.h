@@ -1078,7 +1078,8 @@ BERGSON_API int bergson_embedding_backward(const bergson_embedding_grad_args* ar
  *   m         fp32 [rows, cols], the momentum, updated in place; zeros before the first step.
  *   lr_scale  multiplies the call's lr;  ortho_scale  the orthogonalised update (e.g. 0.2
  *             sqrt(max(rows, cols)));  weight_decay  decoupled.
- * rows, cols in [1, 2^20], the smaller of them <= 2^16.  Matrices share no memory.
+ * rows, cols in [1, 2^20], the smaller of them <= 2^16, and an iteration's 256 x 256 tiles times the
+ * iterations within 2^26 (2^16 x 2^20 at 60).  Matrices share no memory.
  */
 typedef struct bergson_muon_tensor {
   void* param;

@@ -34,6 +34,8 @@
 
 #include <algorithm>
 #include <cmath>
+#include <functional>
+#include <memory>
 #include <vector>
 
 #include "internal.h"
@@ -1246,15 +1248,22 @@ bool encode_side(Side* s, int kind, const void* ptr, int64_t cols, int64_t rows,
           encode_tmap_across(&s->across, ptr, cols, rows, planes, ld, P, chunks) == CUDA_SUCCESS);
 }
 
+constexpr int64_t kMostOfMatrix = INT32_MAX / (2 * kEpilogueWarps);     // tiles, in its counter
+
+using Launch = std::function<cudaError_t(cudaStream_t)>;
+
+// All products of a batch, as `launch`: tensor maps, schedule and limits are done with before anything of
+// the step is enqueued, so that what fails here leaves m and the weights alone.
 template <int P, int G, int S>
-cudaError_t run_products(const Batch& b, const BatchLayout& l, const MuonScalars& a, uint8_t* ws,
-                         int* status, int sms, cudaStream_t s) {
+cudaError_t prepare_products(const Batch& b, const BatchLayout& l, const MuonScalars& a, uint8_t* ws,
+                             int* status, int sms, Launch* launch) {
   const int most_clusters = std::max(1, sms / 2);
   std::vector<int> columns[kParts];
   for (int part = 0; part < kParts; ++part)
     columns[part] = launch_columns(b, part, P, most_clusters);
   static_assert(sizeof(ProdParams<G, S>) <= 32'000, "a launch's parameters");
-  ProdParams<G, S> p = {};
+  const auto params = std::make_shared<ProdParams<G, S>>();
+  ProdParams<G, S>& p = *params;
   p.n = static_cast<int>(b.shapes.size());
   p.counters = reinterpret_cast<int*>(ws + l.counters);
   p.status = status;
@@ -1350,7 +1359,7 @@ cudaError_t run_products(const Batch& b, const BatchLayout& l, const MuonScalars
     int64_t of_mat = 0;
     for (int part = 0; part < kParts; ++part)
       of_mat += static_cast<int64_t>(before[part]) * p.info[k].part[part].per_mat;
-    counted = counted && of_mat <= INT32_MAX / (2 * kEpilogueWarps);
+    counted = counted && of_mat <= kMostOfMatrix;
   }
   if (!counted) return cudaErrorInvalidConfiguration;
   p.n_tiles = static_cast<int>(total);
@@ -1360,8 +1369,11 @@ cudaError_t run_products(const Batch& b, const BatchLayout& l, const MuonScalars
   static PerDeviceOnce attr;
   const cudaError_t e = smem_attr_once(attr, kernel, ProdCfg<P>::kSmemBytes);
   if (e != cudaSuccess) return e;
-  return launch_dependent(kernel, dim3(static_cast<unsigned>(2 * clusters)), dim3(kThreads),
-                          ProdCfg<P>::kSmemBytes, s, p);
+  *launch = [kernel, params, clusters](cudaStream_t s) {
+    return launch_dependent(kernel, dim3(static_cast<unsigned>(2 * clusters)), dim3(kThreads),
+                            ProdCfg<P>::kSmemBytes, s, *params);
+  };
+  return cudaSuccess;
 }
 
 // Sizes of the launches' parameters: few and most.
@@ -1376,22 +1388,42 @@ size_t muon_workspace(const bergson_muon_tensor* t, int n, int products) {
   return most;
 }
 
+bool muon_counts(int64_t rows, int64_t cols, int products, int iterations) {
+  const int64_t m = std::min(rows, cols), width = products == 3 ? kTileN : 2 * kTileN;
+  int64_t tiles = ceil_div(rows, kTileM) * ceil_div(cols, width);
+  for (int64_t r = kTileM; r < m + kTileM; r += kTileM) tiles += 2 * ceil_div(std::min(r, m), width);
+  return tiles * iterations <= kMostOfMatrix;
+}
+
 cudaError_t launch_muon(const bergson_muon_tensor* t, int n, const MuonScalars& a, void* ws,
                         int* status, int sms, cudaStream_t s) {
   uint8_t* w = static_cast<uint8_t*>(ws);
-  for (const Batch& b : batches_of(t, n)) {
-    const BatchLayout l = layout_of(b, a.products == 3 ? 2 : 1);
+  const std::vector<Batch> batches = batches_of(t, n);
+  std::vector<BatchLayout> layouts;
+  std::vector<Launch> products(batches.size());
+  for (size_t i = 0; i < batches.size(); ++i) {
+    const Batch& b = batches[i];
+    layouts.push_back(layout_of(b, a.products == 3 ? 2 : 1));
+    const BatchLayout& l = layouts.back();
+    const bool short_run = b.shapes.size() <= kFewGroups && 3 * a.iterations <= kFewSteps;
+    Launch* to = &products[i];
+    cudaError_t e;
+    if (a.products == 3)
+      e = short_run ? prepare_products<2, kFewGroups, kFewSteps>(b, l, a, w, status, sms, to)
+                    : prepare_products<2, kMaxGroups, kMaxSteps>(b, l, a, w, status, sms, to);
+    else
+      e = short_run ? prepare_products<1, kFewGroups, kFewSteps>(b, l, a, w, status, sms, to)
+                    : prepare_products<1, kMaxGroups, kMaxSteps>(b, l, a, w, status, sms, to);
+    if (e != cudaSuccess) return e;
+  }
+  for (size_t i = 0; i < batches.size(); ++i) {
+    const Batch& b = batches[i];
+    const BatchLayout& l = layouts[i];
     const bool few = b.mats <= kFewMats;
     cudaError_t e = few ? run_moments<kFewMats>(t, b, l, a, w, s)
                         : run_moments<kMaxMats>(t, b, l, a, w, s);
     if (e != cudaSuccess) return e;
-    const bool short_run = b.shapes.size() <= kFewGroups && 3 * a.iterations <= kFewSteps;
-    if (a.products == 3)
-      e = short_run ? run_products<2, kFewGroups, kFewSteps>(b, l, a, w, status, sms, s)
-                    : run_products<2, kMaxGroups, kMaxSteps>(b, l, a, w, status, sms, s);
-    else
-      e = short_run ? run_products<1, kFewGroups, kFewSteps>(b, l, a, w, status, sms, s)
-                    : run_products<1, kMaxGroups, kMaxSteps>(b, l, a, w, status, sms, s);
+    e = products[i](s);
     if (e != cudaSuccess) return e;
     e = few ? run_weights<kFewMats>(t, b, l, a, w, s) : run_weights<kMaxMats>(t, b, l, a, w, s);
     if (e != cudaSuccess) return e;

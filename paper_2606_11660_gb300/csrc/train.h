@@ -77,6 +77,8 @@ struct MuonScalars {
   int products;                // 1 or 3
   const float* grad_scale;     // device, or nullptr
 };
+// Whether a matrix's counter holds its products' tiles, at their widest.
+bool muon_counts(int64_t rows, int64_t cols, int products, int iterations);
 size_t muon_workspace(const bergson_muon_tensor* t, int n, int products);
 cudaError_t launch_muon(const bergson_muon_tensor* t, int n, const MuonScalars& a, void* ws,
                         int* status, int sms, cudaStream_t s);

@@ -592,6 +592,9 @@ int bergson_muon_step(const bergson_muon_tensor* tensors, int n_tensors, double 
   if (!std::isfinite(lr)) return fail(BERGSON_EINVAL, "lr must be finite");
   if (!(beta >= 0.0 && beta < 1.0)) return fail(BERGSON_EINVAL, "beta must be in [0, 1)");
   BERGSON_TRY(check_coefficients(coefficients, n_iterations));
+  for (int i = 0; i < n_tensors; ++i)
+    if (!muon_counts(tensors[i].rows, tensors[i].cols, products, n_iterations))
+      return fail(BERGSON_EUNSUPPORTED, "tensor %d: too large for so many iterations", i);
   if (grad_scale != nullptr) BERGSON_TRY(check_tensor(grad_scale, 4, "grad_scale"));
   try {
     BERGSON_TRY(check_workspace(workspace, ws_bytes, muon_workspace(tensors, n_tensors, products)));

@@ -1,7 +1,7 @@
 """Calls of the operators around a model's linear layers that need no GPU: what the documentation allows
 passes, what it does not is refused by name."""
 import paper_2606_11660_gb300 as bg
-from tests.test_model_ops_abi import built_library  # noqa: F401
+from tests.test_model_ops_abi import QUINTIC, accepted, built_library, muon, no_launch  # noqa: F401
 
 
 def test_workspace_of_thin_matrices():
@@ -14,3 +14,13 @@ def test_workspace_of_thin_matrices():
             assert need([shape] * 300, products) <= each * 2 ** 29 + 65_536
     # one alone may take more
     assert need([(1 << 20, 600)], 1) >= 2 * 2 * 640 * 2 ** 20
+
+
+def test_products_that_pass_a_count():
+    """Refused before anything is enqueued: m keeps its value."""
+    big = dict(rows=1 << 16, cols=1 << 20, ws_bytes=1 << 62)
+    assert muon(k=(QUINTIC,) * 64, **big) == bg.BERGSON_EUNSUPPORTED and "iterations" in bg.bergson_last_error()
+    for st in (muon(k=(QUINTIC,) * 60, **big), muon(k=(QUINTIC,) * 64, products=1, **big),
+               muon(k=(QUINTIC,) * 64, rows=1 << 16, cols=1 << 16, ws_bytes=1 << 62),
+               muon(k=(QUINTIC,) * 64, n=300, rows=1, cols=1 << 20)):
+        assert accepted(st), bg.bergson_last_error()
