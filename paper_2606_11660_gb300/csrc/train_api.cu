@@ -188,9 +188,10 @@ int check_coefficients(const double* k, int n) {
     if (!std::isfinite(a) || !std::isfinite(b) || !std::isfinite(c))
       return fail(BERGSON_EINVAL, "coefficients must be finite");
     const double next = 1.01 * largest(a, b, c, true, top * top);
-    if (!(std::max(std::fabs(h), std::fabs(top * top + h)) <= kMost) ||
-        !(std::fabs(c * h * h) <= kMost) || !(largest(a, b, c, false, top * top) <= kMost) ||
-        !(next <= kMost))
+    // without a square A stands in no plane
+    const bool square = c == 0.0 || (std::max(std::fabs(h), std::fabs(top * top + h)) <= kMost &&
+                                     std::fabs(c * h * h) <= kMost);
+    if (!square || !(largest(a, b, c, false, top * top) <= kMost) || !(next <= kMost))
       return fail(BERGSON_EUNSUPPORTED,
                   "iteration %d: the coefficients let X or a polynomial of A pass 48", i);
     top = next;

@@ -103,6 +103,16 @@ def test_columns_in_several_batches(products):
         check_x(np64(w[k]), np64(grads[k]), FIVE, products)
 
 
+def test_coefficients_without_a_square():
+    """c = 0: A itself is held nowhere, so that |X| may be 10 on the way."""
+    for k in ([(10.0, 0.0, 0.0), (0.1, 0.0, 0.0)], [(9.0, -2.0, 0.0), (0.25, 0.0, 0.0)]):
+        for products in (3, 1):
+            g = update(130, 200, 1e-3)
+            w, m = torch.zeros_like(g), torch.zeros_like(g)
+            step([bg.MuonTensor(w, g, m)], -1.0, 0.0, False, k, products)
+            check_x(np64(w), np64(g), k, products)
+
+
 def test_oracle_at_the_ends():
     """The oracle's own X does not depend on the update's size."""
     u = np64(update(30, 40, 1.0))

@@ -1,7 +1,24 @@
 """Calls of the operators around a model's linear layers that need no GPU: what the documentation allows
 passes, what it does not is refused by name."""
+import pytest
+
 import paper_2606_11660_gb300 as bg
 from tests.test_model_ops_abi import QUINTIC, accepted, built_library, muon, no_launch  # noqa: F401
+
+
+@pytest.mark.parametrize("k", [
+    ((10.0, 0.0, 0.0), (0.1, 0.0, 0.0)), ((9.0, -2.0, 0.0), (0.25, 0.0, 0.0)), ((40.0, 0.0, 0.0), (1.0, 0.0, 0.0))])
+def test_coefficients_without_a_square(k):
+    """c = 0: |X| up to 48 as the header has it, whatever A = X X^T is."""
+    assert accepted(muon(k=k)), bg.bergson_last_error()
+
+
+@pytest.mark.parametrize("k", [
+    ((10.0, 0.0, 0.0), (10.0, 0.0, 0.0)), ((10.0, 0.0, 0.0), (0.1, 0.5, 0.0)),
+    ((10.0, 0.0, 0.0), (0.0, 0.0, 0.001)), ((0.0, -60.0, 0.0),)])
+def test_coefficients_that_pass_the_limits(k):
+    """|X| = 100; b A = 50; A = 100 beside a square; b = 60."""
+    assert muon(k=k) == bg.BERGSON_EUNSUPPORTED and bg.bergson_last_error() != ""
 
 
 def test_workspace_of_thin_matrices():
