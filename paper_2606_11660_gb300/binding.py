@@ -930,9 +930,15 @@ def bergson_factor_moments(mats, correction: float, floor: float, workspace, str
                                         _stream(stream)))
 
 
+def _no_matrix(shape, what: str):
+    raise ValueError(f"{what} must be a matrix [rows, columns], got a tensor of shape {tuple(shape)}")
+
+
 def _matrix(t, what: str) -> tuple:
     """(device pointer, shape, leading dimension, torch's and the library's dtype) of a matrix."""
     shape, dtype = t.shape, t.dtype
+    if len(shape) != 2:
+        _no_matrix(shape, what)
     code = _DTYPES.get(dtype)
     if code is None:
         code = _dtype(t)
@@ -1039,7 +1045,10 @@ class MuonTensor:
     def to_c(self) -> bergson_muon_tensor:
         if not _DTYPES:
             _load_dtypes()
-        rows, cols = shape = self.param.shape
+        shape = self.param.shape
+        if len(shape) != 2:
+            _no_matrix(shape, "param")
+        rows, cols = shape
         for what in ("grad", "m", "master"):
             t = getattr(self, what)
             if t is not None and t.shape != shape:

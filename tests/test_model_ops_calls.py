@@ -1,6 +1,7 @@
 """Calls of the operators around a model's linear layers that need no GPU: what the documentation allows
 passes, what it does not is refused by name."""
 import pytest
+import torch
 
 import paper_2606_11660_gb300 as bg
 from tests.test_model_ops_abi import QUINTIC, accepted, built_library, muon, no_launch  # noqa: F401
@@ -41,3 +42,16 @@ def test_products_that_pass_a_count():
                muon(k=(QUINTIC,) * 64, rows=1 << 16, cols=1 << 16, ws_bytes=1 << 62),
                muon(k=(QUINTIC,) * 64, n=300, rows=1, cols=1 << 20)):
         assert accepted(st), bg.bergson_last_error()
+
+
+@pytest.mark.parametrize("what,call", [
+    ("x", lambda t: bg.bergson_norm(t, None, None, bg.BERGSON_NORM_LAYER, 1e-5, t)),
+    ("x", lambda t: bg.bergson_norm_backward(t, None, bg.BERGSON_NORM_RMS, None, None, t, t, None, None, t)),
+    ("table", lambda t: bg.bergson_embedding(t, torch.zeros(2, dtype=torch.int64), 1.0, t)),
+    ("dy", lambda t: bg.bergson_embedding_backward(t, torch.zeros(6, dtype=torch.int64), 1.0, t[0], False, t)),
+    ("param", lambda t: bg.bergson_muon_tensors([bg.MuonTensor(t, t, t)])),
+])
+@pytest.mark.parametrize("shape", [(2, 3, 8), (8,)])
+def test_tensors_that_are_no_matrices(what, call, shape):
+    with pytest.raises(ValueError, match=rf"^{what} must be a matrix .*{shape[0]}"):
+        call(torch.zeros(shape))
