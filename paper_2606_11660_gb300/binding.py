@@ -1083,9 +1083,9 @@ def bergson_muon_step(tensors, lr: float, beta: float, nesterov: bool, coefficie
     if not _DTYPES:
         _load_dtypes()
     arr = _records(bergson_muon_tensor, tensors)
-    flat = [float(x) for abc in coefficients for x in abc]
-    if len(flat) != 3 * len(coefficients):
+    if any(len(abc) != 3 for abc in coefficients):
         raise ValueError("coefficients must be triples (a, b, c)")
+    flat = [float(x) for abc in coefficients for x in abc]
     scale = (_vector(grad_scale, "grad_scale", _F32, 1) if hasattr(grad_scale, "data_ptr")
              else _ptr(grad_scale))
     _check(lib().bergson_muon_step(arr, len(arr), lr, beta, 1 if nesterov else 0,

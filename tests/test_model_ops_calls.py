@@ -55,3 +55,9 @@ def test_products_that_pass_a_count():
 def test_tensors_that_are_no_matrices(what, call, shape):
     with pytest.raises(ValueError, match=rf"^{what} must be a matrix .*{shape[0]}"):
         call(torch.zeros(shape))
+
+
+@pytest.mark.parametrize("k", [[(1.0, 2.0)], [(1.0, 2.0), (3.0, 4.0, 5.0, 6.0)], [(1.0, 2.0, 3.0, 4.0)]])
+def test_coefficients_that_are_no_triples(k):
+    with pytest.raises(ValueError, match="triples"):
+        bg.bergson_muon_step([], 1.0, 0.9, True, k, 3, torch.zeros(256))
