@@ -1114,8 +1114,10 @@ typedef struct bergson_muon_tensor {
  *   coefficients  HOST array [n_iterations, 3], n_iterations in [1, 64].  From |X|_F = 1 on,
  *             |X|, |a I + b A + c A^2| and, where c is not 0, |A + b / 2c| and b^2 / 4c have to stay
  *             within 48 (else EUNSUPPORTED; by the polynomials alone).
- *   products  3: the products' operands hold 22 bits (X is off by some 1e-6 |X| an iteration).
- *             1: they hold fp16's 11 (some 1e-3), at a third of the work: for weights without a
+ *   products  3: the products' operands hold 22 bits, entries below some 2^-12 to 2^-35 (X is off
+ *             by some 1e-6 |X| an iteration).
+ *             1: they hold fp16's 11 (some 1e-3), at a third of the work, and A loses up to
+ *             max(rows, cols) 2^-27 of itself, for its sums round toward zero: for weights without a
  *             master copy, whose own rounding is larger.
  *   grad_scale  device fp32 [1] or NULL (1).
  *   workspace 256-byte aligned, contents on entry ignored; its size follows from the shapes and

@@ -12,25 +12,27 @@
 //
 // (c = 0: B = b A + a I at once), so that no product reads anything but its two operands.
 //
-// The products run on the tensor cores with fp16 operands and fp32 sums.  An
-// operand is held as one fp16 plane (products = 1) or as the sum of two, hi = fp16(v), lo = fp16(v - hi)
-// (products = 3: hi hi + hi lo + lo hi; what is left out is below 2^-22), in 1024
-// times its value: entries are 1 / 32768 and smaller at first, of the size of
-// 1 / sqrt(columns) later, and stay clear of fp16's subnormals by that.
+// The products run on the tensor cores with fp16 operands and fp32 sums.  An operand is held as
+// one fp16 plane (products = 1) or as the sum of two, hi = fp16(v), lo = fp16(v - hi) (products =
+// 3: hi hi + hi lo + lo hi; what is left out is below 2^-22), in 1024 times its value: entries are
+// 1 / 32768 and smaller at first, of the size of 1 / sqrt(columns) later.  By that hi has its 11
+// bits down to entries of 2^-24, and both have 22 down to some 2^-12; below, lo is subnormal and an
+// entry is off by up to 2^-35, beside |X|_F = 1.
 //
 // Matrices of one shape form a group, their planes stacked in the workspace under one
 // tensor map.  All products of all iterations are one launch of persistent CTA pairs over 256-row
 // tiles, handed out step by step, longest products first; a matrix's tiles wait for its own earlier
 // ones alone.  An operand is read with its rows as they lie (K-major) or across (MN-major)
-// by the tensor cores' own descriptors.  A' and B are symmetric: only tiles on and below the diagonal
-// are computed and stored, and a read above it takes the mirror image across.
+// by the tensor cores' own descriptors.  A' and B are symmetric: only tiles on and below the
+// diagonal are computed and stored, and a read above it takes the mirror image across.
 //
-// Bound: with two planes an accumulator of 256 columns is 12 MMAs of 128 cycles a stage for 64 KB of loads,
-// with one plane two of them are 8 for 48 KB; a CTA's loads come at 39 to 47 bytes a cycle when all SMs load,
-// so that both forms wait for them a little (1.0 to 1.3 of the MMAs' time), and the smallest steps are
-// latency, 5 to 7 us a product.  Four blocks of d 2048 at one plane: 5.5 ms, 1.25 PFLOP/s under the
-// power cap; ten of d 640 at two: 1.8 ms, 0.87 PFLOP/s of MMAs (six of 2048 rows: 84% of the tensor
-// pipe's cycles, 69% at one plane).
+// Bound: with two planes an accumulator of 256 columns is 12 MMAs of 128 cycles a stage for 64 KB
+// of loads, with one plane two of them are 8 for 48 KB; a CTA's loads come at 39 to 47 bytes a
+// cycle when all SMs load, so that both forms wait for them a little (1.0 to 1.3 of the MMAs'
+// time).  The smallest steps wait for one another: 15 products at 5 to 11 us, a chain of planes
+// written, counted, seen and loaded.  Four blocks of d 2048 at one plane: 5.5 ms, 1.25 PFLOP/s
+// under the power cap; ten of d 640 at two: 1.8 ms, 0.87 PFLOP/s of MMAs (six of 2048 rows: 84% of
+// the tensor pipe's cycles, 69% at one plane).
 
 #include <algorithm>
 #include <cmath>
@@ -48,7 +50,7 @@ namespace {
 constexpr float kPlaneScale = 1024.0f;         // of what the planes hold
 constexpr int kMaxGroups = 8;                  // shapes of a batch of matrices
 constexpr int kMaxMats = 300;                  // matrices of a batch
-constexpr int64_t kBatchElements = 1ll << 29;  // of an X plane, where a batch ends: bounds the workspace
+constexpr int64_t kBatchElements = 1ll << 29;  // of X planes where a batch ends: bounds the workspace
 
 int64_t round_to(int64_t n, int64_t to) { return (n + to - 1) / to * to; }
 
@@ -133,8 +135,8 @@ __device__ __forceinline__ void load_eight(const void* p, int type, bool vec, in
   for (int k = 0; k < 8; ++k) x[k] = i + k < n ? load_any(p, type, i + k) : 0.0f;
 }
 
-// Where a thread's 8 elements of a CTA's 2048 stand: side by side in vectors, else 256 apart, so that
-// neighbouring threads take neighbouring elements.
+// Where a thread's 8 elements of a CTA's 2048 stand: side by side in vectors, else 256 apart, so
+// that neighbouring threads take neighbouring elements.
 __device__ __forceinline__ int64_t place(bool vec, int64_t at, int k) {
   return vec ? at + 8 * threadIdx.x + k : at + threadIdx.x + static_cast<int64_t>(kMomentThreads) * k;
 }
@@ -156,9 +158,10 @@ __device__ __forceinline__ int64_t in_plane(int64_t i, int cols, int ld) {
   return row * ld + (i - row * cols);
 }
 
-// m's update and the sums of the squares of 2^100 u, u and 2^-100 u.  The first that is finite holds the
-// norm of any u that fp32 does, with all its digits: the smallest u, 2^-149, has a square of 2^-98 in the first
-// sum, and where a sum of up to 2^36 squares passed 2^128, the largest is 2^-108 or more in the next one.
+// m's update and the sums of the squares of 2^100 u, u and 2^-100 u.  The first that is finite
+// holds the norm of any u that fp32 does, with all its digits: the smallest u, 2^-149, has a square
+// of 2^-98 in the first sum, and where a sum of up to 2^36 squares passed 2^128, the largest is
+// 2^-108 or more in the next one.  Bound by its bytes all the same: 201M elements 305 us, 6.6 TB/s.
 template <int N>
 __global__ void __launch_bounds__(kMomentThreads) moment_kernel(
     const __grid_constant__ MomentParams<N> p) {
@@ -202,13 +205,14 @@ __global__ void __launch_bounds__(kMomentThreads) moment_kernel(
         if (place(false, at, j) < end) e.m[place(false, at, j)] = m[j];
     }
   }
-  const float a = block_sum(up.s, red[0]), b = block_sum(mid.s, red[1]), c = block_sum(down.s, red[0]);
+  const float a = block_sum(up.s, red[0]), b = block_sum(mid.s, red[1]);
+  const float c = block_sum(down.s, red[0]);
   if (threadIdx.x == 0) p.part[blockIdx.x] = make_float3(a, b, c);
 }
 
-// The planes of 1024 u / |u|_F, as (2^k u) (1024 / |2^k u|_F) with the k of the sum that holds the norm:
-// 1024 / |u|_F alone would pass fp32 below 3e-36, and the norm itself above 3.4e38.  A matrix of
-// zeros stays one; one that holds NaN or an infinity is NaN.
+// The planes of 1024 u / |u|_F, as (2^k u) (1024 / |2^k u|_F) with the k of the sum that holds the
+// norm: 1024 / |u|_F alone would pass fp32 below 3e-36, and the norm itself above 3.4e38.  A matrix
+// of zeros stays one; one that holds NaN or an infinity is NaN.
 template <int N, int P>
 __global__ void __launch_bounds__(kMomentThreads) planes_kernel(
     const __grid_constant__ MomentParams<N> p) {
@@ -272,8 +276,9 @@ __global__ void __launch_bounds__(kMomentThreads) planes_kernel(
   }
 }
 
-// w <- w - lr (ortho_scale X + weight_decay w).  In a pass of its own: in the last product's epilogue
-// the scattered rows of a tile cost as much (49M elements with masters: 100 us either way).
+// w <- w - lr (ortho_scale X + weight_decay w).  In a pass of its own: in the last product's
+// epilogue the scattered rows of a tile cost as much (49M elements with masters: 100 us either
+// way).
 template <int N, int P>
 __global__ void __launch_bounds__(kMomentThreads) weights_kernel(
     const __grid_constant__ WeightParams<N> p) {
@@ -500,7 +505,8 @@ __device__ __forceinline__ bool hand_out(Ring* ring, int* counter, int n_tiles, 
   }
 }
 
-// A taker's place in the ring; next() is called by one lane: the tile, -1 at the end, -2 when it gave up.
+// A taker's place in the ring; next() is called by one lane: the tile, -1 at the end, -2 when it
+// gave up.
 struct Taker {
   int slot = 0;
   uint32_t ph = 0;
@@ -702,9 +708,10 @@ __device__ __forceinline__ void put_planes(__half* d, int64_t plane, const float
 // epilogues by multicast commits, and every epilogue warp of both CTAs releases an
 // accumulator on the even CTA's `tempty`.  Every wait is bounded.
 //
-// The tensor cores' fp32 sums round toward zero.  With two planes, an accumulation chain is
-// one stage (12 MMAs, its smallest terms first) and the epilogue adds the chains in registers while the
-// next one runs; with one plane the operands' own rounding is 2^-12 and a tile is one chain.
+// The tensor cores' fp32 sums round toward zero.  With two planes, an accumulation chain is kChain
+// stages (48 MMAs, a stage's smallest terms first) and the epilogue adds the chains in registers
+// while the next one runs; with one plane the operands' own rounding is 2^-12 and a tile is one
+// chain, which loses up to 2^-23 an MMA: 2^-27 a column of K.
 template <int P, int G, int S>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
     products_kernel(const __grid_constant__ ProdParams<G, S> p) {
@@ -838,8 +845,9 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
                     umma_pair_low(d, at + kk * step_a, bt + kk * step_b, idesc,
                                   !first || q != 0 || kk != 0);
                 }
-                // a commit stands with its MMAs, in the branch of the lane that issued them: in a branch of
-                // its own behind the warp's barrier it did not arrive
+                // A commit stands in the branch of the MMAs that it follows.  In a branch of its
+                // own behind the warp's barrier, by the same lane, it did not arrive; why is not
+                // known.
                 if (ends && kc == kb + len - 1) umma_commit_pair(smem_u32(&tfull[cab]), 0x3);
                 if (h == subs - 1) umma_commit_pair(smem_u32(&empty[st]), 0x3);
               }
@@ -865,9 +873,9 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
     __syncwarp();
   } else {
     // ------------------------------------------------------------ epilogue
-    // Thread = a row of this CTA's half (TMEM lane) and up to 64 of an accumulator's columns: summed up
-    // in registers, so that the accumulator is free again before anything is written.  A thread
-    // writes whole 32-byte sectors of its row.
+    // Thread = a row of this CTA's half (TMEM lane) and up to 64 of an accumulator's columns:
+    // summed up in registers, so that the accumulator is free again before anything is written.  A
+    // thread writes whole 32-byte sectors of its row.
     const int ew = warp - kFirstEpilogue;
     const int quarter = warp & 3;
     uint8_t* out = smem + C::kStages * C::kStageBytes + ew * kOutTile;
@@ -985,7 +993,10 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
         __syncwarp();
       }
       if (aborted) break;
-      // through with the tile: its planes may be loaded, by whoever sees the count
+      // Through with the tile: its planes may be loaded, by whoever sees the count.  Two planes:
+      // the warp's barrier puts all lanes' stores before lane 0's release, and the thread that
+      // loads has its proxy fence behind its acquire (wait_matrix): one on the way from the stores
+      // to the copies is enough.  One plane: the copies out have ended before the release.
       if (P == 1 && lane == 0) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
       __syncwarp();
       if (lane == 0)
@@ -1252,11 +1263,11 @@ constexpr int64_t kMostOfMatrix = INT32_MAX / (2 * kEpilogueWarps);     // tiles
 
 using Launch = std::function<cudaError_t(cudaStream_t)>;
 
-// All products of a batch, as `launch`: tensor maps, schedule and limits are done with before anything of
-// the step is enqueued, so that what fails here leaves m and the weights alone.
+// All products of a batch, as `launch`: tensor maps, schedule and limits are done with before
+// anything of the step is enqueued, so that what fails here leaves m and the weights alone.
 template <int P, int G, int S>
-cudaError_t prepare_products(const Batch& b, const BatchLayout& l, const MuonScalars& a, uint8_t* ws,
-                             int* status, int sms, Launch* launch) {
+cudaError_t prepare_products(const Batch& b, const BatchLayout& l, const MuonScalars& a,
+                             uint8_t* ws, int* status, int sms, Launch* launch) {
   const int most_clusters = std::max(1, sms / 2);
   std::vector<int> columns[kParts];
   for (int part = 0; part < kParts; ++part)
@@ -1391,7 +1402,8 @@ size_t muon_workspace(const bergson_muon_tensor* t, int n, int products) {
 bool muon_counts(int64_t rows, int64_t cols, int products, int iterations) {
   const int64_t m = std::min(rows, cols), width = products == 3 ? kTileN : 2 * kTileN;
   int64_t tiles = ceil_div(rows, kTileM) * ceil_div(cols, width);
-  for (int64_t r = kTileM; r < m + kTileM; r += kTileM) tiles += 2 * ceil_div(std::min(r, m), width);
+  for (int64_t r = kTileM; r < m + kTileM; r += kTileM)
+    tiles += 2 * ceil_div(std::min(r, m), width);
   return tiles * iterations <= kMostOfMatrix;
 }
 

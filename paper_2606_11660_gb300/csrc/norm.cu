@@ -5,13 +5,13 @@
 //             dx = rstd (h - mean h - n mean (h n)),  dw = sum_r dy n,  db = sum_r dy
 //
 // (mu = 0 and no mean of h without a mean).  Both are bound by their bytes: a
-// row is read once, stays in the registers of the 4 .. 32 lanes (up to 512 columns;
-// forward up to 1024) or the CTA that have it, 8 to 32 columns a thread, and the next rows are on their way while this
-// one is reduced.  A thread keeps its columns from row to row, so that weights are
-// loaded once a CTA and the backward pass sums dw and db in registers; one row
-// of both a CTA goes to the workspace, and a second kernel adds these up in order.
-// 65,536 x 2048 bf16: 91 us forward (5.9 TB/s) and 139 backward (135 and 4; 6.0 TB/s); the forward pass
-// fills 68% of the issue slots, and did so at 77% in 127 us before its arithmetic went in pairs.
+// row is read once, stays in the registers of the 4 .. 32 lanes (up to 512 columns; forward
+// up to 1024) or the CTA that have it, 8 to 32 columns a thread, and the next rows are on
+// their way while this one is reduced.  A thread keeps its columns from row to row, so that weights
+// are loaded once a CTA and the backward pass sums dw and db in registers; one row of both a CTA
+// goes to the workspace, and a second kernel adds these up in order.
+// 65,536 x 2048 bf16: 91 us forward (5.9 TB/s) and 139 backward (135 and 4; 6.0 TB/s); the forward
+// pass fills 68% of the issue slots, and did so at 77% in 127 us before its arithmetic went in pairs.
 
 #include <algorithm>
 #include <atomic>
@@ -36,7 +36,8 @@ constexpr int kSlabRows = 512;                 // rows of a CTA that sums column
 
 // Sums of one value or two over the threads that share a row, in each of them: G lanes side by
 // side, or the CTA by way of `red` (N values for each of 32 warps, not in use by the row before or
-// after, zeros at first).  Two go through the warp as one: its halves take one each after the first step.
+// after, zeros at first).  Two go through the warp as one: its halves take one each after the first
+// step.
 template <bool kCta, int N>
 __device__ __forceinline__ void row_sums(float (&v)[N], int G, float* red) {
   static_assert(N == 1 || N == 2, "one value or two");
@@ -73,8 +74,8 @@ __device__ __forceinline__ void row_sums(float (&v)[N], int G, float* red) {
     }
   }
 }
-// rstd of a mean square with eps added: NaN where that is infinite, so that a row which holds an infinity
-// is NaN without a mean too (1 / sqrt(inf) = 0 would make its other entries zeros).
+// rstd of a mean square with eps added: NaN where that is infinite, so that a row which holds an
+// infinity is NaN without a mean too (1 / sqrt(inf) = 0 would make its other entries zeros).
 __device__ __forceinline__ float inverse_root(float square) {
   return __frcp_rn(__fsqrt_rn(square)) + (square - square);
 }
@@ -86,8 +87,9 @@ __device__ __forceinline__ void clear_sums(float* red, int n) {
 
 // Rows on their way to a thread.  In vectors: by asynchronous copies to places of its own in
 // shared memory, kSlots rows ahead, so that no thread waits for another and no register is
-// held (a row at a time in registers: too few bytes in flight, 65,536 x 2048 at 4.1 TB/s with 6 CTAs an SM).  A
-// vector past the end copies what there is and zeros.  By elements: one row ahead, in registers.
+// held (a row at a time in registers: too few bytes in flight, 65,536 x 2048 at 4.1 TB/s with 6
+// CTAs an SM).  A vector past the end copies what there is and zeros.  By elements: one row ahead,
+// in registers.
 template <typename T, int kB, int C, int kSlots>
 struct Feed {
   using R = RowPart<T, kB, C>;
@@ -344,7 +346,8 @@ __global__ void __launch_bounds__(kWide ? 1024 : kCta ? 512 : 32 * kWarps)
   constexpr int kSlots = kFed ? kBackwardSlots : 1;
   constexpr int H = C / 2;
   __shared__ __align__(16) float red[2][64];
-  // kWide: weights, dw, db; else the rows on their way, and at the end [2, d] of a CTA's warps to add up
+  // kWide: weights, dw, db; else the rows on their way, and at the end [2, d] of a CTA's warps to
+  // add up
   extern __shared__ __align__(16) float wide[];
   const Turns u = turns<kCta>(p.lanes);
   const int G = u.G, t = u.t, d = static_cast<int>(p.d);
